@@ -302,6 +302,128 @@ int favorsharp_attention_flushed_rows(const void* workspace, int* host_count, vo
 int favorsharp_orthogonal_omega(const float* host_gauss_dir, const float* host_gauss_len, int groups, int M, int d,
                                 float* host_omega);
 
+/*
+ * Rotary positions.  The first rot_dim numbers of a row are rot_dim / 2 pairs; pair i of a row at position p is turned by
+ * the angle p freqs[i] and multiplied by `amplitude`:
+ *   (u, v) -> amplitude (u cos - v sin, v cos + u sin);
+ * the numbers behind rot_dim stay.  Pair i is numbers 2 i and 2 i + 1 (interleaved = 1) or i and i + rot_dim / 2
+ * (interleaved = 0).  Angles are taken in 64 bits, so that far positions keep theirs.
+ */
+typedef struct {
+  const double* freqs;        /* device, rot_dim / 2 values: radians per position */
+  const int32_t* positions;   /* device: row l of sequence b is at positions[b stride_b + l stride_l]; NULL: at l */
+  int64_t stride_b, stride_l; /* >= 0 (stride_b = 0: all sequences share their positions) */
+  int32_t rot_dim;            /* even, 2 .. d */
+  int32_t interleaved;
+  float amplitude;            /* 1 unless the context is scaled */
+} fs_rotary;
+
+typedef enum {
+  FS_ROTARY_PLAIN = 0,   /* freqs[i] = base^(-2 i / rot_dim) */
+  FS_ROTARY_LINEAR = 1,  /* divided by `factor` (positions of a longer context pressed into the one trained on) */
+  FS_ROTARY_BASE = 2,    /* base times factor^(rot_dim / (rot_dim - 2)): the slowest pair as with LINEAR, the fastest as it was */
+  FS_ROTARY_BLEND = 3    /* by the turns a pair makes in original_length positions: as LINEAR up to low_turns, as PLAIN from
+                            high_turns on, in proportion between them */
+} fs_rotary_scaling;
+/* HOST function: host_freqs receives rot_dim / 2 values.  factor > 0 is read unless PLAIN; original_length, low_turns <
+ * high_turns with BLEND.  FS_ERR_INVALID_ARG for what is none of these. */
+int favorsharp_rotary_frequencies(int rot_dim, double base, int scaling, double factor, int original_length,
+                                  double low_turns, double high_turns, double* host_freqs);
+
+/*
+ * Rows turned by their positions: Y = R X for X [B, H, L, d] and, in the same launch, Y2 = R X2 for X2 [B, H2, L, d]
+ * (queries and keys; H2 = 0: X alone, X2 and Y2 are not read).  transposed = 1 applies the transpose of R (turned back,
+ * amplitude kept), which is the backward pass.  Y may be X itself (same pointer, dtype and strides), likewise Y2 and X2;
+ * otherwise they must not overlap.  d <= 1024; each tensor f32 or bf16.  Asynchronous; no workspace.
+ */
+int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d,
+                      int transposed, const fs_tensor* Y, const fs_tensor* Y2, void* stream);
+
+/*
+ * Attention through kept states: key sides that outlive a call.  With K_hat = P S^T (Section 2.1) the keys and values of a
+ * sequence enter attention (Section 2.2) only through S^T [V 1], which grows by appending.  A pool holds `slots` such
+ * states for `heads` key heads each, contiguous, owned by the caller:
+ *   T [slots][heads][M][dv], z [slots][heads][M], shift [slots][heads], all float32 (T 16-byte aligned):
+ *   shift = max_jm e_jm,  T_m = sum_j 2^(e_jm - shift) V_j,  z_m = sum_j 2^(e_jm - shift),  2^e_jm = S_jm,
+ * over the keys appended so far; an empty state is T = z = 0, shift = -infinity.  Keys more than about 2^126 below the
+ * largest of their state are lost to it.
+ *   slots (device, B int32, or NULL: sequence b has slot b): the slot of each sequence.  Where a call writes states
+ *   (append, step, and the gradient of append) a sequence whose slot is not in the pool, or is also that of an earlier
+ *   sequence of the call, is left out: its state stays, its output rows are zeros.  Reading, sequences may share a slot;
+ *   those without one are as if it were empty.
+ *   H query heads share `heads` key heads in order: query head i reads key head i / (H / heads).  H % heads = 0.
+ *   lengths (device, B int32, or NULL: all L): rows l >= lengths[b] are padding: never read, and written as zeros where
+ *   the call has outputs for them.  Lengths below 0 count as 0, above L as L; a sequence of length 0 appends nothing.
+ *   rot (or NULL): queries and keys are turned on the way and not rounded in between; gradients are turned back.
+ *   All products have the accuracy of fp32 for f32 and for bf16 tensors; results are rounded once, to their dtype.
+ *   d, dv <= 128, M <= 2048, B H and slots * heads <= 65535, L H / heads <= 2^29.
+ * Calls on one stream see each other's states; calls that write a state must be ordered with all others on it by the caller.
+ */
+typedef struct {
+  float* T;      /* device */
+  float* z;
+  float* shift;  /* NULL in a pool of gradients */
+  int32_t slots;
+} fs_state;
+
+/* Projection constants of a set of parameters, made once by favorsharp_state_prepare: the caller sets ptr (16-byte
+ * aligned) and bytes (favorsharp_state_features_bytes), the call fills the buffer and the other members. */
+typedef struct {
+  void* ptr;          /* device */
+  size_t bytes;
+  int32_t heads, d, M, sets, dense_c2;
+  float qk_scale;
+} fs_features;
+
+/* theta, Omega: `groups` and `omega_groups` in {1, heads}, one set for every key head or one for each.  SYNCHRONOUS with
+ * respect to `stream` (one word comes back). */
+size_t favorsharp_state_features_bytes(int heads, int d, int M, int groups, int omega_groups);
+int favorsharp_state_prepare(const float* theta, int groups, const float* Omega, int omega_groups, int heads, int d, int M,
+                             float qk_scale, fs_features* host_features, void* stream);
+
+/* Appends K [B, heads, L, d] and V [B, heads, L, dv] (one dtype) to the states; fresh = 1: onto empty states, whatever the slots
+ * held.  left_out (device int32, or NULL): the number of sequences that were left out is ADDED to it. */
+size_t favorsharp_state_append_workspace_bytes(const fs_features* host_features, int B, int L, int dv, int rot_dim);
+int favorsharp_state_append(const fs_features* host_features, const fs_state* state, const int32_t* slots,
+                            const fs_tensor* K, const fs_tensor* V, int B, int L, int dv, const int32_t* lengths,
+                            const fs_rotary* rot, int fresh, int32_t* left_out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Y [B, H, L, dv] = P T / P z for queries Q [B, H, L, d] (cross attention to an encoder kept in the pool; the prompt's part that
+ * attends to what was there before it).  A row whose normaliser is zero (an empty state) is zeros; unread (device int32, or
+ * NULL): the number of such rows is ADDED to it. */
+size_t favorsharp_state_attention_workspace_bytes(const fs_features* host_features, int B, int H, int L, int dv, int rot_dim);
+int favorsharp_state_attention(const fs_features* host_features, const fs_state* state, const int32_t* slots,
+                               const fs_tensor* Q, int B, int H, int L, int dv, const int32_t* lengths,
+                               const fs_rotary* rot, const fs_tensor* Y, int32_t* unread,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of every sequence: K [B, heads, 1, d] and V [B, heads, 1, dv] are appended, then Q [B, H, 1, d] reads the state that
+ * holds them: Y [B, H, 1, dv].  One launch, no workspace.  Q, K, V share a dtype.  unread as above; the rows of sequences
+ * that are left out are counted too. */
+int favorsharp_state_step(const fs_features* host_features, const fs_state* state, const int32_t* slots, const fs_tensor* Q,
+                          const fs_tensor* K, const fs_tensor* V, int B, int H, int dv, const fs_rotary* rot,
+                          const fs_tensor* Y, int32_t* unread, void* stream);
+
+/* Gradients of sum(Y * dY) of favorsharp_state_attention with respect to Q and to T and z (shift constant: Y does not depend on
+ * the scale that T and z share).  dstate: a pool of as many slots, T and z overwritten: sums over the rows of all query heads
+ * and sequences that read the slot, in a fixed order; zeros where none does.  dY, dQ any dtype. */
+size_t favorsharp_state_attention_backward_workspace_bytes(const fs_features* host_features, int B, int H, int L, int dv,
+                                                           int rot_dim);
+int favorsharp_state_attention_backward(const fs_features* host_features, const fs_state* state, const int32_t* slots,
+                                        const fs_tensor* Q, const fs_tensor* dY, int B, int H, int L, int dv,
+                                        const int32_t* lengths, const fs_rotary* rot, const fs_tensor* dQ,
+                                        const fs_state* dstate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of favorsharp_state_append with respect to K and V from those with respect to T and z (dstate).  state: as the append (or
+ * later ones) left it, of which shift is read, and dstate is the gradient at that state.  With respect to the state
+ * before the append the gradient is dstate times 2^(shift before - shift after).  dK, dV any dtype. */
+size_t favorsharp_state_append_backward_workspace_bytes(const fs_features* host_features, int B, int L, int dv, int rot_dim);
+int favorsharp_state_append_backward(const fs_features* host_features, const fs_state* state, const int32_t* slots,
+                                     const fs_state* dstate, const fs_tensor* K, const fs_tensor* V, int B, int L, int dv,
+                                     const int32_t* lengths, const fs_rotary* rot, const fs_tensor* dK, const fs_tensor* dV,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,10 +7,13 @@ the import of `lib()` raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
-from ctypes import c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -26,6 +29,20 @@ THETA_HEADER = 8
 class FsTensor(ctypes.Structure):
     _fields_ = [("ptr", c_void_p), ("dtype", c_int32), ("stride_b", c_int64), ("stride_h", c_int64),
                 ("stride_l", c_int64)]
+
+
+class FsRotary(ctypes.Structure):
+    _fields_ = [("freqs", c_void_p), ("positions", c_void_p), ("stride_b", c_int64), ("stride_l", c_int64), ("rot_dim", c_int32),
+                ("interleaved", c_int32), ("amplitude", c_float)]
+
+
+class FsState(ctypes.Structure):
+    _fields_ = [("T", c_void_p), ("z", c_void_p), ("shift", c_void_p), ("slots", c_int32)]
+
+
+class FsFeatures(ctypes.Structure):
+    _fields_ = [("ptr", c_void_p), ("bytes", c_size_t), ("heads", c_int32), ("d", c_int32), ("M", c_int32), ("sets", c_int32),
+                ("dense_c2", c_int32), ("qk_scale", c_float)]
 
 
 class FavorSharpError(RuntimeError):
@@ -99,6 +116,24 @@ def lib() -> ctypes.CDLL:
         L.favorsharp_kernel_matvec.restype = c_int
         L.favorsharp_kernel_matvec.argtypes = [c_void_p, P, P, c_int, c_int, c_int, c_float, c_float, c_void_p, c_int,
                                                c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
+        R, S, F = ctypes.POINTER(FsRotary), ctypes.POINTER(FsState), ctypes.POINTER(FsFeatures)
+        ws = [c_void_p, c_size_t, c_void_p]
+        for name, restype, argtypes in (
+                ("rotary_frequencies", c_int, [c_int, c_double, c_int, c_double, c_int, c_double, c_double, c_void_p]),
+                ("rotary", c_int, [R, P, c_int, P, c_int, c_int, c_int, c_int, c_int, P, P, c_void_p]),
+                ("state_features_bytes", c_size_t, [c_int] * 5),
+                ("state_prepare", c_int, [c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_int, c_float, F, c_void_p]),
+                ("state_append_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int]),
+                ("state_append", c_int, [F, S, c_void_p, P, P, c_int, c_int, c_int, c_void_p, R, c_int, c_void_p] + ws),
+                ("state_attention_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int, c_int]),
+                ("state_attention", c_int, [F, S, c_void_p, P, c_int, c_int, c_int, c_int, c_void_p, R, P, c_void_p] + ws),
+                ("state_step", c_int, [F, S, c_void_p, P, P, P, c_int, c_int, c_int, R, P, c_void_p, c_void_p]),
+                ("state_attention_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int, c_int]),
+                ("state_attention_backward", c_int, [F, S, c_void_p, P, P, c_int, c_int, c_int, c_int, c_void_p, R, P, S] + ws),
+                ("state_append_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int]),
+                ("state_append_backward", c_int, [F, S, c_void_p, S, P, P, c_int, c_int, c_int, c_void_p, R, P, P] + ws)):
+            fn = getattr(L, "favorsharp_" + name)
+            fn.restype, fn.argtypes = restype, argtypes
         _lib = L
     return _lib
 
@@ -424,3 +459,279 @@ def kernel_matvec(theta: torch.Tensor, X: torch.Tensor, Y: torch.Tensor, qk_scal
                                         ws.numel(), _stream())
     _check(st, "favorsharp_kernel_matvec")
     return out
+
+
+# ------------------------------------------------------------------ rotary positions and attention through kept states
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "blend": 3}
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+class Rotary(NamedTuple):
+    """fs_rotary.  freqs [rot_dim / 2] float64 (radians a position) on the device; positions [B, L] (or [L]: shared) int32, None:
+    row l is at position l."""
+    freqs: torch.Tensor
+    positions: torch.Tensor | None = None
+    interleaved: bool = False
+    amplitude: float = 1.0
+
+
+class Features(NamedTuple):
+    """What state_prepare returns: the buffer of projection constants and the host's fs_features of it."""
+    buffer: torch.Tensor
+    desc: FsFeatures
+
+
+class State(NamedTuple):
+    """fs_state: T [slots, heads, M, dv], z [slots, heads, M], shift [slots, heads] (None in a pool of gradients), float32."""
+    T: torch.Tensor
+    z: torch.Tensor
+    shift: torch.Tensor | None
+
+
+def _on(device):
+    """The library launches on the current device: that of the tensors has to be it."""
+    return _SAME_DEVICE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _one_device(*tensors) -> torch.device:
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("tensors of one call must be on one device")
+    if device.type != "cuda":
+        raise ValueError("device tensor expected")
+    return device
+
+
+def _shaped(name: str, t: torch.Tensor, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _int32(name: str, t: torch.Tensor | None, shape):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous int32")
+    _shaped(name, t, shape)
+    return t.data_ptr()
+
+
+def _counter(name: str, t: torch.Tensor | None):
+    if t is not None and (t.dtype != torch.int32 or t.numel() != 1):
+        raise ValueError(f"{name} must be one int32")
+    return None if t is None else t.data_ptr()
+
+
+def _rotary_desc(rot: Rotary | None, B: int, L: int):
+    """(fs_rotary or None, rot_dim)"""
+    if rot is None:
+        return None, 0
+    if rot.freqs.dtype != torch.float64 or rot.freqs.dim() != 1 or not rot.freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous float64 vector")
+    p, sb, sl = rot.positions, 0, 0
+    if p is not None:
+        if p.dtype != torch.int32:
+            raise ValueError("positions must be int32")
+        _shaped("positions", p, (L,) if p.dim() == 1 else (B, L))
+        sb, sl = (0, p.stride(0)) if p.dim() == 1 else p.stride()
+    rot_dim = 2 * rot.freqs.shape[0]
+    return ctypes.byref(FsRotary(rot.freqs.data_ptr(), None if p is None else p.data_ptr(), sb, sl, rot_dim, int(rot.interleaved),
+                                 rot.amplitude)), rot_dim
+
+
+def _rotary_tensors(rot: Rotary | None):
+    return () if rot is None else (rot.freqs, rot.positions)
+
+
+def _state_desc(f: Features, state: State, dv: int, shift: bool = True):
+    slots, heads, M = state.z.shape
+    if heads != f.desc.heads or M != f.desc.M:
+        raise ValueError("the state has other heads or features than the constants")
+    _shaped("T", state.T, (slots, heads, M, dv))
+    if shift:
+        _shaped("shift", state.shift, (slots, heads))
+    for t in state[:3 if shift else 2]:
+        if t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError("states must be contiguous float32")
+    return ctypes.byref(FsState(state.T.data_ptr(), state.z.data_ptr(), state.shift.data_ptr() if shift else None, slots))
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original_length: int = 0,
+                       low_turns: float = 1.0, high_turns: float = 32.0, device="cuda") -> torch.Tensor:
+    """favorsharp_rotary_frequencies: [rot_dim / 2] float64, radians a position."""
+    out = np.empty(max(rot_dim // 2, 1), dtype=np.float64)
+    _check(lib().favorsharp_rotary_frequencies(rot_dim, base, ROTARY_SCALINGS[scaling], factor, original_length, low_turns, high_turns,
+                                               out.ctypes.data_as(c_void_p)), "favorsharp_rotary_frequencies")
+    return torch.from_numpy(out).to(device)
+
+
+def rotary(X: torch.Tensor, rot: Rotary, X2: torch.Tensor | None = None, transposed: bool = False, out: torch.Tensor | None = None,
+           out2: torch.Tensor | None = None):
+    """favorsharp_rotary: X [B,H,L,d] (and X2 [B,H2,L,d]) turned by their positions -> Y (or (Y, Y2)); transposed: the backward pass.
+    out may be X itself, out2 X2."""
+    B, H, L, d = X.shape
+    if out is None:
+        out = torch.empty((B, H, L, d), dtype=X.dtype, device=X.device)
+    _shaped("out", out, X.shape)
+    H2 = 0
+    if X2 is not None:
+        H2 = X2.shape[1]
+        _shaped("X2", X2, (B, H2, L, d))
+        if out2 is None:
+            out2 = torch.empty((B, H2, L, d), dtype=X2.dtype, device=X.device)
+        _shaped("out2", out2, X2.shape)
+    device = _one_device(X, X2, out, out2, *_rotary_tensors(rot))
+    r, _ = _rotary_desc(rot, B, L)
+    two = (ctypes.byref(_desc4(X2)), ctypes.byref(_desc4(out2))) if H2 else (None, None)
+    with _on(device):
+        st = lib().favorsharp_rotary(r, ctypes.byref(_desc4(X)), H, two[0], H2, B, L, d, int(transposed), ctypes.byref(_desc4(out)), two[1],
+                                     _stream())
+    _check(st, "favorsharp_rotary")
+    return out if X2 is None else (out, out2)
+
+
+def state_prepare(theta: torch.Tensor, Omega: torch.Tensor, qk_scale: float, heads: int | None = None) -> Features:
+    """favorsharp_state_prepare: theta [groups,*], Omega [omega_groups,M,d] -> the constants of `heads` key heads (default: the larger
+    number of sets).  Waits for the stream."""
+    theta, Omega = (theta if theta.dim() == 2 else theta[None]), (Omega if Omega.dim() == 3 else Omega[None])
+    og, M, d = Omega.shape
+    heads = max(theta.shape[0], og) if heads is None else heads
+    if theta.dtype != torch.float32 or Omega.dtype != torch.float32 or not theta.is_contiguous() or not Omega.is_contiguous():
+        raise ValueError("theta and Omega must be contiguous float32")
+    _shaped("theta", theta, (theta.shape[0], theta_floats(d)))
+    device = _one_device(theta, Omega)
+    nbytes = int(lib().favorsharp_state_features_bytes(heads, d, M, theta.shape[0], og))
+    buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    desc = FsFeatures(buf.data_ptr(), buf.numel())
+    with _on(device):
+        st = lib().favorsharp_state_prepare(theta.data_ptr(), theta.shape[0], Omega.data_ptr(), og, heads, d, M, qk_scale, ctypes.byref(desc),
+                                            _stream())
+    _check(st, "favorsharp_state_prepare")
+    return Features(buf, desc)
+
+
+def state_new(slots: int, heads: int, M: int, dv: int, device="cuda") -> State:
+    """Empty states."""
+    return State(torch.zeros((slots, heads, M, dv), dtype=torch.float32, device=device),
+                 torch.zeros((slots, heads, M), dtype=torch.float32, device=device),
+                 torch.full((slots, heads), -math.inf, dtype=torch.float32, device=device))
+
+
+def state_append(f: Features, state: State, K: torch.Tensor, V: torch.Tensor, lengths: torch.Tensor | None = None,
+                 slots: torch.Tensor | None = None, rotary: Rotary | None = None, fresh: bool = False,
+                 left_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> State:
+    """favorsharp_state_append: K [B,heads,L,d], V [B,heads,L,dv] onto the states of the slots (in place)."""
+    B, heads, L, d = K.shape
+    dv = V.shape[3]
+    _shaped("K", K, (B, f.desc.heads, L, f.desc.d))
+    _shaped("V", V, (B, heads, L, dv))
+    device = _one_device(K, V, f.buffer, *state, lengths, slots, left_out, workspace, *_rotary_tensors(rotary))
+    r, rot_dim = _rotary_desc(rotary, B, L)
+    if slots is None and B > state.z.shape[0]:
+        raise ValueError("more sequences than slots")
+    fd = ctypes.byref(f.desc)
+    ws = _workspace(lib().favorsharp_state_append_workspace_bytes(fd, B, L, dv, rot_dim), device, workspace)
+    with _on(device):
+        st = lib().favorsharp_state_append(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(K)),
+                                           ctypes.byref(_desc4(V)), B, L, dv, _int32("lengths", lengths, (B,)), r, int(fresh),
+                                           _counter("left_out", left_out), ws.data_ptr(), ws.numel(), _stream())
+    _check(st, "favorsharp_state_append")
+    return state
+
+
+def state_attention(f: Features, state: State, Q: torch.Tensor, lengths: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+                    rotary: Rotary | None = None, out: torch.Tensor | None = None, out_dtype=None, unread: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """favorsharp_state_attention: Q [B,H,L,d] against the states of the slots -> Y [B,H,L,dv]."""
+    B, H, L, d = Q.shape
+    dv = state.T.shape[3]
+    _shaped("Q", Q, (B, H, L, f.desc.d))
+    if out is None:
+        out = torch.empty((B, H, L, dv), dtype=out_dtype or Q.dtype, device=Q.device)
+    _shaped("out", out, (B, H, L, dv))
+    device = _one_device(Q, out, f.buffer, *state, lengths, slots, unread, workspace, *_rotary_tensors(rotary))
+    r, rot_dim = _rotary_desc(rotary, B, L)
+    fd = ctypes.byref(f.desc)
+    ws = _workspace(lib().favorsharp_state_attention_workspace_bytes(fd, B, H, L, dv, rot_dim), device, workspace)
+    with _on(device):
+        st = lib().favorsharp_state_attention(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)), B, H, L, dv,
+                                              _int32("lengths", lengths, (B,)), r, ctypes.byref(_desc4(out)), _counter("unread", unread),
+                                              ws.data_ptr(), ws.numel(), _stream())
+    _check(st, "favorsharp_state_attention")
+    return out
+
+
+def state_step(f: Features, state: State, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor | None = None,
+               rotary: Rotary | None = None, out: torch.Tensor | None = None, out_dtype=None,
+               unread: torch.Tensor | None = None) -> torch.Tensor:
+    """favorsharp_state_step: K [B,heads,1,d], V [B,heads,1,dv] onto the states (in place), then Q [B,H,1,d] against them -> Y."""
+    B, H, L, d = Q.shape
+    dv = V.shape[3]
+    _shaped("Q", Q, (B, H, 1, f.desc.d))
+    _shaped("K", K, (B, f.desc.heads, 1, d))
+    _shaped("V", V, (B, f.desc.heads, 1, dv))
+    if out is None:
+        out = torch.empty((B, H, 1, dv), dtype=out_dtype or Q.dtype, device=Q.device)
+    _shaped("out", out, (B, H, 1, dv))
+    device = _one_device(Q, K, V, out, f.buffer, *state, slots, unread, *_rotary_tensors(rotary))
+    r, _ = _rotary_desc(rotary, B, 1)
+    with _on(device):
+        st = lib().favorsharp_state_step(ctypes.byref(f.desc), _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)),
+                                         ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, H, dv, r, ctypes.byref(_desc4(out)),
+                                         _counter("unread", unread), _stream())
+    _check(st, "favorsharp_state_step")
+    return out
+
+
+def state_attention_backward(f: Features, state: State, Q: torch.Tensor, dY: torch.Tensor, lengths: torch.Tensor | None = None,
+                             slots: torch.Tensor | None = None, rotary: Rotary | None = None, grad_dtype=None,
+                             dQ: torch.Tensor | None = None, dstate: State | None = None, workspace: torch.Tensor | None = None):
+    """favorsharp_state_attention_backward: gradients of sum(Y * dY) -> (dQ, dstate), dstate a State of the pool's shape without shift."""
+    B, H, L, d = Q.shape
+    dv = state.T.shape[3]
+    _shaped("Q", Q, (B, H, L, f.desc.d))
+    _shaped("dY", dY, (B, H, L, dv))
+    if dQ is None:
+        dQ = torch.empty((B, H, L, d), dtype=grad_dtype or Q.dtype, device=Q.device)
+    if dstate is None:
+        dstate = State(torch.empty_like(state.T), torch.empty_like(state.z), None)
+    _shaped("dQ", dQ, Q.shape)
+    device = _one_device(Q, dY, dQ, f.buffer, *state, *dstate, lengths, slots, workspace, *_rotary_tensors(rotary))
+    r, rot_dim = _rotary_desc(rotary, B, L)
+    fd = ctypes.byref(f.desc)
+    ws = _workspace(lib().favorsharp_state_attention_backward_workspace_bytes(fd, B, H, L, dv, rot_dim), device, workspace)
+    with _on(device):
+        st = lib().favorsharp_state_attention_backward(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)),
+                                                       ctypes.byref(_desc4(dY)), B, H, L, dv, _int32("lengths", lengths, (B,)), r,
+                                                       ctypes.byref(_desc4(dQ)), _state_desc(f, dstate, dv, False), ws.data_ptr(), ws.numel(),
+                                                       _stream())
+    _check(st, "favorsharp_state_attention_backward")
+    return dQ, dstate
+
+
+def state_append_backward(f: Features, state: State, dstate: State, K: torch.Tensor, V: torch.Tensor, lengths: torch.Tensor | None = None,
+                          slots: torch.Tensor | None = None, rotary: Rotary | None = None, grad_dtype=None, grads=None,
+                          workspace: torch.Tensor | None = None):
+    """favorsharp_state_append_backward: dstate (at `state`, the append's result) -> (dK, dV)."""
+    B, heads, L, d = K.shape
+    dv = V.shape[3]
+    _shaped("K", K, (B, f.desc.heads, L, f.desc.d))
+    _shaped("V", V, (B, heads, L, dv))
+    if grads is None:
+        grads = (torch.empty((B, heads, L, d), dtype=grad_dtype or K.dtype, device=K.device),
+                 torch.empty((B, heads, L, dv), dtype=grad_dtype or V.dtype, device=K.device))
+    dK, dV = grads
+    _shaped("dK", dK, K.shape)
+    _shaped("dV", dV, V.shape)
+    device = _one_device(K, V, dK, dV, f.buffer, *state, *dstate, lengths, slots, workspace, *_rotary_tensors(rotary))
+    r, rot_dim = _rotary_desc(rotary, B, L)
+    fd = ctypes.byref(f.desc)
+    ws = _workspace(lib().favorsharp_state_append_backward_workspace_bytes(fd, B, L, dv, rot_dim), device, workspace)
+    with _on(device):
+        st = lib().favorsharp_state_append_backward(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)),
+                                                    _state_desc(f, dstate, dv, False), ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, L, dv,
+                                                    _int32("lengths", lengths, (B,)), r, ctypes.byref(_desc4(dK)), ctypes.byref(_desc4(dV)),
+                                                    ws.data_ptr(), ws.numel(), _stream())
+    _check(st, "favorsharp_state_append_backward")
+    return dK, dV

@@ -28,6 +28,11 @@ SOURCES = {
     "kernels_bf16_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kernels_op.hip": [],
     "kernels_fit.hip": [],
+    "state_api.hip": [],
+    "kernels_rotary.hip": [],
+    "kernels_state.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "kernels_state_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "kernels_state_step.hip": [],
     "host_fit.cpp": [],
 }
 

@@ -1,0 +1,343 @@
+// What the kernels on kept states share: rows turned by their positions, operands as bf16 pieces, the buffer of projection constants.
+//
+// A state of a sequence and a key head is shift = max e, z_m = sum_j 2^(e_jm - shift), T_m = sum_j 2^(e_jm - shift) V_j over the keys
+// appended so far, with e_jm = (W2 k_j)_m + bias_m + r(k_j) (base 2, scale of the keys and log2 e inside W2, bias and r); a query reads it
+// with the features 2^((W1 q)_m + bias_m).
+#pragma once
+#include "fs_common.h"
+#include "kernels.h"
+#include "split3.h"
+
+namespace fs {
+namespace st {
+
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+constexpr float kNone = -__builtin_huge_valf();
+
+// Widths: rows of up to 32, 64 and 128 numbers, in steps of 32 (an operand's contraction) and tiles of 16 (its columns).
+template <int W> constexpr int STEPS = W / 32;
+template <int W> constexpr int TILES = W / 16;
+inline int width_class(int d, int dv) { const int n = d > dv ? d : dv; return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
+
+// ---------------------------------------------------------------------------------------------- projection constants
+// One block per parameter set: operand images of W1 and W2 with the coordinates as contraction index (rows: [32 features][steps][3
+// pieces][2 tiles x 512 numbers]) and with the features as contraction index ([32 features][coordinate tiles][3][512]), those of C2 + C2', the
+// biases (-inf behind the last feature), W1 and W2 in fp32 for single tokens ([4 coordinates][features][4]), C2.
+struct FeaturePlan {
+  int Mp, steps, tiles, d4;      // features in 32s, steps of 32 coordinates, tiles of 16 coordinates, coordinates in fours
+  size_t off_row[2], off_col[2], off_csym, off_bias, off_w[2], off_c2, set, total;
+};
+inline FeaturePlan feature_plan(int d, int M, int sets) {
+  FeaturePlan p;
+  p.Mp = (M + 31) / 32 * 32;
+  p.steps = (d + 31) / 32;
+  p.tiles = 2 * p.steps;
+  p.d4 = (d + 3) / 4;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  size_t off = 0;
+  for (int s = 0; s < 2; ++s) { p.off_row[s] = off; off = up(off + (size_t)p.Mp * p.steps * 3 * 32 * 2); }
+  for (int s = 0; s < 2; ++s) { p.off_col[s] = off; off = up(off + (size_t)p.Mp * p.steps * 3 * 32 * 2); }
+  p.off_csym = off; off = up(off + (size_t)p.tiles * p.steps * 3 * 512 * 2);
+  p.off_bias = off; off = up(off + (size_t)p.Mp * 4);
+  for (int s = 0; s < 2; ++s) { p.off_w[s] = off; off = up(off + (size_t)p.d4 * p.Mp * 4 * 4); }
+  p.off_c2 = off; off = up(off + (size_t)d * d * 4);
+  p.set = off;
+  p.total = 256 + (size_t)sets * p.set;       // a word that says whether some C2 is dense, then the sets
+  return p;
+}
+struct Features {
+  const char* base;              // the first set
+  FeaturePlan p;
+  int sets, d, M;
+  float scale2;                  // qk_scale^2
+  int dense;
+  __device__ const char* set(int h) const { return base + (sets == 1 ? 0 : (size_t)h * p.set); }
+};
+
+// ---------------------------------------------------------------------------------------------- rows
+struct RotaryDev {
+  const double* freqs;           // [rot / 2] radians a position
+  const int32_t* positions;      // [B][L] or nullptr: row l is at position l
+  long long sb, sl;
+  int rot, interleaved;
+  float amplitude;
+};
+// The angle is taken in turns and in 64 bits (position f / 2 pi, less its nearest whole number): in 32 a position of 2^20 would leave
+// four bits of it.  What is left, within half a turn, is exact enough in 32 bits, where cosine and sine are taken.
+__device__ __forceinline__ float2 cos_sin(int position, double freq, float amplitude) {
+  const double turns = (double)position * (freq * 0.15915494309189533577);        // 1 / (2 pi)
+  float s, c;
+  sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+  return make_float2(amplitude * c, amplitude * s);
+}
+__device__ __forceinline__ int position_of(const RotaryDev& r, int b, int l) { return r.positions ? r.positions[b * r.sb + l * r.sl] : l; }
+
+// Rotary positions as the kernels on states see them: rot = 0: rows as they are.  `table` [B][L][rot / 2] holds amplitude (cos, sin).
+struct Turn {
+  const float2* table = nullptr;
+  int rot = 0, interleaved = 0;
+};
+struct Rows {
+  TensorDev X;
+  int L, G;                      // rows of a sequence and heads (G to a state): row v is row v % L of head v / L
+  const int32_t* lengths;        // [B] or nullptr
+  int cols;
+  Turn turn;
+};
+__device__ __forceinline__ int length_of(const Rows& r, int b) { return r.lengths ? max(0, min(r.lengths[b], r.L)) : r.L; }
+struct RowAt { int head, row; };
+__device__ __forceinline__ RowAt row_at(const Rows& r, int v) {
+  const int g = r.G == 1 ? 0 : v / r.L;
+  return {g, v - g * r.L};
+}
+__device__ __forceinline__ long long row_base(const TensorDev& t, int b, int h, int row) { return b * t.sb + h * t.sh + row * t.sl; }
+
+// Eight numbers of a row from column c0 (a multiple of eight) on, zero from `cols` on.
+__device__ __forceinline__ f32x8 load8(const TensorDev& t, long long base, int c0, int cols) {
+  f32x8 x;
+  if (c0 + 8 <= cols) {
+    if (t.dtype == 0) {
+      const f32x4 a = *(const f32x4*)((const float*)t.ptr + base + c0), b = *(const f32x4*)((const float*)t.ptr + base + c0 + 4);
+      x = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    } else {
+      const u32x4 u = *(const u32x4*)((const uint16_t*)t.ptr + base + c0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = c0 + i < cols ? load_elem(t, base + c0 + i) : 0.f;
+  }
+  return x;
+}
+__device__ __forceinline__ void store8(const TensorDev& t, long long base, int c0, int cols, f32x8 x) {
+  if (c0 + 8 <= cols) {
+    if (t.dtype == 0) {
+      float* p = (float*)t.ptr + base + c0;
+      *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
+      *(f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+      u32x4 u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = (uint32_t)f32_to_bf16_bits(x[2 * i]) | (uint32_t)f32_to_bf16_bits(x[2 * i + 1]) << 16;
+      *(u32x4*)((uint16_t*)t.ptr + base + c0) = u;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c0 + i < cols) store_elem(t, base + c0 + i, x[i]);
+  }
+}
+// x turned by the angles cs of its row: y = x cos - partner sin for the first of a pair, x cos + partner sin for the second (sgn -1: turned
+// back).  other(c) gives number c of the row, other8(c0) eight of them.
+template <class Other, class Other8>
+__device__ __forceinline__ f32x8 turned8(f32x8 x, int c0, const Turn& t, const float2* cs, float sgn, Other other, Other8 other8) {
+  if (c0 >= t.rot) return x;
+  const int r = t.rot >> 1;
+  f32x8 y = x;
+  if (t.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c0 + 2 * i < t.rot) {
+        const float2 a = cs[(c0 >> 1) + i];
+        const float s = sgn * a.y;
+        y[2 * i] = x[2 * i] * a.x - x[2 * i + 1] * s;
+        y[2 * i + 1] = x[2 * i + 1] * a.x + x[2 * i] * s;
+      }
+  } else if ((r & 7) == 0) {
+    const bool second = c0 >= r;
+    const f32x8 p = other8(second ? c0 - r : c0 + r);
+    const float2* a = cs + (second ? c0 - r : c0);
+    const float s = second ? sgn : -sgn;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i] * a[i].x + p[i] * (s * a[i].y);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = c0 + i;
+      if (c < t.rot) {
+        const bool second = c >= r;
+        const float2 a = cs[second ? c - r : c];
+        y[i] = x[i] * a.x + other(second ? c - r : c + r) * ((second ? sgn : -sgn) * a.y);
+      }
+    }
+  }
+  return y;
+}
+// Numbers c0 .. c0 + 7 of row v of a state's rows, turned.
+__device__ __forceinline__ f32x8 row8(const Rows& r, int b, int state_head, RowAt at, int c0) {
+  if (c0 >= r.cols) return f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const long long base = row_base(r.X, b, state_head * r.G + at.head, at.row);
+  const f32x8 x = load8(r.X, base, c0, r.cols);
+  if (c0 >= r.turn.rot) return x;
+  const float2* cs = r.turn.table + ((long long)b * r.L + at.row) * (r.turn.rot >> 1);
+  return turned8(x, c0, r.turn, cs, 1.f, [&](int c) { return load_elem(r.X, base + c); }, [&](int c) { return load8(r.X, base, c, r.cols); });
+}
+
+// ---------------------------------------------------------------------------------------------- slots
+// Slot of sequence b, -1 where there is none.  unique: also where an earlier sequence has the same one (for all threads of a workgroup).
+__device__ __forceinline__ int slot_of(const int32_t* slots, int nslots, int b) {
+  const int s = slots ? slots[b] : b;
+  return s >= 0 && s < nslots ? s : -1;
+}
+__device__ __forceinline__ int unique_slot_of(const int32_t* slots, int nslots, int b) {
+  const int s = slot_of(slots, nslots, b);
+  if (slots == nullptr || s < 0) return s;
+  int twice = 0;
+  for (int i = threadIdx.x; i < b; i += blockDim.x) twice |= slots[i] == s;
+  return __syncthreads_or(twice) ? -1 : s;
+}
+
+// ---------------------------------------------------------------------------------------------- operands
+// P pieces of an operand: 1 (a bf16 number is its own piece) or 3.
+template <int P> struct Op { bf16x8 p[P]; };
+template <int P> __device__ __forceinline__ Op<P> as_op(f32x8 x) {
+  Op<P> o;
+  if constexpr (P == 1) {
+    o.p[0] = __builtin_convertvector(x, bf16x8);
+  } else {
+    const Split3 s = split3(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
+    o.p[0] = s.h; o.p[1] = s.m; o.p[2] = s.l;
+  }
+  return o;
+}
+template <int P> __device__ __forceinline__ Op<P> image_op(const uint16_t* img, int lane) {      // images of 512 numbers, one per piece
+  Op<P> o;
+#pragma unroll
+  for (int i = 0; i < P; ++i) o.p[i] = *(const bf16x8*)(img + i * 512 + lane * 8);
+  return o;
+}
+template <int P> __device__ __forceinline__ Op<P> row_op(const uint16_t* s, int plane) {         // eight numbers of a row
+  Op<P> o;
+#pragma unroll
+  for (int i = 0; i < P; ++i) o.p[i] = *(const bf16x8*)(s + i * plane);
+  return o;
+}
+__device__ __forceinline__ u32x2 read_tr(const uint16_t* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
+}
+// A column of the rows 4 g .. 4 g + 3 and 16 + 4 g .. of a tile of 32 (lane l = (g, c) = (l / 16, l % 16)): the order in which two stacked
+// accumulators hold their rows.  s: this lane's piece of row 4 g (see lane_tr).
+template <int P> __device__ __forceinline__ Op<P> column_op(const uint16_t* s, int ld, int plane) {
+  Op<P> o;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const u32x2 a = read_tr(s + i * plane), b = read_tr(s + i * plane + 16 * ld);
+    o.p[i] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+  }
+  return o;
+}
+// Lanes 4 i + a of a group of sixteen name the four 8-byte pieces a of row 4 g + i; lane (a, b) = (c / 4, c % 4) gets column c of the rows.
+__device__ __forceinline__ int lane_tr(int lane, int ld) { return (4 * (lane >> 4) + ((lane & 15) >> 2)) * ld + 4 * (lane & 3); }
+
+// c + a b, small products first.
+template <int PA, int PB>
+__device__ __forceinline__ f32x4 times(const Op<PA>& a, const Op<PB>& b, f32x4 c) {
+  if constexpr (PA == 3 && PB == 3) {
+    c = mfma_bf16(a.p[2], b.p[0], c);
+    c = mfma_bf16(a.p[0], b.p[2], c);
+    c = mfma_bf16(a.p[1], b.p[1], c);
+    c = mfma_bf16(a.p[1], b.p[0], c);
+    c = mfma_bf16(a.p[0], b.p[1], c);
+    return mfma_bf16(a.p[0], b.p[0], c);
+  } else {
+    constexpr int P = PA > PB ? PA : PB;
+#pragma unroll
+    for (int i = P - 1; i >= 0; --i) c = mfma_bf16(a.p[PA > 1 ? i : 0], b.p[PB > 1 ? i : 0], c);
+    return c;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- arguments of the kernels
+struct State {
+  float *T, *z, *shift;
+  int slots;
+};
+// Sums over rows: T[m][c] += 2^(e_vm - ref) V_v[c], z[m] += 2^(e_vm - ref) w_v.
+struct BuildArgs {
+  Features f;
+  int side;                      // 0: features of queries, 1: of keys
+  Rows x, v;
+  const float* terms;            // [B*Hk][rows] row terms (nullptr: those of C2 = -I / 2); -inf: the row is left out
+  const float* weights;          // [B*Hk][rows] w (nullptr: ones)
+  const int32_t* slots;
+  int nslots;
+  int B, Hk, dv;
+  int nsplit, rows_per_split, nblock;
+  float *part, *zpart;           // [B*Hk][nsplit][M][dv], [B*Hk][nsplit][M]
+  float2* refs;                  // [B*Hk][nsplit][Mp / 32]: reference and largest exponent (-inf: nothing summed)
+  const float* shift;            // of the pool, copied to old_shift (nullptr: not)
+  float* old_shift;              // [B*Hk]
+};
+int launch_build(const BuildArgs& a, hipStream_t st);
+// Partial sums onto the states (append), or their sum alone (gradients: slots that no sequence names get zeros).
+struct JoinArgs {
+  const float *part, *zpart;
+  const float2* refs;
+  const float* old_shift;        // nullptr: new states
+  const int32_t* slots;
+  State state;
+  int B, Hk, M, Mp, dv, nsplit;
+  int* left_out;
+};
+int launch_join(const JoinArgs& a, hipStream_t st);
+int launch_join_sum(const JoinArgs& a, hipStream_t st);
+
+// Features of rows times a state.
+enum { OUT_QUOTIENT = 0, OUT_STATS = 1, OUT_SUM = 2 };
+struct ValueArgs {
+  Features f;
+  int side, mode;
+  Rows x;
+  const float* terms;            // [B*Hk][rows] row terms (nullptr: zero)
+  const int32_t* slots;
+  State state;                   // T and z (OUT_SUM: z is not used)
+  int B, Hk, dv;
+  TensorDev out;                 // OUT_QUOTIENT: Y; OUT_SUM: the sums
+  TensorDev dY;                  // OUT_STATS
+  float *lse, *weights;          // OUT_STATS: [B*Hk][rows] -log2 of the normaliser, -dY . Y
+  int* unread;                   // OUT_QUOTIENT: rows without a normaliser are added to it
+};
+int launch_values(const ValueArgs& a, hipStream_t st);
+// Gradient of rows through their features: dx = sum_m U_m W_m, U_m = 2^(e_m + term) (R . T_m + w z_m).
+struct GradArgs {
+  Features f;
+  int side;                      // 1: also the row term's gradient
+  Rows x, r;
+  const float *terms, *weights;  // (weights nullptr: ones)
+  const int32_t* slots;
+  State state;
+  int B, Hk, dv;
+  TensorDev dx;
+};
+int launch_grads(const GradArgs& a, hipStream_t st);
+
+int launch_prepare(const float* theta, int groups, const float* Omega, int omega_groups, int sets, int d, int M, float scale, char* buf,
+                   const FeaturePlan& p, hipStream_t st);
+// Row terms r(k) of turned keys, rows behind the lengths -inf.  shift [slots][Hk] (or nullptr): less the shift of their state, sequences
+// without one, or with that of an earlier one, -inf.
+int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, const float* shift, const int32_t* slots, int nslots, float* terms,
+                     hipStream_t st);
+
+int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev& X2, int H2, int B, int L, int d, int transposed,
+                  const TensorDev& Y, const TensorDev& Y2, hipStream_t st);
+int launch_rotary_table(const RotaryDev& r, int B, int L, float2* table, hipStream_t st);
+
+struct StepArgs {
+  Features f;
+  State state;
+  const int32_t* slots;
+  TensorDev Q, K, V, Y;
+  int B, H, Hk, dv;
+  RotaryDev rot;                 // rot = 0: rows as they are
+  int* unread;
+};
+int launch_step(const StepArgs& a, hipStream_t st);
+
+}  // namespace st
+}  // namespace fs
