@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -52,12 +53,11 @@ def _run(cmd, verbose):
 def build(verbose: bool = True) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ, exist_ok=True)
-    objs = []
-    for src, extra in SOURCES.items():
-        obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
-        _run([hipcc, *COMMON, *extra, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
-    _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], verbose)
+    objs = {src: os.path.join(OBJ, os.path.splitext(src)[0] + ".o") for src in SOURCES}
+    with ThreadPoolExecutor(max_workers=4) as pool:       # (a compiler takes up to 2 GB)
+        list(pool.map(lambda src: _run([hipcc, *COMMON, *SOURCES[src], "-x", "hip", "-c", os.path.join(CSRC, src), "-o", objs[src]], verbose),
+                      SOURCES))
+    _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs.values(), "-o", LIB], verbose)
     return LIB
 
 

@@ -16,10 +16,23 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------- projection constants
 // Sums in 64 bits: the constants are made once and used for every row.
+__device__ __forceinline__ void split2_store(uint16_t* at, size_t piece_stride, float v) {
+  const _Float16 h = (_Float16)v, m = (_Float16)(v - (float)h);
+  at[0] = __builtin_bit_cast(uint16_t, h);
+  at[piece_stride] = __builtin_bit_cast(uint16_t, m);
+}
+__device__ __forceinline__ float block_max(float v, float* tmp) {         // of 256 threads
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
+}
 __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups, const float* Omega, int omega_groups, int d, int M, float scale,
                                                  char* buf, FeaturePlan p) {
-  __shared__ float om[32][128];
-  const int blk = blockIdx.x, side = blockIdx.y, set = blockIdx.z, tid = threadIdx.x;
+  __shared__ float om[32][128], wv[32][128], tmp[4];
+  const int blk = blockIdx.x, side = blockIdx.y, set = blockIdx.z, tid = threadIdx.x, n = 32 * p.steps;
   const size_t dd = (size_t)d * d;
   const float* th = theta + (size_t)(groups == 1 ? 0 : set) * (FS_THETA_HEADER_ + d + 4 * dd);
   const float* omega = Omega + (size_t)(omega_groups == 1 ? 0 : set) * M * d;
@@ -32,16 +45,24 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
   __syncthreads();
   uint16_t *row = (uint16_t*)(base + p.off_row[side]), *col = (uint16_t*)(base + p.off_col[side]);
   float* w = (float*)(base + p.off_w[side]);
-  for (int i = tid; i < 32 * 32 * p.steps; i += 256) {
-    const int f = i / (32 * p.steps), c = i - f * 32 * p.steps, m = 32 * blk + f, tile = f >> 4, r = f & 15;
+  float most = 0.f;
+  for (int i = tid; i < 32 * n; i += 256) {
+    const int f = i / n, c = i - f * n, m = 32 * blk + f, tile = f >> 4, r = f & 15;
     double sum = 0.0;
     if (c < d)
       for (int l = 0; l < d; ++l) sum += (double)om[f][l] * (double)Bm[(size_t)l * d + c];
     const float v = (float)(sum * (double)scale * 1.4426950408889634074);
-    split3_store(row + ((size_t)blk * p.steps + (c >> 5)) * 3 * 1024 + tile * 512 + ((c & 31) / 8 * 16 + r) * 8 + (c & 7), 1024, v);
+    wv[f][c] = v;
+    most = fmaxf(most, fabsf(v));
     split3_store(col + ((size_t)blk * p.tiles + (c >> 4)) * 3 * 512 + (r / 4 * 16 + (c & 15)) * 8 + 4 * tile + (r & 3), 512, v);
     if (c < 4 * p.d4) w[((size_t)(c >> 2) * p.Mp + m) * 4 + (c & 3)] = v;
   }
+  const float up = up_to_2_14(block_max(most, tmp));
+  for (int i = tid; i < 32 * n; i += 256) {
+    const int f = i / n, c = i - f * n, tile = f >> 4, r = f & 15;
+    split2_store(row + ((size_t)blk * p.steps + (c >> 5)) * 2 * 1024 + tile * 512 + ((c & 31) / 8 * 16 + r) * 8 + (c & 7), 1024, wv[f][c] * up);
+  }
+  if (tid == 0) ((float*)(base + p.off_scale[side]))[blk] = power_inverse(up);
   if (side == 0) {
     if (tid < 32) {
       const int m = 32 * blk + tid;
@@ -53,63 +74,102 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
   }
   if (blk == 0) {
     uint16_t* csym = (uint16_t*)(base + p.off_csym);
-    const int n = 32 * p.steps;
+    most = 0.f;
+    for (int i = tid; i < (int)dd; i += 256) {
+      const int a = i / d, c = i - a * d;
+      ((float*)(base + p.off_c2))[i] = C2[i];
+      most = fmaxf(most, fabsf(C2[i] + C2[(size_t)c * d + a]));
+    }
+    const float cup = up_to_2_14(block_max(most, tmp));
     for (int i = tid; i < n * n; i += 256) {
       const int a = i / n, c = i - a * n;
       const float v = a < d && c < d ? C2[(size_t)a * d + c] + C2[(size_t)c * d + a] : 0.f;
-      split3_store(csym + ((size_t)(c >> 4) * p.steps + (a >> 5)) * 3 * 512 + ((a & 31) / 8 * 16 + (c & 15)) * 8 + (a & 7), 512, v);
+      split2_store(csym + ((size_t)(c >> 4) * p.steps + (a >> 5)) * 2 * 512 + ((a & 31) / 8 * 16 + (c & 15)) * 8 + (a & 7), 512, v * cup);
     }
-    for (int i = tid; i < (int)dd; i += 256) ((float*)(base + p.off_c2))[i] = C2[i];
-    if (tid == 0 && ((int)th[2] & 1) == 0) atomicOr((unsigned*)buf, 1u);
+    if (tid == 0) {
+      *(float*)(base + p.off_cscale) = power_inverse(cup);
+      if (((int)th[2] & 1) == 0) atomicOr((unsigned*)buf, 1u);
+    }
   }
 }
 
-// ---------------------------------------------------------------------------------------------- row terms of dense quadratic forms
+// ---------------------------------------------------------------------------------------------- row terms
+// x' C2 x = x' (C2 + C2') x / 2 on matrix instructions, sixteen rows a wave; -|x|^2 / 2 where no quadratic form is dense.
+template <int W>
 __global__ void __launch_bounds__(256) k_row_terms(Features f, Rows x, int Hk, const float* shift, const int32_t* slots, int nslots, float* terms) {
-  __shared__ float y[16][132];
-  const int bh = blockIdx.y, b = bh / Hk, h = bh - b * Hk, r0 = 16 * blockIdx.x;
-  const int row = threadIdx.x >> 4, u = threadIdx.x & 15, len = length_of(x, b);
+  constexpr int S = STEPS<W>;
+  __shared__ __align__(16) float lds[4][16][W + 4];
+  const int bh = blockIdx.y, b = bh / Hk, h = bh - b * Hk, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
+  const int row = 64 * blockIdx.x + 16 * w + c, len = length_of(x, b);
   const int slot = shift ? unique_slot_of(slots, nslots, b) : 0;
-  const bool live = r0 + row < len && slot >= 0;
-  f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (live) v = row8(x, b, h, RowAt{0, r0 + row}, 8 * u);
+  const bool live = row < len && slot >= 0;
+  f32x8 n[S];
+  float most = 0.f, sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[row][8 * u + i] = v[i];
-  __syncthreads();
-  float sum = 0.f;
+  for (int s = 0; s < S; ++s) {
+    n[s] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (live && s < f.p.steps) n[s] = row8<false, true>(x, b, h, RowAt{0, row}, 32 * s + 8 * g);
+    most = fmaxf(most, largest_of(n[s]));
+  }
   if (f.dense) {
-    const float* C2 = (const float*)(f.set(h) + f.p.off_c2);
-    for (int c = u; c < f.d; c += 16) {
-      float z = 0.f;
-      for (int a = 0; a < f.d; ++a) z += y[row][a] * C2[a * f.d + c];
-      sum += z * y[row][c];
+    const char* set = f.set(h);
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float scale = up_to_2_14(most);
+    Op16<2> xo[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      xo[s] = as_op16<2>(n[s] * scale);
+      *(f32x4*)&lds[w][c][32 * s + 8 * g] = f32x4{n[s][0], n[s][1], n[s][2], n[s][3]};
+      *(f32x4*)&lds[w][c][32 * s + 8 * g + 4] = f32x4{n[s][4], n[s][5], n[s][6], n[s][7]};
     }
+    __syncthreads();
+#pragma unroll
+    for (int ct = 0; ct < 2 * S; ++ct)
+      if (ct < f.p.tiles) {
+        f32x4 q = {0.f, 0.f, 0.f, 0.f};
+        const uint16_t* img = (const uint16_t*)(set + f.p.off_csym) + (size_t)ct * f.p.steps * 2 * 512;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+          if (s < f.p.steps) {
+            Op16<2> co;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
+            q = times16(co, xo[s], q);
+          }
+        const f32x4 y = *(const f32x4*)&lds[w][c][16 * ct + 4 * g];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
+      }
+    sum *= 0.5f * power_inverse(scale) * *(const float*)(set + f.p.off_cscale);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += v[i] * v[i];
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += n[s][i] * n[s][i];
     sum *= -0.5f;
   }
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (u == 0 && r0 + row < x.L)
-    terms[(size_t)bh * x.L + r0 + row] = live ? kLog2e * f.scale2 * sum - (shift ? shift[(size_t)slot * Hk + h] : 0.f) : kNone;
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (g == 0 && row < x.L)
+    terms[(size_t)bh * x.L + row] = live ? kLog2e * f.scale2 * sum - (shift ? shift[(size_t)slot * Hk + h] : 0.f) : kNone;
 }
 
 // ---------------------------------------------------------------------------------------------- sums over rows
 template <int W, int XP, int VP> struct BuildLds {
   uint16_t x[2][XP][32][W + 8];
   uint16_t v[2][VP][32][W + 8];
-  float term[2][32], weight[2][32];
+  float term[2][32], weight[2][32], undo[2][32];
 };
 
-template <int W, int XP, int VP, int NW>
+template <int W, int XP, int VP, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 8, NTH = 64 * NW, U = (64 * UPR + NTH - 1) / NTH, LD = W + 8;
   extern __shared__ __align__(16) char lds_raw[];
   BuildLds<W, XP, VP>& lds = *(BuildLds<W, XP, VP>*)lds_raw;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
   const int split = blockIdx.x, bh = blockIdx.z, b = bh / a.Hk, h = bh - b * a.Hk;
-  const int fb = blockIdx.y * NW + w, nfb = a.f.p.Mp / 32, steps = a.f.p.steps, dv = a.dv;
+  const int fb = blockIdx.y * NW + w, nfb = a.f.p.Mp / 32, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv;
   const int slot = slot_of(a.slots, a.nslots, b);
   if (a.old_shift != nullptr && split == 0 && blockIdx.y == 0 && tid == 0) a.old_shift[bh] = slot >= 0 ? a.shift[(size_t)slot * a.Hk + h] : kNone;
   const int len = length_of(a.x, b), rows = a.x.L * a.x.G;
@@ -120,27 +180,6 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     return;
   }
   const char* set = a.f.set(h);
-  Op<3> wop[2][S];
-  float bias[2] = {kNone, kNone};
-  if (active) {
-    const uint16_t* img = (const uint16_t*)(set + a.f.p.off_row[a.side]) + (size_t)fb * steps * 3 * 1024;
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (s < steps)
-#pragma unroll
-        for (int ft = 0; ft < 2; ++ft)
-#pragma unroll
-          for (int p = 0; p < 3; ++p) wop[ft][s].p[p] = *(const bf16x8*)(img + (s * 3 + p) * 1024 + ft * 512 + lane * 8);
-#pragma unroll
-    for (int ft = 0; ft < 2; ++ft) bias[ft] = ((const float*)(set + a.f.p.off_bias))[32 * fb + 16 * ft + c];
-  }
-  f32x4 T[2][VT];
-  float z[2] = {0.f, 0.f}, ref = kNone, top = kNone;
-#pragma unroll
-  for (int ft = 0; ft < 2; ++ft)
-#pragma unroll
-    for (int vt = 0; vt < VT; ++vt) T[ft][vt] = f32x4{0.f, 0.f, 0.f, 0.f};
-
   // units of eight numbers of a row: those of x, then those of v
   f32x8 next[U];
   float next_term[U], next_weight[U];
@@ -157,11 +196,11 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       const RowAt at = row_at(a.x, v + row);
       if (at.row >= len) continue;
       if (is_x) {
-        next[i] = row8(a.x, b, h, at, c0);
+        next[i] = row8<FULL, XP == 2>(a.x, b, h, at, c0);
         next_term[i] = a.terms ? a.terms[(size_t)bh * rows + v + row] : 0.f;
         next_weight[i] = a.weights ? a.weights[(size_t)bh * rows + v + row] : 1.f;
       } else {
-        next[i] = row8(a.v, b, h, at, c0);
+        next[i] = row8<FULL, false>(a.v, b, h, at, c0);
       }
     }
   };
@@ -173,21 +212,22 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       const int q = is_x ? e : e - 32 * UPR, row = q / UPR, u = q % UPR;
       if (q >= 32 * UPR) continue;
       if (is_x) {
-        const Op<XP> o = as_op<XP>(next[i]);
+        float most = largest_of(next[i]), n = 0.f;
 #pragma unroll
-        for (int p = 0; p < XP; ++p) *(bf16x8*)&lds.x[buf][p][row][8 * u] = o.p[p];
-        float t = next_term[i];
-        if (a.terms == nullptr) {                       // C2 = -I / 2
-          float n = 0.f;
+        for (int j = 0; j < 8; ++j) n += next[i][j] * next[i][j];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) n += next[i][j] * next[i][j];
-#pragma unroll
-          for (int o2 = UPR / 2; o2 > 0; o2 >>= 1) n += __shfl_xor(n, o2);
-          t += -0.5f * kLog2e * a.f.scale2 * n;
+        for (int o = UPR / 2; o > 0; o >>= 1) {
+          most = fmaxf(most, __shfl_xor(most, o));
+          n += __shfl_xor(n, o);
         }
+        const float scale = up_to_2_14(most);
+        const Op16<XP> o = as_op16<XP>(next[i] * scale);
+#pragma unroll
+        for (int p = 0; p < XP; ++p) *(f16x8*)&lds.x[buf][p][row][8 * u] = o.p[p];
         if (u == 0) {
-          lds.term[buf][row] = t;
+          lds.term[buf][row] = a.terms ? next_term[i] : next_term[i] - 0.5f * kLog2e * a.f.scale2 * n;      // (C2 = -I / 2)
           lds.weight[buf][row] = next_weight[i];
+          lds.undo[buf][row] = power_inverse(scale);
         }
       } else {
         const Op<VP> o = as_op<VP>(next[i]);
@@ -198,6 +238,27 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   };
 
   fetch(v0);
+  Op16<2> wop[2][S];
+  float bias[2] = {kNone, kNone}, wscale = 0.f;
+  if (active) {
+    const uint16_t* img = (const uint16_t*)(set + a.f.p.off_row[a.side]) + (size_t)fb * steps * 2 * 1024;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (FULL || s < steps)
+#pragma unroll
+        for (int ft = 0; ft < 2; ++ft)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) wop[ft][s].p[p] = *(const f16x8*)(img + (s * 2 + p) * 1024 + ft * 512 + lane * 8);
+#pragma unroll
+    for (int ft = 0; ft < 2; ++ft) bias[ft] = ((const float*)(set + a.f.p.off_bias))[32 * fb + 16 * ft + c];
+    wscale = ((const float*)(set + a.f.p.off_scale[a.side]))[fb];
+  }
+  f32x4 T[2][VT];
+  float z[2] = {0.f, 0.f}, ref = kNone, top = kNone;
+#pragma unroll
+  for (int ft = 0; ft < 2; ++ft)
+#pragma unroll
+    for (int vt = 0; vt < VT; ++vt) T[ft][vt] = f32x4{0.f, 0.f, 0.f, 0.f};
   put(0);
   __syncthreads();
   int buf = 0;
@@ -207,28 +268,29 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     if (active) {
       f32x4 E[2][2];             // [tile of rows][tile of features]
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        E[t][0] = E[t][1] = zero;
+      for (int t = 0; t < 2; ++t) E[t][0] = E[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < S; ++s)
-          if (s < steps) {
-            const Op<XP> x = row_op<XP>(&lds.x[buf][0][16 * t + c][32 * s + 8 * g], 32 * LD);
-            E[t][0] = times(x, wop[0][s], E[t][0]);
-            E[t][1] = times(x, wop[1][s], E[t][1]);
+      for (int s = 0; s < S; ++s)
+        if (FULL || s < steps)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            Op16<XP> x;
+#pragma unroll
+            for (int p = 0; p < XP; ++p) x.p[p] = *(const f16x8*)&lds.x[buf][p][16 * t + c][32 * s + 8 * g];
+            E[t][0] = times16(x, wop[0][s], E[t][0]);
+            E[t][1] = times16(x, wop[1][s], E[t][1]);
           }
-      }
       f32x4 weight[2];
       float most = kNone;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const f32x4 term = *(const f32x4*)&lds.term[buf][16 * t + 4 * g];
+        const f32x4 term = *(const f32x4*)&lds.term[buf][16 * t + 4 * g], undo = *(const f32x4*)&lds.undo[buf][16 * t + 4 * g] * wscale;
         weight[t] = *(const f32x4*)&lds.weight[buf][16 * t + 4 * g];
 #pragma unroll
         for (int ft = 0; ft < 2; ++ft)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            E[t][ft][r] = (E[t][ft][r] + bias[ft]) + term[r];
+            E[t][ft][r] = E[t][ft][r] * undo[r] + (bias[ft] + term[r]);
             most = fmaxf(most, E[t][ft][r]);
           }
       }
@@ -263,7 +325,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       }
 #pragma unroll
       for (int vt = 0; vt < VT; ++vt)
-        if (16 * vt < dv) {
+        if (FULL || 16 * vt < dv) {
           const Op<VP> vo = column_op<VP>(&lds.v[buf][0][0][16 * vt] + lane_tr(lane, LD), LD, 32 * LD);
           T[0][vt] = times(so[0], vo, T[0][vt]);
           T[1][vt] = times(so[1], vo, T[1][vt]);
@@ -286,7 +348,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     if (g == 0 && m0 + c < a.f.M) a.zpart[at * a.f.M + m0 + c] = zs;
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt)
-      if (16 * vt + c < dv)
+      if (FULL || 16 * vt + c < dv)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (m0 + 4 * g + r < a.f.M) a.part[(at * a.f.M + m0 + 4 * g + r) * dv + 16 * vt + c] = T[ft][vt][r];
@@ -295,14 +357,6 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
 
 // ---------------------------------------------------------------------------------------------- join
 constexpr int kJoinWeights = 4096;       // references of a state's partial sums: at most 64 splits of 2048 features
-
-__device__ __forceinline__ float block_max(float v, float* tmp) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
-}
 
 template <int VEC>
 __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
@@ -374,9 +428,9 @@ __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
   }
 }
 
-template <int W, int XP, int VP, int NW> int build(const BuildArgs& a, hipStream_t st) {
+template <int W, int XP, int VP, int NW, bool FULL> int build(const BuildArgs& a, hipStream_t st) {
   constexpr size_t lds = sizeof(BuildLds<W, XP, VP>);
-  auto kernel = k_build<W, XP, VP, NW>;
+  auto kernel = k_build<W, XP, VP, NW, FULL>;
   if (lds > 64 * 1024 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return 5;
@@ -384,12 +438,15 @@ template <int W, int XP, int VP, int NW> int build(const BuildArgs& a, hipStream
   hipLaunchKernelGGL(kernel, dim3(a.nsplit, a.nblock, a.B * a.Hk), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int W, int XP, int VP> int build_nw(const BuildArgs& a, hipStream_t st) {
-  return a.f.p.Mp > 128 ? build<W, XP, VP, 8>(a, st) : build<W, XP, VP, 4>(a, st);
+template <int W, int XP, int VP, bool FULL> int build_waves(const BuildArgs& a, hipStream_t st) {
+  return a.f.p.Mp > 128 ? build<W, XP, VP, 8, FULL>(a, st) : build<W, XP, VP, 4, FULL>(a, st);
 }
-template <int W> int build_pieces(const BuildArgs& a, hipStream_t st) {
-  if (a.v.X.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? build_nw<W, 1, 1>(a, st) : build_nw<W, 3, 1>(a, st);
-  return build_nw<W, 3, 3>(a, st);
+template <int W, bool FULL> int build_pieces(const BuildArgs& a, hipStream_t st) {
+  if (a.v.X.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? build_waves<W, 1, 1, FULL>(a, st) : build_waves<W, 2, 1, FULL>(a, st);
+  return build_waves<W, 2, 3, FULL>(a, st);
+}
+template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
+  return a.f.d == W && a.dv == W ? build_pieces<W, true>(a, st) : build_pieces<W, false>(a, st);
 }
 int join_grid(const JoinArgs& a, int vec) { return std::max(1, std::min((a.M * a.dv / vec + a.M + 255) / 256, 64)); }
 
@@ -397,9 +454,9 @@ int join_grid(const JoinArgs& a, int vec) { return std::max(1, std::min((a.M * a
 
 int launch_build(const BuildArgs& a, hipStream_t st) {
   switch (width_class(a.f.d, a.dv)) {
-    case 32: return build_pieces<32>(a, st);
-    case 64: return build_pieces<64>(a, st);
-    default: return build_pieces<128>(a, st);
+    case 32: return build_width<32>(a, st);
+    case 64: return build_width<64>(a, st);
+    default: return build_width<128>(a, st);
   }
 }
 int launch_join(const JoinArgs& a, hipStream_t st) {
@@ -420,7 +477,8 @@ int launch_prepare(const float* theta, int groups, const float* Omega, int omega
 }
 int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, const float* shift, const int32_t* slots, int nslots, float* terms,
                      hipStream_t st) {
-  hipLaunchKernelGGL(k_row_terms, dim3((k.L + 15) / 16, B * Hk), dim3(256), 0, st, f, k, Hk, shift, slots, nslots, terms);
+  auto kernel = f.d <= 32 ? k_row_terms<32> : f.d <= 64 ? k_row_terms<64> : k_row_terms<128>;
+  hipLaunchKernelGGL(kernel, dim3((k.L + 63) / 64, B * Hk), dim3(256), 0, st, f, k, Hk, shift, slots, nslots, terms);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 

@@ -1,10 +1,14 @@
-// Rows against a finished state: the features of queries (or keys) times the state's rows, and the gradient of rows through their features.
+// Rows against finished states: queries times a state's rows, and the gradients of queries, keys and values.
 //
-// A wave takes whole rows (16 RT of them) through all features, 32 at a time; the workgroup brings the operand images of W and the
-// state's 32 rows, split into bf16 pieces, to LDS for all its waves, the next ones on their way meanwhile.  The exponents come out
-// row by lane and feature by register: two stacked tiles are, without a move, the operand of the product with the state (whose
-// columns come from the transposing LDS read) and of that with W.  A row's reference is raised when an exponent passes it by 2^16,
-// which its first 32 features as a rule prevent; the quotient loses it.
+// All of them walk the features 32 at a time.  The exponents come out row by lane and feature by register: two stacked tiles are,
+// without a move, the operand of the products with the state (whose columns come from the transposing LDS read) and with W.  The
+// state's rows are split into bf16 pieces on their way to LDS: two where the result is rounded to bf16 (an error of 2^-16 beside its 2^-9), three
+// where not.  A row's reference is raised when an exponent passes it by 2^16, which its first 32 features as a rule prevent; the
+// quotient loses it.
+//
+// Many rows (DIRECT = false): a wave takes 16 RT rows of its own through all features, the workgroup brings images of W and the
+// state to LDS for all its waves, the next ones on their way meanwhile.  Few rows: the waves of a workgroup take the same rows and a part
+// of the features each, with the state in LDS of their own and W from L2, no barrier until their sums meet at the end.
 #include <algorithm>
 
 #include "state_common.h"
@@ -13,258 +17,406 @@ namespace fs {
 namespace st {
 namespace {
 
-// What a step of 32 features needs in LDS.
-template <int W, bool COL> struct StepLds {
-  uint16_t row[STEPS<W>][3][1024];
-  uint16_t col[COL ? TILES<W> : 1][3][COL ? 512 : 8];
-  uint16_t t[3][32][W + 8];
+// 32 features' rows of the state in TP pieces.
+template <int W, int TP> struct StateLds {
+  uint16_t t[TP][32][W + 8];
   float z[32], bias[32];
 };
-template <int W, bool COL, int NW> struct Stage {
-  static constexpr int NTH = 64 * NW, NI = (STEPS<W> * 384 + NTH - 1) / NTH, NT = (8 * W + NTH - 1) / NTH;
-  u32x4 row[NI], col[COL ? NI : 1];
+template <int W, int CP> struct ImageLds {
+  uint16_t row[STEPS<W>][2][1024];
+  uint16_t col[CP ? TILES<W> : 1][CP ? CP : 1][CP ? 512 : 8];
+};
+// Where they come from; NTH threads carry them.
+template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
+  static constexpr int NR = IMAGES ? (STEPS<W> * 256 + NTH - 1) / NTH : 1, NC = IMAGES && CP ? (TILES<W> * CP * 64 + NTH - 1) / NTH : 1,
+                       NT = (8 * W + NTH - 1) / NTH;
+  u32x4 row[NR], col[NC];
   f32x4 t[NT];
   float z, bias;
   const char *row_img, *col_img;
   const float *T, *zs, *biases;
-  int units, M, dv;                 // units of 16 bytes of an image of 32 features
+  int steps, M, dv;
 
   __device__ __forceinline__ void start(const Features& f, int side, const char* set, const float* T_, const float* z_, int dv_) {
     row_img = set + f.p.off_row[side];
     col_img = set + f.p.off_col[side];
     biases = (const float*)(set + f.p.off_bias);
-    T = T_; zs = z_; dv = dv_; M = f.M;
-    units = f.p.steps * 384;
+    T = T_; zs = z_; dv = FULL ? W : dv_; M = f.M;
+    steps = FULL ? STEPS<W> : f.p.steps;
   }
   __device__ __forceinline__ void fetch(int fb, int tid) {
+    if constexpr (IMAGES) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int e = tid + NTH * i;
-      if (e < units) {
-        row[i] = *(const u32x4*)(row_img + ((size_t)fb * units + e) * 16);
-        if constexpr (COL) col[i] = *(const u32x4*)(col_img + ((size_t)fb * units + e) * 16);
+      for (int i = 0; i < NR; ++i) {
+        const int e = tid + NTH * i;
+        if (e < steps * 256) row[i] = *(const u32x4*)(row_img + ((size_t)fb * steps * 256 + e) * 16);
       }
+      if constexpr (CP > 0)
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          const int e = tid + NTH * i, tile = e / (CP * 64);
+          if (tile < 2 * steps) col[i] = *(const u32x4*)(col_img + ((size_t)(fb * 2 * steps + tile) * 192 + (e - tile * CP * 64)) * 16);
+        }
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int e = tid + NTH * i, m = 32 * fb + e / (W / 4), c = 4 * (e % (W / 4));
       t[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (e < 8 * W && m < M && c < dv) {
+      if (e < 8 * W && m < M && (FULL || c < dv)) {
         const float* p = T + (size_t)m * dv + c;
-        if ((dv & 3) == 0) t[i] = *(const f32x4*)p;
+        if (FULL || (dv & 3) == 0) t[i] = *(const f32x4*)p;
         else
 #pragma unroll
           for (int j = 0; j < 4; ++j) t[i][j] = c + j < dv ? p[j] : 0.f;
       }
     }
     if (tid < 32) {
-      z = zs != nullptr && 32 * fb + tid < M ? zs[32 * fb + tid] : 0.f;
+      z = 32 * fb + tid < M ? zs[32 * fb + tid] : 0.f;
       bias = biases[32 * fb + tid];
     }
   }
-  __device__ __forceinline__ void put(StepLds<W, COL>& lds, int tid) {
+  __device__ __forceinline__ void put(StateLds<W, TP>& s, ImageLds<W, CP>* img, int tid) {
+    if constexpr (IMAGES) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int e = tid + NTH * i;
-      if (e < units) {
-        *(u32x4*)((char*)lds.row + e * 16) = row[i];
-        if constexpr (COL) *(u32x4*)((char*)lds.col + e * 16) = col[i];
+      for (int i = 0; i < NR; ++i) {
+        const int e = tid + NTH * i;
+        if (e < steps * 256) *(u32x4*)((char*)img->row + e * 16) = row[i];
       }
+      if constexpr (CP > 0)
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          const int e = tid + NTH * i;
+          if (e < 2 * steps * CP * 64) *(u32x4*)((char*)img->col + e * 16) = col[i];
+        }
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int e = tid + NTH * i, m = e / (W / 4), c = 4 * (e % (W / 4));
       if (e < 8 * W) {
-        const Split3 s = split3(t[i], t[i]);
-        *(u32x2*)&lds.t[0][m][c] = u32x2{__builtin_bit_cast(u32x4, s.h)[0], __builtin_bit_cast(u32x4, s.h)[1]};
-        *(u32x2*)&lds.t[1][m][c] = u32x2{__builtin_bit_cast(u32x4, s.m)[0], __builtin_bit_cast(u32x4, s.m)[1]};
-        *(u32x2*)&lds.t[2][m][c] = u32x2{__builtin_bit_cast(u32x4, s.l)[0], __builtin_bit_cast(u32x4, s.l)[1]};
+        const f32x8 v = {t[i][0], t[i][1], t[i][2], t[i][3], 0.f, 0.f, 0.f, 0.f};
+        const Op<TP> o = as_op<TP>(v);
+#pragma unroll
+        for (int p = 0; p < TP; ++p) {
+          const u32x4 u = __builtin_bit_cast(u32x4, o.p[p]);
+          *(u32x2*)&s.t[p][m][c] = u32x2{u[0], u[1]};
+        }
       }
     }
     if (tid < 32) {
-      lds.z[tid] = z;
-      lds.bias[tid] = bias;
+      s.z[tid] = z;
+      s.bias[tid] = bias;
     }
   }
 };
+// W of 32 features as operands, from LDS or (img = nullptr) from where the images lie.
+template <int W, int CP> struct Weights {
+  const ImageLds<W, CP>* img;
+  const char *row_img, *col_img;
+  int fb, steps;
+  __device__ __forceinline__ Op16<2> row(int s, int ft, int lane) const {
+    Op16<2> o;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int at = (s * 2 + p) * 1024 + ft * 512 + lane * 8;
+      o.p[p] = img ? *(const f16x8*)&img->row[0][0][at] : *(const f16x8*)(row_img + ((size_t)fb * steps * 2048 + at) * 2);
+    }
+    return o;
+  }
+  __device__ __forceinline__ Op<CP> col(int ct, int lane) const {
+    return img ? image_op<CP>(&img->col[ct][0][0], lane) : image_op<CP>((const uint16_t*)col_img + (size_t)(fb * 2 * steps + ct) * 1536, lane);
+  }
+};
 
-// A tile of 16 rows from the accumulators (register r of lane (g, c): row 4 g + r, column 16 ct + c) to a wave's own part of LDS.
-template <int W> __device__ __forceinline__ void tile_to_lds(float* dst, const f32x4 (&acc)[TILES<W>], int lane) {
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The rows of a wave: their number as operands of the exponents and what undoes their scale.
+template <int W, int XP, int RT, bool FULL> struct RowOps {
+  static constexpr int S = STEPS<W>;
+  Op16<XP> x[RT][S];
+  float undo[RT];
+  RowAt at[RT];
+  bool live[RT];
+  __device__ __forceinline__ void load(const Rows& r, int b, int h, int v0, int rows, int len, int steps, int lane) {
+    const int g = lane >> 4, c = lane & 15;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int v = v0 + 16 * rt + c;
+      at[rt] = row_at(r, min(v, rows - 1));
+      live[rt] = v < rows && at[rt].row < len;
+      f32x8 n[S];
+      float most = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        n[s] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (live[rt] && (FULL || s < steps)) n[s] = row8<FULL, XP == 2>(r, b, h, at[rt], 32 * s + 8 * g);
+        most = fmaxf(most, largest_of(n[s]));
+      }
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float scale = up_to_2_14(most);
+      undo[rt] = power_inverse(scale);
+#pragma unroll
+      for (int s = 0; s < S; ++s) x[rt][s] = as_op16<XP>(n[s] * scale);
+    }
+  }
+};
+template <int W, int XP, int CP, int RT, bool FULL>
+__device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, const Weights<W, CP>& weights, int steps, int lane, f32x4 (&E)[RT][2]) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) E[rt][0] = E[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < STEPS<W>; ++s)
+    if (FULL || s < steps)
+#pragma unroll
+      for (int ft = 0; ft < 2; ++ft) {
+        const Op16<2> w = weights.row(s, ft, lane);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) E[rt][ft] = times16(w, x.x[rt][s], E[rt][ft]);
+      }
+}
+__device__ __forceinline__ float over_groups_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float over_groups_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+// Numbers of rows 4 g .. 4 g + 3 of a tile from the lanes of the rows.
+__device__ __forceinline__ f32x4 by_row(float v, int lane) {
+  f32x4 k;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) k[r] = __shfl(v, 4 * (lane >> 4) + r);
+  return k;
+}
+// E: exponents of a tile of rows less their references (`first`: none yet, 0).  Raises those that an exponent passes by 2^16, and what was
+// summed to them.
+template <int N, int K, int TA, int TB>
+__device__ __forceinline__ void raise(bool first, f32x4 (&E)[2], float& ref, float (&sums)[N], f32x4 (&acc)[K][TA], f32x4 (&more)[K][TB], int rt,
+                                      int lane) {
+  float most = kNone;
+#pragma unroll
+  for (int ft = 0; ft < 2; ++ft)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) most = fmaxf(most, E[ft][r]);
+  if (first) {
+    most = over_groups_max(most);
+    ref = most == kNone ? 0.f : most - 8.f;
+#pragma unroll
+    for (int ft = 0; ft < 2; ++ft) E[ft] -= ref;
+  } else if (__any(most > 16.f)) {
+    most = over_groups_max(most);
+    const float up = most > 16.f ? most - 8.f : 0.f, keep = fast_exp2(-up);
+    ref += up;
+#pragma unroll
+    for (int n = 0; n < N; ++n) sums[n] *= keep;
+    const f32x4 k = by_row(keep, lane);
+#pragma unroll
+    for (int t = 0; t < TA; ++t) acc[rt][t] *= k;
+#pragma unroll
+    for (int t = 0; t < TB; ++t) more[rt][t] *= k;
+#pragma unroll
+    for (int ft = 0; ft < 2; ++ft) E[ft] -= up;
+  }
+}
+
+// A tile of 16 rows from the accumulators (register r of lane (g, c): row 4 g + r, column 16 ct + c), times a number of the row, to LDS.
+template <int W> __device__ __forceinline__ void tile_to_lds(float* dst, const f32x4 (&acc)[TILES<W>], f32x4 factor, int lane) {
   const int g = lane >> 4, c = lane & 15;
 #pragma unroll
   for (int ct = 0; ct < TILES<W>; ++ct)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) dst[(4 * g + r) * (W + 4) + 16 * ct + c] = acc[ct][r];
-  __builtin_amdgcn_wave_barrier();
-  asm volatile("" ::: "memory");
+    for (int r = 0; r < 4; ++r) dst[(4 * g + r) * (W + 4) + 16 * ct + c] = acc[ct][r] * factor[r];
+}
+template <int W> __device__ __forceinline__ f32x8 from_tile(const float* row, int c0) {
+  const f32x4 a = *(const f32x4*)(row + c0), b = *(const f32x4*)(row + c0 + 4);
+  return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-template <int W, int XP, int NW>
-__global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
-  constexpr int S = STEPS<W>, VT = TILES<W>, RT = 2, LD = W + 8;
-  extern __shared__ __align__(16) char lds_raw[];
-  StepLds<W, false>* lds = (StepLds<W, false>*)lds_raw;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, steps = a.f.p.steps, dv = a.dv, nfb = a.f.p.Mp / 32;
-  const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
-  const int v0 = (blockIdx.x * NW + w) * 16 * RT;
-  const char* set = a.f.set(h);
-  const size_t st = (size_t)max(slot, 0) * a.Hk + h;
+constexpr size_t most_of(size_t a, size_t b) { return a > b ? a : b; }
+template <int W, int TP, int CP, int NW, int RT, bool DIRECT> constexpr size_t rows_lds() {
+  return DIRECT ? most_of(NW * sizeof(StateLds<W, TP>), (size_t)NW * 16 * RT * (W + 4) * 4)
+                : most_of(2 * (sizeof(StateLds<W, TP>) + sizeof(ImageLds<W, CP>)), (size_t)NW * 16 * (W + 4) * 4);
+}
 
-  // this lane's row of each tile: row v0 + 16 rt + c
-  Op<XP> x[RT][S];
-  float term[RT], ref[RT], den[RT];
-  f32x4 acc[RT][VT];
-  bool live[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int v = v0 + 16 * rt + c;
-    const RowAt at = row_at(a.x, min(v, rows - 1));
-    live[rt] = v < rows && at.row < len;
-    term[rt] = a.terms && live[rt] ? a.terms[(size_t)bh * rows + v] : 0.f;
-    ref[rt] = kNone;
-    den[rt] = 0.f;
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (s < steps) {
-        f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live[rt]) n = row8(a.x, b, h, at, 32 * s + 8 * g);
-        x[rt][s] = as_op<XP>(n);
-      }
-#pragma unroll
-    for (int vt = 0; vt < VT; ++vt) acc[rt][vt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  if (slot >= 0) {
-    Stage<W, false, NW> stage;
-    stage.start(a.f, a.side, set, a.state.T + st * a.f.M * dv, a.state.z ? a.state.z + st * a.f.M : nullptr, dv);
+// Calls body(state in LDS, W, first step of this wave?) for the features of this wave.
+template <int W, int TP, int CP, int NW, bool FULL, bool DIRECT, class Body>
+__device__ __forceinline__ void walk_features(const Features& f, int side, const char* set, const float* T, const float* z, int dv, char* lds, int w,
+                                              int tid, int lane, Body body) {
+  const int nfb = f.p.Mp / 32;
+  if constexpr (DIRECT) {
+    Stage<W, TP, 0, 64, FULL, false> stage;
+    stage.start(f, side, set, T, z, dv);
+    StateLds<W, TP>& mine = ((StateLds<W, TP>*)lds)[w];
+    if (w < nfb) stage.fetch(w, lane);
+    for (int fb = w; fb < nfb; fb += NW) {
+      stage.put(mine, nullptr, lane);
+      if (fb + NW < nfb) stage.fetch(fb + NW, lane);
+      wave_fence();
+      body(mine, Weights<W, CP>{nullptr, stage.row_img, stage.col_img, fb, stage.steps}, fb == w);
+      wave_fence();
+    }
+  } else {
+    Stage<W, TP, CP, 64 * NW, FULL, true> stage;
+    stage.start(f, side, set, T, z, dv);
+    struct Both { StateLds<W, TP> s; ImageLds<W, CP> img; };
+    Both* both = (Both*)lds;
     stage.fetch(0, tid);
-    stage.put(lds[0], tid);
+    stage.put(both[0].s, &both[0].img, tid);
     __syncthreads();
     for (int fb = 0; fb < nfb; ++fb) {
-      const StepLds<W, false>& l = lds[fb & 1];
+      Both &now = both[fb & 1], &next = both[~fb & 1];
       const bool more = fb + 1 < nfb;
       if (more) stage.fetch(fb + 1, tid);
-      f32x4 E[RT][2];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) E[rt][0] = E[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < S; ++s)
-        if (s < steps)
-#pragma unroll
-          for (int ft = 0; ft < 2; ++ft) {
-            Op<3> wo;
-#pragma unroll
-            for (int p = 0; p < 3; ++p) wo.p[p] = *(const bf16x8*)&l.row[0][0][(s * 3 + p) * 1024 + ft * 512 + lane * 8];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) E[rt][ft] = times(wo, x[rt][s], E[rt][ft]);
-          }
-      f32x4 zf[2];
-      Op<3> po[RT];
-#pragma unroll
-      for (int ft = 0; ft < 2; ++ft) {
-        const f32x4 bias = *(const f32x4*)&l.bias[16 * ft + 4 * g];
-        zf[ft] = *(const f32x4*)&l.z[16 * ft + 4 * g];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) E[rt][ft][r] = (E[rt][ft][r] + bias[r]) + term[rt];
-      }
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float most = kNone;
-#pragma unroll
-        for (int ft = 0; ft < 2; ++ft)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) most = fmaxf(most, E[rt][ft][r]);
-        if (__any(most > ref[rt] + 16.f)) {
-          most = fmaxf(most, __shfl_xor(most, 16));
-          most = fmaxf(most, __shfl_xor(most, 32));
-          const float now = most > ref[rt] + 16.f ? most - 8.f : ref[rt];
-          const float keep = now == ref[rt] ? 1.f : fast_exp2(ref[rt] - now);
-          ref[rt] = now;
-          den[rt] *= keep;
-          f32x4 k;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) k[r] = __shfl(keep, 4 * g + r);
-#pragma unroll
-          for (int vt = 0; vt < VT; ++vt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[rt][vt][r] *= k[r];
-        }
-        const float at = ref[rt] == kNone ? 0.f : ref[rt];
-        f32x8 p;
-#pragma unroll
-        for (int ft = 0; ft < 2; ++ft)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            p[4 * ft + r] = fast_exp2(E[rt][ft][r] - at);
-            den[rt] += p[4 * ft + r] * zf[ft][r];
-          }
-        po[rt] = as_op<3>(p);
-      }
-#pragma unroll
-      for (int vt = 0; vt < VT; ++vt)
-        if (16 * vt < dv) {
-          const Op<3> t = column_op<3>(&l.t[0][0][16 * vt] + lane_tr(lane, LD), LD, 32 * LD);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][vt] = times(po[rt], t, acc[rt][vt]);
-        }
-      if (more) stage.put(lds[(fb + 1) & 1], tid);
+      body(now.s, Weights<W, CP>{&now.img, nullptr, nullptr, fb, stage.steps}, fb == 0);
+      if (more) stage.put(next.s, &next.img, tid);
       __syncthreads();
     }
   }
-  float* tile = (float*)lds_raw + w * 16 * (W + 4);
+}
+// Common reference and sums of a row over the waves of a DIRECT workgroup: what this wave's are multiplied by.  red: [RT][NW][16] refs, then
+// N times the same of sums.
+template <int NW, int RT, int N>
+__device__ __forceinline__ void meet(float (&ref)[RT], float (&sums)[RT][N], float (&factor)[RT], float* red, bool any, int w, int lane) {
+  const int c = lane & 15;
+  if (lane < 16)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      red[(rt * NW + w) * 16 + c] = any ? ref[rt] : kNone;
+#pragma unroll
+      for (int n = 0; n < N; ++n) red[((n + 1) * RT * NW + rt * NW + w) * 16 + c] = any ? sums[rt][n] : 0.f;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = kNone;
+    for (int i = 0; i < NW; ++i) top = fmaxf(top, red[(rt * NW + i) * 16 + c]);
+    factor[rt] = any ? fast_exp2(ref[rt] - top) : 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float sum = 0.f;
+      for (int i = 0; i < NW; ++i) {
+        const float r = red[(rt * NW + i) * 16 + c];
+        if (r != kNone) sum += fast_exp2(r - top) * red[((n + 1) * RT * NW + rt * NW + i) * 16 + c];
+      }
+      sums[rt][n] = sum;
+    }
+    ref[rt] = top;
+  }
+}
+
+template <int W, int XP, int P, int NW, int RT, bool FULL, bool DIRECT>
+__global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
+  constexpr int VT = TILES<W>, LD = W + 8;
+  extern __shared__ __align__(16) char lds[];
+  __shared__ float red[DIRECT ? 2 * RT * NW * 16 : 1];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
+  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, steps = a.f.p.steps, dv = FULL ? W : a.dv;
+  const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
+  const int v0 = (DIRECT ? blockIdx.x : blockIdx.x * NW + w) * 16 * RT;
+  const char* set = a.f.set(h);
+  const float* scales = (const float*)(set + a.f.p.off_scale[0]);
+  const size_t st = (size_t)max(slot, 0) * a.Hk + h;
+
+  RowOps<W, XP, RT, FULL> x;
+  x.load(a.x, b, h, v0, rows, len, steps, lane);
+  float ref[RT], den[RT][1];
+  f32x4 acc[RT][VT], none[RT][1];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    ref[rt] = 0.f;
+    den[rt][0] = 0.f;
+#pragma unroll
+    for (int vt = 0; vt < VT; ++vt) acc[rt][vt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    none[rt][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (slot >= 0)
+    walk_features<W, P, 0, NW, FULL, DIRECT>(
+        a.f, 0, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
+        [&](const StateLds<W, P>& l, const Weights<W, 0>& weights, bool first) {
+          f32x4 E[RT][2];
+          exponents(x, weights, steps, lane, E);
+          const float scale = scales[weights.fb];
+          f32x4 bias[2], zf[2];
+#pragma unroll
+          for (int ft = 0; ft < 2; ++ft) {
+            bias[ft] = *(const f32x4*)&l.bias[16 * ft + 4 * g];
+            zf[ft] = *(const f32x4*)&l.z[16 * ft + 4 * g];
+          }
+          Op<P> po[RT];
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const float undo = x.undo[rt] * scale;
+#pragma unroll
+            for (int ft = 0; ft < 2; ++ft) E[rt][ft] = E[rt][ft] * undo + (bias[ft] - ref[rt]);
+            raise(first, E[rt], ref[rt], den[rt], acc, none, rt, lane);
+            f32x8 p;
+#pragma unroll
+            for (int ft = 0; ft < 2; ++ft)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                p[4 * ft + r] = fast_exp2(E[rt][ft][r]);
+                den[rt][0] += p[4 * ft + r] * zf[ft][r];
+              }
+            po[rt] = as_op<P>(p);
+          }
+#pragma unroll
+          for (int vt = 0; vt < VT; ++vt)
+            if (FULL || 16 * vt < dv) {
+              const Op<P> t = column_op<P>(&l.t[0][0][16 * vt] + lane_tr(lane, LD), LD, 32 * LD);
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt) acc[rt][vt] = times(po[rt], t, acc[rt][vt]);
+            }
+        });
+  float factor[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    den[rt][0] = over_groups_sum(den[rt][0]);
+    factor[rt] = 1.f;
+  }
+  if constexpr (DIRECT) {
+    __syncthreads();       // (the waves' states in LDS make room for their sums)
+    meet<NW, RT, 1>(ref, den, factor, red, slot >= 0 && w < a.f.p.Mp / 32, w, lane);
+  }
   int unread = 0;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    den[rt] += __shfl_xor(den[rt], 16);
-    den[rt] += __shfl_xor(den[rt], 32);
-    const int v = v0 + 16 * rt + c;
-    float factor;
-    if (a.mode == OUT_SUM) factor = ref[rt] == kNone ? 0.f : fast_exp2(ref[rt]);
-    else factor = den[rt] == 0.f ? 0.f : 1.f / den[rt];
-    unread += g == 0 && live[rt] && den[rt] == 0.f;
-    if (a.mode == OUT_STATS) {
-      const float inv = factor;
-      float delta[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool zero = den[rt][0] == 0.f;
+    unread += (lane < 16) && (!DIRECT || w == 0) && x.live[rt] && zero;
+    // (a quotient whose divisor is subnormal has no inverse)
+    const f32x4 k = by_row(zero ? 0.f : DIRECT ? factor[rt] : 1.f, lane), d4 = by_row(zero ? 1.f : den[rt][0], lane);
+    float* tile = (float*)lds + (DIRECT ? (size_t)w * RT + rt : (size_t)w) * 16 * (W + 4);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int vr = v0 + 16 * rt + 4 * g + r;
-        const RowAt at = row_at(a.x, min(vr, rows - 1));
-        if (vr < rows && at.row < len) {
-          const long long base = row_base(a.dY, b, h * a.x.G + at.head, at.row);
-#pragma unroll
-          for (int vt = 0; vt < VT; ++vt)
-            if (16 * vt + c < dv) delta[r] += acc[rt][vt][r] * load_elem(a.dY, base + 16 * vt + c);
-        }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) delta[r] += __shfl_xor(delta[r], o);
-        delta[r] *= __shfl(inv, 4 * g + r);
-        if (c == 0 && vr < rows) a.weights[(size_t)bh * rows + vr] = -delta[r];
+    for (int vt = 0; vt < VT; ++vt) acc[rt][vt] /= d4;
+    tile_to_lds<W>(tile, acc[rt], k, lane);
+    if constexpr (!DIRECT) {
+      wave_fence();
+      for (int u = lane; u < 16 * (W / 8); u += 64) {
+        const int r = u / (W / 8), c0 = 8 * (u % (W / 8)), vr = v0 + 16 * rt + r;
+        if (vr >= rows || (!FULL && c0 >= dv)) continue;
+        const RowAt at = row_at(a.x, vr);
+        f32x8 y = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (at.row < len) y = from_tile<W>(tile + r * (W + 4), c0);
+        store8(a.Y, row_base(a.Y, b, h * a.x.G + at.head, at.row), c0, dv, y);
       }
-      if (g == 0 && v < rows) a.lse[(size_t)bh * rows + v] = live[rt] && den[rt] != 0.f ? -(ref[rt] + __log2f(den[rt])) : kNone;
-      continue;
+      wave_fence();
     }
-    f32x4 k;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) k[r] = __shfl(factor, 4 * g + r);
-#pragma unroll
-    for (int vt = 0; vt < VT; ++vt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) acc[rt][vt][r] *= k[r];
-    tile_to_lds<W>(tile, acc[rt], lane);
-    for (int u = lane; u < 16 * (W / 8); u += 64) {
-      const int r = u / (W / 8), c0 = 8 * (u % (W / 8)), vr = v0 + 16 * rt + r;
-      if (vr >= rows || c0 >= dv) continue;
+  }
+  if constexpr (DIRECT) {
+    __syncthreads();
+    for (int u = tid; u < 16 * RT * (W / 8); u += 64 * NW) {
+      const int r = u / (W / 8), c0 = 8 * (u % (W / 8)), vr = v0 + r;
+      if (vr >= rows || (!FULL && c0 >= dv)) continue;
       const RowAt at = row_at(a.x, vr);
-      f32x8 y;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = tile[r * (W + 4) + c0 + i];
-      if (at.row >= len) y = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      store8(a.out, row_base(a.out, b, h * a.x.G + at.head, at.row), c0, dv, y);
+      f32x8 y = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (at.row < len)
+        for (int i = 0; i < NW; ++i) y += from_tile<W>((const float*)lds + (size_t)(i * 16 * RT + r) * (W + 4), c0);
+      store8(a.Y, row_base(a.Y, b, h * a.x.G + at.head, at.row), c0, dv, y);
     }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
   }
   if (a.unread != nullptr) {
 #pragma unroll
@@ -273,174 +425,202 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   }
 }
 
-template <int W, int XP, int RP, int NW, int RT>
+// Gradients.  KEYS = false: with p relative to a row's reference, u = p (dY . T + 0) and p z against W in two sums, of which, with the row's
+// normaliser and delta = sum u / sum p z, dx = (first - delta second) / normaliser.  KEYS = true: the features are those the state has
+// (terms hold its shift): u = s (r . T + z) against W, s against T.
+template <int W, int XP, int RP, int P, int NW, int RT, bool FULL, bool DIRECT, bool KEYS>
 __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
-  constexpr int S = STEPS<W>, CT = TILES<W>;
-  extern __shared__ __align__(16) char lds_raw[];
-  StepLds<W, true>* lds = (StepLds<W, true>*)lds_raw;
+  constexpr int S = STEPS<W>, CT = TILES<W>, LD = W + 8, TP = KEYS ? P : 3;       // (delta enters a sum of the state's gradient: 24 bits)
+  extern __shared__ __align__(16) char lds[];
+  __shared__ float red[DIRECT ? 3 * RT * NW * 16 : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, steps = a.f.p.steps, dv = a.dv, nfb = a.f.p.Mp / 32, d = a.f.d;
-  const int slot = slot_of(a.slots, a.state.slots, b);
-  const int len = length_of(a.x, b), rows = a.x.L * a.x.G;
-  const int v0 = (blockIdx.x * NW + w) * 16 * RT;
+  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv, d = FULL ? W : a.f.d;
+  const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
+  const int v0 = (DIRECT ? blockIdx.x : blockIdx.x * NW + w) * 16 * RT;
   const char* set = a.f.set(h);
+  const float* scales = (const float*)(set + a.f.p.off_scale[KEYS]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
 
-  Op<XP> x[RT][S];
+  RowOps<W, XP, RT, FULL> x;
+  x.load(a.x, b, h, v0, rows, len, steps, lane);
   Op<RP> rr[RT][S];
-  float term[RT], weight[RT], rho[RT];
-  f32x4 acc[RT][CT];
+  float ref[RT], term[RT], sums[RT][2];            // queries: normaliser, sum u; keys: -, sum u
+  f32x4 acc[RT][CT], more[RT][CT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int v = v0 + 16 * rt + c;
-    const RowAt at = row_at(a.x, min(v, rows - 1));
-    const bool live = slot >= 0 && v < rows && at.row < len;
-    term[rt] = kNone;
-    weight[rt] = rho[rt] = 0.f;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      if (s < steps) {
-        f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) n = row8(a.x, b, h, at, 32 * s + 8 * g);
-        x[rt][s] = as_op<XP>(n);
-      }
-      if (32 * s < dv) {
-        f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) n = row8(a.r, b, h, at, 32 * s + 8 * g);
-        rr[rt][s] = as_op<RP>(n);
-      }
+      f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (x.live[rt] && (FULL || 32 * s < dv)) n = row8<FULL, false>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
+      rr[rt][s] = as_op<RP>(n);
     }
-    if (live) {
-      term[rt] = a.terms[(size_t)bh * rows + v];
-      weight[rt] = a.weights ? a.weights[(size_t)bh * rows + v] : 1.f;
-    }
+    term[rt] = KEYS ? (x.live[rt] && slot >= 0 ? a.terms[(size_t)bh * rows + v0 + 16 * rt + c] : kNone) : 0.f;
+    ref[rt] = sums[rt][0] = sums[rt][1] = 0.f;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) acc[rt][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int ct = 0; ct < CT; ++ct) acc[rt][ct] = more[rt][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (slot >= 0) {
-    Stage<W, true, NW> stage;
-    stage.start(a.f, a.side, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv);
-    stage.fetch(0, tid);
-    stage.put(lds[0], tid);
-    __syncthreads();
-    for (int fb = 0; fb < nfb; ++fb) {
-      const StepLds<W, true>& l = lds[fb & 1];
-      const bool more = fb + 1 < nfb;
-      if (more) stage.fetch(fb + 1, tid);
-      f32x4 E[RT][2], P[RT][2];
+  if (slot >= 0)
+    walk_features<W, TP, P, NW, FULL, DIRECT>(
+        a.f, KEYS, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
+        [&](const StateLds<W, TP>& l, const Weights<W, P>& weights, bool first) {
+          f32x4 E[RT][2], D[RT][2];
+          exponents(x, weights, steps, lane, E);
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) E[rt][0] = E[rt][1] = P[rt][0] = P[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < S; ++s)
-        if (s < steps)
-#pragma unroll
-          for (int ft = 0; ft < 2; ++ft) {
-            Op<3> wo;
-#pragma unroll
-            for (int p = 0; p < 3; ++p) wo.p[p] = *(const bf16x8*)&l.row[0][0][(s * 3 + p) * 1024 + ft * 512 + lane * 8];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) E[rt][ft] = times(wo, x[rt][s], E[rt][ft]);
-          }
-#pragma unroll
-      for (int s = 0; s < S; ++s)
-        if (32 * s < dv)
-#pragma unroll
-          for (int ft = 0; ft < 2; ++ft) {
-            const Op<3> t = row_op<3>(&l.t[0][16 * ft + c][32 * s + 8 * g], 32 * (W + 8));
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) P[rt][ft] = times(t, rr[rt][s], P[rt][ft]);
-          }
-      Op<3> uo[RT];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        f32x8 u;
-#pragma unroll
-        for (int ft = 0; ft < 2; ++ft) {
-          const f32x4 bias = *(const f32x4*)&l.bias[16 * ft + 4 * g], zf = *(const f32x4*)&l.z[16 * ft + 4 * g];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = fast_exp2((E[rt][ft][r] + bias[r]) + term[rt]);
-            u[4 * ft + r] = p * (P[rt][ft][r] + weight[rt] * zf[r]);
-            rho[rt] += u[4 * ft + r];
-          }
-        }
-        uo[rt] = as_op<3>(u);
-      }
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-        if (16 * ct < d) {
-          const Op<3> wo = image_op<3>(&l.col[ct][0][0], lane);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][ct] = times(uo[rt], wo, acc[rt][ct]);
-        }
-      if (more) stage.put(lds[(fb + 1) & 1], tid);
-      __syncthreads();
-    }
-  }
-  float* tile = (float*)lds_raw + w * 16 * (W + 4);
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    rho[rt] += __shfl_xor(rho[rt], 16);
-    rho[rt] += __shfl_xor(rho[rt], 32);
-    f32x4 rho_row;                   // of row 4 g + r, with the factor of the row term's gradient
-#pragma unroll
-    for (int r = 0; r < 4; ++r) rho_row[r] = __shfl(rho[rt], 4 * g + r) * a.f.scale2;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-      if (16 * ct < d) {
-        acc[rt][ct] *= kLn2;
-        if (a.side == 1 && a.f.dense) {
-          f32x4 q = {0.f, 0.f, 0.f, 0.f};
-          const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 3 * 512;
+          for (int rt = 0; rt < RT; ++rt) D[rt][0] = D[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int s = 0; s < S; ++s)
-            if (s < steps) q = times(x[rt][s], image_op<3>(img + s * 3 * 512, lane), q);
+            if (FULL || 32 * s < dv)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[rt][ct][r] += rho_row[r] * q[r];
-        }
-      }
-    tile_to_lds<W>(tile, acc[rt], lane);
-    for (int u = lane; u < 16 * (W / 8); u += 64) {
-      const int r = u / (W / 8), c0 = 8 * (u % (W / 8)), vr = v0 + 16 * rt + r;
-      const float rho_r = __shfl(rho[rt], r & 15) * a.f.scale2;      // (every lane takes part: 16 W / 8 units are whole waves or W = 32's one)
-      if (vr >= rows || c0 >= d) continue;
+              for (int ft = 0; ft < 2; ++ft) {
+                const Op<TP> t = row_op<TP>(&l.t[0][16 * ft + c][32 * s + 8 * g], 32 * LD);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) D[rt][ft] = times(t, rr[rt][s], D[rt][ft]);
+              }
+          const float scale = scales[weights.fb];
+          f32x4 bias[2], zf[2];
+#pragma unroll
+          for (int ft = 0; ft < 2; ++ft) {
+            bias[ft] = *(const f32x4*)&l.bias[16 * ft + 4 * g];
+            zf[ft] = *(const f32x4*)&l.z[16 * ft + 4 * g];
+          }
+          Op<P> uo[RT], so[RT];
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const float undo = x.undo[rt] * scale;
+#pragma unroll
+            for (int ft = 0; ft < 2; ++ft) E[rt][ft] = E[rt][ft] * undo + (KEYS ? bias[ft] + term[rt] : bias[ft] - ref[rt]);
+            if constexpr (!KEYS) raise(first, E[rt], ref[rt], sums[rt], acc, more, rt, lane);
+            f32x8 u, s;
+#pragma unroll
+            for (int ft = 0; ft < 2; ++ft)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float p = fast_exp2(E[rt][ft][r]);
+                u[4 * ft + r] = p * (KEYS ? D[rt][ft][r] + zf[ft][r] : D[rt][ft][r]);
+                s[4 * ft + r] = KEYS ? p : p * zf[ft][r];
+                sums[rt][1] += u[4 * ft + r];
+                if constexpr (!KEYS) sums[rt][0] += s[4 * ft + r];
+              }
+            uo[rt] = as_op<P>(u);
+            so[rt] = as_op<P>(s);
+          }
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            if (FULL || 16 * ct < d) {
+              const Op<P> wo = weights.col(ct, lane);
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt) {
+                acc[rt][ct] = times(uo[rt], wo, acc[rt][ct]);
+                if constexpr (!KEYS) more[rt][ct] = times(so[rt], wo, more[rt][ct]);
+              }
+            }
+            if constexpr (KEYS)
+              if (FULL || 16 * ct < dv) {
+                const Op<P> t = column_op<P>(&l.t[0][0][16 * ct] + lane_tr(lane, LD), LD, 32 * LD);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) more[rt][ct] = times(so[rt], t, more[rt][ct]);
+              }
+          }
+        });
+  float factor[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    sums[rt][0] = over_groups_sum(sums[rt][0]);
+    sums[rt][1] = over_groups_sum(sums[rt][1]);
+    factor[rt] = 1.f;
+  }
+  if constexpr (DIRECT) {
+    __syncthreads();
+    meet<NW, RT, 2>(ref, sums, factor, red, slot >= 0 && w < a.f.p.Mp / 32, w, lane);
+  }
+  float* tiles = (float*)lds;
+  // out (of n numbers a row) from the tiles: row r of the workgroup's, or of the wave's, rows
+  auto store = [&](const TensorDev& out, int n, int rt, const Turn* turn, auto&& finish) {
+    const float* tile = tiles + (DIRECT ? 0 : (size_t)w * 16 * (W + 4));
+    for (int u = DIRECT ? tid : lane; u < 16 * (DIRECT ? RT : 1) * (W / 8); u += DIRECT ? 64 * NW : 64) {
+      const int r = u / (W / 8), c0 = 8 * (u % (W / 8)), vr = v0 + (DIRECT ? 0 : 16 * rt) + r;
+      if (vr >= rows || (!FULL && c0 >= n)) continue;
       const RowAt at = row_at(a.x, vr);
-      const long long base = row_base(a.dx, b, h * a.x.G + at.head, at.row);
       f32x8 y = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (slot >= 0 && at.row < len) {
-        if (a.side == 1 && !a.f.dense) {       // C2 + C2' = -I, onto the tile itself: the numbers of a pair meet when they are turned back
-          const f32x8 xs = row8(a.x, b, h, at, c0);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) tile[r * (W + 4) + c0 + i] -= rho_r * xs[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = tile[r * (W + 4) + c0 + i];
-      }
-      if (a.x.turn.rot == 0) store8(a.dx, base, c0, d, y);
+      if (slot >= 0 && at.row < len) y = finish(tile, r, at, c0, turn);
+      store8(out, row_base(out, b, h * a.x.G + at.head, at.row), c0, n, y);
     }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
-    if (a.x.turn.rot > 0)
-      for (int u = lane; u < 16 * (W / 8); u += 64) {
-        const int r = u / (W / 8), c0 = 8 * (u % (W / 8)), vr = v0 + 16 * rt + r;
-        if (vr >= rows || c0 >= d) continue;
-        const RowAt at = row_at(a.x, vr);
-        f32x8 y = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (slot >= 0 && at.row < len) {
-          const float* q = tile + r * (W + 4);
-          auto eight = [&](int col) {
-            f32x8 e;
+  };
+  auto sum_of = [&](const float* tile, int r, int c0) {
+    f32x8 y = from_tile<W>(tile + r * (W + 4), c0);
+    if constexpr (DIRECT)
+      for (int i = 1; i < NW; ++i) y += from_tile<W>(tile + (size_t)(i * 16 * RT + r) * (W + 4), c0);
+    return y;
+  };
+  auto turned_back = [&](const float* tile, int r, RowAt at, int c0, const Turn* turn) {
+    const f32x8 y = sum_of(tile, r, c0);
+    if (XP == 1 || turn == nullptr || turn->rot == 0) return y;
+    const float2* cs = turn->table + ((long long)b * a.x.L + at.row) * (turn->rot >> 1);
+    return turned8(y, c0, *turn, cs, -1.f,
+                   [&](int col) {
+                     float q = tile[r * (W + 4) + col];
+                     if constexpr (DIRECT)
+                       for (int i = 1; i < NW; ++i) q += tile[(size_t)(i * 16 * RT + r) * (W + 4) + col];
+                     return q;
+                   },
+                   [&](int col) { return sum_of(tile, r, col); });
+  };
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = q[col + i];
-            return e;
-          };
-          const float2* cs = a.x.turn.table + ((long long)b * a.x.L + at.row) * (a.x.turn.rot >> 1);
-          y = turned8(eight(c0), c0, a.x.turn, cs, -1.f, [&](int col) { return q[col]; }, eight);
+  for (int part = 0; part < (KEYS ? 2 : 1); ++part) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float* tile = tiles + (DIRECT ? (size_t)w * RT + rt : (size_t)w) * 16 * (W + 4);
+      if (part == 1) {
+        tile_to_lds<W>(tile, more[rt], f32x4{1.f, 1.f, 1.f, 1.f}, lane);
+      } else if constexpr (KEYS) {
+        // the row term: (sum u) s^2 (C2 + C2') x, by the first wave where several have a part of the features
+        const float rho = !DIRECT || w == 0 ? sums[rt][1] * a.f.scale2 : 0.f;
+        const f32x4 rho4 = by_row(rho * x.undo[rt], lane);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+          if (FULL || 16 * ct < d) {
+            acc[rt][ct] *= kLn2;
+            if (!DIRECT || w == 0) {
+              f32x4 q = {0.f, 0.f, 0.f, 0.f};
+              const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 2 * 512;
+#pragma unroll
+              for (int s = 0; s < S; ++s)
+                if (FULL || s < steps) {
+                  Op16<2> co;
+#pragma unroll
+                  for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
+                  q = times16(x.x[rt][s], co, q);
+                }
+              acc[rt][ct] += (rho4 * *(const float*)(set + a.f.p.off_cscale)) * q;
+            }
+          }
+        tile_to_lds<W>(tile, acc[rt], f32x4{1.f, 1.f, 1.f, 1.f}, lane);
+      } else {
+        const bool zero = sums[rt][0] == 0.f;
+        const float inv = zero ? 0.f : 1.f / sums[rt][0], delta = zero ? 0.f : sums[rt][1] / sums[rt][0];
+        const int v = v0 + 16 * rt + c;
+        if (lane < 16 && v < rows && (!DIRECT || w == 0)) {
+          a.lse[(size_t)bh * rows + v] = x.live[rt] && slot >= 0 && !zero ? -(ref[rt] + __log2f(sums[rt][0])) : kNone;
+          a.weights[(size_t)bh * rows + v] = -delta;
         }
-        store8(a.dx, row_base(a.dx, b, h * a.x.G + at.head, at.row), c0, d, y);
+        const f32x4 d4 = by_row(delta, lane);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) acc[rt][ct] -= d4 * more[rt][ct];
+        tile_to_lds<W>(tile, acc[rt], by_row(kLn2 * inv * factor[rt], lane), lane);
       }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
+      if constexpr (!DIRECT) {
+        wave_fence();
+        if (part == 0) store(a.dx, d, rt, &a.x.turn, turned_back);
+        else store(a.dr, dv, rt, nullptr, turned_back);
+        wave_fence();
+      }
+    }
+    if constexpr (DIRECT) {
+      __syncthreads();
+      if (part == 0) store(a.dx, d, 0, &a.x.turn, turned_back);
+      else store(a.dr, dv, 0, nullptr, turned_back);
+      __syncthreads();
+    }
   }
 }
 
@@ -451,53 +631,69 @@ int lds_room(const void* kernel, size_t lds) {
   }
   return 0;
 }
-template <int W, int XP, int NW> int values(const ValueArgs& a, hipStream_t st) {
-  constexpr size_t lds = 2 * sizeof(StepLds<W, false>);
-  static_assert(lds >= sizeof(float) * NW * 16 * (W + 4), "the waves' tiles of output rows");
-  auto kernel = k_values<W, XP, NW>;
+// Few rows: fewer workgroups of 256 than CUs would have.
+bool few_rows(int BH, long long rows) { return BH * ((rows + 255) / 256) < 192; }
+
+template <int W, int XP, int P, bool FULL, bool DIRECT> int values(const ValueArgs& a, hipStream_t st) {
+  constexpr int NW = DIRECT && W == 128 ? 4 : 8, RT = 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr size_t lds = rows_lds<W, P, 0, NW, RT, DIRECT>();
+  static_assert(lds <= 156 * 1024, "LDS of a CU");
+  auto kernel = k_values<W, XP, P, NW, RT, FULL, DIRECT>;
   if (int rc = lds_room((const void*)kernel, lds)) return rc;
-  hipLaunchKernelGGL(kernel, dim3((a.x.L * a.x.G + 32 * NW - 1) / (32 * NW), a.B * a.Hk), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3((a.x.L * a.x.G + ROWS - 1) / ROWS, a.B * a.Hk), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int W, int XP> int values_nw(const ValueArgs& a, hipStream_t st) {
-  return a.x.L * a.x.G > 128 ? values<W, XP, 8>(a, st) : values<W, XP, 4>(a, st);
+template <int W, int XP, int P, bool FULL> int values_rows(const ValueArgs& a, hipStream_t st) {
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G) ? values<W, XP, P, FULL, true>(a, st) : values<W, XP, P, FULL, false>(a, st);
 }
-template <int W> int values_pieces(const ValueArgs& a, hipStream_t st) {
-  return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? values_nw<W, 1>(a, st) : values_nw<W, 3>(a, st);
+template <int W, bool FULL> int values_pieces(const ValueArgs& a, hipStream_t st) {
+  if (a.Y.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? values_rows<W, 1, 2, FULL>(a, st) : values_rows<W, 2, 2, FULL>(a, st);
+  return values_rows<W, 2, 3, FULL>(a, st);
 }
-template <int W, int XP, int RP, int NW> int grads(const GradArgs& a, hipStream_t st) {
-  constexpr size_t lds = 2 * sizeof(StepLds<W, true>);
-  constexpr int RT = W == 128 ? 1 : 2;
-  static_assert(lds >= sizeof(float) * NW * 16 * (W + 4) && lds <= 160 * 1024, "the waves' tiles of output rows; LDS of a CU");
-  auto kernel = k_grads<W, XP, RP, NW, RT>;
+template <int W> int values_width(const ValueArgs& a, hipStream_t st) {
+  return a.f.d == W && a.dv == W ? values_pieces<W, true>(a, st) : values_pieces<W, false>(a, st);
+}
+
+template <int W, int XP, int RP, int P, bool FULL, bool DIRECT, bool KEYS> int grads(const GradArgs& a, hipStream_t st) {
+  constexpr int NW = DIRECT && W == 128 ? 4 : 8, RT = W == 128 ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr size_t lds = rows_lds<W, KEYS ? P : 3, P, NW, RT, DIRECT>();
+  static_assert(lds <= 156 * 1024, "LDS of a CU");
+  auto kernel = k_grads<W, XP, RP, P, NW, RT, FULL, DIRECT, KEYS>;
   if (int rc = lds_room((const void*)kernel, lds)) return rc;
-  hipLaunchKernelGGL(kernel, dim3((a.x.L * a.x.G + 16 * RT * NW - 1) / (16 * RT * NW), a.B * a.Hk), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3((a.x.L * a.x.G + ROWS - 1) / ROWS, a.B * a.Hk), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int W, int XP, int RP> int grads_nw(const GradArgs& a, hipStream_t st) {
-  return a.x.L * a.x.G > 128 ? grads<W, XP, RP, 8>(a, st) : grads<W, XP, RP, 4>(a, st);
+template <int W, int XP, int RP, int P, bool FULL, bool KEYS> int grads_rows(const GradArgs& a, hipStream_t st) {
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G) ? grads<W, XP, RP, P, FULL, true, KEYS>(a, st) : grads<W, XP, RP, P, FULL, false, KEYS>(a, st);
 }
-template <int W> int grads_pieces(const GradArgs& a, hipStream_t st) {
-  if (a.r.X.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? grads_nw<W, 1, 1>(a, st) : grads_nw<W, 3, 1>(a, st);
-  return grads_nw<W, 3, 3>(a, st);
+template <int W, bool FULL, bool KEYS> int grads_pieces(const GradArgs& a, hipStream_t st) {
+  const bool two = a.dx.dtype == 1 && (!KEYS || a.dr.dtype == 1);
+  if (a.r.X.dtype == 1 && a.x.X.dtype == 1 && two)
+    return a.x.turn.rot == 0 ? grads_rows<W, 1, 1, 2, FULL, KEYS>(a, st) : grads_rows<W, 2, 1, 2, FULL, KEYS>(a, st);
+  return grads_rows<W, 2, 3, 3, FULL, KEYS>(a, st);
+}
+template <int W, bool KEYS> int grads_width(const GradArgs& a, hipStream_t st) {
+  return a.f.d == W && a.dv == W ? grads_pieces<W, true, KEYS>(a, st) : grads_pieces<W, false, KEYS>(a, st);
+}
+template <bool KEYS> int grads_any(const GradArgs& a, hipStream_t st) {
+  switch (width_class(a.f.d, a.dv)) {
+    case 32: return grads_width<32, KEYS>(a, st);
+    case 64: return grads_width<64, KEYS>(a, st);
+    default: return grads_width<128, KEYS>(a, st);
+  }
 }
 
 }  // namespace
 
 int launch_values(const ValueArgs& a, hipStream_t st) {
   switch (width_class(a.f.d, a.dv)) {
-    case 32: return values_pieces<32>(a, st);
-    case 64: return values_pieces<64>(a, st);
-    default: return values_pieces<128>(a, st);
+    case 32: return values_width<32>(a, st);
+    case 64: return values_width<64>(a, st);
+    default: return values_width<128>(a, st);
   }
 }
-int launch_grads(const GradArgs& a, hipStream_t st) {
-  switch (width_class(a.f.d, a.dv)) {
-    case 32: return grads_pieces<32>(a, st);
-    case 64: return grads_pieces<64>(a, st);
-    default: return grads_pieces<128>(a, st);
-  }
-}
+int launch_query_grads(const GradArgs& a, hipStream_t st) { return grads_any<false>(a, st); }
+int launch_key_grads(const GradArgs& a, hipStream_t st) { return grads_any<true>(a, st); }
 
 }  // namespace st
 }  // namespace fs

@@ -57,12 +57,19 @@ SumPlan plan_sum(int BH, long long tokens, long long rows, int d, int dv, int M,
   SumPlan p;
   const int Mp = (M + 31) / 32 * 32, waves = Mp > 128 ? 8 : 4;
   p.nblock = ceil_div(Mp / 32, waves);
-  // a workgroup for every CU, from 64 rows a split on; a split costs a state written and read again
-  const long long want = std::max<long long>(1, 512 / ((long long)BH * p.nblock));
-  const long long most = std::min<long long>({(rows + 63) / 64, 64, 4096 / (Mp / 32)});
-  long long n = std::max<long long>(1, std::min(want, most));
-  p.rows_per_split = (int)(((rows + n - 1) / n + 31) / 32 * 32);
-  p.nsplit = std::max(1, (int)((rows + p.rows_per_split - 1) / std::max(1, p.rows_per_split)));
+  // splits of the rows: passes of 256 workgroups, each its start and its chunks of 32 rows, and a partial state written and read for
+  // every split (measured, us: a chunk of 64 numbers a row 1, of 128 2.5; a start 5; 4 TB/s)
+  const int wide = d > 64 || dv > 64;
+  const long long chunks = std::max<long long>(1, (rows + 31) / 32), most = std::min<long long>({chunks, 64, 4096 / (Mp / 32)});
+  double best = 0.0;
+  long long n = 1;
+  for (long long k = 1; k <= most; ++k) {
+    const long long per = (chunks + k - 1) / k, used = (chunks + per - 1) / per, passes = (BH * used * p.nblock + 255) / 256;
+    const double us = (double)passes * (5.0 + (double)per * (wide ? 2.5 : 1.0)) + (double)BH * used * M * (dv + 1) * 8 / 4e6;
+    if (k == 1 || us < best) { best = us; n = used; }
+  }
+  p.rows_per_split = (int)((chunks + n - 1) / n * 32);
+  p.nsplit = (int)n;
   size_t off = 0;
   p.off_table = off; off = align_up(off + (size_t)tokens * (rot / 2) * sizeof(float2));
   p.off_terms = off; off = align_up(off + (terms ? (size_t)BH * rows * sizeof(float) : 0));
@@ -226,14 +233,12 @@ int favorsharp_state_attention(const fs_features* f, const fs_state* state, cons
   hipStream_t s = (hipStream_t)stream;
   st::ValueArgs a{};
   a.f = features_of(f);
-  a.side = 0;
-  a.mode = st::OUT_QUOTIENT;
   a.x = st::Rows{dev(Q), L, H / f->heads, lengths, f->d, st::Turn{}};
   if (int rc = turn_of(rot, B, L, (char*)workspace, p.off_table, &a.x.turn, s)) return rc;
   a.slots = slots;
   a.state = state_of(state);
   a.B = B; a.Hk = f->heads; a.dv = dv;
-  a.out = dev(Y);
+  a.Y = dev(Y);
   a.unread = unread;
   return st::launch_values(a, s);
 }
@@ -272,34 +277,31 @@ int favorsharp_state_attention_backward(const fs_features* f, const fs_state* st
   hipStream_t s = (hipStream_t)stream;
   char* ws = (char*)workspace;
   const int G = H / f->heads;
-  // normalisers and dY . Y of every row, then its gradient, then the state's
-  st::ValueArgs v{};
-  v.f = features_of(f);
-  v.side = 0;
-  v.mode = st::OUT_STATS;
-  v.x = st::Rows{dev(Q), L, G, lengths, f->d, st::Turn{}};
-  v.slots = slots;
-  v.state = state_of(state);
-  v.B = B; v.Hk = f->heads; v.dv = dv;
-  v.dY = dev(dY);
-  v.lse = (float*)(ws + p.off_terms);
-  v.weights = (float*)(ws + p.off_weights);
+  // the rows' gradients with their normalisers and dY . Y, then the states'
+  st::GradArgs g{};
+  g.f = features_of(f);
+  g.x = st::Rows{dev(Q), L, G, lengths, f->d, st::Turn{}};
+  g.r = st::Rows{dev(dY), L, G, lengths, dv, st::Turn{}};
+  g.lse = (float*)(ws + p.off_terms);
+  g.weights = (float*)(ws + p.off_weights);
+  g.slots = slots;
+  g.state = state_of(state);
+  g.B = B; g.Hk = f->heads; g.dv = dv;
+  g.dx = dev(dQ);
+  if (L > 0) {
+    if (int rc = turn_of(rot, B, L, ws, p.off_table, &g.x.turn, s)) return rc;
+    if (int rc = st::launch_query_grads(g, s)) return rc;
+  }
   st::BuildArgs a{};
-  a.f = v.f;
+  a.f = g.f;
   a.side = 0;
-  a.v = st::Rows{dev(dY), L, G, lengths, dv, st::Turn{}};
-  a.terms = v.lse; a.weights = v.weights;
+  a.x = g.x;
+  a.v = g.r;
+  a.terms = g.lse; a.weights = g.weights;
   a.slots = slots; a.nslots = state->slots;
   a.B = B; a.Hk = f->heads; a.dv = dv;
   a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split; a.nblock = p.nblock;
   a.part = (float*)(ws + p.off_part); a.zpart = (float*)(ws + p.off_zpart); a.refs = (float2*)(ws + p.off_refs);
-  if (L > 0) {
-    if (int rc = turn_of(rot, B, L, ws, p.off_table, &v.x.turn, s)) return rc;
-    if (int rc = st::launch_values(v, s)) return rc;
-    st::GradArgs g{v.f, 0, v.x, a.v, v.lse, v.weights, slots, state_of(state), B, f->heads, dv, dev(dQ)};
-    if (int rc = st::launch_grads(g, s)) return rc;
-  }
-  a.x = v.x;
   if (int rc = st::launch_build(a, s)) return rc;
   st::JoinArgs j{a.part, a.zpart, a.refs, nullptr, slots, state_of(dstate), B, f->heads, f->M, a.f.p.Mp, dv, p.nsplit, nullptr};
   return st::launch_join_sum(j, s);
@@ -325,22 +327,19 @@ int favorsharp_state_append_backward(const fs_features* f, const fs_state* state
   hipStream_t s = (hipStream_t)stream;
   char* ws = (char*)workspace;
   float* terms = (float*)(ws + p.off_terms);
-  st::ValueArgs v{};
-  v.f = features_of(f);
-  v.side = 1;
-  v.mode = st::OUT_SUM;
-  v.x = st::Rows{dev(K), L, 1, lengths, f->d, st::Turn{}};
-  if (int rc = turn_of(rot, B, L, ws, p.off_table, &v.x.turn, s)) return rc;
-  if (int rc = st::launch_row_terms(v.f, v.x, B, f->heads, state->shift, slots, state->slots, terms, s)) return rc;
-  v.terms = terms;
-  v.slots = slots;
-  v.state = state_of(dstate);
-  v.state.z = nullptr;
-  v.B = B; v.Hk = f->heads; v.dv = dv;
-  v.out = dev(dV);
-  if (int rc = st::launch_values(v, s)) return rc;
-  st::GradArgs g{v.f, 1, v.x, st::Rows{dev(V), L, 1, lengths, dv, st::Turn{}}, terms, nullptr, slots, state_of(dstate), B, f->heads, dv, dev(dK)};
-  return st::launch_grads(g, s);
+  st::GradArgs g{};
+  g.f = features_of(f);
+  g.x = st::Rows{dev(K), L, 1, lengths, f->d, st::Turn{}};
+  g.r = st::Rows{dev(V), L, 1, lengths, dv, st::Turn{}};
+  if (int rc = turn_of(rot, B, L, ws, p.off_table, &g.x.turn, s)) return rc;
+  if (int rc = st::launch_row_terms(g.f, g.x, B, f->heads, state->shift, slots, state->slots, terms, s)) return rc;
+  g.terms = terms;
+  g.slots = slots;
+  g.state = state_of(dstate);
+  g.B = B; g.Hk = f->heads; g.dv = dv;
+  g.dx = dev(dK);
+  g.dr = dev(dV);
+  return st::launch_key_grads(g, s);
 }
 
 }  // extern "C"

@@ -22,12 +22,15 @@ template <int W> constexpr int TILES = W / 16;
 inline int width_class(int d, int dv) { const int n = d > dv ? d : dv; return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
 // ---------------------------------------------------------------------------------------------- projection constants
-// One block per parameter set: operand images of W1 and W2 with the coordinates as contraction index (rows: [32 features][steps][3
-// pieces][2 tiles x 512 numbers]) and with the features as contraction index ([32 features][coordinate tiles][3][512]), those of C2 + C2', the
-// biases (-inf behind the last feature), W1 and W2 in fp32 for single tokens ([4 coordinates][features][4]), C2.
+// One block per parameter set.  Row images of W1 and W2 (the coordinates are the contraction index: [32 features][steps][2 pieces][2 tiles x
+// 512 numbers]) and C2 + C2' ([coordinate tiles][steps][2][512]) are two fp16 pieces of a number: exponents and row terms need absolute
+// accuracy only, so 22 bits of the largest number of a row or of 32 features do, and three products of pieces (two against bf16 rows) take half of
+// what bf16 pieces need.  `scale` is what a block of 32 features (or C2 + C2') was divided by, to lie below 2^14.  Column images (the features
+// are the contraction index: [32 features][coordinate tiles][3][512]) in bf16 pieces, biases (-inf behind the last feature), W1 and W2 in
+// fp32 for single tokens ([4 coordinates][features][4]), C2.
 struct FeaturePlan {
   int Mp, steps, tiles, d4;      // features in 32s, steps of 32 coordinates, tiles of 16 coordinates, coordinates in fours
-  size_t off_row[2], off_col[2], off_csym, off_bias, off_w[2], off_c2, set, total;
+  size_t off_row[2], off_scale[2], off_col[2], off_csym, off_cscale, off_bias, off_w[2], off_c2, set, total;
 };
 inline FeaturePlan feature_plan(int d, int M, int sets) {
   FeaturePlan p;
@@ -37,9 +40,11 @@ inline FeaturePlan feature_plan(int d, int M, int sets) {
   p.d4 = (d + 3) / 4;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t off = 0;
-  for (int s = 0; s < 2; ++s) { p.off_row[s] = off; off = up(off + (size_t)p.Mp * p.steps * 3 * 32 * 2); }
+  for (int s = 0; s < 2; ++s) { p.off_row[s] = off; off = up(off + (size_t)p.Mp * p.steps * 2 * 32 * 2); }
+  for (int s = 0; s < 2; ++s) { p.off_scale[s] = off; off = up(off + (size_t)p.Mp / 32 * 4); }
   for (int s = 0; s < 2; ++s) { p.off_col[s] = off; off = up(off + (size_t)p.Mp * p.steps * 3 * 32 * 2); }
-  p.off_csym = off; off = up(off + (size_t)p.tiles * p.steps * 3 * 512 * 2);
+  p.off_csym = off; off = up(off + (size_t)p.tiles * p.steps * 2 * 512 * 2);
+  p.off_cscale = off; off = up(off + 4);
   p.off_bias = off; off = up(off + (size_t)p.Mp * 4);
   for (int s = 0; s < 2; ++s) { p.off_w[s] = off; off = up(off + (size_t)p.d4 * p.Mp * 4 * 4); }
   p.off_c2 = off; off = up(off + (size_t)d * d * 4);
@@ -95,9 +100,9 @@ __device__ __forceinline__ RowAt row_at(const Rows& r, int v) {
 __device__ __forceinline__ long long row_base(const TensorDev& t, int b, int h, int row) { return b * t.sb + h * t.sh + row * t.sl; }
 
 // Eight numbers of a row from column c0 (a multiple of eight) on, zero from `cols` on.
-__device__ __forceinline__ f32x8 load8(const TensorDev& t, long long base, int c0, int cols) {
+template <bool FULL = false> __device__ __forceinline__ f32x8 load8(const TensorDev& t, long long base, int c0, int cols) {
   f32x8 x;
-  if (c0 + 8 <= cols) {
+  if (FULL || c0 + 8 <= cols) {
     if (t.dtype == 0) {
       const f32x4 a = *(const f32x4*)((const float*)t.ptr + base + c0), b = *(const f32x4*)((const float*)t.ptr + base + c0 + 4);
       x = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
@@ -170,13 +175,15 @@ __device__ __forceinline__ f32x8 turned8(f32x8 x, int c0, const Turn& t, const f
   return y;
 }
 // Numbers c0 .. c0 + 7 of row v of a state's rows, turned.
+// FULL: the row's numbers come in whole eights (cols is the kernel's width).  TURN: it may be turned at all.
+template <bool FULL, bool TURN>
 __device__ __forceinline__ f32x8 row8(const Rows& r, int b, int state_head, RowAt at, int c0) {
-  if (c0 >= r.cols) return f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (!FULL && c0 >= r.cols) return f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const long long base = row_base(r.X, b, state_head * r.G + at.head, at.row);
-  const f32x8 x = load8(r.X, base, c0, r.cols);
-  if (c0 >= r.turn.rot) return x;
+  const f32x8 x = load8<FULL>(r.X, base, c0, r.cols);
+  if (!TURN || c0 >= r.turn.rot) return x;
   const float2* cs = r.turn.table + ((long long)b * r.L + at.row) * (r.turn.rot >> 1);
-  return turned8(x, c0, r.turn, cs, 1.f, [&](int c) { return load_elem(r.X, base + c); }, [&](int c) { return load8(r.X, base, c, r.cols); });
+  return turned8(x, c0, r.turn, cs, 1.f, [&](int c) { return load_elem(r.X, base + c); }, [&](int c) { return load8<FULL>(r.X, base, c, r.cols); });
 }
 
 // ---------------------------------------------------------------------------------------------- slots
@@ -194,12 +201,25 @@ __device__ __forceinline__ int unique_slot_of(const int32_t* slots, int nslots, 
 }
 
 // ---------------------------------------------------------------------------------------------- operands
-// P pieces of an operand: 1 (a bf16 number is its own piece) or 3.
+// P bf16 pieces of an operand: 1 (a bf16 number is its own piece), 2 (16 bits: products that are rounded to bf16) or 3 (24 bits).
 template <int P> struct Op { bf16x8 p[P]; };
 template <int P> __device__ __forceinline__ Op<P> as_op(f32x8 x) {
   Op<P> o;
   if constexpr (P == 1) {
     o.p[0] = __builtin_convertvector(x, bf16x8);
+  } else if constexpr (P == 2) {
+    bf16x2_t h[4], m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x2_t v = {x[2 * i], x[2 * i + 1]};
+      h[i] = __builtin_convertvector(v, bf16x2_t);
+      m[i] = __builtin_convertvector(less_piece(v, h[i]), bf16x2_t);
+    }
+    auto join = [](const bf16x2_t (&v)[4]) {
+      return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
+                                              __builtin_bit_cast(uint32_t, v[3])});
+    };
+    o.p[0] = join(h); o.p[1] = join(m);
   } else {
     const Split3 s = split3(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
     o.p[0] = s.h; o.p[1] = s.m; o.p[2] = s.l;
@@ -212,6 +232,36 @@ template <int P> __device__ __forceinline__ Op<P> image_op(const uint16_t* img, 
   for (int i = 0; i < P; ++i) o.p[i] = *(const bf16x8*)(img + i * 512 + lane * 8);
   return o;
 }
+
+// fp16 pieces of the factors of an exponent (see FeaturePlan): 2, or 1 of a bf16 number.  The numbers of a row are multiplied by a power of
+// two first, that of up_to_2_14, so that the largest is below 2^14; what is below 2^-39 of it is lost.
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+template <int P> struct Op16 { f16x8 p[P]; };
+template <int P> __device__ __forceinline__ Op16<P> as_op16(f32x8 x) {
+  Op16<P> o;
+  o.p[0] = __builtin_convertvector(x, f16x8);
+  if constexpr (P == 2) o.p[1] = __builtin_convertvector(x - __builtin_convertvector(o.p[0], f32x8), f16x8);
+  return o;
+}
+// (2^13 <= factor * largest < 2^14; 1 where largest is zero, subnormal or not finite; the factor's inverse is a power of two, too)
+__device__ __forceinline__ float up_to_2_14(float largest) {
+  const int e = (int)(__float_as_uint(largest) >> 23 & 255u);
+  return e == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)min(max(127 + 127 + 13 - e, 1), 253) << 23);
+}
+__device__ __forceinline__ float power_inverse(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
+__device__ __forceinline__ float largest_of(f32x8 x) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
+  return m;
+}
+template <int PA, int PB>
+__device__ __forceinline__ f32x4 times16(const Op16<PA>& a, const Op16<PB>& b, f32x4 c) {
+  if constexpr (PB == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[0], b.p[1], c, 0, 0, 0);
+  if constexpr (PA == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[1], b.p[0], c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[0], b.p[0], c, 0, 0, 0);
+}
+
 template <int P> __device__ __forceinline__ Op<P> row_op(const uint16_t* s, int plane) {         // eight numbers of a row
   Op<P> o;
 #pragma unroll
@@ -245,7 +295,12 @@ __device__ __forceinline__ f32x4 times(const Op<PA>& a, const Op<PB>& b, f32x4 c
     c = mfma_bf16(a.p[1], b.p[0], c);
     c = mfma_bf16(a.p[0], b.p[1], c);
     return mfma_bf16(a.p[0], b.p[0], c);
+  } else if constexpr (PA == 2 && PB == 2) {
+    c = mfma_bf16(a.p[1], b.p[0], c);
+    c = mfma_bf16(a.p[0], b.p[1], c);
+    return mfma_bf16(a.p[0], b.p[0], c);
   } else {
+    static_assert(PA == 1 || PB == 1, "");
     constexpr int P = PA > PB ? PA : PB;
 #pragma unroll
     for (int i = P - 1; i >= 0; --i) c = mfma_bf16(a.p[PA > 1 ? i : 0], b.p[PB > 1 ? i : 0], c);
@@ -288,34 +343,31 @@ struct JoinArgs {
 int launch_join(const JoinArgs& a, hipStream_t st);
 int launch_join_sum(const JoinArgs& a, hipStream_t st);
 
-// Features of rows times a state.
-enum { OUT_QUOTIENT = 0, OUT_STATS = 1, OUT_SUM = 2 };
+// Rows against states: Y = P T / P z.
 struct ValueArgs {
   Features f;
-  int side, mode;
   Rows x;
-  const float* terms;            // [B*Hk][rows] row terms (nullptr: zero)
-  const int32_t* slots;
-  State state;                   // T and z (OUT_SUM: z is not used)
-  int B, Hk, dv;
-  TensorDev out;                 // OUT_QUOTIENT: Y; OUT_SUM: the sums
-  TensorDev dY;                  // OUT_STATS
-  float *lse, *weights;          // OUT_STATS: [B*Hk][rows] -log2 of the normaliser, -dY . Y
-  int* unread;                   // OUT_QUOTIENT: rows without a normaliser are added to it
-};
-int launch_values(const ValueArgs& a, hipStream_t st);
-// Gradient of rows through their features: dx = sum_m U_m W_m, U_m = 2^(e_m + term) (R . T_m + w z_m).
-struct GradArgs {
-  Features f;
-  int side;                      // 1: also the row term's gradient
-  Rows x, r;
-  const float *terms, *weights;  // (weights nullptr: ones)
   const int32_t* slots;
   State state;
   int B, Hk, dv;
-  TensorDev dx;
+  TensorDev Y;
+  int* unread;                   // rows without a normaliser are added to it
 };
-int launch_grads(const GradArgs& a, hipStream_t st);
+int launch_values(const ValueArgs& a, hipStream_t st);
+// Gradients of rows.  Queries: dx of Y = P T / P z for dY = r, and what the state's gradient needs of each row: -log2 of its normaliser,
+// -dY . Y.  Keys: dx and dr of T = S' r, z = S' 1 for the gradients T, z of those in `state`.
+struct GradArgs {
+  Features f;
+  Rows x, r;
+  const float* terms;            // keys: [B*Hk][rows] row terms less the state's shift
+  float *lse, *weights;          // queries: [B*Hk][rows]
+  const int32_t* slots;
+  State state;
+  int B, Hk, dv;
+  TensorDev dx, dr;
+};
+int launch_query_grads(const GradArgs& a, hipStream_t st);
+int launch_key_grads(const GradArgs& a, hipStream_t st);
 
 int launch_prepare(const float* theta, int groups, const float* Omega, int omega_groups, int sets, int d, int M, float scale, char* buf,
                    const FeaturePlan& p, hipStream_t st);
