@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(256) k_row_terms(Features f, Rows x, int Hk, c
             Op16<2> co;
 #pragma unroll
             for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
-            q = times16(co, xo[s], q);
+            each_product<2, 2>([&](int i, int j) { q = mfma(co.p[i], xo[s].p[j], q); });
           }
         const f32x4 y = *(const f32x4*)&lds[w][c][16 * ct + 4 * g];
 #pragma unroll
@@ -162,9 +162,66 @@ template <int W, int XP, int VP> struct BuildLds {
   float term[2][32], weight[2][32], undo[2][32];
 };
 
+// Four numbers of a row on their way to LDS.  P = 1: of a bf16 tensor, as they are.
+template <bool FULL, bool TURN> __device__ __forceinline__ f32x4 row4(const Rows& r, int b, int state_head, RowAt at, int c0) {
+  const long long base = row_base(r.X, b, state_head * r.G + at.head, at.row);
+  auto load = [&](int c) {
+    f32x4 x;
+    if (FULL || c + 4 <= r.cols) {
+      if (r.X.dtype == 0) {
+        x = *(const f32x4*)((const float*)r.X.ptr + base + c);
+      } else {
+        const u32x2 u = *(const u32x2*)((const uint16_t*)r.X.ptr + base + c);
+        x = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = c + i < r.cols ? load_elem(r.X, base + c + i) : 0.f;
+    }
+    return x;
+  };
+  const f32x4 x = load(c0);
+  const Turn& t = r.turn;
+  if (!TURN || c0 >= t.rot) return x;
+  const int half = t.rot >> 1;
+  const float2* cs = t.table + ((long long)b * r.L + at.row) * half;
+  f32x4 y = x;
+  if (t.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (c0 + 2 * i < t.rot) {
+        const float2 a = cs[(c0 >> 1) + i];
+        y[2 * i] = x[2 * i] * a.x - x[2 * i + 1] * a.y;
+        y[2 * i + 1] = x[2 * i + 1] * a.x + x[2 * i] * a.y;
+      }
+  } else if ((half & 3) == 0) {
+    const bool second = c0 >= half;
+    const f32x4 p = load(second ? c0 - half : c0 + half);
+    const f32x4* a = (const f32x4*)(cs + (second ? c0 - half : c0));        // (cos, sin) twice
+    const f32x4 a0 = a[0], a1 = a[1];
+    const float s = second ? 1.f : -1.f;
+    y[0] = x[0] * a0[0] + p[0] * (s * a0[1]);
+    y[1] = x[1] * a0[2] + p[1] * (s * a0[3]);
+    y[2] = x[2] * a1[0] + p[2] * (s * a1[1]);
+    y[3] = x[3] * a1[2] + p[3] * (s * a1[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = c0 + i;
+      if (c < t.rot) {
+        const bool second = c >= half;
+        const float2 a = cs[second ? c - half : c];
+        y[i] = x[i] * a.x + load_elem(r.X, base + (second ? c - half : c + half)) * ((second ? 1.f : -1.f) * a.y);
+      }
+    }
+  }
+  return y;
+}
+
 template <int W, int XP, int VP, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
-  constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 8, NTH = 64 * NW, U = (64 * UPR + NTH - 1) / NTH, LD = W + 8;
+  // a row's numbers in fours: 32 rows of x and of v are N fours a thread each, so that every wave brings as much
+  constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 4, NTH = 64 * NW, N = (32 * UPR + NTH - 1) / NTH, LD = W + 8;
   extern __shared__ __align__(16) char lds_raw[];
   BuildLds<W, XP, VP>& lds = *(BuildLds<W, XP, VP>*)lds_raw;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
@@ -180,65 +237,71 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     return;
   }
   const char* set = a.f.set(h);
-  // units of eight numbers of a row: those of x, then those of v
-  f32x8 next[U];
-  float next_term[U], next_weight[U];
+  f32x4 next_x[N], next_v[N];
+  u32x2 next_bits[N];
+  float next_term[N], next_weight[N];
   auto fetch = [&](int v) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int e = tid + NTH * i;
-      const bool is_x = e < 32 * UPR;
-      const int q = is_x ? e : e - 32 * UPR, row = q / UPR, c0 = 8 * (q % UPR);
-      next[i] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + NTH * i, row = e / UPR, c0 = 4 * (e % UPR);
+      next_x[i] = next_v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      next_bits[i] = u32x2{0u, 0u};
       next_term[i] = kNone;
       next_weight[i] = 0.f;
-      if (q >= 32 * UPR || v + row >= v1) continue;
+      if ((32 * UPR % NTH != 0 && row >= 32) || v + row >= v1) continue;
       const RowAt at = row_at(a.x, v + row);
       if (at.row >= len) continue;
-      if (is_x) {
-        next[i] = row8<FULL, XP == 2>(a.x, b, h, at, c0);
-        next_term[i] = a.terms ? a.terms[(size_t)bh * rows + v + row] : 0.f;
-        next_weight[i] = a.weights ? a.weights[(size_t)bh * rows + v + row] : 1.f;
-      } else {
-        next[i] = row8<FULL, false>(a.v, b, h, at, c0);
+      if (FULL || c0 < a.x.cols) next_x[i] = row4<FULL, XP == 2>(a.x, b, h, at, c0);
+      next_term[i] = a.terms ? a.terms[(size_t)bh * rows + v + row] : 0.f;
+      next_weight[i] = a.weights ? a.weights[(size_t)bh * rows + v + row] : 1.f;
+      if (FULL || c0 < dv) {
+        if (VP == 1 && (FULL || c0 + 4 <= dv))
+          next_bits[i] = *(const u32x2*)((const uint16_t*)a.v.X.ptr + row_base(a.v.X, b, h * a.v.G + at.head, at.row) + c0);
+        else next_v[i] = row4<FULL, false>(a.v, b, h, at, c0);
       }
     }
   };
   auto put = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int e = tid + NTH * i;
-      const bool is_x = e < 32 * UPR;
-      const int q = is_x ? e : e - 32 * UPR, row = q / UPR, u = q % UPR;
-      if (q >= 32 * UPR) continue;
-      if (is_x) {
-        float most = largest_of(next[i]), n = 0.f;
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + NTH * i, row = e / UPR, u = e % UPR;
+      if (32 * UPR % NTH != 0 && row >= 32) continue;
+      const f32x4 x = next_x[i];
+      const float most = over_lanes<UPR>(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))), [](float p, float q) { return fmaxf(p, q); });
+      const float n = over_lanes<UPR>(x[0] * x[0] + x[1] * x[1] + (x[2] * x[2] + x[3] * x[3]), [](float p, float q) { return p + q; });
+      const float scale = up_to_2_14(most);
+      const Op16<XP> o = as_op16<XP>(f32x8{x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f} * scale);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) n += next[i][j] * next[i][j];
-#pragma unroll
-        for (int o = UPR / 2; o > 0; o >>= 1) {
-          most = fmaxf(most, __shfl_xor(most, o));
-          n += __shfl_xor(n, o);
+      for (int p = 0; p < XP; ++p) {
+        const u32x4 bits = __builtin_bit_cast(u32x4, o.p[p]);
+        *(u32x2*)&lds.x[buf][p][row][4 * u] = u32x2{bits[0], bits[1]};
+      }
+      if (u == 0) {
+        lds.term[buf][row] = a.terms ? next_term[i] : next_term[i] - 0.5f * kLog2e * a.f.scale2 * n;        // (C2 = -I / 2)
+        lds.weight[buf][row] = next_weight[i];
+        lds.undo[buf][row] = power_inverse(scale);
+      }
+      const f32x4 y = next_v[i];
+      if constexpr (VP == 1) {
+        u32x2 bits = next_bits[i];
+        if (!FULL && 4 * u + 4 > dv) {
+          const u32x4 z = __builtin_bit_cast(u32x4, as_op<1>(f32x8{y[0], y[1], y[2], y[3], 0.f, 0.f, 0.f, 0.f}).p[0]);
+          bits = u32x2{z[0], z[1]};
         }
-        const float scale = up_to_2_14(most);
-        const Op16<XP> o = as_op16<XP>(next[i] * scale);
-#pragma unroll
-        for (int p = 0; p < XP; ++p) *(f16x8*)&lds.x[buf][p][row][8 * u] = o.p[p];
-        if (u == 0) {
-          lds.term[buf][row] = a.terms ? next_term[i] : next_term[i] - 0.5f * kLog2e * a.f.scale2 * n;      // (C2 = -I / 2)
-          lds.weight[buf][row] = next_weight[i];
-          lds.undo[buf][row] = power_inverse(scale);
-        }
+        *(u32x2*)&lds.v[buf][0][row][4 * u] = bits;
       } else {
-        const Op<VP> o = as_op<VP>(next[i]);
+        const Op<VP> q = as_op<VP>(f32x8{y[0], y[1], y[2], y[3], 0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int p = 0; p < VP; ++p) *(bf16x8*)&lds.v[buf][p][row][8 * u] = o.p[p];
+        for (int p = 0; p < VP; ++p) {
+          const u32x4 bits = __builtin_bit_cast(u32x4, q.p[p]);
+          *(u32x2*)&lds.v[buf][p][row][4 * u] = u32x2{bits[0], bits[1]};
+        }
       }
     }
   };
 
   fetch(v0);
-  Op16<2> wop[2][S];
+  Op16<2> wop[S][2];
   float bias[2] = {kNone, kNone}, wscale = 0.f;
   if (active) {
     const uint16_t* img = (const uint16_t*)(set + a.f.p.off_row[a.side]) + (size_t)fb * steps * 2 * 1024;
@@ -248,7 +311,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
 #pragma unroll
         for (int ft = 0; ft < 2; ++ft)
 #pragma unroll
-          for (int p = 0; p < 2; ++p) wop[ft][s].p[p] = *(const f16x8*)(img + (s * 2 + p) * 1024 + ft * 512 + lane * 8);
+          for (int p = 0; p < 2; ++p) wop[s][ft].p[p] = *(const f16x8*)(img + (s * 2 + p) * 1024 + ft * 512 + lane * 8);
 #pragma unroll
     for (int ft = 0; ft < 2; ++ft) bias[ft] = ((const float*)(set + a.f.p.off_bias))[32 * fb + 16 * ft + c];
     wscale = ((const float*)(set + a.f.p.off_scale[a.side]))[fb];
@@ -271,15 +334,14 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       for (int t = 0; t < 2; ++t) E[t][0] = E[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < S; ++s)
-        if (FULL || s < steps)
+        if (FULL || s < steps) {
+          Op16<XP> x[2];
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            Op16<XP> x;
+          for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int p = 0; p < XP; ++p) x.p[p] = *(const f16x8*)&lds.x[buf][p][16 * t + c][32 * s + 8 * g];
-            E[t][0] = times16(x, wop[0][s], E[t][0]);
-            E[t][1] = times16(x, wop[1][s], E[t][1]);
-          }
+            for (int p = 0; p < XP; ++p) x[t].p[p] = *(const f16x8*)&lds.x[buf][p][16 * t + c][32 * s + 8 * g];
+          outer(x, wop[s], E);
+        }
       f32x4 weight[2];
       float most = kNone;
 #pragma unroll
@@ -324,11 +386,11 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         so[ft] = as_op<3>(sv);
       }
 #pragma unroll
-      for (int vt = 0; vt < VT; ++vt)
+      for (int vt = 0; vt < VT; vt += 2)
         if (FULL || 16 * vt < dv) {
-          const Op<VP> vo = column_op<VP>(&lds.v[buf][0][0][16 * vt] + lane_tr(lane, LD), LD, 32 * LD);
-          T[0][vt] = times(so[0], vo, T[0][vt]);
-          T[1][vt] = times(so[1], vo, T[1][vt]);
+          const uint16_t* at_v = &lds.v[buf][0][0][16 * vt] + lane_tr(lane, LD);
+          const Op<VP> vo[2] = {column_op<VP>(at_v, LD, 32 * LD), column_op<VP>(at_v + 16, LD, 32 * LD)};
+          outer_at(so, vo, T, vt);
         }
     }
     if (more) put(buf ^ 1);

@@ -170,13 +170,15 @@ __device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, cons
   for (int rt = 0; rt < RT; ++rt) E[rt][0] = E[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < STEPS<W>; ++s)
-    if (FULL || s < steps)
+    if (FULL || s < steps) {
+      const Op16<2> w[2] = {weights.row(s, 0, lane), weights.row(s, 1, lane)};
+      each_product<2, XP>([&](int i, int j) {
 #pragma unroll
-      for (int ft = 0; ft < 2; ++ft) {
-        const Op16<2> w = weights.row(s, ft, lane);
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) E[rt][ft] = times16(w, x.x[rt][s], E[rt][ft]);
-      }
+          for (int ft = 0; ft < 2; ++ft) E[rt][ft] = mfma(w[ft].p[i], x.x[rt][s].p[j], E[rt][ft]);
+      });
+    }
 }
 __device__ __forceinline__ float over_groups_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
@@ -241,6 +243,21 @@ constexpr size_t most_of(size_t a, size_t b) { return a > b ? a : b; }
 template <int W, int TP, int CP, int NW, int RT, bool DIRECT> constexpr size_t rows_lds() {
   return DIRECT ? most_of(NW * sizeof(StateLds<W, TP>), (size_t)NW * 16 * RT * (W + 4) * 4)
                 : most_of(2 * (sizeof(StateLds<W, TP>) + sizeof(ImageLds<W, CP>)), (size_t)NW * 16 * (W + 4) * 4);
+}
+
+// Whether a workgroup's rows v0 .. v0 + n - 1 are all padding; they are then zeros of `out`.
+template <int W, int NTH>
+__device__ __forceinline__ bool all_padding(const Rows& r, int b, int h, int v0, int n, int len, const TensorDev& out, int cols, int tid) {
+  const int rows = r.L * r.G, v1 = min(v0 + n, rows), first = v0 % r.L;
+  // (a row below `len` is among them unless they end before the next head's first one)
+  if (first < len || (first + (v1 - v0) > r.L && len > 0)) return false;
+  const f32x8 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int u = tid; u < (v1 - v0) * (W / 8); u += NTH) {
+    const int c0 = 8 * (u % (W / 8));
+    const RowAt at = row_at(r, v0 + u / (W / 8));
+    if (c0 < cols) store8(out, row_base(out, b, h * r.G + at.head, at.row), c0, cols, zero);
+  }
+  return true;
 }
 
 // Calls body(state in LDS, W, first step of this wave?) for the features of this wave.
@@ -321,6 +338,8 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   const char* set = a.f.set(h);
   const float* scales = (const float*)(set + a.f.p.off_scale[0]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
+  constexpr int WG_ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  if (all_padding<W, 64 * NW>(a.x, b, h, blockIdx.x * WG_ROWS, WG_ROWS, len, a.Y, dv, tid)) return;
 
   RowOps<W, XP, RT, FULL> x;
   x.load(a.x, b, h, v0, rows, len, steps, lane);
@@ -365,11 +384,11 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
             po[rt] = as_op<P>(p);
           }
 #pragma unroll
-          for (int vt = 0; vt < VT; ++vt)
+          for (int vt = 0; vt < VT; vt += 2)
             if (FULL || 16 * vt < dv) {
-              const Op<P> t = column_op<P>(&l.t[0][0][16 * vt] + lane_tr(lane, LD), LD, 32 * LD);
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt) acc[rt][vt] = times(po[rt], t, acc[rt][vt]);
+              const uint16_t* at_t = &l.t[0][0][16 * vt] + lane_tr(lane, LD);
+              const Op<P> t[2] = {column_op<P>(at_t, LD, 32 * LD), column_op<P>(at_t + 16, LD, 32 * LD)};
+              outer_at(po, t, acc, vt);
             }
         });
   float factor[RT];
@@ -440,6 +459,16 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
   const char* set = a.f.set(h);
   const float* scales = (const float*)(set + a.f.p.off_scale[KEYS]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
+  constexpr int WG_ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  if (all_padding<W, 64 * NW>(a.x, b, h, blockIdx.x * WG_ROWS, WG_ROWS, len, a.dx, d, tid)) {
+    if constexpr (KEYS) all_padding<W, 64 * NW>(a.x, b, h, blockIdx.x * WG_ROWS, WG_ROWS, len, a.dr, dv, tid);
+    else
+      for (int v = blockIdx.x * WG_ROWS + tid; v < min((int)(blockIdx.x + 1) * WG_ROWS, rows); v += 64 * NW) {
+        a.lse[(size_t)bh * rows + v] = kNone;
+        a.weights[(size_t)bh * rows + v] = 0.f;
+      }
+    return;
+  }
 
   RowOps<W, XP, RT, FULL> x;
   x.load(a.x, b, h, v0, rows, len, steps, lane);
@@ -450,9 +479,15 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
   for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (x.live[rt] && (FULL || 32 * s < dv)) n = row8<FULL, false>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
-      rr[rt][s] = as_op<RP>(n);
+      if constexpr (RP == 1) {
+        u32x4 n = {0u, 0u, 0u, 0u};
+        if (x.live[rt]) n = row8_bits<FULL>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
+        rr[rt][s].p[0] = __builtin_bit_cast(bf16x8, n);
+      } else {
+        f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (x.live[rt]) n = row8<FULL, false>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
+        rr[rt][s] = as_op<RP>(n);
+      }
     }
     term[rt] = KEYS ? (x.live[rt] && slot >= 0 ? a.terms[(size_t)bh * rows + v0 + 16 * rt + c] : kNone) : 0.f;
     ref[rt] = sums[rt][0] = sums[rt][1] = 0.f;
@@ -463,26 +498,29 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
     walk_features<W, TP, P, NW, FULL, DIRECT>(
         a.f, KEYS, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
         [&](const StateLds<W, TP>& l, const Weights<W, P>& weights, bool first) {
-          f32x4 E[RT][2], D[RT][2];
-          exponents(x, weights, steps, lane, E);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) D[rt][0] = D[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = 0; s < S; ++s)
-            if (FULL || 32 * s < dv)
-#pragma unroll
-              for (int ft = 0; ft < 2; ++ft) {
-                const Op<TP> t = row_op<TP>(&l.t[0][16 * ft + c][32 * s + 8 * g], 32 * LD);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) D[rt][ft] = times(t, rr[rt][s], D[rt][ft]);
-              }
-          const float scale = scales[weights.fb];
-          f32x4 bias[2], zf[2];
+          f32x4 E[RT][2], D[RT][2], bias[2], zf[2];
 #pragma unroll
           for (int ft = 0; ft < 2; ++ft) {
             bias[ft] = *(const f32x4*)&l.bias[16 * ft + 4 * g];
             zf[ft] = *(const f32x4*)&l.z[16 * ft + 4 * g];
           }
+          exponents(x, weights, steps, lane, E);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int ft = 0; ft < 2; ++ft) D[rt][ft] = KEYS ? zf[ft] : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < S; ++s)
+            if (FULL || 32 * s < dv) {
+              const Op<TP> t[2] = {row_op<TP>(&l.t[0][c][32 * s + 8 * g], 32 * LD), row_op<TP>(&l.t[0][16 + c][32 * s + 8 * g], 32 * LD)};
+              each_product<TP, RP>([&](int i, int j) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                  for (int ft = 0; ft < 2; ++ft) D[rt][ft] = mfma(t[ft].p[i], rr[rt][s].p[j], D[rt][ft]);
+              });
+            }
+          const float scale = scales[weights.fb];
           Op<P> uo[RT], so[RT];
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
@@ -496,7 +534,7 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const float p = fast_exp2(E[rt][ft][r]);
-                u[4 * ft + r] = p * (KEYS ? D[rt][ft][r] + zf[ft][r] : D[rt][ft][r]);
+                u[4 * ft + r] = p * D[rt][ft][r];
                 s[4 * ft + r] = KEYS ? p : p * zf[ft][r];
                 sums[rt][1] += u[4 * ft + r];
                 if constexpr (!KEYS) sums[rt][0] += s[4 * ft + r];
@@ -505,20 +543,17 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
             so[rt] = as_op<P>(s);
           }
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
+          for (int ct = 0; ct < CT; ct += 2) {
             if (FULL || 16 * ct < d) {
-              const Op<P> wo = weights.col(ct, lane);
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt) {
-                acc[rt][ct] = times(uo[rt], wo, acc[rt][ct]);
-                if constexpr (!KEYS) more[rt][ct] = times(so[rt], wo, more[rt][ct]);
-              }
+              const Op<P> wo[2] = {weights.col(ct, lane), weights.col(ct + 1, lane)};
+              outer_at(uo, wo, acc, ct);
+              if constexpr (!KEYS) outer_at(so, wo, more, ct);
             }
             if constexpr (KEYS)
               if (FULL || 16 * ct < dv) {
-                const Op<P> t = column_op<P>(&l.t[0][0][16 * ct] + lane_tr(lane, LD), LD, 32 * LD);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) more[rt][ct] = times(so[rt], t, more[rt][ct]);
+                const uint16_t* at_t = &l.t[0][0][16 * ct] + lane_tr(lane, LD);
+                const Op<P> t[2] = {column_op<P>(at_t, LD, 32 * LD), column_op<P>(at_t + 16, LD, 32 * LD)};
+                outer_at(so, t, more, ct);
               }
           }
         });
@@ -589,7 +624,7 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
                   Op16<2> co;
 #pragma unroll
                   for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
-                  q = times16(x.x[rt][s], co, q);
+                  each_product<XP, 2>([&](int i, int j) { q = mfma(x.x[rt][s].p[i], co.p[j], q); });
                 }
               acc[rt][ct] += (rho4 * *(const float*)(set + a.f.p.off_cscale)) * q;
             }

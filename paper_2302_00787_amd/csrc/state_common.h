@@ -127,10 +127,7 @@ __device__ __forceinline__ void store8(const TensorDev& t, long long base, int c
       *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
       *(f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
     } else {
-      u32x4 u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = (uint32_t)f32_to_bf16_bits(x[2 * i]) | (uint32_t)f32_to_bf16_bits(x[2 * i + 1]) << 16;
-      *(u32x4*)((uint16_t*)t.ptr + base + c0) = u;
+      *(bf16x8*)((uint16_t*)t.ptr + base + c0) = __builtin_convertvector(x, bf16x8);
     }
   } else {
 #pragma unroll
@@ -186,6 +183,19 @@ __device__ __forceinline__ f32x8 row8(const Rows& r, int b, int state_head, RowA
   return turned8(x, c0, r.turn, cs, 1.f, [&](int c) { return load_elem(r.X, base + c); }, [&](int c) { return load8<FULL>(r.X, base, c, r.cols); });
 }
 
+// The same of a bf16 tensor that is not turned, bits as they are.
+template <bool FULL>
+__device__ __forceinline__ u32x4 row8_bits(const Rows& r, int b, int state_head, RowAt at, int c0) {
+  if (!FULL && c0 >= r.cols) return u32x4{0u, 0u, 0u, 0u};
+  const uint16_t* p = (const uint16_t*)r.X.ptr + row_base(r.X, b, state_head * r.G + at.head, at.row) + c0;
+  if (FULL || c0 + 8 <= r.cols) return *(const u32x4*)p;
+  u32x4 u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    u[i] = (c0 + 2 * i < r.cols ? (uint32_t)p[2 * i] : 0u) | (c0 + 2 * i + 1 < r.cols ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+  return u;
+}
+
 // ---------------------------------------------------------------------------------------------- slots
 // Slot of sequence b, -1 where there is none.  unique: also where an earlier sequence has the same one (for all threads of a workgroup).
 __device__ __forceinline__ int slot_of(const int32_t* slots, int nslots, int b) {
@@ -233,6 +243,19 @@ template <int P> __device__ __forceinline__ Op<P> image_op(const uint16_t* img, 
   return o;
 }
 
+// Sum and largest over N = 4, 8, 16 or 32 neighbouring lanes: within sixteen by the lane permutations of a vector instruction.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <int N, class Op2> __device__ __forceinline__ float over_lanes(float v, Op2 op) {
+  v = op(v, dpp<0xb1>(v));                          // lanes 1 0 3 2 of a quad
+  v = op(v, dpp<0x4e>(v));                          // 2 3 0 1
+  if constexpr (N >= 8) v = op(v, dpp<0x141>(v));   // eight lanes backwards
+  if constexpr (N >= 16) v = op(v, dpp<0x140>(v));  // sixteen
+  if constexpr (N >= 32) v = op(v, __shfl_xor(v, 16));
+  return v;
+}
+
 // fp16 pieces of the factors of an exponent (see FeaturePlan): 2, or 1 of a bf16 number.  The numbers of a row are multiplied by a power of
 // two first, that of up_to_2_14, so that the largest is below 2^14; what is below 2^-39 of it is lost.
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -255,13 +278,6 @@ __device__ __forceinline__ float largest_of(f32x8 x) {
   for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
   return m;
 }
-template <int PA, int PB>
-__device__ __forceinline__ f32x4 times16(const Op16<PA>& a, const Op16<PB>& b, f32x4 c) {
-  if constexpr (PB == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[0], b.p[1], c, 0, 0, 0);
-  if constexpr (PA == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[1], b.p[0], c, 0, 0, 0);
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[0], b.p[0], c, 0, 0, 0);
-}
-
 template <int P> __device__ __forceinline__ Op<P> row_op(const uint16_t* s, int plane) {         // eight numbers of a row
   Op<P> o;
 #pragma unroll
@@ -285,27 +301,36 @@ template <int P> __device__ __forceinline__ Op<P> column_op(const uint16_t* s, i
 // Lanes 4 i + a of a group of sixteen name the four 8-byte pieces a of row 4 g + i; lane (a, b) = (c / 4, c % 4) gets column c of the rows.
 __device__ __forceinline__ int lane_tr(int lane, int ld) { return (4 * (lane >> 4) + ((lane & 15) >> 2)) * ld + 4 * (lane & 3); }
 
-// c + a b, small products first.
-template <int PA, int PB>
-__device__ __forceinline__ f32x4 times(const Op<PA>& a, const Op<PB>& b, f32x4 c) {
-  if constexpr (PA == 3 && PB == 3) {
-    c = mfma_bf16(a.p[2], b.p[0], c);
-    c = mfma_bf16(a.p[0], b.p[2], c);
-    c = mfma_bf16(a.p[1], b.p[1], c);
-    c = mfma_bf16(a.p[1], b.p[0], c);
-    c = mfma_bf16(a.p[0], b.p[1], c);
-    return mfma_bf16(a.p[0], b.p[0], c);
-  } else if constexpr (PA == 2 && PB == 2) {
-    c = mfma_bf16(a.p[1], b.p[0], c);
-    c = mfma_bf16(a.p[0], b.p[1], c);
-    return mfma_bf16(a.p[0], b.p[0], c);
-  } else {
-    static_assert(PA == 1 || PB == 1, "");
-    constexpr int P = PA > PB ? PA : PB;
+// f(i, j) for the products of piece i of an operand of PA and piece j of one of PB that are above 2^-24 (2^-16, 2^-22) of it, small ones first.
+// One product for all accumulators before the next: those of one accumulator wait for each other.
+template <int PA, int PB, class F> __device__ __forceinline__ void each_product(F f) {
 #pragma unroll
-    for (int i = P - 1; i >= 0; --i) c = mfma_bf16(a.p[PA > 1 ? i : 0], b.p[PB > 1 ? i : 0], c);
-    return c;
-  }
+  for (int sum = (PA > PB ? PA : PB) - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int i = PA - 1; i >= 0; --i)
+      if (sum - i >= 0 && sum - i < PB) f(i, sum - i);
+}
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+// c[i][j] += a[i] b[j]
+template <template <int> class O, int PA, int PB, int NA, int NB>
+__device__ __forceinline__ void outer(const O<PA> (&a)[NA], const O<PB> (&b)[NB], f32x4 (&c)[NA][NB]) {
+  each_product<PA, PB>([&](int pa, int pb) {
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) c[i][j] = mfma(a[i].p[pa], b[j].p[pb], c[i][j]);
+  });
+}
+// c[i][at + j] += a[i] b[j]
+template <int PA, int PB, int NA, int NB, int NC>
+__device__ __forceinline__ void outer_at(const Op<PA> (&a)[NA], const Op<PB> (&b)[NB], f32x4 (&c)[NA][NC], int at) {
+  each_product<PA, PB>([&](int pa, int pb) {
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) c[i][at + j] = mfma(a[i].p[pa], b[j].p[pb], c[i][at + j]);
+  });
 }
 
 // ---------------------------------------------------------------------------------------------- arguments of the kernels
