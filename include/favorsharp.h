@@ -399,11 +399,12 @@ int favorsharp_state_attention(const fs_features* host_features, const fs_state*
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token of every sequence: K [B, heads, 1, d] and V [B, heads, 1, dv] are appended, then Q [B, H, 1, d] reads the state that
- * holds them: Y [B, H, 1, dv].  One launch, no workspace.  Q, K, V share a dtype.  unread as above; the rows of sequences
- * that are left out are counted too. */
+ * holds them: Y [B, H, 1, dv].  Q, K, V share a dtype.  unread as above; the rows of sequences that are left out are counted
+ * too. */
+size_t favorsharp_state_step_workspace_bytes(const fs_features* host_features, int B, int H);
 int favorsharp_state_step(const fs_features* host_features, const fs_state* state, const int32_t* slots, const fs_tensor* Q,
                           const fs_tensor* K, const fs_tensor* V, int B, int H, int dv, const fs_rotary* rot,
-                          const fs_tensor* Y, int32_t* unread, void* stream);
+                          const fs_tensor* Y, int32_t* unread, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Gradients of sum(Y * dY) of favorsharp_state_attention with respect to Q and to T and z (shift constant: Y does not depend on
  * the scale that T and z share).  dstate: a pool of as many slots, T and z overwritten: sums over the rows of all query heads

@@ -127,7 +127,8 @@ def lib() -> ctypes.CDLL:
                 ("state_append", c_int, [F, S, c_void_p, P, P, c_int, c_int, c_int, c_void_p, R, c_int, c_void_p] + ws),
                 ("state_attention_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int, c_int]),
                 ("state_attention", c_int, [F, S, c_void_p, P, c_int, c_int, c_int, c_int, c_void_p, R, P, c_void_p] + ws),
-                ("state_step", c_int, [F, S, c_void_p, P, P, P, c_int, c_int, c_int, R, P, c_void_p, c_void_p]),
+                ("state_step_workspace_bytes", c_size_t, [F, c_int, c_int]),
+                ("state_step", c_int, [F, S, c_void_p, P, P, P, c_int, c_int, c_int, R, P, c_void_p] + ws),
                 ("state_attention_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int, c_int]),
                 ("state_attention_backward", c_int, [F, S, c_void_p, P, P, c_int, c_int, c_int, c_int, c_void_p, R, P, S] + ws),
                 ("state_append_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int]),
@@ -664,7 +665,7 @@ def state_attention(f: Features, state: State, Q: torch.Tensor, lengths: torch.T
 
 def state_step(f: Features, state: State, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor | None = None,
                rotary: Rotary | None = None, out: torch.Tensor | None = None, out_dtype=None,
-               unread: torch.Tensor | None = None) -> torch.Tensor:
+               unread: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """favorsharp_state_step: K [B,heads,1,d], V [B,heads,1,dv] onto the states (in place), then Q [B,H,1,d] against them -> Y."""
     B, H, L, d = Q.shape
     dv = V.shape[3]
@@ -674,12 +675,14 @@ def state_step(f: Features, state: State, Q: torch.Tensor, K: torch.Tensor, V: t
     if out is None:
         out = torch.empty((B, H, 1, dv), dtype=out_dtype or Q.dtype, device=Q.device)
     _shaped("out", out, (B, H, 1, dv))
-    device = _one_device(Q, K, V, out, f.buffer, *state, slots, unread, *_rotary_tensors(rotary))
+    device = _one_device(Q, K, V, out, f.buffer, *state, slots, unread, workspace, *_rotary_tensors(rotary))
     r, _ = _rotary_desc(rotary, B, 1)
+    fd = ctypes.byref(f.desc)
+    ws = _workspace(lib().favorsharp_state_step_workspace_bytes(fd, B, H), device, workspace)
     with _on(device):
-        st = lib().favorsharp_state_step(ctypes.byref(f.desc), _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)),
+        st = lib().favorsharp_state_step(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)),
                                          ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, H, dv, r, ctypes.byref(_desc4(out)),
-                                         _counter("unread", unread), _stream())
+                                         _counter("unread", unread), ws.data_ptr(), ws.numel(), _stream())
     _check(st, "favorsharp_state_step")
     return out
 

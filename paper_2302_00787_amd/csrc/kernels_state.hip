@@ -44,10 +44,9 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
   }
   __syncthreads();
   uint16_t *row = (uint16_t*)(base + p.off_row[side]), *col = (uint16_t*)(base + p.off_col[side]);
-  float* w = (float*)(base + p.off_w[side]);
   float most = 0.f;
   for (int i = tid; i < 32 * n; i += 256) {
-    const int f = i / n, c = i - f * n, m = 32 * blk + f, tile = f >> 4, r = f & 15;
+    const int f = i / n, c = i - f * n, tile = f >> 4, r = f & 15;
     double sum = 0.0;
     if (c < d)
       for (int l = 0; l < d; ++l) sum += (double)om[f][l] * (double)Bm[(size_t)l * d + c];
@@ -55,7 +54,6 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
     wv[f][c] = v;
     most = fmaxf(most, fabsf(v));
     split3_store(col + ((size_t)blk * p.tiles + (c >> 4)) * 3 * 512 + (r / 4 * 16 + (c & 15)) * 8 + 4 * tile + (r & 3), 512, v);
-    if (c < 4 * p.d4) w[((size_t)(c >> 2) * p.Mp + m) * 4 + (c & 3)] = v;
   }
   const float up = up_to_2_14(block_max(most, tmp));
   for (int i = tid; i < 32 * n; i += 256) {
@@ -77,7 +75,6 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
     most = 0.f;
     for (int i = tid; i < (int)dd; i += 256) {
       const int a = i / d, c = i - a * d;
-      ((float*)(base + p.off_c2))[i] = C2[i];
       most = fmaxf(most, fabsf(C2[i] + C2[(size_t)c * d + a]));
     }
     const float cup = up_to_2_14(block_max(most, tmp));
@@ -105,12 +102,13 @@ __global__ void __launch_bounds__(256) k_row_terms(Features f, Rows x, int Hk, c
   const bool live = row < len && slot >= 0;
   f32x8 n[S];
   float most = 0.f, sum = 0.f;
+  const int at = min(row, x.L - 1);
+  const long long base = row_base(x.X, b, h, at);
+  RowUnits<S, false, true> units;
+  units.fetch(x.X, base, x.cols, x.turn, live, g);
+  units.finish(x.X, base, x.cols, x.turn, x.turn.table + ((long long)b * x.L + at) * (x.turn.rot >> 1), live, g, n);
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    n[s] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (live && s < f.p.steps) n[s] = row8<false, true>(x, b, h, RowAt{0, row}, 32 * s + 8 * g);
-    most = fmaxf(most, largest_of(n[s]));
-  }
+  for (int s = 0; s < S; ++s) most = fmaxf(most, largest_of(n[s]));
   if (f.dense) {
     const char* set = f.set(h);
     most = fmaxf(most, __shfl_xor(most, 16));
@@ -125,22 +123,19 @@ __global__ void __launch_bounds__(256) k_row_terms(Features f, Rows x, int Hk, c
     }
     __syncthreads();
 #pragma unroll
-    for (int ct = 0; ct < 2 * S; ++ct)
-      if (ct < f.p.tiles) {
-        f32x4 q = {0.f, 0.f, 0.f, 0.f};
-        const uint16_t* img = (const uint16_t*)(set + f.p.off_csym) + (size_t)ct * f.p.steps * 2 * 512;
+    for (int ct = 0; ct < 2 * S; ++ct) {         // (no branches, so that the images are on their way together: behind d the row is zeros)
+      f32x4 q = {0.f, 0.f, 0.f, 0.f};
+      const uint16_t* img = (const uint16_t*)(set + f.p.off_csym) + (size_t)min(ct, f.p.tiles - 1) * f.p.steps * 1024 + lane * 8;
 #pragma unroll
-        for (int s = 0; s < S; ++s)
-          if (s < f.p.steps) {
-            Op16<2> co;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
-            each_product<2, 2>([&](int i, int j) { q = mfma(co.p[i], xo[s].p[j], q); });
-          }
-        const f32x4 y = *(const f32x4*)&lds[w][c][16 * ct + 4 * g];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
+      for (int s = 0; s < S; ++s) {
+        const uint16_t* from = img + min(s, f.p.steps - 1) * 1024;
+        const f16x8 p[2] = {*(const f16x8*)from, *(const f16x8*)(from + 512)};
+        each_product<2, 2>([&](int i, int j) { q = mfma(p[i], xo[s].p[j], q); });
       }
+      const f32x4 y = *(const f32x4*)&lds[w][c][16 * ct + 4 * g];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
+    }
     sum *= 0.5f * power_inverse(scale) * *(const float*)(set + f.p.off_cscale);
   } else {
 #pragma unroll
@@ -162,61 +157,86 @@ template <int W, int XP, int VP> struct BuildLds {
   float term[2][32], weight[2][32], undo[2][32];
 };
 
-// Four numbers of a row on their way to LDS.  P = 1: of a bf16 tensor, as they are.
-template <bool FULL, bool TURN> __device__ __forceinline__ f32x4 row4(const Rows& r, int b, int state_head, RowAt at, int c0) {
-  const long long base = row_base(r.X, b, state_head * r.G + at.head, at.row);
-  auto load = [&](int c) {
-    f32x4 x;
-    if (FULL || c + 4 <= r.cols) {
-      if (r.X.dtype == 0) {
-        x = *(const f32x4*)((const float*)r.X.ptr + base + c);
+// Four numbers of a row (columns c0 ..), their partners and angles, on their way to LDS: as they lie, so that nothing waits for them before they are
+// put there.  TURN = false: numbers alone.
+template <bool FULL, bool TURN> struct Four {
+  u32x4 x, p;
+  f32x4 cs[TURN ? 2 : 1];
+  __device__ __forceinline__ static u32x4 bits(const TensorDev& t, long long base, int c, int cols) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (FULL || c + 4 <= cols) {
+      if (t.dtype == 0) {
+        v = *(const u32x4*)((const float*)t.ptr + base + c);
       } else {
-        const u32x2 u = *(const u32x2*)((const uint16_t*)r.X.ptr + base + c);
-        x = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+        const u32x2 u = *(const u32x2*)((const uint16_t*)t.ptr + base + c);
+        v[0] = u[0];
+        v[1] = u[1];
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = c + i < r.cols ? load_elem(r.X, base + c + i) : 0.f;
+      for (int i = 0; i < 4; ++i)
+        if (c + i < cols) v[i] = t.dtype == 0 ? ((const uint32_t*)t.ptr)[base + c + i] : (uint32_t)((const uint16_t*)t.ptr)[base + c + i];
     }
-    return x;
-  };
-  const f32x4 x = load(c0);
-  const Turn& t = r.turn;
-  if (!TURN || c0 >= t.rot) return x;
-  const int half = t.rot >> 1;
-  const float2* cs = t.table + ((long long)b * r.L + at.row) * half;
-  f32x4 y = x;
-  if (t.interleaved) {
+    return v;
+  }
+  __device__ __forceinline__ static f32x4 numbers(u32x4 v, int dtype, int c, int cols) {
+    if (dtype == 0) return __builtin_bit_cast(f32x4, v);
+    if (!FULL && c + 4 > cols) return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[1] << 16), __uint_as_float(v[2] << 16), 0.f};
+    return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xffff0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xffff0000u)};
+  }
+  __device__ __forceinline__ void none() { x = u32x4{0u, 0u, 0u, 0u}; }
+  // base: the row's first number; a: its angles
+  __device__ __forceinline__ void get(const Rows& r, long long base, const float2* a, int c0) {
+    none();
+    if (!FULL && c0 >= r.cols) return;
+    x = bits(r.X, base, c0, r.cols);
+    if (!TURN || c0 >= r.turn.rot) return;
+    const int half = r.turn.rot >> 1;
+    if (r.turn.interleaved) {
+      const float2 u = a[c0 >> 1], v = a[min((c0 >> 1) + 1, half - 1)];
+      cs[0] = f32x4{u.x, u.y, v.x, v.y};
+    } else if ((half & 3) == 0) {
+      const int i = c0 >= half ? c0 - half : c0;
+      p = bits(r.X, base, c0 >= half ? i : c0 + half, r.cols);
+      cs[0] = *(const f32x4*)(a + i);
+      cs[1] = *(const f32x4*)(a + i + 2);
+    } else {                     // (partners one by one)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (c0 + 2 * i < t.rot) {
-        const float2 a = cs[(c0 >> 1) + i];
-        y[2 * i] = x[2 * i] * a.x - x[2 * i + 1] * a.y;
-        y[2 * i + 1] = x[2 * i + 1] * a.x + x[2 * i] * a.y;
-      }
-  } else if ((half & 3) == 0) {
-    const bool second = c0 >= half;
-    const f32x4 p = load(second ? c0 - half : c0 + half);
-    const f32x4* a = (const f32x4*)(cs + (second ? c0 - half : c0));        // (cos, sin) twice
-    const f32x4 a0 = a[0], a1 = a[1];
-    const float s = second ? 1.f : -1.f;
-    y[0] = x[0] * a0[0] + p[0] * (s * a0[1]);
-    y[1] = x[1] * a0[2] + p[1] * (s * a0[3]);
-    y[2] = x[2] * a1[0] + p[2] * (s * a1[1]);
-    y[3] = x[3] * a1[2] + p[3] * (s * a1[3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = c0 + i;
-      if (c < t.rot) {
-        const bool second = c >= half;
-        const float2 a = cs[second ? c - half : c];
-        y[i] = x[i] * a.x + load_elem(r.X, base + (second ? c - half : c + half)) * ((second ? 1.f : -1.f) * a.y);
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + i;
+        if (c < r.turn.rot) {
+          const int k = c >= half ? c - half : c, o = c >= half ? k : c + half;
+          p[i] = r.X.dtype == 0 ? ((const uint32_t*)r.X.ptr)[base + o] : (uint32_t)((const uint16_t*)r.X.ptr)[base + o] << 16;
+          const float2 u = a[k];
+          cs[i >> 1][2 * (i & 1)] = u.x;
+          cs[i >> 1][2 * (i & 1) + 1] = u.y;
+        }
       }
     }
   }
-  return y;
-}
+  __device__ __forceinline__ f32x4 put(const Rows& r, int c0, bool live) const {
+    const f32x4 v = numbers(x, r.X.dtype, c0, r.cols);
+    if (!TURN || !live || c0 >= r.turn.rot) return v;
+    const int half = r.turn.rot >> 1;
+    f32x4 y = v;
+    if (r.turn.interleaved) {
+      y[0] = v[0] * cs[0][0] - v[1] * cs[0][1];
+      y[1] = v[1] * cs[0][0] + v[0] * cs[0][1];
+      if (c0 + 2 < r.turn.rot) {
+        y[2] = v[2] * cs[0][2] - v[3] * cs[0][3];
+        y[3] = v[3] * cs[0][2] + v[2] * cs[0][3];
+      }
+    } else {
+      const bool quad = (half & 3) == 0;
+      const f32x4 q = quad ? numbers(p, r.X.dtype, c0, r.turn.rot) : __builtin_bit_cast(f32x4, p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (quad || c0 + i < r.turn.rot)
+          y[i] = v[i] * cs[i >> 1][2 * (i & 1)] + q[i] * (c0 + i >= half ? cs[i >> 1][2 * (i & 1) + 1] : -cs[i >> 1][2 * (i & 1) + 1]);
+    }
+    return y;
+  }
+};
 
 template <int W, int XP, int VP, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
@@ -237,36 +257,59 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     return;
   }
   const char* set = a.f.set(h);
-  f32x4 next_x[N], next_v[N];
-  u32x2 next_bits[N];
+  Four<FULL, XP == 2> next_x[N];
+  Four<FULL, false> next_v[N];
+  bool next_live[N];
   float next_term[N], next_weight[N];
+  const float *terms = a.terms ? a.terms + (size_t)bh * rows : nullptr, *weights = a.weights ? a.weights + (size_t)bh * rows : nullptr;
+  // one head: this thread's rows are 32 apart, and so are their addresses
+  const int row0 = tid / UPR, c0 = 4 * (tid % UPR);
+  constexpr int ROWS = NTH / UPR;            // rows that the threads bring at a time
+  const int v_live = a.x.G == 1 ? v1 : 0;
+  long long x_at = row_base(a.x.X, b, h, v0 + row0), v_at = row_base(a.v.X, b, h, v0 + row0);
+  const float2* cs_at = a.x.turn.table + ((long long)b * a.x.L + v0 + row0) * (a.x.turn.rot >> 1);
+  constexpr int STEP = ROWS < 32 ? ROWS : 32;
+  const long long x_step = STEP * a.x.X.sl, v_step = STEP * a.v.X.sl;
+  const int cs_step = STEP * (a.x.turn.rot >> 1);
   auto fetch = [&](int v) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = tid + NTH * i, row = e / UPR, c0 = 4 * (e % UPR);
-      next_x[i] = next_v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      next_bits[i] = u32x2{0u, 0u};
+      const int row = row0 + ROWS * i;
+      next_x[i].none();
+      next_v[i].none();
+      next_live[i] = false;
       next_term[i] = kNone;
       next_weight[i] = 0.f;
-      if ((32 * UPR % NTH != 0 && row >= 32) || v + row >= v1) continue;
-      const RowAt at = row_at(a.x, v + row);
-      if (at.row >= len) continue;
-      if (FULL || c0 < a.x.cols) next_x[i] = row4<FULL, XP == 2>(a.x, b, h, at, c0);
-      next_term[i] = a.terms ? a.terms[(size_t)bh * rows + v + row] : 0.f;
-      next_weight[i] = a.weights ? a.weights[(size_t)bh * rows + v + row] : 1.f;
-      if (FULL || c0 < dv) {
-        if (VP == 1 && (FULL || c0 + 4 <= dv))
-          next_bits[i] = *(const u32x2*)((const uint16_t*)a.v.X.ptr + row_base(a.v.X, b, h * a.v.G + at.head, at.row) + c0);
-        else next_v[i] = row4<FULL, false>(a.v, b, h, at, c0);
+      const bool mine = 32 * UPR % NTH == 0 || row < 32;
+      if (v_live > 0) {
+        if (mine && v + row < v_live) {
+          next_live[i] = true;
+          next_x[i].get(a.x, x_at, cs_at, c0);
+          next_v[i].get(a.v, v_at, nullptr, c0);
+          next_term[i] = terms ? terms[v + row] : 0.f;
+          next_weight[i] = weights ? weights[v + row] : 1.f;
+        }
+        x_at += x_step;
+        v_at += v_step;
+        if constexpr (XP == 2) cs_at += cs_step;
+      } else {
+        if (!mine || v + row >= v1) continue;
+        const RowAt at = row_at(a.x, v + row);
+        if (at.row >= len) continue;
+        next_live[i] = true;
+        next_x[i].get(a.x, row_base(a.x.X, b, h * a.x.G + at.head, at.row), a.x.turn.table + ((long long)b * a.x.L + at.row) * (a.x.turn.rot >> 1), c0);
+        next_v[i].get(a.v, row_base(a.v.X, b, h * a.v.G + at.head, at.row), nullptr, c0);
+        next_term[i] = terms ? terms[v + row] : 0.f;
+        next_weight[i] = weights ? weights[v + row] : 1.f;
       }
     }
   };
   auto put = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = tid + NTH * i, row = e / UPR, u = e % UPR;
+      const int row = row0 + ROWS * i, u = tid % UPR;
       if (32 * UPR % NTH != 0 && row >= 32) continue;
-      const f32x4 x = next_x[i];
+      const f32x4 x = next_x[i].put(a.x, 4 * u, next_live[i]);
       const float most = over_lanes<UPR>(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))), [](float p, float q) { return fmaxf(p, q); });
       const float n = over_lanes<UPR>(x[0] * x[0] + x[1] * x[1] + (x[2] * x[2] + x[3] * x[3]), [](float p, float q) { return p + q; });
       const float scale = up_to_2_14(most);
@@ -281,15 +324,10 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         lds.weight[buf][row] = next_weight[i];
         lds.undo[buf][row] = power_inverse(scale);
       }
-      const f32x4 y = next_v[i];
-      if constexpr (VP == 1) {
-        u32x2 bits = next_bits[i];
-        if (!FULL && 4 * u + 4 > dv) {
-          const u32x4 z = __builtin_bit_cast(u32x4, as_op<1>(f32x8{y[0], y[1], y[2], y[3], 0.f, 0.f, 0.f, 0.f}).p[0]);
-          bits = u32x2{z[0], z[1]};
-        }
-        *(u32x2*)&lds.v[buf][0][row][4 * u] = bits;
+      if (VP == 1 && (FULL || 4 * u + 4 <= dv)) {
+        *(u32x2*)&lds.v[buf][0][row][4 * u] = u32x2{next_v[i].x[0], next_v[i].x[1]};
       } else {
+        const f32x4 y = next_v[i].put(a.v, 4 * u, false);
         const Op<VP> q = as_op<VP>(f32x8{y[0], y[1], y[2], y[3], 0.f, 0.f, 0.f, 0.f});
 #pragma unroll
         for (int p = 0; p < VP; ++p) {
@@ -317,7 +355,8 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     wscale = ((const float*)(set + a.f.p.off_scale[a.side]))[fb];
   }
   f32x4 T[2][VT];
-  float z[2] = {0.f, 0.f}, ref = kNone, top = kNone;
+  float z[2] = {0.f, 0.f}, ref = 0.f, top = kNone;
+  bool referred = false;
 #pragma unroll
   for (int ft = 0; ft < 2; ++ft)
 #pragma unroll
@@ -352,25 +391,27 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         for (int ft = 0; ft < 2; ++ft)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            E[t][ft][r] = E[t][ft][r] * undo[r] + (bias[ft] + term[r]);
+            E[t][ft][r] = E[t][ft][r] * undo[r] + (bias[ft] + (term[r] - ref));
             most = fmaxf(most, E[t][ft][r]);
           }
       }
-      top = fmaxf(top, most);
-      if (__any(most > ref + 16.f)) {
+      top = fmaxf(top, ref + most);
+      if (__any(most > 16.f || (!referred && most > kNone))) {
         float m = most;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-        const float keep = fast_exp2(ref - (m - 8.f));
-        ref = m - 8.f;
+        const float up = m - 8.f, keep = referred ? fast_exp2(-up) : 0.f;
+        ref += up;
+        referred = true;
 #pragma unroll
         for (int ft = 0; ft < 2; ++ft) {
           z[ft] *= keep;
 #pragma unroll
           for (int vt = 0; vt < VT; ++vt) T[ft][vt] *= keep;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) E[t][ft] -= up;
         }
       }
-      const float at = ref == kNone ? 0.f : ref;
       Op<3> so[2];
 #pragma unroll
       for (int ft = 0; ft < 2; ++ft) {
@@ -379,7 +420,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float x = fast_exp2(E[t][ft][r] - at);
+            const float x = fast_exp2(E[t][ft][r]);
             sv[4 * t + r] = x;
             z[ft] += x * weight[t][r];
           }
@@ -420,6 +461,20 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
 // ---------------------------------------------------------------------------------------------- join
 constexpr int kJoinWeights = 4096;       // references of a state's partial sums: at most 64 splits of 2048 features
 
+// x += sum of weight(s) from[s stride]: eight loads on their way at a time.  What has no weight may be anything.
+template <class V, class F> __device__ __forceinline__ void sum_parts(V& x, const V* from, size_t stride, int n, F weight) {
+  for (int s0 = 0; s0 < n; s0 += 8) {
+    V v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = from[(size_t)min(s0 + i, n - 1) * stride];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float k = s0 + i < n ? weight(s0 + i) : 0.f;
+      if (k != 0.f) x += k * v[i];
+    }
+  }
+}
+
 template <int VEC>
 __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
   __shared__ float weight[kJoinWeights], tmp[4];
@@ -445,21 +500,16 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
     if (e < nt) {
       const int m = e * VEC / a.dv, fb = m >> 5;
       vec* to = (vec*)(a.state.T + at * a.M * a.dv) + e;
+      const vec* from = (const vec*)(a.part + (size_t)bh * a.nsplit * a.M * a.dv) + e;
       vec x = {};
       if (keep != 0.f) x = keep * *to;
-      for (int s = 0; s < a.nsplit; ++s) {
-        const float k = weight[s * nfb + fb];
-        if (k != 0.f) x += k * ((const vec*)(a.part + ((size_t)bh * a.nsplit + s) * a.M * a.dv))[e];
-      }
+      sum_parts(x, from, nt, a.nsplit, [&](int s) { return weight[s * nfb + fb]; });
       *to = x;
     } else {
       const int m = e - nt, fb = m >> 5;
       float* to = a.state.z + at * a.M + m;
       float x = keep != 0.f ? keep * *to : 0.f;
-      for (int s = 0; s < a.nsplit; ++s) {
-        const float k = weight[s * nfb + fb];
-        if (k != 0.f) x += k * a.zpart[((size_t)bh * a.nsplit + s) * a.M + m];
-      }
+      sum_parts(x, a.zpart + (size_t)bh * a.nsplit * a.M + m, a.M, a.nsplit, [&](int s) { return weight[s * nfb + fb]; });
       *to = x;
     }
   }
@@ -477,12 +527,15 @@ __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
     for (int b = b0; b < b1; ++b) {
       if (slot_of(a.slots, a.state.slots, b) != slot) continue;
       const size_t at = ((size_t)b * a.Hk + h) * a.nsplit;
-      for (int s = 0; s < a.nsplit; ++s) {
+      auto weight = [&](int s) {
         const float2 ref = a.refs[(at + s) * nfb + fb];
-        if (ref.y == kNone) continue;
-        const float k = fast_exp2(ref.x);
-        if (e < nt) x += k * ((const vec*)(a.part + (at + s) * a.M * a.dv))[e];
-        else x[0] += k * a.zpart[(at + s) * a.M + m];
+        return ref.y == kNone ? 0.f : fast_exp2(ref.x);
+      };
+      if (e < nt) sum_parts(x, (const vec*)(a.part + at * a.M * a.dv) + e, nt, a.nsplit, weight);
+      else {
+        float y = x[0];
+        sum_parts(y, a.zpart + at * a.M + m, a.M, a.nsplit, weight);
+        x[0] = y;
       }
     }
     if (e < nt) ((vec*)(a.state.T + (size_t)sh * a.M * a.dv))[e] = x;

@@ -142,19 +142,23 @@ template <int W, int XP, int RT, bool FULL> struct RowOps {
   bool live[RT];
   __device__ __forceinline__ void load(const Rows& r, int b, int h, int v0, int rows, int len, int steps, int lane) {
     const int g = lane >> 4, c = lane & 15;
+    RowUnits<S, FULL, XP == 2> units[RT];
+    long long base[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int v = v0 + 16 * rt + c;
       at[rt] = row_at(r, min(v, rows - 1));
       live[rt] = v < rows && at[rt].row < len;
+      base[rt] = row_base(r.X, b, h * r.G + at[rt].head, at[rt].row);
+      units[rt].fetch(r.X, base[rt], r.cols, r.turn, live[rt], g);
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
       f32x8 n[S];
+      units[rt].finish(r.X, base[rt], r.cols, r.turn, r.turn.table + ((long long)b * r.L + at[rt].row) * (r.turn.rot >> 1), live[rt], g, n);
       float most = 0.f;
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        n[s] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live[rt] && (FULL || s < steps)) n[s] = row8<FULL, XP == 2>(r, b, h, at[rt], 32 * s + 8 * g);
-        most = fmaxf(most, largest_of(n[s]));
-      }
+      for (int s = 0; s < S; ++s) most = fmaxf(most, largest_of(n[s]));
       most = fmaxf(most, __shfl_xor(most, 16));
       most = fmaxf(most, __shfl_xor(most, 32));
       const float scale = up_to_2_14(most);
@@ -485,7 +489,9 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
         rr[rt][s].p[0] = __builtin_bit_cast(bf16x8, n);
       } else {
         f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (x.live[rt]) n = row8<FULL, false>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
+        const int c0 = 32 * s + 8 * g;
+        if (x.live[rt] && (FULL || c0 < dv))
+          n = load8<FULL>(a.r.X, row_base(a.r.X, b, h * a.r.G + x.at[rt].head, x.at[rt].row), c0, dv);
         rr[rt][s] = as_op<RP>(n);
       }
     }

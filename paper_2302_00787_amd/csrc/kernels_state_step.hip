@@ -1,8 +1,10 @@
-// The next token of every sequence: its key and value onto the state, then its queries against it, in one launch.
+// The next token of every sequence: its key and value onto the state, then its queries against it.
 //
-// A workgroup has a state of one key head: it reads it once and writes it once, which bounds the call (2 M (dv + 1) numbers of 4 bytes).  Its
-// first rows are on their way from the start, while the exponents are made (a thread a feature, W in fp32 from L2, the row from LDS); the
-// shift is the largest exponent ever met, exactly as in kernels_state.hip.
+// The states are read once and written once (2 M (dv + 1) numbers of 4 bytes a key head), which bounds the call, so a launch of its own makes the
+// exponents first, sixteen rows of a head at a time on the matrix instructions as in the other kernels: W is read once for sixteen
+// rows and not once for each state, whose size it has (one launch, a state a workgroup with W from L2: 45 states of 512 x 128 with
+// four query heads 44 us, 2048 of 256 x 64 73).  It also keeps the states' z and shift as they were, so that the second launch can cut a
+// state into columns for as many workgroups as fill the chip.
 #include <algorithm>
 
 #include "state_common.h"
@@ -11,230 +13,284 @@ namespace fs {
 namespace st {
 namespace {
 
-constexpr int NTH = 512, NW = NTH / 64, GC = 4, AHEAD = 8;     // GC: query heads served by a pass over the state
-
-__device__ __forceinline__ float wave_max(float v) {
+// ---------------------------------------------------------------------------------------------- exponents
+// Tiles of sixteen rows: keys of sequences (first a.key_tiles of them), then queries, row v = query head v % G of sequence v / G.
+template <int S>
+__global__ void __launch_bounds__(256) k_step_exponents(StepArgs a) {
+  __shared__ float2 angles[16][64];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+  const int h = blockIdx.y, G = a.H / a.Hk, fb = blockIdx.x * 4 + w, Mp = a.f.p.Mp, nfb = Mp / 32, steps = a.f.p.steps, d = a.f.d, M = a.f.M;
+  const bool keys = (int)blockIdx.z < a.key_tiles;
+  const int per = keys ? 1 : G, rows = a.B * per, v0 = 16 * (keys ? blockIdx.z : blockIdx.z - a.key_tiles);
+  const char* set = a.f.set(h);
+  const int pairs = a.rot.rot >> 1;
+  f16x8 wo[S][2][2];             // [step][piece][tile]
+  if (fb < nfb) {
+    const uint16_t* at = (const uint16_t*)(set + a.f.p.off_row[keys]) + (size_t)fb * steps * 2048 + lane * 8;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
+    for (int s = 0; s < S; ++s)
+      if (s < steps)
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int ft = 0; ft < 2; ++ft) wo[s][i][ft] = *(const f16x8*)(at + (s * 2 + i) * 1024 + ft * 512);
+  }
+  const TensorDev& X = keys ? a.K : a.Q;
+  const int v = v0 + c, vc = min(v, rows - 1), b = vc / per;
+  const long long base = row_base(X, b, keys ? h : h * G + vc % per, 0);
+  const Turn turn{nullptr, a.rot.rot, a.rot.interleaved};
+  RowUnits<S, false, true> units;
+  units.fetch(X, base, d, turn, true, g);
+  for (int e = tid; e < 16 * pairs; e += 256) {
+    const int r = e / pairs, i = e - r * pairs, row = min(v0 + r, rows - 1);
+    angles[r][i] = cos_sin(position_of(a.rot, row / per, 0), a.rot.freqs[i], a.rot.amplitude);
+  }
+  __syncthreads();
+  if (fb >= nfb) return;
+  f32x8 n[S];
+  float most = 0.f, norm = 0.f;
+  units.finish(X, base, d, turn, &angles[c][0], true, g, n);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    most = fmaxf(most, largest_of(n[s]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) norm += n[s][i] * n[s][i];
+  }
+  most = fmaxf(most, __shfl_xor(most, 16));
+  most = fmaxf(most, __shfl_xor(most, 32));
+  const float scale = up_to_2_14(most);
+  Op16<2> x[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) x[s] = as_op16<2>(n[s] * scale);
+  f32x4 E[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+    if (s < steps)
+      each_product<2, 2>([&](int i, int j) {
+#pragma unroll
+        for (int ft = 0; ft < 2; ++ft) E[ft] = mfma(wo[s][i][ft], x[s].p[j], E[ft]);
+      });
+  const float undo = power_inverse(scale) * ((const float*)(set + a.f.p.off_scale[keys]))[fb];
+  const float* bias = (const float*)(set + a.f.p.off_bias);
+  if (v < rows) {
+    float* to = a.exps + ((size_t)(b * a.Hk + h) * (1 + G) + (keys ? 0 : 1 + vc % per)) * Mp;
+#pragma unroll
+    for (int ft = 0; ft < 2; ++ft) {
+      const int m = 32 * fb + 16 * ft + 4 * g;
+      *(f32x4*)(to + m) = E[ft] * undo + *(const f32x4*)(bias + m);
+    }
+  }
+  if (!keys) return;
+  // the sequences' z of these features as they are, and once their shift and the keys' row terms
+  const int slot = slot_of(a.slots, a.state.slots, b);
+  if (v < rows && slot >= 0) {
+    const float* z = a.state.z + ((size_t)slot * a.Hk + h) * M;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int m = 32 * fb + 8 * g + i;
+      if (m < M) a.old_z[(size_t)(b * a.Hk + h) * Mp + m] = z[m];
+    }
+  }
+  if (fb > 0) return;
+  float term;
+  if (a.f.dense) {               // k' (C2 + C2') k / 2, whose rows of sixteen coordinates meet the row's numbers by way of LDS
+    __shared__ __align__(16) float y[16][32 * S + 4];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      *(f32x4*)&y[c][32 * s + 8 * g] = f32x4{n[s][0], n[s][1], n[s][2], n[s][3]};
+      *(f32x4*)&y[c][32 * s + 8 * g + 4] = f32x4{n[s][4], n[s][5], n[s][6], n[s][7]};
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    term = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 2 * S; ++ct) {         // (no branches, so that the images are on their way together: behind d the row is zeros)
+      f32x4 q = {0.f, 0.f, 0.f, 0.f};
+      const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)min(ct, 2 * steps - 1) * steps * 1024 + lane * 8;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const uint16_t* at = img + min(s, steps - 1) * 1024;
+        const f16x8 p[2] = {*(const f16x8*)at, *(const f16x8*)(at + 512)};
+        each_product<2, 2>([&](int i, int j) { q = mfma(p[i], x[s].p[j], q); });
+      }
+      const f32x4 k = *(const f32x4*)&y[c][16 * ct + 4 * g];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) term += q[r] * k[r];
+    }
+    term *= 0.5f * power_inverse(scale) * *(const float*)(set + a.f.p.off_cscale);
+  } else {
+    term = -0.5f * norm;
+  }
+  term += __shfl_xor(term, 16);
+  term += __shfl_xor(term, 32);
+  if (v < rows && g == 0)
+    a.old_shift[b * a.Hk + h] = make_float2(slot >= 0 ? a.state.shift[(size_t)slot * a.Hk + h] : kNone, term * kLog2e * a.f.scale2);
 }
 
-// Floats in LDS: rows (key, queries), value, angles, exponents and features (key, queries), z, the partial outputs.
-__host__ __device__ inline int step_lds_floats(int Mp) { return (GC + 1) * 128 + 128 + 128 + (GC + 2) * Mp + 4 * GC * NTH + 16; }
+// ---------------------------------------------------------------------------------------------- states
+// Floats in LDS: features (key, GC queries), the threads' partial outputs, maxima and normalisers by wave.
+template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int Mp) { return (GC + 1) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64); }
 
-template <int VEC>
-__global__ void __launch_bounds__(NTH) k_step(StepArgs a) {
+// GC: query heads that a pass over the state serves.  Workgroup z has the columns z cols .. (z + 1) cols - 1.
+template <int VEC, int GC, int NTH>
+__global__ void __launch_bounds__(NTH, NTH == 256 ? 4 : 2) k_step(StepArgs a) {
   typedef __attribute__((ext_vector_type(VEC))) float vec;
+  constexpr int NW = NTH / 64, AHEAD = GC == 1 ? 8 : 4;          // fours of the state on their way for each thread
   extern __shared__ __align__(16) float lds[];
-  const int Mp = a.f.p.Mp, M = a.f.M, d = a.f.d, dv = a.dv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  float* x = lds;                              // [GC + 1][128]: the key, then queries
-  float* value = x + (GC + 1) * 128;
-  float2* cs = (float2*)(value + 128);         // [64]
-  float* feat = (float*)cs + 128;              // [GC + 1][Mp]
-  float* zn = feat + (GC + 1) * Mp;            // [Mp]
-  float* part = zn + Mp;                       // [GC][rows of the pass][dv]
-  float* word = part + 4 * GC * NTH;           // keep; row term by wave; normalisers
-  const int b = blockIdx.x, h = blockIdx.y, G = a.H / a.Hk;
+  const int Mp = a.f.p.Mp, M = a.f.M, dv = a.dv, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  float* feat = lds;                           // [GC + 1][Mp]
+  float* part = feat + (GC + 1) * Mp;          // [GC][rows of a pass][columns]
+  float* tops = part + 4 * GC * NTH;           // [GC + 1][NW]
+  float* dens = tops + (1 + GC) * NW;          // [GC][NW]
+  const int b = blockIdx.x, h = blockIdx.y, G = GC == 1 ? 1 : a.H / a.Hk, col0 = blockIdx.z * a.cols, cols = min(a.cols, dv - col0);
   const int slot = unique_slot_of(a.slots, a.state.slots, b);
   if (slot < 0) {
-    for (int e = tid; e < G * dv; e += NTH) store_elem(a.Y, row_base(a.Y, b, h * G + e / dv, 0) + e % dv, 0.f);
-    if (tid == 0 && a.unread != nullptr) atomicAdd(a.unread, G);
+    for (int e = tid; e < G * cols; e += NTH) store_elem(a.Y, row_base(a.Y, b, h * G + e / cols, 0) + col0 + e % cols, 0.f);
+    if (tid == 0 && blockIdx.z == 0 && a.unread != nullptr) atomicAdd(a.unread, G);
     return;
   }
-  const size_t at = (size_t)slot * a.Hk + h;
-  const int quads = (dv + VEC - 1) / VEC, pass = NTH / quads, q0 = tid % quads, r0 = tid / quads;       // rows of a pass over the state
+  const size_t at = (size_t)slot * a.Hk + h, bh = (size_t)b * a.Hk + h;
+  const int quads = (cols + VEC - 1) / VEC, pass = NTH / quads, q0 = tid % quads, r0 = tid / quads;       // rows of a pass over the state
   const bool worker = r0 < pass;
-  vec* T = (vec*)(a.state.T + at * M * dv);
-  vec first[AHEAD];
+  const int mine = worker ? (M - r0 + pass - 1) / pass : 0, step = pass * (dv / VEC);                      // rows r0, r0 + pass, ...: `mine` of them
+  vec* T = (vec*)(a.state.T + at * M * dv + col0) + (worker ? r0 * (dv / VEC) + q0 : 0);
+  vec t[AHEAD];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) {
-    const int m = r0 + i * pass;
-    if (worker && m < M) first[i] = T[(size_t)m * quads + q0];
-  }
-  const char* set = a.f.set(h);
-  const float *W1 = (const float*)(set + a.f.p.off_w[0]), *W2 = (const float*)(set + a.f.p.off_w[1]), *bias = (const float*)(set + a.f.p.off_bias);
-  const float old = a.state.shift[at];
-  const int pairs = a.rot.rot >> 1;
-  if (tid < pairs) cs[tid] = cos_sin(position_of(a.rot, b, 0), a.rot.freqs[tid], a.rot.amplitude);
-  if (tid >= 128 && tid < 128 + dv) value[tid - 128] = load_elem(a.V, row_base(a.V, b, h, 0) + tid - 128);
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < mine) t[i] = T[(size_t)i * step];
+  const float2 before = a.old_shift[bh];       // shift, the key's row term
+  vec v;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) v[i] = worker ? load_elem(a.V, row_base(a.V, b, h, 0) + col0 + VEC * q0 + i) : 0.f;
+  const float* exps = a.exps + bh * (1 + G) * Mp;
+  const float* old_z = a.old_z + bh * Mp;
   float keep = 0.f;
   int unread = 0;
   for (int g0 = 0; g0 < G; g0 += GC) {
-    const int n = min(GC, G - g0), from = g0 == 0 ? 0 : 1;        // rows of x: the key in the first pass only
-    __syncthreads();
-    for (int e = tid + from * 128; e < (n + 1) * 128; e += NTH) {
-      const int r = e >> 7, c = e & 127;
-      const TensorDev& t = r == 0 ? a.K : a.Q;
-      const long long base = row_base(t, b, r == 0 ? h : h * G + g0 + r - 1, 0);
-      float y = 0.f;
-      if (c < d) {
-        y = load_elem(t, base + c);
-        if (c < a.rot.rot) {
-          const bool second = a.rot.interleaved ? c & 1 : c >= pairs;
-          const int i = a.rot.interleaved ? c >> 1 : (second ? c - pairs : c);
-          const float other = load_elem(t, base + (a.rot.interleaved ? c ^ 1 : (second ? c - pairs : c + pairs)));
-          y = y * cs[i].x + (second ? other : -other) * cs[i].y;
+    const int n = GC == 1 ? 1 : min(GC, G - g0);
+    if (g0 > 0) __syncthreads();
+    // features: a thread has the same ones of all rows; the key's again with every pass
+    float top[GC + 1];
+#pragma unroll
+    for (int j = 0; j <= GC; ++j) {
+      top[j] = kNone;
+      if (j <= n)
+        for (int m = tid; m < Mp; m += NTH) {
+          const float e = exps[(size_t)(j == 0 ? 0 : g0 + j) * Mp + m] + (j == 0 ? before.y : 0.f);
+          feat[j * Mp + m] = e;
+          top[j] = fmaxf(top[j], e);
         }
-      }
-      x[e] = y;
+      top[j] = over_lanes<32>(top[j], [](float p, float q) { return fmaxf(p, q); });
+      top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
+      if (lane == 0) tops[j * NW + w] = top[j];
     }
     __syncthreads();
-    // row term of the key: wave w sums over the columns c = w, w + NW, ...
-    if (g0 == 0) {
-      float sum = 0.f;
-      if (a.f.dense) {
-        const float* C2 = (const float*)(set + a.f.p.off_c2);
-        for (int c = w; c < d; c += NW) {
-          float z = 0.f;
-          for (int l = lane; l < d; l += 64) z += x[l] * C2[c * d + l];
-          sum += x[c] * z;
+#pragma unroll
+    for (int j = 0; j <= GC; ++j)
+#pragma unroll
+      for (int i = 0; i < NW; ++i) top[j] = fmaxf(top[j], tops[j * NW + i]);
+    top[0] = fmaxf(top[0], before.x);
+    keep = before.x == kNone ? 0.f : fast_exp2(before.x - top[0]);
+    float den[GC];
+#pragma unroll
+    for (int j = 0; j < GC; ++j) den[j] = 0.f;
+    for (int m = tid; m < Mp; m += NTH) {
+      const float s = top[0] == kNone ? 0.f : fast_exp2(feat[m] - top[0]);
+      float z = s;
+      if (keep != 0.f && m < M) z += keep * old_z[m];
+      feat[m] = s;
+      if (m < M && g0 == 0 && blockIdx.z == 0) a.state.z[at * M + m] = z;
+#pragma unroll
+      for (int j = 0; j < GC; ++j)
+        if (j < n) {
+          const float p = fast_exp2(feat[(1 + j) * Mp + m] - top[1 + j]);
+          feat[(1 + j) * Mp + m] = p;
+          den[j] += p * z;
         }
-      } else if (w == 0) {
-        sum = -0.5f * (x[lane] * x[lane] + x[64 + lane] * x[64 + lane]);
-      }
-      sum = wave_sum(sum);
-      if (lane == 0) word[w] = sum;
     }
-    // exponents: features of the key, then those of the queries
-    for (int e = tid + from * Mp; e < 2 * Mp; e += NTH) {
-      const bool key = e < Mp;
-      const int m = key ? e : e - Mp;
-      const float* Wm = (key ? W2 : W1) + (size_t)m * 4;
-      float s[GC] = {0.f, 0.f, 0.f, 0.f};
-      if (key || n == 1) {
-        const float* row = x + (key ? 0 : 128);
-#pragma unroll 8
-        for (int c = 0; c < a.f.p.d4; ++c) {
-          const f32x4 u = *(const f32x4*)(Wm + (size_t)c * Mp * 4), v = *(const f32x4*)(row + 4 * c);
+    if (tid == 0 && g0 == 0 && blockIdx.z == 0) a.state.shift[at] = top[0];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[0] += u[i] * v[i];
-        }
-      } else {
-#pragma unroll 4
-        for (int c = 0; c < a.f.p.d4; ++c) {
-          const f32x4 u = *(const f32x4*)(Wm + (size_t)c * Mp * 4);
-#pragma unroll
-          for (int j = 0; j < GC; ++j) {
-            const f32x4 v = *(const f32x4*)(x + (1 + min(j, n - 1)) * 128 + 4 * c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[j] += u[i] * v[i];
-          }
-        }
-      }
-      if (key) feat[m] = s[0] + bias[m];
-      else
-#pragma unroll
-        for (int j = 0; j < GC; ++j)
-          if (j < n) feat[(1 + j) * Mp + m] = s[j] + bias[m];
+    for (int j = 0; j < GC; ++j) {
+      den[j] = over_lanes<32>(den[j], [](float p, float q) { return p + q; });
+      den[j] += __shfl_xor(den[j], 32);
+      if (lane == 0) dens[j * NW + w] = den[j];
     }
     __syncthreads();
-    // features: wave 0 the key's and z, the others the queries'
-    if (w == 0 && g0 == 0) {
-      float term = 0.f;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) term += word[i];
-      term *= kLog2e * a.f.scale2;
-      float top = kNone;
-      for (int m = lane; m < Mp; m += 64) top = fmaxf(top, feat[m] + term);
-      top = fmaxf(wave_max(top), old);
-      const float k = old == kNone ? 0.f : fast_exp2(old - top);
-      for (int m = lane; m < Mp; m += 64) {
-        const float s = top == kNone ? 0.f : fast_exp2((feat[m] + term) - top);
-        feat[m] = s;
-        float z = s;
-        if (m < M) {
-          float* to = a.state.z + at * M + m;
-          if (k != 0.f) z += k * *to;
-          *to = z;
-        }
-        zn[m] = z;
-      }
-      if (lane == 0) {
-        word[8] = k;
-        a.state.shift[at] = top;
-      }
-    } else {
-      const int j = w - (g0 == 0 ? 1 : 0);
-      if (j < n) {
-        float* p = feat + (1 + j) * Mp;
-        float top = kNone;
-        for (int m = lane; m < Mp; m += 64) top = fmaxf(top, p[m]);
-        top = wave_max(top);
-        for (int m = lane; m < Mp; m += 64) p[m] = fast_exp2(p[m] - top);
-      }
-    }
-    __syncthreads();
-    keep = word[8];
-    if (w < n) {
-      float den = 0.f;
-      for (int m = lane; m < Mp; m += 64) den += feat[(1 + w) * Mp + m] * zn[m];
-      den = wave_sum(den);
-      if (lane == 0) word[12 + w] = den;
-    }
     // the state
     vec acc[GC] = {};
-    vec v;
+    for (int k0 = 0; k0 < mine; k0 += AHEAD) {
+      if (g0 > 0 || k0 > 0)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = worker ? value[VEC * q0 + i] : 0.f;
-    if (worker)
-      for (int m0 = r0; m0 < M; m0 += AHEAD * pass) {
-        vec t[AHEAD];
+        for (int i = 0; i < AHEAD; ++i)
+          if (k0 + i < mine) t[i] = T[(size_t)(k0 + i) * step];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-          const int m = m0 + i * pass;
-          if (g0 == 0 && m0 == r0) t[i] = first[i];
-          else if (m < M) t[i] = T[(size_t)m * quads + q0];
+      for (int i = 0; i < AHEAD; ++i) {
+        if (k0 + i >= mine) continue;
+        const int m = r0 + (k0 + i) * pass;
+        if (g0 == 0) {
+          t[i] = keep != 0.f ? keep * t[i] + feat[m] * v : feat[m] * v;
+          T[(size_t)(k0 + i) * step] = t[i];
         }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-          const int m = m0 + i * pass;
-          if (m >= M) continue;
-          if (g0 == 0) {
-            vec n2 = feat[m] * v;
-            if (keep != 0.f) n2 += keep * t[i];
-            t[i] = n2;
-            T[(size_t)m * quads + q0] = n2;
-          }
-#pragma unroll
-          for (int j = 0; j < GC; ++j)
-            if (j < n) acc[j] += feat[(1 + j) * Mp + m] * t[i];
-        }
+        for (int j = 0; j < GC; ++j)
+          if (j < n) acc[j] += feat[(1 + j) * Mp + m] * t[i];
       }
+    }
     if (worker)
 #pragma unroll
       for (int j = 0; j < GC; ++j)
         if (j < n)
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) part[(j * pass + r0) * dv + VEC * q0 + i] = acc[j][i];
+          for (int i = 0; i < VEC; ++i) part[(j * pass + r0) * cols + VEC * q0 + i] = acc[j][i];
     __syncthreads();
-    for (int e = tid; e < n * dv; e += NTH) {
-      const int j = e / dv, c = e - j * dv;
-      float sum = 0.f;
-      for (int r = 0; r < pass; ++r) sum += part[(j * pass + r) * dv + c];
-      const float den = word[12 + j];
-      store_elem(a.Y, row_base(a.Y, b, h * G + g0 + j, 0) + c, den == 0.f ? 0.f : sum / den);
-      unread += c == 0 && den == 0.f;
+    for (int e = tid; e < n * cols; e += NTH) {
+      const int j = e / cols, c = e - j * cols;
+      float sum = 0.f, d = 0.f;
+#pragma unroll 4
+      for (int r = 0; r < pass; ++r) sum += part[(j * pass + r) * cols + c];
+#pragma unroll
+      for (int i = 0; i < NW; ++i) d += dens[j * NW + i];
+      store_elem(a.Y, row_base(a.Y, b, h * G + g0 + j, 0) + col0 + c, d == 0.f ? 0.f : sum / d);
+      unread += col0 + c == 0 && d == 0.f;
     }
   }
   if (unread > 0 && a.unread != nullptr) atomicAdd(a.unread, unread);
 }
 
-}  // namespace
-
-int launch_step(const StepArgs& a, hipStream_t st) {
-  const size_t lds = step_lds_floats(a.f.p.Mp) * sizeof(float);
-  auto kernel = a.dv % 4 == 0 ? k_step<4> : k_step<1>;
+template <int VEC, int GC, int NTH> int step(const StepArgs& a, hipStream_t st) {
+  const size_t lds = step_lds_floats<GC, NTH>(a.f.p.Mp) * sizeof(float);
+  auto kernel = k_step<VEC, GC, NTH>;
   if (lds > 64 * 1024 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return 5;
   }
-  hipLaunchKernelGGL(kernel, dim3(a.B, a.Hk), dim3(NTH), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(a.B, a.Hk, (a.dv + a.cols - 1) / a.cols), dim3(NTH), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
+}
+
+}  // namespace
+
+size_t step_floats(int B, int H, int Hk, int Mp) { return (size_t)B * ((size_t)(H + Hk) * Mp + (size_t)Hk * Mp + 2 * Hk); }
+
+int launch_step(StepArgs a, float* room, hipStream_t st) {
+  const int Mp = a.f.p.Mp, S = a.f.p.steps, G = a.H / a.Hk;
+  a.old_shift = (float2*)room;
+  a.exps = room + 2 * (size_t)a.B * a.Hk;
+  a.exps += (4 - ((a.exps - room) & 3)) & 3;
+  a.old_z = a.exps + (size_t)a.B * (a.H + a.Hk) * Mp;
+  a.key_tiles = (a.B + 15) / 16;
+  const long long tiles = a.key_tiles + ((long long)a.B * G + 15) / 16;
+  const dim3 grid((Mp / 32 + 3) / 4, a.Hk, (unsigned)tiles);
+  if (S == 1) hipLaunchKernelGGL(k_step_exponents<1>, grid, dim3(256), 0, st, a);
+  else if (S == 2) hipLaunchKernelGGL(k_step_exponents<2>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_step_exponents<4>, grid, dim3(256), 0, st, a);
+  if (hipGetLastError() != hipSuccess) return 5;
+  // a state in halves or quarters of its columns, 16 at least, until four workgroups a CU are there
+  a.cols = a.dv;
+  while ((long long)a.B * a.Hk * ((a.dv + a.cols - 1) / a.cols) < 1024 && a.cols % 32 == 0 && 4 * a.cols > a.dv) a.cols /= 2;
+  if (a.H == a.Hk) return a.dv % 4 == 0 ? step<4, 1, 256>(a, st) : step<1, 1, 256>(a, st);
+  return a.dv % 4 == 0 ? step<4, 4, 256>(a, st) : step<1, 4, 256>(a, st);
 }
 
 }  // namespace st

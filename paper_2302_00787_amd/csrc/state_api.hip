@@ -243,11 +243,18 @@ int favorsharp_state_attention(const fs_features* f, const fs_state* state, cons
   return st::launch_values(a, s);
 }
 
+size_t favorsharp_state_step_workspace_bytes(const fs_features* f, int B, int H) {
+  if (!sizes_ok(f, B, H, 1, 1, 0)) return 0;
+  return align_up(st::step_floats(B, H, f->heads, st::feature_plan(f->d, f->M, 1).Mp) * sizeof(float) + 16);
+}
+
 int favorsharp_state_step(const fs_features* f, const fs_state* state, const int32_t* slots, const fs_tensor* Q, const fs_tensor* K,
-                          const fs_tensor* V, int B, int H, int dv, const fs_rotary* rot, const fs_tensor* Y, int32_t* unread, void* stream) {
+                          const fs_tensor* V, int B, int H, int dv, const fs_rotary* rot, const fs_tensor* Y, int32_t* unread,
+                          void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check(f, state, true, B, H, 1, dv, rot)) return rc;
   if (!tensor_ok(Q, f->d) || !tensor_ok(K, f->d) || !tensor_ok(V, dv) || !tensor_ok(Y, dv)) return FS_ERR_INVALID_ARG;
-  if (Q->dtype != K->dtype || Q->dtype != V->dtype) return FS_ERR_INVALID_ARG;
+  if (Q->dtype != K->dtype || Q->dtype != V->dtype || workspace == nullptr || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
+  if (workspace_bytes < favorsharp_state_step_workspace_bytes(f, B, H)) return FS_ERR_WORKSPACE_TOO_SMALL;
   st::StepArgs a{};
   a.f = features_of(f);
   a.state = state_of(state);
@@ -256,7 +263,7 @@ int favorsharp_state_step(const fs_features* f, const fs_state* state, const int
   a.B = B; a.H = H; a.Hk = f->heads; a.dv = dv;
   a.rot = dev(rot);
   a.unread = unread;
-  return st::launch_step(a, (hipStream_t)stream);
+  return st::launch_step(a, (float*)workspace, (hipStream_t)stream);
 }
 
 size_t favorsharp_state_attention_backward_workspace_bytes(const fs_features* f, int B, int H, int L, int dv, int rot_dim) {

@@ -26,18 +26,16 @@ inline int width_class(int d, int dv) { const int n = d > dv ? d : dv; return n 
 // 512 numbers]) and C2 + C2' ([coordinate tiles][steps][2][512]) are two fp16 pieces of a number: exponents and row terms need absolute
 // accuracy only, so 22 bits of the largest number of a row or of 32 features do, and three products of pieces (two against bf16 rows) take half of
 // what bf16 pieces need.  `scale` is what a block of 32 features (or C2 + C2') was divided by, to lie below 2^14.  Column images (the features
-// are the contraction index: [32 features][coordinate tiles][3][512]) in bf16 pieces, biases (-inf behind the last feature), W1 and W2 in
-// fp32 for single tokens ([4 coordinates][features][4]), C2.
+// are the contraction index: [32 features][coordinate tiles][3][512]) in bf16 pieces, biases (-inf behind the last feature).
 struct FeaturePlan {
-  int Mp, steps, tiles, d4;      // features in 32s, steps of 32 coordinates, tiles of 16 coordinates, coordinates in fours
-  size_t off_row[2], off_scale[2], off_col[2], off_csym, off_cscale, off_bias, off_w[2], off_c2, set, total;
+  int Mp, steps, tiles;          // features in 32s, steps of 32 coordinates, tiles of 16 coordinates
+  size_t off_row[2], off_scale[2], off_col[2], off_csym, off_cscale, off_bias, set, total;
 };
 inline FeaturePlan feature_plan(int d, int M, int sets) {
   FeaturePlan p;
   p.Mp = (M + 31) / 32 * 32;
   p.steps = (d + 31) / 32;
   p.tiles = 2 * p.steps;
-  p.d4 = (d + 3) / 4;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t off = 0;
   for (int s = 0; s < 2; ++s) { p.off_row[s] = off; off = up(off + (size_t)p.Mp * p.steps * 2 * 32 * 2); }
@@ -46,8 +44,6 @@ inline FeaturePlan feature_plan(int d, int M, int sets) {
   p.off_csym = off; off = up(off + (size_t)p.tiles * p.steps * 2 * 512 * 2);
   p.off_cscale = off; off = up(off + 4);
   p.off_bias = off; off = up(off + (size_t)p.Mp * 4);
-  for (int s = 0; s < 2; ++s) { p.off_w[s] = off; off = up(off + (size_t)p.d4 * p.Mp * 4 * 4); }
-  p.off_c2 = off; off = up(off + (size_t)d * d * 4);
   p.set = off;
   p.total = 256 + (size_t)sets * p.set;       // a word that says whether some C2 is dense, then the sets
   return p;
@@ -99,26 +95,49 @@ __device__ __forceinline__ RowAt row_at(const Rows& r, int v) {
 }
 __device__ __forceinline__ long long row_base(const TensorDev& t, int b, int h, int row) { return b * t.sb + h * t.sh + row * t.sl; }
 
-// Eight numbers of a row from column c0 (a multiple of eight) on, zero from `cols` on.
-template <bool FULL = false> __device__ __forceinline__ f32x8 load8(const TensorDev& t, long long base, int c0, int cols) {
-  f32x8 x;
+// Eight numbers of a row from column c0 (a multiple of eight) on, zero from `cols` on: as they lie, so that nothing waits for them until they are
+// expanded.  FULL: rows have no ragged end.
+struct Raw8 { u32x4 a, b; };
+template <bool FULL = false> __device__ __forceinline__ Raw8 fetch8(const TensorDev& t, long long base, int c0, int cols) {
+  Raw8 r{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
   if (FULL || c0 + 8 <= cols) {
     if (t.dtype == 0) {
-      const f32x4 a = *(const f32x4*)((const float*)t.ptr + base + c0), b = *(const f32x4*)((const float*)t.ptr + base + c0 + 4);
-      x = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      r.a = *(const u32x4*)((const float*)t.ptr + base + c0);
+      r.b = *(const u32x4*)((const float*)t.ptr + base + c0 + 4);
     } else {
-      const u32x4 u = *(const u32x4*)((const uint16_t*)t.ptr + base + c0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(u[i] << 16);
-        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-      }
+      r.a = *(const u32x4*)((const uint16_t*)t.ptr + base + c0);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = c0 + i < cols ? load_elem(t, base + c0 + i) : 0.f;
+    for (int i = 0; i < 8; ++i)
+      if (c0 + i < cols) {
+        const uint32_t v = t.dtype == 0 ? ((const uint32_t*)t.ptr)[base + c0 + i] : (uint32_t)((const uint16_t*)t.ptr)[base + c0 + i];
+        if (i < 4) r.a[i] = v;
+        else r.b[i - 4] = v;
+      }
+  }
+  return r;
+}
+template <bool FULL = false> __device__ __forceinline__ f32x8 expand8(const Raw8& r, int dtype, int c0, int cols) {
+  f32x8 x;
+  if (dtype == 0 || (!FULL && c0 + 8 > cols)) {
+    const int up = dtype == 0 ? 0 : 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = __uint_as_float(r.a[i] << up);
+      x[4 + i] = __uint_as_float(r.b[i] << up);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(r.a[i] << 16);
+      x[2 * i + 1] = __uint_as_float(r.a[i] & 0xffff0000u);
+    }
   }
   return x;
+}
+template <bool FULL = false> __device__ __forceinline__ f32x8 load8(const TensorDev& t, long long base, int c0, int cols) {
+  return expand8<FULL>(fetch8<FULL>(t, base, c0, cols), t.dtype, c0, cols);
 }
 __device__ __forceinline__ void store8(const TensorDev& t, long long base, int c0, int cols, f32x8 x) {
   if (c0 + 8 <= cols) {
@@ -171,17 +190,35 @@ __device__ __forceinline__ f32x8 turned8(f32x8 x, int c0, const Turn& t, const f
   }
   return y;
 }
-// Numbers c0 .. c0 + 7 of row v of a state's rows, turned.
-// FULL: the row's numbers come in whole eights (cols is the kernel's width).  TURN: it may be turned at all.
-template <bool FULL, bool TURN>
-__device__ __forceinline__ f32x8 row8(const Rows& r, int b, int state_head, RowAt at, int c0) {
-  if (!FULL && c0 >= r.cols) return f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const long long base = row_base(r.X, b, state_head * r.G + at.head, at.row);
-  const f32x8 x = load8<FULL>(r.X, base, c0, r.cols);
-  if (!TURN || c0 >= r.turn.rot) return x;
-  const float2* cs = r.turn.table + ((long long)b * r.L + at.row) * (r.turn.rot >> 1);
-  return turned8(x, c0, r.turn, cs, 1.f, [&](int c) { return load_elem(r.X, base + c); }, [&](int c) { return load8<FULL>(r.X, base, c, r.cols); });
-}
+// Units of eight numbers 32 s + 8 g .. of a row (s < S), turned: what a lane of group g has of an operand.  All of them are on their way before
+// the first is waited for.
+template <int S, bool FULL, bool TURN> struct RowUnits {
+  Raw8 raw[S], other[TURN ? S : 1];
+  __device__ __forceinline__ void fetch(const TensorDev& X, long long base, int cols, const Turn& turn, bool live, int g) {
+    const int r = turn.rot >> 1;
+    const bool whole = TURN && !turn.interleaved && (r & 7) == 0;        // (a unit's partners are a unit)
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int c0 = 32 * s + 8 * g;
+      raw[s] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+      if (live && (FULL || c0 < cols)) raw[s] = fetch8<FULL>(X, base, c0, cols);
+      if constexpr (TURN)
+        if (live && whole && c0 < turn.rot) other[s] = fetch8<FULL>(X, base, c0 >= r ? c0 - r : c0 + r, cols);
+    }
+  }
+  __device__ __forceinline__ void finish(const TensorDev& X, long long base, int cols, const Turn& turn, const float2* cs, bool live, int g,
+                                         f32x8 (&n)[S]) const {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int c0 = 32 * s + 8 * g;
+      n[s] = expand8<FULL>(raw[s], X.dtype, c0, cols);
+      if constexpr (TURN)
+        if (live && c0 < turn.rot)
+          n[s] = turned8(n[s], c0, turn, cs, 1.f, [&](int c) { return load_elem(X, base + c); },
+                         [&](int c) { return expand8<FULL>(other[s], X.dtype, c, cols); });
+    }
+  }
+};
 
 // The same of a bf16 tensor that is not turned, bits as they are.
 template <bool FULL>
@@ -413,8 +450,13 @@ struct StepArgs {
   int B, H, Hk, dv;
   RotaryDev rot;                 // rot = 0: rows as they are
   int* unread;
+  // (launch_step's own)
+  float *exps, *old_z;           // [B][Hk][1 + H / Hk][Mp] exponents of the key (less its row term) and the queries; [B][Hk][Mp]
+  float2* old_shift;             // [B][Hk] shift before, the key's row term
+  int key_tiles, cols;
 };
-int launch_step(const StepArgs& a, hipStream_t st);
+size_t step_floats(int B, int H, int Hk, int Mp);
+int launch_step(StepArgs a, float* room, hipStream_t st);
 
 }  // namespace st
 }  // namespace fs

@@ -78,8 +78,9 @@ def test_the_other_entry_points_refuse(fs):
     assert L.favorsharp_state_attention(P(f), P(s), None, None, 2, 4, 8, 64, None, None, P(t), None, *ws) == 1
     assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 4, 8, 64, None, None, P(t), None, A, 0, None) == 4
     assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 4, 8, 64, None, None, None, None, *ws) == 1
-    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 2, 3, 64, None, P(t), None, None) == 1
-    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(tensor(fs, dtype=0)), P(t), 2, 4, 64, None, P(t), None, None) == 1
+    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 2, 3, 64, None, P(t), None, *ws) == 1
+    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(tensor(fs, dtype=0)), P(t), 2, 4, 64, None, P(t), None, *ws) == 1
+    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 2, 4, 64, None, P(t), None, A, 512, None) == 4
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, P(t), P(pool(fs, slots=5)), *ws) == 1
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, None, P(ds), *ws) == 1
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, P(t), P(ds), A, 1000, None) == 4
@@ -125,7 +126,8 @@ def test_workspace_sizes(fs):
     assert L.favorsharp_state_append_workspace_bytes(None, 4, 4096, 64, 0) == 0
     assert L.favorsharp_state_append_workspace_bytes(P(f), 4, 4096, 129, 0) == 0
     assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 3, 4096, 64, 0) == 0
-    assert L.favorsharp_state_features_bytes(2, 64, 256, 1, 2) > 2 * 2 * 256 * 64 * (6 + 6 + 4)
+    assert L.favorsharp_state_step_workspace_bytes(P(f), 4, 4) >= 4 * (4 + 2 + 2) * 256 * 4
+    assert L.favorsharp_state_features_bytes(2, 64, 256, 1, 2) > 2 * 2 * 256 * 64 * (4 + 6)
     assert L.favorsharp_state_features_bytes(2, 64, 256, 3, 2) == L.favorsharp_state_features_bytes(2, 64, 4000, 1, 1) == 0
 
 
