@@ -7,6 +7,7 @@
 // the sum over rows.  A wave has a reference of its own, raised when an exponent passes it by 2^16 (never after the first rows, as a
 // rule): features lie up to 2^8 above one at first, so that those far below the largest still split into whole pieces.
 #include <algorithm>
+#include <type_traits>
 
 #include "state_common.h"
 
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(256) k_row_terms(Features f, Rows x, int Hk, c
   const int at = min(row, x.L - 1);
   const long long base = row_base(x.X, b, h, at);
   RowUnits<S, false, true> units;
-  units.fetch(x.X, base, x.cols, x.turn, live, g);
+  units.fetch(x.X, base, x.cols, x.turn, g);
   units.finish(x.X, base, x.cols, x.turn, x.turn.table + ((long long)b * x.L + at) * (x.turn.rot >> 1), live, g, n);
 #pragma unroll
   for (int s = 0; s < S; ++s) most = fmaxf(most, largest_of(n[s]));
@@ -238,7 +239,9 @@ template <bool FULL, bool TURN> struct Four {
   }
 };
 
-template <int W, int XP, int VP, int NW, bool FULL>
+// ONE: whole rows of known type, turned whole in halves or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
+// take 1100 cycles of a wave where their addresses and conditions are found one by one).
+template <int W, int XP, int VP, int NW, bool FULL, bool ONE, bool TURN>
 __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   // a row's numbers in fours: 32 rows of x and of v are N fours a thread each, so that every wave brings as much
   constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 4, NTH = 64 * NW, N = (32 * UPR + NTH - 1) / NTH, LD = W + 8;
@@ -262,15 +265,8 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   bool next_live[N];
   float next_term[N], next_weight[N];
   const float *terms = a.terms ? a.terms + (size_t)bh * rows : nullptr, *weights = a.weights ? a.weights + (size_t)bh * rows : nullptr;
-  // one head: this thread's rows are 32 apart, and so are their addresses
   const int row0 = tid / UPR, c0 = 4 * (tid % UPR);
   constexpr int ROWS = NTH / UPR;            // rows that the threads bring at a time
-  const int v_live = a.x.G == 1 ? v1 : 0;
-  long long x_at = row_base(a.x.X, b, h, v0 + row0), v_at = row_base(a.v.X, b, h, v0 + row0);
-  const float2* cs_at = a.x.turn.table + ((long long)b * a.x.L + v0 + row0) * (a.x.turn.rot >> 1);
-  constexpr int STEP = ROWS < 32 ? ROWS : 32;
-  const long long x_step = STEP * a.x.X.sl, v_step = STEP * a.v.X.sl;
-  const int cs_step = STEP * (a.x.turn.rot >> 1);
   auto fetch = [&](int v) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -280,36 +276,80 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       next_live[i] = false;
       next_term[i] = kNone;
       next_weight[i] = 0.f;
-      const bool mine = 32 * UPR % NTH == 0 || row < 32;
-      if (v_live > 0) {
-        if (mine && v + row < v_live) {
-          next_live[i] = true;
-          next_x[i].get(a.x, x_at, cs_at, c0);
-          next_v[i].get(a.v, v_at, nullptr, c0);
-          next_term[i] = terms ? terms[v + row] : 0.f;
-          next_weight[i] = weights ? weights[v + row] : 1.f;
-        }
-        x_at += x_step;
-        v_at += v_step;
-        if constexpr (XP == 2) cs_at += cs_step;
-      } else {
-        if (!mine || v + row >= v1) continue;
-        const RowAt at = row_at(a.x, v + row);
-        if (at.row >= len) continue;
-        next_live[i] = true;
-        next_x[i].get(a.x, row_base(a.x.X, b, h * a.x.G + at.head, at.row), a.x.turn.table + ((long long)b * a.x.L + at.row) * (a.x.turn.rot >> 1), c0);
-        next_v[i].get(a.v, row_base(a.v.X, b, h * a.v.G + at.head, at.row), nullptr, c0);
-        next_term[i] = terms ? terms[v + row] : 0.f;
-        next_weight[i] = weights ? weights[v + row] : 1.f;
-      }
+      if ((32 * UPR % NTH != 0 && row >= 32) || v + row >= v1) continue;
+      const RowAt at = row_at(a.x, v + row);
+      if (at.row >= len) continue;
+      next_live[i] = true;
+      next_x[i].get(a.x, row_base(a.x.X, b, h * a.x.G + at.head, at.row), a.x.turn.table + ((long long)b * a.x.L + at.row) * (a.x.turn.rot >> 1), c0);
+      next_v[i].get(a.v, row_base(a.v.X, b, h * a.v.G + at.head, at.row), nullptr, c0);
+      next_term[i] = terms ? terms[v + row] : 0.f;
+      next_weight[i] = weights ? weights[v + row] : 1.f;
     }
+  };
+  // (ONE)
+  constexpr int DT = VP == 1 ? 1 : 0;
+  typedef typename std::conditional<DT == 1, u32x2, u32x4>::type quad;
+  quad one_x[N], one_p[N], one_v[N];
+  f32x4 one_cs[N][2];
+  const int half = W / 2, other0 = c0 >= half ? c0 - half : c0 + half, pair0 = c0 >= half ? c0 - half : c0;
+  const float sgn = c0 >= half ? 1.f : -1.f;
+  const float *one_t = terms ? terms : (const float*)a.f.base, *one_w = weights ? weights : (const float*)a.f.base;
+  const int t_step = terms ? 1 : 0, w_step = weights ? 1 : 0;
+  const char *xp = (const char*)a.x.X.ptr, *vp = (const char*)a.v.X.ptr;
+  const long long x0 = row_base(a.x.X, b, h * a.x.G, 0), y0 = row_base(a.v.X, b, h * a.v.G, 0);
+  const float2* cs0 = a.x.turn.table + (long long)b * a.x.L * half;
+  auto fetch_one = [&](int v) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int mine = v + row0 + ROWS * i, at = min(mine, v1 - 1);          // (rows behind the last one are it, and put as zeros)
+      constexpr int E = DT == 1 ? 2 : 4;
+      long long xo = x0 + c0, vo = y0 + c0;
+      int row = at;
+      if (a.x.G > 1) {
+        const int head = at / a.x.L;
+        row -= head * a.x.L;
+        xo += head * a.x.X.sh;
+        vo += head * a.v.X.sh;
+      }
+      next_live[i] = mine < v1 && row < len;
+      xo += row * a.x.X.sl;
+      vo += row * a.v.X.sl;
+      one_x[i] = *(const quad*)(xp + xo * E);
+      one_v[i] = *(const quad*)(vp + vo * E);
+      if constexpr (TURN) {
+        one_p[i] = *(const quad*)(xp + (xo - c0 + other0) * E);
+        const f32x4* cs = (const f32x4*)(cs0 + (long long)row * half + pair0);
+        one_cs[i][0] = cs[0];
+        one_cs[i][1] = cs[1];
+      }
+      next_term[i] = one_t[at * t_step];
+      next_weight[i] = one_w[at * w_step];
+    }
+  };
+  auto numbers = [](quad q) {
+    if constexpr (DT == 1)
+      return f32x4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16), __uint_as_float(q[1] & 0xffff0000u)};
+    else return __builtin_bit_cast(f32x4, q);
   };
   auto put = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = row0 + ROWS * i, u = tid % UPR;
       if (32 * UPR % NTH != 0 && row >= 32) continue;
-      const f32x4 x = next_x[i].put(a.x, 4 * u, next_live[i]);
+      f32x4 x;
+      bool live = next_live[i];
+      if constexpr (ONE) {
+        x = numbers(one_x[i]);
+        if constexpr (TURN) {
+          const f32x4 p = numbers(one_p[i]) * sgn;
+          x = f32x4{x[0] * one_cs[i][0][0] + p[0] * one_cs[i][0][1], x[1] * one_cs[i][0][2] + p[1] * one_cs[i][0][3],
+                    x[2] * one_cs[i][1][0] + p[2] * one_cs[i][1][1], x[3] * one_cs[i][1][2] + p[3] * one_cs[i][1][3]};
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = live ? x[j] : 0.f;
+      } else {
+        x = next_x[i].put(a.x, 4 * u, live);
+      }
       const float most = over_lanes<UPR>(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))), [](float p, float q) { return fmaxf(p, q); });
       const float n = over_lanes<UPR>(x[0] * x[0] + x[1] * x[1] + (x[2] * x[2] + x[3] * x[3]), [](float p, float q) { return p + q; });
       const float scale = up_to_2_14(most);
@@ -320,11 +360,27 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         *(u32x2*)&lds.x[buf][p][row][4 * u] = u32x2{bits[0], bits[1]};
       }
       if (u == 0) {
-        lds.term[buf][row] = a.terms ? next_term[i] : next_term[i] - 0.5f * kLog2e * a.f.scale2 * n;        // (C2 = -I / 2)
-        lds.weight[buf][row] = next_weight[i];
+        const float t = a.terms ? next_term[i] : -0.5f * kLog2e * a.f.scale2 * n;        // (C2 = -I / 2)
+        lds.term[buf][row] = live ? t : kNone;
+        lds.weight[buf][row] = a.weights ? next_weight[i] : 1.f;
         lds.undo[buf][row] = power_inverse(scale);
       }
-      if (VP == 1 && (FULL || 4 * u + 4 <= dv)) {
+      if constexpr (ONE) {
+        quad q = one_v[i];
+#pragma unroll
+        for (int j = 0; j < (DT == 1 ? 2 : 4); ++j) q[j] = live ? q[j] : 0u;
+        if constexpr (DT == 1) {
+          *(u32x2*)&lds.v[buf][0][row][4 * u] = q;
+        } else {
+          const f32x4 y = numbers(q);
+          const Op<VP> o3 = as_op<VP>(f32x8{y[0], y[1], y[2], y[3], 0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int p = 0; p < VP; ++p) {
+            const u32x4 bits = __builtin_bit_cast(u32x4, o3.p[p]);
+            *(u32x2*)&lds.v[buf][p][row][4 * u] = u32x2{bits[0], bits[1]};
+          }
+        }
+      } else if (VP == 1 && (FULL || 4 * u + 4 <= dv)) {
         *(u32x2*)&lds.v[buf][0][row][4 * u] = u32x2{next_v[i].x[0], next_v[i].x[1]};
       } else {
         const f32x4 y = next_v[i].put(a.v, 4 * u, false);
@@ -338,7 +394,11 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     }
   };
 
-  fetch(v0);
+  auto bring = [&](int v) {
+    if constexpr (ONE) fetch_one(v);
+    else fetch(v);
+  };
+  bring(v0);
   Op16<2> wop[S][2];
   float bias[2] = {kNone, kNone}, wscale = 0.f;
   if (active) {
@@ -366,7 +426,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   int buf = 0;
   for (int v = v0; v < v1; v += 32, buf ^= 1) {
     const bool more = v + 32 < v1;
-    if (more) fetch(v + 32);
+    if (more) bring(v + 32);
     if (active) {
       f32x4 E[2][2];             // [tile of rows][tile of features]
 #pragma unroll
@@ -543,9 +603,9 @@ __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
   }
 }
 
-template <int W, int XP, int VP, int NW, bool FULL> int build(const BuildArgs& a, hipStream_t st) {
+template <int W, int XP, int VP, int NW, bool FULL, bool ONE, bool TURN> int build(const BuildArgs& a, hipStream_t st) {
   constexpr size_t lds = sizeof(BuildLds<W, XP, VP>);
-  auto kernel = k_build<W, XP, VP, NW, FULL>;
+  auto kernel = k_build<W, XP, VP, NW, FULL, ONE, TURN>;
   if (lds > 64 * 1024 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return 5;
@@ -553,15 +613,17 @@ template <int W, int XP, int VP, int NW, bool FULL> int build(const BuildArgs& a
   hipLaunchKernelGGL(kernel, dim3(a.nsplit, a.nblock, a.B * a.Hk), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int W, int XP, int VP, bool FULL> int build_waves(const BuildArgs& a, hipStream_t st) {
-  return a.f.p.Mp > 128 ? build<W, XP, VP, 8, FULL>(a, st) : build<W, XP, VP, 4, FULL>(a, st);
-}
-template <int W, bool FULL> int build_pieces(const BuildArgs& a, hipStream_t st) {
-  if (a.v.X.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? build_waves<W, 1, 1, FULL>(a, st) : build_waves<W, 2, 1, FULL>(a, st);
-  return build_waves<W, 2, 3, FULL>(a, st);
+template <int W, int XP, int VP, bool FULL, bool ONE, bool TURN> int build_waves(const BuildArgs& a, hipStream_t st) {
+  return a.f.p.Mp > 128 ? build<W, XP, VP, 8, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, FULL, ONE, TURN>(a, st);
 }
 template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
-  return a.f.d == W && a.dv == W ? build_pieces<W, true>(a, st) : build_pieces<W, false>(a, st);
+  const Turn& t = a.x.turn;
+  const bool bf16 = a.x.X.dtype == 1 && a.v.X.dtype == 1, whole = t.rot == W && !t.interleaved;
+  if (a.f.d == W && a.dv == W && a.x.X.dtype == a.v.X.dtype && (t.rot == 0 || whole)) {
+    if (bf16) return t.rot == 0 ? build_waves<W, 1, 1, true, true, false>(a, st) : build_waves<W, 2, 1, true, true, true>(a, st);
+    return t.rot == 0 ? build_waves<W, 2, 3, true, true, false>(a, st) : build_waves<W, 2, 3, true, true, true>(a, st);
+  }
+  return a.v.X.dtype == 1 ? build_waves<W, 2, 1, false, false, true>(a, st) : build_waves<W, 2, 3, false, false, true>(a, st);
 }
 int join_grid(const JoinArgs& a, int vec) { return std::max(1, std::min((a.M * a.dv / vec + a.M + 255) / 256, 64)); }
 

@@ -142,7 +142,7 @@ template <int W, int XP, int RT, bool FULL> struct RowOps {
   bool live[RT];
   __device__ __forceinline__ void load(const Rows& r, int b, int h, int v0, int rows, int len, int steps, int lane) {
     const int g = lane >> 4, c = lane & 15;
-    RowUnits<S, FULL, XP == 2> units[RT];
+    RowUnits<S, FULL, XP == 2, XP == 1 ? 1 : -1> units[RT];
     long long base[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -150,7 +150,7 @@ template <int W, int XP, int RT, bool FULL> struct RowOps {
       at[rt] = row_at(r, min(v, rows - 1));
       live[rt] = v < rows && at[rt].row < len;
       base[rt] = row_base(r.X, b, h * r.G + at[rt].head, at[rt].row);
-      units[rt].fetch(r.X, base[rt], r.cols, r.turn, live[rt], g);
+      units[rt].fetch(r.X, base[rt], r.cols, r.turn, g);
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -484,8 +484,9 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       if constexpr (RP == 1) {
-        u32x4 n = {0u, 0u, 0u, 0u};
-        if (x.live[rt]) n = row8_bits<FULL>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
+        u32x4 n = row8_bits<FULL>(a.r, b, h, x.at[rt], 32 * s + 8 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = x.live[rt] ? n[i] : 0u;
         rr[rt][s].p[0] = __builtin_bit_cast(bf16x8, n);
       } else {
         f32x8 n = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};

@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256) k_step_exponents(StepArgs a) {
   const long long base = row_base(X, b, keys ? h : h * G + vc % per, 0);
   const Turn turn{nullptr, a.rot.rot, a.rot.interleaved};
   RowUnits<S, false, true> units;
-  units.fetch(X, base, d, turn, true, g);
+  units.fetch(X, base, d, turn, g);
   for (int e = tid; e < 16 * pairs; e += 256) {
     const int r = e / pairs, i = e - r * pairs, row = min(v0 + r, rows - 1);
     angles[r][i] = cos_sin(position_of(a.rot, row / per, 0), a.rot.freqs[i], a.rot.amplitude);

@@ -97,11 +97,12 @@ __device__ __forceinline__ long long row_base(const TensorDev& t, int b, int h, 
 
 // Eight numbers of a row from column c0 (a multiple of eight) on, zero from `cols` on: as they lie, so that nothing waits for them until they are
 // expanded.  FULL: rows have no ragged end.
+// DT: the tensor's dtype where the kernel is made for one (-1: whichever it is).
 struct Raw8 { u32x4 a, b; };
-template <bool FULL = false> __device__ __forceinline__ Raw8 fetch8(const TensorDev& t, long long base, int c0, int cols) {
+template <bool FULL = false, int DT = -1> __device__ __forceinline__ Raw8 fetch8(const TensorDev& t, long long base, int c0, int cols) {
   Raw8 r{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
   if (FULL || c0 + 8 <= cols) {
-    if (t.dtype == 0) {
+    if (DT == 0 || (DT < 0 && t.dtype == 0)) {
       r.a = *(const u32x4*)((const float*)t.ptr + base + c0);
       r.b = *(const u32x4*)((const float*)t.ptr + base + c0 + 4);
     } else {
@@ -118,8 +119,9 @@ template <bool FULL = false> __device__ __forceinline__ Raw8 fetch8(const Tensor
   }
   return r;
 }
-template <bool FULL = false> __device__ __forceinline__ f32x8 expand8(const Raw8& r, int dtype, int c0, int cols) {
+template <bool FULL = false, int DT = -1> __device__ __forceinline__ f32x8 expand8(const Raw8& r, int any_dtype, int c0, int cols) {
   f32x8 x;
+  const int dtype = DT < 0 ? any_dtype : DT;
   if (dtype == 0 || (!FULL && c0 + 8 > cols)) {
     const int up = dtype == 0 ? 0 : 16;
 #pragma unroll
@@ -192,18 +194,23 @@ __device__ __forceinline__ f32x8 turned8(f32x8 x, int c0, const Turn& t, const f
 }
 // Units of eight numbers 32 s + 8 g .. of a row (s < S), turned: what a lane of group g has of an operand.  All of them are on their way before
 // the first is waited for.
-template <int S, bool FULL, bool TURN> struct RowUnits {
+// live: the row is there (others are zeros; what is read for them is some row of the tensor).
+template <int S, bool FULL, bool TURN, int DT = -1> struct RowUnits {
   Raw8 raw[S], other[TURN ? S : 1];
-  __device__ __forceinline__ void fetch(const TensorDev& X, long long base, int cols, const Turn& turn, bool live, int g) {
+  __device__ __forceinline__ void fetch(const TensorDev& X, long long base, int cols, const Turn& turn, int g) {
     const int r = turn.rot >> 1;
     const bool whole = TURN && !turn.interleaved && (r & 7) == 0;        // (a unit's partners are a unit)
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c0 = 32 * s + 8 * g;
-      raw[s] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-      if (live && (FULL || c0 < cols)) raw[s] = fetch8<FULL>(X, base, c0, cols);
+      if (FULL) {
+        raw[s] = fetch8<FULL, DT>(X, base, c0, cols);
+      } else {
+        raw[s] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+        if (c0 < cols) raw[s] = fetch8<FULL, DT>(X, base, c0, cols);
+      }
       if constexpr (TURN)
-        if (live && whole && c0 < turn.rot) other[s] = fetch8<FULL>(X, base, c0 >= r ? c0 - r : c0 + r, cols);
+        if (whole && c0 < turn.rot) other[s] = fetch8<FULL, DT>(X, base, c0 >= r ? c0 - r : c0 + r, cols);
     }
   }
   __device__ __forceinline__ void finish(const TensorDev& X, long long base, int cols, const Turn& turn, const float2* cs, bool live, int g,
@@ -211,11 +218,13 @@ template <int S, bool FULL, bool TURN> struct RowUnits {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c0 = 32 * s + 8 * g;
-      n[s] = expand8<FULL>(raw[s], X.dtype, c0, cols);
+      n[s] = expand8<FULL, DT>(raw[s], X.dtype, c0, cols);
       if constexpr (TURN)
-        if (live && c0 < turn.rot)
+        if (c0 < turn.rot)
           n[s] = turned8(n[s], c0, turn, cs, 1.f, [&](int c) { return load_elem(X, base + c); },
-                         [&](int c) { return expand8<FULL>(other[s], X.dtype, c, cols); });
+                         [&](int c) { return expand8<FULL, DT>(other[s], X.dtype, c, cols); });
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[s][i] = live ? n[s][i] : 0.f;
     }
   }
 };
