@@ -241,22 +241,23 @@ template <bool FULL, bool TURN> struct Four {
 
 // ONE: whole rows of known type, turned whole in halves or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
 // take 1100 cycles of a wave where their addresses and conditions are found one by one).
-template <int W, int XP, int VP, int NW, bool FULL, bool ONE, bool TURN>
+template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
 __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
-  // a row's numbers in fours: 32 rows of x and of v are N fours a thread each, so that every wave brings as much
-  constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 4, NTH = 64 * NW, N = (32 * UPR + NTH - 1) / NTH, LD = W + 8;
+  // a row's numbers in fours: N of x and N of v for a thread, or of one of them where there are threads for both (APART)
+  constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 4, NTH = 64 * NW, ROWS = (NTH < 32 * UPR ? NTH : 32 * UPR) / UPR, N = 32 / ROWS, LD = W + 8;
+  constexpr bool APART = NTH >= 64 * UPR;
   extern __shared__ __align__(16) char lds_raw[];
   BuildLds<W, XP, VP>& lds = *(BuildLds<W, XP, VP>*)lds_raw;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
   const int split = blockIdx.x, bh = blockIdx.z, b = bh / a.Hk, h = bh - b * a.Hk;
-  const int fb = blockIdx.y * NW + w, nfb = a.f.p.Mp / 32, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv;
+  const int tile = (blockIdx.y * NW + w) * FT, ntiles = a.f.p.Mp / 16, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv;
   const int slot = slot_of(a.slots, a.nslots, b);
   if (a.old_shift != nullptr && split == 0 && blockIdx.y == 0 && tid == 0) a.old_shift[bh] = slot >= 0 ? a.shift[(size_t)slot * a.Hk + h] : kNone;
   const int len = length_of(a.x, b), rows = a.x.L * a.x.G;
   const int v0 = split * a.rows_per_split, v1 = slot < 0 ? 0 : min(a.x.G == 1 ? len : rows, v0 + a.rows_per_split);
-  const bool active = fb < nfb;
+  const bool active = tile < ntiles;
   if (v0 >= v1) {
-    if (active && lane == 0) a.refs[((size_t)bh * a.nsplit + split) * nfb + fb] = make_float2(0.f, kNone);
+    if (active && lane < FT) a.refs[((size_t)bh * a.nsplit + split) * ntiles + tile + lane] = make_float2(0.f, kNone);
     return;
   }
   const char* set = a.f.set(h);
@@ -265,8 +266,8 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   bool next_live[N];
   float next_term[N], next_weight[N];
   const float *terms = a.terms ? a.terms + (size_t)bh * rows : nullptr, *weights = a.weights ? a.weights + (size_t)bh * rows : nullptr;
-  const int row0 = tid / UPR, c0 = 4 * (tid % UPR);
-  constexpr int ROWS = NTH / UPR;            // rows that the threads bring at a time
+  const int row0 = (APART ? tid % (32 * UPR) : tid) / UPR, c0 = 4 * (tid % UPR);
+  const bool do_x = !APART || w < UPR / 2, do_v = !APART || (w >= UPR / 2 && w < UPR);       // (32 UPR threads are UPR / 2 waves)
   auto fetch = [&](int v) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -276,12 +277,12 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       next_live[i] = false;
       next_term[i] = kNone;
       next_weight[i] = 0.f;
-      if ((32 * UPR % NTH != 0 && row >= 32) || v + row >= v1) continue;
+      if (v + row >= v1) continue;
       const RowAt at = row_at(a.x, v + row);
       if (at.row >= len) continue;
       next_live[i] = true;
-      next_x[i].get(a.x, row_base(a.x.X, b, h * a.x.G + at.head, at.row), a.x.turn.table + ((long long)b * a.x.L + at.row) * (a.x.turn.rot >> 1), c0);
-      next_v[i].get(a.v, row_base(a.v.X, b, h * a.v.G + at.head, at.row), nullptr, c0);
+      if (do_x) next_x[i].get(a.x, row_base(a.x.X, b, h * a.x.G + at.head, at.row), a.x.turn.table + ((long long)b * a.x.L + at.row) * (a.x.turn.rot >> 1), c0);
+      if (do_v) next_v[i].get(a.v, row_base(a.v.X, b, h * a.v.G + at.head, at.row), nullptr, c0);
       next_term[i] = terms ? terms[v + row] : 0.f;
       next_weight[i] = weights ? weights[v + row] : 1.f;
     }
@@ -314,16 +315,18 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
       next_live[i] = mine < v1 && row < len;
       xo += row * a.x.X.sl;
       vo += row * a.v.X.sl;
-      one_x[i] = *(const quad*)(xp + xo * E);
-      one_v[i] = *(const quad*)(vp + vo * E);
-      if constexpr (TURN) {
-        one_p[i] = *(const quad*)(xp + (xo - c0 + other0) * E);
-        const f32x4* cs = (const f32x4*)(cs0 + (long long)row * half + pair0);
-        one_cs[i][0] = cs[0];
-        one_cs[i][1] = cs[1];
+      if (do_v) one_v[i] = *(const quad*)(vp + vo * E);
+      if (do_x) {
+        one_x[i] = *(const quad*)(xp + xo * E);
+        if constexpr (TURN) {
+          one_p[i] = *(const quad*)(xp + (xo - c0 + other0) * E);
+          const f32x4* cs = (const f32x4*)(cs0 + (long long)row * half + pair0);
+          one_cs[i][0] = cs[0];
+          one_cs[i][1] = cs[1];
+        }
+        next_term[i] = one_t[at * t_step];
+        next_weight[i] = one_w[at * w_step];
       }
-      next_term[i] = one_t[at * t_step];
-      next_weight[i] = one_w[at * w_step];
     }
   };
   auto numbers = [](quad q) {
@@ -335,9 +338,9 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = row0 + ROWS * i, u = tid % UPR;
-      if (32 * UPR % NTH != 0 && row >= 32) continue;
+      const bool live = next_live[i];
+      if (do_x) {
       f32x4 x;
-      bool live = next_live[i];
       if constexpr (ONE) {
         x = numbers(one_x[i]);
         if constexpr (TURN) {
@@ -365,6 +368,8 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         lds.weight[buf][row] = a.weights ? next_weight[i] : 1.f;
         lds.undo[buf][row] = power_inverse(scale);
       }
+      }
+      if (!do_v) continue;
       if constexpr (ONE) {
         quad q = one_v[i];
 #pragma unroll
@@ -399,28 +404,30 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     else fetch(v);
   };
   bring(v0);
-  Op16<2> wop[S][2];
-  float bias[2] = {kNone, kNone}, wscale = 0.f;
+  Op16<2> wop[S][FT];
+  float bias[FT], wscale = 0.f;
   if (active) {
-    const uint16_t* img = (const uint16_t*)(set + a.f.p.off_row[a.side]) + (size_t)fb * steps * 2 * 1024;
+    const uint16_t* img = (const uint16_t*)(set + a.f.p.off_row[a.side]) + (size_t)(tile >> 1) * steps * 2 * 1024 + (tile & 1) * 512;
 #pragma unroll
     for (int s = 0; s < S; ++s)
       if (FULL || s < steps)
 #pragma unroll
-        for (int ft = 0; ft < 2; ++ft)
+        for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
           for (int p = 0; p < 2; ++p) wop[s][ft].p[p] = *(const f16x8*)(img + (s * 2 + p) * 1024 + ft * 512 + lane * 8);
 #pragma unroll
-    for (int ft = 0; ft < 2; ++ft) bias[ft] = ((const float*)(set + a.f.p.off_bias))[32 * fb + 16 * ft + c];
-    wscale = ((const float*)(set + a.f.p.off_scale[a.side]))[fb];
+    for (int ft = 0; ft < FT; ++ft) bias[ft] = ((const float*)(set + a.f.p.off_bias))[16 * (tile + ft) + c];
+    wscale = ((const float*)(set + a.f.p.off_scale[a.side]))[tile >> 1];
   }
-  f32x4 T[2][VT];
-  float z[2] = {0.f, 0.f}, ref = 0.f, top = kNone;
+  f32x4 T[FT][VT];
+  float z[FT], ref = 0.f, top = kNone;
   bool referred = false;
 #pragma unroll
-  for (int ft = 0; ft < 2; ++ft)
+  for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt) T[ft][vt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) z[ft] = 0.f;
   put(0);
   __syncthreads();
   int buf = 0;
@@ -428,9 +435,11 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     const bool more = v + 32 < v1;
     if (more) bring(v + 32);
     if (active) {
-      f32x4 E[2][2];             // [tile of rows][tile of features]
+      f32x4 E[2][FT];            // [tile of rows][tile of features]
 #pragma unroll
-      for (int t = 0; t < 2; ++t) E[t][0] = E[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int ft = 0; ft < FT; ++ft) E[t][ft] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < S; ++s)
         if (FULL || s < steps) {
@@ -448,7 +457,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         const f32x4 term = *(const f32x4*)&lds.term[buf][16 * t + 4 * g], undo = *(const f32x4*)&lds.undo[buf][16 * t + 4 * g] * wscale;
         weight[t] = *(const f32x4*)&lds.weight[buf][16 * t + 4 * g];
 #pragma unroll
-        for (int ft = 0; ft < 2; ++ft)
+        for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             E[t][ft][r] = E[t][ft][r] * undo[r] + (bias[ft] + (term[r] - ref));
@@ -464,7 +473,7 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
         ref += up;
         referred = true;
 #pragma unroll
-        for (int ft = 0; ft < 2; ++ft) {
+        for (int ft = 0; ft < FT; ++ft) {
           z[ft] *= keep;
 #pragma unroll
           for (int vt = 0; vt < VT; ++vt) T[ft][vt] *= keep;
@@ -472,9 +481,9 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
           for (int t = 0; t < 2; ++t) E[t][ft] -= up;
         }
       }
-      Op<3> so[2];
+      Op<3> so[FT];
 #pragma unroll
-      for (int ft = 0; ft < 2; ++ft) {
+      for (int ft = 0; ft < FT; ++ft) {
         f32x8 sv;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -501,10 +510,10 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
   const size_t at = (size_t)bh * a.nsplit + split;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (lane == 0) a.refs[at * nfb + fb] = make_float2(ref, top);
+  if (lane < FT) a.refs[at * ntiles + tile + lane] = make_float2(ref, top);
 #pragma unroll
-  for (int ft = 0; ft < 2; ++ft) {
-    const int m0 = 32 * fb + 16 * ft;
+  for (int ft = 0; ft < FT; ++ft) {
+    const int m0 = 16 * (tile + ft);
     float zs = z[ft];
     zs += __shfl_xor(zs, 16);
     zs += __shfl_xor(zs, 32);
@@ -539,7 +548,7 @@ template <int VEC>
 __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
   __shared__ float weight[kJoinWeights], tmp[4];
   typedef __attribute__((ext_vector_type(VEC))) float vec;
-  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, tid = threadIdx.x, nfb = a.Mp / 32;
+  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, tid = threadIdx.x, nfb = a.Mp / 16;
   const int slot = unique_slot_of(a.slots, a.state.slots, b);
   if (slot < 0) {
     if (blockIdx.x == 0 && h == 0 && tid == 0 && a.left_out != nullptr) atomicAdd(a.left_out, 1);
@@ -558,7 +567,7 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
   const int nt = a.M * a.dv / VEC;
   for (int e = blockIdx.x * 256 + tid; e < nt + a.M; e += gridDim.x * 256) {
     if (e < nt) {
-      const int m = e * VEC / a.dv, fb = m >> 5;
+      const int m = e * VEC / a.dv, fb = m >> 4;
       vec* to = (vec*)(a.state.T + at * a.M * a.dv) + e;
       const vec* from = (const vec*)(a.part + (size_t)bh * a.nsplit * a.M * a.dv) + e;
       vec x = {};
@@ -566,7 +575,7 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
       sum_parts(x, from, nt, a.nsplit, [&](int s) { return weight[s * nfb + fb]; });
       *to = x;
     } else {
-      const int m = e - nt, fb = m >> 5;
+      const int m = e - nt, fb = m >> 4;
       float* to = a.state.z + at * a.M + m;
       float x = keep != 0.f ? keep * *to : 0.f;
       sum_parts(x, a.zpart + (size_t)bh * a.nsplit * a.M + m, a.M, a.nsplit, [&](int s) { return weight[s * nfb + fb]; });
@@ -579,10 +588,10 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
 template <int VEC>
 __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
   typedef __attribute__((ext_vector_type(VEC))) float vec;
-  const int sh = blockIdx.y, slot = sh / a.Hk, h = sh - slot * a.Hk, nfb = a.Mp / 32, nt = a.M * a.dv / VEC;
+  const int sh = blockIdx.y, slot = sh / a.Hk, h = sh - slot * a.Hk, nfb = a.Mp / 16, nt = a.M * a.dv / VEC;
   const int b0 = a.slots ? 0 : slot, b1 = a.slots ? a.B : min(slot + 1, a.B);
   for (int e = blockIdx.x * 256 + threadIdx.x; e < nt + a.M; e += gridDim.x * 256) {
-    const int m = e < nt ? e * VEC / a.dv : e - nt, fb = m >> 5;
+    const int m = e < nt ? e * VEC / a.dv : e - nt, fb = m >> 4;
     vec x = {};
     for (int b = b0; b < b1; ++b) {
       if (slot_of(a.slots, a.state.slots, b) != slot) continue;
@@ -603,18 +612,22 @@ __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
   }
 }
 
-template <int W, int XP, int VP, int NW, bool FULL, bool ONE, bool TURN> int build(const BuildArgs& a, hipStream_t st) {
+template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN> int build(const BuildArgs& a, hipStream_t st) {
   constexpr size_t lds = sizeof(BuildLds<W, XP, VP>);
-  auto kernel = k_build<W, XP, VP, NW, FULL, ONE, TURN>;
+  auto kernel = k_build<W, XP, VP, NW, FT, FULL, ONE, TURN>;
   if (lds > 64 * 1024 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return 5;
   }
-  hipLaunchKernelGGL(kernel, dim3(a.nsplit, a.nblock, a.B * a.Hk), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(a.nsplit, (a.f.p.Mp / 16 + NW * FT - 1) / (NW * FT), a.B * a.Hk), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int VP, bool FULL, bool ONE, bool TURN> int build_waves(const BuildArgs& a, hipStream_t st) {
-  return a.f.p.Mp > 128 ? build<W, XP, VP, 8, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, FULL, ONE, TURN>(a, st);
+  // sixteen features a wave and sixteen waves, four to a SIMD, where the rows of W and of the sum leave a wave 128 registers; else 32
+  if constexpr (W <= 64 && ONE) return a.f.p.Mp > 64 ? build<W, XP, VP, 16, 1, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 1, FULL, ONE, TURN>(a, st);
+  else if constexpr (W <= 64) return a.f.p.Mp > 64 ? build<W, XP, VP, 8, 2, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 1, FULL, ONE, TURN>(a, st);
+  else if constexpr (ONE) return a.f.p.Mp > 128 ? build<W, XP, VP, 8, 2, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 2, FULL, ONE, TURN>(a, st);
+  else return build<W, XP, VP, 4, 2, FULL, ONE, TURN>(a, st);
 }
 template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
   const Turn& t = a.x.turn;

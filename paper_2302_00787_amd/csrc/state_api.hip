@@ -50,21 +50,21 @@ st::State state_of(const fs_state* s) { return st::State{s->T, s->z, s->shift, s
 
 // Sums over `rows` rows of every state (append; gradient of a state): splits of the rows, and what a call keeps between its launches.
 struct SumPlan {
-  int nblock, nsplit, rows_per_split;
+  int nsplit, rows_per_split;
   size_t off_table, off_terms, off_weights, off_old, off_refs, off_part, off_zpart, total;
 };
 SumPlan plan_sum(int BH, long long tokens, long long rows, int d, int dv, int M, int rot, bool terms, bool weights, bool sums) {
   SumPlan p;
-  const int Mp = (M + 31) / 32 * 32, waves = Mp > 128 ? 8 : 4;
-  p.nblock = ceil_div(Mp / 32, waves);
+  const int Mp = (M + 31) / 32 * 32;
+  const int nblock = ceil_div(Mp, st::build_features(d, dv, Mp));
   // splits of the rows: passes of 256 workgroups, each its start and its chunks of 32 rows, and a partial state written and read for
   // every split (measured, us: a chunk of 64 numbers a row 1, of 128 2.5; a start 5; 4 TB/s)
   const int wide = d > 64 || dv > 64;
-  const long long chunks = std::max<long long>(1, (rows + 31) / 32), most = std::min<long long>({chunks, 64, 4096 / (Mp / 32)});
+  const long long chunks = std::max<long long>(1, (rows + 31) / 32), most = std::min<long long>({chunks, 64, 4096 / (Mp / 16)});
   double best = 0.0;
   long long n = 1;
   for (long long k = 1; k <= most; ++k) {
-    const long long per = (chunks + k - 1) / k, used = (chunks + per - 1) / per, passes = (BH * used * p.nblock + 255) / 256;
+    const long long per = (chunks + k - 1) / k, used = (chunks + per - 1) / per, passes = (BH * used * nblock + 255) / 256;
     const double us = (double)passes * (5.0 + (double)per * (wide ? 2.5 : 1.0)) + (double)BH * used * M * (dv + 1) * 8 / 4e6;
     if (k == 1 || us < best) { best = us; n = used; }
   }
@@ -76,7 +76,7 @@ SumPlan plan_sum(int BH, long long tokens, long long rows, int d, int dv, int M,
   p.off_weights = off; off = align_up(off + (weights ? (size_t)BH * rows * sizeof(float) : 0));
   const size_t parts = sums ? (size_t)BH * p.nsplit : 0;
   p.off_old = off; off = align_up(off + (sums ? (size_t)BH * sizeof(float) : 0));
-  p.off_refs = off; off = align_up(off + parts * (Mp / 32) * sizeof(float2));
+  p.off_refs = off; off = align_up(off + parts * (Mp / 16) * sizeof(float2));
   p.off_part = off; off = align_up(off + parts * M * dv * sizeof(float));
   p.off_zpart = off; off = align_up(off + parts * M * sizeof(float));
   p.total = std::max(off, kAlign);
@@ -202,7 +202,7 @@ int favorsharp_state_append(const fs_features* f, const fs_state* state, const i
   a.v = st::Rows{dev(V), L, 1, lengths, dv, st::Turn{}};
   a.slots = slots; a.nslots = state->slots;
   a.B = B; a.Hk = f->heads; a.dv = dv;
-  a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split; a.nblock = p.nblock;
+  a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split;
   a.part = (float*)(ws + p.off_part); a.zpart = (float*)(ws + p.off_zpart); a.refs = (float2*)(ws + p.off_refs);
   if (!fresh) { a.shift = state->shift; a.old_shift = (float*)(ws + p.off_old); }
   if (L > 0) {
@@ -307,7 +307,7 @@ int favorsharp_state_attention_backward(const fs_features* f, const fs_state* st
   a.terms = g.lse; a.weights = g.weights;
   a.slots = slots; a.nslots = state->slots;
   a.B = B; a.Hk = f->heads; a.dv = dv;
-  a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split; a.nblock = p.nblock;
+  a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split;
   a.part = (float*)(ws + p.off_part); a.zpart = (float*)(ws + p.off_zpart); a.refs = (float2*)(ws + p.off_refs);
   if (int rc = st::launch_build(a, s)) return rc;
   st::JoinArgs j{a.part, a.zpart, a.refs, nullptr, slots, state_of(dstate), B, f->heads, f->M, a.f.p.Mp, dv, p.nsplit, nullptr};

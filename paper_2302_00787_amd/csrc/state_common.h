@@ -394,12 +394,13 @@ struct BuildArgs {
   const int32_t* slots;
   int nslots;
   int B, Hk, dv;
-  int nsplit, rows_per_split, nblock;
+  int nsplit, rows_per_split;
   float *part, *zpart;           // [B*Hk][nsplit][M][dv], [B*Hk][nsplit][M]
-  float2* refs;                  // [B*Hk][nsplit][Mp / 32]: reference and largest exponent (-inf: nothing summed)
+  float2* refs;                  // [B*Hk][nsplit][Mp / 16]: reference and largest exponent (-inf: nothing summed)
   const float* shift;            // of the pool, copied to old_shift (nullptr: not)
   float* old_shift;              // [B*Hk]
 };
+inline int build_features(int d, int dv, int Mp) { return width_class(d, dv) <= 64 ? (Mp > 64 ? 256 : 64) : (Mp > 128 ? 256 : 128); }     // of a workgroup
 int launch_build(const BuildArgs& a, hipStream_t st);
 // Partial sums onto the states (append), or their sum alone (gradients: slots that no sequence names get zeros).
 struct JoinArgs {
