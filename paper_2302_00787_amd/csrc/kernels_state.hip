@@ -239,27 +239,60 @@ template <bool FULL, bool TURN> struct Four {
   }
 };
 
+// How the rows of a call are shared out.  Chunks of 32 rows, head by head and sequence by sequence, are one line that `nwg` workgroups cut into
+// equal pieces, so that a padded batch keeps all of them busy alike; what a workgroup sums of one state is a part, number (workgroup +
+// states before).  nwg = 0: a workgroup and a part for every state.
+struct Shares {
+  const Rows& x;
+  const int32_t* slots;
+  int nslots, B, Hk, nwg;
+  __device__ __forceinline__ int rows_of(int b) const {
+    const int len = slot_of(slots, nslots, b) < 0 ? 0 : length_of(x, b);
+    return x.G == 1 || len == 0 ? len : x.L * x.G;
+  }
+  __device__ __forceinline__ int chunks_of(int b) const { return (rows_of(b) + 31) / 32; }
+  __device__ __forceinline__ static int scan(int v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int t = __shfl_up(v, o);
+      if (lane >= o) v += t;
+    }
+    return v;
+  }
+  // chunks of the sequences before b of one head (b = B: of all); each wave for itself
+  __device__ __forceinline__ long long before(int b, int lane) const {
+    long long sum = 0;
+    for (int b0 = 0; b0 < b; b0 += 64) sum += __builtin_amdgcn_readlane(scan(b0 + lane < b ? chunks_of(b0 + lane) : 0, lane), 63);
+    return sum;
+  }
+  // the sequence of chunk q of a head, and the chunks before it
+  __device__ __forceinline__ int find(long long q, int lane, long long* first) const {
+    long long sum = 0;
+    for (int b0 = 0;; b0 += 64) {
+      const int n = b0 + lane < B ? chunks_of(b0 + lane) : 0, upto = scan(n, lane);
+      const unsigned long long behind = __ballot(sum + upto > q);
+      if (behind != 0ull || b0 + 64 >= B) {
+        const int l = behind != 0ull ? __builtin_ctzll(behind) : 63;
+        *first = sum + __builtin_amdgcn_readlane(upto - n, l);
+        return b0 + l;
+      }
+      sum += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  __device__ __forceinline__ static long long start(long long i, long long total, long long n) { return i * total / n; }
+};
+
 // ONE: whole rows of known type, turned whole in halves or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
 // take 1100 cycles of a wave where their addresses and conditions are found one by one).
 template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
-__global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
+__device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, VP>& lds, int b, int h, int v0, int v1, size_t part) {
   // a row's numbers in fours: N of x and N of v for a thread, or of one of them where there are threads for both (APART)
   constexpr int S = STEPS<W>, VT = TILES<W>, UPR = W / 4, NTH = 64 * NW, ROWS = (NTH < 32 * UPR ? NTH : 32 * UPR) / UPR, N = 32 / ROWS, LD = W + 8;
   constexpr bool APART = NTH >= 64 * UPR;
-  extern __shared__ __align__(16) char lds_raw[];
-  BuildLds<W, XP, VP>& lds = *(BuildLds<W, XP, VP>*)lds_raw;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-  const int split = blockIdx.x, bh = blockIdx.z, b = bh / a.Hk, h = bh - b * a.Hk;
-  const int tile = (blockIdx.y * NW + w) * FT, ntiles = a.f.p.Mp / 16, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv;
-  const int slot = slot_of(a.slots, a.nslots, b);
-  if (a.old_shift != nullptr && split == 0 && blockIdx.y == 0 && tid == 0) a.old_shift[bh] = slot >= 0 ? a.shift[(size_t)slot * a.Hk + h] : kNone;
+  const int bh = b * a.Hk + h, tile = (blockIdx.y * NW + w) * FT, ntiles = a.f.p.Mp / 16, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv;
   const int len = length_of(a.x, b), rows = a.x.L * a.x.G;
-  const int v0 = split * a.rows_per_split, v1 = slot < 0 ? 0 : min(a.x.G == 1 ? len : rows, v0 + a.rows_per_split);
   const bool active = tile < ntiles;
-  if (v0 >= v1) {
-    if (active && lane < FT) a.refs[((size_t)bh * a.nsplit + split) * ntiles + tile + lane] = make_float2(0.f, kNone);
-    return;
-  }
   const char* set = a.f.set(h);
   Four<FULL, XP == 2> next_x[N];
   Four<FULL, false> next_v[N];
@@ -507,38 +540,83 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
     __syncthreads();
   }
   if (!active) return;
-  const size_t at = (size_t)bh * a.nsplit + split;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (lane < FT) a.refs[at * ntiles + tile + lane] = make_float2(ref, top);
+  if (lane < FT) a.refs[part * ntiles + tile + lane] = make_float2(ref, top);
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) {
     const int m0 = 16 * (tile + ft);
     float zs = z[ft];
     zs += __shfl_xor(zs, 16);
     zs += __shfl_xor(zs, 32);
-    if (g == 0 && m0 + c < a.f.M) a.zpart[at * a.f.M + m0 + c] = zs;
+    if (g == 0 && m0 + c < a.f.M) a.zpart[part * a.f.M + m0 + c] = zs;
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt)
       if (FULL || 16 * vt + c < dv)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (m0 + 4 * g + r < a.f.M) a.part[(at * a.f.M + m0 + 4 * g + r) * dv + 16 * vt + c] = T[ft][vt][r];
+          if (m0 + 4 * g + r < a.f.M) a.part[(part * a.f.M + m0 + 4 * g + r) * dv + 16 * vt + c] = T[ft][vt][r];
+  }
+}
+
+template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
+__global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
+  extern __shared__ __align__(16) char lds_raw[];
+  BuildLds<W, XP, VP>& lds = *(BuildLds<W, XP, VP>*)lds_raw;
+  const int lane = threadIdx.x & 63;
+  const Shares shares{a.x, a.slots, a.nslots, a.B, a.Hk, a.nwg};
+  // the state's shift as it is before the call, for the join, by whoever has its first rows
+  auto keep_shift = [&](int b, int h) {
+    if (a.old_shift != nullptr && blockIdx.y == 0 && threadIdx.x == 0) {
+      const int slot = slot_of(a.slots, a.nslots, b);
+      a.old_shift[b * a.Hk + h] = slot >= 0 ? a.shift[(size_t)slot * a.Hk + h] : kNone;
+    }
+  };
+  if (a.nwg == 0) {
+    const int b = blockIdx.x / a.Hk, h = blockIdx.x - b * a.Hk, rows = shares.rows_of(b);
+    keep_shift(b, h);
+    if (blockIdx.y == 0 && threadIdx.x == 0) a.parts[blockIdx.x] = make_int2(blockIdx.x, rows > 0 ? 1 : 0);
+    if (rows > 0) build_part<W, XP, VP, NW, FT, FULL, ONE, TURN>(a, lds, b, h, 0, rows, blockIdx.x);
+    return;
+  }
+  const long long C = shares.before(a.B, lane), total = C * a.Hk, n = min((long long)a.nwg, total);
+  // the parts of the states, for the join
+  if (blockIdx.y == 0 && threadIdx.x >= 64 * (NW - 1))
+    for (int bh = blockIdx.x; bh < a.B * a.Hk; bh += gridDim.x) {
+      const int b = bh / a.Hk, h = bh - b * a.Hk;
+      const long long S = h * C + shares.before(b, lane), mine = shares.chunks_of(b);
+      const long long i0 = mine > 0 ? ((S + 1) * n - 1) / total : 0, i1 = mine > 0 ? ((S + mine) * n - 1) / total : -1;
+      if (lane == 0) a.parts[bh] = make_int2((int)(i0 + (long long)h * a.B + b), (int)(i1 - i0 + 1));
+    }
+  if ((long long)blockIdx.x >= n) return;
+  long long q = Shares::start(blockIdx.x, total, n);
+  const long long end = Shares::start((long long)blockIdx.x + 1, total, n);
+  while (q < end) {
+    const int h = (int)(q / C);
+    long long first;
+    const int b = shares.find(q - h * C, lane, &first);
+    const long long at = q - h * C - first, here = min(end - q, shares.chunks_of(b) - at);
+    if (at == 0) keep_shift(b, h);
+    build_part<W, XP, VP, NW, FT, FULL, ONE, TURN>(a, lds, b, h, (int)(32 * at), min((int)(32 * (at + here)), shares.rows_of(b)),
+                                                  (size_t)blockIdx.x + (size_t)h * a.B + b);
+    q += here;
   }
 }
 
 // ---------------------------------------------------------------------------------------------- join
-constexpr int kJoinWeights = 4096;       // references of a state's partial sums: at most 64 splits of 2048 features
-
-// x += sum of weight(s) from[s stride]: eight loads on their way at a time.  What has no weight may be anything.
-template <class V, class F> __device__ __forceinline__ void sum_parts(V& x, const V* from, size_t stride, int n, F weight) {
+// x += the parts' numbers, from their references to `top`: eight loads on their way at a time.
+template <class V> __device__ __forceinline__ void sum_parts(V& x, const V* from, size_t stride, int n, const float2* refs, int ref_stride, float top) {
   for (int s0 = 0; s0 < n; s0 += 8) {
     V v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = from[(size_t)min(s0 + i, n - 1) * stride];
+    float2 ref[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float k = s0 + i < n ? weight(s0 + i) : 0.f;
+      v[i] = from[(size_t)min(s0 + i, n - 1) * stride];
+      ref[i] = refs[min(s0 + i, n - 1) * ref_stride];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float k = s0 + i < n && ref[i].y != kNone ? fast_exp2(ref[i].x - top) : 0.f;
       if (k != 0.f) x += k * v[i];
     }
   }
@@ -546,7 +624,7 @@ template <class V, class F> __device__ __forceinline__ void sum_parts(V& x, cons
 
 template <int VEC>
 __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
-  __shared__ float weight[kJoinWeights], tmp[4];
+  __shared__ float tmp[4];
   typedef __attribute__((ext_vector_type(VEC))) float vec;
   const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, tid = threadIdx.x, nfb = a.Mp / 16;
   const int slot = unique_slot_of(a.slots, a.state.slots, b);
@@ -554,14 +632,14 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
     if (blockIdx.x == 0 && h == 0 && tid == 0 && a.left_out != nullptr) atomicAdd(a.left_out, 1);
     return;
   }
-  const int n = a.nsplit * nfb;
-  const float2* refs = a.refs + (size_t)bh * n;
+  const size_t part = a.parts[bh].x;
+  const int parts = a.parts[bh].y;
+  if (parts == 0 && a.old_shift != nullptr) return;              // nothing was appended: the state is what it was
+  const float2* refs = a.refs + part * nfb;
   const float old = a.old_shift ? a.old_shift[bh] : kNone;
   float top = old;
-  for (int i = tid; i < n; i += 256) top = fmaxf(top, refs[i].y);
+  for (int i = tid; i < parts * nfb; i += 256) top = fmaxf(top, refs[i].y);
   top = block_max(top, tmp);
-  for (int i = tid; i < n; i += 256) weight[i] = refs[i].y == kNone ? 0.f : fast_exp2(refs[i].x - top);
-  __syncthreads();
   const float keep = old == kNone ? 0.f : fast_exp2(old - top);
   const size_t at = (size_t)slot * a.Hk + h;
   const int nt = a.M * a.dv / VEC;
@@ -569,16 +647,15 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
     if (e < nt) {
       const int m = e * VEC / a.dv, fb = m >> 4;
       vec* to = (vec*)(a.state.T + at * a.M * a.dv) + e;
-      const vec* from = (const vec*)(a.part + (size_t)bh * a.nsplit * a.M * a.dv) + e;
       vec x = {};
       if (keep != 0.f) x = keep * *to;
-      sum_parts(x, from, nt, a.nsplit, [&](int s) { return weight[s * nfb + fb]; });
+      sum_parts(x, (const vec*)(a.part + part * a.M * a.dv) + e, nt, parts, refs + fb, nfb, top);
       *to = x;
     } else {
       const int m = e - nt, fb = m >> 4;
       float* to = a.state.z + at * a.M + m;
       float x = keep != 0.f ? keep * *to : 0.f;
-      sum_parts(x, a.zpart + (size_t)bh * a.nsplit * a.M + m, a.M, a.nsplit, [&](int s) { return weight[s * nfb + fb]; });
+      sum_parts(x, a.zpart + part * a.M + m, a.M, parts, refs + fb, nfb, top);
       *to = x;
     }
   }
@@ -595,15 +672,12 @@ __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
     vec x = {};
     for (int b = b0; b < b1; ++b) {
       if (slot_of(a.slots, a.state.slots, b) != slot) continue;
-      const size_t at = ((size_t)b * a.Hk + h) * a.nsplit;
-      auto weight = [&](int s) {
-        const float2 ref = a.refs[(at + s) * nfb + fb];
-        return ref.y == kNone ? 0.f : fast_exp2(ref.x);
-      };
-      if (e < nt) sum_parts(x, (const vec*)(a.part + at * a.M * a.dv) + e, nt, a.nsplit, weight);
+      const size_t part = a.parts[b * a.Hk + h].x;
+      const int parts = a.parts[b * a.Hk + h].y;
+      if (e < nt) sum_parts(x, (const vec*)(a.part + part * a.M * a.dv) + e, nt, parts, a.refs + part * nfb + fb, nfb, 0.f);
       else {
         float y = x[0];
-        sum_parts(y, a.zpart + at * a.M + m, a.M, a.nsplit, weight);
+        sum_parts(y, a.zpart + part * a.M + m, a.M, parts, a.refs + part * nfb + fb, nfb, 0.f);
         x[0] = y;
       }
     }
@@ -619,7 +693,7 @@ template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
     (void)hipGetLastError();
     return 5;
   }
-  hipLaunchKernelGGL(kernel, dim3(a.nsplit, (a.f.p.Mp / 16 + NW * FT - 1) / (NW * FT), a.B * a.Hk), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(a.nwg > 0 ? a.nwg : a.B * a.Hk, (a.f.p.Mp / 16 + NW * FT - 1) / (NW * FT)), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int VP, bool FULL, bool ONE, bool TURN> int build_waves(const BuildArgs& a, hipStream_t st) {

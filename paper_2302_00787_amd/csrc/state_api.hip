@@ -48,34 +48,30 @@ st::Features features_of(const fs_features* f) {
 }
 st::State state_of(const fs_state* s) { return st::State{s->T, s->z, s->shift, s->slots}; }
 
-// Sums over `rows` rows of every state (append; gradient of a state): splits of the rows, and what a call keeps between its launches.
+// Sums over `rows` rows of every state (append; gradient of a state): the workgroups that share them, and what a call keeps between its launches.
 struct SumPlan {
-  int nsplit, rows_per_split;
-  size_t off_table, off_terms, off_weights, off_old, off_refs, off_part, off_zpart, total;
+  int nwg;
+  size_t off_table, off_terms, off_weights, off_old, off_parts, off_refs, off_part, off_zpart, total;
 };
-SumPlan plan_sum(int BH, long long tokens, long long rows, int d, int dv, int M, int rot, bool terms, bool weights, bool sums) {
+SumPlan plan_sum(int B, int heads, long long tokens, long long rows, int d, int dv, int M, int rot, bool terms, bool weights, bool sums) {
   SumPlan p;
-  const int Mp = (M + 31) / 32 * 32;
-  const int nblock = ceil_div(Mp, st::build_features(d, dv, Mp));
-  // splits of the rows: passes of 256 workgroups, each its start and its chunks of 32 rows, and a partial state written and read for
-  // every split (measured, us: a chunk of 64 numbers a row 1, of 128 2.5; a start 5; 4 TB/s)
-  const int wide = d > 64 || dv > 64;
-  const long long chunks = std::max<long long>(1, (rows + 31) / 32), most = std::min<long long>({chunks, 64, 4096 / (Mp / 16)});
-  double best = 0.0;
-  long long n = 1;
-  for (long long k = 1; k <= most; ++k) {
-    const long long per = (chunks + k - 1) / k, used = (chunks + per - 1) / per, passes = (BH * used * nblock + 255) / 256;
-    const double us = (double)passes * (5.0 + (double)per * (wide ? 2.5 : 1.0)) + (double)BH * used * M * (dv + 1) * 8 / 4e6;
-    if (k == 1 || us < best) { best = us; n = used; }
-  }
-  p.rows_per_split = (int)((chunks + n - 1) / n * 32);
-  p.nsplit = (int)n;
+  const int Mp = (M + 31) / 32 * 32, BH = B * heads;
+  const st::BuildShape shape = st::build_shape(d, dv, Mp);
+  const int nblock = ceil_div(Mp, shape.features);
+  // as many as the chip holds at a time, but a few chunks of 32 rows each at least (a part is a state written and read again, what a chunk or
+  // two take) and 64 to a state; a workgroup for each state where it has no more chunks than that, where there are eight states a CU, or
+  // more sequences than a wave should count
+  const long long each = (rows + 31) / 32, chunks = each * BH, few = st::width_class(d, dv) <= 64 ? 4 : 2;
+  p.nwg = B > 256 || each <= few || (long long)BH * nblock >= 2048
+              ? 0
+              : (int)std::max<long long>(1, std::min<long long>({256 * shape.per_cu / nblock, (chunks + few - 1) / few, 64ll * BH}));
   size_t off = 0;
   p.off_table = off; off = align_up(off + (size_t)tokens * (rot / 2) * sizeof(float2));
   p.off_terms = off; off = align_up(off + (terms ? (size_t)BH * rows * sizeof(float) : 0));
   p.off_weights = off; off = align_up(off + (weights ? (size_t)BH * rows * sizeof(float) : 0));
-  const size_t parts = sums ? (size_t)BH * p.nsplit : 0;
+  const size_t parts = sums ? (size_t)BH + p.nwg : 0;
   p.off_old = off; off = align_up(off + (sums ? (size_t)BH * sizeof(float) : 0));
+  p.off_parts = off; off = align_up(off + (sums ? (size_t)BH * sizeof(int2) : 0));
   p.off_refs = off; off = align_up(off + parts * (Mp / 16) * sizeof(float2));
   p.off_part = off; off = align_up(off + parts * M * dv * sizeof(float));
   p.off_zpart = off; off = align_up(off + parts * M * sizeof(float));
@@ -83,14 +79,14 @@ SumPlan plan_sum(int BH, long long tokens, long long rows, int d, int dv, int M,
   return p;
 }
 SumPlan plan_append(const fs_features* f, int B, int L, int dv, int rot) {
-  return plan_sum(B * f->heads, (long long)B * L, L, f->d, dv, f->M, rot, f->dense_c2 != 0, false, true);
+  return plan_sum(B, f->heads, (long long)B * L, L, f->d, dv, f->M, rot, f->dense_c2 != 0, false, true);
 }
-SumPlan plan_attention(int B, int L, int rot) { return plan_sum(1, (long long)B * L, 0, 1, 1, 1, rot, false, false, false); }
+SumPlan plan_attention(int B, int L, int rot) { return plan_sum(1, 1, (long long)B * L, 0, 1, 1, 1, rot, false, false, false); }
 SumPlan plan_attention_backward(const fs_features* f, int B, int H, int L, int dv, int rot) {
-  return plan_sum(B * f->heads, (long long)B * L, (long long)L * (H / f->heads), f->d, dv, f->M, rot, true, true, true);
+  return plan_sum(B, f->heads, (long long)B * L, (long long)L * (H / f->heads), f->d, dv, f->M, rot, true, true, true);
 }
 SumPlan plan_append_backward(const fs_features* f, int B, int L, int dv, int rot) {
-  return plan_sum(B * f->heads, (long long)B * L, L, f->d, dv, f->M, rot, true, false, false);
+  return plan_sum(B, f->heads, (long long)B * L, L, f->d, dv, f->M, rot, true, false, false);
 }
 bool sizes_ok(const fs_features* f, int B, int H, int L, int dv, int rot) {
   return f != nullptr && f->heads >= 1 && f->d >= 1 && f->d <= 128 && f->M >= 1 && f->M <= kMaxFeatures && B >= 1 && H >= 1 && H % f->heads == 0 &&
@@ -202,7 +198,7 @@ int favorsharp_state_append(const fs_features* f, const fs_state* state, const i
   a.v = st::Rows{dev(V), L, 1, lengths, dv, st::Turn{}};
   a.slots = slots; a.nslots = state->slots;
   a.B = B; a.Hk = f->heads; a.dv = dv;
-  a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split;
+  a.nwg = p.nwg; a.parts = (int2*)(ws + p.off_parts);
   a.part = (float*)(ws + p.off_part); a.zpart = (float*)(ws + p.off_zpart); a.refs = (float2*)(ws + p.off_refs);
   if (!fresh) { a.shift = state->shift; a.old_shift = (float*)(ws + p.off_old); }
   if (L > 0) {
@@ -213,7 +209,7 @@ int favorsharp_state_append(const fs_features* f, const fs_state* state, const i
     }
   }
   if (int rc = st::launch_build(a, s)) return rc;
-  st::JoinArgs j{a.part, a.zpart, a.refs, a.old_shift, slots, state_of(state), B, f->heads, f->M, a.f.p.Mp, dv, p.nsplit, left_out};
+  st::JoinArgs j{a.part, a.zpart, a.refs, a.old_shift, slots, state_of(state), a.parts, B, f->heads, f->M, a.f.p.Mp, dv, left_out};
   return st::launch_join(j, s);
 }
 
@@ -307,10 +303,10 @@ int favorsharp_state_attention_backward(const fs_features* f, const fs_state* st
   a.terms = g.lse; a.weights = g.weights;
   a.slots = slots; a.nslots = state->slots;
   a.B = B; a.Hk = f->heads; a.dv = dv;
-  a.nsplit = p.nsplit; a.rows_per_split = p.rows_per_split;
+  a.nwg = p.nwg; a.parts = (int2*)(ws + p.off_parts);
   a.part = (float*)(ws + p.off_part); a.zpart = (float*)(ws + p.off_zpart); a.refs = (float2*)(ws + p.off_refs);
   if (int rc = st::launch_build(a, s)) return rc;
-  st::JoinArgs j{a.part, a.zpart, a.refs, nullptr, slots, state_of(dstate), B, f->heads, f->M, a.f.p.Mp, dv, p.nsplit, nullptr};
+  st::JoinArgs j{a.part, a.zpart, a.refs, nullptr, slots, state_of(dstate), a.parts, B, f->heads, f->M, a.f.p.Mp, dv, nullptr};
   return st::launch_join_sum(j, s);
 }
 

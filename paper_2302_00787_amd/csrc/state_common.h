@@ -394,13 +394,19 @@ struct BuildArgs {
   const int32_t* slots;
   int nslots;
   int B, Hk, dv;
-  int nsplit, rows_per_split;
-  float *part, *zpart;           // [B*Hk][nsplit][M][dv], [B*Hk][nsplit][M]
-  float2* refs;                  // [B*Hk][nsplit][Mp / 16]: reference and largest exponent (-inf: nothing summed)
+  int nwg;                       // (struct Shares in kernels_state.hip; the parts are nwg + B*Hk or, nwg = 0, B*Hk)
+  float *part, *zpart;           // [parts][M][dv], [parts][M]
+  float2* refs;                  // [parts][Mp / 16]: reference and largest exponent (-inf: nothing summed)
+  int2* parts;                   // [B*Hk] number of a state's first part, and how many
   const float* shift;            // of the pool, copied to old_shift (nullptr: not)
   float* old_shift;              // [B*Hk]
 };
-inline int build_features(int d, int dv, int Mp) { return width_class(d, dv) <= 64 ? (Mp > 64 ? 256 : 64) : (Mp > 128 ? 256 : 128); }     // of a workgroup
+// Workgroups of k_build that a CU holds, by the registers of its waves, and the features of one.
+struct BuildShape { int per_cu, features; };
+inline BuildShape build_shape(int d, int dv, int Mp) {
+  if (width_class(d, dv) <= 64) return Mp > 64 ? BuildShape{1, 256} : BuildShape{4, 64};
+  return Mp > 128 ? BuildShape{1, 256} : BuildShape{2, 128};
+}
 int launch_build(const BuildArgs& a, hipStream_t st);
 // Partial sums onto the states (append), or their sum alone (gradients: slots that no sequence names get zeros).
 struct JoinArgs {
@@ -409,7 +415,8 @@ struct JoinArgs {
   const float* old_shift;        // nullptr: new states
   const int32_t* slots;
   State state;
-  int B, Hk, M, Mp, dv, nsplit;
+  const int2* parts;
+  int B, Hk, M, Mp, dv;
   int* left_out;
 };
 int launch_join(const JoinArgs& a, hipStream_t st);
