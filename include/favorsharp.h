@@ -356,6 +356,7 @@ int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_
  *   the call has outputs for them.  Lengths below 0 count as 0, above L as L; a sequence of length 0 appends nothing.
  *   rot (or NULL): queries and keys are turned on the way and not rounded in between; gradients are turned back.
  *   All products have the accuracy of fp32 for f32 and for bf16 tensors; results are rounded once, to their dtype.
+ *   Where a *_workspace_bytes query answers 0 the workspace may be NULL (a query for sizes that are refused answers 0, too).
  *   d, dv <= 128, M <= 2048, B H and slots * heads <= 65535, L H / heads <= 2^29.
  * Calls on one stream see each other's states; calls that write a state must be ordered with all others on it by the caller.
  */

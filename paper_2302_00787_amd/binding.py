@@ -494,6 +494,18 @@ def _on(device):
     return _SAME_DEVICE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
+# (current_stream() makes a Stream object, 2.7 of the 17 us of a small call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _room(nbytes: int, device, workspace: torch.Tensor | None):
+    """Workspace of a call on states: (pointer, bytes, what holds it)."""
+    if workspace is None and nbytes == 0:
+        return None, 0, None
+    ws = _workspace(nbytes, device, workspace)
+    return ws.data_ptr(), ws.numel(), ws
+
+
 def _one_device(*tensors) -> torch.device:
     device = tensors[0].device
     for t in tensors:
@@ -505,7 +517,7 @@ def _one_device(*tensors) -> torch.device:
 
 
 def _shaped(name: str, t: torch.Tensor, shape):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:          # (a torch.Size is a tuple)
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
@@ -587,7 +599,7 @@ def rotary(X: torch.Tensor, rot: Rotary, X2: torch.Tensor | None = None, transpo
     two = (ctypes.byref(_desc4(X2)), ctypes.byref(_desc4(out2))) if H2 else (None, None)
     with _on(device):
         st = lib().favorsharp_rotary(r, ctypes.byref(_desc4(X)), H, two[0], H2, B, L, d, int(transposed), ctypes.byref(_desc4(out)), two[1],
-                                     _stream())
+                                     _raw_stream(device.index))
     _check(st, "favorsharp_rotary")
     return out if X2 is None else (out, out2)
 
@@ -607,7 +619,7 @@ def state_prepare(theta: torch.Tensor, Omega: torch.Tensor, qk_scale: float, hea
     desc = FsFeatures(buf.data_ptr(), buf.numel())
     with _on(device):
         st = lib().favorsharp_state_prepare(theta.data_ptr(), theta.shape[0], Omega.data_ptr(), og, heads, d, M, qk_scale, ctypes.byref(desc),
-                                            _stream())
+                                            _raw_stream(device.index))
     _check(st, "favorsharp_state_prepare")
     return Features(buf, desc)
 
@@ -632,11 +644,11 @@ def state_append(f: Features, state: State, K: torch.Tensor, V: torch.Tensor, le
     if slots is None and B > state.z.shape[0]:
         raise ValueError("more sequences than slots")
     fd = ctypes.byref(f.desc)
-    ws = _workspace(lib().favorsharp_state_append_workspace_bytes(fd, B, L, dv, rot_dim), device, workspace)
+    ws, ws_bytes, held = _room(lib().favorsharp_state_append_workspace_bytes(fd, B, L, dv, rot_dim), device, workspace)
     with _on(device):
         st = lib().favorsharp_state_append(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(K)),
                                            ctypes.byref(_desc4(V)), B, L, dv, _int32("lengths", lengths, (B,)), r, int(fresh),
-                                           _counter("left_out", left_out), ws.data_ptr(), ws.numel(), _stream())
+                                           _counter("left_out", left_out), ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_state_append")
     return state
 
@@ -654,11 +666,11 @@ def state_attention(f: Features, state: State, Q: torch.Tensor, lengths: torch.T
     device = _one_device(Q, out, f.buffer, *state, lengths, slots, unread, workspace, *_rotary_tensors(rotary))
     r, rot_dim = _rotary_desc(rotary, B, L)
     fd = ctypes.byref(f.desc)
-    ws = _workspace(lib().favorsharp_state_attention_workspace_bytes(fd, B, H, L, dv, rot_dim), device, workspace)
+    ws, ws_bytes, held = _room(lib().favorsharp_state_attention_workspace_bytes(fd, B, H, L, dv, rot_dim), device, workspace)
     with _on(device):
         st = lib().favorsharp_state_attention(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)), B, H, L, dv,
                                               _int32("lengths", lengths, (B,)), r, ctypes.byref(_desc4(out)), _counter("unread", unread),
-                                              ws.data_ptr(), ws.numel(), _stream())
+                                              ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_state_attention")
     return out
 
@@ -678,11 +690,11 @@ def state_step(f: Features, state: State, Q: torch.Tensor, K: torch.Tensor, V: t
     device = _one_device(Q, K, V, out, f.buffer, *state, slots, unread, workspace, *_rotary_tensors(rotary))
     r, _ = _rotary_desc(rotary, B, 1)
     fd = ctypes.byref(f.desc)
-    ws = _workspace(lib().favorsharp_state_step_workspace_bytes(fd, B, H), device, workspace)
+    ws, ws_bytes, held = _room(lib().favorsharp_state_step_workspace_bytes(fd, B, H), device, workspace)
     with _on(device):
         st = lib().favorsharp_state_step(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)),
                                          ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, H, dv, r, ctypes.byref(_desc4(out)),
-                                         _counter("unread", unread), ws.data_ptr(), ws.numel(), _stream())
+                                         _counter("unread", unread), ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_state_step")
     return out
 
@@ -703,12 +715,12 @@ def state_attention_backward(f: Features, state: State, Q: torch.Tensor, dY: tor
     device = _one_device(Q, dY, dQ, f.buffer, *state, *dstate, lengths, slots, workspace, *_rotary_tensors(rotary))
     r, rot_dim = _rotary_desc(rotary, B, L)
     fd = ctypes.byref(f.desc)
-    ws = _workspace(lib().favorsharp_state_attention_backward_workspace_bytes(fd, B, H, L, dv, rot_dim), device, workspace)
+    ws, ws_bytes, held = _room(lib().favorsharp_state_attention_backward_workspace_bytes(fd, B, H, L, dv, rot_dim), device, workspace)
     with _on(device):
         st = lib().favorsharp_state_attention_backward(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)),
                                                        ctypes.byref(_desc4(dY)), B, H, L, dv, _int32("lengths", lengths, (B,)), r,
-                                                       ctypes.byref(_desc4(dQ)), _state_desc(f, dstate, dv, False), ws.data_ptr(), ws.numel(),
-                                                       _stream())
+                                                       ctypes.byref(_desc4(dQ)), _state_desc(f, dstate, dv, False), ws, ws_bytes,
+                                                       _raw_stream(device.index))
     _check(st, "favorsharp_state_attention_backward")
     return dQ, dstate
 
@@ -730,11 +742,11 @@ def state_append_backward(f: Features, state: State, dstate: State, K: torch.Ten
     device = _one_device(K, V, dK, dV, f.buffer, *state, *dstate, lengths, slots, workspace, *_rotary_tensors(rotary))
     r, rot_dim = _rotary_desc(rotary, B, L)
     fd = ctypes.byref(f.desc)
-    ws = _workspace(lib().favorsharp_state_append_backward_workspace_bytes(fd, B, L, dv, rot_dim), device, workspace)
+    ws, ws_bytes, held = _room(lib().favorsharp_state_append_backward_workspace_bytes(fd, B, L, dv, rot_dim), device, workspace)
     with _on(device):
         st = lib().favorsharp_state_append_backward(fd, _state_desc(f, state, dv), _int32("slots", slots, (B,)),
                                                     _state_desc(f, dstate, dv, False), ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, L, dv,
                                                     _int32("lengths", lengths, (B,)), r, ctypes.byref(_desc4(dK)), ctypes.byref(_desc4(dV)),
-                                                    ws.data_ptr(), ws.numel(), _stream())
+                                                    ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_state_append_backward")
     return dK, dV

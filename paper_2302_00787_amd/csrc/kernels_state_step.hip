@@ -1,10 +1,11 @@
 // The next token of every sequence: its key and value onto the state, then its queries against it.
 //
-// The states are read once and written once (2 M (dv + 1) numbers of 4 bytes a key head), which bounds the call, so a launch of its own makes the
-// exponents first, sixteen rows of a head at a time on the matrix instructions as in the other kernels: W is read once for sixteen
-// rows and not once for each state, whose size it has (one launch, a state a workgroup with W from L2: 45 states of 512 x 128 with
-// four query heads 44 us, 2048 of 256 x 64 73).  It also keeps the states' z and shift as they were, so that the second launch can cut a
-// state into columns for as many workgroups as fill the chip.
+// The states are read once and written once (2 M (dv + 1) numbers of 4 bytes a key head), which bounds the call.  Many states: a launch of its own
+// makes the exponents first, sixteen rows of a head at a time on the matrix instructions as in the other kernels, so that W is read once for
+// sixteen rows and not once for each state, whose size it has; it also keeps the states' z and shift as they were, so that the second
+// launch can cut a state into columns for as many workgroups as fill the chip.  Fewer states than CUs: one launch (ONE), a state a workgroup,
+// W from L2.  (us, one launch / two: 8 states of 256 x 64 18.4 / 23.5, 180 of 512 x 128 with four query heads 43.9 / 48.0, 2048 of 256 x 64
+// 75 / 74.)
 #include <algorithm>
 
 #include "state_common.h"
@@ -130,19 +131,78 @@ __global__ void __launch_bounds__(256) k_step_exponents(StepArgs a) {
 
 // ---------------------------------------------------------------------------------------------- states
 // Floats in LDS: features (key, GC queries), the threads' partial outputs, maxima and normalisers by wave.
-template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int Mp) { return (GC + 1) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64); }
+template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int Mp) {
+  return (GC + 1) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64) + (GC + 1) * 128 + NTH / 64;
+}
+
+// (ONE) W of 32 features and a row of LDS as operands, the row in every column.
+template <int S> struct StepWeights {
+  f16x8 p[S][2][2];              // [step][piece][tile]
+  __device__ __forceinline__ void load(const char* img, int fb, int steps, int lane) {
+    const uint16_t* at = (const uint16_t*)img + (size_t)fb * steps * 2048 + lane * 8;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int ft = 0; ft < 2; ++ft) p[s][i][ft] = *(const f16x8*)(at + (min(s, steps - 1) * 2 + i) * 1024 + ft * 512);
+  }
+};
+template <int S> struct StepRow {
+  Op16<2> x[S];                  // (zeros behind the row's end)
+  float undo, norm;              // norm: |x|^2
+  __device__ __forceinline__ void load(const float* row, int lane) {
+    f32x8 n[S];
+    float most = 0.f;
+    norm = 0.f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const f32x4 a = *(const f32x4*)(row + 32 * s + 8 * (lane >> 4)), b = *(const f32x4*)(row + 32 * s + 8 * (lane >> 4) + 4);
+      n[s] = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      most = fmaxf(most, largest_of(n[s]));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) norm += n[s][i] * n[s][i];
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    norm += __shfl_xor(norm, 16);
+    norm += __shfl_xor(norm, 32);
+    const float scale = up_to_2_14(most);
+    undo = power_inverse(scale);
+#pragma unroll
+    for (int s = 0; s < S; ++s) x[s] = as_op16<2>(n[s] * scale);
+  }
+  // of 32 features to `to`, of which this lane writes its column's where `mine`
+  __device__ __forceinline__ void exponents(const StepWeights<S>& w, float scale, const float* bias, float* to, bool mine, int lane) const {
+    f32x4 E[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      each_product<2, 2>([&](int i, int j) {
+#pragma unroll
+        for (int ft = 0; ft < 2; ++ft) E[ft] = mfma(w.p[s][i][ft], x[s].p[j], E[ft]);
+      });
+    if (mine)
+#pragma unroll
+      for (int ft = 0; ft < 2; ++ft) {
+        const int m = 16 * ft + 4 * (lane >> 4);
+        *(f32x4*)(to + m) = E[ft] * (undo * scale) + *(const f32x4*)(bias + m);
+      }
+  }
+};
 
 // GC: query heads that a pass over the state serves.  Workgroup z has the columns z cols .. (z + 1) cols - 1.
-template <int VEC, int GC, int NTH>
-__global__ void __launch_bounds__(NTH, NTH == 256 ? 4 : 2) k_step(StepArgs a) {
+template <int S, int VEC, int GC, int NTH, bool ONE>
+__global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
   typedef __attribute__((ext_vector_type(VEC))) float vec;
-  constexpr int NW = NTH / 64, AHEAD = GC == 1 ? 8 : 4;          // fours of the state on their way for each thread
+  constexpr int NW = NTH / 64, AHEAD = GC == 1 || ONE ? 8 : 4;   // fours of the state on their way for each thread
   extern __shared__ __align__(16) float lds[];
   const int Mp = a.f.p.Mp, M = a.f.M, dv = a.dv, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   float* feat = lds;                           // [GC + 1][Mp]
   float* part = feat + (GC + 1) * Mp;          // [GC][rows of a pass][columns]
   float* tops = part + 4 * GC * NTH;           // [GC + 1][NW]
   float* dens = tops + (1 + GC) * NW;          // [GC][NW]
+  float* x = dens + (1 + GC) * NW;             // (ONE) [GC + 1][128] the key, queries
+  float* word = x + (GC + 1) * 128;            // (ONE) the key's row term by wave
   const int b = blockIdx.x, h = blockIdx.y, G = GC == 1 ? 1 : a.H / a.Hk, col0 = blockIdx.z * a.cols, cols = min(a.cols, dv - col0);
   const int slot = unique_slot_of(a.slots, a.state.slots, b);
   if (slot < 0) {
@@ -159,17 +219,83 @@ __global__ void __launch_bounds__(NTH, NTH == 256 ? 4 : 2) k_step(StepArgs a) {
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
     if (i < mine) t[i] = T[(size_t)i * step];
-  const float2 before = a.old_shift[bh];       // shift, the key's row term
+  float2 before;                               // shift, the key's row term
+  const char* set = a.f.set(h);
+  const int steps = a.f.p.steps, nfb = Mp / 32, pairs = a.rot.rot >> 1;
+  StepWeights<S> weights;
+  if constexpr (ONE) {
+    before = make_float2(a.state.shift[at], 0.f);
+    if (w < nfb) weights.load(set + a.f.p.off_row[1], w, steps, lane);
+  } else {
+    before = a.old_shift[bh];
+  }
   vec v;
 #pragma unroll
   for (int i = 0; i < VEC; ++i) v[i] = worker ? load_elem(a.V, row_base(a.V, b, h, 0) + col0 + VEC * q0 + i) : 0.f;
-  const float* exps = a.exps + bh * (1 + G) * Mp;
-  const float* old_z = a.old_z + bh * Mp;
+  const float* exps = ONE ? nullptr : a.exps + bh * (1 + G) * Mp;
+  const float* old_z = ONE ? a.state.z + at * M : a.old_z + bh * Mp;
   float keep = 0.f;
   int unread = 0;
   for (int g0 = 0; g0 < G; g0 += GC) {
     const int n = GC == 1 ? 1 : min(GC, G - g0);
     if (g0 > 0) __syncthreads();
+    if constexpr (ONE) {
+      // rows: a thread a number, of a turned pair both
+      const float* bias = (const float*)(set + a.f.p.off_bias);
+      for (int e = tid; e < (n + 1) * 128; e += NTH) {
+        const int r = e >> 7, c = e & 127;
+        const TensorDev& src = r == 0 ? a.K : a.Q;
+        const long long base = row_base(src, b, r == 0 ? h : h * G + g0 + r - 1, 0);
+        float* to = x + r * 128;
+        if (c < pairs) {
+          const int i0 = a.rot.interleaved ? 2 * c : c, i1 = a.rot.interleaved ? 2 * c + 1 : c + pairs;
+          const float u = load_elem(src, base + i0), q = load_elem(src, base + i1);
+          const float2 cs = cos_sin(position_of(a.rot, b, 0), a.rot.freqs[c], a.rot.amplitude);
+          to[i0] = u * cs.x - q * cs.y;
+          to[i1] = q * cs.x + u * cs.y;
+        }
+        if (c >= 2 * pairs) to[c] = c < a.f.d ? load_elem(src, base + c) : 0.f;
+      }
+      __syncthreads();
+      // exponents, 32 features a wave at a time
+      StepRow<S> row;
+      row.load(x, lane);
+      for (int fb = w; fb < nfb; fb += NW) {
+        if (fb != w || g0 > 0) weights.load(set + a.f.p.off_row[1], fb, steps, lane);
+        row.exponents(weights, ((const float*)(set + a.f.p.off_scale[1]))[fb], bias + 32 * fb, feat + 32 * fb, (lane & 15) == 0, lane);
+      }
+      float term = w == 0 ? -0.5f * kLog2e * a.f.scale2 * row.norm : 0.f;
+      if (a.f.dense) {           // k' (C2 + C2') k / 2, sixteen coordinates a wave at a time
+        float sum = 0.f;
+        for (int ct = w; ct < 2 * steps; ct += NW) {
+          f32x4 q = {0.f, 0.f, 0.f, 0.f};
+          const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 1024 + lane * 8;
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            const uint16_t* from = img + min(s, steps - 1) * 1024;
+            const f16x8 p[2] = {*(const f16x8*)from, *(const f16x8*)(from + 512)};
+            each_product<2, 2>([&](int i, int j) { q = mfma(p[i], row.x[s].p[j], q); });
+          }
+          const f32x4 y = *(const f32x4*)(x + 16 * ct + 4 * (lane >> 4));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        term = sum * (0.5f * kLog2e * a.f.scale2 * row.undo * *(const float*)(set + a.f.p.off_cscale));
+      }
+      if (lane == 0) word[w] = term;
+      row.load(x + (1 + min(lane & 15, n - 1)) * 128, lane);
+      for (int fb = w; fb < nfb; fb += NW) {
+        weights.load(set + a.f.p.off_row[0], fb, steps, lane);
+        row.exponents(weights, ((const float*)(set + a.f.p.off_scale[0]))[fb], bias + 32 * fb, feat + (1 + min(lane & 15, n - 1)) * Mp + 32 * fb,
+                      (lane & 15) < n, lane);
+      }
+      __syncthreads();
+      before.y = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) before.y += word[i];
+    }
     // features: a thread has the same ones of all rows; the key's again with every pass
     float top[GC + 1];
 #pragma unroll
@@ -177,7 +303,7 @@ __global__ void __launch_bounds__(NTH, NTH == 256 ? 4 : 2) k_step(StepArgs a) {
       top[j] = kNone;
       if (j <= n)
         for (int m = tid; m < Mp; m += NTH) {
-          const float e = exps[(size_t)(j == 0 ? 0 : g0 + j) * Mp + m] + (j == 0 ? before.y : 0.f);
+          const float e = (ONE ? feat[j * Mp + m] : exps[(size_t)(j == 0 ? 0 : g0 + j) * Mp + m]) + (j == 0 ? before.y : 0.f);
           feat[j * Mp + m] = e;
           top[j] = fmaxf(top[j], e);
         }
@@ -198,7 +324,8 @@ __global__ void __launch_bounds__(NTH, NTH == 256 ? 4 : 2) k_step(StepArgs a) {
     for (int m = tid; m < Mp; m += NTH) {
       const float s = top[0] == kNone ? 0.f : fast_exp2(feat[m] - top[0]);
       float z = s;
-      if (keep != 0.f && m < M) z += keep * old_z[m];
+      if (ONE && g0 > 0) z = m < M ? old_z[m] : 0.f;             // (this thread's own, written by the first pass)
+      else if (keep != 0.f && m < M) z += keep * old_z[m];
       feat[m] = s;
       if (m < M && g0 == 0 && blockIdx.z == 0) a.state.z[at * M + m] = z;
 #pragma unroll
@@ -258,9 +385,9 @@ __global__ void __launch_bounds__(NTH, NTH == 256 ? 4 : 2) k_step(StepArgs a) {
   if (unread > 0 && a.unread != nullptr) atomicAdd(a.unread, unread);
 }
 
-template <int VEC, int GC, int NTH> int step(const StepArgs& a, hipStream_t st) {
+template <int S, int VEC, int GC, int NTH, bool ONE> int step(const StepArgs& a, hipStream_t st) {
   const size_t lds = step_lds_floats<GC, NTH>(a.f.p.Mp) * sizeof(float);
-  auto kernel = k_step<VEC, GC, NTH>;
+  auto kernel = k_step<S, VEC, GC, NTH, ONE>;
   if (lds > 64 * 1024 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return 5;
@@ -268,13 +395,21 @@ template <int VEC, int GC, int NTH> int step(const StepArgs& a, hipStream_t st) 
   hipLaunchKernelGGL(kernel, dim3(a.B, a.Hk, (a.dv + a.cols - 1) / a.cols), dim3(NTH), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
+template <int S, int NTH, bool ONE> int step_heads(const StepArgs& a, hipStream_t st) {
+  if (a.H == a.Hk) return a.dv % 4 == 0 ? step<S, 4, 1, NTH, ONE>(a, st) : step<S, 1, 1, NTH, ONE>(a, st);
+  return a.dv % 4 == 0 ? step<S, 4, 4, NTH, ONE>(a, st) : step<S, 1, 4, NTH, ONE>(a, st);
+}
+bool step_in_one(int B, int Hk) { return (long long)B * Hk < 256; }
 
 }  // namespace
 
-size_t step_floats(int B, int H, int Hk, int Mp) { return (size_t)B * ((size_t)(H + Hk) * Mp + (size_t)Hk * Mp + 2 * Hk); }
+size_t step_floats(int B, int H, int Hk, int Mp) { return step_in_one(B, Hk) ? 0 : (size_t)B * ((size_t)(H + Hk) * Mp + (size_t)Hk * Mp + 2 * Hk) + 4; }
 
 int launch_step(StepArgs a, float* room, hipStream_t st) {
-  const int Mp = a.f.p.Mp, S = a.f.p.steps, G = a.H / a.Hk;
+  const int Mp = a.f.p.Mp, steps = a.f.p.steps, G = a.H / a.Hk;
+  a.cols = a.dv;
+  if (step_in_one(a.B, a.Hk))
+    return steps == 1 ? step_heads<1, 512, true>(a, st) : steps == 2 ? step_heads<2, 512, true>(a, st) : step_heads<4, 512, true>(a, st);
   a.old_shift = (float2*)room;
   a.exps = room + 2 * (size_t)a.B * a.Hk;
   a.exps += (4 - ((a.exps - room) & 3)) & 3;
@@ -282,15 +417,13 @@ int launch_step(StepArgs a, float* room, hipStream_t st) {
   a.key_tiles = (a.B + 15) / 16;
   const long long tiles = a.key_tiles + ((long long)a.B * G + 15) / 16;
   const dim3 grid((Mp / 32 + 3) / 4, a.Hk, (unsigned)tiles);
-  if (S == 1) hipLaunchKernelGGL(k_step_exponents<1>, grid, dim3(256), 0, st, a);
-  else if (S == 2) hipLaunchKernelGGL(k_step_exponents<2>, grid, dim3(256), 0, st, a);
+  if (steps == 1) hipLaunchKernelGGL(k_step_exponents<1>, grid, dim3(256), 0, st, a);
+  else if (steps == 2) hipLaunchKernelGGL(k_step_exponents<2>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_step_exponents<4>, grid, dim3(256), 0, st, a);
   if (hipGetLastError() != hipSuccess) return 5;
   // a state in halves or quarters of its columns, 16 at least, until four workgroups a CU are there
-  a.cols = a.dv;
   while ((long long)a.B * a.Hk * ((a.dv + a.cols - 1) / a.cols) < 1024 && a.cols % 32 == 0 && 4 * a.cols > a.dv) a.cols /= 2;
-  if (a.H == a.Hk) return a.dv % 4 == 0 ? step<4, 1, 256>(a, st) : step<1, 1, 256>(a, st);
-  return a.dv % 4 == 0 ? step<4, 4, 256>(a, st) : step<1, 4, 256>(a, st);
+  return step_heads<1, 256, false>(a, st);
 }
 
 }  // namespace st

@@ -75,7 +75,7 @@ SumPlan plan_sum(int B, int heads, long long tokens, long long rows, int d, int 
   p.off_refs = off; off = align_up(off + parts * (Mp / 16) * sizeof(float2));
   p.off_part = off; off = align_up(off + parts * M * dv * sizeof(float));
   p.off_zpart = off; off = align_up(off + parts * M * sizeof(float));
-  p.total = std::max(off, kAlign);
+  p.total = off;
   return p;
 }
 SumPlan plan_append(const fs_features* f, int B, int L, int dv, int rot) {
@@ -222,8 +222,9 @@ int favorsharp_state_attention(const fs_features* f, const fs_state* state, cons
                                const int32_t* lengths, const fs_rotary* rot, const fs_tensor* Y, int32_t* unread, void* workspace,
                                size_t workspace_bytes, void* stream) {
   if (int rc = check(f, state, true, B, H, L, dv, rot)) return rc;
-  if (!tensor_ok(Q, f->d, L > 0) || !tensor_ok(Y, dv, L > 0) || workspace == nullptr || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
+  if (!tensor_ok(Q, f->d, L > 0) || !tensor_ok(Y, dv, L > 0) || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
   const SumPlan p = plan_attention(B, L, rot ? rot->rot_dim : 0);
+  if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
   if (L == 0) return FS_OK;
   hipStream_t s = (hipStream_t)stream;
@@ -241,7 +242,7 @@ int favorsharp_state_attention(const fs_features* f, const fs_state* state, cons
 
 size_t favorsharp_state_step_workspace_bytes(const fs_features* f, int B, int H) {
   if (!sizes_ok(f, B, H, 1, 1, 0)) return 0;
-  return align_up(st::step_floats(B, H, f->heads, st::feature_plan(f->d, f->M, 1).Mp) * sizeof(float) + 16);
+  return align_up(st::step_floats(B, H, f->heads, st::feature_plan(f->d, f->M, 1).Mp) * sizeof(float));
 }
 
 int favorsharp_state_step(const fs_features* f, const fs_state* state, const int32_t* slots, const fs_tensor* Q, const fs_tensor* K,
@@ -249,8 +250,10 @@ int favorsharp_state_step(const fs_features* f, const fs_state* state, const int
                           void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check(f, state, true, B, H, 1, dv, rot)) return rc;
   if (!tensor_ok(Q, f->d) || !tensor_ok(K, f->d) || !tensor_ok(V, dv) || !tensor_ok(Y, dv)) return FS_ERR_INVALID_ARG;
-  if (Q->dtype != K->dtype || Q->dtype != V->dtype || workspace == nullptr || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
-  if (workspace_bytes < favorsharp_state_step_workspace_bytes(f, B, H)) return FS_ERR_WORKSPACE_TOO_SMALL;
+  if (Q->dtype != K->dtype || Q->dtype != V->dtype || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
+  const size_t need = favorsharp_state_step_workspace_bytes(f, B, H);
+  if (need > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return FS_ERR_WORKSPACE_TOO_SMALL;
   st::StepArgs a{};
   a.f = features_of(f);
   a.state = state_of(state);

@@ -76,11 +76,14 @@ def test_the_other_entry_points_refuse(fs):
     # query heads that are no multiple of the key heads; a pool of gradients with other slots; null tensors
     assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 3, 8, 64, None, None, P(t), None, *ws) == 1
     assert L.favorsharp_state_attention(P(f), P(s), None, None, 2, 4, 8, 64, None, None, P(t), None, *ws) == 1
-    assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 4, 8, 64, None, None, P(t), None, A, 0, None) == 4
+    rot = fs.FsRotary(A, None, 0, 0, 64, 0, 1.0)
+    assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 4, 8, 64, None, P(rot), P(t), None, A, 0, None) == 4
+    assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 4, 8, 64, None, P(rot), P(t), None, None, 1 << 20, None) == 1
     assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 2, 4, 8, 64, None, None, None, None, *ws) == 1
     assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 2, 3, 64, None, P(t), None, *ws) == 1
     assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(tensor(fs, dtype=0)), P(t), 2, 4, 64, None, P(t), None, *ws) == 1
-    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 2, 4, 64, None, P(t), None, A, 512, None) == 4
+    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 128, 4, 64, None, P(t), None, A, 512, None) == 4
+    assert L.favorsharp_state_step(P(f), P(s), None, P(t), P(t), P(t), 128, 4, 64, None, P(t), None, None, 1 << 30, None) == 1
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, P(t), P(pool(fs, slots=5)), *ws) == 1
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, None, P(ds), *ws) == 1
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, P(t), P(ds), A, 1000, None) == 4
@@ -120,13 +123,15 @@ def test_workspace_sizes(fs):
     assert n >= 4 * 2 * state
     assert L.favorsharp_state_append_workspace_bytes(P(f), 4, 4096, 64, 64) >= n + 4 * 4096 * 32 * 8        # the angles
     assert L.favorsharp_state_append_workspace_bytes(P(features(fs, dense=1)), 4, 4096, 64, 0) >= n + 8 * 4096 * 4
-    assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 4, 4096, 64, 0) > 0
+    assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 4, 4096, 64, 0) == 0             # nothing is kept between launches
+    assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 4, 4096, 64, 64) >= 4 * 4096 * 32 * 8
     assert L.favorsharp_state_attention_backward_workspace_bytes(P(f), 4, 4, 4096, 64, 0) >= 16 * 4096 * 8 + 8 * state
     assert L.favorsharp_state_append_backward_workspace_bytes(P(f), 4, 4096, 64, 0) >= 8 * 4096 * 4
     assert L.favorsharp_state_append_workspace_bytes(None, 4, 4096, 64, 0) == 0
     assert L.favorsharp_state_append_workspace_bytes(P(f), 4, 4096, 129, 0) == 0
     assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 3, 4096, 64, 0) == 0
-    assert L.favorsharp_state_step_workspace_bytes(P(f), 4, 4) >= 4 * (4 + 2 + 2) * 256 * 4
+    assert L.favorsharp_state_step_workspace_bytes(P(f), 4, 4) == 0                                # one launch
+    assert L.favorsharp_state_step_workspace_bytes(P(f), 256, 4) >= 256 * (4 + 2 + 2) * 256 * 4
     assert L.favorsharp_state_features_bytes(2, 64, 256, 1, 2) > 2 * 2 * 256 * 64 * (4 + 6)
     assert L.favorsharp_state_features_bytes(2, 64, 256, 3, 2) == L.favorsharp_state_features_bytes(2, 64, 4000, 1, 1) == 0
 
