@@ -108,22 +108,44 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
     }
   }
 };
-// W of 32 features as operands, from LDS or (img = nullptr) from where the images lie.
-template <int W, int CP> struct Weights {
+// W of 32 features as operands: from LDS where the workgroup has the images there, or (DIRECT) in registers, on their way long before their use
+// (the rows of the next 32 features once this wave's exponents are done, the columns ahead of the exponents).
+template <int W, int CP, bool DIRECT> struct Weights {
   const ImageLds<W, CP>* img;
-  const char *row_img, *col_img;
-  int fb, steps;
+  int fb;
   __device__ __forceinline__ Op16<2> row(int s, int ft, int lane) const {
     Op16<2> o;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int at = (s * 2 + p) * 1024 + ft * 512 + lane * 8;
-      o.p[p] = img ? *(const f16x8*)&img->row[0][0][at] : *(const f16x8*)(row_img + ((size_t)fb * steps * 2048 + at) * 2);
-    }
+    for (int p = 0; p < 2; ++p) o.p[p] = *(const f16x8*)&img->row[s][p][ft * 512 + lane * 8];
     return o;
   }
-  __device__ __forceinline__ Op<CP> col(int ct, int lane) const {
-    return img ? image_op<CP>(&img->col[ct][0][0], lane) : image_op<CP>((const uint16_t*)col_img + (size_t)(fb * 2 * steps + ct) * 1536, lane);
+  __device__ __forceinline__ Op<CP> col(int ct, int lane) const { return image_op<CP>(&img->col[ct][0][0], lane); }
+  __device__ __forceinline__ void rows_used(int) {}
+};
+template <int W, int CP> struct Weights<W, CP, true> {
+  static constexpr int S = STEPS<W>, CT = CP ? TILES<W> : 1, P = CP ? CP : 1;
+  const char *row_img, *col_img;
+  int fb, next, steps;
+  Op16<2> rows[S][2];
+  Op<P> cols[CT];
+  __device__ __forceinline__ void load_rows(int f, int lane) {
+    const uint16_t* at = (const uint16_t*)row_img + (size_t)f * steps * 2048 + lane * 8;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int ft = 0; ft < 2; ++ft)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) rows[s][ft].p[p] = *(const f16x8*)(at + (min(s, steps - 1) * 2 + p) * 1024 + ft * 512);
+  }
+  __device__ __forceinline__ void load_cols(int lane) {
+    if constexpr (CP > 0)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) cols[ct] = image_op<CP>((const uint16_t*)col_img + (size_t)(fb * 2 * steps + min(ct, 2 * steps - 1)) * 1536, lane);
+  }
+  __device__ __forceinline__ Op16<2> row(int s, int ft, int) const { return rows[s][ft]; }
+  __device__ __forceinline__ Op<P> col(int ct, int) const { return cols[ct]; }
+  __device__ __forceinline__ void rows_used(int lane) {
+    if (next >= 0) load_rows(next, lane);
   }
 };
 
@@ -168,8 +190,8 @@ template <int W, int XP, int RT, bool FULL> struct RowOps {
     }
   }
 };
-template <int W, int XP, int CP, int RT, bool FULL>
-__device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, const Weights<W, CP>& weights, int steps, int lane, f32x4 (&E)[RT][2]) {
+template <int W, int XP, int CP, int RT, bool FULL, bool DIRECT>
+__device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, Weights<W, CP, DIRECT>& weights, int steps, int lane, f32x4 (&E)[RT][2]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) E[rt][0] = E[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -183,6 +205,7 @@ __device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, cons
           for (int ft = 0; ft < 2; ++ft) E[rt][ft] = mfma(w[ft].p[i], x.x[rt][s].p[j], E[rt][ft]);
       });
     }
+  weights.rows_used(lane);
 }
 __device__ __forceinline__ float over_groups_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
@@ -243,6 +266,16 @@ template <int W> __device__ __forceinline__ f32x8 from_tile(const float* row, in
   return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
+// A workgroup's state and piece of rows.  Workgroups go to the eight XCDs in turn, so that with eight states or a multiple the pieces of a state
+// meet in one L2; where sequences have lengths of their own and an XCD would have some of them only, the states turn with the piece.  (Cross
+// attention of 8 padded sequences with 8 heads, gradients of the keys: pieces in turn, so that two XCDs had the sequences' ends, 109 us.)
+struct Piece { int bh, rows; };
+__device__ __forceinline__ Piece piece_of(int BH, int Hk, bool padded) {
+  const int y = blockIdx.y + (blockIdx.z << 15);
+  return Piece{(int)(padded && Hk % 8 != 0 ? (blockIdx.x + (unsigned)y) % (unsigned)BH : blockIdx.x), y};
+}
+dim3 pieces(int BH, long long n) { return dim3(BH, (unsigned)std::min(n, 1ll << 15), (unsigned)((n + (1 << 15) - 1) >> 15)); }
+
 constexpr size_t most_of(size_t a, size_t b) { return a > b ? a : b; }
 template <int W, int TP, int CP, int NW, int RT, bool DIRECT> constexpr size_t rows_lds() {
   return DIRECT ? most_of(NW * sizeof(StateLds<W, TP>), (size_t)NW * 16 * RT * (W + 4) * 4)
@@ -273,12 +306,22 @@ __device__ __forceinline__ void walk_features(const Features& f, int side, const
     Stage<W, TP, 0, 64, FULL, false> stage;
     stage.start(f, side, set, T, z, dv);
     StateLds<W, TP>& mine = ((StateLds<W, TP>*)lds)[w];
-    if (w < nfb) stage.fetch(w, lane);
+    Weights<W, CP, true> weights;
+    weights.row_img = stage.row_img;
+    weights.col_img = stage.col_img;
+    weights.steps = stage.steps;
+    if (w < nfb) {
+      stage.fetch(w, lane);
+      weights.load_rows(w, lane);
+    }
     for (int fb = w; fb < nfb; fb += NW) {
+      weights.fb = fb;
+      weights.next = fb + NW < nfb ? fb + NW : -1;
       stage.put(mine, nullptr, lane);
+      weights.load_cols(lane);
       if (fb + NW < nfb) stage.fetch(fb + NW, lane);
       wave_fence();
-      body(mine, Weights<W, CP>{nullptr, stage.row_img, stage.col_img, fb, stage.steps}, fb == w);
+      body(mine, weights, fb == w);
       wave_fence();
     }
   } else {
@@ -293,7 +336,8 @@ __device__ __forceinline__ void walk_features(const Features& f, int side, const
       Both &now = both[fb & 1], &next = both[~fb & 1];
       const bool more = fb + 1 < nfb;
       if (more) stage.fetch(fb + 1, tid);
-      body(now.s, Weights<W, CP>{&now.img, nullptr, nullptr, fb, stage.steps}, fb == 0);
+      Weights<W, CP, false> weights{&now.img, fb};
+      body(now.s, weights, fb == 0);
       if (more) stage.put(next.s, &next.img, tid);
       __syncthreads();
     }
@@ -336,14 +380,16 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   extern __shared__ __align__(16) char lds[];
   __shared__ float red[DIRECT ? 2 * RT * NW * 16 : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
-  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, steps = a.f.p.steps, dv = FULL ? W : a.dv;
+  const Piece piece = piece_of(a.B * a.Hk, a.Hk, a.x.lengths != nullptr);
+  const int bh = piece.bh, b = bh / a.Hk, h = bh - b * a.Hk, steps = a.f.p.steps, dv = FULL ? W : a.dv;
   const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
-  const int v0 = (DIRECT ? blockIdx.x : blockIdx.x * NW + w) * 16 * RT;
+  const int v0 = (DIRECT ? piece.rows : piece.rows * NW + w) * 16 * RT;
   const char* set = a.f.set(h);
   const float* scales = (const float*)(set + a.f.p.off_scale[0]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
   constexpr int WG_ROWS = 16 * RT * (DIRECT ? 1 : NW);
-  if (all_padding<W, 64 * NW>(a.x, b, h, blockIdx.x * WG_ROWS, WG_ROWS, len, a.Y, dv, tid)) return;
+  if (piece.rows * WG_ROWS >= rows) return;
+  if (all_padding<W, 64 * NW>(a.x, b, h, piece.rows * WG_ROWS, WG_ROWS, len, a.Y, dv, tid)) return;
 
   RowOps<W, XP, RT, FULL> x;
   x.load(a.x, b, h, v0, rows, len, steps, lane);
@@ -360,7 +406,7 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   if (slot >= 0)
     walk_features<W, P, 0, NW, FULL, DIRECT>(
         a.f, 0, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
-        [&](const StateLds<W, P>& l, const Weights<W, 0>& weights, bool first) {
+        [&](const StateLds<W, P>& l, Weights<W, 0, DIRECT>& weights, bool first) {
           f32x4 E[RT][2];
           exponents(x, weights, steps, lane, E);
           const float scale = scales[weights.fb];
@@ -457,17 +503,19 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
   extern __shared__ __align__(16) char lds[];
   __shared__ float red[DIRECT ? 3 * RT * NW * 16 : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-  const int bh = blockIdx.y, b = bh / a.Hk, h = bh - b * a.Hk, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv, d = FULL ? W : a.f.d;
+  const Piece piece = piece_of(a.B * a.Hk, a.Hk, a.x.lengths != nullptr);
+  const int bh = piece.bh, b = bh / a.Hk, h = bh - b * a.Hk, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv, d = FULL ? W : a.f.d;
   const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
-  const int v0 = (DIRECT ? blockIdx.x : blockIdx.x * NW + w) * 16 * RT;
+  const int v0 = (DIRECT ? piece.rows : piece.rows * NW + w) * 16 * RT;
   const char* set = a.f.set(h);
   const float* scales = (const float*)(set + a.f.p.off_scale[KEYS]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
   constexpr int WG_ROWS = 16 * RT * (DIRECT ? 1 : NW);
-  if (all_padding<W, 64 * NW>(a.x, b, h, blockIdx.x * WG_ROWS, WG_ROWS, len, a.dx, d, tid)) {
-    if constexpr (KEYS) all_padding<W, 64 * NW>(a.x, b, h, blockIdx.x * WG_ROWS, WG_ROWS, len, a.dr, dv, tid);
+  if (piece.rows * WG_ROWS >= rows) return;
+  if (all_padding<W, 64 * NW>(a.x, b, h, piece.rows * WG_ROWS, WG_ROWS, len, a.dx, d, tid)) {
+    if constexpr (KEYS) all_padding<W, 64 * NW>(a.x, b, h, piece.rows * WG_ROWS, WG_ROWS, len, a.dr, dv, tid);
     else
-      for (int v = blockIdx.x * WG_ROWS + tid; v < min((int)(blockIdx.x + 1) * WG_ROWS, rows); v += 64 * NW) {
+      for (int v = piece.rows * WG_ROWS + tid; v < min((piece.rows + 1) * WG_ROWS, rows); v += 64 * NW) {
         a.lse[(size_t)bh * rows + v] = kNone;
         a.weights[(size_t)bh * rows + v] = 0.f;
       }
@@ -504,7 +552,7 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
   if (slot >= 0)
     walk_features<W, TP, P, NW, FULL, DIRECT>(
         a.f, KEYS, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
-        [&](const StateLds<W, TP>& l, const Weights<W, P>& weights, bool first) {
+        [&](const StateLds<W, TP>& l, Weights<W, P, DIRECT>& weights, bool first) {
           f32x4 E[RT][2], D[RT][2], bias[2], zf[2];
 #pragma unroll
           for (int ft = 0; ft < 2; ++ft) {
@@ -615,14 +663,13 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
       if (part == 1) {
         tile_to_lds<W>(tile, more[rt], f32x4{1.f, 1.f, 1.f, 1.f}, lane);
       } else if constexpr (KEYS) {
-        // the row term: (sum u) s^2 (C2 + C2') x, by the first wave where several have a part of the features
-        const float rho = !DIRECT || w == 0 ? sums[rt][1] * a.f.scale2 : 0.f;
-        const f32x4 rho4 = by_row(rho * x.undo[rt], lane);
+        // the row term: (sum u) s^2 (C2 + C2') x; waves that have the same rows take sixteen columns each in turn
+        const f32x4 rho4 = by_row(sums[rt][1] * a.f.scale2 * x.undo[rt], lane) * *(const float*)(set + a.f.p.off_cscale);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
           if (FULL || 16 * ct < d) {
             acc[rt][ct] *= kLn2;
-            if (!DIRECT || w == 0) {
+            if (!DIRECT || ct % NW == w) {
               f32x4 q = {0.f, 0.f, 0.f, 0.f};
               const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 2 * 512;
 #pragma unroll
@@ -633,7 +680,7 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
                   for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
                   each_product<XP, 2>([&](int i, int j) { q = mfma(x.x[rt][s].p[i], co.p[j], q); });
                 }
-              acc[rt][ct] += (rho4 * *(const float*)(set + a.f.p.off_cscale)) * q;
+              acc[rt][ct] += rho4 * q;
             }
           }
         tile_to_lds<W>(tile, acc[rt], f32x4{1.f, 1.f, 1.f, 1.f}, lane);
@@ -682,7 +729,7 @@ template <int W, int XP, int P, bool FULL, bool DIRECT> int values(const ValueAr
   static_assert(lds <= 156 * 1024, "LDS of a CU");
   auto kernel = k_values<W, XP, P, NW, RT, FULL, DIRECT>;
   if (int rc = lds_room((const void*)kernel, lds)) return rc;
-  hipLaunchKernelGGL(kernel, dim3((a.x.L * a.x.G + ROWS - 1) / ROWS, a.B * a.Hk), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(kernel, pieces(a.B * a.Hk, ((long long)a.x.L * a.x.G + ROWS - 1) / ROWS), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int P, bool FULL> int values_rows(const ValueArgs& a, hipStream_t st) {
@@ -697,12 +744,12 @@ template <int W> int values_width(const ValueArgs& a, hipStream_t st) {
 }
 
 template <int W, int XP, int RP, int P, bool FULL, bool DIRECT, bool KEYS> int grads(const GradArgs& a, hipStream_t st) {
-  constexpr int NW = DIRECT && W == 128 ? 4 : 8, RT = W == 128 ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr int NW = DIRECT && W == 128 ? 4 : 8, RT = W == 128 || (DIRECT && W == 64) ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
   constexpr size_t lds = rows_lds<W, KEYS ? P : 3, P, NW, RT, DIRECT>();
   static_assert(lds <= 156 * 1024, "LDS of a CU");
   auto kernel = k_grads<W, XP, RP, P, NW, RT, FULL, DIRECT, KEYS>;
   if (int rc = lds_room((const void*)kernel, lds)) return rc;
-  hipLaunchKernelGGL(kernel, dim3((a.x.L * a.x.G + ROWS - 1) / ROWS, a.B * a.Hk), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(kernel, pieces(a.B * a.Hk, ((long long)a.x.L * a.x.G + ROWS - 1) / ROWS), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int RP, int P, bool FULL, bool KEYS> int grads_rows(const GradArgs& a, hipStream_t st) {
