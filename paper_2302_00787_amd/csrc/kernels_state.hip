@@ -92,63 +92,64 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
 }
 
 // ---------------------------------------------------------------------------------------------- row terms
-// x' C2 x = x' (C2 + C2') x / 2 on matrix instructions, sixteen rows a wave; -|x|^2 / 2 where no quadratic form is dense.
+// x' C2 x = x' (C2 + C2') x / 2 of sixteen rows a workgroup on matrix instructions, for dense quadratic forms.  A wave has sixteen coordinates of the
+// product, or twice that, and brings their part of the form while the rows are on their way: the call is the latency of both.  (6000
+// rows of 128: 14 us where a wave took all coordinates, one after the other, AFTER so.)
 template <int W>
-__global__ void __launch_bounds__(256) k_row_terms(Features f, Rows x, int Hk, const float* shift, const int32_t* slots, int nslots, float* terms) {
-  constexpr int S = STEPS<W>;
-  __shared__ __align__(16) float lds[4][16][W + 4];
+__global__ void __launch_bounds__(W == 32 ? 128 : 256) k_row_terms(Features f, Rows x, int Hk, float* terms) {
+  constexpr int S = STEPS<W>, NW = W == 32 ? 2 : 4, CT = 2 * S / NW;
+  __shared__ __align__(16) float rows[NW][16][W + 4];
+  __shared__ float parts[NW][16];
   const int bh = blockIdx.y, b = bh / Hk, h = bh - b * Hk, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
-  const int row = 64 * blockIdx.x + 16 * w + c, len = length_of(x, b);
-  const int slot = shift ? unique_slot_of(slots, nslots, b) : 0;
-  const bool live = row < len && slot >= 0;
-  f32x8 n[S];
-  float most = 0.f, sum = 0.f;
-  const int at = min(row, x.L - 1);
+  const int row = 16 * blockIdx.x + c, len = length_of(x, b), at = min(row, x.L - 1);
+  const char* set = f.set(h);
   const long long base = row_base(x.X, b, h, at);
   RowUnits<S, false, true> units;
   units.fetch(x.X, base, x.cols, x.turn, g);
-  units.finish(x.X, base, x.cols, x.turn, x.turn.table + ((long long)b * x.L + at) * (x.turn.rot >> 1), live, g, n);
+  Op16<2> form[CT][S];
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+#pragma unroll
+    for (int s = 0; s < S; ++s)                  // (behind d the row is zeros)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        form[i][s].p[p] = *(const f16x8*)((const uint16_t*)(set + f.p.off_csym) + (size_t)min(w + NW * i, f.p.tiles - 1) * f.p.steps * 1024 +
+                                          (min(s, f.p.steps - 1) * 2 + p) * 512 + lane * 8);
+  const float undo = *(const float*)(set + f.p.off_cscale);
+  f32x8 n[S];
+  units.finish(x.X, base, x.cols, x.turn, x.turn.table + ((long long)b * x.L + at) * (x.turn.rot >> 1), row < len, g, n);
+  float most = 0.f, sum = 0.f;
 #pragma unroll
   for (int s = 0; s < S; ++s) most = fmaxf(most, largest_of(n[s]));
-  if (f.dense) {
-    const char* set = f.set(h);
-    most = fmaxf(most, __shfl_xor(most, 16));
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const float scale = up_to_2_14(most);
-    Op16<2> xo[S];
+  most = fmaxf(most, __shfl_xor(most, 16));
+  most = fmaxf(most, __shfl_xor(most, 32));
+  const float scale = up_to_2_14(most);
+  Op16<2> xo[S];
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      xo[s] = as_op16<2>(n[s] * scale);
-      *(f32x4*)&lds[w][c][32 * s + 8 * g] = f32x4{n[s][0], n[s][1], n[s][2], n[s][3]};
-      *(f32x4*)&lds[w][c][32 * s + 8 * g + 4] = f32x4{n[s][4], n[s][5], n[s][6], n[s][7]};
-    }
-    __syncthreads();
+  for (int s = 0; s < S; ++s) {
+    xo[s] = as_op16<2>(n[s] * scale);
+    *(f32x4*)&rows[w][c][32 * s + 8 * g] = f32x4{n[s][0], n[s][1], n[s][2], n[s][3]};
+    *(f32x4*)&rows[w][c][32 * s + 8 * g + 4] = f32x4{n[s][4], n[s][5], n[s][6], n[s][7]};
+  }
+  __syncthreads();
 #pragma unroll
-    for (int ct = 0; ct < 2 * S; ++ct) {         // (no branches, so that the images are on their way together: behind d the row is zeros)
-      f32x4 q = {0.f, 0.f, 0.f, 0.f};
-      const uint16_t* img = (const uint16_t*)(set + f.p.off_csym) + (size_t)min(ct, f.p.tiles - 1) * f.p.steps * 1024 + lane * 8;
+  for (int i = 0; i < CT; ++i) {
+    f32x4 q = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const uint16_t* from = img + min(s, f.p.steps - 1) * 1024;
-        const f16x8 p[2] = {*(const f16x8*)from, *(const f16x8*)(from + 512)};
-        each_product<2, 2>([&](int i, int j) { q = mfma(p[i], xo[s].p[j], q); });
-      }
-      const f32x4 y = *(const f32x4*)&lds[w][c][16 * ct + 4 * g];
+    for (int s = 0; s < S; ++s) each_product<2, 2>([&](int j, int k) { q = mfma(form[i][s].p[j], xo[s].p[k], q); });
+    const f32x4 y = *(const f32x4*)&rows[w][c][16 * (w + NW * i) + 4 * g];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
-    }
-    sum *= 0.5f * power_inverse(scale) * *(const float*)(set + f.p.off_cscale);
-  } else {
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += n[s][i] * n[s][i];
-    sum *= -0.5f;
+    for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
   }
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
-  if (g == 0 && row < x.L)
-    terms[(size_t)bh * x.L + row] = live ? kLog2e * f.scale2 * sum - (shift ? shift[(size_t)slot * Hk + h] : 0.f) : kNone;
+  parts[w][c] = sum;
+  __syncthreads();
+  if (w > 0 || g > 0 || row >= x.L) return;
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) sum += parts[i][c];
+  terms[(size_t)bh * x.L + row] = row < len ? 0.5f * kLog2e * f.scale2 * power_inverse(scale) * undo * sum : kNone;
 }
 
 // ---------------------------------------------------------------------------------------------- sums over rows
@@ -739,10 +740,11 @@ int launch_prepare(const float* theta, int groups, const float* Omega, int omega
   hipLaunchKernelGGL(k_prepare, dim3(p.Mp / 32, 2, sets), dim3(256), 0, st, theta, groups, Omega, omega_groups, d, M, scale, buf, p);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, const float* shift, const int32_t* slots, int nslots, float* terms,
-                     hipStream_t st) {
-  auto kernel = f.d <= 32 ? k_row_terms<32> : f.d <= 64 ? k_row_terms<64> : k_row_terms<128>;
-  hipLaunchKernelGGL(kernel, dim3((k.L + 63) / 64, B * Hk), dim3(256), 0, st, f, k, Hk, shift, slots, nslots, terms);
+int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, float* terms, hipStream_t st) {
+  const dim3 grid((k.L + 15) / 16, B * Hk);
+  if (f.d <= 32) hipLaunchKernelGGL(k_row_terms<32>, grid, dim3(128), 0, st, f, k, Hk, terms);
+  else if (f.d <= 64) hipLaunchKernelGGL(k_row_terms<64>, grid, dim3(256), 0, st, f, k, Hk, terms);
+  else hipLaunchKernelGGL(k_row_terms<128>, grid, dim3(256), 0, st, f, k, Hk, terms);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 

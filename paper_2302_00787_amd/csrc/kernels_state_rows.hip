@@ -159,7 +159,7 @@ __device__ __forceinline__ void wave_fence() {
 template <int W, int XP, int RT, bool FULL> struct RowOps {
   static constexpr int S = STEPS<W>;
   Op16<XP> x[RT][S];
-  float undo[RT];
+  float undo[RT], square[RT];    // square: this lane's part of |x|^2
   RowAt at[RT];
   bool live[RT];
   __device__ __forceinline__ void load(const Rows& r, int b, int h, int v0, int rows, int len, int steps, int lane) {
@@ -179,8 +179,13 @@ template <int W, int XP, int RT, bool FULL> struct RowOps {
       f32x8 n[S];
       units[rt].finish(r.X, base[rt], r.cols, r.turn, r.turn.table + ((long long)b * r.L + at[rt].row) * (r.turn.rot >> 1), live[rt], g, n);
       float most = 0.f;
+      square[rt] = 0.f;
 #pragma unroll
-      for (int s = 0; s < S; ++s) most = fmaxf(most, largest_of(n[s]));
+      for (int s = 0; s < S; ++s) {
+        most = fmaxf(most, largest_of(n[s]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) square[rt] += n[s][i] * n[s][i];
+      }
       most = fmaxf(most, __shfl_xor(most, 16));
       most = fmaxf(most, __shfl_xor(most, 32));
       const float scale = up_to_2_14(most);
@@ -501,11 +506,12 @@ template <int W, int XP, int RP, int P, int NW, int RT, bool FULL, bool DIRECT, 
 __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
   constexpr int S = STEPS<W>, CT = TILES<W>, LD = W + 8, TP = KEYS ? P : 3;       // (delta enters a sum of the state's gradient: 24 bits)
   extern __shared__ __align__(16) char lds[];
-  __shared__ float red[DIRECT ? 3 * RT * NW * 16 : 1];
+  __shared__ __align__(16) float red[DIRECT ? 3 * RT * NW * 16 : KEYS ? RT * NW * 16 : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
   const Piece piece = piece_of(a.B * a.Hk, a.Hk, a.x.lengths != nullptr);
   const int bh = piece.bh, b = bh / a.Hk, h = bh - b * a.Hk, steps = FULL ? S : a.f.p.steps, dv = FULL ? W : a.dv, d = FULL ? W : a.f.d;
-  const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
+  const int slot = KEYS ? unique_slot_of(a.slots, a.state.slots, b) : slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b),
+            rows = a.x.L * a.x.G;
   const int v0 = (DIRECT ? piece.rows : piece.rows * NW + w) * 16 * RT;
   const char* set = a.f.set(h);
   const float* scales = (const float*)(set + a.f.p.off_scale[KEYS]);
@@ -544,10 +550,71 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
         rr[rt][s] = as_op<RP>(n);
       }
     }
-    term[rt] = KEYS ? (x.live[rt] && slot >= 0 ? a.terms[(size_t)bh * rows + v0 + 16 * rt + c] : kNone) : 0.f;
+    term[rt] = over_groups_sum(x.square[rt]) * -0.5f * kLog2e * a.f.scale2;     // (keys)
     ref[rt] = sums[rt][0] = sums[rt][1] = 0.f;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc[rt][ct] = more[rt][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // (C2 + C2') x of a tile's rows, sixteen coordinates; waves that have the same rows take them in turn
+  auto form_of = [&](int rt, int ct) {
+    f32x4 q = {0.f, 0.f, 0.f, 0.f};
+    const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 2 * 512;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (FULL || s < steps) {
+        Op16<2> co;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
+        each_product<XP, 2>([&](int i, int j) { q = mfma(x.x[rt][s].p[i], co.p[j], q); });
+      }
+    return q;
+  };
+  if constexpr (KEYS) {
+    if (a.f.dense) {
+      const float undo = 0.5f * kLog2e * a.f.scale2 * *(const float*)(set + a.f.p.off_cscale);
+      float* tile = (float*)lds + (size_t)w * 16 * (W + 4);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int i = 0; i < 8; i += 4) {
+            f32x4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              y[j] = (float)x.x[rt][s].p[0][i + j];
+              if constexpr (XP == 2) y[j] += (float)x.x[rt][s].p[1][i + j];
+            }
+            *(f32x4*)(tile + c * (W + 4) + 32 * s + 8 * g + i) = y;
+          }
+        wave_fence();
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+          if ((FULL || 16 * ct < d) && (!DIRECT || ct % NW == w)) {
+            const f32x4 q = form_of(rt, ct);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[r] += q[r] * tile[(4 * g + r) * (W + 4) + 16 * ct + c];
+          }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] = over_lanes<16>(sum[r], [](float p, float q) { return p + q; });
+        if (c == 0) *(f32x4*)&red[(rt * NW + w) * 16 + 4 * g] = sum;
+        wave_fence();
+      }
+      __syncthreads();         // (and the tiles make room for the state)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        term[rt] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+          if (DIRECT || i == w) term[rt] += red[(rt * NW + i) * 16 + c];
+        term[rt] = term[rt] * x.undo[rt] * (x.undo[rt] * undo);
+      }
+      if constexpr (DIRECT) __syncthreads();      // (red is used again)
+    }
+    const float shift = slot >= 0 ? a.shift[st] : 0.f;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) term[rt] = x.live[rt] && slot >= 0 ? term[rt] - shift : kNone;
   }
   if (slot >= 0)
     walk_features<W, TP, P, NW, FULL, DIRECT>(
@@ -669,19 +736,7 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
         for (int ct = 0; ct < CT; ++ct)
           if (FULL || 16 * ct < d) {
             acc[rt][ct] *= kLn2;
-            if (!DIRECT || ct % NW == w) {
-              f32x4 q = {0.f, 0.f, 0.f, 0.f};
-              const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 2 * 512;
-#pragma unroll
-              for (int s = 0; s < S; ++s)
-                if (FULL || s < steps) {
-                  Op16<2> co;
-#pragma unroll
-                  for (int p = 0; p < 2; ++p) co.p[p] = *(const f16x8*)(img + (s * 2 + p) * 512 + lane * 8);
-                  each_product<XP, 2>([&](int i, int j) { q = mfma(x.x[rt][s].p[i], co.p[j], q); });
-                }
-              acc[rt][ct] += rho4 * q;
-            }
+            if (!DIRECT || ct % NW == w) acc[rt][ct] += rho4 * form_of(rt, ct);
           }
         tile_to_lds<W>(tile, acc[rt], f32x4{1.f, 1.f, 1.f, 1.f}, lane);
       } else {

@@ -81,12 +81,9 @@ SumPlan plan_sum(int B, int heads, long long tokens, long long rows, int d, int 
 SumPlan plan_append(const fs_features* f, int B, int L, int dv, int rot) {
   return plan_sum(B, f->heads, (long long)B * L, L, f->d, dv, f->M, rot, f->dense_c2 != 0, false, true);
 }
-SumPlan plan_attention(int B, int L, int rot) { return plan_sum(1, 1, (long long)B * L, 0, 1, 1, 1, rot, false, false, false); }
+SumPlan plan_rows(int B, int L, int rot) { return plan_sum(1, 1, (long long)B * L, 0, 1, 1, 1, rot, false, false, false); }
 SumPlan plan_attention_backward(const fs_features* f, int B, int H, int L, int dv, int rot) {
   return plan_sum(B, f->heads, (long long)B * L, (long long)L * (H / f->heads), f->d, dv, f->M, rot, true, true, true);
-}
-SumPlan plan_append_backward(const fs_features* f, int B, int L, int dv, int rot) {
-  return plan_sum(B, f->heads, (long long)B * L, L, f->d, dv, f->M, rot, true, false, false);
 }
 bool sizes_ok(const fs_features* f, int B, int H, int L, int dv, int rot) {
   return f != nullptr && f->heads >= 1 && f->d >= 1 && f->d <= 128 && f->M >= 1 && f->M <= kMaxFeatures && B >= 1 && H >= 1 && H % f->heads == 0 &&
@@ -205,7 +202,7 @@ int favorsharp_state_append(const fs_features* f, const fs_state* state, const i
     if (int rc = turn_of(rot, B, L, ws, p.off_table, &a.x.turn, s)) return rc;
     if (f->dense_c2) {
       a.terms = (float*)(ws + p.off_terms);
-      if (int rc = st::launch_row_terms(a.f, a.x, B, f->heads, nullptr, slots, state->slots, (float*)(ws + p.off_terms), s)) return rc;
+      if (int rc = st::launch_row_terms(a.f, a.x, B, f->heads, (float*)(ws + p.off_terms), s)) return rc;
     }
   }
   if (int rc = st::launch_build(a, s)) return rc;
@@ -215,7 +212,7 @@ int favorsharp_state_append(const fs_features* f, const fs_state* state, const i
 
 size_t favorsharp_state_attention_workspace_bytes(const fs_features* f, int B, int H, int L, int dv, int rot_dim) {
   if (!sizes_ok(f, B, H, L, dv, rot_dim)) return 0;
-  return plan_attention(B, L, rot_dim).total;
+  return plan_rows(B, L, rot_dim).total;
 }
 
 int favorsharp_state_attention(const fs_features* f, const fs_state* state, const int32_t* slots, const fs_tensor* Q, int B, int H, int L, int dv,
@@ -223,7 +220,7 @@ int favorsharp_state_attention(const fs_features* f, const fs_state* state, cons
                                size_t workspace_bytes, void* stream) {
   if (int rc = check(f, state, true, B, H, L, dv, rot)) return rc;
   if (!tensor_ok(Q, f->d, L > 0) || !tensor_ok(Y, dv, L > 0) || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
-  const SumPlan p = plan_attention(B, L, rot ? rot->rot_dim : 0);
+  const SumPlan p = plan_rows(B, L, rot ? rot->rot_dim : 0);
   if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
   if (L == 0) return FS_OK;
@@ -315,7 +312,7 @@ int favorsharp_state_attention_backward(const fs_features* f, const fs_state* st
 
 size_t favorsharp_state_append_backward_workspace_bytes(const fs_features* f, int B, int L, int dv, int rot_dim) {
   if (!sizes_ok(f, B, f ? f->heads : 0, L, dv, rot_dim)) return 0;
-  return plan_append_backward(f, B, L, dv, rot_dim).total;
+  return plan_rows(B, L, rot_dim).total;
 }
 
 int favorsharp_state_append_backward(const fs_features* f, const fs_state* state, const int32_t* slots, const fs_state* dstate, const fs_tensor* K,
@@ -325,21 +322,20 @@ int favorsharp_state_append_backward(const fs_features* f, const fs_state* state
   if (int rc = check(f, dstate, false, B, f->heads, L, dv, rot)) return rc;
   if (dstate->slots != state->slots) return FS_ERR_INVALID_ARG;
   if (!tensor_ok(K, f->d, L > 0) || !tensor_ok(V, dv, L > 0) || !tensor_ok(dK, f->d, L > 0) || !tensor_ok(dV, dv, L > 0) || K->dtype != V->dtype ||
-      workspace == nullptr || (uintptr_t)workspace % 16)
+      (uintptr_t)workspace % 16)
     return FS_ERR_INVALID_ARG;
-  const SumPlan p = plan_append_backward(f, B, L, dv, rot ? rot->rot_dim : 0);
+  const SumPlan p = plan_rows(B, L, rot ? rot->rot_dim : 0);
+  if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
   if (L == 0) return FS_OK;
   hipStream_t s = (hipStream_t)stream;
   char* ws = (char*)workspace;
-  float* terms = (float*)(ws + p.off_terms);
   st::GradArgs g{};
   g.f = features_of(f);
   g.x = st::Rows{dev(K), L, 1, lengths, f->d, st::Turn{}};
   g.r = st::Rows{dev(V), L, 1, lengths, dv, st::Turn{}};
   if (int rc = turn_of(rot, B, L, ws, p.off_table, &g.x.turn, s)) return rc;
-  if (int rc = st::launch_row_terms(g.f, g.x, B, f->heads, state->shift, slots, state->slots, terms, s)) return rc;
-  g.terms = terms;
+  g.shift = state->shift;
   g.slots = slots;
   g.state = state_of(dstate);
   g.B = B; g.Hk = f->heads; g.dv = dv;

@@ -438,7 +438,7 @@ int launch_values(const ValueArgs& a, hipStream_t st);
 struct GradArgs {
   Features f;
   Rows x, r;
-  const float* terms;            // keys: [B*Hk][rows] row terms less the state's shift
+  const float* shift;            // keys: [slots][Hk] of the states
   float *lse, *weights;          // queries: [B*Hk][rows]
   const int32_t* slots;
   State state;
@@ -450,10 +450,8 @@ int launch_key_grads(const GradArgs& a, hipStream_t st);
 
 int launch_prepare(const float* theta, int groups, const float* Omega, int omega_groups, int sets, int d, int M, float scale, char* buf,
                    const FeaturePlan& p, hipStream_t st);
-// Row terms r(k) of turned keys, rows behind the lengths -inf.  shift [slots][Hk] (or nullptr): less the shift of their state, sequences
-// without one, or with that of an earlier one, -inf.
-int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, const float* shift, const int32_t* slots, int nslots, float* terms,
-                     hipStream_t st);
+// Row terms r(k) of turned keys with a dense quadratic form, rows behind the lengths -inf.
+int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, float* terms, hipStream_t st);
 
 int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev& X2, int H2, int B, int L, int d, int transposed,
                   const TensorDev& Y, const TensorDev& Y2, hipStream_t st);

@@ -89,7 +89,8 @@ def test_the_other_entry_points_refuse(fs):
     assert L.favorsharp_state_attention_backward(P(f), P(s), None, P(t), P(t), 2, 4, 8, 64, None, None, P(t), P(ds), A, 1000, None) == 4
     assert L.favorsharp_state_append_backward(P(f), P(s), None, P(pool(fs, z=None)), P(t), P(t), 2, 8, 64, None, None, P(t), P(t), *ws) == 1
     assert L.favorsharp_state_append_backward(P(f), P(s), None, P(ds), P(t), P(t), 2, 8, 64, None, None, P(t), None, *ws) == 1
-    assert L.favorsharp_state_append_backward(P(f), P(s), None, P(ds), P(t), P(t), 2, 8, 64, None, None, P(t), P(t), A, 8, None) == 4
+    rot = fs.FsRotary(A, None, 0, 0, 64, 0, 1.0)
+    assert L.favorsharp_state_append_backward(P(f), P(s), None, P(ds), P(t), P(t), 2, 8, 64, None, P(rot), P(t), P(t), A, 8, None) == 4
     # more rows of a state than are counted in 32 bits
     assert L.favorsharp_state_attention(P(f), P(s), None, P(t), 1, 8, 1 << 28, 64, None, None, P(t), None, *ws) == 2
     # nothing to do
@@ -126,7 +127,8 @@ def test_workspace_sizes(fs):
     assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 4, 4096, 64, 0) == 0             # nothing is kept between launches
     assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 4, 4096, 64, 64) >= 4 * 4096 * 32 * 8
     assert L.favorsharp_state_attention_backward_workspace_bytes(P(f), 4, 4, 4096, 64, 0) >= 16 * 4096 * 8 + 8 * state
-    assert L.favorsharp_state_append_backward_workspace_bytes(P(f), 4, 4096, 64, 0) >= 8 * 4096 * 4
+    assert L.favorsharp_state_append_backward_workspace_bytes(P(f), 4, 4096, 64, 0) == 0
+    assert L.favorsharp_state_append_backward_workspace_bytes(P(f), 4, 4096, 64, 64) >= 4 * 4096 * 32 * 8
     assert L.favorsharp_state_append_workspace_bytes(None, 4, 4096, 64, 0) == 0
     assert L.favorsharp_state_append_workspace_bytes(P(f), 4, 4096, 129, 0) == 0
     assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 3, 4096, 64, 0) == 0
