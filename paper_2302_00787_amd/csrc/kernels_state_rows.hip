@@ -20,7 +20,7 @@ namespace {
 // 32 features' rows of the state in TP pieces.
 template <int W, int TP> struct StateLds {
   uint16_t t[TP][32][W + 8];
-  float z[32], bias[32];
+  float z[32], bias[32], scale[4];      // scale (its first): of W's 32 features
 };
 template <int W, int CP> struct ImageLds {
   uint16_t row[STEPS<W>][2][1024];
@@ -32,15 +32,16 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
                        NT = (8 * W + NTH - 1) / NTH;
   u32x4 row[NR], col[NC];
   f32x4 t[NT];
-  float z, bias;
+  float z, bias, scale;
   const char *row_img, *col_img;
-  const float *T, *zs, *biases;
+  const float *T, *zs, *biases, *scales;
   int steps, M, dv;
 
   __device__ __forceinline__ void start(const Features& f, int side, const char* set, const float* T_, const float* z_, int dv_) {
     row_img = set + f.p.off_row[side];
     col_img = set + f.p.off_col[side];
     biases = (const float*)(set + f.p.off_bias);
+    scales = (const float*)(set + f.p.off_scale[side]);
     T = T_; zs = z_; dv = FULL ? W : dv_; M = f.M;
     steps = FULL ? STEPS<W> : f.p.steps;
   }
@@ -73,6 +74,7 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
     if (tid < 32) {
       z = 32 * fb + tid < M ? zs[32 * fb + tid] : 0.f;
       bias = biases[32 * fb + tid];
+      scale = scales[fb];
     }
   }
   __device__ __forceinline__ void put(StateLds<W, TP>& s, ImageLds<W, CP>* img, int tid) {
@@ -105,6 +107,7 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
     if (tid < 32) {
       s.z[tid] = z;
       s.bias[tid] = bias;
+      if (tid < 4) s.scale[tid] = scale;
     }
   }
 };
@@ -390,7 +393,6 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   const int slot = slot_of(a.slots, a.state.slots, b), len = length_of(a.x, b), rows = a.x.L * a.x.G;
   const int v0 = (DIRECT ? piece.rows : piece.rows * NW + w) * 16 * RT;
   const char* set = a.f.set(h);
-  const float* scales = (const float*)(set + a.f.p.off_scale[0]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
   constexpr int WG_ROWS = 16 * RT * (DIRECT ? 1 : NW);
   if (piece.rows * WG_ROWS >= rows) return;
@@ -414,7 +416,7 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
         [&](const StateLds<W, P>& l, Weights<W, 0, DIRECT>& weights, bool first) {
           f32x4 E[RT][2];
           exponents(x, weights, steps, lane, E);
-          const float scale = scales[weights.fb];
+          const float scale = l.scale[0];
           f32x4 bias[2], zf[2];
 #pragma unroll
           for (int ft = 0; ft < 2; ++ft) {
@@ -514,7 +516,6 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
             rows = a.x.L * a.x.G;
   const int v0 = (DIRECT ? piece.rows : piece.rows * NW + w) * 16 * RT;
   const char* set = a.f.set(h);
-  const float* scales = (const float*)(set + a.f.p.off_scale[KEYS]);
   const size_t st = (size_t)max(slot, 0) * a.Hk + h;
   constexpr int WG_ROWS = 16 * RT * (DIRECT ? 1 : NW);
   if (piece.rows * WG_ROWS >= rows) return;
@@ -642,7 +643,7 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
                   for (int ft = 0; ft < 2; ++ft) D[rt][ft] = mfma(t[ft].p[i], rr[rt][s].p[j], D[rt][ft]);
               });
             }
-          const float scale = scales[weights.fb];
+          const float scale = l.scale[0];
           Op<P> uo[RT], so[RT];
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
@@ -779,7 +780,7 @@ int lds_room(const void* kernel, size_t lds) {
 bool few_rows(int BH, long long rows) { return BH * ((rows + 255) / 256) < 192; }
 
 template <int W, int XP, int P, bool FULL, bool DIRECT> int values(const ValueArgs& a, hipStream_t st) {
-  constexpr int NW = DIRECT && W == 128 ? 4 : 8, RT = 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr int NW = DIRECT == (W == 128) ? 4 : 8, RT = 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
   constexpr size_t lds = rows_lds<W, P, 0, NW, RT, DIRECT>();
   static_assert(lds <= 156 * 1024, "LDS of a CU");
   auto kernel = k_values<W, XP, P, NW, RT, FULL, DIRECT>;
@@ -799,7 +800,7 @@ template <int W> int values_width(const ValueArgs& a, hipStream_t st) {
 }
 
 template <int W, int XP, int RP, int P, bool FULL, bool DIRECT, bool KEYS> int grads(const GradArgs& a, hipStream_t st) {
-  constexpr int NW = DIRECT && W == 128 ? 4 : 8, RT = W == 128 || (DIRECT && W == 64) ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr int NW = DIRECT == (W == 128) ? 4 : 8, RT = W == 128 || (DIRECT && W == 64) ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
   constexpr size_t lds = rows_lds<W, KEYS ? P : 3, P, NW, RT, DIRECT>();
   static_assert(lds <= 156 * 1024, "LDS of a CU");
   auto kernel = k_grads<W, XP, RP, P, NW, RT, FULL, DIRECT, KEYS>;
