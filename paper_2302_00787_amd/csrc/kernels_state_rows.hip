@@ -463,11 +463,13 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   for (int rt = 0; rt < RT; ++rt) {
     const bool zero = den[rt][0] == 0.f;
     unread += (lane < 16) && (!DIRECT || w == 0) && x.live[rt] && zero;
-    // (a quotient whose divisor is subnormal has no inverse)
-    const f32x4 k = by_row(zero ? 0.f : DIRECT ? factor[rt] : 1.f, lane), d4 = by_row(zero ? 1.f : den[rt][0], lane);
+    // (a subnormal divisor has no inverse: it and the sums are raised by 2^64 first, what the sums, smaller still times Y, allow)
+    const float up = den[rt][0] < 0x1p-64f ? 0x1p64f : 1.f;
+    const f32x4 k = by_row(zero ? 0.f : factor[rt] / (den[rt][0] * up), lane), up4 = by_row(up, lane);
     float* tile = (float*)lds + (DIRECT ? (size_t)w * RT + rt : (size_t)w) * 16 * (W + 4);
+    if (__any(up != 1.f))
 #pragma unroll
-    for (int vt = 0; vt < VT; ++vt) acc[rt][vt] /= d4;
+      for (int vt = 0; vt < VT; ++vt) acc[rt][vt] *= up4;
     tile_to_lds<W>(tile, acc[rt], k, lane);
     if constexpr (!DIRECT) {
       wave_fence();

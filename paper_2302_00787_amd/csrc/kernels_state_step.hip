@@ -14,128 +14,7 @@ namespace fs {
 namespace st {
 namespace {
 
-// ---------------------------------------------------------------------------------------------- exponents
-// Tiles of sixteen rows: keys of sequences (first a.key_tiles of them), then queries, row v = query head v % G of sequence v / G.
-template <int S>
-__global__ void __launch_bounds__(256) k_step_exponents(StepArgs a) {
-  __shared__ float2 angles[16][64];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-  const int h = blockIdx.y, G = a.H / a.Hk, fb = blockIdx.x * 4 + w, Mp = a.f.p.Mp, nfb = Mp / 32, steps = a.f.p.steps, d = a.f.d, M = a.f.M;
-  const bool keys = (int)blockIdx.z < a.key_tiles;
-  const int per = keys ? 1 : G, rows = a.B * per, v0 = 16 * (keys ? blockIdx.z : blockIdx.z - a.key_tiles);
-  const char* set = a.f.set(h);
-  const int pairs = a.rot.rot >> 1;
-  f16x8 wo[S][2][2];             // [step][piece][tile]
-  if (fb < nfb) {
-    const uint16_t* at = (const uint16_t*)(set + a.f.p.off_row[keys]) + (size_t)fb * steps * 2048 + lane * 8;
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (s < steps)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int ft = 0; ft < 2; ++ft) wo[s][i][ft] = *(const f16x8*)(at + (s * 2 + i) * 1024 + ft * 512);
-  }
-  const TensorDev& X = keys ? a.K : a.Q;
-  const int v = v0 + c, vc = min(v, rows - 1), b = vc / per;
-  const long long base = row_base(X, b, keys ? h : h * G + vc % per, 0);
-  const Turn turn{nullptr, a.rot.rot, a.rot.interleaved};
-  RowUnits<S, false, true> units;
-  units.fetch(X, base, d, turn, g);
-  for (int e = tid; e < 16 * pairs; e += 256) {
-    const int r = e / pairs, i = e - r * pairs, row = min(v0 + r, rows - 1);
-    angles[r][i] = cos_sin(position_of(a.rot, row / per, 0), a.rot.freqs[i], a.rot.amplitude);
-  }
-  __syncthreads();
-  if (fb >= nfb) return;
-  f32x8 n[S];
-  float most = 0.f, norm = 0.f;
-  units.finish(X, base, d, turn, &angles[c][0], true, g, n);
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-    most = fmaxf(most, largest_of(n[s]));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) norm += n[s][i] * n[s][i];
-  }
-  most = fmaxf(most, __shfl_xor(most, 16));
-  most = fmaxf(most, __shfl_xor(most, 32));
-  const float scale = up_to_2_14(most);
-  Op16<2> x[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) x[s] = as_op16<2>(n[s] * scale);
-  f32x4 E[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-  for (int s = 0; s < S; ++s)
-    if (s < steps)
-      each_product<2, 2>([&](int i, int j) {
-#pragma unroll
-        for (int ft = 0; ft < 2; ++ft) E[ft] = mfma(wo[s][i][ft], x[s].p[j], E[ft]);
-      });
-  const float undo = power_inverse(scale) * ((const float*)(set + a.f.p.off_scale[keys]))[fb];
-  const float* bias = (const float*)(set + a.f.p.off_bias);
-  if (v < rows) {
-    float* to = a.exps + ((size_t)(b * a.Hk + h) * (1 + G) + (keys ? 0 : 1 + vc % per)) * Mp;
-#pragma unroll
-    for (int ft = 0; ft < 2; ++ft) {
-      const int m = 32 * fb + 16 * ft + 4 * g;
-      *(f32x4*)(to + m) = E[ft] * undo + *(const f32x4*)(bias + m);
-    }
-  }
-  if (!keys) return;
-  // the sequences' z of these features as they are, and once their shift and the keys' row terms
-  const int slot = slot_of(a.slots, a.state.slots, b);
-  if (v < rows && slot >= 0) {
-    const float* z = a.state.z + ((size_t)slot * a.Hk + h) * M;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int m = 32 * fb + 8 * g + i;
-      if (m < M) a.old_z[(size_t)(b * a.Hk + h) * Mp + m] = z[m];
-    }
-  }
-  if (fb > 0) return;
-  float term;
-  if (a.f.dense) {               // k' (C2 + C2') k / 2, whose rows of sixteen coordinates meet the row's numbers by way of LDS
-    __shared__ __align__(16) float y[16][32 * S + 4];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      *(f32x4*)&y[c][32 * s + 8 * g] = f32x4{n[s][0], n[s][1], n[s][2], n[s][3]};
-      *(f32x4*)&y[c][32 * s + 8 * g + 4] = f32x4{n[s][4], n[s][5], n[s][6], n[s][7]};
-    }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-    term = 0.f;
-#pragma unroll
-    for (int ct = 0; ct < 2 * S; ++ct) {         // (no branches, so that the images are on their way together: behind d the row is zeros)
-      f32x4 q = {0.f, 0.f, 0.f, 0.f};
-      const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)min(ct, 2 * steps - 1) * steps * 1024 + lane * 8;
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const uint16_t* at = img + min(s, steps - 1) * 1024;
-        const f16x8 p[2] = {*(const f16x8*)at, *(const f16x8*)(at + 512)};
-        each_product<2, 2>([&](int i, int j) { q = mfma(p[i], x[s].p[j], q); });
-      }
-      const f32x4 k = *(const f32x4*)&y[c][16 * ct + 4 * g];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) term += q[r] * k[r];
-    }
-    term *= 0.5f * power_inverse(scale) * *(const float*)(set + a.f.p.off_cscale);
-  } else {
-    term = -0.5f * norm;
-  }
-  term += __shfl_xor(term, 16);
-  term += __shfl_xor(term, 32);
-  if (v < rows && g == 0)
-    a.old_shift[b * a.Hk + h] = make_float2(slot >= 0 ? a.state.shift[(size_t)slot * a.Hk + h] : kNone, term * kLog2e * a.f.scale2);
-}
-
-// ---------------------------------------------------------------------------------------------- states
-// Floats in LDS: features (key, GC queries), the threads' partial outputs, maxima and normalisers by wave.
-template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int Mp) {
-  return (GC + 1) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64) + (GC + 1) * 128 + NTH / 64;
-}
-
-// (ONE) W of 32 features and a row of LDS as operands, the row in every column.
+// W of 32 features and a row of LDS (zeros behind its end) as operands.
 template <int S> struct StepWeights {
   f16x8 p[S][2][2];              // [step][piece][tile]
   __device__ __forceinline__ void load(const char* img, int fb, int steps, int lane) {
@@ -149,7 +28,7 @@ template <int S> struct StepWeights {
   }
 };
 template <int S> struct StepRow {
-  Op16<2> x[S];                  // (zeros behind the row's end)
+  Op16<2> x[S];
   float undo, norm;              // norm: |x|^2
   __device__ __forceinline__ void load(const float* row, int lane) {
     f32x8 n[S];
@@ -189,6 +68,114 @@ template <int S> struct StepRow {
       }
   }
 };
+
+// x' (C2 + C2') x / 2 of the rows' keys, coordinates of sixteen w, w + of, ... (y: the row that this lane has in the operands).
+template <int S>
+__device__ __forceinline__ float form_of(const StepRow<S>& row, const Features& f, const char* set, const float* y, int w, int of, int lane) {
+  float sum = 0.f;
+  const int steps = f.p.steps;
+#pragma unroll 1
+  for (int ct = w; ct < 2 * steps; ct += of) {
+    f32x4 q = {0.f, 0.f, 0.f, 0.f};
+    const uint16_t* img = (const uint16_t*)(set + f.p.off_csym) + (size_t)ct * steps * 1024 + lane * 8;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {                // (behind d the row is zeros)
+      const uint16_t* from = img + min(s, steps - 1) * 1024;
+      const f16x8 p[2] = {*(const f16x8*)from, *(const f16x8*)(from + 512)};
+      each_product<2, 2>([&](int i, int j) { q = mfma(p[i], row.x[s].p[j], q); });
+    }
+    const f32x4 k = *(const f32x4*)(y + 16 * ct + 4 * (lane >> 4));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sum += q[r] * k[r];
+  }
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  return sum * (0.5f * kLog2e * f.scale2 * row.undo * *(const float*)(set + f.p.off_cscale));
+}
+
+// ---------------------------------------------------------------------------------------------- exponents
+// Tiles of sixteen rows: keys of sequences (first a.key_tiles of them), then queries, row v = query head v % G of sequence v / G.  Workgroups x have
+// 128 features each; where quadratic forms are dense, one more makes the keys' row terms meanwhile, its waves sixteen coordinates at a time.
+template <int S>
+__global__ void __launch_bounds__(256) k_step_exponents(StepArgs a) {
+  __shared__ __align__(16) float x[16][132];
+  __shared__ int position[16];
+  __shared__ float parts[4][16];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+  const int h = blockIdx.y, G = a.H / a.Hk, fb = blockIdx.x * 4 + w, Mp = a.f.p.Mp, nfb = Mp / 32, steps = a.f.p.steps, M = a.f.M;
+  const bool keys = (int)blockIdx.z < a.key_tiles, form = a.f.dense && blockIdx.x == gridDim.x - 1;
+  if (form && !keys) return;
+  const int per = keys ? 1 : G, rows = a.B * per, v0 = 16 * (keys ? blockIdx.z : blockIdx.z - a.key_tiles);
+  const char* set = a.f.set(h);
+  StepWeights<S> weights;
+  if (fb < nfb) weights.load(set + a.f.p.off_row[keys], fb, steps, lane);
+  // the rows' numbers: a thread has a column of every other row, all on their way together
+  const TensorDev& X = keys ? a.K : a.Q;
+  const int col = tid & 127, at_col = min(col, a.f.d - 1);
+  long long at[8];
+  uint32_t bits[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = min(v0 + 2 * i + (tid >> 7), rows - 1);
+    at[i] = row_base(X, r / per, keys ? h : h * G + r % per, 0) + at_col;
+  }
+  if (X.dtype == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bits[i] = ((const uint32_t*)X.ptr)[at[i]];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bits[i] = (uint32_t)((const uint16_t*)X.ptr)[at[i]] << 16;
+  }
+  const int v = v0 + c, vc = min(v, rows - 1), b = vc / per;
+  if (tid < 16 && a.rot.rot > 0) position[tid] = position_of(a.rot, b, 0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[2 * i + (tid >> 7)][col] = col < a.f.d ? __uint_as_float(bits[i]) : 0.f;
+  __syncthreads();
+  const int pairs = a.rot.rot >> 1;
+#pragma unroll 1
+  for (int e = tid; e < 16 * pairs; e += 256) {
+    const int r = e / pairs, i = e - r * pairs, i0 = a.rot.interleaved ? 2 * i : i, i1 = a.rot.interleaved ? 2 * i + 1 : i + pairs;
+    const float2 cs = cos_sin(position[r], a.rot.freqs[i], a.rot.amplitude);
+    const float p = x[r][i0], q = x[r][i1];
+    x[r][i0] = p * cs.x - q * cs.y;
+    x[r][i1] = q * cs.x + p * cs.y;
+  }
+  __syncthreads();
+  StepRow<S> row;
+  row.load(&x[c][0], lane);
+  const int slot = slot_of(a.slots, a.state.slots, b);
+  const float shift = keys && v < rows && slot >= 0 ? a.state.shift[(size_t)slot * a.Hk + h] : kNone;
+  if (form) {
+    parts[w][c] = form_of(row, a.f, set, &x[c][0], w, 4, lane);
+    __syncthreads();
+    if (w > 0 || g > 0 || v >= rows) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += parts[i][c];
+    a.old_shift[b * a.Hk + h] = make_float2(shift, sum);
+    return;
+  }
+  if (fb >= nfb) return;
+  row.exponents(weights, ((const float*)(set + a.f.p.off_scale[keys]))[fb], (const float*)(set + a.f.p.off_bias) + 32 * fb,
+                a.exps + ((size_t)(b * a.Hk + h) * (1 + G) + (keys ? 0 : 1 + vc % per)) * Mp + 32 * fb, v < rows, lane);
+  if (!keys) return;
+  // the sequences' z of these features as they are, and once their shift and the keys' row terms
+  if (v < rows && slot >= 0) {
+    const float* z = a.state.z + ((size_t)slot * a.Hk + h) * M;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int m = 32 * fb + 8 * g + i;
+      if (m < M) a.old_z[(size_t)(b * a.Hk + h) * Mp + m] = z[m];
+    }
+  }
+  if (fb == 0 && !a.f.dense && v < rows && g == 0) a.old_shift[b * a.Hk + h] = make_float2(shift, -0.5f * kLog2e * a.f.scale2 * row.norm);
+}
+
+// ---------------------------------------------------------------------------------------------- states
+// Floats in LDS: features (key, GC queries), the threads' partial outputs, maxima and normalisers by wave.
+template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int Mp) {
+  return (GC + 1) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64) + (GC + 1) * 128 + NTH / 64;
+}
 
 // GC: query heads that a pass over the state serves.  Workgroup z has the columns z cols .. (z + 1) cols - 1.
 template <int S, int VEC, int GC, int NTH, bool ONE>
@@ -264,26 +251,7 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
         if (fb != w || g0 > 0) weights.load(set + a.f.p.off_row[1], fb, steps, lane);
         row.exponents(weights, ((const float*)(set + a.f.p.off_scale[1]))[fb], bias + 32 * fb, feat + 32 * fb, (lane & 15) == 0, lane);
       }
-      float term = w == 0 ? -0.5f * kLog2e * a.f.scale2 * row.norm : 0.f;
-      if (a.f.dense) {           // k' (C2 + C2') k / 2, sixteen coordinates a wave at a time
-        float sum = 0.f;
-        for (int ct = w; ct < 2 * steps; ct += NW) {
-          f32x4 q = {0.f, 0.f, 0.f, 0.f};
-          const uint16_t* img = (const uint16_t*)(set + a.f.p.off_csym) + (size_t)ct * steps * 1024 + lane * 8;
-#pragma unroll
-          for (int s = 0; s < S; ++s) {
-            const uint16_t* from = img + min(s, steps - 1) * 1024;
-            const f16x8 p[2] = {*(const f16x8*)from, *(const f16x8*)(from + 512)};
-            each_product<2, 2>([&](int i, int j) { q = mfma(p[i], row.x[s].p[j], q); });
-          }
-          const f32x4 y = *(const f32x4*)(x + 16 * ct + 4 * (lane >> 4));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sum += q[r] * y[r];
-        }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        term = sum * (0.5f * kLog2e * a.f.scale2 * row.undo * *(const float*)(set + a.f.p.off_cscale));
-      }
+      const float term = a.f.dense ? form_of(row, a.f, set, x, w, NW, lane) : w == 0 ? -0.5f * kLog2e * a.f.scale2 * row.norm : 0.f;
       if (lane == 0) word[w] = term;
       row.load(x + (1 + min(lane & 15, n - 1)) * 128, lane);
       for (int fb = w; fb < nfb; fb += NW) {
@@ -399,7 +367,7 @@ template <int S, int NTH, bool ONE> int step_heads(const StepArgs& a, hipStream_
   if (a.H == a.Hk) return a.dv % 4 == 0 ? step<S, 4, 1, NTH, ONE>(a, st) : step<S, 1, 1, NTH, ONE>(a, st);
   return a.dv % 4 == 0 ? step<S, 4, 4, NTH, ONE>(a, st) : step<S, 1, 4, NTH, ONE>(a, st);
 }
-bool step_in_one(int B, int Hk) { return (long long)B * Hk < 256; }
+bool step_in_one(int B, int Hk) { return (long long)B * Hk < 64; }
 
 }  // namespace
 
@@ -416,7 +384,7 @@ int launch_step(StepArgs a, float* room, hipStream_t st) {
   a.old_z = a.exps + (size_t)a.B * (a.H + a.Hk) * Mp;
   a.key_tiles = (a.B + 15) / 16;
   const long long tiles = a.key_tiles + ((long long)a.B * G + 15) / 16;
-  const dim3 grid((Mp / 32 + 3) / 4, a.Hk, (unsigned)tiles);
+  const dim3 grid((Mp / 32 + 3) / 4 + (a.f.dense ? 1 : 0), a.Hk, (unsigned)tiles);
   if (steps == 1) hipLaunchKernelGGL(k_step_exponents<1>, grid, dim3(256), 0, st, a);
   else if (steps == 2) hipLaunchKernelGGL(k_step_exponents<2>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_step_exponents<4>, grid, dim3(256), 0, st, a);
