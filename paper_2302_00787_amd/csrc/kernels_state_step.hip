@@ -1,11 +1,12 @@
 // The next token of every sequence: its key and value onto the state, then its queries against it.
 //
-// The states are read once and written once (2 M (dv + 1) numbers of 4 bytes a key head), which bounds the call.  Many states: a launch of its own
-// makes the exponents first, sixteen rows of a head at a time on the matrix instructions as in the other kernels, so that W is read once for
-// sixteen rows and not once for each state, whose size it has; it also keeps the states' z and shift as they were, so that the second
-// launch can cut a state into columns for as many workgroups as fill the chip.  Fewer states than CUs: one launch (ONE), a state a workgroup,
-// W from L2.  (us, one launch / two: 8 states of 256 x 64 18.4 / 23.5, 180 of 512 x 128 with four query heads 43.9 / 48.0, 2048 of 256 x 64
-// 75 / 74.)
+// The states are read once and written once (2 M (dv + 1) numbers of 4 bytes a key head), which bounds the call.  A launch of its own makes the
+// exponents first, sixteen rows of a head at a time on the matrix instructions as in the other kernels, so that W is read once for sixteen
+// rows and not once for each state, whose size it has; it also keeps the states' z and shift as they were, so that the second launch can
+// cut a state into columns for as many workgroups as fill the chip.  Few small states (at most 256, as many as CUs, one query head to a
+// key head, W of 256 features of 64 numbers, 32 features a wave): one launch (ONE), a state a workgroup, W from L2.  (Kernels' us, one launch /
+// two: 8 states of 256 x 64 10.5 / 14.3, 248 of them 13.1 / 18.6; where the rule ends: 8 of 512 x 128 19.4 / 18.0, 8 of 1024 x 64 19.5 / 19.6,
+// 128 of those 30.1 / 28.0, 180 of 512 x 128 with four query heads 49.8 / 38.5.  Two launches: 2048 of 256 x 64 55.)
 #include <algorithm>
 
 #include "state_common.h"
@@ -181,14 +182,14 @@ template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int
 template <int S, int VEC, int GC, int NTH, bool ONE>
 __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
   typedef __attribute__((ext_vector_type(VEC))) float vec;
-  constexpr int NW = NTH / 64, AHEAD = GC == 1 || ONE ? 8 : 4;   // fours of the state on their way for each thread
+  constexpr int NW = NTH / 64, AHEAD = GC == 1 ? 8 : 4;   // fours of the state on their way for each thread
   extern __shared__ __align__(16) float lds[];
   const int Mp = a.f.p.Mp, M = a.f.M, dv = a.dv, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   float* feat = lds;                           // [GC + 1][Mp]
   float* part = feat + (GC + 1) * Mp;          // [GC][rows of a pass][columns]
   float* tops = part + 4 * GC * NTH;           // [GC + 1][NW]
   float* dens = tops + (1 + GC) * NW;          // [GC][NW]
-  float* x = dens + (1 + GC) * NW;             // (ONE) [GC + 1][128] the key, queries
+  float* x = dens + (1 + GC) * NW;             // (ONE) [2][128] the key, the query
   float* word = x + (GC + 1) * 128;            // (ONE) the key's row term by wave
   const int b = blockIdx.x, h = blockIdx.y, G = GC == 1 ? 1 : a.H / a.Hk, col0 = blockIdx.z * a.cols, cols = min(a.cols, dv - col0);
   const int slot = unique_slot_of(a.slots, a.state.slots, b);
@@ -209,10 +210,12 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
   float2 before;                               // shift, the key's row term
   const char* set = a.f.set(h);
   const int steps = a.f.p.steps, nfb = Mp / 32, pairs = a.rot.rot >> 1;
-  StepWeights<S> weights;
+  StepWeights<S> weights[2];     // (ONE) the queries', the key's
   if constexpr (ONE) {
     before = make_float2(a.state.shift[at], 0.f);
-    if (w < nfb) weights.load(set + a.f.p.off_row[1], w, steps, lane);
+    if (w < nfb)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) weights[i].load(set + a.f.p.off_row[i], w, steps, lane);
   } else {
     before = a.old_shift[bh];
   }
@@ -228,11 +231,10 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
     if (g0 > 0) __syncthreads();
     if constexpr (ONE) {
       // rows: a thread a number, of a turned pair both
-      const float* bias = (const float*)(set + a.f.p.off_bias);
-      for (int e = tid; e < (n + 1) * 128; e += NTH) {
+      for (int e = tid; e < 256; e += NTH) {
         const int r = e >> 7, c = e & 127;
         const TensorDev& src = r == 0 ? a.K : a.Q;
-        const long long base = row_base(src, b, r == 0 ? h : h * G + g0 + r - 1, 0);
+        const long long base = row_base(src, b, h, 0);
         float* to = x + r * 128;
         if (c < pairs) {
           const int i0 = a.rot.interleaved ? 2 * c : c, i1 = a.rot.interleaved ? 2 * c + 1 : c + pairs;
@@ -244,21 +246,15 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
         if (c >= 2 * pairs) to[c] = c < a.f.d ? load_elem(src, base + c) : 0.f;
       }
       __syncthreads();
-      // exponents, 32 features a wave at a time
+      // exponents: the same row in every column of the operands
+      const float* bias = (const float*)(set + a.f.p.off_bias) + 32 * w;
       StepRow<S> row;
       row.load(x, lane);
-      for (int fb = w; fb < nfb; fb += NW) {
-        if (fb != w || g0 > 0) weights.load(set + a.f.p.off_row[1], fb, steps, lane);
-        row.exponents(weights, ((const float*)(set + a.f.p.off_scale[1]))[fb], bias + 32 * fb, feat + 32 * fb, (lane & 15) == 0, lane);
-      }
+      if (w < nfb) row.exponents(weights[1], ((const float*)(set + a.f.p.off_scale[1]))[w], bias, feat + 32 * w, (lane & 15) == 0, lane);
       const float term = a.f.dense ? form_of(row, a.f, set, x, w, NW, lane) : w == 0 ? -0.5f * kLog2e * a.f.scale2 * row.norm : 0.f;
       if (lane == 0) word[w] = term;
-      row.load(x + (1 + min(lane & 15, n - 1)) * 128, lane);
-      for (int fb = w; fb < nfb; fb += NW) {
-        weights.load(set + a.f.p.off_row[0], fb, steps, lane);
-        row.exponents(weights, ((const float*)(set + a.f.p.off_scale[0]))[fb], bias + 32 * fb, feat + (1 + min(lane & 15, n - 1)) * Mp + 32 * fb,
-                      (lane & 15) < n, lane);
-      }
+      row.load(x + 128, lane);
+      if (w < nfb) row.exponents(weights[0], ((const float*)(set + a.f.p.off_scale[0]))[w], bias, feat + Mp + 32 * w, (lane & 15) == 0, lane);
       __syncthreads();
       before.y = 0.f;
 #pragma unroll
@@ -292,8 +288,7 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
     for (int m = tid; m < Mp; m += NTH) {
       const float s = top[0] == kNone ? 0.f : fast_exp2(feat[m] - top[0]);
       float z = s;
-      if (ONE && g0 > 0) z = m < M ? old_z[m] : 0.f;             // (this thread's own, written by the first pass)
-      else if (keep != 0.f && m < M) z += keep * old_z[m];
+      if (keep != 0.f && m < M) z += keep * old_z[m];
       feat[m] = s;
       if (m < M && g0 == 0 && blockIdx.z == 0) a.state.z[at * M + m] = z;
 #pragma unroll
@@ -363,21 +358,21 @@ template <int S, int VEC, int GC, int NTH, bool ONE> int step(const StepArgs& a,
   hipLaunchKernelGGL(kernel, dim3(a.B, a.Hk, (a.dv + a.cols - 1) / a.cols), dim3(NTH), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int S, int NTH, bool ONE> int step_heads(const StepArgs& a, hipStream_t st) {
-  if (a.H == a.Hk) return a.dv % 4 == 0 ? step<S, 4, 1, NTH, ONE>(a, st) : step<S, 1, 1, NTH, ONE>(a, st);
-  return a.dv % 4 == 0 ? step<S, 4, 4, NTH, ONE>(a, st) : step<S, 1, 4, NTH, ONE>(a, st);
+template <int S> int step_one(const StepArgs& a, hipStream_t st) {
+  return a.dv % 4 == 0 ? step<S, 4, 1, 512, true>(a, st) : step<S, 1, 1, 512, true>(a, st);
 }
-bool step_in_one(int B, int Hk) { return (long long)B * Hk < 64; }
+bool step_in_one(int B, int H, int Hk, int d, int Mp) { return H == Hk && (long long)B * Hk <= 256 && d <= 64 && Mp <= 256; }
 
 }  // namespace
 
-size_t step_floats(int B, int H, int Hk, int Mp) { return step_in_one(B, Hk) ? 0 : (size_t)B * ((size_t)(H + Hk) * Mp + (size_t)Hk * Mp + 2 * Hk) + 4; }
+size_t step_floats(int B, int H, int Hk, int d, int Mp) {
+  return step_in_one(B, H, Hk, d, Mp) ? 0 : (size_t)B * ((size_t)(H + Hk) * Mp + (size_t)Hk * Mp + 2 * Hk) + 4;
+}
 
 int launch_step(StepArgs a, float* room, hipStream_t st) {
   const int Mp = a.f.p.Mp, steps = a.f.p.steps, G = a.H / a.Hk;
   a.cols = a.dv;
-  if (step_in_one(a.B, a.Hk))
-    return steps == 1 ? step_heads<1, 512, true>(a, st) : steps == 2 ? step_heads<2, 512, true>(a, st) : step_heads<4, 512, true>(a, st);
+  if (step_in_one(a.B, a.H, a.Hk, a.f.d, Mp)) return steps == 1 ? step_one<1>(a, st) : step_one<2>(a, st);
   a.old_shift = (float2*)room;
   a.exps = room + 2 * (size_t)a.B * a.Hk;
   a.exps += (4 - ((a.exps - room) & 3)) & 3;
@@ -391,7 +386,8 @@ int launch_step(StepArgs a, float* room, hipStream_t st) {
   if (hipGetLastError() != hipSuccess) return 5;
   // a state in halves or quarters of its columns, 16 at least, until four workgroups a CU are there
   while ((long long)a.B * a.Hk * ((a.dv + a.cols - 1) / a.cols) < 1024 && a.cols % 32 == 0 && 4 * a.cols > a.dv) a.cols /= 2;
-  return step_heads<1, 256, false>(a, st);
+  if (G == 1) return a.dv % 4 == 0 ? step<1, 4, 1, 256, false>(a, st) : step<1, 1, 1, 256, false>(a, st);
+  return a.dv % 4 == 0 ? step<1, 4, 4, 256, false>(a, st) : step<1, 1, 4, 256, false>(a, st);
 }
 
 }  // namespace st

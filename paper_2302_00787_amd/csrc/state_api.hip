@@ -239,7 +239,7 @@ int favorsharp_state_attention(const fs_features* f, const fs_state* state, cons
 
 size_t favorsharp_state_step_workspace_bytes(const fs_features* f, int B, int H) {
   if (!sizes_ok(f, B, H, 1, 1, 0)) return 0;
-  return align_up(st::step_floats(B, H, f->heads, st::feature_plan(f->d, f->M, 1).Mp) * sizeof(float));
+  return align_up(st::step_floats(B, H, f->heads, f->d, st::feature_plan(f->d, f->M, 1).Mp) * sizeof(float));
 }
 
 int favorsharp_state_step(const fs_features* f, const fs_state* state, const int32_t* slots, const fs_tensor* Q, const fs_tensor* K,

@@ -470,7 +470,7 @@ struct StepArgs {
   float2* old_shift;             // [B][Hk] shift before, the key's row term
   int key_tiles, cols;
 };
-size_t step_floats(int B, int H, int Hk, int Mp);
+size_t step_floats(int B, int H, int Hk, int d, int Mp);
 int launch_step(StepArgs a, float* room, hipStream_t st);
 
 }  // namespace st

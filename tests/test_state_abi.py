@@ -132,7 +132,7 @@ def test_workspace_sizes(fs):
     assert L.favorsharp_state_append_workspace_bytes(None, 4, 4096, 64, 0) == 0
     assert L.favorsharp_state_append_workspace_bytes(P(f), 4, 4096, 129, 0) == 0
     assert L.favorsharp_state_attention_workspace_bytes(P(f), 4, 3, 4096, 64, 0) == 0
-    assert L.favorsharp_state_step_workspace_bytes(P(f), 4, 4) == 0                                # one launch
+    assert L.favorsharp_state_step_workspace_bytes(P(f), 4, 2) == 0                                # one launch
     assert L.favorsharp_state_step_workspace_bytes(P(f), 256, 4) >= 256 * (4 + 2 + 2) * 256 * 4
     assert L.favorsharp_state_features_bytes(2, 64, 256, 1, 2) > 2 * 2 * 256 * 64 * (4 + 6)
     assert L.favorsharp_state_features_bytes(2, 64, 256, 3, 2) == L.favorsharp_state_features_bytes(2, 64, 4000, 1, 1) == 0
