@@ -498,6 +498,13 @@ def _on(device):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+def _empty(shape, dtype, device) -> torch.Tensor:
+    """A result, its rows at multiples of 16 bytes as the library wants them."""
+    if shape[-1] % 8 == 0:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return torch.empty((*shape[:-1], shape[-1] + 7 & ~7), dtype=dtype, device=device)[..., :shape[-1]]
+
+
 def _room(nbytes: int, device, workspace: torch.Tensor | None):
     """Workspace of a call on states: (pointer, bytes, what holds it)."""
     if workspace is None and nbytes == 0:
@@ -585,14 +592,14 @@ def rotary(X: torch.Tensor, rot: Rotary, X2: torch.Tensor | None = None, transpo
     out may be X itself, out2 X2."""
     B, H, L, d = X.shape
     if out is None:
-        out = torch.empty((B, H, L, d), dtype=X.dtype, device=X.device)
+        out = _empty((B, H, L, d), X.dtype, X.device)
     _shaped("out", out, X.shape)
     H2 = 0
     if X2 is not None:
         H2 = X2.shape[1]
         _shaped("X2", X2, (B, H2, L, d))
         if out2 is None:
-            out2 = torch.empty((B, H2, L, d), dtype=X2.dtype, device=X.device)
+            out2 = _empty((B, H2, L, d), X2.dtype, X.device)
         _shaped("out2", out2, X2.shape)
     device = _one_device(X, X2, out, out2, *_rotary_tensors(rot))
     r, _ = _rotary_desc(rot, B, L)
@@ -661,7 +668,7 @@ def state_attention(f: Features, state: State, Q: torch.Tensor, lengths: torch.T
     dv = state.T.shape[3]
     _shaped("Q", Q, (B, H, L, f.desc.d))
     if out is None:
-        out = torch.empty((B, H, L, dv), dtype=out_dtype or Q.dtype, device=Q.device)
+        out = _empty((B, H, L, dv), out_dtype or Q.dtype, Q.device)
     _shaped("out", out, (B, H, L, dv))
     device = _one_device(Q, out, f.buffer, *state, lengths, slots, unread, workspace, *_rotary_tensors(rotary))
     r, rot_dim = _rotary_desc(rotary, B, L)
@@ -685,7 +692,7 @@ def state_step(f: Features, state: State, Q: torch.Tensor, K: torch.Tensor, V: t
     _shaped("K", K, (B, f.desc.heads, 1, d))
     _shaped("V", V, (B, f.desc.heads, 1, dv))
     if out is None:
-        out = torch.empty((B, H, 1, dv), dtype=out_dtype or Q.dtype, device=Q.device)
+        out = _empty((B, H, 1, dv), out_dtype or Q.dtype, Q.device)
     _shaped("out", out, (B, H, 1, dv))
     device = _one_device(Q, K, V, out, f.buffer, *state, slots, unread, workspace, *_rotary_tensors(rotary))
     r, _ = _rotary_desc(rotary, B, 1)
@@ -708,7 +715,7 @@ def state_attention_backward(f: Features, state: State, Q: torch.Tensor, dY: tor
     _shaped("Q", Q, (B, H, L, f.desc.d))
     _shaped("dY", dY, (B, H, L, dv))
     if dQ is None:
-        dQ = torch.empty((B, H, L, d), dtype=grad_dtype or Q.dtype, device=Q.device)
+        dQ = _empty((B, H, L, d), grad_dtype or Q.dtype, Q.device)
     if dstate is None:
         dstate = State(torch.empty_like(state.T), torch.empty_like(state.z), None)
     _shaped("dQ", dQ, Q.shape)
@@ -734,8 +741,8 @@ def state_append_backward(f: Features, state: State, dstate: State, K: torch.Ten
     _shaped("K", K, (B, f.desc.heads, L, f.desc.d))
     _shaped("V", V, (B, heads, L, dv))
     if grads is None:
-        grads = (torch.empty((B, heads, L, d), dtype=grad_dtype or K.dtype, device=K.device),
-                 torch.empty((B, heads, L, dv), dtype=grad_dtype or V.dtype, device=K.device))
+        grads = (_empty((B, heads, L, d), grad_dtype or K.dtype, K.device),
+                 _empty((B, heads, L, dv), grad_dtype or V.dtype, K.device))
     dK, dV = grads
     _shaped("dK", dK, K.shape)
     _shaped("dV", dV, V.shape)

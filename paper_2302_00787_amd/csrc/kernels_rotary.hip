@@ -108,7 +108,7 @@ int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev
   RotaryArgs a{r, X, X2, Y, Y2, H, H2, B, L, d, 0, 0, transposed ? -1.f : 1.f};
   a.units = (r.rot / 2 + 7) / 8 + (d - r.rot + 7) / 8;
   const long long threads = (long long)B * L * a.units, blocks = (threads + 255) / 256;
-  if (blocks > 0x7fffffffLL) return 2;
+  if (blocks > 0xffffffLL) return 2;             // (threads of a launch have 32 bits)
   // a token's heads in one thread only where that leaves a workgroup for every place of a CU
   int parts = 1;
   while (parts < H + H2 && blocks * parts < 2048) parts *= 2;
@@ -121,7 +121,7 @@ int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev
 
 int launch_rotary_table(const RotaryDev& r, int B, int L, float2* table, hipStream_t st) {
   const long long n = (long long)B * L * (r.rot / 2);
-  if ((n + 255) / 256 > 0x7fffffffLL) return 2;
+  if ((n + 255) / 256 > 0xffffffLL) return 2;
   hipLaunchKernelGGL(k_rotary_table, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, r, B, L, table);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }

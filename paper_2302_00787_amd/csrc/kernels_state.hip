@@ -94,14 +94,15 @@ __global__ void __launch_bounds__(256) k_prepare(const float* theta, int groups,
 // ---------------------------------------------------------------------------------------------- row terms
 // x' C2 x = x' (C2 + C2') x / 2 of sixteen rows a workgroup on matrix instructions, for dense quadratic forms.  A wave has sixteen coordinates of the
 // product, or twice that, and brings their part of the form while the rows are on their way: the call is the latency of both.  (6000
-// rows of 128: 14 us where a wave took all coordinates, one after the other, AFTER so.)
+// rows of 128: 14 us where a wave took all coordinates, one after the other, 7.1 so.)
 template <int W>
 __global__ void __launch_bounds__(W == 32 ? 128 : 256) k_row_terms(Features f, Rows x, int Hk, float* terms) {
   constexpr int S = STEPS<W>, NW = W == 32 ? 2 : 4, CT = 2 * S / NW;
   __shared__ __align__(16) float rows[NW][16][W + 4];
   __shared__ float parts[NW][16];
   const int bh = blockIdx.y, b = bh / Hk, h = bh - b * Hk, lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
-  const int row = 16 * blockIdx.x + c, len = length_of(x, b), at = min(row, x.L - 1);
+  const int v0 = 16 * (blockIdx.x + (blockIdx.z << 20)), row = v0 + c, len = length_of(x, b), at = min(row, x.L - 1);
+  if (v0 >= x.L) return;
   const char* set = f.set(h);
   const long long base = row_base(x.X, b, h, at);
   RowUnits<S, false, true> units;
@@ -374,34 +375,34 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
       const int row = row0 + ROWS * i, u = tid % UPR;
       const bool live = next_live[i];
       if (do_x) {
-      f32x4 x;
-      if constexpr (ONE) {
-        x = numbers(one_x[i]);
-        if constexpr (TURN) {
-          const f32x4 p = numbers(one_p[i]) * sgn;
-          x = f32x4{x[0] * one_cs[i][0][0] + p[0] * one_cs[i][0][1], x[1] * one_cs[i][0][2] + p[1] * one_cs[i][0][3],
-                    x[2] * one_cs[i][1][0] + p[2] * one_cs[i][1][1], x[3] * one_cs[i][1][2] + p[3] * one_cs[i][1][3]};
+        f32x4 x;
+        if constexpr (ONE) {
+          x = numbers(one_x[i]);
+          if constexpr (TURN) {
+            const f32x4 p = numbers(one_p[i]) * sgn;
+            x = f32x4{x[0] * one_cs[i][0][0] + p[0] * one_cs[i][0][1], x[1] * one_cs[i][0][2] + p[1] * one_cs[i][0][3],
+                      x[2] * one_cs[i][1][0] + p[2] * one_cs[i][1][1], x[3] * one_cs[i][1][2] + p[3] * one_cs[i][1][3]};
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = live ? x[j] : 0.f;
+        } else {
+          x = next_x[i].put(a.x, 4 * u, live);
         }
+        const float most = over_lanes<UPR>(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))), [](float p, float q) { return fmaxf(p, q); });
+        const float n = over_lanes<UPR>(x[0] * x[0] + x[1] * x[1] + (x[2] * x[2] + x[3] * x[3]), [](float p, float q) { return p + q; });
+        const float scale = up_to_2_14(most);
+        const Op16<XP> o = as_op16<XP>(f32x8{x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f} * scale);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = live ? x[j] : 0.f;
-      } else {
-        x = next_x[i].put(a.x, 4 * u, live);
-      }
-      const float most = over_lanes<UPR>(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))), [](float p, float q) { return fmaxf(p, q); });
-      const float n = over_lanes<UPR>(x[0] * x[0] + x[1] * x[1] + (x[2] * x[2] + x[3] * x[3]), [](float p, float q) { return p + q; });
-      const float scale = up_to_2_14(most);
-      const Op16<XP> o = as_op16<XP>(f32x8{x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f} * scale);
-#pragma unroll
-      for (int p = 0; p < XP; ++p) {
-        const u32x4 bits = __builtin_bit_cast(u32x4, o.p[p]);
-        *(u32x2*)&lds.x[buf][p][row][4 * u] = u32x2{bits[0], bits[1]};
-      }
-      if (u == 0) {
-        const float t = a.terms ? next_term[i] : -0.5f * kLog2e * a.f.scale2 * n;        // (C2 = -I / 2)
-        lds.term[buf][row] = live ? t : kNone;
-        lds.weight[buf][row] = a.weights ? next_weight[i] : 1.f;
-        lds.undo[buf][row] = power_inverse(scale);
-      }
+        for (int p = 0; p < XP; ++p) {
+          const u32x4 bits = __builtin_bit_cast(u32x4, o.p[p]);
+          *(u32x2*)&lds.x[buf][p][row][4 * u] = u32x2{bits[0], bits[1]};
+        }
+        if (u == 0) {
+          const float t = a.terms ? next_term[i] : -0.5f * kLog2e * a.f.scale2 * n;        // (C2 = -I / 2)
+          lds.term[buf][row] = live ? t : kNone;
+          lds.weight[buf][row] = a.weights ? next_weight[i] : 1.f;
+          lds.undo[buf][row] = power_inverse(scale);
+        }
       }
       if (!do_v) continue;
       if constexpr (ONE) {
@@ -741,7 +742,8 @@ int launch_prepare(const float* theta, int groups, const float* Omega, int omega
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, float* terms, hipStream_t st) {
-  const dim3 grid((k.L + 15) / 16, B * Hk);
+  const int n = (k.L + 15) / 16;         // (workgroups times threads of a dimension have 32 bits)
+  const dim3 grid(std::min(n, 1 << 20), B * Hk, (n + (1 << 20) - 1) >> 20);
   if (f.d <= 32) hipLaunchKernelGGL(k_row_terms<32>, grid, dim3(128), 0, st, f, k, Hk, terms);
   else if (f.d <= 64) hipLaunchKernelGGL(k_row_terms<64>, grid, dim3(256), 0, st, f, k, Hk, terms);
   else hipLaunchKernelGGL(k_row_terms<128>, grid, dim3(256), 0, st, f, k, Hk, terms);
