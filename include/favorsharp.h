@@ -352,7 +352,7 @@ int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_
  *   sequence of the call, is left out: its state stays, its output rows are zeros.  Reading, sequences may share a slot;
  *   those without one are as if it were empty.
  *   H query heads share `heads` key heads in order: query head i reads key head i / (H / heads).  H % heads = 0.
- *   lengths (device, B int32, or NULL: all L): rows l >= lengths[b] are padding: never read, and written as zeros where
+ *   lengths (device, B int32, or NULL: all L): rows l >= lengths[b] are padding: what they hold does not matter, and zeros are written where
  *   the call has outputs for them.  Lengths below 0 count as 0, above L as L; a sequence of length 0 appends nothing.
  *   rot (or NULL): queries and keys are turned on the way and not rounded in between; gradients are turned back.
  *   All products have the accuracy of fp32 for f32 and for bf16 tensors; results are rounded once, to their dtype.

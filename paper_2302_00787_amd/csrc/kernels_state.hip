@@ -284,7 +284,7 @@ struct Shares {
   __device__ __forceinline__ static long long start(long long i, long long total, long long n) { return i * total / n; }
 };
 
-// ONE: whole rows of known type, turned whole in halves or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
+// ONE: whole rows of known type, turned in halves, fours whole, or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
 // take 1100 cycles of a wave where their addresses and conditions are found one by one).
 template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
 __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, VP>& lds, int b, int h, int v0, int v1, size_t part) {
@@ -327,8 +327,10 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
   typedef typename std::conditional<DT == 1, u32x2, u32x4>::type quad;
   quad one_x[N], one_p[N], one_v[N];
   f32x4 one_cs[N][2];
-  const int half = W / 2, other0 = c0 >= half ? c0 - half : c0 + half, pair0 = c0 >= half ? c0 - half : c0;
-  const float sgn = c0 >= half ? 1.f : -1.f;
+  const int half = a.x.turn.rot >> 1;            // (a multiple of 4: fours are turned whole)
+  const bool turned = c0 < 2 * half;
+  const int other0 = c0 < half ? c0 + half : turned ? c0 - half : c0, pair0 = c0 < half ? c0 : turned ? c0 - half : 0;
+  const float sgn = c0 < half ? -1.f : turned ? 1.f : 0.f;
   const float *one_t = terms ? terms : (const float*)a.f.base, *one_w = weights ? weights : (const float*)a.f.base;
   const int t_step = terms ? 1 : 0, w_step = weights ? 1 : 0;
   const char *xp = (const char*)a.x.X.ptr, *vp = (const char*)a.v.X.ptr;
@@ -380,6 +382,9 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
           x = numbers(one_x[i]);
           if constexpr (TURN) {
             const f32x4 p = numbers(one_p[i]) * sgn;
+            f32x4(&cs)[2] = one_cs[i];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) cs[j][0] = turned ? cs[j][0] : 1.f, cs[j][2] = turned ? cs[j][2] : 1.f;
             x = f32x4{x[0] * one_cs[i][0][0] + p[0] * one_cs[i][0][1], x[1] * one_cs[i][0][2] + p[1] * one_cs[i][0][3],
                       x[2] * one_cs[i][1][0] + p[2] * one_cs[i][1][1], x[3] * one_cs[i][1][2] + p[3] * one_cs[i][1][3]};
           }
@@ -707,8 +712,8 @@ template <int W, int XP, int VP, bool FULL, bool ONE, bool TURN> int build_waves
 }
 template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
   const Turn& t = a.x.turn;
-  const bool bf16 = a.x.X.dtype == 1 && a.v.X.dtype == 1, whole = t.rot == W && !t.interleaved;
-  if (a.f.d == W && a.dv == W && a.x.X.dtype == a.v.X.dtype && (t.rot == 0 || whole)) {
+  const bool bf16 = a.x.X.dtype == 1 && a.v.X.dtype == 1, fours = t.rot % 8 == 0 && !t.interleaved;
+  if (a.f.d == W && a.dv == W && a.x.X.dtype == a.v.X.dtype && fours) {
     if (bf16) return t.rot == 0 ? build_waves<W, 1, 1, true, true, false>(a, st) : build_waves<W, 2, 1, true, true, true>(a, st);
     return t.rot == 0 ? build_waves<W, 2, 3, true, true, false>(a, st) : build_waves<W, 2, 3, true, true, true>(a, st);
   }

@@ -51,6 +51,9 @@ CASES = [  # d, dv, M, B, heads, group, L, dtype, family, rotation
     (128, 128, 200, 4, 2, 2, 260, "f32", "dense", ("half", 1.0)),
     (128, 100, 520, 3, 1, 2, 300, "bf16", "dense", ("interleaved", 1.0)),
     (24, 16, 600, 6, 8, 1, 333, "bf16", "iso", ("half", 0.5)),
+    (64, 64, 64, 6, 2, 1, 300, "bf16", "iso", ("half", 0.5)),
+    (32, 32, 512, 5, 3, 1, 77, "f32", "dense", ("half", 0.25)),
+    (128, 128, 64, 4, 1, 2, 200, "bf16", "dense", ("half", 0.75)),
     # a workgroup a state
     (32, 32, 40, 300, 1, 1, 200, "bf16", "iso", None),
     (16, 24, 32, 270, 2, 2, 90, "f32", "dense", None),
