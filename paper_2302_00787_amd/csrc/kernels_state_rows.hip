@@ -778,8 +778,10 @@ int lds_room(const void* kernel, size_t lds) {
   }
   return 0;
 }
-// Few rows: fewer workgroups of 256 than CUs would have.
-bool few_rows(int BH, long long rows) { return BH * ((rows + 255) / 256) < 192; }
+// Few rows: fewer than `most` pieces of 256, a quarter of the CUs.  (us, few rows' form / the other.  8 states of 64 x 256, bf16: values of 512 rows
+// each 9.1 / 15.3, 2048 17.5 / 16.7, 4096 32 / 18; gradients of keys 10.2 / 22.5, 33 / 24, 62 / 26, and so equal at 1300.  4 states of 128 x 512,
+// fp32: values of 2048 rows 28 / 63, 4096 50 / 65, 8192 94 / 71; gradients of keys 64 / 112, 120 / 118, 227 / 130.)
+bool few_rows(int BH, long long rows, int most) { return BH * ((rows + 255) / 256) < most; }
 
 template <int W, int XP, int P, bool FULL, bool DIRECT> int values(const ValueArgs& a, hipStream_t st) {
   constexpr int NW = DIRECT == (W == 128) ? 4 : 8, RT = 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
@@ -791,7 +793,7 @@ template <int W, int XP, int P, bool FULL, bool DIRECT> int values(const ValueAr
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int P, bool FULL> int values_rows(const ValueArgs& a, hipStream_t st) {
-  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G) ? values<W, XP, P, FULL, true>(a, st) : values<W, XP, P, FULL, false>(a, st);
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, 64) ? values<W, XP, P, FULL, true>(a, st) : values<W, XP, P, FULL, false>(a, st);
 }
 template <int W, bool FULL> int values_pieces(const ValueArgs& a, hipStream_t st) {
   if (a.Y.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? values_rows<W, 1, 2, FULL>(a, st) : values_rows<W, 2, 2, FULL>(a, st);
@@ -811,7 +813,8 @@ template <int W, int XP, int RP, int P, bool FULL, bool DIRECT, bool KEYS> int g
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int RP, int P, bool FULL, bool KEYS> int grads_rows(const GradArgs& a, hipStream_t st) {
-  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G) ? grads<W, XP, RP, P, FULL, true, KEYS>(a, st) : grads<W, XP, RP, P, FULL, false, KEYS>(a, st);
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, W == 128 ? 64 : 40) ? grads<W, XP, RP, P, FULL, true, KEYS>(a, st)
+                                                                            : grads<W, XP, RP, P, FULL, false, KEYS>(a, st);
 }
 template <int W, bool FULL, bool KEYS> int grads_pieces(const GradArgs& a, hipStream_t st) {
   const bool two = a.dx.dtype == 1 && (!KEYS || a.dr.dtype == 1);

@@ -59,12 +59,14 @@ SumPlan plan_sum(int B, int heads, long long tokens, long long rows, int d, int 
   const st::BuildShape shape = st::build_shape(d, dv, Mp);
   const int nblock = ceil_div(Mp, shape.features);
   // as many as the chip holds at a time, but a few chunks of 32 rows each at least (a part is a state written and read again, what a chunk or
-  // two take) and 64 to a state; a workgroup for each state where it has no more chunks than that, where there are eight states a CU, or
-  // more sequences than a wave should count
-  const long long each = (rows + 31) / 32, chunks = each * BH, few = st::width_class(d, dv) <= 64 ? 4 : 2;
+  // two take; 8 states of 10 chunks, 64 x 256: 21 us in pieces of four, 14 of two, of 20 chunks 18 and 15) and 64 to a state; a workgroup
+  // for each state where it has no more chunks than that (15 states of 3 chunks, 32 x 512: 10.7 us, 12.5 in pieces of one), where there
+  // are eight states a CU, or more sequences than a wave should count
+  const long long each = (rows + 31) / 32, chunks = each * BH, few = st::width_class(d, dv) <= 64 ? 4 : 2,
+                  piece = (long long)BH * nblock <= 64 ? 2 : few;
   p.nwg = B > 256 || each <= few || (long long)BH * nblock >= 2048
               ? 0
-              : (int)std::max<long long>(1, std::min<long long>({256 * shape.per_cu / nblock, (chunks + few - 1) / few, 64ll * BH}));
+              : (int)std::max<long long>(1, std::min<long long>({256 * shape.per_cu / nblock, (chunks + piece - 1) / piece, 64ll * BH}));
   size_t off = 0;
   p.off_table = off; off = align_up(off + (size_t)tokens * (rot / 2) * sizeof(float2));
   p.off_terms = off; off = align_up(off + (terms ? (size_t)BH * rows * sizeof(float) : 0));
