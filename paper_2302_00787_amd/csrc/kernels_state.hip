@@ -1,11 +1,12 @@
 // States of sequences: the projection constants they are built and read with, sums over rows (keys and values onto a state; the gradient of
 // a state), and the join of partial sums.
 //
-// k_build: a workgroup takes a part of the rows 32 at a time; its waves have 32 features each, whose rows of W and of the sum stay in
-// registers.  Rows are read, turned and split into bf16 pieces once for all waves (split3.h: fp32 products on the bf16 matrix
-// instructions).  The exponents come out feature by lane and row by register: two stacked tiles are, without a move, the operand of
-// the sum over rows.  A wave has a reference of its own, raised when an exponent passes it by 2^16 (never after the first rows, as a
-// rule): features lie up to 2^8 above one at first, so that those far below the largest still split into whole pieces.
+// k_build: a workgroup takes a part of the rows 32 at a time; its waves have 16 or 32 features each, whose rows of W and of the sum stay in
+// registers.  Rows are read, turned and split into pieces once for all waves.  The exponents come out feature by lane and row by
+// register: two stacked tiles are, without a move, the operand of the sum over rows.  A wave has a reference of its own,
+// raised when an exponent passes it by 2^16 (never after the first rows, as a rule): features lie up to 2^8 above one at first, so that
+// those far below the largest still split into whole pieces.  Vector instructions (exponentials, pieces) and matrix instructions share the
+// SIMDs' issue and bound it: 64 states of up to 4096 rows, 64 x 256, bf16: 35 us, turned on the way 57, of which the bytes need 10.
 #include <algorithm>
 #include <type_traits>
 

@@ -7,8 +7,12 @@
 // quotient loses it.
 //
 // Many rows (DIRECT = false): a wave takes 16 RT rows of its own through all features, the workgroup brings images of W and the
-// state to LDS for all its waves, the next ones on their way meanwhile.  Few rows: the waves of a workgroup take the same rows and a part
-// of the features each, with the state in LDS of their own and W from L2, no barrier until their sums meet at the end.
+// state to LDS for all its waves, the next ones on their way meanwhile.  Four waves up to 64 numbers a row, so that two or three
+// workgroups of a CU do not wait for each other (of eight waves: values of 262144 queries of 64 x 256 82 us, 76; 256 workgroups of eight
+// are better by a twentieth where they fill the chip once).  Few rows: the waves of a workgroup take the same rows and a part of the
+// features each, with the state in LDS of their own and W in registers, no barrier until their sums meet at the end.
+// Vector and matrix instructions on the same SIMDs bound many rows (values of 262144 queries, 64 x 256, bf16: 62 us; gradients of 23000 keys
+// of each of 8 heads 77 us, of 8192 queries of each 35); loads and barriers few rows (1499 keys of 4 heads, 128 x 512, fp32: 61 us).
 #include <algorithm>
 
 #include "state_common.h"
