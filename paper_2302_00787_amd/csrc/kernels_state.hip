@@ -285,7 +285,7 @@ struct Shares {
   __device__ __forceinline__ static long long start(long long i, long long total, long long n) { return i * total / n; }
 };
 
-// ONE: whole rows of known type, turned in halves, fours whole, or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
+// ONE: rows of fours of known type, turned in halves, fours whole, or (TURN = false) not at all: their way to LDS is without a branch (a chunk's loads
 // take 1100 cycles of a wave where their addresses and conditions are found one by one).
 template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
 __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, VP>& lds, int b, int h, int v0, int v1, size_t part) {
@@ -330,19 +330,22 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
   f32x4 one_cs[N][2];
   const int half = a.x.turn.rot >> 1;            // (a multiple of 4: fours are turned whole)
   const bool turned = c0 < 2 * half;
-  const int other0 = c0 < half ? c0 + half : turned ? c0 - half : c0, pair0 = c0 < half ? c0 : turned ? c0 - half : 0;
+  // (fours behind the end of a row are its last one, and put as zeros)
+  const int xc = FULL ? c0 : min(c0, a.f.d - 4), vc = FULL ? c0 : min(c0, dv - 4);
+  const bool in_x = FULL || c0 < a.f.d, in_v = FULL || c0 < dv;
+  const int other0 = c0 < half ? c0 + half : turned ? c0 - half : xc, pair0 = c0 < half ? c0 : turned ? c0 - half : 0;
   const float sgn = c0 < half ? -1.f : turned ? 1.f : 0.f;
   const float *one_t = terms ? terms : (const float*)a.f.base, *one_w = weights ? weights : (const float*)a.f.base;
   const int t_step = terms ? 1 : 0, w_step = weights ? 1 : 0;
   const char *xp = (const char*)a.x.X.ptr, *vp = (const char*)a.v.X.ptr;
   const long long x0 = row_base(a.x.X, b, h * a.x.G, 0), y0 = row_base(a.v.X, b, h * a.v.G, 0);
-  const float2* cs0 = a.x.turn.table + (long long)b * a.x.L * half;
+  const float2* cs0 = half > 0 ? a.x.turn.table + (long long)b * a.x.L * half : (const float2*)a.f.base;
   auto fetch_one = [&](int v) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int mine = v + row0 + ROWS * i, at = min(mine, v1 - 1);          // (rows behind the last one are it, and put as zeros)
       constexpr int E = DT == 1 ? 2 : 4;
-      long long xo = x0 + c0, vo = y0 + c0;
+      long long xo = x0 + xc, vo = y0 + vc;
       int row = at;
       if (a.x.G > 1) {
         const int head = at / a.x.L;
@@ -357,7 +360,7 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
       if (do_x) {
         one_x[i] = *(const quad*)(xp + xo * E);
         if constexpr (TURN) {
-          one_p[i] = *(const quad*)(xp + (xo - c0 + other0) * E);
+          one_p[i] = *(const quad*)(xp + (xo - xc + other0) * E);
           const f32x4* cs = (const f32x4*)(cs0 + (long long)row * half + pair0);
           one_cs[i][0] = cs[0];
           one_cs[i][1] = cs[1];
@@ -390,7 +393,7 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
                       x[2] * one_cs[i][1][0] + p[2] * one_cs[i][1][1], x[3] * one_cs[i][1][2] + p[3] * one_cs[i][1][3]};
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = live ? x[j] : 0.f;
+          for (int j = 0; j < 4; ++j) x[j] = live && in_x ? x[j] : 0.f;
         } else {
           x = next_x[i].put(a.x, 4 * u, live);
         }
@@ -414,7 +417,7 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
       if constexpr (ONE) {
         quad q = one_v[i];
 #pragma unroll
-        for (int j = 0; j < (DT == 1 ? 2 : 4); ++j) q[j] = live ? q[j] : 0u;
+        for (int j = 0; j < (DT == 1 ? 2 : 4); ++j) q[j] = live && in_v ? q[j] : 0u;
         if constexpr (DT == 1) {
           *(u32x2*)&lds.v[buf][0][row][4 * u] = q;
         } else {
@@ -706,9 +709,9 @@ template <int W, int XP, int VP, int NW, int FT, bool FULL, bool ONE, bool TURN>
 }
 template <int W, int XP, int VP, bool FULL, bool ONE, bool TURN> int build_waves(const BuildArgs& a, hipStream_t st) {
   // sixteen features a wave and sixteen waves, four to a SIMD, where the rows of W and of the sum leave a wave 128 registers; else 32
-  if constexpr (W <= 64 && ONE) return a.f.p.Mp > 64 ? build<W, XP, VP, 16, 1, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 1, FULL, ONE, TURN>(a, st);
+  if constexpr (W <= 64 && ONE && FULL) return a.f.p.Mp > 64 ? build<W, XP, VP, 16, 1, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 1, FULL, ONE, TURN>(a, st);
   else if constexpr (W <= 64) return a.f.p.Mp > 64 ? build<W, XP, VP, 8, 2, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 1, FULL, ONE, TURN>(a, st);
-  else if constexpr (ONE) return a.f.p.Mp > 128 ? build<W, XP, VP, 8, 2, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 2, FULL, ONE, TURN>(a, st);
+  else if constexpr (ONE && FULL) return a.f.p.Mp > 128 ? build<W, XP, VP, 8, 2, FULL, ONE, TURN>(a, st) : build<W, XP, VP, 4, 2, FULL, ONE, TURN>(a, st);
   else return build<W, XP, VP, 4, 2, FULL, ONE, TURN>(a, st);
 }
 template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
@@ -718,6 +721,8 @@ template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
     if (bf16) return t.rot == 0 ? build_waves<W, 1, 1, true, true, false>(a, st) : build_waves<W, 2, 1, true, true, true>(a, st);
     return t.rot == 0 ? build_waves<W, 2, 3, true, true, false>(a, st) : build_waves<W, 2, 3, true, true, true>(a, st);
   }
+  if (a.f.d % 4 == 0 && a.dv % 4 == 0 && a.x.X.dtype == a.v.X.dtype && fours)
+    return bf16 ? build_waves<W, 2, 1, false, true, true>(a, st) : build_waves<W, 2, 3, false, true, true>(a, st);
   return a.v.X.dtype == 1 ? build_waves<W, 2, 1, false, false, true>(a, st) : build_waves<W, 2, 3, false, false, true>(a, st);
 }
 int join_grid(const JoinArgs& a, int vec) { return std::max(1, std::min((a.M * a.dv / vec + a.M + 255) / 256, 64)); }
