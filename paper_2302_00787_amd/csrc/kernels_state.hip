@@ -725,7 +725,11 @@ template <int W> int build_width(const BuildArgs& a, hipStream_t st) {
     return bf16 ? build_waves<W, 2, 1, false, true, true>(a, st) : build_waves<W, 2, 3, false, true, true>(a, st);
   return a.v.X.dtype == 1 ? build_waves<W, 2, 1, false, false, true>(a, st) : build_waves<W, 2, 3, false, false, true>(a, st);
 }
-int join_grid(const JoinArgs& a, int vec) { return std::max(1, std::min((a.M * a.dv / vec + a.M + 255) / 256, 64)); }
+// Workgroups for a state: one for 256 numbers, up to 64, and 4096 for all states (what a workgroup does first, its state's parts and their
+// largest reference, is three loads in a chain: 660 states of 48 x 512, 64 each 65 us, 46 so).
+int join_grid(const JoinArgs& a, int vec, int states) {
+  return std::max(1, std::min({(a.M * a.dv / vec + a.M + 255) / 256, 64, (4096 + states - 1) / states}));
+}
 
 }  // namespace
 
@@ -737,13 +741,13 @@ int launch_build(const BuildArgs& a, hipStream_t st) {
   }
 }
 int launch_join(const JoinArgs& a, hipStream_t st) {
-  if (a.dv % 4 == 0) hipLaunchKernelGGL(k_join<4>, dim3(join_grid(a, 4), a.B * a.Hk), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_join<1>, dim3(join_grid(a, 1), a.B * a.Hk), dim3(256), 0, st, a);
+  if (a.dv % 4 == 0) hipLaunchKernelGGL(k_join<4>, dim3(join_grid(a, 4, a.B * a.Hk), a.B * a.Hk), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_join<1>, dim3(join_grid(a, 1, a.B * a.Hk), a.B * a.Hk), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 int launch_join_sum(const JoinArgs& a, hipStream_t st) {
-  if (a.dv % 4 == 0) hipLaunchKernelGGL(k_join_sum<4>, dim3(join_grid(a, 4), a.state.slots * a.Hk), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_join_sum<1>, dim3(join_grid(a, 1), a.state.slots * a.Hk), dim3(256), 0, st, a);
+  if (a.dv % 4 == 0) hipLaunchKernelGGL(k_join_sum<4>, dim3(join_grid(a, 4, a.state.slots * a.Hk), a.state.slots * a.Hk), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_join_sum<1>, dim3(join_grid(a, 1, a.state.slots * a.Hk), a.state.slots * a.Hk), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 int launch_prepare(const float* theta, int groups, const float* Omega, int omega_groups, int sets, int d, int M, float scale, char* buf,
