@@ -2,8 +2,8 @@
 //
 // All of them walk the features 32 at a time.  The exponents come out row by lane and feature by register: two stacked tiles are,
 // without a move, the operand of the products with the state (whose columns come from the transposing LDS read) and with W.  The
-// state's rows are split into bf16 pieces on their way to LDS: two where the result is rounded to bf16 (an error of 2^-16 beside its 2^-9), three
-// where not.  A row's reference is raised when an exponent passes it by 2^16, which its first 32 features as a rule prevent; the
+// state's rows are split into three bf16 pieces, 24 bits, on their way to LDS, for results of either type: the two sums of a gradient of queries, and
+// the two terms of V . dT + dz, cancel where values share a mean, and what pieces had lost would stay.  A row's reference is raised when an exponent passes it by 2^16, which its first 32 features as a rule prevent; the
 // quotient loses it.
 //
 // Many rows (DIRECT = false): a wave takes 16 RT rows of its own through all features, the workgroup brings images of W and the
@@ -21,18 +21,20 @@ namespace fs {
 namespace st {
 namespace {
 
-// 32 features' rows of the state in TP pieces.
-template <int W, int TP> struct StateLds {
-  uint16_t t[TP][32][W + 8];
+constexpr int P = 3;                    // bf16 pieces of features, of the state and of W's columns
+
+// 32 features' rows of the state.
+template <int W> struct StateLds {
+  uint16_t t[P][32][W + 8];
   float z[32], bias[32], scale[4];      // scale (its first): of W's 32 features
 };
-template <int W, int CP> struct ImageLds {
+template <int W, bool COLS> struct ImageLds {
   uint16_t row[STEPS<W>][2][1024];
-  uint16_t col[CP ? TILES<W> : 1][CP ? CP : 1][CP ? 512 : 8];
+  uint16_t col[COLS ? TILES<W> : 1][COLS ? P : 1][COLS ? 512 : 8];
 };
 // Where they come from; NTH threads carry them.
-template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
-  static constexpr int NR = IMAGES ? (STEPS<W> * 256 + NTH - 1) / NTH : 1, NC = IMAGES && CP ? (TILES<W> * CP * 64 + NTH - 1) / NTH : 1,
+template <int W, bool COLS, int NTH, bool FULL, bool IMAGES> struct Stage {
+  static constexpr int NR = IMAGES ? (STEPS<W> * 256 + NTH - 1) / NTH : 1, NC = IMAGES && COLS ? (TILES<W> * P * 64 + NTH - 1) / NTH : 1,
                        NT = (8 * W + NTH - 1) / NTH;
   u32x4 row[NR], col[NC];
   f32x4 t[NT];
@@ -56,11 +58,11 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
         const int e = tid + NTH * i;
         if (e < steps * 256) row[i] = *(const u32x4*)(row_img + ((size_t)fb * steps * 256 + e) * 16);
       }
-      if constexpr (CP > 0)
+      if constexpr (COLS)
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-          const int e = tid + NTH * i, tile = e / (CP * 64);
-          if (tile < 2 * steps) col[i] = *(const u32x4*)(col_img + ((size_t)(fb * 2 * steps + tile) * 192 + (e - tile * CP * 64)) * 16);
+          const int e = tid + NTH * i;
+          if (e < 2 * steps * P * 64) col[i] = *(const u32x4*)(col_img + ((size_t)fb * 2 * steps * P * 64 + e) * 16);
         }
     }
 #pragma unroll
@@ -81,18 +83,18 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
       scale = scales[fb];
     }
   }
-  __device__ __forceinline__ void put(StateLds<W, TP>& s, ImageLds<W, CP>* img, int tid) {
+  __device__ __forceinline__ void put(StateLds<W>& s, ImageLds<W, COLS>* img, int tid) {
     if constexpr (IMAGES) {
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         const int e = tid + NTH * i;
         if (e < steps * 256) *(u32x4*)((char*)img->row + e * 16) = row[i];
       }
-      if constexpr (CP > 0)
+      if constexpr (COLS)
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
           const int e = tid + NTH * i;
-          if (e < 2 * steps * CP * 64) *(u32x4*)((char*)img->col + e * 16) = col[i];
+          if (e < 2 * steps * P * 64) *(u32x4*)((char*)img->col + e * 16) = col[i];
         }
     }
 #pragma unroll
@@ -100,9 +102,9 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
       const int e = tid + NTH * i, m = e / (W / 4), c = 4 * (e % (W / 4));
       if (e < 8 * W) {
         const f32x8 v = {t[i][0], t[i][1], t[i][2], t[i][3], 0.f, 0.f, 0.f, 0.f};
-        const Op<TP> o = as_op<TP>(v);
+        const Op<P> o = as_op<P>(v);
 #pragma unroll
-        for (int p = 0; p < TP; ++p) {
+        for (int p = 0; p < P; ++p) {
           const u32x4 u = __builtin_bit_cast(u32x4, o.p[p]);
           *(u32x2*)&s.t[p][m][c] = u32x2{u[0], u[1]};
         }
@@ -117,8 +119,8 @@ template <int W, int TP, int CP, int NTH, bool FULL, bool IMAGES> struct Stage {
 };
 // W of 32 features as operands: from LDS where the workgroup has the images there, or (DIRECT) in registers, on their way long before their use
 // (the rows of the next 32 features once this wave's exponents are done, the columns ahead of the exponents).
-template <int W, int CP, bool DIRECT> struct Weights {
-  const ImageLds<W, CP>* img;
+template <int W, bool COLS, bool DIRECT> struct Weights {
+  const ImageLds<W, COLS>* img;
   int fb;
   __device__ __forceinline__ Op16<2> row(int s, int ft, int lane) const {
     Op16<2> o;
@@ -126,11 +128,11 @@ template <int W, int CP, bool DIRECT> struct Weights {
     for (int p = 0; p < 2; ++p) o.p[p] = *(const f16x8*)&img->row[s][p][ft * 512 + lane * 8];
     return o;
   }
-  __device__ __forceinline__ Op<CP> col(int ct, int lane) const { return image_op<CP>(&img->col[ct][0][0], lane); }
+  __device__ __forceinline__ Op<P> col(int ct, int lane) const { return image_op<P>(&img->col[ct][0][0], lane); }
   __device__ __forceinline__ void rows_used(int) {}
 };
-template <int W, int CP> struct Weights<W, CP, true> {
-  static constexpr int S = STEPS<W>, CT = CP ? TILES<W> : 1, P = CP ? CP : 1;
+template <int W, bool COLS> struct Weights<W, COLS, true> {
+  static constexpr int S = STEPS<W>, CT = COLS ? TILES<W> : 1;
   const char *row_img, *col_img;
   int fb, next, steps;
   Op16<2> rows[S][2];
@@ -145,9 +147,9 @@ template <int W, int CP> struct Weights<W, CP, true> {
         for (int p = 0; p < 2; ++p) rows[s][ft].p[p] = *(const f16x8*)(at + (min(s, steps - 1) * 2 + p) * 1024 + ft * 512);
   }
   __device__ __forceinline__ void load_cols(int lane) {
-    if constexpr (CP > 0)
+    if constexpr (COLS)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) cols[ct] = image_op<CP>((const uint16_t*)col_img + (size_t)(fb * 2 * steps + min(ct, 2 * steps - 1)) * 1536, lane);
+      for (int ct = 0; ct < CT; ++ct) cols[ct] = image_op<P>((const uint16_t*)col_img + (size_t)(fb * 2 * steps + min(ct, 2 * steps - 1)) * 1536, lane);
   }
   __device__ __forceinline__ Op16<2> row(int s, int ft, int) const { return rows[s][ft]; }
   __device__ __forceinline__ Op<P> col(int ct, int) const { return cols[ct]; }
@@ -202,8 +204,8 @@ template <int W, int XP, int RT, bool FULL> struct RowOps {
     }
   }
 };
-template <int W, int XP, int CP, int RT, bool FULL, bool DIRECT>
-__device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, Weights<W, CP, DIRECT>& weights, int steps, int lane, f32x4 (&E)[RT][2]) {
+template <int W, int XP, bool COLS, int RT, bool FULL, bool DIRECT>
+__device__ __forceinline__ void exponents(const RowOps<W, XP, RT, FULL>& x, Weights<W, COLS, DIRECT>& weights, int steps, int lane, f32x4 (&E)[RT][2]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) E[rt][0] = E[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -289,9 +291,9 @@ __device__ __forceinline__ Piece piece_of(int BH, int Hk, bool padded) {
 dim3 pieces(int BH, long long n) { return dim3(BH, (unsigned)std::min(n, 1ll << 15), (unsigned)((n + (1 << 15) - 1) >> 15)); }
 
 constexpr size_t most_of(size_t a, size_t b) { return a > b ? a : b; }
-template <int W, int TP, int CP, int NW, int RT, bool DIRECT> constexpr size_t rows_lds() {
-  return DIRECT ? most_of(NW * sizeof(StateLds<W, TP>), (size_t)NW * 16 * RT * (W + 4) * 4)
-                : most_of(2 * (sizeof(StateLds<W, TP>) + sizeof(ImageLds<W, CP>)), (size_t)NW * 16 * (W + 4) * 4);
+template <int W, bool COLS, int NW, int RT, bool DIRECT> constexpr size_t rows_lds() {
+  return DIRECT ? most_of(NW * sizeof(StateLds<W>), (size_t)NW * 16 * RT * (W + 4) * 4)
+                : most_of(2 * (sizeof(StateLds<W>) + sizeof(ImageLds<W, COLS>)), (size_t)NW * 16 * (W + 4) * 4);
 }
 
 // Whether a workgroup's rows v0 .. v0 + n - 1 are all padding; they are then zeros of `out`.
@@ -310,15 +312,15 @@ __device__ __forceinline__ bool all_padding(const Rows& r, int b, int h, int v0,
 }
 
 // Calls body(state in LDS, W, first step of this wave?) for the features of this wave.
-template <int W, int TP, int CP, int NW, bool FULL, bool DIRECT, class Body>
+template <int W, bool COLS, int NW, bool FULL, bool DIRECT, class Body>
 __device__ __forceinline__ void walk_features(const Features& f, int side, const char* set, const float* T, const float* z, int dv, char* lds, int w,
                                               int tid, int lane, Body body) {
   const int nfb = f.p.Mp / 32;
   if constexpr (DIRECT) {
-    Stage<W, TP, 0, 64, FULL, false> stage;
+    Stage<W, false, 64, FULL, false> stage;
     stage.start(f, side, set, T, z, dv);
-    StateLds<W, TP>& mine = ((StateLds<W, TP>*)lds)[w];
-    Weights<W, CP, true> weights;
+    StateLds<W>& mine = ((StateLds<W>*)lds)[w];
+    Weights<W, COLS, true> weights;
     weights.row_img = stage.row_img;
     weights.col_img = stage.col_img;
     weights.steps = stage.steps;
@@ -337,9 +339,9 @@ __device__ __forceinline__ void walk_features(const Features& f, int side, const
       wave_fence();
     }
   } else {
-    Stage<W, TP, CP, 64 * NW, FULL, true> stage;
+    Stage<W, COLS, 64 * NW, FULL, true> stage;
     stage.start(f, side, set, T, z, dv);
-    struct Both { StateLds<W, TP> s; ImageLds<W, CP> img; };
+    struct Both { StateLds<W> s; ImageLds<W, COLS> img; };
     Both* both = (Both*)lds;
     stage.fetch(0, tid);
     stage.put(both[0].s, &both[0].img, tid);
@@ -348,7 +350,7 @@ __device__ __forceinline__ void walk_features(const Features& f, int side, const
       Both &now = both[fb & 1], &next = both[~fb & 1];
       const bool more = fb + 1 < nfb;
       if (more) stage.fetch(fb + 1, tid);
-      Weights<W, CP, false> weights{&now.img, fb};
+      Weights<W, COLS, false> weights{&now.img, fb};
       body(now.s, weights, fb == 0);
       if (more) stage.put(next.s, &next.img, tid);
       __syncthreads();
@@ -386,7 +388,7 @@ __device__ __forceinline__ void meet(float (&ref)[RT], float (&sums)[RT][N], flo
   }
 }
 
-template <int W, int XP, int P, int NW, int RT, bool FULL, bool DIRECT>
+template <int W, int XP, int NW, int RT, bool FULL, bool DIRECT>
 __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   constexpr int VT = TILES<W>, LD = W + 8;
   extern __shared__ __align__(16) char lds[];
@@ -415,9 +417,9 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
     none[rt][0] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (slot >= 0)
-    walk_features<W, P, 0, NW, FULL, DIRECT>(
+    walk_features<W, false, NW, FULL, DIRECT>(
         a.f, 0, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
-        [&](const StateLds<W, P>& l, Weights<W, 0, DIRECT>& weights, bool first) {
+        [&](const StateLds<W>& l, Weights<W, false, DIRECT>& weights, bool first) {
           f32x4 E[RT][2];
           exponents(x, weights, steps, lane, E);
           const float scale = l.scale[0];
@@ -510,9 +512,9 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
 // Gradients.  KEYS = false: with p relative to a row's reference, u = p (dY . T + 0) and p z against W in two sums, of which, with the row's
 // normaliser and delta = sum u / sum p z, dx = (first - delta second) / normaliser.  KEYS = true: the features are those the state has
 // (terms hold its shift): u = s (r . T + z) against W, s against T.
-template <int W, int XP, int RP, int P, int NW, int RT, bool FULL, bool DIRECT, bool KEYS>
-__global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
-  constexpr int S = STEPS<W>, CT = TILES<W>, LD = W + 8, TP = KEYS ? P : 3;       // (delta enters a sum of the state's gradient: 24 bits)
+template <int W, int XP, int RP, int NW, int RT, bool FULL, bool DIRECT, bool KEYS>
+__global__ void __launch_bounds__(64 * NW, W == 64 && RP == 1 ? 2 : 1) k_grads(GradArgs a) {
+  constexpr int S = STEPS<W>, CT = TILES<W>, LD = W + 8;
   extern __shared__ __align__(16) char lds[];
   __shared__ __align__(16) float red[DIRECT ? 3 * RT * NW * 16 : KEYS ? RT * NW * 16 : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
@@ -624,9 +626,9 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
     for (int rt = 0; rt < RT; ++rt) term[rt] = x.live[rt] && slot >= 0 ? term[rt] - shift : kNone;
   }
   if (slot >= 0)
-    walk_features<W, TP, P, NW, FULL, DIRECT>(
+    walk_features<W, true, NW, FULL, DIRECT>(
         a.f, KEYS, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
-        [&](const StateLds<W, TP>& l, Weights<W, P, DIRECT>& weights, bool first) {
+        [&](const StateLds<W>& l, Weights<W, true, DIRECT>& weights, bool first) {
           f32x4 E[RT][2], D[RT][2], bias[2], zf[2];
 #pragma unroll
           for (int ft = 0; ft < 2; ++ft) {
@@ -641,8 +643,8 @@ __global__ void __launch_bounds__(64 * NW) k_grads(GradArgs a) {
 #pragma unroll
           for (int s = 0; s < S; ++s)
             if (FULL || 32 * s < dv) {
-              const Op<TP> t[2] = {row_op<TP>(&l.t[0][c][32 * s + 8 * g], 32 * LD), row_op<TP>(&l.t[0][16 + c][32 * s + 8 * g], 32 * LD)};
-              each_product<TP, RP>([&](int i, int j) {
+              const Op<P> t[2] = {row_op<P>(&l.t[0][c][32 * s + 8 * g], 32 * LD), row_op<P>(&l.t[0][16 + c][32 * s + 8 * g], 32 * LD)};
+              each_product<P, RP>([&](int i, int j) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -787,44 +789,46 @@ int lds_room(const void* kernel, size_t lds) {
 // fp32: values of 2048 rows 28 / 63, 4096 50 / 65, 8192 94 / 71; gradients of keys 64 / 112, 120 / 118, 227 / 130.)
 bool few_rows(int BH, long long rows, int most) { return BH * ((rows + 255) / 256) < most; }
 
-template <int W, int XP, int P, bool FULL, bool DIRECT> int values(const ValueArgs& a, hipStream_t st) {
-  constexpr int NW = DIRECT == (W == 128) ? 4 : 8, RT = 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
-  constexpr size_t lds = rows_lds<W, P, 0, NW, RT, DIRECT>();
+// Waves of a workgroup and tiles of sixteen rows of a wave.  Values of 64 numbers: eight waves of one tile, which have 128 registers (262144 queries of
+// 64 x 256, bf16: 94 us traced, four waves of two tiles 100).  Their gradients, bf16: two tiles and 256 registers, queries in eight waves (46; 61 in four),
+// keys in four (112; 125 in eight, 135 of one tile); in fp32, which would not fit in 256, four waves to a CU (keys 179; 221 with spills).
+template <int W, int XP, bool FULL, bool DIRECT> int values(const ValueArgs& a, hipStream_t st) {
+  constexpr int NW = DIRECT == (W == 128) && W != 64 ? 4 : 8, RT = W == 64 && !DIRECT ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr size_t lds = rows_lds<W, false, NW, RT, DIRECT>();
   static_assert(lds <= 156 * 1024, "LDS of a CU");
-  auto kernel = k_values<W, XP, P, NW, RT, FULL, DIRECT>;
+  auto kernel = k_values<W, XP, NW, RT, FULL, DIRECT>;
   if (int rc = lds_room((const void*)kernel, lds)) return rc;
   hipLaunchKernelGGL(kernel, pieces(a.B * a.Hk, ((long long)a.x.L * a.x.G + ROWS - 1) / ROWS), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int W, int XP, int P, bool FULL> int values_rows(const ValueArgs& a, hipStream_t st) {
-  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, 64) ? values<W, XP, P, FULL, true>(a, st) : values<W, XP, P, FULL, false>(a, st);
+template <int W, int XP, bool FULL> int values_rows(const ValueArgs& a, hipStream_t st) {
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, 64) ? values<W, XP, FULL, true>(a, st) : values<W, XP, FULL, false>(a, st);
 }
 template <int W, bool FULL> int values_pieces(const ValueArgs& a, hipStream_t st) {
-  if (a.Y.dtype == 1) return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? values_rows<W, 1, 2, FULL>(a, st) : values_rows<W, 2, 2, FULL>(a, st);
-  return values_rows<W, 2, 3, FULL>(a, st);
+  return a.x.X.dtype == 1 && a.x.turn.rot == 0 ? values_rows<W, 1, FULL>(a, st) : values_rows<W, 2, FULL>(a, st);
 }
 template <int W> int values_width(const ValueArgs& a, hipStream_t st) {
   return a.f.d == W && a.dv == W ? values_pieces<W, true>(a, st) : values_pieces<W, false>(a, st);
 }
 
-template <int W, int XP, int RP, int P, bool FULL, bool DIRECT, bool KEYS> int grads(const GradArgs& a, hipStream_t st) {
-  constexpr int NW = DIRECT == (W == 128) ? 4 : 8, RT = W == 128 || (DIRECT && W == 64) ? 1 : 2, ROWS = 16 * RT * (DIRECT ? 1 : NW);
-  constexpr size_t lds = rows_lds<W, KEYS ? P : 3, P, NW, RT, DIRECT>();
+template <int W, int XP, int RP, bool FULL, bool DIRECT, bool KEYS> int grads(const GradArgs& a, hipStream_t st) {
+  constexpr int NW = DIRECT == (W == 128) && !(W == 64 && RP == 1 && !KEYS) ? 4 : 8, RT = W == 128 || (DIRECT && W == 64) ? 1 : 2,
+                ROWS = 16 * RT * (DIRECT ? 1 : NW);
+  constexpr size_t lds = rows_lds<W, true, NW, RT, DIRECT>();
   static_assert(lds <= 156 * 1024, "LDS of a CU");
-  auto kernel = k_grads<W, XP, RP, P, NW, RT, FULL, DIRECT, KEYS>;
+  auto kernel = k_grads<W, XP, RP, NW, RT, FULL, DIRECT, KEYS>;
   if (int rc = lds_room((const void*)kernel, lds)) return rc;
   hipLaunchKernelGGL(kernel, pieces(a.B * a.Hk, ((long long)a.x.L * a.x.G + ROWS - 1) / ROWS), dim3(64 * NW), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
-template <int W, int XP, int RP, int P, bool FULL, bool KEYS> int grads_rows(const GradArgs& a, hipStream_t st) {
-  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, W == 128 ? 64 : 40) ? grads<W, XP, RP, P, FULL, true, KEYS>(a, st)
-                                                                            : grads<W, XP, RP, P, FULL, false, KEYS>(a, st);
+template <int W, int XP, int RP, bool FULL, bool KEYS> int grads_rows(const GradArgs& a, hipStream_t st) {
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, W == 128 ? 64 : 40) ? grads<W, XP, RP, FULL, true, KEYS>(a, st)
+                                                                            : grads<W, XP, RP, FULL, false, KEYS>(a, st);
 }
 template <int W, bool FULL, bool KEYS> int grads_pieces(const GradArgs& a, hipStream_t st) {
-  const bool two = a.dx.dtype == 1 && (!KEYS || a.dr.dtype == 1);
-  if (a.r.X.dtype == 1 && a.x.X.dtype == 1 && two)
-    return a.x.turn.rot == 0 ? grads_rows<W, 1, 1, 2, FULL, KEYS>(a, st) : grads_rows<W, 2, 1, 2, FULL, KEYS>(a, st);
-  return grads_rows<W, 2, 3, 3, FULL, KEYS>(a, st);
+  if (a.r.X.dtype == 1 && a.x.X.dtype == 1)
+    return a.x.turn.rot == 0 ? grads_rows<W, 1, 1, FULL, KEYS>(a, st) : grads_rows<W, 2, 1, FULL, KEYS>(a, st);
+  return grads_rows<W, 2, 3, FULL, KEYS>(a, st);
 }
 template <int W, bool KEYS> int grads_width(const GradArgs& a, hipStream_t st) {
   return a.f.d == W && a.dv == W ? grads_pieces<W, true, KEYS>(a, st) : grads_pieces<W, false, KEYS>(a, st);

@@ -257,25 +257,12 @@ __device__ __forceinline__ int unique_slot_of(const int32_t* slots, int nslots, 
 }
 
 // ---------------------------------------------------------------------------------------------- operands
-// P bf16 pieces of an operand: 1 (a bf16 number is its own piece), 2 (16 bits: products that are rounded to bf16) or 3 (24 bits).
+// P bf16 pieces of an operand: 1 (a bf16 number is its own piece) or 3 (24 bits).
 template <int P> struct Op { bf16x8 p[P]; };
 template <int P> __device__ __forceinline__ Op<P> as_op(f32x8 x) {
   Op<P> o;
   if constexpr (P == 1) {
     o.p[0] = __builtin_convertvector(x, bf16x8);
-  } else if constexpr (P == 2) {
-    bf16x2_t h[4], m[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x2_t v = {x[2 * i], x[2 * i + 1]};
-      h[i] = __builtin_convertvector(v, bf16x2_t);
-      m[i] = __builtin_convertvector(less_piece(v, h[i]), bf16x2_t);
-    }
-    auto join = [](const bf16x2_t (&v)[4]) {
-      return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
-                                              __builtin_bit_cast(uint32_t, v[3])});
-    };
-    o.p[0] = join(h); o.p[1] = join(m);
   } else {
     const Split3 s = split3(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
     o.p[0] = s.h; o.p[1] = s.m; o.p[2] = s.l;
@@ -347,7 +334,7 @@ template <int P> __device__ __forceinline__ Op<P> column_op(const uint16_t* s, i
 // Lanes 4 i + a of a group of sixteen name the four 8-byte pieces a of row 4 g + i; lane (a, b) = (c / 4, c % 4) gets column c of the rows.
 __device__ __forceinline__ int lane_tr(int lane, int ld) { return (4 * (lane >> 4) + ((lane & 15) >> 2)) * ld + 4 * (lane & 3); }
 
-// f(i, j) for the products of piece i of an operand of PA and piece j of one of PB that are above 2^-24 (2^-16, 2^-22) of it, small ones first.
+// f(i, j) for the products of piece i of an operand of PA and piece j of one of PB that are above 2^-24 (fp16 pieces 2^-22) of it, small ones first.
 // One product for all accumulators before the next: those of one accumulator wait for each other.
 template <int PA, int PB, class F> __device__ __forceinline__ void each_product(F f) {
 #pragma unroll

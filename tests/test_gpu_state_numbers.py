@@ -1,0 +1,58 @@
+"""Numbers that kept states meet besides the everyday ones, against the formulas in 64 bits of test_gpu_state.
+
+Values with a mean.  dq is s sum_m p_m (dY . T_m - delta z_m) W_m, dk s sum_m S_m (V . dT_m + dz_m) W_m and s^2 sum_m S_m (V . dT_m + dz_m) times (C2 + C2') k:
+where values share a mean, the two terms of each bracket are far larger than their difference.  The products are fp32's: a term is off by a
+few roundings of 2^-24 of itself, each in its own direction, sums over m by a few more; sixteen of them, 2^-20 of the root of the terms' sum of
+squares (`parts`), is the bar.  Two bf16 pieces of a factor would be off by up to 2^-17 of it.  A result rounded to bf16 is off by up to half a step, 2^-8 of
+the power of two below it, and so by 2^-8 / sqrt(3) of the norm; features are off by GRAD (test_gpu_state).
+"""
+import math
+
+import pytest
+
+from .test_gpu_state import F32, GRAD, make_theta, rows, turned
+from .test_gpu_state_shares import fs, oracle  # noqa: F401 (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+ROUNDED = 2.0 ** -8 / math.sqrt(3.0)
+
+
+@pytest.mark.parametrize("d,dv,M,B,heads,L,Lk,turn", [
+    (64, 64, 256, 2, 2, 512, 300, False), (64, 64, 256, 8, 8, 70, 90, False), (64, 64, 96, 8, 8, 40, 60, True), (64, 64, 96, 2, 1, 90, 200, True),
+    (128, 128, 512, 2, 2, 100, 130, False), (128, 128, 64, 8, 8, 40, 50, True), (32, 32, 64, 8, 8, 40, 70, False), (32, 32, 64, 2, 2, 300, 200, True),
+    (48, 40, 100, 8, 8, 40, 50, False), (96, 128, 70, 2, 1, 80, 100, True)])
+def test_gradients_of_values_with_a_mean(fs, d, dv, M, B, heads, L, Lk, turn):  # noqa: F811
+    import torch
+    gen, s, dt = torch.Generator().manual_seed(d + M + L), d ** -0.25, torch.bfloat16
+    theta, omega = make_theta(gen, "iso", heads, d), torch.randn((heads, M, d), generator=gen)
+    o, f = oracle(theta, omega, s, heads), fs.state_prepare(theta.cuda(), omega.cuda(), s)
+    K, V, Q, dY = (rows(gen, torch.float32, B, heads, n, c) for n, c in ((Lk, d), (Lk, dv), (L, d), (L, dv)))
+    K, V, Q, dY = K.to(dt), (V + 128).to(dt), Q.to(dt), (dY + 1).to(dt)
+    rot = fs.Rotary(fs.rotary_frequencies(d // 16 * 16)) if turn else None
+    k64, q64 = (turned(x.double().cpu(), rot).cuda() for x in (K, Q))
+    state = fs.state_append(f, fs.state_new(B, heads, M, dv), K, V, rotary=rot, fresh=True)
+    Y = fs.state_attention(f, state, Q, rotary=rot)
+    dQ, ds = fs.state_attention_backward(f, state, Q, dY, rotary=rot)
+    dK, dV = fs.state_append_backward(f, state, ds, K, V, rotary=rot)
+    want = [torch.empty(t.shape, dtype=torch.float64, device="cuda") for t in (Y, dQ, dK, dV)]
+    parts = [0.0] * 4                            # sums of their squares
+    for b in range(B):
+        for h in range(heads):
+            T, z, shift = state.T[b, h].double(), state.z[b, h].double(), state.shift[b, h].double()
+            q, k, v, dy, dT, dz = q64[b, h], k64[b, h], V[b, h].double(), dY[b, h].double(), ds.T[b, h].double(), ds.z[b, h].double()
+            want[0][b, h] = o.read((T, z, None), h, q)
+            want[1][b, h] = o.read_backward((T, z, None), h, q, dy)[0]
+            want[2][b, h], want[3][b, h] = o.append_backward(shift, h, k, v, dT, dz)
+            e = s * q @ o.W1[h].T + o.bias[h]
+            p = torch.exp(e - e.max(1, keepdim=True).values)
+            p = p / (p @ z)[:, None]
+            delta = ((p @ T) * dy).sum(1, keepdim=True)
+            parts[1] += float(s * s * ((p * ((dy @ T.T).abs() + delta.abs() * z)).square() @ o.W1[h].square()).sum())
+            u = (torch.exp(o.key_exponents(h, k) - shift * math.log(2)) * ((v @ dT.T).abs() + dz.abs())).square()
+            parts[2] += float((s * s * u @ o.W2[h].square() + s ** 4 * u.sum(1, keepdim=True) * (k @ (o.C2[h] + o.C2[h].T)).square()).sum())
+    if rot is not None:
+        want[1], want[2] = (turned(x.cpu(), rot, transposed=True).cuda() for x in want[1:3])
+    for name, got, ref, part, tol in zip(("Y", "dQ", "dK", "dV"), (Y, dQ, dK, dV), want, parts, (F32, GRAD, GRAD, F32)):
+        off, norm = float((got.double() - ref).norm()), float(ref.norm())
+        assert off <= (ROUNDED + tol) * norm + 2.0 ** -20 * math.sqrt(part), (name, off / norm, math.sqrt(part) / norm)
