@@ -615,8 +615,10 @@ __global__ void __launch_bounds__(64 * NW) k_build(BuildArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------- join
-// x += the parts' numbers, from their references to `top`: eight loads on their way at a time.
-template <class V> __device__ __forceinline__ void sum_parts(V& x, const V* from, size_t stride, int n, const float2* refs, int ref_stride, float top) {
+// x += the parts' numbers, from their references to `top`: eight loads on their way at a time.  HIGH: references can be more than 2^127 above `top` and
+// the products still be numbers, or zeros.
+template <bool HIGH, class V>
+__device__ __forceinline__ void sum_parts(V& x, const V* from, size_t stride, int n, const float2* refs, int ref_stride, float top) {
   for (int s0 = 0; s0 < n; s0 += 8) {
     V v[8];
     float2 ref[8];
@@ -627,8 +629,8 @@ template <class V> __device__ __forceinline__ void sum_parts(V& x, const V* from
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float k = s0 + i < n && ref[i].y != kNone ? fast_exp2(ref[i].x - top) : 0.f;
-      if (k != 0.f) x += k * v[i];
+      const float up = ref[i].x - top, k = s0 + i < n && ref[i].y != kNone ? fast_exp2(HIGH ? fminf(up, 64.f) : up) : 0.f;
+      if (k != 0.f) x += HIGH ? fast_exp2(fmaxf(up - 64.f, 0.f)) * (k * v[i]) : k * v[i];
     }
   }
 }
@@ -660,13 +662,13 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
       vec* to = (vec*)(a.state.T + at * a.M * a.dv) + e;
       vec x = {};
       if (keep != 0.f) x = keep * *to;
-      sum_parts(x, (const vec*)(a.part + part * a.M * a.dv) + e, nt, parts, refs + fb, nfb, top);
+      sum_parts<false>(x, (const vec*)(a.part + part * a.M * a.dv) + e, nt, parts, refs + fb, nfb, top);
       *to = x;
     } else {
       const int m = e - nt, fb = m >> 4;
       float* to = a.state.z + at * a.M + m;
       float x = keep != 0.f ? keep * *to : 0.f;
-      sum_parts(x, a.zpart + part * a.M + m, a.M, parts, refs + fb, nfb, top);
+      sum_parts<false>(x, a.zpart + part * a.M + m, a.M, parts, refs + fb, nfb, top);
       *to = x;
     }
   }
@@ -685,10 +687,10 @@ __global__ void __launch_bounds__(256) k_join_sum(JoinArgs a) {
       if (slot_of(a.slots, a.state.slots, b) != slot) continue;
       const size_t part = a.parts[b * a.Hk + h].x;
       const int parts = a.parts[b * a.Hk + h].y;
-      if (e < nt) sum_parts(x, (const vec*)(a.part + part * a.M * a.dv) + e, nt, parts, a.refs + part * nfb + fb, nfb, 0.f);
+      if (e < nt) sum_parts<true>(x, (const vec*)(a.part + part * a.M * a.dv) + e, nt, parts, a.refs + part * nfb + fb, nfb, 0.f);
       else {
         float y = x[0];
-        sum_parts(y, a.zpart + part * a.M + m, a.M, parts, a.refs + part * nfb + fb, nfb, 0.f);
+        sum_parts<true>(y, a.zpart + part * a.M + m, a.M, parts, a.refs + part * nfb + fb, nfb, 0.f);
         x[0] = y;
       }
     }

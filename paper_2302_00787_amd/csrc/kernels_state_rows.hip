@@ -3,8 +3,12 @@
 // All of them walk the features 32 at a time.  The exponents come out row by lane and feature by register: two stacked tiles are,
 // without a move, the operand of the products with the state (whose columns come from the transposing LDS read) and with W.  The
 // state's rows are split into three bf16 pieces, 24 bits, on their way to LDS, for results of either type: the two sums of a gradient of queries, and
-// the two terms of V . dT + dz, cancel where values share a mean, and what pieces had lost would stay.  A row's reference is raised when an exponent passes it by 2^16, which its first 32 features as a rule prevent; the
-// quotient loses it.
+// the two terms of V . dT + dz, cancel where values share a mean, and what pieces had lost would stay.
+//
+// Queries: a feature's T and z are divided by the power of two of its z on their way to LDS, which its exponent gets instead, p_m T_m = (p_m 2^e) (T_m 2^-e):
+// so exponents say what a feature contributes, and a row's reference is the largest of those.  A row that reads only what its state holds very
+// little of (keys far below the largest) then has a normaliser of 2^7 or more and all bits of T in the pieces, which end at 2^-133.  The reference is
+// raised when an exponent passes it by 2^16, which a row's first 32 features as a rule prevent; the quotient loses it.
 //
 // Many rows (DIRECT = false): a wave takes 16 RT rows of its own through all features, the workgroup brings images of W and the
 // state to LDS for all its waves, the next ones on their way meanwhile.  Four waves up to 64 numbers a row, so that two or three
@@ -33,7 +37,8 @@ template <int W, bool COLS> struct ImageLds {
   uint16_t col[COLS ? TILES<W> : 1][COLS ? P : 1][COLS ? 512 : 8];
 };
 // Where they come from; NTH threads carry them.
-template <int W, bool COLS, int NTH, bool FULL, bool IMAGES> struct Stage {
+// (SCALED: T and z by the powers of two of z)
+template <int W, bool COLS, bool SCALED, int NTH, bool FULL, bool IMAGES> struct Stage {
   static constexpr int NR = IMAGES ? (STEPS<W> * 256 + NTH - 1) / NTH : 1, NC = IMAGES && COLS ? (TILES<W> * P * 64 + NTH - 1) / NTH : 1,
                        NT = (8 * W + NTH - 1) / NTH;
   u32x4 row[NR], col[NC];
@@ -77,8 +82,8 @@ template <int W, bool COLS, int NTH, bool FULL, bool IMAGES> struct Stage {
           for (int j = 0; j < 4; ++j) t[i][j] = c + j < dv ? p[j] : 0.f;
       }
     }
+    z = 32 * fb + (tid & 31) < M ? zs[32 * fb + (tid & 31)] : 0.f;
     if (tid < 32) {
-      z = 32 * fb + tid < M ? zs[32 * fb + tid] : 0.f;
       bias = biases[32 * fb + tid];
       scale = scales[fb];
     }
@@ -97,11 +102,19 @@ template <int W, bool COLS, int NTH, bool FULL, bool IMAGES> struct Stage {
           if (e < 2 * steps * P * 64) *(u32x4*)((char*)img->col + e * 16) = col[i];
         }
     }
+    const int power = SCALED ? __builtin_amdgcn_frexp_expf(z) : 0;       // of feature tid % 32 (0 where z is 0 or not finite)
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int e = tid + NTH * i, m = e / (W / 4), c = 4 * (e % (W / 4));
       if (e < 8 * W) {
-        const f32x8 v = {t[i][0], t[i][1], t[i][2], t[i][3], 0.f, 0.f, 0.f, 0.f};
+        f32x8 v = {t[i][0], t[i][1], t[i][2], t[i][3], 0.f, 0.f, 0.f, 0.f};
+        if constexpr (SCALED) {
+          const int down = __builtin_amdgcn_ds_bpermute(4 * m, -power);
+          v[0] = __builtin_amdgcn_ldexpf(v[0], down);
+          v[1] = __builtin_amdgcn_ldexpf(v[1], down);
+          v[2] = __builtin_amdgcn_ldexpf(v[2], down);
+          v[3] = __builtin_amdgcn_ldexpf(v[3], down);
+        }
         const Op<P> o = as_op<P>(v);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -111,8 +124,8 @@ template <int W, bool COLS, int NTH, bool FULL, bool IMAGES> struct Stage {
       }
     }
     if (tid < 32) {
-      s.z[tid] = z;
-      s.bias[tid] = bias;
+      s.z[tid] = __builtin_amdgcn_ldexpf(z, -power);
+      s.bias[tid] = SCALED && z == 0.f ? kNone : bias + (float)power;
       if (tid < 4) s.scale[tid] = scale;
     }
   }
@@ -236,25 +249,22 @@ __device__ __forceinline__ f32x4 by_row(float v, int lane) {
   for (int r = 0; r < 4; ++r) k[r] = __shfl(v, 4 * (lane >> 4) + r);
   return k;
 }
-// E: exponents of a tile of rows less their references (`first`: none yet, 0).  Raises those that an exponent passes by 2^16, and what was
-// summed to them.
+// E: exponents of a tile of rows less their references.  Raises those that an exponent passes by `limit` (2^16; -inf: there is no reference yet, 0, and
+// nothing summed), and what was summed to them.
 template <int N, int K, int TA, int TB>
-__device__ __forceinline__ void raise(bool first, f32x4 (&E)[2], float& ref, float (&sums)[N], f32x4 (&acc)[K][TA], f32x4 (&more)[K][TB], int rt,
+__device__ __forceinline__ void raise(f32x4 (&E)[2], float& ref, float& limit, float (&sums)[N], f32x4 (&acc)[K][TA], f32x4 (&more)[K][TB], int rt,
                                       int lane) {
   float most = kNone;
 #pragma unroll
   for (int ft = 0; ft < 2; ++ft)
 #pragma unroll
     for (int r = 0; r < 4; ++r) most = fmaxf(most, E[ft][r]);
-  if (first) {
+  if (__any(most > limit)) {
     most = over_groups_max(most);
-    ref = most == kNone ? 0.f : most - 8.f;
-#pragma unroll
-    for (int ft = 0; ft < 2; ++ft) E[ft] -= ref;
-  } else if (__any(most > 16.f)) {
-    most = over_groups_max(most);
-    const float up = most > 16.f ? most - 8.f : 0.f, keep = fast_exp2(-up);
+    const bool raised = most > limit;
+    const float up = raised ? most - 8.f : 0.f, keep = limit == kNone ? 1.f : fast_exp2(-up);
     ref += up;
+    limit = raised ? 16.f : limit;
 #pragma unroll
     for (int n = 0; n < N; ++n) sums[n] *= keep;
     const f32x4 k = by_row(keep, lane);
@@ -311,13 +321,13 @@ __device__ __forceinline__ bool all_padding(const Rows& r, int b, int h, int v0,
   return true;
 }
 
-// Calls body(state in LDS, W, first step of this wave?) for the features of this wave.
-template <int W, bool COLS, int NW, bool FULL, bool DIRECT, class Body>
+// Calls body(state in LDS, W) for the features of this wave.
+template <int W, bool COLS, bool SCALED, int NW, bool FULL, bool DIRECT, class Body>
 __device__ __forceinline__ void walk_features(const Features& f, int side, const char* set, const float* T, const float* z, int dv, char* lds, int w,
                                               int tid, int lane, Body body) {
   const int nfb = f.p.Mp / 32;
   if constexpr (DIRECT) {
-    Stage<W, false, 64, FULL, false> stage;
+    Stage<W, false, SCALED, 64, FULL, false> stage;
     stage.start(f, side, set, T, z, dv);
     StateLds<W>& mine = ((StateLds<W>*)lds)[w];
     Weights<W, COLS, true> weights;
@@ -335,11 +345,11 @@ __device__ __forceinline__ void walk_features(const Features& f, int side, const
       weights.load_cols(lane);
       if (fb + NW < nfb) stage.fetch(fb + NW, lane);
       wave_fence();
-      body(mine, weights, fb == w);
+      body(mine, weights);
       wave_fence();
     }
   } else {
-    Stage<W, COLS, 64 * NW, FULL, true> stage;
+    Stage<W, COLS, SCALED, 64 * NW, FULL, true> stage;
     stage.start(f, side, set, T, z, dv);
     struct Both { StateLds<W> s; ImageLds<W, COLS> img; };
     Both* both = (Both*)lds;
@@ -351,37 +361,35 @@ __device__ __forceinline__ void walk_features(const Features& f, int side, const
       const bool more = fb + 1 < nfb;
       if (more) stage.fetch(fb + 1, tid);
       Weights<W, COLS, false> weights{&now.img, fb};
-      body(now.s, weights, fb == 0);
+      body(now.s, weights);
       if (more) stage.put(next.s, &next.img, tid);
       __syncthreads();
     }
   }
 }
-// Common reference and sums of a row over the waves of a DIRECT workgroup: what this wave's are multiplied by.  red: [RT][NW][16] refs, then
-// N times the same of sums.
+// Common reference and sums of a row over the waves of a DIRECT workgroup: what this wave's are multiplied by.  A wave without a reference (-inf) has
+// sums of zeros, or of what is not a number.  red: [RT][NW][16] refs, then N times the same of sums.
 template <int NW, int RT, int N>
-__device__ __forceinline__ void meet(float (&ref)[RT], float (&sums)[RT][N], float (&factor)[RT], float* red, bool any, int w, int lane) {
+__device__ __forceinline__ void meet(float (&ref)[RT], float (&sums)[RT][N], float (&factor)[RT], float* red, int w, int lane) {
   const int c = lane & 15;
   if (lane < 16)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      red[(rt * NW + w) * 16 + c] = any ? ref[rt] : kNone;
+      red[(rt * NW + w) * 16 + c] = ref[rt];
 #pragma unroll
-      for (int n = 0; n < N; ++n) red[((n + 1) * RT * NW + rt * NW + w) * 16 + c] = any ? sums[rt][n] : 0.f;
+      for (int n = 0; n < N; ++n) red[((n + 1) * RT * NW + rt * NW + w) * 16 + c] = sums[rt][n];
     }
   __syncthreads();
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = kNone;
     for (int i = 0; i < NW; ++i) top = fmaxf(top, red[(rt * NW + i) * 16 + c]);
-    factor[rt] = any ? fast_exp2(ref[rt] - top) : 0.f;
+    auto to_top = [&](float from) { return from == kNone ? 1.f : fast_exp2(from - top); };
+    factor[rt] = to_top(ref[rt]);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       float sum = 0.f;
-      for (int i = 0; i < NW; ++i) {
-        const float r = red[(rt * NW + i) * 16 + c];
-        if (r != kNone) sum += fast_exp2(r - top) * red[((n + 1) * RT * NW + rt * NW + i) * 16 + c];
-      }
+      for (int i = 0; i < NW; ++i) sum += to_top(red[(rt * NW + i) * 16 + c]) * red[((n + 1) * RT * NW + rt * NW + i) * 16 + c];
       sums[rt][n] = sum;
     }
     ref[rt] = top;
@@ -389,7 +397,7 @@ __device__ __forceinline__ void meet(float (&ref)[RT], float (&sums)[RT][N], flo
 }
 
 template <int W, int XP, int NW, int RT, bool FULL, bool DIRECT>
-__global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
+__global__ void __launch_bounds__(64 * NW, W == 64 && !DIRECT ? 4 : 1) k_values(ValueArgs a) {
   constexpr int VT = TILES<W>, LD = W + 8;
   extern __shared__ __align__(16) char lds[];
   __shared__ float red[DIRECT ? 2 * RT * NW * 16 : 1];
@@ -406,20 +414,21 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
 
   RowOps<W, XP, RT, FULL> x;
   x.load(a.x, b, h, v0, rows, len, steps, lane);
-  float ref[RT], den[RT][1];
+  float ref[RT], limit[RT], den[RT][1];
   f32x4 acc[RT][VT], none[RT][1];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     ref[rt] = 0.f;
+    limit[rt] = kNone;
     den[rt][0] = 0.f;
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt) acc[rt][vt] = f32x4{0.f, 0.f, 0.f, 0.f};
     none[rt][0] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (slot >= 0)
-    walk_features<W, false, NW, FULL, DIRECT>(
+    walk_features<W, false, true, NW, FULL, DIRECT>(
         a.f, 0, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
-        [&](const StateLds<W>& l, Weights<W, false, DIRECT>& weights, bool first) {
+        [&](const StateLds<W>& l, Weights<W, false, DIRECT>& weights) {
           f32x4 E[RT][2];
           exponents(x, weights, steps, lane, E);
           const float scale = l.scale[0];
@@ -435,7 +444,7 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
             const float undo = x.undo[rt] * scale;
 #pragma unroll
             for (int ft = 0; ft < 2; ++ft) E[rt][ft] = E[rt][ft] * undo + (bias[ft] - ref[rt]);
-            raise(first, E[rt], ref[rt], den[rt], acc, none, rt, lane);
+            raise(E[rt], ref[rt], limit[rt], den[rt], acc, none, rt, lane);
             f32x8 p;
 #pragma unroll
             for (int ft = 0; ft < 2; ++ft)
@@ -459,23 +468,19 @@ __global__ void __launch_bounds__(64 * NW) k_values(ValueArgs a) {
   for (int rt = 0; rt < RT; ++rt) {
     den[rt][0] = over_groups_sum(den[rt][0]);
     factor[rt] = 1.f;
+    if (limit[rt] == kNone) ref[rt] = kNone;
   }
   if constexpr (DIRECT) {
     __syncthreads();       // (the waves' states in LDS make room for their sums)
-    meet<NW, RT, 1>(ref, den, factor, red, slot >= 0 && w < a.f.p.Mp / 32, w, lane);
+    meet<NW, RT, 1>(ref, den, factor, red, w, lane);
   }
   int unread = 0;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const bool zero = den[rt][0] == 0.f;
     unread += (lane < 16) && (!DIRECT || w == 0) && x.live[rt] && zero;
-    // (a subnormal divisor has no inverse: it and the sums are raised by 2^64 first, what the sums, smaller still times Y, allow)
-    const float up = den[rt][0] < 0x1p-64f ? 0x1p64f : 1.f;
-    const f32x4 k = by_row(zero ? 0.f : factor[rt] / (den[rt][0] * up), lane), up4 = by_row(up, lane);
+    const f32x4 k = by_row(zero ? 0.f : factor[rt] / den[rt][0], lane);
     float* tile = (float*)lds + (DIRECT ? (size_t)w * RT + rt : (size_t)w) * 16 * (W + 4);
-    if (__any(up != 1.f))
-#pragma unroll
-      for (int vt = 0; vt < VT; ++vt) acc[rt][vt] *= up4;
     tile_to_lds<W>(tile, acc[rt], k, lane);
     if constexpr (!DIRECT) {
       wave_fence();
@@ -540,7 +545,7 @@ __global__ void __launch_bounds__(64 * NW, W == 64 && RP == 1 ? 2 : 1) k_grads(G
   RowOps<W, XP, RT, FULL> x;
   x.load(a.x, b, h, v0, rows, len, steps, lane);
   Op<RP> rr[RT][S];
-  float ref[RT], term[RT], sums[RT][2];            // queries: normaliser, sum u; keys: -, sum u
+  float ref[RT], limit[RT], term[RT], sums[RT][2];            // queries: normaliser, sum u; keys: -, sum u
   f32x4 acc[RT][CT], more[RT][CT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -561,6 +566,7 @@ __global__ void __launch_bounds__(64 * NW, W == 64 && RP == 1 ? 2 : 1) k_grads(G
     }
     term[rt] = over_groups_sum(x.square[rt]) * -0.5f * kLog2e * a.f.scale2;     // (keys)
     ref[rt] = sums[rt][0] = sums[rt][1] = 0.f;
+    limit[rt] = kNone;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc[rt][ct] = more[rt][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -626,9 +632,9 @@ __global__ void __launch_bounds__(64 * NW, W == 64 && RP == 1 ? 2 : 1) k_grads(G
     for (int rt = 0; rt < RT; ++rt) term[rt] = x.live[rt] && slot >= 0 ? term[rt] - shift : kNone;
   }
   if (slot >= 0)
-    walk_features<W, true, NW, FULL, DIRECT>(
+    walk_features<W, true, !KEYS, NW, FULL, DIRECT>(
         a.f, KEYS, set, a.state.T + st * a.f.M * dv, a.state.z + st * a.f.M, dv, lds, w, tid, lane,
-        [&](const StateLds<W>& l, Weights<W, true, DIRECT>& weights, bool first) {
+        [&](const StateLds<W>& l, Weights<W, true, DIRECT>& weights) {
           f32x4 E[RT][2], D[RT][2], bias[2], zf[2];
 #pragma unroll
           for (int ft = 0; ft < 2; ++ft) {
@@ -658,7 +664,7 @@ __global__ void __launch_bounds__(64 * NW, W == 64 && RP == 1 ? 2 : 1) k_grads(G
             const float undo = x.undo[rt] * scale;
 #pragma unroll
             for (int ft = 0; ft < 2; ++ft) E[rt][ft] = E[rt][ft] * undo + (KEYS ? bias[ft] + term[rt] : bias[ft] - ref[rt]);
-            if constexpr (!KEYS) raise(first, E[rt], ref[rt], sums[rt], acc, more, rt, lane);
+            if constexpr (!KEYS) raise(E[rt], ref[rt], limit[rt], sums[rt], acc, more, rt, lane);
             f32x8 u, s;
 #pragma unroll
             for (int ft = 0; ft < 2; ++ft)
@@ -694,10 +700,11 @@ __global__ void __launch_bounds__(64 * NW, W == 64 && RP == 1 ? 2 : 1) k_grads(G
     sums[rt][0] = over_groups_sum(sums[rt][0]);
     sums[rt][1] = over_groups_sum(sums[rt][1]);
     factor[rt] = 1.f;
+    if (!KEYS && limit[rt] == kNone) ref[rt] = kNone;
   }
   if constexpr (DIRECT) {
     __syncthreads();
-    meet<NW, RT, 2>(ref, sums, factor, red, slot >= 0 && w < a.f.p.Mp / 32, w, lane);
+    meet<NW, RT, 2>(ref, sums, factor, red, w, lane);
   }
   float* tiles = (float*)lds;
   // out (of n numbers a row) from the tiles: row r of the workgroup's, or of the wave's, rows

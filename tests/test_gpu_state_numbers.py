@@ -10,8 +10,8 @@ import math
 
 import pytest
 
-from .test_gpu_state import F32, GRAD, make_theta, rows, turned
-from .test_gpu_state_shares import fs, oracle  # noqa: F401 (a fixture)
+from .test_gpu_state import F32, GRAD, check, make_theta, rows, turned
+from .test_gpu_state_shares import fs, oracle, parts_of  # noqa: F401 (fs: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,47 @@ def test_gradients_of_values_with_a_mean(fs, d, dv, M, B, heads, L, Lk, turn):  
     for name, got, ref, part, tol in zip(("Y", "dQ", "dK", "dV"), (Y, dQ, dK, dV), want, parts, (F32, GRAD, GRAD, F32)):
         off, norm = float((got.double() - ref).norm()), float(ref.norm())
         assert off <= (ROUNDED + tol) * norm + 2.0 ** -20 * math.sqrt(part), (name, off / norm, math.sqrt(part) / norm)
+
+
+@pytest.mark.parametrize("d,dv,M,heads,group,L", [(64, 64, 256, 1, 1, 20), (64, 64, 96, 1, 2, 9000), (128, 128, 300, 2, 1, 33), (128, 100, 64, 1, 1, 17000),
+                                                   (32, 32, 64, 1, 3, 40), (20, 32, 70, 2, 1, 6000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("power", [-70, -135])
+def test_rows_that_read_what_a_state_holds_little_of(fs, d, dv, M, heads, group, L, dtype, power):  # noqa: F811
+    """States whose T and z are 2^power where rows peak: everywhere (the first sequence's), or for one row of many (the second's).  Normalisers of 2^power of
+    a row's largest feature, below the smallest normal number at -135, have quotients and gradients like any others; the tolerances are the usual ones
+    (T and z are what the state holds, rounded or not).  dY is 2^-30, so that the gradients of T, 2^(-power - 30), are numbers."""
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen, s = torch.Generator().manual_seed(d + M + L), d ** -0.25
+    theta, omega = make_theta(gen, "iso", heads, d), torch.randn((heads, M, d), generator=gen)
+    o, f = oracle(theta, omega, s, heads), fs.state_prepare(theta.cuda(), omega.cuda(), s)
+    H = heads * group
+    Q, dY = rows(gen, dt, 2, H, L, d), rows(gen, dt, 2, H, L, dv, scale=2.0 ** -30)
+    Q[1, :, 3] *= 6
+    state = fs.state_new(2, heads, M, dv)
+    state.T.copy_(torch.randn(state.T.shape, generator=gen))
+    state.z.copy_(0.5 + torch.rand(state.z.shape, generator=gen))
+    state.shift.zero_()
+    for h in range(heads):
+        e = (s * Q[1, h * group, 3].double() @ o.W1[h].T + o.bias[h]) / math.log(2.0)
+        less = (power - (e - e.max())).clamp(max=0.0)          # every feature adds as much to that row, or less, as the largest
+        for t, scale in ((state.T, torch.exp2(less)[:, None]), (state.z, torch.exp2(less))):
+            t[0, h] = (t[0, h].double() * 2.0 ** power).float()
+            t[1, h] = (t[1, h].double() * scale).float()
+    unread = torch.zeros(1, dtype=torch.int32, device="cuda")
+    Y = fs.state_attention(f, state, Q, unread=unread)
+    dQ, ds = fs.state_attention_backward(f, state, Q, dY)
+    assert int(unread) == 0
+    for b in range(2):
+        for h in range(heads):
+            st = (state.T[b, h].double(), state.z[b, h].double(), None)
+            dT, dz = torch.zeros_like(st[0]), torch.zeros_like(st[1])
+            for i in range(h * group, (h + 1) * group):
+                check(Y[b, i], o.read(st, h, Q[b, i].double()).cpu(), F32, "Y")
+                dq, t, z = o.read_backward(st, h, Q[b, i].double(), dY[b, i].double())
+                dT, dz = dT + t, dz + z
+                # (dy is of the outputs' size times 2^-30: the two parts of dq as in test_gpu_state_shares)
+                check(dQ[b, i], dq.cpu(), GRAD, "dQ", parts_of(o, st, h, dY[b, i].double()).cpu())
+            check(ds.T[b, h].reshape(1, -1), dT.reshape(1, -1).cpu(), F32, "dT")
+            check(ds.z[b, h][None], dz[None].cpu(), GRAD, "dz")
