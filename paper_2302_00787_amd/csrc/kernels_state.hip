@@ -553,6 +553,11 @@ __device__ __forceinline__ void build_part(const BuildArgs& a, BuildLds<W, XP, V
   if (!active) return;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  // (maxima pass over what is not a number: a row that is none must not pass for one that is not there)
+  bool no_number = false;
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) no_number |= z[ft] != z[ft];
+  if (__any(no_number)) ref = top = kNoNumber;
   if (lane < FT) a.refs[part * ntiles + tile + lane] = make_float2(ref, top);
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) {
@@ -629,8 +634,10 @@ __device__ __forceinline__ void sum_parts(V& x, const V* from, size_t stride, in
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float up = ref[i].x - top, k = s0 + i < n && ref[i].y != kNone ? fast_exp2(HIGH ? fminf(up, 64.f) : up) : 0.f;
-      if (k != 0.f) x += HIGH ? fast_exp2(fmaxf(up - 64.f, 0.f)) * (k * v[i]) : k * v[i];
+      const float up = ref[i].x - top;
+      const bool high = HIGH && up > 64.f;
+      const float k = s0 + i < n && ref[i].y != kNone ? fast_exp2(high ? 64.f : up) : 0.f;
+      if (k != 0.f) x += HIGH ? (high ? fast_exp2(up - 64.f) : 1.f) * (k * v[i]) : k * v[i];
     }
   }
 }
@@ -651,8 +658,14 @@ __global__ void __launch_bounds__(256) k_join(JoinArgs a) {
   const float2* refs = a.refs + part * nfb;
   const float old = a.old_shift ? a.old_shift[bh] : kNone;
   float top = old;
-  for (int i = tid; i < parts * nfb; i += 256) top = fmaxf(top, refs[i].y);
+  bool no_number = old != old;
+  for (int i = tid; i < parts * nfb; i += 256) {
+    const float part_top = refs[i].y;
+    top = fmaxf(top, part_top);
+    no_number |= part_top != part_top;
+  }
   top = block_max(top, tmp);
+  if (__syncthreads_or(no_number)) top = kNoNumber;              // (and with it all of the state)
   const float keep = old == kNone ? 0.f : fast_exp2(old - top);
   const size_t at = (size_t)slot * a.Hk + h;
   const int nt = a.M * a.dv / VEC;

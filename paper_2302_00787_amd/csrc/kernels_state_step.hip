@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
     }
     // features: a thread has the same ones of all rows; the key's again with every pass
     float top[GC + 1];
+    bool no_number = before.x != before.x;       // (maxima pass over what is not a number)
 #pragma unroll
     for (int j = 0; j <= GC; ++j) {
       top[j] = kNone;
@@ -270,17 +271,18 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
           const float e = (ONE ? feat[j * Mp + m] : exps[(size_t)(j == 0 ? 0 : g0 + j) * Mp + m]) + (j == 0 ? before.y : 0.f);
           feat[j * Mp + m] = e;
           top[j] = fmaxf(top[j], e);
+          no_number |= j == 0 && e != e;
         }
       top[j] = over_lanes<32>(top[j], [](float p, float q) { return fmaxf(p, q); });
       top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
       if (lane == 0) tops[j * NW + w] = top[j];
     }
-    __syncthreads();
+    const bool lost = __syncthreads_or(no_number);
 #pragma unroll
     for (int j = 0; j <= GC; ++j)
 #pragma unroll
       for (int i = 0; i < NW; ++i) top[j] = fmaxf(top[j], tops[j * NW + i]);
-    top[0] = fmaxf(top[0], before.x);
+    top[0] = lost ? kNoNumber : fmaxf(top[0], before.x);         // (and with it all of the state)
     keep = before.x == kNone ? 0.f : fast_exp2(before.x - top[0]);
     float den[GC];
 #pragma unroll

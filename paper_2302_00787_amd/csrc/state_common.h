@@ -14,7 +14,7 @@ namespace st {
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
-constexpr float kNone = -__builtin_huge_valf();
+constexpr float kNone = -__builtin_huge_valf(), kNoNumber = __builtin_nanf("");
 
 // Widths: rows of up to 32, 64 and 128 numbers, in steps of 32 (an operand's contraction) and tiles of 16 (its columns).
 template <int W> constexpr int STEPS = W / 32;

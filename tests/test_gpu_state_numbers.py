@@ -100,3 +100,59 @@ def test_rows_that_read_what_a_state_holds_little_of(fs, d, dv, M, heads, group,
                 check(dQ[b, i], dq.cpu(), GRAD, "dQ", parts_of(o, st, h, dY[b, i].double()).cpu())
             check(ds.T[b, h].reshape(1, -1), dT.reshape(1, -1).cpu(), F32, "dT")
             check(ds.z[b, h][None], dz[None].cpu(), GRAD, "dz")
+
+
+@pytest.mark.parametrize("B,heads,L,M,d,dtype", [(2, 1, 1, 64, 64, "f32"), (3, 2, 40, 64, 64, "bf16"), (2, 2, 700, 256, 64, "bf16"), (2, 1, 300, 100, 48, "f32"),
+                                                 (260, 1, 5, 32, 16, "f32"), (2, 1, 90, 512, 128, "bf16")])
+def test_a_key_that_is_not_a_number_shows_in_its_state(fs, B, heads, L, M, d, dtype):  # noqa: F811
+    """All of that state, and no other; appended to an empty state and to one with keys, as a sequence's only keys, among others and as a token."""
+    import torch
+    dt, nan = torch.bfloat16 if dtype == "bf16" else torch.float32, float("nan")
+    gen, s = torch.Generator().manual_seed(B + L), d ** -0.25
+    theta, omega = make_theta(gen, "iso", heads, d), torch.randn((heads, M, d), generator=gen)
+    f = fs.state_prepare(theta.cuda(), omega.cuda(), s)
+    K, V, q = (rows(gen, dt, B, heads, n, d) for n in (L, L, 1))
+    h = heads - 1
+    for first, last in ((0, L), (L // 2, L // 2 + 1)):
+        bad = K.clone()
+        bad[1, h, first:last, d // 2] = nan
+        for fresh in (True, False):
+            state = fs.state_append(f, fs.state_new(B, heads, M, d), K, V)
+            good = fs.state_append(f, fs.state_append(f, fs.state_new(B, heads, M, d), K, V), K, V, fresh=fresh)
+            fs.state_append(f, state, bad, V, fresh=fresh)
+            for t, g in zip(state, good):
+                assert t[1, h].isnan().all()
+                t[1, h] = g[1, h]
+                assert torch.equal(t, g)
+    # a token onto an empty state and onto one with keys; then a good one, and good keys
+    k, v = K[:, :, :1], V[:, :, :1]
+    bad = k.clone()
+    bad[1, h, 0, 0] = nan
+    for state in (fs.state_new(B, heads, M, d), fs.state_append(f, fs.state_new(B, heads, M, d), K, V)):
+        good = fs.State(*(t.clone() for t in state))
+        for key in (bad, k):
+            Y, Yg = fs.state_step(f, state, q, key, v), fs.state_step(f, good, q, k, v)
+            assert Y[1, h].isnan().all() and all(t[1, h].isnan().all() for t in state)
+            Y[1, h] = Yg[1, h]
+            assert torch.equal(Y, Yg)
+        fs.state_append(f, state, K, V)
+        fs.state_append(f, good, K, V)
+        for t, g in zip(state, good):
+            assert t[1, h].isnan().all()
+            t[1, h] = g[1, h]
+            assert torch.equal(t, g)
+    # a query: its row, and the gradient of what it read
+    state = fs.state_append(f, fs.state_new(B, heads, M, d), K, V)
+    for n in (1, L):
+        Q, dY = rows(gen, dt, B, heads, n, d), rows(gen, dt, B, heads, n, d)
+        Yg, (dQg, dg) = fs.state_attention(f, state, Q), fs.state_attention_backward(f, state, Q, dY)
+        Q[1, h, n // 2, 0] = nan
+        Y, (dQ, ds) = fs.state_attention(f, state, Q), fs.state_attention_backward(f, state, Q, dY)
+        for t, g in ((Y, Yg), (dQ, dQg)):
+            assert t[1, h, n // 2].isnan().all()
+            t[1, h, n // 2] = g[1, h, n // 2]
+            assert torch.equal(t, g)
+        for t, g in ((ds.T, dg.T), (ds.z, dg.z)):
+            assert t[1, h].isnan().all()
+            t[1, h] = g[1, h]
+            assert torch.equal(t, g)
