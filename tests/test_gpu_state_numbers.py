@@ -156,3 +156,35 @@ def test_a_key_that_is_not_a_number_shows_in_its_state(fs, B, heads, L, M, d, dt
             assert t[1, h].isnan().all()
             t[1, h] = g[1, h]
             assert torch.equal(t, g)
+
+
+@pytest.mark.parametrize("B,slots,heads", [(3000, 2500, 1), (2600, 1, 2), (1500, 3, 1), (300, 5, 1), (1025, 1, 1)])
+def test_gradients_of_states_with_many_readers(fs, B, slots, heads):  # noqa: F811
+    """Readers of a slot anywhere among thousands of sequences, and thousands of readers of one slot; some sequences have none."""
+    import torch
+    gen, d, M, L = torch.Generator().manual_seed(B), 16, 32, 2
+    s = d ** -0.25
+    theta, omega = make_theta(gen, "iso", heads, d), torch.randn((heads, M, d), generator=gen)
+    o, f = oracle(theta, omega, s, heads), fs.state_prepare(theta.cuda(), omega.cuda(), s)
+    where = torch.randint(-1, slots + 1, (B,), generator=gen).to(torch.int32)
+    Q, dY = (rows(gen, torch.float32, B, heads, L, d) for _ in range(2))
+    state = fs.state_new(slots, heads, M, d)
+    state.T.copy_(torch.randn(state.T.shape, generator=gen))
+    state.z.copy_(0.5 + torch.rand(state.z.shape, generator=gen))
+    state.shift.zero_()
+    dQ, ds = fs.state_attention_backward(f, state, Q, dY, slots=where.cuda())
+    for h in range(heads):
+        e = s * Q[:, h].double() @ o.W1[h].T + o.bias[h]
+        p = torch.exp(e - e.amax(2, keepdim=True))
+        at = where.long().clamp(0, slots - 1).cuda()
+        z, T, dy = state.z[at, h].double()[:, None], state.T[at, h].double(), dY[:, h].double()
+        p = p / (p * z).sum(2, keepdim=True)
+        delta = (torch.bmm(p, T) * dy).sum(2, keepdim=True)
+        gT, gz = torch.bmm(p.transpose(1, 2).contiguous(), dy), -(p * delta).sum(1)
+        there = ((where >= 0) & (where < slots)).cuda().double()
+        dT = torch.zeros_like(state.T[:, h], dtype=torch.float64).index_add_(0, at, gT * there[:, None, None])
+        dz = torch.zeros_like(state.z[:, h], dtype=torch.float64).index_add_(0, at, gz * there[:, None])
+        check(ds.T[:, h].reshape(1, -1), dT.reshape(1, -1).cpu(), F32, "dT")
+        check(ds.z[:, h].reshape(1, -1), dz.reshape(1, -1).cpu(), GRAD, "dz")
+    again = fs.state_attention_backward(f, state, Q, dY, slots=where.cuda())[1]
+    assert torch.equal(again.T, ds.T) and torch.equal(again.z, ds.z)
