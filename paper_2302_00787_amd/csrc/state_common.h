@@ -66,12 +66,15 @@ struct RotaryDev {
   float amplitude;
 };
 // The angle is taken in turns and in 64 bits (position f / 2 pi, less its nearest whole number): in 32 a position of 2^20 would leave
-// four bits of it.  What is left, within half a turn, is exact enough in 32 bits, where cosine and sine are taken.
+// four bits of it.  What is left, within half a turn, goes to cosine and sine in 32 bits, and the bits that it loses there to their first-order
+// correction (without it the angle alone costs 1.6 steps of 2^-24).
 __device__ __forceinline__ float2 cos_sin(int position, double freq, float amplitude) {
   const double turns = (double)position * (freq * 0.15915494309189533577);        // 1 / (2 pi)
+  const double halves = 2.0 * (turns - rint(turns));
+  const float near = (float)halves, rest = (float)(halves - (double)near) * 3.14159265f;
   float s, c;
-  sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-  return make_float2(amplitude * c, amplitude * s);
+  sincospif(near, &s, &c);
+  return make_float2(amplitude * (c - s * rest), amplitude * (s + c * rest));
 }
 __device__ __forceinline__ int position_of(const RotaryDev& r, int b, int l) { return r.positions ? r.positions[b * r.sb + l * r.sl] : l; }
 

@@ -188,3 +188,17 @@ def test_gradients_of_states_with_many_readers(fs, B, slots, heads):  # noqa: F8
         check(ds.z[:, h].reshape(1, -1), dz.reshape(1, -1).cpu(), GRAD, "dz")
     again = fs.state_attention_backward(f, state, Q, dY, slots=where.cuda())[1]
     assert torch.equal(again.T, ds.T) and torch.equal(again.z, ds.z)
+
+
+def test_angles_lose_nothing_before_cosine_and_sine(fs):  # noqa: F811
+    """Rows (1, 0) turned: cosine and sine themselves.  Each is off by a step of numbers below 1, 2^-24, at most, and by the half step of the sum
+    with what the angle had below 32 bits."""
+    import torch
+    n, L = 128, 4096
+    rot = fs.Rotary(fs.rotary_frequencies(n), torch.arange(L, dtype=torch.int32, device="cuda") * 31)
+    x = torch.zeros((1, 1, L, n), device="cuda")
+    x[..., : n // 2] = 1
+    y = fs.rotary(x, rot).double().cpu()[0, 0]
+    ang = rot.positions.cpu().double()[:, None] * rot.freqs.cpu()
+    want = torch.cat([torch.cos(ang), torch.sin(ang)], dim=1)
+    assert float((y - want).abs().max()) <= 1.5 * 2.0 ** -24
