@@ -307,7 +307,7 @@ int favorsharp_orthogonal_omega(const float* host_gauss_dir, const float* host_g
  * the angle p freqs[i] and multiplied by `amplitude`:
  *   (u, v) -> amplitude (u cos - v sin, v cos + u sin);
  * the numbers behind rot_dim stay.  Pair i is numbers 2 i and 2 i + 1 (interleaved = 1) or i and i + rot_dim / 2
- * (interleaved = 0).  Angles are taken in 64 bits, so that far positions keep theirs.
+ * (interleaved = 0).  Angles are reduced in 64 bits, so that far positions keep theirs; cosine and sine are those of fp32.
  */
 typedef struct {
   const double* freqs;        /* device, rot_dim / 2 values: radians per position */
@@ -334,7 +334,7 @@ int favorsharp_rotary_frequencies(int rot_dim, double base, int scaling, double 
  * Rows turned by their positions: Y = R X for X [B, H, L, d] and, in the same launch, Y2 = R X2 for X2 [B, H2, L, d]
  * (queries and keys; H2 = 0: X alone, X2 and Y2 are not read).  transposed = 1 applies the transpose of R (turned back,
  * amplitude kept), which is the backward pass.  Y may be X itself (same pointer, dtype and strides), likewise Y2 and X2;
- * otherwise they must not overlap.  d <= 1024; each tensor f32 or bf16.  Asynchronous; no workspace.
+ * otherwise they must not overlap.  d <= 1024, B L <= 2^31, B L d / 8 < 2^32; each tensor f32 or bf16.  Asynchronous; no workspace.
  */
 int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d,
                       int transposed, const fs_tensor* Y, const fs_tensor* Y2, void* stream);
@@ -346,7 +346,7 @@ int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_
  *   T [slots][heads][M][dv], z [slots][heads][M], shift [slots][heads], all float32 (T 16-byte aligned):
  *   shift = max_jm e_jm,  T_m = sum_j 2^(e_jm - shift) V_j,  z_m = sum_j 2^(e_jm - shift),  2^e_jm = S_jm,
  * over the keys appended so far; an empty state is T = z = 0, shift = -infinity.  Keys more than about 2^126 below the
- * largest of their state are lost to it.
+ * largest of their state are lost to it.  A key with a number that is none makes all of its state no number.
  *   slots (device, B int32, or NULL: sequence b has slot b): the slot of each sequence.  Where a call writes states
  *   (append, step, and the gradient of append) a sequence whose slot is not in the pool, or is also that of an earlier
  *   sequence of the call, is left out: its state stays, its output rows are zeros.  Reading, sequences may share a slot;
@@ -355,9 +355,10 @@ int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_
  *   lengths (device, B int32, or NULL: all L): rows l >= lengths[b] are padding: what they hold does not matter, and zeros are written where
  *   the call has outputs for them.  Lengths below 0 count as 0, above L as L; a sequence of length 0 appends nothing.
  *   rot (or NULL): queries and keys are turned on the way and not rounded in between; gradients are turned back.
- *   All products have the accuracy of fp32 for f32 and for bf16 tensors; results are rounded once, to their dtype.
+ *   All products have the accuracy of fp32 for f32 and for bf16 tensors (24 bits of a factor, in exponents and the keys' quadratic forms 22); results are
+ *   rounded once, to their dtype.
  *   Where a *_workspace_bytes query answers 0 the workspace may be NULL (a query for sizes that are refused answers 0, too).
- *   d, dv <= 128, M <= 2048, B H and slots * heads <= 65535, L H / heads <= 2^29.
+ *   d, dv <= 128, M <= 2048, B H and slots * heads <= 65535, L H / heads <= 2^29, with rot also B L rot_dim / 2 < 2^32.
  * Calls on one stream see each other's states; calls that write a state must be ordered with all others on it by the caller.
  */
 typedef struct {
@@ -390,9 +391,9 @@ int favorsharp_state_append(const fs_features* host_features, const fs_state* st
                             const fs_rotary* rot, int fresh, int32_t* left_out,
                             void* workspace, size_t workspace_bytes, void* stream);
 
-/* Y [B, H, L, dv] = P T / P z for queries Q [B, H, L, d] (cross attention to an encoder kept in the pool; the prompt's part that
- * attends to what was there before it).  A row whose normaliser is zero (an empty state) is zeros; unread (device int32, or
- * NULL): the number of such rows is ADDED to it. */
+/* Y [B, H, L, dv] = P T / P z for queries Q [B, H, L, d]: every row against all of its state (cross attention to an encoder kept in
+ * the pool; tokens of a sequence that see no other of the call).  A row whose normaliser is zero (an empty state) is zeros; unread
+ * (device int32, or NULL): the number of such rows is ADDED to it. */
 size_t favorsharp_state_attention_workspace_bytes(const fs_features* host_features, int B, int H, int L, int dv, int rot_dim);
 int favorsharp_state_attention(const fs_features* host_features, const fs_state* state, const int32_t* slots,
                                const fs_tensor* Q, int B, int H, int L, int dv, const int32_t* lengths,
@@ -401,7 +402,7 @@ int favorsharp_state_attention(const fs_features* host_features, const fs_state*
 
 /* One token of every sequence: K [B, heads, 1, d] and V [B, heads, 1, dv] are appended, then Q [B, H, 1, d] reads the state that
  * holds them: Y [B, H, 1, dv].  Q, K, V share a dtype.  unread as above; the rows of sequences that are left out are counted
- * too. */
+ * too, and those whose normaliser is below 2^-149 of their largest feature (favorsharp_state_attention reads these). */
 size_t favorsharp_state_step_workspace_bytes(const fs_features* host_features, int B, int H);
 int favorsharp_state_step(const fs_features* host_features, const fs_state* state, const int32_t* slots, const fs_tensor* Q,
                           const fs_tensor* K, const fs_tensor* V, int B, int H, int dv, const fs_rotary* rot,
@@ -409,7 +410,8 @@ int favorsharp_state_step(const fs_features* host_features, const fs_state* stat
 
 /* Gradients of sum(Y * dY) of favorsharp_state_attention with respect to Q and to T and z (shift constant: Y does not depend on
  * the scale that T and z share).  dstate: a pool of as many slots, T and z overwritten: sums over the rows of all query heads
- * and sequences that read the slot, in a fixed order; zeros where none does.  dY, dQ any dtype. */
+ * and sequences that read the slot, in a fixed order; zeros where none does.  They are as large as the state is small where a row reads
+ * it, and infinite beyond fp32's largest number.  dY, dQ any dtype. */
 size_t favorsharp_state_attention_backward_workspace_bytes(const fs_features* host_features, int B, int H, int L, int dv,
                                                            int rot_dim);
 int favorsharp_state_attention_backward(const fs_features* host_features, const fs_state* state, const int32_t* slots,

@@ -11,12 +11,11 @@
 // raised when an exponent passes it by 2^16, which a row's first 32 features as a rule prevent; the quotient loses it.
 //
 // Many rows (DIRECT = false): a wave takes 16 RT rows of its own through all features, the workgroup brings images of W and the
-// state to LDS for all its waves, the next ones on their way meanwhile.  Four waves up to 64 numbers a row, so that two or three
-// workgroups of a CU do not wait for each other (of eight waves: values of 262144 queries of 64 x 256 82 us, 76; 256 workgroups of eight
-// are better by a twentieth where they fill the chip once).  Few rows: the waves of a workgroup take the same rows and a part of the
+// state to LDS for all its waves, the next ones on their way meanwhile.  Few rows: the waves of a workgroup take the same rows and a part of the
 // features each, with the state in LDS of their own and W in registers, no barrier until their sums meet at the end.
-// Vector and matrix instructions on the same SIMDs bound many rows (values of 262144 queries, 64 x 256, bf16: 62 us; gradients of 23000 keys
-// of each of 8 heads 77 us, of 8192 queries of each 35); loads and barriers few rows (1499 keys of 4 heads, 128 x 512, fp32: 61 us).
+// Vector and matrix instructions on the same SIMDs bound many rows (64 x 256, bf16; vector issue and busy matrix pipes, of a SIMD's cycles: values of
+// 262144 queries 84 us, 55 % and 34 %; gradients of 23000 keys of each of 8 heads 97 us, 43 and 39; of 8192 queries of each 41, 42 and 39); loads and
+// barriers few rows (1499 keys of 4 heads, 128 x 512, fp32: 57 us).
 #include <algorithm>
 
 #include "state_common.h"
@@ -791,9 +790,10 @@ int lds_room(const void* kernel, size_t lds) {
   }
   return 0;
 }
-// Few rows: fewer than `most` pieces of 256, a quarter of the CUs.  (us, few rows' form / the other.  8 states of 64 x 256, bf16: values of 512 rows
-// each 9.1 / 15.3, 2048 17.5 / 16.7, 4096 32 / 18; gradients of keys 10.2 / 22.5, 33 / 24, 62 / 26, and so equal at 1300.  4 states of 128 x 512,
-// fp32: values of 2048 rows 28 / 63, 4096 50 / 65, 8192 94 / 71; gradients of keys 64 / 112, 120 / 118, 227 / 130.)
+// Few rows: fewer than `most` pieces of 256, a quarter of the CUs, for gradients of up to 64 numbers 40, but those of 64-wide queries.  (us, few rows' form / the
+// other.  8 states of 64 x 256, bf16: values of 512 rows each 9.3 / 15.4, 1536 17.3 / 15.8, 4096 34 / 18; gradients of keys 9.7 / 27, 25 / 28, 64 / 30;
+// of queries, with the state's, 25 / 54, 47 / 62, 88 / 68, in fp32 29 / 48, 56 / 57, 106 / 66.  8 of 32 x 128: keys 512 rows 7.0 / 10.5, 1280 12.9 / 11.0.  4 of
+// 128 x 512, fp32: values of 2048 rows 26 / 64, 4096 50 / 66, 8192 97 / 72; gradients of keys 51 / 91, 102 / 96, 192 / 112.)
 bool few_rows(int BH, long long rows, int most) { return BH * ((rows + 255) / 256) < most; }
 
 // Waves of a workgroup and tiles of sixteen rows of a wave.  Values of 64 numbers: eight waves of one tile, which have 128 registers (262144 queries of
@@ -829,8 +829,8 @@ template <int W, int XP, int RP, bool FULL, bool DIRECT, bool KEYS> int grads(co
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 template <int W, int XP, int RP, bool FULL, bool KEYS> int grads_rows(const GradArgs& a, hipStream_t st) {
-  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, W == 128 ? 64 : 40) ? grads<W, XP, RP, FULL, true, KEYS>(a, st)
-                                                                            : grads<W, XP, RP, FULL, false, KEYS>(a, st);
+  return few_rows(a.B * a.Hk, (long long)a.x.L * a.x.G, W == 128 || (W == 64 && !KEYS) ? 64 : 40) ? grads<W, XP, RP, FULL, true, KEYS>(a, st)
+                                                                                                     : grads<W, XP, RP, FULL, false, KEYS>(a, st);
 }
 template <int W, bool FULL, bool KEYS> int grads_pieces(const GradArgs& a, hipStream_t st) {
   if (a.r.X.dtype == 1 && a.x.X.dtype == 1)

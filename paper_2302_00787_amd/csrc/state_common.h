@@ -391,7 +391,10 @@ struct BuildArgs {
   const float* shift;            // of the pool, copied to old_shift (nullptr: not)
   float* old_shift;              // [B*Hk]
 };
-// Workgroups of k_build that a CU holds, by the registers of its waves, and the features of one.
+// Workgroups of k_build that a CU holds, by the registers of its waves, and the features of one, for whole rows of 32, 64 or 128 numbers in bf16.  A
+// workspace's size does not depend on the tensors, so others are counted alike: rows of 65 to 127 numbers, interleaved pairs and tensors of two
+// dtypes have 128 features a workgroup at W = 128, fp32 rows LDS for one workgroup (of two) or three (of four), and these calls up to twice the
+// workgroups that the chip holds at a time.
 struct BuildShape { int per_cu, features; };
 inline BuildShape build_shape(int d, int dv, int Mp) {
   if (width_class(d, dv) <= 64) return Mp > 64 ? BuildShape{1, 256} : BuildShape{4, 64};
