@@ -334,7 +334,8 @@ int favorsharp_rotary_frequencies(int rot_dim, double base, int scaling, double 
  * Rows turned by their positions: Y = R X for X [B, H, L, d] and, in the same launch, Y2 = R X2 for X2 [B, H2, L, d]
  * (queries and keys; H2 = 0: X alone, X2 and Y2 are not read).  transposed = 1 applies the transpose of R (turned back,
  * amplitude kept), which is the backward pass.  Y may be X itself (same pointer, dtype and strides), likewise Y2 and X2;
- * otherwise they must not overlap.  d <= 1024, B L <= 2^31, B L d / 8 < 2^32; each tensor f32 or bf16.  Asynchronous; no workspace.
+ * otherwise they must not overlap.  d <= 1024, B L <= 2^31, and B L (d / 8 + 2) <= 2^32 - 256 (larger ones may be
+ * FS_ERR_UNSUPPORTED); each tensor f32 or bf16.  Asynchronous; no workspace.
  */
 int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d,
                       int transposed, const fs_tensor* Y, const fs_tensor* Y2, void* stream);
@@ -358,7 +359,7 @@ int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_
  *   All products have the accuracy of fp32 for f32 and for bf16 tensors (24 bits of a factor, in exponents and the keys' quadratic forms 22); results are
  *   rounded once, to their dtype.
  *   Where a *_workspace_bytes query answers 0 the workspace may be NULL (a query for sizes that are refused answers 0, too).
- *   d, dv <= 128, M <= 2048, B H and slots * heads <= 65535, L H / heads <= 2^29, with rot also B L rot_dim / 2 < 2^32.
+ *   d, dv <= 128, M <= 2048, B H and slots * heads <= 65535, L H / heads <= 2^29, with rot also B L rot_dim / 2 <= 2^32 - 256.
  * Calls on one stream see each other's states; calls that write a state must be ordered with all others on it by the caller.
  */
 typedef struct {
