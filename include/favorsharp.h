@@ -403,7 +403,7 @@ int favorsharp_state_attention(const fs_features* host_features, const fs_state*
 
 /* One token of every sequence: K [B, heads, 1, d] and V [B, heads, 1, dv] are appended, then Q [B, H, 1, d] reads the state that
  * holds them: Y [B, H, 1, dv].  Q, K, V share a dtype.  unread as above; the rows of sequences that are left out are counted
- * too, and those whose normaliser is below 2^-149 of their largest feature (favorsharp_state_attention reads these). */
+ * too. */
 size_t favorsharp_state_step_workspace_bytes(const fs_features* host_features, int B, int H);
 int favorsharp_state_step(const fs_features* host_features, const fs_state* state, const int32_t* slots, const fs_tensor* Q,
                           const fs_tensor* K, const fs_tensor* V, int B, int H, int dv, const fs_rotary* rot,

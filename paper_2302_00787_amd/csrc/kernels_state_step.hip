@@ -173,9 +173,9 @@ __global__ void __launch_bounds__(256) k_step_exponents(StepArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------- states
-// Floats in LDS: features (key, GC queries), the threads' partial outputs, maxima and normalisers by wave.
+// Floats in LDS: features (key, GC queries), z, the threads' partial outputs, maxima and normalisers by wave.
 template <int GC, int NTH> __host__ __device__ constexpr int step_lds_floats(int Mp) {
-  return (GC + 1) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64) + (GC + 1) * 128 + NTH / 64;
+  return (GC + 2) * Mp + 4 * GC * NTH + (1 + GC) * 2 * (NTH / 64) + (GC + 1) * 128 + NTH / 64;
 }
 
 // GC: query heads that a pass over the state serves.  Workgroup z has the columns z cols .. (z + 1) cols - 1.
@@ -186,7 +186,8 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
   extern __shared__ __align__(16) float lds[];
   const int Mp = a.f.p.Mp, M = a.f.M, dv = a.dv, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   float* feat = lds;                           // [GC + 1][Mp]
-  float* part = feat + (GC + 1) * Mp;          // [GC][rows of a pass][columns]
+  float* zs = feat + (GC + 1) * Mp;            // [Mp]
+  float* part = zs + Mp;                       // [GC][rows of a pass][columns]
   float* tops = part + 4 * GC * NTH;           // [GC + 1][NW]
   float* dens = tops + (1 + GC) * NW;          // [GC][NW]
   float* x = dens + (1 + GC) * NW;             // (ONE) [2][128] the key, the query
@@ -261,47 +262,70 @@ __global__ void __launch_bounds__(NTH, ONE ? 2 : 4) k_step(StepArgs a) {
       for (int i = 0; i < NW; ++i) before.y += word[i];
     }
     // features: a thread has the same ones of all rows; the key's again with every pass
-    float top[GC + 1];
+    float top = kNone;
     bool no_number = before.x != before.x;       // (maxima pass over what is not a number)
+    for (int m = tid; m < Mp; m += NTH) {
+      const float e = (ONE ? feat[m] : exps[m]) + before.y;
+      feat[m] = e;
+      top = fmaxf(top, e);
+      no_number |= e != e;
+      if constexpr (!ONE)
 #pragma unroll
-    for (int j = 0; j <= GC; ++j) {
-      top[j] = kNone;
-      if (j <= n)
-        for (int m = tid; m < Mp; m += NTH) {
-          const float e = (ONE ? feat[j * Mp + m] : exps[(size_t)(j == 0 ? 0 : g0 + j) * Mp + m]) + (j == 0 ? before.y : 0.f);
-          feat[j * Mp + m] = e;
-          top[j] = fmaxf(top[j], e);
-          no_number |= j == 0 && e != e;
-        }
-      top[j] = over_lanes<32>(top[j], [](float p, float q) { return fmaxf(p, q); });
-      top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
-      if (lane == 0) tops[j * NW + w] = top[j];
+        for (int j = 1; j <= GC; ++j)
+          if (j <= n) feat[j * Mp + m] = exps[(size_t)(g0 + j) * Mp + m];
     }
+    auto largest = [](float v) {
+      v = over_lanes<32>(v, [](float p, float q) { return fmaxf(p, q); });
+      return fmaxf(v, __shfl_xor(v, 32));
+    };
+    top = largest(top);
+    if (lane == 0) tops[w] = top;
     const bool lost = __syncthreads_or(no_number);
 #pragma unroll
-    for (int j = 0; j <= GC; ++j)
+    for (int i = 0; i < NW; ++i) top = fmaxf(top, tops[i]);
+    top = lost ? kNoNumber : fmaxf(top, before.x);               // (and with it all of the state)
+    keep = before.x == kNone ? 0.f : fast_exp2(before.x - top);
+    // z, and the queries' references: their largest contribution p z, to its power of two
+    float most[GC];
 #pragma unroll
-      for (int i = 0; i < NW; ++i) top[j] = fmaxf(top[j], tops[j * NW + i]);
-    top[0] = lost ? kNoNumber : fmaxf(top[0], before.x);         // (and with it all of the state)
-    keep = before.x == kNone ? 0.f : fast_exp2(before.x - top[0]);
-    float den[GC];
-#pragma unroll
-    for (int j = 0; j < GC; ++j) den[j] = 0.f;
+    for (int j = 0; j < GC; ++j) most[j] = kNone;
     for (int m = tid; m < Mp; m += NTH) {
-      const float s = top[0] == kNone ? 0.f : fast_exp2(feat[m] - top[0]);
+      const float s = top == kNone ? 0.f : fast_exp2(feat[m] - top);
       float z = s;
       if (keep != 0.f && m < M) z += keep * old_z[m];
       feat[m] = s;
+      zs[m] = z;
       if (m < M && g0 == 0 && blockIdx.z == 0) a.state.z[at * M + m] = z;
+      const float power = z == 0.f ? kNone : (float)__builtin_amdgcn_frexp_expf(z);
+#pragma unroll
+      for (int j = 0; j < GC; ++j)
+        if (j < n) most[j] = fmaxf(most[j], feat[(1 + j) * Mp + m] + power);
+    }
+    if (tid == 0 && g0 == 0 && blockIdx.z == 0) a.state.shift[at] = top;
+#pragma unroll
+    for (int j = 0; j < GC; ++j) {
+      most[j] = largest(most[j]);
+      if (lane == 0) tops[(1 + j) * NW + w] = most[j];
+    }
+    __syncthreads();
+    // p, 2^24 below: up to 2^124 where z is the smallest number
+    float den[GC];
+#pragma unroll
+    for (int j = 0; j < GC; ++j) {
+      den[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) most[j] = fmaxf(most[j], tops[(1 + j) * NW + i]);
+    }
+    for (int m = tid; m < Mp; m += NTH) {
+      const float z = zs[m];
 #pragma unroll
       for (int j = 0; j < GC; ++j)
         if (j < n) {
-          const float p = fast_exp2(feat[(1 + j) * Mp + m] - top[1 + j]);
+          const float p = z == 0.f ? 0.f : fast_exp2(feat[(1 + j) * Mp + m] - most[j] - 24.f);
           feat[(1 + j) * Mp + m] = p;
           den[j] += p * z;
         }
     }
-    if (tid == 0 && g0 == 0 && blockIdx.z == 0) a.state.shift[at] = top[0];
 #pragma unroll
     for (int j = 0; j < GC; ++j) {
       den[j] = over_lanes<32>(den[j], [](float p, float q) { return p + q; });

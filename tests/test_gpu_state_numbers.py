@@ -202,3 +202,35 @@ def test_angles_lose_nothing_before_cosine_and_sine(fs):  # noqa: F811
     ang = rot.positions.cpu().double()[:, None] * rot.freqs.cpu()
     want = torch.cat([torch.cos(ang), torch.sin(ang)], dim=1)
     assert float((y - want).abs().max()) <= 1.5 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("B,heads,group,d,dv,M", [(4, 2, 1, 64, 64, 256), (4, 1, 1, 32, 30, 64), (6, 1, 4, 128, 128, 300), (300, 1, 1, 64, 40, 256), (4, 2, 5, 48, 48, 512)])
+@pytest.mark.parametrize("power", [-70, -135])
+def test_tokens_that_read_what_a_state_holds_little_of(fs, B, heads, group, d, dv, M, power):  # noqa: F811
+    """As above, for tokens: in one launch and in two.  The states' shift is 300, so that the new key adds nothing (it is 2^-300 of them)."""
+    import torch
+    gen, s = torch.Generator().manual_seed(B + d), d ** -0.25
+    theta, omega = make_theta(gen, "iso", heads, d), torch.randn((heads, M, d), generator=gen)
+    o, f = oracle(theta, omega, s, heads), fs.state_prepare(theta.cuda(), omega.cuda(), s)
+    q, k, v = (rows(gen, torch.float32, B, *n) for n in ((heads * group, 1, d), (heads, 1, d), (heads, 1, dv)))
+    q[1::2] *= 6
+    state = fs.state_new(B, heads, M, dv)
+    state.T.copy_(torch.randn(state.T.shape, generator=gen))
+    state.z.copy_(0.5 + torch.rand(state.z.shape, generator=gen))
+    state.shift.fill_(300.0)
+    for b in range(B):
+        for h in range(heads):
+            less = torch.full((M,), float(power), dtype=torch.float64, device="cuda")
+            if b % 2:
+                e = (s * q[b, h * group, 0].double() @ o.W1[h].T + o.bias[h]) / math.log(2.0)
+                less = (power - (e - e.max())).clamp(max=0.0)
+            state.T[b, h] = (state.T[b, h].double() * torch.exp2(less)[:, None]).float()
+            state.z[b, h] = (state.z[b, h].double() * torch.exp2(less)).float()
+    before = [t.clone() for t in state]
+    unread = torch.zeros(1, dtype=torch.int32, device="cuda")
+    Y = fs.state_step(f, state, q, k, v, unread=unread)
+    assert int(unread) == 0 and all(torch.equal(t, g) for t, g in zip(state, before))
+    for b in range(B):
+        for i in range(heads * group):
+            h = i // group
+            check(Y[b, i], o.read((state.T[b, h].double(), state.z[b, h].double(), None), h, q[b, i].double()).cpu(), F32, "Y")
