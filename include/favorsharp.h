@@ -341,6 +341,37 @@ int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_
                       int transposed, const fs_tensor* Y, const fs_tensor* Y2, void* stream);
 
 /*
+ * Rotary positions with several axes (time, height and width of a patch, say): a position has a number for each axis, pair i of a
+ * row belongs to axis axis_of[i] and is turned by the angle positions[axis_of[i]] freqs[i].  A pair whose axis is none of 0 .. axes - 1
+ * is at position 0 (multiplied by amplitude alone).  Everything else is as above; a text's rows have the same position on all axes.
+ */
+#define FS_ROTARY_MAX_AXES 8
+typedef struct {
+  const double* freqs;        /* device, rot_dim / 2 values: radians per position */
+  const int32_t* axis_of;     /* device, rot_dim / 2 values */
+  const int32_t* positions;   /* device: row l of sequence b is at positions[a stride_a + b stride_b + l stride_l] of axis a */
+  int64_t stride_a, stride_b, stride_l; /* >= 0 */
+  int32_t axes;               /* 1 .. FS_ROTARY_MAX_AXES */
+  int32_t rot_dim;            /* even, 2 .. d */
+  int32_t interleaved;
+  float amplitude;
+} fs_rotary_axes;
+
+typedef enum {
+  FS_AXES_BLOCKS = 0,   /* the pairs of the first axis, then those of the second, ... */
+  FS_AXES_CYCLIC = 1    /* one pair of each axis in turn; axes whose pairs are used up are left out */
+} fs_axes_order;
+/* HOST function: the frequencies and axes of sum(host_pairs) pairs, host_pairs[a] of them of axis a, in an order.  whole = 0: the
+ * j-th pair of an axis with n has base^(-j / n), as if each axis were a row of its own; whole = 1: the i-th pair of the row's n
+ * has base^(-i / n), as in a row of one axis.  1 .. 512 pairs. */
+int favorsharp_rotary_sections(int axes, const int32_t* host_pairs, double base, int order, int whole, double* host_freqs,
+                               int32_t* host_axis_of);
+
+/* favorsharp_rotary for positions with several axes. */
+int favorsharp_rotary_axes(const fs_rotary_axes* rot, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d,
+                           int transposed, const fs_tensor* Y, const fs_tensor* Y2, void* stream);
+
+/*
  * Attention through kept states: key sides that outlive a call.  With K_hat = P S^T (Section 2.1) the keys and values of a
  * sequence enter attention (Section 2.2) only through S^T [V 1], which grows by appending.  A pool holds `slots` such
  * states for `heads` key heads each, contiguous, owned by the caller:
@@ -428,6 +459,60 @@ int favorsharp_state_append_backward(const fs_features* host_features, const fs_
                                      const fs_state* dstate, const fs_tensor* K, const fs_tensor* V, int B, int L, int dv,
                                      const int32_t* lengths, const fs_rotary* rot, const fs_tensor* dK, const fs_tensor* dV,
                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Linear attention with a decay for each head: causal, without a normaliser, and with states that forget.  Key head h has
+ * lambda = exp(log_decay[h]) (device, float32, one for each of `heads` key heads; values above 0 count as 0, -infinity keeps no
+ * row for the next), and a state S [d, dv] of a sequence and a key head becomes
+ *   S_i = lambda S_(i-1) + K_i V_i',   Y_i = scale Q_i S_i
+ * row by row; the calls compute that in chunks of 64 rows.  A pool holds `slots` states for each key head, contiguous, owned by
+ * the caller, S [slots][heads][d][dv] float32 (16-byte aligned); an empty state is zeros.
+ *   H query heads share the key heads in order, their decays and states: query head i reads key head i / (H / heads).  H % heads = 0.
+ *   slots, lengths: as for the states above.  Rows l >= lengths[b] are padding: not read, their output rows are zeros.  Where a call
+ *   writes states a sequence whose slot is not in the pool, or is also that of an earlier sequence, is left out: its state
+ *   stays, its output rows are zeros.  Where it reads them alone sequences may share a slot; those without one are as if it were empty.
+ *   All products have the accuracy of fp32 for f32 tensors; for bf16 tensors the states have it, and so have rows that are written
+ *   in f32, while rows that are rounded to bf16 have scores and states rounded to 16 bits before their products.  Results are
+ *   rounded once, to their dtype.  Numbers below 2^-109 lose bits, as the rest of a number has no exponent there.
+ *   log_decay and scale are constants: there is no gradient with respect to them.
+ *   d, dv <= 128 (the columns of V and S are independent of each other: wider values are calls on parts of them), B H and
+ *   slots * heads <= 65535, L H / heads <= 2^29.  Q, K, V and dY of a call share a dtype.
+ * Calls that write a state must be ordered with all others on it by the caller.  Asynchronous.  Where a *_workspace_bytes query
+ * answers 0 the workspace may be NULL (a query for sizes that are refused answers 0, too).
+ */
+typedef struct {
+  float* S;       /* device */
+  int32_t slots;
+} fs_decay_state;
+
+/* Rows Q [B, H, L, d], K [B, heads, L, d], V [B, heads, L, dv] after what the states `before` hold (NULL: empty ones) -> Y [B, H, L, dv],
+ * and the states after the last row into `after` (NULL: not wanted; the same pool as `before`: in place; another: as many slots, those
+ * that no sequence names stay as they are; no other overlap).  left_out (device int32, or NULL): the number of sequences that were left
+ * out is ADDED to it. */
+size_t favorsharp_decay_attention_workspace_bytes(int B, int H, int heads, int L, int d, int dv);
+int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_tensor* V, int B, int H, int heads, int L, int d, int dv,
+                               const float* log_decay, float scale, const fs_decay_state* before, const fs_decay_state* after,
+                               const int32_t* slots, const int32_t* lengths, const fs_tensor* Y, int32_t* left_out,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sum(Y * dY) + sum(after * dafter) with respect to Q, K, V and (dbefore, or NULL) the states before.  before: as they
+ * were before the forward call (NULL: empty).  dafter: the gradient at the states after it (NULL: zero).  exclusive = 1 if that
+ * call had `after`, so that sequences were left out as above (they have no part in any gradient); it has to be 1 with dafter, and
+ * needs a pool then.  dbefore: overwritten; each slot has the sum over the sequences that read it, in their order, zeros where none
+ * does; it must not overlap the other pools.  All pools have as many slots.  dQ, dK, dV any dtype. */
+size_t favorsharp_decay_attention_backward_workspace_bytes(int B, int H, int heads, int L, int d, int dv, int with_dbefore);
+int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, const fs_tensor* V, const fs_tensor* dY, int B, int H,
+                                        int heads, int L, int d, int dv, const float* log_decay, float scale,
+                                        const fs_decay_state* before, const fs_decay_state* dafter, const int32_t* slots,
+                                        const int32_t* lengths, int exclusive, const fs_tensor* dQ, const fs_tensor* dK,
+                                        const fs_tensor* dV, const fs_decay_state* dbefore,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of every sequence: K [B, heads, 1, d], V [B, heads, 1, dv] into the states (in place), then Y [B, H, 1, dv] for
+ * Q [B, H, 1, d].  left_out as above.  No workspace. */
+int favorsharp_decay_step(const fs_decay_state* state, const int32_t* slots, const fs_tensor* Q, const fs_tensor* K, const fs_tensor* V,
+                          int B, int H, int heads, int d, int dv, const float* log_decay, float scale, const fs_tensor* Y,
+                          int32_t* left_out, void* stream);
 
 #ifdef __cplusplus
 }

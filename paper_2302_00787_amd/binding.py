@@ -45,6 +45,15 @@ class FsFeatures(ctypes.Structure):
                 ("dense_c2", c_int32), ("qk_scale", c_float)]
 
 
+class FsRotaryAxes(ctypes.Structure):
+    _fields_ = [("freqs", c_void_p), ("axis_of", c_void_p), ("positions", c_void_p), ("stride_a", c_int64), ("stride_b", c_int64),
+                ("stride_l", c_int64), ("axes", c_int32), ("rot_dim", c_int32), ("interleaved", c_int32), ("amplitude", c_float)]
+
+
+class FsDecayState(ctypes.Structure):
+    _fields_ = [("S", c_void_p), ("slots", c_int32)]
+
+
 class FavorSharpError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -117,6 +126,7 @@ def lib() -> ctypes.CDLL:
         L.favorsharp_kernel_matvec.argtypes = [c_void_p, P, P, c_int, c_int, c_int, c_float, c_float, c_void_p, c_int,
                                                c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         R, S, F = ctypes.POINTER(FsRotary), ctypes.POINTER(FsState), ctypes.POINTER(FsFeatures)
+        X, D = ctypes.POINTER(FsRotaryAxes), ctypes.POINTER(FsDecayState)
         ws = [c_void_p, c_size_t, c_void_p]
         for name, restype, argtypes in (
                 ("rotary_frequencies", c_int, [c_int, c_double, c_int, c_double, c_int, c_double, c_double, c_void_p]),
@@ -132,7 +142,14 @@ def lib() -> ctypes.CDLL:
                 ("state_attention_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int, c_int]),
                 ("state_attention_backward", c_int, [F, S, c_void_p, P, P, c_int, c_int, c_int, c_int, c_void_p, R, P, S] + ws),
                 ("state_append_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int]),
-                ("state_append_backward", c_int, [F, S, c_void_p, S, P, P, c_int, c_int, c_int, c_void_p, R, P, P] + ws)):
+                ("state_append_backward", c_int, [F, S, c_void_p, S, P, P, c_int, c_int, c_int, c_void_p, R, P, P] + ws),
+                ("rotary_sections", c_int, [c_int, c_void_p, c_double, c_int, c_int, c_void_p, c_void_p]),
+                ("rotary_axes", c_int, [X, P, c_int, P, c_int, c_int, c_int, c_int, c_int, P, P, c_void_p]),
+                ("decay_attention_workspace_bytes", c_size_t, [c_int] * 6),
+                ("decay_attention", c_int, [P, P, P] + [c_int] * 6 + [c_void_p, c_float, D, D, c_void_p, c_void_p, P, c_void_p] + ws),
+                ("decay_attention_backward_workspace_bytes", c_size_t, [c_int] * 7),
+                ("decay_attention_backward", c_int, [P, P, P, P] + [c_int] * 6 + [c_void_p, c_float, D, D, c_void_p, c_void_p, c_int, P, P, P, D] + ws),
+                ("decay_step", c_int, [D, c_void_p, P, P, P] + [c_int] * 5 + [c_void_p, c_float, P, c_void_p, c_void_p])):
             fn = getattr(L, "favorsharp_" + name)
             fn.restype, fn.argtypes = restype, argtypes
         _lib = L
@@ -463,6 +480,7 @@ def kernel_matvec(theta: torch.Tensor, X: torch.Tensor, Y: torch.Tensor, qk_scal
 
 
 # ------------------------------------------------------------------ rotary positions and attention through kept states
+AXES_ORDERS = {"blocks": 0, "cyclic": 1}
 ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "blend": 3}
 _SAME_DEVICE = contextlib.nullcontext()
 
@@ -472,6 +490,16 @@ class Rotary(NamedTuple):
     row l is at position l."""
     freqs: torch.Tensor
     positions: torch.Tensor | None = None
+    interleaved: bool = False
+    amplitude: float = 1.0
+
+
+class RotaryAxes(NamedTuple):
+    """fs_rotary_axes.  freqs [rot_dim / 2] float64 and axis_of [rot_dim / 2] int32 on the device; positions [axes, B, L] (or [axes, L]:
+    shared) int32."""
+    freqs: torch.Tensor
+    axis_of: torch.Tensor
+    positions: torch.Tensor
     interleaved: bool = False
     amplitude: float = 1.0
 
@@ -547,6 +575,8 @@ def _rotary_desc(rot: Rotary | None, B: int, L: int):
     """(fs_rotary or None, rot_dim)"""
     if rot is None:
         return None, 0
+    if isinstance(rot, RotaryAxes):
+        raise TypeError("positions with several axes are for rotary() alone: turn the rows first")
     if rot.freqs.dtype != torch.float64 or rot.freqs.dim() != 1 or not rot.freqs.is_contiguous():
         raise ValueError("freqs must be a contiguous float64 vector")
     p, sb, sl = rot.positions, 0, 0
@@ -560,7 +590,22 @@ def _rotary_desc(rot: Rotary | None, B: int, L: int):
                                  rot.amplitude)), rot_dim
 
 
-def _rotary_tensors(rot: Rotary | None):
+def _rotary_axes_desc(rot: RotaryAxes, B: int, L: int):
+    if rot.freqs.dtype != torch.float64 or rot.freqs.dim() != 1 or not rot.freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous float64 vector")
+    _int32("axis_of", rot.axis_of, rot.freqs.shape)
+    p = rot.positions
+    if p.dtype != torch.int32:
+        raise ValueError("positions must be int32")
+    _shaped("positions", p, (p.shape[0], L) if p.dim() == 2 else (p.shape[0], B, L))
+    sa, sb, sl = (p.stride(0), 0, p.stride(1)) if p.dim() == 2 else p.stride()
+    return ctypes.byref(FsRotaryAxes(rot.freqs.data_ptr(), rot.axis_of.data_ptr(), p.data_ptr(), sa, sb, sl, p.shape[0], 2 * rot.freqs.shape[0],
+                                     int(rot.interleaved), rot.amplitude))
+
+
+def _rotary_tensors(rot: Rotary | RotaryAxes | None):
+    if isinstance(rot, RotaryAxes):
+        return (rot.freqs, rot.axis_of, rot.positions)
     return () if rot is None else (rot.freqs, rot.positions)
 
 
@@ -586,9 +631,18 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plai
     return torch.from_numpy(out).to(device)
 
 
-def rotary(X: torch.Tensor, rot: Rotary, X2: torch.Tensor | None = None, transposed: bool = False, out: torch.Tensor | None = None,
+def rotary_sections(pairs, base: float = 10000.0, order: str = "blocks", whole: bool = False, device="cuda"):
+    """favorsharp_rotary_sections: pairs[a] pairs of axis a -> (freqs float64, axis_of int32) of a RotaryAxes."""
+    n = np.asarray(pairs, dtype=np.int32)
+    freqs, axis_of = np.empty(max(int(n.sum()), 1), dtype=np.float64), np.empty(max(int(n.sum()), 1), dtype=np.int32)
+    _check(lib().favorsharp_rotary_sections(n.size, n.ctypes.data_as(c_void_p), base, AXES_ORDERS[order], int(whole),
+                                            freqs.ctypes.data_as(c_void_p), axis_of.ctypes.data_as(c_void_p)), "favorsharp_rotary_sections")
+    return torch.from_numpy(freqs).to(device), torch.from_numpy(axis_of).to(device)
+
+
+def rotary(X: torch.Tensor, rot: Rotary | RotaryAxes, X2: torch.Tensor | None = None, transposed: bool = False, out: torch.Tensor | None = None,
            out2: torch.Tensor | None = None):
-    """favorsharp_rotary: X [B,H,L,d] (and X2 [B,H2,L,d]) turned by their positions -> Y (or (Y, Y2)); transposed: the backward pass.
+    """favorsharp_rotary, or favorsharp_rotary_axes for a RotaryAxes: X [B,H,L,d] (and X2 [B,H2,L,d]) turned by their positions -> Y (or (Y, Y2)); transposed: the backward pass.
     out may be X itself, out2 X2."""
     B, H, L, d = X.shape
     if out is None:
@@ -602,12 +656,14 @@ def rotary(X: torch.Tensor, rot: Rotary, X2: torch.Tensor | None = None, transpo
             out2 = _empty((B, H2, L, d), X2.dtype, X.device)
         _shaped("out2", out2, X2.shape)
     device = _one_device(X, X2, out, out2, *_rotary_tensors(rot))
-    r, _ = _rotary_desc(rot, B, L)
+    axes = isinstance(rot, RotaryAxes)
+    r = _rotary_axes_desc(rot, B, L) if axes else _rotary_desc(rot, B, L)[0]
+    turn = lib().favorsharp_rotary_axes if axes else lib().favorsharp_rotary
     two = (ctypes.byref(_desc4(X2)), ctypes.byref(_desc4(out2))) if H2 else (None, None)
     with _on(device):
-        st = lib().favorsharp_rotary(r, ctypes.byref(_desc4(X)), H, two[0], H2, B, L, d, int(transposed), ctypes.byref(_desc4(out)), two[1],
-                                     _raw_stream(device.index))
-    _check(st, "favorsharp_rotary")
+        st = turn(r, ctypes.byref(_desc4(X)), H, two[0], H2, B, L, d, int(transposed), ctypes.byref(_desc4(out)), two[1],
+                  _raw_stream(device.index))
+    _check(st, "favorsharp_rotary_axes" if axes else "favorsharp_rotary")
     return out if X2 is None else (out, out2)
 
 
@@ -757,3 +813,111 @@ def state_append_backward(f: Features, state: State, dstate: State, K: torch.Ten
                                                     ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_state_append_backward")
     return dK, dV
+
+
+# ------------------------------------------------------------------ linear attention with a decay for each head
+def _decay_pools(heads: int, d: int, dv: int, B: int, slots, *pools):
+    """fs_decay_state of each pool [slots, heads, d, dv] (None: NULL)."""
+    n = None
+    for p in pools:
+        if p is None:
+            continue
+        if p.dtype != torch.float32 or not p.is_contiguous():
+            raise ValueError("states must be contiguous float32")
+        n = p.shape[0] if n is None else n
+        _shaped("state", p, (n, heads, d, dv))
+        if slots is None and B > n:
+            raise ValueError("more sequences than slots")
+    return [None if p is None else ctypes.byref(FsDecayState(p.data_ptr(), n)) for p in pools]
+
+
+def _log_decay(log_decay: torch.Tensor, heads: int) -> int:
+    if log_decay.dtype != torch.float32 or not log_decay.is_contiguous():
+        raise ValueError("log_decay must be contiguous float32")
+    _shaped("log_decay", log_decay, (heads,))
+    return log_decay.data_ptr()
+
+
+def decay_state_new(slots: int, heads: int, d: int, dv: int, device="cuda") -> torch.Tensor:
+    """Empty states of decay_attention and decay_step: [slots, heads, d, dv] float32."""
+    return torch.zeros((slots, heads, d, dv), dtype=torch.float32, device=device)
+
+
+def decay_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: torch.Tensor, scale: float = 1.0,
+                    before: torch.Tensor | None = None, after: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                    slots: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=None, left_out: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """favorsharp_decay_attention: Q [B,H,L,d], K [B,heads,L,d], V [B,heads,L,dv], log_decay [heads] -> Y [B,H,L,dv].  before, after: pools
+    [slots,heads,d,dv] (the same one: in place)."""
+    B, H, L, d = Q.shape
+    heads, dv = K.shape[1], V.shape[3]
+    _shaped("K", K, (B, heads, L, d))
+    _shaped("V", V, (B, heads, L, dv))
+    if out is None:
+        out = _empty((B, H, L, dv), out_dtype or Q.dtype, Q.device)
+    _shaped("out", out, (B, H, L, dv))
+    device = _one_device(Q, K, V, out, log_decay, before, after, lengths, slots, left_out, workspace)
+    old, new = _decay_pools(heads, d, dv, B, slots, before, after)
+    L_ = lib()
+    ws, ws_bytes, held = _room(L_.favorsharp_decay_attention_workspace_bytes(B, H, heads, L, d, dv), device, workspace)
+    with _on(device):
+        st = L_.favorsharp_decay_attention(ctypes.byref(_desc4(Q)), ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, H, heads, L, d, dv,
+                                           _log_decay(log_decay, heads), scale, old, new, _int32("slots", slots, (B,)),
+                                           _int32("lengths", lengths, (B,)), ctypes.byref(_desc4(out)), _counter("left_out", left_out),
+                                           ws, ws_bytes, _raw_stream(device.index))
+    _check(st, "favorsharp_decay_attention")
+    return out
+
+
+def decay_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, dY: torch.Tensor, log_decay: torch.Tensor, scale: float = 1.0,
+                             before: torch.Tensor | None = None, dafter: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                             slots: torch.Tensor | None = None, exclusive: bool | None = None, grad_dtype=None, grads=None,
+                             dbefore: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """favorsharp_decay_attention_backward: gradients of sum(Y * dY) + sum(after * dafter) -> (dQ, dK, dV, dbefore), dbefore a pool if there
+    is one of `before` (or is given), else None.  exclusive: the forward call had `after` (None: it did if there is dafter)."""
+    B, H, L, d = Q.shape
+    heads, dv = K.shape[1], V.shape[3]
+    _shaped("K", K, (B, heads, L, d))
+    _shaped("V", V, (B, heads, L, dv))
+    _shaped("dY", dY, (B, H, L, dv))
+    if grads is None:
+        grads = tuple(_empty(t.shape, grad_dtype or t.dtype, t.device) for t in (Q, K, V))
+    for name, t, like in zip(("dQ", "dK", "dV"), grads, (Q, K, V)):
+        _shaped(name, t, like.shape)
+    if dbefore is None and before is not None:
+        dbefore = torch.empty_like(before)
+    device = _one_device(Q, K, V, dY, *grads, log_decay, before, dafter, dbefore, lengths, slots, workspace)
+    old, dnew, dold = _decay_pools(heads, d, dv, B, slots, before, dafter, dbefore)
+    exclusive = dafter is not None if exclusive is None else exclusive
+    L_ = lib()
+    ws, ws_bytes, held = _room(L_.favorsharp_decay_attention_backward_workspace_bytes(B, H, heads, L, d, dv, int(dbefore is not None)), device,
+                               workspace)
+    with _on(device):
+        st = L_.favorsharp_decay_attention_backward(*(ctypes.byref(_desc4(t)) for t in (Q, K, V, dY)), B, H, heads, L, d, dv,
+                                                    _log_decay(log_decay, heads), scale, old, dnew, _int32("slots", slots, (B,)),
+                                                    _int32("lengths", lengths, (B,)), int(exclusive),
+                                                    *(ctypes.byref(_desc4(t)) for t in grads), dold, ws, ws_bytes, _raw_stream(device.index))
+    _check(st, "favorsharp_decay_attention_backward")
+    return (*grads, dbefore)
+
+
+def decay_step(state: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: torch.Tensor, scale: float = 1.0,
+               slots: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=None,
+               left_out: torch.Tensor | None = None) -> torch.Tensor:
+    """favorsharp_decay_step: K [B,heads,1,d], V [B,heads,1,dv] into the states (in place), then Q [B,H,1,d] -> Y [B,H,1,dv]."""
+    B, H, L, d = Q.shape
+    heads, dv = K.shape[1], V.shape[3]
+    _shaped("Q", Q, (B, H, 1, d))
+    _shaped("K", K, (B, heads, 1, d))
+    _shaped("V", V, (B, heads, 1, dv))
+    if out is None:
+        out = _empty((B, H, 1, dv), out_dtype or Q.dtype, Q.device)
+    _shaped("out", out, (B, H, 1, dv))
+    device = _one_device(Q, K, V, out, log_decay, state, slots, left_out)
+    pool, = _decay_pools(heads, d, dv, B, slots, state)
+    with _on(device):
+        st = lib().favorsharp_decay_step(pool, _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)), ctypes.byref(_desc4(K)),
+                                         ctypes.byref(_desc4(V)), B, H, heads, d, dv, _log_decay(log_decay, heads), scale,
+                                         ctypes.byref(_desc4(out)), _counter("left_out", left_out), _raw_stream(device.index))
+    _check(st, "favorsharp_decay_step")
+    return out

@@ -34,6 +34,9 @@ SOURCES = {
     "kernels_state.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kernels_state_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kernels_state_step.hip": [],
+    "decay_api.hip": [],
+    "kernels_decay.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "kernels_decay_step.hip": [],
     "host_fit.cpp": [],
 }
 

@@ -12,14 +12,15 @@ namespace {
 
 struct RotaryArgs {
   RotaryDev r;
+  AxesDev x;                     // positions with several axes, instead of r's
   TensorDev X, X2, Y, Y2;
   int H, H2, B, L, d, units, heads_per_part;
   float sgn;
 };
 
 // Threads: units of sixteen turned numbers (pairs 8 u .. 8 u + 7 with their partners), then units of eight that stay; FAST: rot a multiple of
-// 16, so that both halves of a unit are whole.
-template <bool FAST>
+// 16, so that both halves of a unit are whole.  AXES: a pair's position is that of its axis.
+template <bool FAST, bool AXES>
 __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
   const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   const int u = (int)(id % a.units);
@@ -39,12 +40,12 @@ __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
       next[1] = fetch8<true>(X, from, f1, a.d);
     };
     if constexpr (FAST) bring(h0);
-    const int pos = position_of(a.r, b, l);
+    const int pos = AXES ? 0 : position_of(a.r, b, l);
     float cs[8], sn[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int p = 8 * u + i;
-      const float2 x = cos_sin(pos, a.r.freqs[min(p, r - 1)], a.r.amplitude);
+      const int p = 8 * u + i, q = min(p, r - 1);
+      const float2 x = cos_sin(AXES ? position_of(a.x, q, b, l) : pos, a.r.freqs[q], a.r.amplitude);
       cs[i] = x.x;
       sn[i] = a.sgn * x.y;
     }
@@ -115,9 +116,9 @@ __global__ void __launch_bounds__(256) k_rotary_table(RotaryDev r, int B, int L,
 
 }  // namespace
 
-int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev& X2, int H2, int B, int L, int d, int transposed,
+int launch_rotary(const RotaryDev& r, const AxesDev& axes, const TensorDev& X, int H, const TensorDev& X2, int H2, int B, int L, int d, int transposed,
                   const TensorDev& Y, const TensorDev& Y2, hipStream_t st) {
-  RotaryArgs a{r, X, X2, Y, Y2, H, H2, B, L, d, 0, 0, transposed ? -1.f : 1.f};
+  RotaryArgs a{r, axes, X, X2, Y, Y2, H, H2, B, L, d, 0, 0, transposed ? -1.f : 1.f};
   a.units = (r.rot / 2 + 7) / 8 + (d - r.rot + 7) / 8;
   const long long threads = (long long)B * L * a.units, blocks = (threads + 255) / 256;
   if (blocks > 0xffffffLL) return 2;             // (threads of a launch have 32 bits)
@@ -127,8 +128,8 @@ int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev
   while (parts < H + H2 && blocks * parts < 2048) parts *= 2;
   a.heads_per_part = (H + H2 + parts - 1) / parts;
   const dim3 grid((unsigned)blocks, (H + H2 + a.heads_per_part - 1) / a.heads_per_part);
-  if (r.rot % 16 == 0) hipLaunchKernelGGL(k_rotary<true>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_rotary<false>, grid, dim3(256), 0, st, a);
+  auto kernel = axes.axes ? (r.rot % 16 == 0 ? k_rotary<true, true> : k_rotary<false, true>) : (r.rot % 16 == 0 ? k_rotary<true, false> : k_rotary<false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : 5;
 }
 

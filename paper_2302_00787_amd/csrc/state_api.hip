@@ -101,6 +101,23 @@ int turn_of(const fs_rotary* rot, int B, int L, char* ws, size_t off, st::Turn* 
   return st::launch_rotary_table(dev(rot), B, L, (float2*)(ws + off), stream);
 }
 
+// Rows turned by their positions, of either kind.
+int turn_rows(const st::RotaryDev& r, const st::AxesDev& axes, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d, int transposed,
+              const fs_tensor* Y, const fs_tensor* Y2, hipStream_t stream) {
+  if (B < 1 || L < 0 || d < 1 || H < 1 || H2 < 0 || (transposed != 0 && transposed != 1)) return FS_ERR_INVALID_ARG;
+  if (!tensor_ok(X, d, L > 0) || !tensor_ok(Y, d, L > 0)) return FS_ERR_INVALID_ARG;
+  if (H2 > 0 && (!tensor_ok(X2, d, L > 0) || !tensor_ok(Y2, d, L > 0))) return FS_ERR_INVALID_ARG;
+  if (d > 1024 || (long long)H + H2 > 65535 || (long long)B * L > (1ll << 31)) return FS_ERR_UNSUPPORTED;
+  // in place: the same rows, or none of them
+  auto same = [](const fs_tensor* a, const fs_tensor* b) {
+    return a->ptr != b->ptr || (a->dtype == b->dtype && a->stride_b == b->stride_b && a->stride_h == b->stride_h && a->stride_l == b->stride_l);
+  };
+  if (!same(X, Y) || (H2 > 0 && !same(X2, Y2))) return FS_ERR_INVALID_ARG;
+  if (L == 0) return FS_OK;
+  const TensorDev none{nullptr, 0, 0, 0, 0};
+  return st::launch_rotary(r, axes, fs::dev(X), H, H2 ? fs::dev(X2) : none, H2, B, L, d, transposed, fs::dev(Y), H2 ? fs::dev(Y2) : none, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -129,18 +146,39 @@ int favorsharp_rotary_frequencies(int rot_dim, double base, int scaling, double 
 
 int favorsharp_rotary(const fs_rotary* rot, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d, int transposed,
                       const fs_tensor* Y, const fs_tensor* Y2, void* stream) {
-  if (rot == nullptr || B < 1 || L < 0 || d < 1 || H < 1 || H2 < 0 || (transposed != 0 && transposed != 1)) return FS_ERR_INVALID_ARG;
-  if (!rotary_ok(rot, d) || !tensor_ok(X, d, L > 0) || !tensor_ok(Y, d, L > 0)) return FS_ERR_INVALID_ARG;
-  if (H2 > 0 && (!tensor_ok(X2, d, L > 0) || !tensor_ok(Y2, d, L > 0))) return FS_ERR_INVALID_ARG;
-  if (d > 1024 || (long long)H + H2 > 65535 || (long long)B * L > (1ll << 31)) return FS_ERR_UNSUPPORTED;
-  // in place: the same rows, or none of them
-  auto same = [](const fs_tensor* a, const fs_tensor* b) {
-    return a->ptr != b->ptr || (a->dtype == b->dtype && a->stride_b == b->stride_b && a->stride_h == b->stride_h && a->stride_l == b->stride_l);
-  };
-  if (!same(X, Y) || (H2 > 0 && !same(X2, Y2))) return FS_ERR_INVALID_ARG;
-  if (L == 0) return FS_OK;
-  const TensorDev none{nullptr, 0, 0, 0, 0};
-  return st::launch_rotary(dev(rot), dev(X), H, H2 ? dev(X2) : none, H2, B, L, d, transposed, dev(Y), H2 ? dev(Y2) : none, (hipStream_t)stream);
+  if (rot == nullptr || d < 1 || !rotary_ok(rot, d)) return FS_ERR_INVALID_ARG;
+  return turn_rows(dev(rot), st::AxesDev{}, X, H, X2, H2, B, L, d, transposed, Y, Y2, (hipStream_t)stream);
+}
+
+int favorsharp_rotary_sections(int axes, const int32_t* host_pairs, double base, int order, int whole, double* host_freqs, int32_t* host_axis_of) {
+  if (axes < 1 || axes > FS_ROTARY_MAX_AXES || host_pairs == nullptr || host_freqs == nullptr || host_axis_of == nullptr || !(base > 1.0) ||
+      !std::isfinite(base) || (order != FS_AXES_BLOCKS && order != FS_AXES_CYCLIC) || (whole != 0 && whole != 1))
+    return FS_ERR_INVALID_ARG;
+  int pairs = 0, used[FS_ROTARY_MAX_AXES] = {};
+  for (int a = 0; a < axes; ++a) {
+    if (host_pairs[a] < 0 || host_pairs[a] > 512) return FS_ERR_INVALID_ARG;       // rows of up to 1024 numbers
+    pairs += host_pairs[a];
+  }
+  if (pairs < 1 || pairs > 512) return FS_ERR_INVALID_ARG;
+  for (int p = 0, a = order == FS_AXES_BLOCKS ? 0 : axes - 1; p < pairs; ++p) {
+    if (order == FS_AXES_CYCLIC) a = (a + 1) % axes;
+    while (used[a] == host_pairs[a]) a = (a + 1) % axes;
+    host_axis_of[p] = a;
+    host_freqs[p] = std::pow(base, whole ? -(double)p / pairs : -(double)used[a] / host_pairs[a]);
+    ++used[a];
+  }
+  return FS_OK;
+}
+
+int favorsharp_rotary_axes(const fs_rotary_axes* rot, const fs_tensor* X, int H, const fs_tensor* X2, int H2, int B, int L, int d, int transposed,
+                           const fs_tensor* Y, const fs_tensor* Y2, void* stream) {
+  if (rot == nullptr || d < 1) return FS_ERR_INVALID_ARG;
+  const fs_rotary r{rot->freqs, rot->positions, rot->stride_b, rot->stride_l, rot->rot_dim, rot->interleaved, rot->amplitude};
+  if (!rotary_ok(&r, d) || rot->positions == nullptr || rot->stride_a < 0 || rot->axis_of == nullptr || (uintptr_t)rot->axis_of % 4 || rot->axes < 1 ||
+      rot->axes > FS_ROTARY_MAX_AXES)
+    return FS_ERR_INVALID_ARG;
+  const st::AxesDev axes{rot->axis_of, rot->positions, rot->stride_a, rot->stride_b, rot->stride_l, rot->axes};
+  return turn_rows(dev(&r), axes, X, H, X2, H2, B, L, d, transposed, Y, Y2, (hipStream_t)stream);
 }
 
 // ------------------------------------------------------------------------------------------ states

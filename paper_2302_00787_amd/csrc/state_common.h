@@ -77,6 +77,17 @@ __device__ __forceinline__ float2 cos_sin(int position, double freq, float ampli
   return make_float2(amplitude * (c - s * rest), amplitude * (s + c * rest));
 }
 __device__ __forceinline__ int position_of(const RotaryDev& r, int b, int l) { return r.positions ? r.positions[b * r.sb + l * r.sl] : l; }
+// Positions with several axes: pair p of a row is at positions[axis_of[p]] of it (at zero where that is no axis).  axes = 0: there are none.
+struct AxesDev {
+  const int32_t* axis_of;        // [rot / 2]
+  const int32_t* positions;
+  long long sa, sb, sl;
+  int axes;
+};
+__device__ __forceinline__ int position_of(const AxesDev& x, int pair, int b, int l) {
+  const int axis = x.axis_of[pair];
+  return axis >= 0 && axis < x.axes ? x.positions[axis * x.sa + b * x.sb + l * x.sl] : 0;
+}
 
 // Rotary positions as the kernels on states see them: rot = 0: rows as they are.  `table` [B][L][rot / 2] holds amplitude (cos, sin).
 struct Turn {
@@ -446,7 +457,7 @@ int launch_prepare(const float* theta, int groups, const float* Omega, int omega
 // Row terms r(k) of turned keys with a dense quadratic form, rows behind the lengths -inf.
 int launch_row_terms(const Features& f, const Rows& k, int B, int Hk, float* terms, hipStream_t st);
 
-int launch_rotary(const RotaryDev& r, const TensorDev& X, int H, const TensorDev& X2, int H2, int B, int L, int d, int transposed,
+int launch_rotary(const RotaryDev& r, const AxesDev& axes, const TensorDev& X, int H, const TensorDev& X2, int H2, int B, int L, int d, int transposed,
                   const TensorDev& Y, const TensorDev& Y2, hipStream_t st);
 int launch_rotary_table(const RotaryDev& r, int B, int L, float2* table, hipStream_t st);
 
