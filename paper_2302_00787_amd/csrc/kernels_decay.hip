@@ -208,8 +208,10 @@ __global__ void __launch_bounds__(256) k_decay_walk(WalkSet set, int ncb) {
   const Keep whole = keep_of(ld, kChunk);
   const Tiles<W, TB> t(wave);
   StateTiles<W, TB> S;
-  const float* from = p.seg > 0 ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
-                                : (w.init && p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
+  // (with segments the pool may hold the states after the call already)
+  const float* from = w.init == nullptr && p.seg == 0 ? nullptr
+                      : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
+                                                      : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<W, TB>(S, t, from, w.sa, w.sb, w.wa, w.wb, b0);
   bool filled = from != nullptr;
   __syncthreads();

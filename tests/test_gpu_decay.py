@@ -181,6 +181,18 @@ def test_segments(fs, dtype, B, H, Hk, L, d, dv, decay):
             close(got[3][b], want[3], F32)
 
 
+def test_segments_in_place(fs):
+    """States before and after in one pool, sequences long enough to be shared out."""
+    import torch
+    c = Case(fs, "f32", 2, 2, 1, 700, 32, 32, "slow", [700, 500])
+    pool = c.S0.clone()
+    Y = fs.decay_attention(c.Q, c.K, c.V, c.g, c.s, before=pool, after=pool, lengths=c.lengths)
+    for b in range(2):
+        y, S = c.forward(b, c.S0[b])
+        close(Y[b], y, F32)
+        close(pool[b], S, F32)
+
+
 @pytest.mark.parametrize("lengths", [[0, 1, 63, 64], [65, 100, -3, 1000], [128, 127, 0, 0]])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_padded_batches(fs, dtype, lengths):
