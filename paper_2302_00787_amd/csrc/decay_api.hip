@@ -33,13 +33,20 @@ Plan plan(int B, int heads, int L, int d, int dv, int blocks, int sets, bool end
 }
 Plan plan_forward(int B, int heads, int L, int d, int dv) { return plan(B, heads, L, d, dv, dec::column_blocks(dv), 1, false); }
 Plan plan_backward(int B, int heads, int L, int d, int dv, bool dbefore) {
-  return plan(B, heads, L, d, dv, 2 * dec::column_blocks(d) + dec::column_blocks(dv), 2, dbefore);
+  return plan(B, heads, L, d, dv, dec::column_blocks(std::max(d, dv)), 2, dbefore);
 }
 
 int sizes(int B, int H, int heads, int L, int d, int dv) {
   if (B < 1 || L < 0 || d < 1 || dv < 1 || H < 1 || heads < 1 || H % heads) return FS_ERR_INVALID_ARG;
   if (d > 128 || dv > 128 || !sequences_ok(B, H) || (long long)L * (H / heads) > kMaxRows) return FS_ERR_UNSUPPORTED;
   return FS_OK;
+}
+// offsets within a chunk of rows have 32 bits
+constexpr int64_t kMaxStride = 1 << 23;
+bool strides_ok(std::initializer_list<const fs_tensor*> list, int L) {
+  for (const fs_tensor* t : list)
+    if (L > 1 && t->stride_l > kMaxStride) return false;
+  return true;
 }
 int pools(std::initializer_list<const fs_decay_state*> list, int heads, int* slots) {
   *slots = 0;
@@ -77,6 +84,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
   if (!numbers_ok(log_decay, scale, slots, lengths) || (uintptr_t)left_out % 4 || (uintptr_t)workspace % 16) return FS_ERR_INVALID_ARG;
   if (!tensor_ok(Q, d, L > 0) || !tensor_ok(K, d, L > 0) || !tensor_ok(V, dv, L > 0) || !tensor_ok(Y, dv, L > 0)) return FS_ERR_INVALID_ARG;
   if (Q->dtype != K->dtype || Q->dtype != V->dtype) return FS_ERR_INVALID_ARG;
+  if (!strides_ok({Q, K, V, Y}, L)) return FS_ERR_UNSUPPORTED;
   const Plan p = plan_forward(B, heads, L, d, dv);
   if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
@@ -124,6 +132,7 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
   if (!tensor_ok(Q, d, L > 0) || !tensor_ok(K, d, L > 0) || !tensor_ok(V, dv, L > 0) || !tensor_ok(dY, dv, L > 0)) return FS_ERR_INVALID_ARG;
   if (!tensor_ok(dQ, d, L > 0) || !tensor_ok(dK, d, L > 0) || !tensor_ok(dV, dv, L > 0)) return FS_ERR_INVALID_ARG;
   if (Q->dtype != K->dtype || Q->dtype != V->dtype || Q->dtype != dY->dtype) return FS_ERR_INVALID_ARG;
+  if (!strides_ok({Q, K, V, dY, dQ, dK, dV}, L)) return FS_ERR_UNSUPPORTED;
   const Plan p = plan_backward(B, heads, L, d, dv, dbefore != nullptr);
   if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
@@ -163,7 +172,10 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
     if (int rc = dec::launch_join(j, s)) return rc;
   }
   const bool fine = dQ->dtype == FS_F32 || dK->dtype == FS_F32 || dV->dtype == FS_F32;
-  if (int rc = dec::launch_walks(a, 0, 3, Q->dtype, fine, s)) return rc;
+  const bool one = std::max(d, dv) <= 64;           // dK and dV in one walk
+  if (int rc = dec::launch_walks(a, 0, one ? 1 : 3, Q->dtype, fine, s)) return rc;
+  if (one)
+    if (int rc = dec::launch_back(a, 1, Q->dtype, fine, s)) return rc;
   return dbefore != nullptr && !direct ? dec::launch_slot_sums(a.c, ends, dbefore->S, s) : FS_OK;
 }
 

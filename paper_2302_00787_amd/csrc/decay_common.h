@@ -62,6 +62,7 @@ struct JoinSet {
   int count;
 };
 int launch_walks(const WalkSet& a, int from, int count, int dtype, bool fine, hipStream_t st);
+int launch_back(const WalkSet& a, int from, int dtype, bool fine, hipStream_t st);
 int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st);
 int launch_join(const JoinSet& a, hipStream_t st);
 // Pool of gradients: the sums over the sequences that read a slot, in their order (zeros where none does).
@@ -80,23 +81,30 @@ struct StepArgs {
 };
 int launch_step(const StepArgs& a, hipStream_t st);
 
-// exp(n log_decay) for a whole number n >= 0, rounded once; log decays above zero count as zero, those below -10^30 as that (0 times
-// -infinity would be none).
-__device__ __forceinline__ double exponent(float log_decay) { return (double)fmaxf(log_decay > 0.f ? 0.f : log_decay, -1e30f); }
-__device__ __forceinline__ float power(float log_decay, long long n) {
-  if (log_decay != log_decay) return log_decay;
-  return (float)exp((double)n * exponent(log_decay));
+// exp(n log_decay) for a whole number n >= 0; log decays above zero count as zero, those below -10^30 as that (0 times -infinity would be
+// none).  The product's rounding error goes into the result (|x| 2^-24 of it otherwise).
+struct Exponent { float x, rest; };
+__device__ __forceinline__ Exponent exponent(float log_decay, float n) {
+  const float g = log_decay > 0.f ? 0.f : fmaxf(log_decay, -1e30f), x = n * g;
+  return {log_decay != log_decay ? log_decay : x, fmaf(n, g, -x)};
 }
-// A state's factor lambda^n as S + S (lambda^n - 1) where it is near one: that rounds the product alone, and not the factor in the same way
-// at every chunk of a long sequence.
-struct Keep { float whole, part; };
-__device__ __forceinline__ Keep keep_of(float log_decay, long long n) {
-  if (log_decay != log_decay) return {0.f, log_decay};
-  const double x = (double)n * exponent(log_decay);
-  if (x > -0.69) return {1.f, (float)expm1(x)};
-  return {0.f, (float)exp(x)};
+__device__ __forceinline__ float power(float log_decay, int n) {
+  const Exponent e = exponent(log_decay, (float)n);
+  const float p = expf(e.x);
+  return e.x < -104.f ? p : fmaf(p, e.rest, p);
 }
-__device__ __forceinline__ float kept(Keep k, float s) { return fmaf(s, k.part, s * k.whole); }
+// A state's factor lambda^n: as S + S (lambda^n - 1) where it is near one, as that rounds the product alone, and not the factor in the same
+// way at every chunk of a long sequence.
+struct Keep { float part; bool near; };
+__device__ __forceinline__ Keep keep_of(float log_decay, int n) {
+  const Exponent e = exponent(log_decay, (float)n);
+  if (e.x > -0.69f) {
+    const float p = expm1f(e.x);
+    return {fmaf(1.f + p, e.rest, p), true};
+  }
+  return {power(log_decay, n), false};
+}
+__device__ __forceinline__ float kept(Keep k, float s) { return k.near ? fmaf(s, k.part, s) : s * k.part; }
 
 }  // namespace dec
 }  // namespace fs

@@ -8,6 +8,8 @@
 // of a in the sums of the state are weighed in 32 bits and have three pieces, as the states themselves are results in fp32.
 #include "decay_common.h"
 
+#include <type_traits>
+
 namespace fs {
 namespace dec {
 namespace {
@@ -17,6 +19,13 @@ using st::Raw8;
 using st::f32x8;
 using st::each_product;
 using st::read_tr;
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }      // (a scalar: branches on it, too)
+__device__ __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+__device__ __forceinline__ Keep scalar(Keep k) { return {scalar(k.part), __builtin_amdgcn_readfirstlane((int)k.near) != 0}; }
+
+// Operands of a part of a chunk are not fetched before the part: that would take registers that hold more waves otherwise.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int P> __device__ __forceinline__ Op<P> pieces(f32x8 x) {
   if constexpr (P == 2) {
@@ -46,39 +55,99 @@ __device__ __forceinline__ bool place(const Call& c, int nseg, int ncb, Place* p
   const int s = (int)(u / nseg);
   p->b = s / c.Hk;
   p->h = s - p->b * c.Hk;
-  p->len = c.lengths ? max(0, min(c.lengths[p->b], c.L)) : c.L;
+  int len = c.lengths ? max(0, min(c.lengths[p->b], c.L)) : c.L, slot;
   if (c.unique) {
-    p->slot = st::unique_slot_of(c.slots, c.nslots, p->b);
-    if (p->slot < 0) { p->slot = -2; p->len = 0; }
+    slot = st::unique_slot_of(c.slots, c.nslots, p->b);
+    if (slot < 0) { slot = -2; len = 0; }
   } else {
-    p->slot = st::slot_of(c.slots, c.nslots, p->b);
+    slot = st::slot_of(c.slots, c.nslots, p->b);
   }
+  p->len = __builtin_amdgcn_readfirstlane(len);          // (the same in all lanes; addresses are to be scalar)
+  p->slot = __builtin_amdgcn_readfirstlane(slot);
   return true;
 }
 
-// Rows of a chunk, from memory to LDS as P bf16 pieces: 256 threads, units of eight numbers.
+// Rows of a chunk of one head: `at` is the chunk's lowest row in memory, row i of the n that are there at i pitch (back: (n - 1 - i) pitch)
+// bytes.
+struct Chunk {
+  const char* at;
+  int n;
+};
+// A head's rows (of `heads` consecutive ones), and a chunk's of them.
+struct Head {
+  const char* at;
+  long long next;                // bytes from head to head
+  int pitch;
+  __device__ __forceinline__ Head(const TensorDev& t, int b, int h) {
+    const int size = t.dtype == 0 ? 4 : 2;
+    at = (const char*)t.ptr + st::row_base(t, b, h, 0) * size;
+    next = t.sh * size;
+    pitch = (int)t.sl * size;
+  }
+  __device__ __forceinline__ Chunk chunk(int i, int r0, int n, int len, int back) const {
+    return {at + i * next + (long long)(back ? len - r0 - n : r0) * pitch, n};
+  }
+};
+// A buffer over what lies from a pointer on; an offset of kNowhere reads zeros and writes nothing.
+constexpr int kNowhere = (int)0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
+}
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+
+// From memory to LDS as P bf16 pieces: 256 threads, units of eight numbers.  FULL: rows have no ragged end, and units are loads whose
+// offsets from the chunk's first row stay; else number by number at the ends.
 template <int P, int W, bool FULL, int DT> struct Stage {
-  static constexpr int UNITS = W / 8, N = kChunk * UNITS / 256, LD = W + 8, PLANE = kChunk * LD;
+  static constexpr int UNITS = W / 8, N = kChunk * UNITS / 256, LD = W + 8, PLANE = kChunk * LD, SIZE = DT == 0 ? 4 : 2;
   Raw8 raw[N];
-  // rows r0 .. of the walk (n of them are there), numbers c0 .. c0 + W - 1
-  __device__ __forceinline__ void fetch(const TensorDev& t, int b, int h, int r0, int n, int len, int back, int c0, int cols) {
+  int off[FULL ? N : 1];
+  int row0, c, cols, back, pitch;
+  // numbers c0 .. c0 + W - 1 of the rows
+  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int backwards) : cols(ncols), back(backwards), pitch(h.pitch) {
+    row0 = threadIdx.x / UNITS;
+    c = c0 + 8 * (threadIdx.x % UNITS);
+    if constexpr (FULL) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + 256 * i, row = id / UNITS, c = c0 + 8 * (id % UNITS);
-      raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-      if (row < n && c < cols) raw[i] = st::fetch8<FULL, DT>(t, st::row_base(t, b, h, back ? len - 1 - r0 - row : r0 + row), c, cols);
+      for (int i = 0; i < N; ++i) off[i] = offset(i, kChunk);
     }
   }
-  __device__ __forceinline__ void store(uint16_t* s, int c0, int cols) const {
+  __device__ __forceinline__ int offset(int i, int n) const {
+    const int row = row0 + 256 / UNITS * i;
+    return row < n && c < cols ? (back ? n - 1 - row : row) * pitch + c * SIZE : kNowhere;
+  }
+  __device__ __forceinline__ void fetch(const Chunk& k) {
+    if constexpr (FULL) {
+      const __amdgpu_buffer_rsrc_t r = buffer_at(k.at);
+      auto load = [&](int i, int o) {
+        raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
+        if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
+      };
+      if (k.n == kChunk) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) load(i, off[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) load(i, offset(i, k.n));
+      }
+    } else {
+      const TensorDev t{k.at, DT, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = row0 + 256 / UNITS * i;
+        raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+        if (row < k.n && c < cols) raw[i] = st::fetch8<FULL, DT>(t, (long long)(back ? k.n - 1 - row : row) * (pitch / SIZE), c, cols);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* s, int c0) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + 256 * i, row = id / UNITS, c = 8 * (id % UNITS);
-      uint16_t* to = s + row * LD + c;
+      uint16_t* to = s + (row0 + 256 / UNITS * i) * LD + (c - c0);
       if constexpr (P == 1 && FULL) {
         *(u32x4*)to = raw[i].a;
       } else {
         // (number by number: they are numbers of different rows or columns of a state)
-        const f32x8 x = st::expand8<FULL, DT>(raw[i], DT, c0 + c, cols);
+        const f32x8 x = st::expand8<FULL, DT>(raw[i], DT, c, cols);
         if constexpr (P == 1) {
           *(bf16x8*)to = __builtin_convertvector(x, bf16x8);
         } else {
@@ -91,6 +160,106 @@ template <int P, int W, bool FULL, int DT> struct Stage {
     }
   }
 };
+
+// A wave's sixteen rows as operands: a lane has eight numbers 32 k + 8 g .. of row 16 wave + (lane % 16) for each step k, or (PERM) numbers
+// 32 k + 4 g .. and 32 k + 16 + 4 g .., the order in which two stacked accumulators hold theirs.
+template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps {
+  static constexpr int SIZE = DT == 0 ? 4 : 2;
+  Raw8 raw[STEPS];
+  int row, cols, back, pitch;
+  __device__ __forceinline__ RowOps(const Head& h, int ncols, int backwards) : cols(ncols), back(backwards), pitch(h.pitch) {
+    row = 16 * wave_id() + (threadIdx.x & 15);
+  }
+  __device__ __forceinline__ void fetch(const Chunk& k) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const bool there = row < k.n;
+    const int first = (back ? k.n - 1 - row : row) * pitch;
+    if constexpr (FULL) {
+      const __amdgpu_buffer_rsrc_t r = buffer_at(k.at);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        if constexpr (!PERM) {
+          const int o = there && 32 * i + 8 * g < cols ? first + 8 * g * SIZE : kNowhere;
+          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 32 * i * SIZE, 0);
+          if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 32 * i * SIZE + 16, 0);
+        } else {
+          const int o = there && 32 * i + 4 * g < cols ? first + 4 * g * SIZE : kNowhere, p = there && 32 * i + 16 + 4 * g < cols ? first + 4 * g * SIZE : kNowhere;
+          if constexpr (DT == 0) {
+            raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 32 * i * SIZE, 0);
+            raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, p, (32 * i + 16) * SIZE, 0);
+          } else {
+            const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, o, 32 * i * SIZE, 0), y = __builtin_amdgcn_raw_buffer_load_b64(r, p, (32 * i + 16) * SIZE, 0);
+            raw[i].a = u32x4{x[0], x[1], y[0], y[1]};
+          }
+        }
+      }
+    } else {
+      const long long at = first / SIZE;
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+        if constexpr (!PERM) {
+          const TensorDev t{k.at, DT, 0, 0, 0};
+          if (there && 32 * i + 8 * g < cols) raw[i] = st::fetch8<FULL, DT>(t, at, 32 * i + 8 * g, cols);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int n = 32 * i + 16 * (j >> 2) + 4 * g + (j & 3);
+            if (there && n < cols) {
+              const uint32_t v = DT == 0 ? ((const uint32_t*)k.at)[at + n] : (uint32_t)((const uint16_t*)k.at)[at + n] << 16;
+              if (j < 4) raw[i].a[j] = v;
+              else raw[i].b[j - 4] = v;
+            }
+          }
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void ops(Op<P> (&x)[STEPS]) const {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      if constexpr (P == 1 && FULL) x[i].p[0] = __builtin_bit_cast(bf16x8, raw[i].a);
+      else if constexpr (PERM && !FULL) x[i] = st::as_op<P>(st::expand8<false, 0>(raw[i], 0, 0, 8));
+      else x[i] = st::as_op<P>(st::expand8<FULL, DT>(raw[i], DT, 32 * i + 8 * g, cols));
+    }
+  }
+};
+
+// Numbers b0 + 16 j + 4 g .. of a wave's rows, results of either dtype.
+template <int TB, bool FULL>
+__device__ __forceinline__ void store_rows(int dtype, int pitch, const Chunk& k, int back, int b0, int wb, const f32x4 (&acc)[TB]) {
+  const int g = (threadIdx.x & 63) >> 4, row = 16 * wave_id() + (threadIdx.x & 15), b = b0 + 4 * g;
+  const int at = (back ? k.n - 1 - row : row) * pitch;
+  if constexpr (FULL) {
+    const __amdgpu_buffer_rsrc_t r = buffer_at(k.at);
+    const int first = at + b * (dtype == 0 ? 4 : 2);
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const int o = row < k.n && b + 16 * j < wb ? first : kNowhere;
+      if (dtype == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o, 64 * j, 0);
+      else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j], bf16x4)), r, o, 32 * j, 0);
+    }
+  } else if (row < k.n) {
+    const TensorDev t{k.at + at, dtype, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < TB; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (b + 16 * j + i < wb) store_elem(t, b + 16 * j + i, acc[j][i]);
+  }
+}
+
+// Zeros for the rows of a segment that lie behind the sequence.
+__device__ __forceinline__ void zero_rows(const TensorDev& Y, int b, int h, int heads, int from, int to, int b0, int cols) {
+  if (from >= to) return;
+  const int per = (to - from) * cols;
+  for (int i = 0; i < heads; ++i)
+    for (int id = threadIdx.x; id < per; id += 256) {
+      const int row = id / cols;
+      store_elem(Y, st::row_base(Y, b, h * heads + i, from + row) + b0 + id - row * cols, 0.f);
+    }
+}
 
 // Sixteen columns of rows 4 g .. 4 g + 3 of two tiles of sixteen rows (at s0 and s1).
 template <int P> __device__ __forceinline__ Op<P> columns(const uint16_t* s0, const uint16_t* s1, int plane) {
@@ -140,33 +309,33 @@ __device__ __forceinline__ void store_state(const StateTiles<W, TB>& S, const Ti
       }
 }
 
-// Weights of a chunk's n rows in the sums of a state: lambda^(n - j - first) of rows j = 32 q + 4 g + r and 32 q + 16 + 4 g + r.
-__device__ __forceinline__ void update_weights(f32x8 (&w)[2], const float* pw, int n, int first, float scale) {
-  const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int q = 0; q < 2; ++q)
-#pragma unroll
-    for (int r = 0; r < 8; ++r) w[q][r] = scale * pw[max(0, n - first - (32 * q + 16 * (r >> 2) + 4 * g + (r & 3)))];
+// Weights of a chunk's n rows in the sums of a state, lambda^(n - j - first) scale for row j, in LDS from the powers there.
+__device__ __forceinline__ void put_weights(float* uw, const float* pw, int n, int first, float scale) {
+  if (threadIdx.x < kChunk) uw[threadIdx.x] = scale * pw[max(0, n - first - (int)threadIdx.x)];
 }
-// S += sum over the chunk's rows of w a b'
-template <int P, int W, int TB>
-__device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, TB>& t, const uint16_t* sa, const uint16_t* sb, const f32x8 (&w)[2]) {
+// S += sum over the chunk's rows of w a b', w a as PU pieces
+template <int P, int PU, int W, int TB>
+__device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, TB>& t, const uint16_t* sa, const uint16_t* sb, const float* uw) {
   constexpr int LDA = W + 8, LDB = 16 * TB + 8, PA = kChunk * LDA, PB = kChunk * LDB, AT = Tiles<W, TB>::AT, BT = Tiles<W, TB>::BT;
   const int lane = threadIdx.x & 63;
   const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + st::lane_tr(lane, LDB);
+  const float* u = uw + 4 * (lane >> 4);
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    Op<3> a[AT];
+    phase();
+    const f32x4 w0 = *(const f32x4*)(u + 32 * q), w1 = *(const f32x4*)(u + 32 * q + 16);
+    const f32x8 w = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+    Op<PU> a[AT];
 #pragma unroll
     for (int i = 0; i < AT; ++i) {
       const uint16_t* p = la + 32 * q * LDA + 16 * (t.at + i);
-      a[i] = st::as_op<3>(number<P>(columns<P>(p, p + 16 * LDA, PA)) * w[q]);
+      a[i] = pieces<PU>(number<P>(columns<P>(p, p + 16 * LDA, PA)) * w);
     }
 #pragma unroll
     for (int j = 0; j < BT; ++j) {
       const uint16_t* p = lb + 32 * q * LDB + 16 * (t.bt + j);
       const Op<P> b = columns<P>(p, p + 16 * LDB, PB);
-      each_product<3, P>([&](int x, int y) {
+      each_product<PU, P>([&](int x, int y) {
 #pragma unroll
         for (int i = 0; i < AT; ++i) S[i][j] = st::mfma(a[i].p[x], b.p[y], S[i][j]);
       });
@@ -174,38 +343,106 @@ __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, T
   }
 }
 
+constexpr size_t kTables = (kChunk + 68) * 4;             // bytes of the weights and the powers
+template <int W, int TB> __device__ __forceinline__ void decay_state(StateTiles<W, TB>& S, Keep k) {
+#pragma unroll
+  for (int i = 0; i < Tiles<W, TB>::AT; ++i)
+#pragma unroll
+    for (int j = 0; j < Tiles<W, TB>::BT; ++j) {
+      if (k.near) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[i][j][r] = fmaf(S[i][j][r], k.part, S[i][j][r]);
+      } else {
+        S[i][j] *= k.part;
+      }
+    }
+}
+// Weights s lambda^(16 q + col - 4 g - r) of the scores of rows 4 g + r with the row col, q tiles of sixteen apart.
+__device__ __forceinline__ void score_weights(f32x4 (&near)[4], const float* pw, float s) {
+  const int g = (threadIdx.x & 63) >> 4, col = threadIdx.x & 15;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int n = 16 * q + col - 4 * g - r;
+      near[q][r] = n >= 0 ? s * pw[max(n, 0)] : 0.f;
+    }
+}
+// acc[j] += B' (weighed scores of the rows x with the rows A), both of a chunk of n rows in LDS; PERM: the order of x's numbers (RowOps).
+template <int P, int PM, int STEPS, int TB, bool PERM>
+__device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[STEPS], const uint16_t* sa, int LDA, const uint16_t* sb, int LDB,
+                                           const f32x4 (&near)[4], int n) {
+  const int wave = wave_id(), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, PA = kChunk * LDA, PB = kChunk * LDB;
+  // tiles of rows wave, wave - 1, ... two at a time
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int j0 = wave - 2 * q, j1 = max(j0 - 1, 0);
+    phase();
+    if (j0 < 0 || 16 * j0 >= n) continue;
+    f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      auto row = [&](int j) {
+        if constexpr (!PERM) {
+          return st::row_op<P>(sa + (16 * j + col) * LDA + 32 * k + 8 * g, PA);
+        } else {
+          Op<P> o;
+          const uint16_t* p = sa + (16 * j + col) * LDA + 32 * k + 4 * g;
+#pragma unroll
+          for (int i = 0; i < P; ++i) {
+            const u32x2 a = *(const u32x2*)(p + i * PA), b = *(const u32x2*)(p + i * PA + 16);
+            o.p[i] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+          }
+          return o;
+        }
+      };
+      const Op<P> o0 = row(j0), o1 = row(j1);
+      each_product<P, P>([&](int m, int y) {
+        sc[0] = st::mfma(o0.p[m], x[k].p[y], sc[0]);
+        sc[1] = st::mfma(o1.p[m], x[k].p[y], sc[1]);
+      });
+    }
+    f32x8 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      v[r] = q > 0 || col >= 4 * g + r ? sc[0][r] * near[2 * q][r] : 0.f;
+      v[4 + r] = j0 > 0 ? sc[1][r] * near[2 * q + 1][r] : 0.f;
+    }
+    const Op<PM> o = pieces<PM>(v);
+    const uint16_t* lb = sb + st::lane_tr(lane, LDB);
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const Op<P> bt = columns<P>(lb + 16 * j0 * LDB + 16 * j, lb + 16 * j1 * LDB + 16 * j, PB);
+      each_product<P, PM>([&](int m, int y) { acc[j] = st::mfma(bt.p[m], o.p[y], acc[j]); });
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ rows
-template <int P, int PM, int W, int TB, bool FULL, int DT>
-__global__ void __launch_bounds__(256) k_decay_walk(WalkSet set, int ncb) {
+// Waves to a SIMD: what LDS allows, or registers without spills.
+constexpr int walk_waves(int P, int W) { return P == 1 ? (W <= 64 ? 3 : 2) : (W <= 64 ? 2 : 1); }
+template <int P, int PM, int PU, int W, int TB, bool FULL, int DT>
+__global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet set, int ncb) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = kChunk * LDA, PB = kChunk * LDB;
   constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA, *img = sb + P * PB;
-  float* pw = (float*)(img + TB * IMG);                       // lambda^0 .. lambda^64
+  float *uw = (float*)(img + TB * IMG), *pw = uw + kChunk;    // weights of the chunk's rows; lambda^0 .. lambda^64
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
   if (!place(c, c.nseg, ncb, &p)) return;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = 64 * p.cb;
+  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = 64 * p.cb;
   if (b0 >= w.wb) return;
   if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
   const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows);
-  // rows behind the sequence
-  const int pad0 = max(lo, p.len), pad1 = p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows);
-  if (pad0 < pad1) {
-    const int nb = min(64, w.wb - b0), per = (pad1 - pad0) * nb;
-    for (int gx = 0; gx < w.GX; ++gx)
-      for (int id = tid; id < per; id += 256) {
-        const int row = id / nb;
-        store_elem(w.Y, st::row_base(w.Y, p.b, p.h * w.GX + gx, pad0 + row) + b0 + id - row * nb, 0.f);
-      }
-  }
+  zero_rows(w.Y, p.b, p.h, w.GX, max(lo, p.len), p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows), b0, min(64, w.wb - b0));
   const int s = p.b * c.Hk + p.h;
   const bool ends = w.end != nullptr && c.nseg == 1 && (p.slot >= 0 || !w.end_pool);
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
-  const Keep whole = keep_of(ld, kChunk);
+  const Keep whole = scalar(keep_of(ld, kChunk));
   const Tiles<W, TB> t(wave);
   StateTiles<W, TB> S;
   // (with segments the pool may hold the states after the call already)
@@ -214,18 +451,23 @@ __global__ void __launch_bounds__(256) k_decay_walk(WalkSet set, int ncb) {
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<W, TB>(S, t, from, w.sa, w.sb, w.wa, w.wb, b0);
   bool filled = from != nullptr;
+  const int back = w.back, GX = w.GX, GA = w.GA, wb = w.wb;
+  const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
+  Stage<P, W, FULL, DT> ra(ha, 0, w.wa, back);
+  Stage<P, NB, FULL, DT> rb(hb, b0, wb, back);
+  RowOps<P, STEPS, FULL, DT> rx(hx, w.wa, back);
+  auto fetch_x = [&](int r0, int gx) { rx.fetch(hx.chunk(gx, r0, min(kChunk, hi - r0), p.len, back)); };
+  auto fetch_rows = [&](int r0, int ga) {
+    const int n = min(kChunk, hi - r0);
+    ra.fetch(ha.chunk(ga, r0, n, p.len, back));
+    rb.fetch(hb.chunk(ga, r0, n, p.len, back));
+  };
+  if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo, 0); }
   __syncthreads();
   f32x4 near[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = 16 * q + col - 4 * g - r;
-      near[q][r] = n >= 0 ? w.s_score * pw[max(n, 0)] : 0.f;
-    }
+  score_weights(near, pw, w.s_score);
   const float inter = w.s_inter * pw[16 * wave + col + w.first];
-  f32x8 uw[2];
-  update_weights(uw, pw, kChunk, w.first, w.s_update);
+  put_weights(uw, pw, kChunk, w.first, w.s_update);
 
   auto put_image = [&]() {
 #pragma unroll
@@ -237,53 +479,29 @@ __global__ void __launch_bounds__(256) k_decay_walk(WalkSet set, int ncb) {
         f32x4 x = S[i][j];
 #pragma unroll
         for (int k = 0; k < PM; ++k) {
-          typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
           const bf16x4 h = __builtin_convertvector(x, bf16x4);
           *(bf16x4*)(to + k * 512) = h;
           x -= __builtin_convertvector(h, f32x4);
         }
       }
   };
-
-  Stage<P, W, FULL, DT> ra;
-  Stage<P, NB, FULL, DT> rb;
-  Raw8 rx[STEPS];
-  auto fetch_x = [&](int r0, int gx) {
-    const int row = r0 + 16 * wave + col;
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      const int c0 = 32 * k + 8 * g;
-      rx[k] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-      if (row < hi && c0 < w.wa)
-        rx[k] = st::fetch8<FULL, DT>(w.X, st::row_base(w.X, p.b, p.h * w.GX + gx, w.back ? p.len - 1 - row : row), c0, w.wa);
-    }
-  };
-  auto fetch_rows = [&](int r0, int ga) {
-    const int n = min(kChunk, hi - r0);
-    ra.fetch(w.A, p.b, p.h * w.GA + ga, r0, n, p.len, w.back, 0, w.wa);
-    rb.fetch(w.B, p.b, p.h * w.GA + ga, r0, n, p.len, w.back, b0, w.wb);
-  };
-  if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo, 0); }
   if (filled) put_image();
   Op<P> x[STEPS];
   f32x4 acc[TB];
   for (int r0 = lo; r0 < hi; r0 += kChunk) {
     const int n = min(kChunk, hi - r0);
-    const bool more = r0 + kChunk < hi, update = more || ends;
-    for (int ga = 0; ga < w.GA; ++ga) {
-      ra.store(sa, 0, w.wa);
-      rb.store(sb, b0, w.wb);
+    const bool more = r0 + kChunk < hi;
+    if (n < kChunk) put_weights(uw, pw, n, w.first, w.s_update);
+    for (int ga = 0; ga < GA; ++ga) {
+      ra.store(sa, 0);
+      rb.store(sb, b0);
       __syncthreads();
-      if (ga + 1 < w.GA) fetch_rows(r0, ga + 1);
+      if (ga + 1 < GA) fetch_rows(r0, ga + 1);
       else if (more) fetch_rows(r0 + kChunk, 0);
-      for (int gx = 0; gx < w.GX; ++gx) {
+      for (int gx = 0; gx < GX; ++gx) {
         if (ga == 0) {
-#pragma unroll
-          for (int k = 0; k < STEPS; ++k) {
-            if constexpr (P == 1 && FULL) x[k].p[0] = __builtin_bit_cast(bf16x8, rx[k].a);
-            else x[k] = st::as_op<P>(st::expand8<FULL, DT>(rx[k], DT, 32 * k + 8 * g, w.wa));
-          }
-          if (gx + 1 < w.GX) fetch_x(r0, gx + 1);
+          rx.ops(x);
+          if (gx + 1 < GX) fetch_x(r0, gx + 1);
           else if (more) fetch_x(r0 + kChunk, 0);
 #pragma unroll
           for (int j = 0; j < TB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -299,68 +517,12 @@ __global__ void __launch_bounds__(256) k_decay_walk(WalkSet set, int ncb) {
             for (int j = 0; j < TB; ++j) acc[j] *= inter;
           }
         }
-        // scores with the tiles of rows wave, wave - 1, ... two at a time
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int j0 = wave - 2 * q, j1 = max(j0 - 1, 0);
-          if (j0 < 0 || 16 * j0 >= n) continue;
-          f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-          for (int k = 0; k < STEPS; ++k) {
-            const Op<P> o0 = st::row_op<P>(sa + (16 * j0 + col) * LDA + 32 * k + 8 * g, PA);
-            const Op<P> o1 = st::row_op<P>(sa + (16 * j1 + col) * LDA + 32 * k + 8 * g, PA);
-            each_product<P, P>([&](int m, int y) {
-              sc[0] = st::mfma(o0.p[m], x[k].p[y], sc[0]);
-              sc[1] = st::mfma(o1.p[m], x[k].p[y], sc[1]);
-            });
-          }
-          f32x8 v;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            v[r] = q > 0 || col >= 4 * g + r ? sc[0][r] * near[2 * q][r] : 0.f;
-            v[4 + r] = j0 > 0 ? sc[1][r] * near[2 * q + 1][r] : 0.f;
-          }
-          const Op<PM> o = pieces<PM>(v);
-          const uint16_t* lb = sb + st::lane_tr(lane, LDB);
-#pragma unroll
-          for (int j = 0; j < TB; ++j) {
-            const Op<P> bt = columns<P>(lb + 16 * j0 * LDB + 16 * j, lb + 16 * j1 * LDB + 16 * j, PB);
-            each_product<P, PM>([&](int m, int y) { acc[j] = st::mfma(bt.p[m], o.p[y], acc[j]); });
-          }
-        }
-        const int row = r0 + 16 * wave + col;
-        if (ga == w.GA - 1 && row < hi) {
-          const long long to = st::row_base(w.Y, p.b, p.h * w.GX + gx, w.back ? p.len - 1 - row : row);
-#pragma unroll
-          for (int j = 0; j < TB; ++j) {
-            const int b = b0 + 16 * j + 4 * g;
-            if (FULL ? b < w.wb : b + 4 <= w.wb) {
-              if (w.Y.dtype == 0) {
-                *(f32x4*)((float*)w.Y.ptr + to + b) = acc[j];
-              } else {
-                typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-                *(bf16x4*)((uint16_t*)w.Y.ptr + to + b) = __builtin_convertvector(acc[j], bf16x4);
-              }
-            } else if (!FULL) {
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (b + r < w.wb) store_elem(w.Y, to + b + r, acc[j][r]);
-            }
-          }
-        }
+        add_scores<P, PM, STEPS, TB, false>(acc, x, sa, LDA, sb, LDB, near, n);
+        if (ga == GA - 1) store_rows<TB, FULL>(w.Y.dtype, hy.pitch, hy.chunk(gx, r0, n, p.len, back), back, b0, wb, acc);
       }
-      if (update) {
-        if (n < kChunk) update_weights(uw, pw, n, w.first, w.s_update);
-        if (ga == 0) {
-          const Keep keep = n < kChunk ? keep_of(ld, n) : whole;
-#pragma unroll
-          for (int i = 0; i < Tiles<W, TB>::AT; ++i)
-#pragma unroll
-            for (int j = 0; j < Tiles<W, TB>::BT; ++j)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) S[i][j][r] = kept(keep, S[i][j][r]);
-        }
-        add_chunk<P, W, TB>(S, t, sa, sb, uw);
+      if (more || ends) {
+        if (ga == 0) decay_state<W, TB>(S, n < kChunk ? scalar(keep_of(ld, n)) : whole);
+        add_chunk<P, PU, W, TB>(S, t, sa, sb, uw);
       }
       __syncthreads();
     }
@@ -370,13 +532,134 @@ __global__ void __launch_bounds__(256) k_decay_walk(WalkSet set, int ncb) {
     store_state<W, TB>(S, t, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, b0);
 }
 
+// Gradients of keys and values in one walk from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
+// dy behind, in LDS as rows of D', of which the one takes columns and the other rows.  set.w[0]: the values (X = V, A = dY, B = Q, Y = dK),
+// set.w[1]: the keys (X = K, A = Q, B = dY, Y = dV).
+template <int P, int PM, int PU, int W, bool FULL, int DT>
+__global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set) {
+  constexpr int TB = W / 16, STEPS = W / 32, LD = W + 8, PL = kChunk * LD, PI = W * LD;
+  extern __shared__ char lds[];
+  uint16_t *sq = (uint16_t*)lds, *sd = sq + P * PL, *img = sd + P * PL;
+  float *uw = (float*)(img + PM * PI), *pw = uw + kChunk;
+  const Call& c = set.c;
+  const Walk &wk = set.w[0], &wv = set.w[1];
+  Place p;
+  if (!place(c, c.nseg, 1, &p)) return;
+  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15;
+  const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows), pad = p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows);
+  zero_rows(wk.Y, p.b, p.h, 1, max(lo, p.len), pad, 0, wk.wb);
+  zero_rows(wv.Y, p.b, p.h, 1, max(lo, p.len), pad, 0, wv.wb);
+  const int s = p.b * c.Hk + p.h, G = wv.GA;
+  const bool ends = wv.end != nullptr && c.nseg == 1 && (p.slot >= 0 || !wv.end_pool);
+  if (hi <= lo && !ends) return;
+  const float ld = c.log_decay[p.h];
+  for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
+  const Keep whole = scalar(keep_of(ld, kChunk));
+  const Tiles<W, TB> t(wave);
+  StateTiles<W, TB> S;
+  const float* from = wv.init == nullptr && p.seg == 0 ? nullptr
+                      : c.nseg > 1                     ? set.prefix[1] + ((size_t)s * c.nseg + p.seg) * c.state
+                                                       : (p.slot >= 0 ? wv.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
+  load_state<W, TB>(S, t, from, wv.sa, wv.sb, wv.wa, wv.wb, 0);
+  bool filled = from != nullptr;
+  const Head hq(wv.A, p.b, p.h * G), hd(wv.B, p.b, p.h * G), hk(wv.X, p.b, p.h), hv(wk.X, p.b, p.h), hdk(wk.Y, p.b, p.h), hdv(wv.Y, p.b, p.h);
+  Stage<P, W, FULL, DT> rq(hq, 0, wv.wa, 1), rd(hd, 0, wv.wb, 1);
+  RowOps<P, STEPS, FULL, DT> rk(hk, wv.wa, 1);
+  RowOps<P, STEPS, FULL, DT, true> rv(hv, wk.wa, 1);
+  auto fetch_x = [&](int r0) {
+    const int n = min(kChunk, hi - r0);
+    rk.fetch(hk.chunk(0, r0, n, p.len, 1));
+    rv.fetch(hv.chunk(0, r0, n, p.len, 1));
+  };
+  auto fetch_rows = [&](int r0, int ga) {
+    const int n = min(kChunk, hi - r0);
+    rq.fetch(hq.chunk(ga, r0, n, p.len, 1));
+    rd.fetch(hd.chunk(ga, r0, n, p.len, 1));
+  };
+  if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo); }
+  __syncthreads();
+  f32x4 near[4];
+  score_weights(near, pw, wv.s_score);
+  const float inter = pw[16 * wave + col];
+  put_weights(uw, pw, kChunk, 0, wv.s_update);
+  auto put_image = [&]() {
+#pragma unroll
+    for (int i = 0; i < Tiles<W, TB>::AT; ++i)
+#pragma unroll
+      for (int j = 0; j < Tiles<W, TB>::BT; ++j) {
+        uint16_t* to = img + (16 * (t.bt + j) + col) * LD + 16 * (t.at + i) + 4 * g;
+        f32x4 x = S[i][j];
+#pragma unroll
+        for (int k = 0; k < PM; ++k) {
+          const bf16x4 h = __builtin_convertvector(x, bf16x4);
+          *(bf16x4*)(to + k * PI) = h;
+          x -= __builtin_convertvector(h, f32x4);
+        }
+      }
+  };
+  if (filled) put_image();
+  Op<P> xk[STEPS], xv[STEPS];
+  f32x4 dk[TB], dv[TB];
+  for (int r0 = lo; r0 < hi; r0 += kChunk) {
+    const int n = min(kChunk, hi - r0);
+    const bool more = r0 + kChunk < hi;
+    if (n < kChunk) put_weights(uw, pw, n, 0, wv.s_update);
+    for (int ga = 0; ga < G; ++ga) {
+      rq.store(sq, 0);
+      rd.store(sd, 0);
+      __syncthreads();
+      if (ga + 1 < G) fetch_rows(r0, ga + 1);
+      else if (more) fetch_rows(r0 + kChunk, 0);
+      if (ga == 0) {
+        rk.ops(xk);
+        rv.ops(xv);
+        if (more) fetch_x(r0 + kChunk);
+#pragma unroll
+        for (int j = 0; j < TB; ++j) dk[j] = dv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (filled) {
+          const uint16_t* li = img + st::lane_tr(lane, LD);
+#pragma unroll
+          for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) {
+              const Op<PM> o = st::row_op<PM>(img + (16 * j + col) * LD + 32 * k + 8 * g, PI);
+              each_product<PM, P>([&](int m, int y) { dv[j] = st::mfma(o.p[m], xk[k].p[y], dv[j]); });
+              const uint16_t* q = li + 32 * k * LD + 16 * j;
+              const Op<PM> u = columns<PM>(q, q + 16 * LD, PI);
+              each_product<PM, P>([&](int m, int y) { dk[j] = st::mfma(u.p[m], xv[k].p[y], dk[j]); });
+            }
+#pragma unroll
+          for (int j = 0; j < TB; ++j) {
+            dk[j] *= inter;
+            dv[j] *= inter;
+          }
+        }
+      }
+      add_scores<P, PM, STEPS, TB, true>(dk, xv, sd, LD, sq, LD, near, n);
+      add_scores<P, PM, STEPS, TB, false>(dv, xk, sq, LD, sd, LD, near, n);
+      if (ga == G - 1) {
+        store_rows<TB, FULL>(wk.Y.dtype, hdk.pitch, hdk.chunk(0, r0, n, p.len, 1), 1, 0, wk.wb, dk);
+        store_rows<TB, FULL>(wv.Y.dtype, hdv.pitch, hdv.chunk(0, r0, n, p.len, 1), 1, 0, wv.wb, dv);
+      }
+      if (more || ends) {
+        if (ga == 0) decay_state<W, TB>(S, n < kChunk ? scalar(keep_of(ld, n)) : whole);
+        add_chunk<P, PU, W, TB>(S, t, sq, sd, uw);
+      }
+      __syncthreads();
+    }
+    if (more) { put_image(); filled = true; }
+  }
+  if (ends)
+    store_state<W, TB>(S, t, wv.end + (wv.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, wv.sa, wv.sb, wv.wa, wv.wb, 0);
+}
+
 // ------------------------------------------------------------------------------------------------ sums of segments
 template <int P, int W, int TB, bool FULL, int DT>
 __global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
   constexpr int NB = 16 * TB, PA = kChunk * (W + 8), PB = kChunk * (NB + 8);
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA;
-  float* pw = (float*)(sb + P * PB);
+  float *uw = (float*)(sb + P * PB), *pw = uw + kChunk;
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
@@ -387,40 +670,32 @@ __global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
   if (hi <= lo || b0 >= w.wb) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
-  const Keep whole = keep_of(ld, kChunk);
-  const Tiles<W, TB> t(tid >> 6);
+  const Keep whole = scalar(keep_of(ld, kChunk));
+  const Tiles<W, TB> t(wave_id());
   StateTiles<W, TB> S;
   load_state<W, TB>(S, t, nullptr, 0, 0, 0, 0, 0);
-  __syncthreads();
-  f32x8 uw[2];
-  update_weights(uw, pw, kChunk, w.first, w.s_update);
-  Stage<P, W, FULL, DT> ra;
-  Stage<P, NB, FULL, DT> rb;
+  const Head ha(w.A, p.b, p.h * w.GA), hb(w.B, p.b, p.h * w.GA);
+  Stage<P, W, FULL, DT> ra(ha, 0, w.wa, w.back);
+  Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, w.back);
   auto fetch_rows = [&](int r0, int ga) {
     const int n = min(kChunk, hi - r0);
-    ra.fetch(w.A, p.b, p.h * w.GA + ga, r0, n, p.len, w.back, 0, w.wa);
-    rb.fetch(w.B, p.b, p.h * w.GA + ga, r0, n, p.len, w.back, b0, w.wb);
+    ra.fetch(ha.chunk(ga, r0, n, p.len, w.back));
+    rb.fetch(hb.chunk(ga, r0, n, p.len, w.back));
   };
   fetch_rows(lo, 0);
+  __syncthreads();
+  put_weights(uw, pw, kChunk, w.first, w.s_update);
   for (int r0 = lo; r0 < hi; r0 += kChunk) {
     const int n = min(kChunk, hi - r0);
-    if (n < kChunk) update_weights(uw, pw, n, w.first, w.s_update);
+    if (n < kChunk) put_weights(uw, pw, n, w.first, w.s_update);
     for (int ga = 0; ga < w.GA; ++ga) {
-      ra.store(sa, 0, w.wa);
-      rb.store(sb, b0, w.wb);
+      ra.store(sa, 0);
+      rb.store(sb, b0);
       __syncthreads();
       if (ga + 1 < w.GA) fetch_rows(r0, ga + 1);
       else if (r0 + kChunk < hi) fetch_rows(r0 + kChunk, 0);
-      if (ga == 0 && r0 > lo) {
-        const Keep keep = n < kChunk ? keep_of(ld, n) : whole;
-#pragma unroll
-        for (int i = 0; i < Tiles<W, TB>::AT; ++i)
-#pragma unroll
-          for (int j = 0; j < Tiles<W, TB>::BT; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[i][j][r] = kept(keep, S[i][j][r]);
-      }
-      add_chunk<P, W, TB>(S, t, sa, sb, uw);
+      if (ga == 0 && r0 > lo) decay_state<W, TB>(S, n < kChunk ? scalar(keep_of(ld, n)) : whole);
+      add_chunk<P, 3, W, TB>(S, t, sa, sb, uw);
       __syncthreads();
     }
   }
@@ -470,7 +745,7 @@ __global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
 // The readers of a slot are found once for 1024 numbers of its states, in the order of the sequences.
 __global__ void __launch_bounds__(256) k_decay_slot_sums(Call c, const float* each, float* pool) {
   __shared__ int list[256], count[4];
-  const int slot = blockIdx.y / c.Hk, h = blockIdx.y - slot * c.Hk, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int slot = blockIdx.y / c.Hk, h = blockIdx.y - slot * c.Hk, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   const int id = blockIdx.x * 1024 + tid;
   bool found = false;
@@ -511,22 +786,31 @@ template <class K> int room(K kernel, size_t bytes) {
   return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? 0 : 5;
 }
 
-template <int P, int PM, int W, int TB, bool FULL, int DT>
+template <int P, int PM, int PU, int W, int TB, bool FULL, int DT>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
-  const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + (size_t)TB * (W / 32) * PM * 1024 + 68 * 4;
-  if (int rc = room(k_decay_walk<P, PM, W, TB, FULL, DT>, lds)) return rc;
+  const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + (size_t)TB * (W / 32) * PM * 1024 + kTables;
+  if (int rc = room(k_decay_walk<P, PM, PU, W, TB, FULL, DT>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_walk<P, PM, W, TB, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
+  hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
+  return status();
+}
+template <int P, int PM, int PU, int W, bool FULL, int DT>
+int back_launch(const WalkSet& a, hipStream_t st) {
+  const size_t lds = (size_t)P * kChunk * (W + 8) * 4 + (size_t)PM * W * (W + 8) * 2 + kTables;
+  if (int rc = room(k_decay_back<P, PM, PU, W, FULL, DT>, lds)) return rc;
+  const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
+  if (units > 0x7fffffffLL) return 2;
+  hipLaunchKernelGGL((k_decay_back<P, PM, PU, W, FULL, DT>), dim3((unsigned)units), dim3(256), lds, st, a);
   return status();
 }
 template <int P, int W, int TB, bool FULL, int DT>
 int sum_launch(const SumSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
-  const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + 68 * 4;
+  const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + kTables;
   if (int rc = room(k_decay_sum<P, W, TB, FULL, DT>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * (a.last ? a.c.nseg : a.c.nseg - 1) + 7) / 8 * 8;
   if (units == 0) return 0;
@@ -537,10 +821,13 @@ int sum_launch(const SumSet& a, int count, hipStream_t st) {
 
 int class_of(int n) { return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
-template <int P, int PM, bool FULL, int DT> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
-  if (class_of(wa) == 128) return walk_launch<P, PM, 128, 4, FULL, DT>(a, count, st);
-  if (class_of(wa) == 64) return walk_launch<P, PM, 64, 4, FULL, DT>(a, count, st);
-  return wb <= 32 ? walk_launch<P, PM, 32, 2, FULL, DT>(a, count, st) : walk_launch<P, PM, 32, 4, FULL, DT>(a, count, st);
+template <int P, int PM, int PU, bool FULL, int DT> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
+  if (class_of(wa) == 128) return walk_launch<P, PM, PU, 128, 4, FULL, DT>(a, count, st);
+  if (class_of(wa) == 64) return walk_launch<P, PM, PU, 64, 4, FULL, DT>(a, count, st);
+  return wb <= 32 ? walk_launch<P, PM, PU, 32, 2, FULL, DT>(a, count, st) : walk_launch<P, PM, PU, 32, 4, FULL, DT>(a, count, st);
+}
+template <int P, int PM, int PU, bool FULL, int DT> int back_width(const WalkSet& a, int w, hipStream_t st) {
+  return w <= 32 ? back_launch<P, PM, PU, 32, FULL, DT>(a, st) : back_launch<P, PM, PU, 64, FULL, DT>(a, st);
 }
 template <int P, bool FULL, int DT> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
   if (class_of(wa) == 128) return sum_launch<P, 128, 4, FULL, DT>(a, count, st);
@@ -554,17 +841,41 @@ template <int P, bool FULL, int DT> int sum_width(const SumSet& a, int count, in
 int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, hipStream_t st) {
   WalkSet a = all;
   int wa = 0, wb = 0;
-  bool full = true;
+  bool full = true, ends = false;
   for (int i = 0; i < count; ++i) {
     a.w[i] = all.w[from + i];
+    ends = ends || (a.w[i].end != nullptr && a.c.nseg == 1);
     a.prefix[i] = all.prefix[from + i];
     wa = max(wa, a.w[i].wa);
     wb = max(wb, a.w[i].wb);
     full = full && a.w[i].wa % 8 == 0 && a.w[i].wb % 8 == 0;
   }
-  if (dtype == 0) return full ? walk_width<3, 3, true, 0>(a, count, wa, wb, st) : walk_width<3, 3, false, 0>(a, count, wa, wb, st);
-  if (fine) return full ? walk_width<1, 3, true, 1>(a, count, wa, wb, st) : walk_width<1, 3, false, 1>(a, count, wa, wb, st);
-  return full ? walk_width<1, 2, true, 1>(a, count, wa, wb, st) : walk_width<1, 2, false, 1>(a, count, wa, wb, st);
+  auto go = [&](auto full_rows) {
+    constexpr bool F = decltype(full_rows)::value;
+    if (dtype == 0) return walk_width<3, 3, 3, F, 0>(a, count, wa, wb, st);
+    if (fine) return walk_width<1, 3, 3, F, 1>(a, count, wa, wb, st);
+    return ends ? walk_width<1, 2, 3, F, 1>(a, count, wa, wb, st) : walk_width<1, 2, 2, F, 1>(a, count, wa, wb, st);
+  };
+  return full ? go(std::true_type{}) : go(std::false_type{});
+}
+
+// The walks of dK and dV (from, from + 1) as one.
+int launch_back(const WalkSet& all, int from, int dtype, bool fine, hipStream_t st) {
+  WalkSet a = all;
+  for (int i = 0; i < 2; ++i) {
+    a.w[i] = all.w[from + i];
+    a.prefix[i] = all.prefix[from + i];
+  }
+  const Walk& w = a.w[1];
+  const int n = max(w.wa, w.wb);
+  const bool ends = w.end != nullptr && a.c.nseg == 1;
+  auto go = [&](auto full_rows) {
+    constexpr bool F = decltype(full_rows)::value;
+    if (dtype == 0) return back_width<3, 3, 3, F, 0>(a, n, st);
+    if (fine) return back_width<1, 3, 3, F, 1>(a, n, st);
+    return ends ? back_width<1, 2, 3, F, 1>(a, n, st) : back_width<1, 2, 2, F, 1>(a, n, st);
+  };
+  return w.wa % 8 == 0 && w.wb % 8 == 0 ? go(std::true_type{}) : go(std::false_type{});
 }
 
 int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st) {
