@@ -476,7 +476,7 @@ int favorsharp_state_append_backward(const fs_features* host_features, const fs_
  *   rounded once, to their dtype.  Numbers below 2^-109 lose bits, as the rest of a number has no exponent there.
  *   log_decay and scale are constants: there is no gradient with respect to them.
  *   d, dv <= 128 (the columns of V and S are independent of each other: wider values are calls on parts of them), B H and
- *   slots * heads <= 65535, L H / heads <= 2^29, stride_l <= 2^23 of tensors of rows.  Q, K, V and dY of a call share a dtype.
+ *   slots * heads <= 65535, L H / heads <= 2^29, stride_l <= 2^22 of tensors of rows.  Q, K, V and dY of a call share a dtype.
  * Calls that write a state must be ordered with all others on it by the caller.  Asynchronous.  Where a *_workspace_bytes query
  * answers 0 the workspace may be NULL (a query for sizes that are refused answers 0, too).
  */

@@ -22,7 +22,7 @@ Plan plan(int B, int heads, int L, int d, int dv, int blocks, int sets, bool end
   Plan p;
   const int chunks = ceil_div(std::max(L, 1), dec::kChunk);
   const long long units = (long long)B * heads * blocks, target = 768;
-  const long long nseg = std::max<long long>(1, std::min<long long>((target + units - 1) / units, chunks / 4));
+  const long long nseg = units >= 512 ? 1 : std::max<long long>(1, std::min<long long>((target + units - 1) / units, chunks / 4));
   const int each = ceil_div(chunks, (int)nseg);
   p.nseg = ceil_div(chunks, each);
   p.seg_rows = each * dec::kChunk;
@@ -42,7 +42,7 @@ int sizes(int B, int H, int heads, int L, int d, int dv) {
   return FS_OK;
 }
 // offsets within a chunk of rows have 32 bits
-constexpr int64_t kMaxStride = 1 << 23;
+constexpr int64_t kMaxStride = 1 << 22;
 bool strides_ok(std::initializer_list<const fs_tensor*> list, int L) {
   for (const fs_tensor* t : list)
     if (L > 1 && t->stride_l > kMaxStride) return false;

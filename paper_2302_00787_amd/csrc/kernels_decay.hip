@@ -24,14 +24,27 @@ __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane
 __device__ __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 __device__ __forceinline__ Keep scalar(Keep k) { return {scalar(k.part), __builtin_amdgcn_readfirstlane((int)k.near) != 0}; }
 
+__device__ __forceinline__ void scale_by(f32x4& v, float f) {       // (one register for the factor, where v *= f takes four)
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] *= f;
+}
+
 // Operands of a part of a chunk are not fetched before the part: that would take registers that hold more waves otherwise.
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int P> __device__ __forceinline__ Op<P> pieces(f32x8 x) {
-  if constexpr (P == 2) {
+  if constexpr (P == 2) {          // (numbers that are summed: one that is not finite makes its neighbour NaN)
+    u32x4 h, m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x2_t v = {x[2 * i], x[2 * i + 1]};
+      const bf16x2_t top = __builtin_convertvector(v, bf16x2_t);
+      h[i] = __builtin_bit_cast(uint32_t, top);
+      m[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(less_piece(v, top), bf16x2_t));
+    }
     Op<2> o;
-    o.p[0] = __builtin_convertvector(x, bf16x8);
-    o.p[1] = __builtin_convertvector(x - __builtin_convertvector(o.p[0], f32x8), bf16x8);
+    o.p[0] = __builtin_bit_cast(bf16x8, h);
+    o.p[1] = __builtin_bit_cast(bf16x8, m);
     return o;
   } else {
     return st::as_op<P>(x);
@@ -67,12 +80,18 @@ __device__ __forceinline__ bool place(const Call& c, int nseg, int ncb, Place* p
   return true;
 }
 
-// Rows of a chunk of one head: `at` is the chunk's lowest row in memory, row i of the n that are there at i pitch (back: (n - 1 - i) pitch)
-// bytes.
+// A chunk's n rows of one head: `at` is their lowest in memory, row i at i pitch (back: (n - 1 - i) pitch) bytes.
 struct Chunk {
   const char* at;
-  int n;
+  int n, pitch, back;
+  // offset of row i where there are kChunk rows -> the present one; rows from n on get offsets that are out of the buffer
+  __device__ __forceinline__ int shift() const { return back ? (kChunk - n) * pitch : 0; }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, n * pitch, 0x00027000);
+  }
 };
+// Offsets from here on, and those less a shift, are out of every buffer: reads give zeros, writes nothing.  (kChunk pitches are at most 2^30.)
+constexpr int kNowhere = (int)0x80000000u;
 // A head's rows (of `heads` consecutive ones), and a chunk's of them.
 struct Head {
   const char* at;
@@ -85,14 +104,9 @@ struct Head {
     pitch = (int)t.sl * size;
   }
   __device__ __forceinline__ Chunk chunk(int i, int r0, int n, int len, int back) const {
-    return {at + i * next + (long long)(back ? len - r0 - n : r0) * pitch, n};
+    return {at + i * next + (long long)(back ? len - r0 - n : r0) * pitch, n, pitch, back};
   }
 };
-// A buffer over what lies from a pointer on; an offset of kNowhere reads zeros and writes nothing.
-constexpr int kNowhere = (int)0x80000000u;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
-}
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
 // From memory to LDS as P bf16 pieces: 256 threads, units of eight numbers.  FULL: rows have no ragged end, and units are loads whose
@@ -100,49 +114,38 @@ typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 template <int P, int W, bool FULL, int DT> struct Stage {
   static constexpr int UNITS = W / 8, N = kChunk * UNITS / 256, LD = W + 8, PLANE = kChunk * LD, SIZE = DT == 0 ? 4 : 2;
   Raw8 raw[N];
-  int off[FULL ? N : 1];
-  int row0, c, cols, back, pitch;
+  int off[N], c, cols;
   // numbers c0 .. c0 + W - 1 of the rows
-  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int backwards) : cols(ncols), back(backwards), pitch(h.pitch) {
-    row0 = threadIdx.x / UNITS;
+  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int back) : cols(ncols) {
     c = c0 + 8 * (threadIdx.x % UNITS);
-    if constexpr (FULL) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) off[i] = offset(i, kChunk);
+    for (int i = 0; i < N; ++i) {
+      const int row = (threadIdx.x + 256 * i) / UNITS;
+      off[i] = c < cols ? (back ? kChunk - 1 - row : row) * h.pitch + c * SIZE : kNowhere;
     }
   }
-  __device__ __forceinline__ int offset(int i, int n) const {
-    const int row = row0 + 256 / UNITS * i;
-    return row < n && c < cols ? (back ? n - 1 - row : row) * pitch + c * SIZE : kNowhere;
-  }
   __device__ __forceinline__ void fetch(const Chunk& k) {
+    const int shift = k.shift();
     if constexpr (FULL) {
-      const __amdgpu_buffer_rsrc_t r = buffer_at(k.at);
-      auto load = [&](int i, int o) {
-        raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
-        if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
-      };
-      if (k.n == kChunk) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) load(i, off[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) load(i, offset(i, k.n));
-      }
-    } else {
-      const TensorDev t{k.at, DT, 0, 0, 0};
+      const __amdgpu_buffer_rsrc_t r = k.buffer();
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int row = row0 + 256 / UNITS * i;
+        raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, off[i] - shift, 0, 0);
+        if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, off[i] - shift, 16, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-        if (row < k.n && c < cols) raw[i] = st::fetch8<FULL, DT>(t, (long long)(back ? k.n - 1 - row : row) * (pitch / SIZE), c, cols);
+        if (c < cols && (unsigned)(off[i] - shift) < (unsigned)(k.n * k.pitch))
+          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (off[i] - shift - c * SIZE), DT, 0, 0, 0}, 0, c, cols);
       }
     }
   }
   __device__ __forceinline__ void store(uint16_t* s, int c0) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      uint16_t* to = s + (row0 + 256 / UNITS * i) * LD + (c - c0);
+      uint16_t* to = s + (threadIdx.x + 256 * i) / UNITS * LD + (c - c0);
       if constexpr (P == 1 && FULL) {
         *(u32x4*)to = raw[i].a;
       } else {
@@ -164,49 +167,51 @@ template <int P, int W, bool FULL, int DT> struct Stage {
 // A wave's sixteen rows as operands: a lane has eight numbers 32 k + 8 g .. of row 16 wave + (lane % 16) for each step k, or (PERM) numbers
 // 32 k + 4 g .. and 32 k + 16 + 4 g .., the order in which two stacked accumulators hold theirs.
 template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps {
-  static constexpr int SIZE = DT == 0 ? 4 : 2;
+  static constexpr int SIZE = DT == 0 ? 4 : 2, PARTS = PERM ? 2 : 1;
   Raw8 raw[STEPS];
-  int row, cols, back, pitch;
-  __device__ __forceinline__ RowOps(const Head& h, int ncols, int backwards) : cols(ncols), back(backwards), pitch(h.pitch) {
-    row = 16 * wave_id() + (threadIdx.x & 15);
+  int row, off[STEPS][PARTS], cols;
+  __device__ __forceinline__ RowOps(const Head& h, int ncols, int back) : cols(ncols) {
+    const int g = (threadIdx.x & 63) >> 4, i = 16 * wave_id() + (threadIdx.x & 15);
+    row = (back ? kChunk - 1 - i : i) * h.pitch;
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        const int c = 32 * k + (PERM ? 16 * j + 4 * g : 8 * g);
+        off[k][j] = c < cols ? row + c * SIZE : kNowhere;
+      }
   }
   __device__ __forceinline__ void fetch(const Chunk& k) {
-    const int g = (threadIdx.x & 63) >> 4;
-    const bool there = row < k.n;
-    const int first = (back ? k.n - 1 - row : row) * pitch;
+    const int g = (threadIdx.x & 63) >> 4, shift = k.shift();
     if constexpr (FULL) {
-      const __amdgpu_buffer_rsrc_t r = buffer_at(k.at);
+      const __amdgpu_buffer_rsrc_t r = k.buffer();
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         if constexpr (!PERM) {
-          const int o = there && 32 * i + 8 * g < cols ? first + 8 * g * SIZE : kNowhere;
-          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 32 * i * SIZE, 0);
-          if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 32 * i * SIZE + 16, 0);
+          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][0] - shift, 0, 0);
+          if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][0] - shift, 16, 0);
+        } else if constexpr (DT == 0) {
+          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][0] - shift, 0, 0);
+          raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][PARTS - 1] - shift, 0, 0);
         } else {
-          const int o = there && 32 * i + 4 * g < cols ? first + 4 * g * SIZE : kNowhere, p = there && 32 * i + 16 + 4 * g < cols ? first + 4 * g * SIZE : kNowhere;
-          if constexpr (DT == 0) {
-            raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 32 * i * SIZE, 0);
-            raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, p, (32 * i + 16) * SIZE, 0);
-          } else {
-            const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, o, 32 * i * SIZE, 0), y = __builtin_amdgcn_raw_buffer_load_b64(r, p, (32 * i + 16) * SIZE, 0);
-            raw[i].a = u32x4{x[0], x[1], y[0], y[1]};
-          }
+          const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off[i][0] - shift, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(r, off[i][PARTS - 1] - shift, 0, 0);
+          raw[i].a = u32x4{x[0], x[1], y[0], y[1]};
         }
       }
     } else {
-      const long long at = first / SIZE;
+      const bool there = (unsigned)(row - shift) < (unsigned)(k.n * k.pitch);
+      const TensorDev t{k.at + (there ? row - shift : 0), DT, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
         if constexpr (!PERM) {
-          const TensorDev t{k.at, DT, 0, 0, 0};
-          if (there && 32 * i + 8 * g < cols) raw[i] = st::fetch8<FULL, DT>(t, at, 32 * i + 8 * g, cols);
+          if (there && 32 * i + 8 * g < cols) raw[i] = st::fetch8<FULL, DT>(t, 0, 32 * i + 8 * g, cols);
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int n = 32 * i + 16 * (j >> 2) + 4 * g + (j & 3);
             if (there && n < cols) {
-              const uint32_t v = DT == 0 ? ((const uint32_t*)k.at)[at + n] : (uint32_t)((const uint16_t*)k.at)[at + n] << 16;
+              const uint32_t v = __float_as_uint(load_elem(t, n));
               if (j < 4) raw[i].a[j] = v;
               else raw[i].b[j - 4] = v;
             }
@@ -226,29 +231,35 @@ template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps 
   }
 };
 
-// Numbers b0 + 16 j + 4 g .. of a wave's rows, results of either dtype.
-template <int TB, bool FULL>
-__device__ __forceinline__ void store_rows(int dtype, int pitch, const Chunk& k, int back, int b0, int wb, const f32x4 (&acc)[TB]) {
-  const int g = (threadIdx.x & 63) >> 4, row = 16 * wave_id() + (threadIdx.x & 15), b = b0 + 4 * g;
-  const int at = (back ? k.n - 1 - row : row) * pitch;
-  if constexpr (FULL) {
-    const __amdgpu_buffer_rsrc_t r = buffer_at(k.at);
-    const int first = at + b * (dtype == 0 ? 4 : 2);
-#pragma unroll
-    for (int j = 0; j < TB; ++j) {
-      const int o = row < k.n && b + 16 * j < wb ? first : kNowhere;
-      if (dtype == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o, 64 * j, 0);
-      else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j], bf16x4)), r, o, 32 * j, 0);
-    }
-  } else if (row < k.n) {
-    const TensorDev t{k.at + at, dtype, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < TB; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (b + 16 * j + i < wb) store_elem(t, b + 16 * j + i, acc[j][i]);
+// Numbers b0 + 16 j + 4 g .. of a wave's rows to a result; OUT: its dtype where the kernel knows it (-1: it does not).
+template <int TB, bool FULL, int OUT> struct RowStore {
+  int row, b, wb, size;
+  __device__ __forceinline__ RowStore(const Head& h, int dtype, int b0, int width, int back) : wb(width), size((OUT < 0 ? dtype : OUT) == 0 ? 4 : 2) {
+    const int i = 16 * wave_id() + (threadIdx.x & 15);
+    b = b0 + 4 * ((threadIdx.x & 63) >> 4);
+    row = (back ? kChunk - 1 - i : i) * h.pitch;
   }
-}
+  __device__ __forceinline__ void put(const Chunk& k, const f32x4 (&acc)[TB]) const {
+    const int first = row - k.shift();
+    if constexpr (FULL) {
+      const __amdgpu_buffer_rsrc_t r = k.buffer();
+      const int at = first + b * size;
+#pragma unroll
+      for (int j = 0; j < TB; ++j) {
+        const int o = b + 16 * j < wb ? at : kNowhere;
+        if (OUT == 0 || (OUT < 0 && size == 4)) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o + 64 * j, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j], bf16x4)), r, o + 32 * j, 0, 0);
+      }
+    } else if ((unsigned)first < (unsigned)(k.n * k.pitch)) {
+      const TensorDev t{k.at + first, size == 4 ? 0 : 1, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < TB; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (b + 16 * j + i < wb) store_elem(t, b + 16 * j + i, acc[j][i]);
+    }
+  }
+};
 
 // Zeros for the rows of a segment that lie behind the sequence.
 __device__ __forceinline__ void zero_rows(const TensorDev& Y, int b, int h, int heads, int from, int to, int b0, int cols) {
@@ -331,15 +342,18 @@ __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, T
       const uint16_t* p = la + 32 * q * LDA + 16 * (t.at + i);
       a[i] = pieces<PU>(number<P>(columns<P>(p, p + 16 * LDA, PA)) * w);
     }
+    Op<P> b[BT];
 #pragma unroll
     for (int j = 0; j < BT; ++j) {
       const uint16_t* p = lb + 32 * q * LDB + 16 * (t.bt + j);
-      const Op<P> b = columns<P>(p, p + 16 * LDB, PB);
-      each_product<PU, P>([&](int x, int y) {
-#pragma unroll
-        for (int i = 0; i < AT; ++i) S[i][j] = st::mfma(a[i].p[x], b.p[y], S[i][j]);
-      });
+      b[j] = columns<P>(p, p + 16 * LDB, PB);
     }
+    each_product<PU, P>([&](int x, int y) {
+#pragma unroll
+      for (int j = 0; j < BT; ++j)
+#pragma unroll
+        for (int i = 0; i < AT; ++i) S[i][j] = st::mfma(a[i].p[x], b[j].p[y], S[i][j]);
+    });
   }
 }
 
@@ -353,7 +367,7 @@ template <int W, int TB> __device__ __forceinline__ void decay_state(StateTiles<
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[i][j][r] = fmaf(S[i][j][r], k.part, S[i][j][r]);
       } else {
-        S[i][j] *= k.part;
+        scale_by(S[i][j], k.part);
       }
     }
 }
@@ -371,14 +385,14 @@ __device__ __forceinline__ void score_weights(f32x4 (&near)[4], const float* pw,
 // acc[j] += B' (weighed scores of the rows x with the rows A), both of a chunk of n rows in LDS; PERM: the order of x's numbers (RowOps).
 template <int P, int PM, int STEPS, int TB, bool PERM>
 __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[STEPS], const uint16_t* sa, int LDA, const uint16_t* sb, int LDB,
-                                           const f32x4 (&near)[4], int n) {
+                                           const f32x4 (&near)[4]) {
   const int wave = wave_id(), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, PA = kChunk * LDA, PB = kChunk * LDB;
   // tiles of rows wave, wave - 1, ... two at a time
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int j0 = wave - 2 * q, j1 = max(j0 - 1, 0);
     phase();
-    if (j0 < 0 || 16 * j0 >= n) continue;
+    if (j0 < 0) continue;
     f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
@@ -408,13 +422,15 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
       v[r] = q > 0 || col >= 4 * g + r ? sc[0][r] * near[2 * q][r] : 0.f;
       v[4 + r] = j0 > 0 ? sc[1][r] * near[2 * q + 1][r] : 0.f;
     }
-    const Op<PM> o = pieces<PM>(v);
     const uint16_t* lb = sb + st::lane_tr(lane, LDB);
+    Op<P> bt[TB];
 #pragma unroll
-    for (int j = 0; j < TB; ++j) {
-      const Op<P> bt = columns<P>(lb + 16 * j0 * LDB + 16 * j, lb + 16 * j1 * LDB + 16 * j, PB);
-      each_product<P, PM>([&](int m, int y) { acc[j] = st::mfma(bt.p[m], o.p[y], acc[j]); });
-    }
+    for (int j = 0; j < TB; ++j) bt[j] = columns<P>(lb + 16 * j0 * LDB + 16 * j, lb + 16 * j1 * LDB + 16 * j, PB);
+    const Op<PM> o = pieces<PM>(v);
+    each_product<P, PM>([&](int m, int y) {
+#pragma unroll
+      for (int j = 0; j < TB; ++j) acc[j] = st::mfma(bt[j].p[m], o.p[y], acc[j]);
+    });
   }
 }
 
@@ -424,6 +440,7 @@ constexpr int walk_waves(int P, int W) { return P == 1 ? (W <= 64 ? 3 : 2) : (W 
 template <int P, int PM, int PU, int W, int TB, bool FULL, int DT>
 __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet set, int ncb) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = kChunk * LDA, PB = kChunk * LDB;
+  constexpr int OUT = P == 1 && PM == 2 ? 1 : -1;             // (two pieces are for results in bf16)
   constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA, *img = sb + P * PB;
@@ -442,7 +459,7 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
-  const Keep whole = scalar(keep_of(ld, kChunk));
+  Keep keep = scalar(keep_of(ld, kChunk));
   const Tiles<W, TB> t(wave);
   StateTiles<W, TB> S;
   // (with segments the pool may hold the states after the call already)
@@ -450,12 +467,13 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<W, TB>(S, t, from, w.sa, w.sb, w.wa, w.wb, b0);
-  bool filled = from != nullptr;
-  const int back = w.back, GX = w.GX, GA = w.GA, wb = w.wb;
+  const int back = w.back, GX = w.GX, GA = w.GA, first = w.first;
+  const float s_update = w.s_update;
   const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
   Stage<P, W, FULL, DT> ra(ha, 0, w.wa, back);
-  Stage<P, NB, FULL, DT> rb(hb, b0, wb, back);
+  Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, back);
   RowOps<P, STEPS, FULL, DT> rx(hx, w.wa, back);
+  const RowStore<TB, FULL, OUT> ry(hy, w.Y.dtype, b0, w.wb, back);
   auto fetch_x = [&](int r0, int gx) { rx.fetch(hx.chunk(gx, r0, min(kChunk, hi - r0), p.len, back)); };
   auto fetch_rows = [&](int r0, int ga) {
     const int n = min(kChunk, hi - r0);
@@ -466,8 +484,8 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
   __syncthreads();
   f32x4 near[4];
   score_weights(near, pw, w.s_score);
-  const float inter = w.s_inter * pw[16 * wave + col + w.first];
-  put_weights(uw, pw, kChunk, w.first, w.s_update);
+  const float inter = w.s_inter * pw[16 * wave + col + first];
+  put_weights(uw, pw, kChunk, first, s_update);
 
   auto put_image = [&]() {
 #pragma unroll
@@ -485,13 +503,17 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
         }
       }
   };
-  if (filled) put_image();
+  put_image();
   Op<P> x[STEPS];
   f32x4 acc[TB];
   for (int r0 = lo; r0 < hi; r0 += kChunk) {
-    const int n = min(kChunk, hi - r0);
+    int n = min(kChunk, hi - r0);
     const bool more = r0 + kChunk < hi;
-    if (n < kChunk) put_weights(uw, pw, n, w.first, w.s_update);
+    if (n < kChunk && ends) {
+      asm("" : "+s"(n));                                      // (or powers for it would be found for every chunk)
+      put_weights(uw, pw, n, first, s_update);
+      keep = scalar(keep_of(ld, n));
+    }
     for (int ga = 0; ga < GA; ++ga) {
       ra.store(sa, 0);
       rb.store(sb, b0);
@@ -505,28 +527,29 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
           else if (more) fetch_x(r0 + kChunk, 0);
 #pragma unroll
           for (int j = 0; j < TB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (filled) {
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k)
+          for (int k = 0; k < STEPS; ++k) {
+            Op<PM> o[TB];
 #pragma unroll
-              for (int j = 0; j < TB; ++j) {
-                const Op<PM> o = st::image_op<PM>(img + j * IMG + k * PM * 512, lane);
-                each_product<PM, P>([&](int m, int y) { acc[j] = st::mfma(o.p[m], x[k].p[y], acc[j]); });
-              }
+            for (int j = 0; j < TB; ++j) o[j] = st::image_op<PM>(img + j * IMG + k * PM * 512, lane);
+            each_product<PM, P>([&](int m, int y) {
 #pragma unroll
-            for (int j = 0; j < TB; ++j) acc[j] *= inter;
+              for (int j = 0; j < TB; ++j) acc[j] = st::mfma(o[j].p[m], x[k].p[y], acc[j]);
+            });
           }
+#pragma unroll
+          for (int j = 0; j < TB; ++j) scale_by(acc[j], inter);
         }
-        add_scores<P, PM, STEPS, TB, false>(acc, x, sa, LDA, sb, LDB, near, n);
-        if (ga == GA - 1) store_rows<TB, FULL>(w.Y.dtype, hy.pitch, hy.chunk(gx, r0, n, p.len, back), back, b0, wb, acc);
+        add_scores<P, PM, STEPS, TB, false>(acc, x, sa, LDA, sb, LDB, near);
+        if (ga == GA - 1) ry.put(hy.chunk(gx, r0, n, p.len, back), acc);
       }
       if (more || ends) {
-        if (ga == 0) decay_state<W, TB>(S, n < kChunk ? scalar(keep_of(ld, n)) : whole);
+        if (ga == 0) decay_state<W, TB>(S, keep);
         add_chunk<P, PU, W, TB>(S, t, sa, sb, uw);
       }
       __syncthreads();
     }
-    if (more) { put_image(); filled = true; }
+    if (more) put_image();
   }
   if (ends)
     store_state<W, TB>(S, t, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, b0);
@@ -537,7 +560,7 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
 // set.w[1]: the keys (X = K, A = Q, B = dY, Y = dV).
 template <int P, int PM, int PU, int W, bool FULL, int DT>
 __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set) {
-  constexpr int TB = W / 16, STEPS = W / 32, LD = W + 8, PL = kChunk * LD, PI = W * LD;
+  constexpr int TB = W / 16, STEPS = W / 32, LD = W + 8, PL = kChunk * LD, PI = W * LD, OUT = P == 1 && PM == 2 ? 1 : -1;
   extern __shared__ char lds[];
   uint16_t *sq = (uint16_t*)lds, *sd = sq + P * PL, *img = sd + P * PL;
   float *uw = (float*)(img + PM * PI), *pw = uw + kChunk;
@@ -554,18 +577,19 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
-  const Keep whole = scalar(keep_of(ld, kChunk));
+  Keep keep = scalar(keep_of(ld, kChunk));
   const Tiles<W, TB> t(wave);
   StateTiles<W, TB> S;
   const float* from = wv.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                     ? set.prefix[1] + ((size_t)s * c.nseg + p.seg) * c.state
                                                        : (p.slot >= 0 ? wv.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<W, TB>(S, t, from, wv.sa, wv.sb, wv.wa, wv.wb, 0);
-  bool filled = from != nullptr;
   const Head hq(wv.A, p.b, p.h * G), hd(wv.B, p.b, p.h * G), hk(wv.X, p.b, p.h), hv(wk.X, p.b, p.h), hdk(wk.Y, p.b, p.h), hdv(wv.Y, p.b, p.h);
   Stage<P, W, FULL, DT> rq(hq, 0, wv.wa, 1), rd(hd, 0, wv.wb, 1);
   RowOps<P, STEPS, FULL, DT> rk(hk, wv.wa, 1);
   RowOps<P, STEPS, FULL, DT, true> rv(hv, wk.wa, 1);
+  const RowStore<TB, FULL, OUT> to_k(hdk, wk.Y.dtype, 0, wk.wb, 1), to_v(hdv, wv.Y.dtype, 0, wv.wb, 1);
+  const float s_update = wv.s_update;
   auto fetch_x = [&](int r0) {
     const int n = min(kChunk, hi - r0);
     rk.fetch(hk.chunk(0, r0, n, p.len, 1));
@@ -581,7 +605,7 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
   f32x4 near[4];
   score_weights(near, pw, wv.s_score);
   const float inter = pw[16 * wave + col];
-  put_weights(uw, pw, kChunk, 0, wv.s_update);
+  put_weights(uw, pw, kChunk, 0, s_update);
   auto put_image = [&]() {
 #pragma unroll
     for (int i = 0; i < Tiles<W, TB>::AT; ++i)
@@ -597,13 +621,18 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
         }
       }
   };
-  if (filled) put_image();
+  put_image();
   Op<P> xk[STEPS], xv[STEPS];
   f32x4 dk[TB], dv[TB];
+  const uint16_t *rows = img + col * LD + 8 * g, *cols = img + st::lane_tr(lane, LD);
   for (int r0 = lo; r0 < hi; r0 += kChunk) {
-    const int n = min(kChunk, hi - r0);
+    int n = min(kChunk, hi - r0);
     const bool more = r0 + kChunk < hi;
-    if (n < kChunk) put_weights(uw, pw, n, 0, wv.s_update);
+    if (n < kChunk && ends) {
+      asm("" : "+s"(n));
+      put_weights(uw, pw, n, 0, s_update);
+      keep = scalar(keep_of(ld, n));
+    }
     for (int ga = 0; ga < G; ++ga) {
       rq.store(sq, 0);
       rd.store(sd, 0);
@@ -616,38 +645,43 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
         if (more) fetch_x(r0 + kChunk);
 #pragma unroll
         for (int j = 0; j < TB; ++j) dk[j] = dv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (filled) {
-          const uint16_t* li = img + st::lane_tr(lane, LD);
 #pragma unroll
-          for (int k = 0; k < STEPS; ++k)
+        for (int k = 0; k < STEPS; ++k) {
+          phase();
+          Op<PM> o[TB];
 #pragma unroll
-            for (int j = 0; j < TB; ++j) {
-              const Op<PM> o = st::row_op<PM>(img + (16 * j + col) * LD + 32 * k + 8 * g, PI);
-              each_product<PM, P>([&](int m, int y) { dv[j] = st::mfma(o.p[m], xk[k].p[y], dv[j]); });
-              const uint16_t* q = li + 32 * k * LD + 16 * j;
-              const Op<PM> u = columns<PM>(q, q + 16 * LD, PI);
-              each_product<PM, P>([&](int m, int y) { dk[j] = st::mfma(u.p[m], xv[k].p[y], dk[j]); });
-            }
+          for (int j = 0; j < TB; ++j) o[j] = st::row_op<PM>(rows + 16 * j * LD + 32 * k, PI);
+          each_product<PM, P>([&](int m, int y) {
 #pragma unroll
-          for (int j = 0; j < TB; ++j) {
-            dk[j] *= inter;
-            dv[j] *= inter;
-          }
+            for (int j = 0; j < TB; ++j) dv[j] = st::mfma(o[j].p[m], xk[k].p[y], dv[j]);
+          });
+          phase();
+#pragma unroll
+          for (int j = 0; j < TB; ++j) o[j] = columns<PM>(cols + 32 * k * LD + 16 * j, cols + (32 * k + 16) * LD + 16 * j, PI);
+          each_product<PM, P>([&](int m, int y) {
+#pragma unroll
+            for (int j = 0; j < TB; ++j) dk[j] = st::mfma(o[j].p[m], xv[k].p[y], dk[j]);
+          });
+        }
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+          scale_by(dk[j], inter);
+          scale_by(dv[j], inter);
         }
       }
-      add_scores<P, PM, STEPS, TB, true>(dk, xv, sd, LD, sq, LD, near, n);
-      add_scores<P, PM, STEPS, TB, false>(dv, xk, sq, LD, sd, LD, near, n);
+      add_scores<P, PM, STEPS, TB, true>(dk, xv, sd, LD, sq, LD, near);
+      add_scores<P, PM, STEPS, TB, false>(dv, xk, sq, LD, sd, LD, near);
       if (ga == G - 1) {
-        store_rows<TB, FULL>(wk.Y.dtype, hdk.pitch, hdk.chunk(0, r0, n, p.len, 1), 1, 0, wk.wb, dk);
-        store_rows<TB, FULL>(wv.Y.dtype, hdv.pitch, hdv.chunk(0, r0, n, p.len, 1), 1, 0, wv.wb, dv);
+        to_k.put(hdk.chunk(0, r0, n, p.len, 1), dk);
+        to_v.put(hdv.chunk(0, r0, n, p.len, 1), dv);
       }
       if (more || ends) {
-        if (ga == 0) decay_state<W, TB>(S, n < kChunk ? scalar(keep_of(ld, n)) : whole);
+        if (ga == 0) decay_state<W, TB>(S, keep);
         add_chunk<P, PU, W, TB>(S, t, sq, sd, uw);
       }
       __syncthreads();
     }
-    if (more) { put_image(); filled = true; }
+    if (more) put_image();
   }
   if (ends)
     store_state<W, TB>(S, t, wv.end + (wv.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, wv.sa, wv.sb, wv.wa, wv.wb, 0);
@@ -670,7 +704,7 @@ __global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
   if (hi <= lo || b0 >= w.wb) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
-  const Keep whole = scalar(keep_of(ld, kChunk));
+  Keep keep = scalar(keep_of(ld, kChunk));
   const Tiles<W, TB> t(wave_id());
   StateTiles<W, TB> S;
   load_state<W, TB>(S, t, nullptr, 0, 0, 0, 0, 0);
@@ -686,15 +720,19 @@ __global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
   __syncthreads();
   put_weights(uw, pw, kChunk, w.first, w.s_update);
   for (int r0 = lo; r0 < hi; r0 += kChunk) {
-    const int n = min(kChunk, hi - r0);
-    if (n < kChunk) put_weights(uw, pw, n, w.first, w.s_update);
+    int n = min(kChunk, hi - r0);
+    if (n < kChunk) {
+      asm("" : "+s"(n));
+      put_weights(uw, pw, n, w.first, w.s_update);
+      keep = scalar(keep_of(ld, n));
+    }
     for (int ga = 0; ga < w.GA; ++ga) {
       ra.store(sa, 0);
       rb.store(sb, b0);
       __syncthreads();
       if (ga + 1 < w.GA) fetch_rows(r0, ga + 1);
       else if (r0 + kChunk < hi) fetch_rows(r0 + kChunk, 0);
-      if (ga == 0 && r0 > lo) decay_state<W, TB>(S, n < kChunk ? scalar(keep_of(ld, n)) : whole);
+      if (ga == 0 && r0 > lo) decay_state<W, TB>(S, keep);
       add_chunk<P, 3, W, TB>(S, t, sa, sb, uw);
       __syncthreads();
     }
@@ -742,13 +780,16 @@ __global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
     set.end[which][(set.end_pool[which] ? (size_t)slot * c.Hk + h : (size_t)s) * c.state + id] = S;
 }
 
-// The readers of a slot are found once for 1024 numbers of its states, in the order of the sequences.
+// Sums of the readers of a slot, for 64 numbers of its states a workgroup: its sixteen groups of sixteen lanes take every sixteenth
+// reader each, in their order, and are then added in theirs.
 __global__ void __launch_bounds__(256) k_decay_slot_sums(Call c, const float* each, float* pool) {
   __shared__ int list[256], count[4];
-  const int slot = blockIdx.y / c.Hk, h = blockIdx.y - slot * c.Hk, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  __shared__ float part[16][64];
+  const int slot = blockIdx.y / c.Hk, h = blockIdx.y - slot * c.Hk, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, group = tid >> 4;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  const int id = blockIdx.x * 1024 + tid;
+  const int id = blockIdx.x * 64 + 4 * (tid & 15);
   bool found = false;
+  int before_all = 0;
   for (int b0 = 0; b0 < c.B; b0 += 256) {
     const int b = b0 + tid;
     const bool reads = b < c.B && st::slot_of(c.slots, c.nslots, b) == slot;
@@ -763,19 +804,24 @@ __global__ void __launch_bounds__(256) k_decay_slot_sums(Call c, const float* ea
     if (reads) list[before] = b;
     __syncthreads();
     if (c.unique) total = found ? 0 : min(total, 1);          // the first sequence of a slot alone had it
-    for (int i = 0; i < total; ++i) {
-      const float* from = each + ((size_t)list[i] * c.Hk + h) * c.state;
+    for (int i = (group - before_all) & 15; i < total; i += 16) {
+      const float* from = each + ((size_t)list[i] * c.Hk + h) * c.state + id;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (id + 256 * k < c.state) sum[k] += from[id + 256 * k];
+        if (id + k < c.state) sum[k] += from[k];
     }
+    before_all += total;
     found = found || total > 0;
     __syncthreads();
   }
-  float* to = pool + ((size_t)slot * c.Hk + h) * c.state;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (id + 256 * k < c.state) to[id + 256 * k] = sum[k];
+  for (int k = 0; k < 4; ++k) part[group][4 * (tid & 15) + k] = sum[k];
+  __syncthreads();
+  if (tid < 64 && blockIdx.x * 64 + tid < c.state) {
+    float t = 0.f;
+    for (int i = 0; i < 16; ++i) t += part[i][tid];
+    pool[((size_t)slot * c.Hk + h) * c.state + blockIdx.x * 64 + tid] = t;
+  }
 }
 
 int status() { return hipGetLastError() == hipSuccess ? 0 : 5; }
@@ -896,7 +942,7 @@ int launch_join(const JoinSet& a, hipStream_t st) {
 }
 
 int launch_slot_sums(const Call& c, const float* each, float* pool, hipStream_t st) {
-  hipLaunchKernelGGL(k_decay_slot_sums, dim3((c.state + 1023) / 1024, c.nslots * c.Hk), dim3(256), 0, st, c, each, pool);
+  hipLaunchKernelGGL(k_decay_slot_sums, dim3((c.state + 63) / 64, c.nslots * c.Hk), dim3(256), 0, st, c, each, pool);
   return status();
 }
 
