@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <stdlib.h>
 
 #include "api_common.h"
 #include "decay_common.h"
@@ -21,7 +22,7 @@ struct Plan {
 Plan plan(int B, int heads, int L, int d, int dv, int blocks, int sets, bool ends) {
   Plan p;
   const int chunks = ceil_div(std::max(L, 1), dec::kChunk);
-  const long long units = (long long)B * heads * blocks, target = 768;
+  const long long units = (long long)B * heads * blocks, target = getenv("TARGET") ? atoi(getenv("TARGET")) : 768;
   const long long nseg = units >= 512 ? 1 : std::max<long long>(1, std::min<long long>((target + units - 1) / units, chunks / 4));
   const int each = ceil_div(chunks, (int)nseg);
   p.nseg = ceil_div(chunks, each);

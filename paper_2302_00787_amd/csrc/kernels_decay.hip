@@ -8,6 +8,7 @@
 // of a in the sums of the state are weighed in 32 bits and have three pieces, as the states themselves are results in fp32.
 #include "decay_common.h"
 
+#include <stdlib.h>
 #include <type_traits>
 
 namespace fs {
@@ -27,6 +28,17 @@ __device__ __forceinline__ Keep scalar(Keep k) { return {scalar(k.part), __built
 __device__ __forceinline__ void scale_by(f32x4& v, float f) {       // (one register for the factor, where v *= f takes four)
 #pragma unroll
   for (int r = 0; r < 4; ++r) v[r] *= f;
+}
+
+// A value that the compiler has to take as it finds it in every turn: what follows from it is worked out there and not kept in registers, or
+// in memory, for all turns.
+__device__ __forceinline__ int afresh(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+__device__ __forceinline__ int afresh_lane(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // Operands of a part of a chunk are not fetched before the part: that would take registers that hold more waves otherwise.
@@ -60,13 +72,15 @@ template <int P> __device__ __forceinline__ f32x8 number(const Op<P>& o) {
 struct Place { int b, h, seg, cb, slot, len; };
 // Units of a grid: (sequence, key head, segment), their column blocks eight workgroups apart, on one XCD.  slot -2: left out.
 __device__ __forceinline__ bool place(const Call& c, int nseg, int ncb, Place* p) {
-  const int x = blockIdx.x, q = x / (8 * ncb), rest = x - q * 8 * ncb;
-  p->cb = rest / 8;
+  // (quotients come from vector instructions: in scalars again, so that addresses are)
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int x = blockIdx.x, q = uniform(x / (8 * ncb)), rest = x - q * 8 * ncb;
+  p->cb = rest >> 3;
   const long long u = (long long)q * 8 + (rest & 7);
   if (u >= (long long)c.B * c.Hk * nseg) return false;
-  p->seg = (int)(u % nseg);
-  const int s = (int)(u / nseg);
-  p->b = s / c.Hk;
+  const int s = uniform((int)u / nseg);                       // (the grid has fewer than 2^31 workgroups)
+  p->seg = (int)u - s * nseg;
+  p->b = uniform(s / c.Hk);
   p->h = s - p->b * c.Hk;
   int len = c.lengths ? max(0, min(c.lengths[p->b], c.L)) : c.L, slot;
   if (c.unique) {
@@ -75,20 +89,24 @@ __device__ __forceinline__ bool place(const Call& c, int nseg, int ncb, Place* p
   } else {
     slot = st::slot_of(c.slots, c.nslots, p->b);
   }
-  p->len = __builtin_amdgcn_readfirstlane(len);          // (the same in all lanes; addresses are to be scalar)
-  p->slot = __builtin_amdgcn_readfirstlane(slot);
+  p->len = uniform(len);
+  p->slot = uniform(slot);
   return true;
 }
 
+// A buffer of `bytes` from p on.  (In scalars whatever way they came: a buffer in vector registers is a loop over the lanes at each load.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int bytes) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
+}
 // A chunk's n rows of one head: `at` is their lowest in memory, row i at i pitch (back: (n - 1 - i) pitch) bytes.
 struct Chunk {
   const char* at;
   int n, pitch, back;
-  // offset of row i where there are kChunk rows -> the present one; rows from n on get offsets that are out of the buffer
-  __device__ __forceinline__ int shift() const { return back ? (kChunk - n) * pitch : 0; }
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, n * pitch, 0x00027000);
-  }
+  // offset of row i where there are `rows` of them -> the present one; rows from n on get offsets that are out of the buffer
+  __device__ __forceinline__ int shift(int rows = kChunk) const { return back ? (rows - n) * pitch : 0; }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const { return buffer_of(at, n * pitch); }
 };
 // Offsets from here on, and those less a shift, are out of every buffer: reads give zeros, writes nothing.  (kChunk pitches are at most 2^30.)
 constexpr int kNowhere = (int)0x80000000u;
@@ -109,43 +127,46 @@ struct Head {
 };
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
-// From memory to LDS as P bf16 pieces: 256 threads, units of eight numbers.  FULL: rows have no ragged end, and units are loads whose
+// From memory to LDS as P bf16 pieces: T threads, units of eight numbers.  FULL: rows have no ragged end, and units are loads whose
 // offsets from the chunk's first row stay; else number by number at the ends.
-template <int P, int W, bool FULL, int DT> struct Stage {
-  static constexpr int UNITS = W / 8, N = kChunk * UNITS / 256, LD = W + 8, PLANE = kChunk * LD, SIZE = DT == 0 ? 4 : 2;
+template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struct Stage {
+  static constexpr int UNITS = W / 8, N = (ROWS * UNITS + T - 1) / T, LD = W + 8, PLANE = ROWS * LD, SIZE = DT == 0 ? 4 : 2;
+  static constexpr bool EVEN = ROWS * UNITS % T == 0;        // (else the last threads have no unit)
   Raw8 raw[N];
-  int off[N], c, cols;
+  int off, step, c, cols;        // offset of the first unit, and from one to the next
   // numbers c0 .. c0 + W - 1 of the rows
   __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int back) : cols(ncols) {
     c = c0 + 8 * (threadIdx.x % UNITS);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int row = (threadIdx.x + 256 * i) / UNITS;
-      off[i] = c < cols ? (back ? kChunk - 1 - row : row) * h.pitch + c * SIZE : kNowhere;
-    }
+    const int row = threadIdx.x / UNITS;
+    off = c < cols && (EVEN || row < ROWS) ? (back ? ROWS - 1 - row : row) * h.pitch + c * SIZE : kNowhere;
+    step = (back ? -T / UNITS : T / UNITS) * h.pitch;
   }
   __device__ __forceinline__ void fetch(const Chunk& k) {
-    const int shift = k.shift();
+    const int shift = k.shift(ROWS);
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
+      const int first = afresh_lane(off - shift);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, off[i] - shift, 0, 0);
-        if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, off[i] - shift, 16, 0);
+        const int o = first + i * step;
+        raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
+        if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
+        const int o = off + (i * step - shift);
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-        if (c < cols && (unsigned)(off[i] - shift) < (unsigned)(k.n * k.pitch))
-          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (off[i] - shift - c * SIZE), DT, 0, 0, 0}, 0, c, cols);
+        if (c < cols && (unsigned)o < (unsigned)(k.n * k.pitch))
+          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (o - c * SIZE), DT, 0, 0, 0}, 0, c, cols);
       }
     }
   }
   __device__ __forceinline__ void store(uint16_t* s, int c0) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      uint16_t* to = s + (threadIdx.x + 256 * i) / UNITS * LD + (c - c0);
+      if (!EVEN && threadIdx.x + T * i >= ROWS * UNITS) break;
+      uint16_t* to = s + (threadIdx.x + T * i) / UNITS * LD + (c - c0);
       if constexpr (P == 1 && FULL) {
         *(u32x4*)to = raw[i].a;
       } else {
@@ -167,34 +188,28 @@ template <int P, int W, bool FULL, int DT> struct Stage {
 // A wave's sixteen rows as operands: a lane has eight numbers 32 k + 8 g .. of row 16 wave + (lane % 16) for each step k, or (PERM) numbers
 // 32 k + 4 g .. and 32 k + 16 + 4 g .., the order in which two stacked accumulators hold theirs.
 template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps {
-  static constexpr int SIZE = DT == 0 ? 4 : 2, PARTS = PERM ? 2 : 1;
+  static constexpr int SIZE = DT == 0 ? 4 : 2;
   Raw8 raw[STEPS];
-  int row, off[STEPS][PARTS], cols;
+  int row, cols;
   __device__ __forceinline__ RowOps(const Head& h, int ncols, int back) : cols(ncols) {
-    const int g = (threadIdx.x & 63) >> 4, i = 16 * wave_id() + (threadIdx.x & 15);
+    const int i = 16 * wave_id() + (threadIdx.x & 15);
     row = (back ? kChunk - 1 - i : i) * h.pitch;
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k)
-#pragma unroll
-      for (int j = 0; j < PARTS; ++j) {
-        const int c = 32 * k + (PERM ? 16 * j + 4 * g : 8 * g);
-        off[k][j] = c < cols ? row + c * SIZE : kNowhere;
-      }
   }
   __device__ __forceinline__ void fetch(const Chunk& k) {
     const int g = (threadIdx.x & 63) >> 4, shift = k.shift();
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
+      const int first = afresh_lane(row - shift + (PERM ? 4 : 8) * g * SIZE);
+      auto at = [&](int c, int more) { return (PERM ? 4 : 8) * g + c < cols ? first + c * SIZE + more : kNowhere; };
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
-        if constexpr (!PERM) {
-          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][0] - shift, 0, 0);
-          if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][0] - shift, 16, 0);
-        } else if constexpr (DT == 0) {
-          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][0] - shift, 0, 0);
-          raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, off[i][PARTS - 1] - shift, 0, 0);
+        if constexpr (DT == 0) {
+          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, at(32 * i, 0), 0, 0);
+          raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, PERM ? at(32 * i + 16, 0) : at(32 * i, 16), 0, 0);
+        } else if constexpr (!PERM) {
+          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, at(32 * i, 0), 0, 0);
         } else {
-          const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off[i][0] - shift, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(r, off[i][PARTS - 1] - shift, 0, 0);
+          const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, at(32 * i, 0), 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(r, at(32 * i + 16, 0), 0, 0);
           raw[i].a = u32x4{x[0], x[1], y[0], y[1]};
         }
       }
@@ -240,7 +255,7 @@ template <int TB, bool FULL, int OUT> struct RowStore {
     row = (back ? kChunk - 1 - i : i) * h.pitch;
   }
   __device__ __forceinline__ void put(const Chunk& k, const f32x4 (&acc)[TB]) const {
-    const int first = row - k.shift();
+    const int first = afresh_lane(row - k.shift());
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
       const int at = first + b * size;
@@ -266,7 +281,7 @@ __device__ __forceinline__ void zero_rows(const TensorDev& Y, int b, int h, int 
   if (from >= to) return;
   const int per = (to - from) * cols;
   for (int i = 0; i < heads; ++i)
-    for (int id = threadIdx.x; id < per; id += 256) {
+    for (int id = threadIdx.x; id < per; id += blockDim.x) {
       const int row = id / cols;
       store_elem(Y, st::row_base(Y, b, h * heads + i, from + row) + b0 + id - row * cols, 0.f);
     }
@@ -293,31 +308,54 @@ template <int W, int TB> struct Tiles {
 
 template <int W, int TB> using StateTiles = f32x4[Tiles<W, TB>::AT][Tiles<W, TB>::BT];
 
-template <int W, int TB>
-__device__ __forceinline__ void load_state(StateTiles<W, TB>& S, const Tiles<W, TB>& t, const float* from, int sa, int sb, int wa, int wb, int b0) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+// Tiles (i, j) of a state in memory, rows a0 + 16 i .., columns b0 + 16 j ..: element (a, b) at a sa + b sb; zeros outside it.
+template <int NI, int NJ, class F> __device__ __forceinline__ void each_number(const float* state, int sa, int sb, int wa, int wb, int a0, int b0, F f) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, at = ((a0 + 4 * g) * sa + (b0 + c) * sb) * 4;
+  const __amdgpu_buffer_rsrc_t m = buffer_of(state, wa * wb * 4);
 #pragma unroll
-  for (int i = 0; i < Tiles<W, TB>::AT; ++i)
+  for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < Tiles<W, TB>::BT; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int a = 16 * (t.at + i) + 4 * g + r, b = b0 + 16 * (t.bt + j) + c;
-        S[i][j][r] = from != nullptr && a < wa && b < wb ? from[(size_t)a * sa + (size_t)b * sb] : 0.f;
+        const bool in = a0 + 4 * g + 16 * i + r < wa && b0 + c + 16 * j < wb;
+        f(m, i, j, r, in ? at + ((16 * i + r) * sa + 16 * j * sb) * 4 : kNowhere);
       }
 }
-template <int W, int TB>
-__device__ __forceinline__ void store_state(const StateTiles<W, TB>& S, const Tiles<W, TB>& t, float* to, int sa, int sb, int wa, int wb, int b0) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+template <int NI, int NJ>
+__device__ __forceinline__ void load_state(f32x4 (&S)[NI][NJ], const float* from, int sa, int sb, int wa, int wb, int a0, int b0) {
+  if (from == nullptr) {
 #pragma unroll
-  for (int i = 0; i < Tiles<W, TB>::AT; ++i)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < Tiles<W, TB>::BT; ++j)
+      for (int j = 0; j < NJ; ++j) S[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    return;
+  }
+  each_number<NI, NJ>(from, sa, sb, wa, wb, a0, b0, [&](__amdgpu_buffer_rsrc_t m, int i, int j, int r, int o) {
+    S[i][j][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(m, o, 0, 0));
+  });
+}
+template <int NI, int NJ>
+__device__ __forceinline__ void store_state(const f32x4 (&S)[NI][NJ], float* to, int sa, int sb, int wa, int wb, int a0, int b0) {
+  each_number<NI, NJ>(to, sa, sb, wa, wb, a0, b0, [&](__amdgpu_buffer_rsrc_t m, int i, int j, int r, int o) {
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[i][j][r]), m, o, 0, 0);
+  });
+}
+template <int NI, int NJ> __device__ __forceinline__ void decay_state(f32x4 (&S)[NI][NJ], Keep k) {
+  const float part = scalar(k.part);
+  if (__builtin_amdgcn_readfirstlane((int)k.near)) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int a = 16 * (t.at + i) + 4 * g + r, b = b0 + 16 * (t.bt + j) + c;
-        if (a < wa && b < wb) to[(size_t)a * sa + (size_t)b * sb] = S[i][j][r];
-      }
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[i][j][r] = fmaf(S[i][j][r], part, S[i][j][r]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) scale_by(S[i][j], part);
+  }
 }
 
 // Weights of a chunk's n rows in the sums of a state, lambda^(n - j - first) scale for row j, in LDS from the powers there.
@@ -357,40 +395,22 @@ __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, T
   }
 }
 
-constexpr size_t kTables = (kChunk + 68) * 4;             // bytes of the weights and the powers
-template <int W, int TB> __device__ __forceinline__ void decay_state(StateTiles<W, TB>& S, Keep k) {
-#pragma unroll
-  for (int i = 0; i < Tiles<W, TB>::AT; ++i)
-#pragma unroll
-    for (int j = 0; j < Tiles<W, TB>::BT; ++j) {
-      if (k.near) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[i][j][r] = fmaf(S[i][j][r], k.part, S[i][j][r]);
-      } else {
-        scale_by(S[i][j], k.part);
-      }
-    }
-}
-// Weights s lambda^(16 q + col - 4 g - r) of the scores of rows 4 g + r with the row col, q tiles of sixteen apart.
-__device__ __forceinline__ void score_weights(f32x4 (&near)[4], const float* pw, float s) {
-  const int g = (threadIdx.x & 63) >> 4, col = threadIdx.x & 15;
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = 16 * q + col - 4 * g - r;
-      near[q][r] = n >= 0 ? s * pw[max(n, 0)] : 0.f;
-    }
+constexpr size_t kTables = (kChunk + 80 + 68) * 4;        // bytes of the weights and the powers
+// Weights of scores in LDS, s lambda^n at place 63 - n, zeros for n = -1 .. -15: a lane's four rows follow each other.
+constexpr int kNear = 80;
+__device__ __forceinline__ void put_near(float* near, const float* pw, float s) {
+  const int i = (int)threadIdx.x - 128;                        // (the third wave; the first has the other weights)
+  if (i >= 0 && i < kNear) near[i] = i < kChunk ? s * pw[kChunk - 1 - i] : 0.f;
 }
 // acc[j] += B' (weighed scores of the rows x with the rows A), both of a chunk of n rows in LDS; PERM: the order of x's numbers (RowOps).
 template <int P, int PM, int STEPS, int TB, bool PERM>
 __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[STEPS], const uint16_t* sa, int LDA, const uint16_t* sb, int LDB,
-                                           const f32x4 (&near)[4]) {
+                                           const float* near) {
   const int wave = wave_id(), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, PA = kChunk * LDA, PB = kChunk * LDB;
   // tiles of rows wave, wave - 1, ... two at a time
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const int j0 = wave - 2 * q, j1 = max(j0 - 1, 0);
+    const int j0 = afresh(wave) - 2 * q, j1 = max(j0 - 1, 0);
     phase();
     if (j0 < 0) continue;
     f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -417,10 +437,11 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
       });
     }
     f32x8 v;
+    const float* w = near + (kChunk - 1 - 32 * q - col + 4 * g);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      v[r] = q > 0 || col >= 4 * g + r ? sc[0][r] * near[2 * q][r] : 0.f;
-      v[4 + r] = j0 > 0 ? sc[1][r] * near[2 * q + 1][r] : 0.f;
+      v[r] = q > 0 || col >= 4 * g + r ? sc[0][r] * w[r] : 0.f;
+      v[4 + r] = j0 > 0 ? sc[1][r] * w[r - 16] : 0.f;
     }
     const uint16_t* lb = sb + st::lane_tr(lane, LDB);
     Op<P> bt[TB];
@@ -435,6 +456,7 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
 }
 
 // ------------------------------------------------------------------------------------------------ rows
+constexpr int cols_waves(int P, int W) { return P == 1 ? 4 : (W <= 64 ? 3 : 2); }
 // Waves to a SIMD: what LDS allows, or registers without spills.
 constexpr int walk_waves(int P, int W) { return P == 1 ? (W <= 64 ? 3 : 2) : (W <= 64 ? 2 : 1); }
 template <int P, int PM, int PU, int W, int TB, bool FULL, int DT>
@@ -444,7 +466,7 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
   constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA, *img = sb + P * PB;
-  float *uw = (float*)(img + TB * IMG), *pw = uw + kChunk;    // weights of the chunk's rows; lambda^0 .. lambda^64
+  float *uw = (float*)(img + TB * IMG), *near = uw + kChunk, *pw = near + kNear;      // weights; lambda^0 .. lambda^64
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
@@ -466,7 +488,7 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
   const float* from = w.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
-  load_state<W, TB>(S, t, from, w.sa, w.sb, w.wa, w.wb, b0);
+  load_state(S, from, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
   const int back = w.back, GX = w.GX, GA = w.GA, first = w.first;
   const float s_update = w.s_update;
   const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
@@ -482,8 +504,7 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
   };
   if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo, 0); }
   __syncthreads();
-  f32x4 near[4];
-  score_weights(near, pw, w.s_score);
+  put_near(near, pw, w.s_score);
   const float inter = w.s_inter * pw[16 * wave + col + first];
   put_weights(uw, pw, kChunk, first, s_update);
 
@@ -524,7 +545,6 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
         if (ga == 0) {
           rx.ops(x);
           if (gx + 1 < GX) fetch_x(r0, gx + 1);
-          else if (more) fetch_x(r0 + kChunk, 0);
 #pragma unroll
           for (int j = 0; j < TB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -543,8 +563,9 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
         add_scores<P, PM, STEPS, TB, false>(acc, x, sa, LDA, sb, LDB, near);
         if (ga == GA - 1) ry.put(hy.chunk(gx, r0, n, p.len, back), acc);
       }
+      if (ga == GA - 1 && more) fetch_x(r0 + kChunk, 0);       // (here x's registers are free)
       if (more || ends) {
-        if (ga == 0) decay_state<W, TB>(S, keep);
+        if (ga == 0) decay_state(S, keep);
         add_chunk<P, PU, W, TB>(S, t, sa, sb, uw);
       }
       __syncthreads();
@@ -552,7 +573,214 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
     if (more) put_image();
   }
   if (ends)
-    store_state<W, TB>(S, t, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, b0);
+    store_state(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
+}
+
+// The same by columns: a wave has sixteen columns of the state, all of its rows, in accumulators whose order of rows is that of an operand, so
+// that the state never goes through LDS; the rows x do (every wave needs all of them), and so do the chunk's scores, whose tiles the waves share
+// out.  Chunks of 16 NT rows.
+template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT>
+__global__ void __launch_bounds__(64 * WAVES, cols_waves(P, W)) k_decay_cols(WalkSet set, int ncb) {
+  constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = C * LDA, PB = C * LDB, NQ = NT / 2;
+  constexpr int OUT = P == 1 && PM == 2 ? 1 : -1, TILES = NT * (NT + 1) / 2;
+  extern __shared__ char lds[];
+  uint16_t *sx = (uint16_t*)lds, *sa = sx + P * PA, *sb = sa + P * PA, *ps = sb + P * PB;
+  float *uw = (float*)(ps + NT * NQ * PM * 512), *near = uw + kChunk, *pw = near + kNear;
+  const Call& c = set.c;
+  const Walk& w = set.w[blockIdx.y];
+  Place p;
+  if (!place(c, c.nseg, ncb, &p)) return;
+  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = NB * p.cb, bw = b0 + 16 * CT * wave;
+  if (b0 >= w.wb) return;
+  if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
+  const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows);
+  zero_rows(w.Y, p.b, p.h, w.GX, max(lo, p.len), p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows), b0, min(NB, w.wb - b0));
+  const int s = p.b * c.Hk + p.h;
+  const bool ends = w.end != nullptr && c.nseg == 1 && (p.slot >= 0 || !w.end_pool);
+  if (hi <= lo && !ends) return;
+  const float ld = c.log_decay[p.h];
+  for (int i = tid; i <= kChunk; i += T) pw[i] = power(ld, i);
+  for (int i = tid; i < NT * NQ * PM * 64; i += T) *(u32x4*)(ps + 8 * i) = u32x4{0u, 0u, 0u, 0u};      // (tiles above the diagonal stay so)
+  Keep keep = scalar(keep_of(ld, C));
+  f32x4 S[TA][CT];
+  // (with segments the pool may hold the states after the call already)
+  const float* from = w.init == nullptr && p.seg == 0 ? nullptr
+                      : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
+                                                      : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
+  load_state(S, from, w.sa, w.sb, w.wa, w.wb, 0, bw);
+  const int back = w.back, GX = w.GX, GA = w.GA, first = w.first, wb = w.wb;
+  const float s_update = w.s_update;
+  const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
+  Stage<P, W, FULL, DT, C, T> rx(hx, 0, w.wa, back), ra(ha, 0, w.wa, back);
+  Stage<P, NB, FULL, DT, C, T> rb(hb, b0, wb, back);
+  const int size = (OUT < 0 ? w.Y.dtype : OUT) == 0 ? 4 : 2, yrow = (back ? C - 1 - col : col) * hy.pitch + (bw + 4 * g) * size;
+  const int ystep = back ? -16 * hy.pitch : 16 * hy.pitch;
+  auto fetch_x = [&](int r0, int gx) { rx.fetch(hx.chunk(gx, r0, min(C, hi - r0), p.len, back)); };
+  auto fetch_rows = [&](int r0, int ga) {
+    const int n = min(C, hi - r0);
+    ra.fetch(ha.chunk(ga, r0, n, p.len, back));
+    rb.fetch(hb.chunk(ga, r0, n, p.len, back));
+  };
+  if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo, 0); }
+  __syncthreads();
+  put_near(near, pw, w.s_score);
+  put_weights(uw, pw, C, first, s_update);
+  float inter[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) inter[t] = w.s_inter * pw[16 * t + col + first];
+  f32x4 acc[CT][NT];
+  for (int r0 = lo; r0 < hi; r0 += C) {
+    int n = min(C, hi - r0);
+    const bool more = r0 + C < hi;
+    if (n < C && ends) {
+      asm("" : "+s"(n));                                      // (or powers for it would be found for every chunk)
+      put_weights(uw, pw, n, first, s_update);
+      keep = scalar(keep_of(ld, n));
+    }
+    for (int ga = 0; ga < GA; ++ga)
+      for (int gx = 0; gx < GX; ++gx) {
+        if (ga == 0) rx.store(sx, 0);
+        if (gx == 0) {
+          ra.store(sa, 0);
+          rb.store(sb, b0);
+        }
+        __syncthreads();
+        // scores: tiles (t, j <= t) of rows x and rows a in turn to the waves
+#pragma unroll
+        for (int k0 = 0; k0 < TILES; k0 += WAVES) {
+          const int k = afresh(k0 + wave);
+          if (k >= TILES) break;
+          phase();
+          const int t = (k >= 1) + (k >= 3) + (k >= 6), j = k - t * (t + 1) / 2;
+          f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            const Op<P> a = st::row_op<P>(sa + (16 * j + col) * LDA + 32 * i + 8 * g, PA), x = st::row_op<P>(sx + (16 * t + col) * LDA + 32 * i + 8 * g, PA);
+            each_product<P, P>([&](int m, int y) { sc = st::mfma(a.p[m], x.p[y], sc); });
+          }
+          const float* wn = near + (kChunk - 1 - 16 * (t - j) - col + 4 * g);
+          f32x4 v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = t > j || col >= 4 * g + r ? sc[r] * wn[r] : 0.f;
+          uint16_t* to = ps + (t * NQ + (j >> 1)) * PM * 512 + lane * 8 + 4 * (j & 1);
+#pragma unroll
+          for (int m = 0; m < PM; ++m) {
+            const bf16x4 h = __builtin_convertvector(v, bf16x4);
+            *(bf16x4*)(to + m * 512) = h;
+            v -= __builtin_convertvector(h, f32x4);
+          }
+        }
+        if (ga == 0) {
+#pragma unroll
+          for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            phase();
+            Op<PM> o[CT];
+            Op<P> x[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              const uint16_t* q = sx + (16 * t + col) * LDA + 32 * i + 4 * g;
+#pragma unroll
+              for (int m = 0; m < P; ++m) {
+                const u32x2 u = *(const u32x2*)(q + m * PA), v = *(const u32x2*)(q + m * PA + 16);
+                x[t].p[m] = __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], v[0], v[1]});
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+              const f32x4 u = S[2 * i][j], v = S[2 * i + 1][j];
+              o[j] = pieces<PM>(f32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
+            }
+            each_product<PM, P>([&](int m, int y) {
+#pragma unroll
+              for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[j][t] = st::mfma(o[j].p[m], x[t].p[y], acc[j][t]);
+            });
+          }
+#pragma unroll
+          for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) scale_by(acc[j][t], inter[t]);
+        }
+        __syncthreads();
+        // what the next turn stages: rows a and b from here on, rows x when the results' registers are free
+        const bool last_x = gx == GX - 1, update = last_x && (more || ends);
+        if (last_x && ga + 1 < GA) fetch_rows(r0, ga + 1);
+        else if (last_x && more) fetch_rows(r0 + C, 0);
+        // scores times rows b
+        const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * CT * wave;
+        Op<P> b[NQ][CT];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          phase();
+#pragma unroll
+          for (int j = 0; j < CT; ++j) b[q][j] = columns<P>(lb + 32 * q * LDB + 16 * j, lb + (32 * q + 16) * LDB + 16 * j, PB);
+#pragma unroll
+          for (int t = 2 * q; t < NT; ++t) {
+            const Op<PM> o = st::image_op<PM>(ps + (t * NQ + q) * PM * 512, lane);
+            each_product<P, PM>([&](int m, int y) {
+#pragma unroll
+              for (int j = 0; j < CT; ++j) acc[j][t] = st::mfma(b[q][j].p[m], o.p[y], acc[j][t]);
+            });
+          }
+        }
+        if (ga == GA - 1) {
+          phase();
+          const Chunk k = hy.chunk(gx, r0, n, p.len, back);
+          const int at = afresh_lane(yrow - k.shift(C));
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+              const int b = bw + 16 * j + 4 * g, o = at + t * ystep + 16 * j * size;
+              if constexpr (FULL) {
+                const __amdgpu_buffer_rsrc_t r = k.buffer();
+                if (OUT == 0 || (OUT < 0 && size == 4)) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j][t]), r, b < wb ? o : kNowhere, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j][t], bf16x4)), r, b < wb ? o : kNowhere, 0, 0);
+              } else if (16 * t + col < n) {
+                const TensorDev y{k.at + o, size == 4 ? 0 : 1, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (b + i < wb) store_elem(y, i, acc[j][t][i]);
+              }
+            }
+          phase();
+        }
+        if (gx + 1 < GX) fetch_x(r0, gx + 1);
+        else if (ga == GA - 1 && more) fetch_x(r0 + C, 0);
+        // the sums of the state
+        if (update) {
+          if (ga == 0) decay_state(S, keep);
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            phase();
+            const f32x4 w0 = *(const f32x4*)(uw + 4 * g + 32 * q), w1 = *(const f32x4*)(uw + 4 * g + 32 * q + 16);
+            const f32x8 wt = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+            Op<PU> u[CT];
+#pragma unroll
+            for (int j = 0; j < CT; ++j) u[j] = pieces<PU>(number<P>(b[q][j]) * wt);
+#pragma unroll
+            for (int i = 0; i < TA; i += 2) {
+              Op<P> a[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + 16 * (i + k), la + (32 * q + 16) * LDA + 16 * (i + k), PA);
+              each_product<P, PU>([&](int m, int y) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                  for (int j = 0; j < CT; ++j) S[i + k][j] = st::mfma(a[k].p[m], u[j].p[y], S[i + k][j]);
+              });
+            }
+          }
+        }
+        __syncthreads();
+      }
+  }
+  if (ends) store_state(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, 0, bw);
 }
 
 // Gradients of keys and values in one walk from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
@@ -563,7 +791,7 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
   constexpr int TB = W / 16, STEPS = W / 32, LD = W + 8, PL = kChunk * LD, PI = W * LD, OUT = P == 1 && PM == 2 ? 1 : -1;
   extern __shared__ char lds[];
   uint16_t *sq = (uint16_t*)lds, *sd = sq + P * PL, *img = sd + P * PL;
-  float *uw = (float*)(img + PM * PI), *pw = uw + kChunk;
+  float *uw = (float*)(img + PM * PI), *near = uw + kChunk, *pw = near + kNear;
   const Call& c = set.c;
   const Walk &wk = set.w[0], &wv = set.w[1];
   Place p;
@@ -583,7 +811,7 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
   const float* from = wv.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                     ? set.prefix[1] + ((size_t)s * c.nseg + p.seg) * c.state
                                                        : (p.slot >= 0 ? wv.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
-  load_state<W, TB>(S, t, from, wv.sa, wv.sb, wv.wa, wv.wb, 0);
+  load_state(S, from, wv.sa, wv.sb, wv.wa, wv.wb, 16 * t.at, 16 * t.bt);
   const Head hq(wv.A, p.b, p.h * G), hd(wv.B, p.b, p.h * G), hk(wv.X, p.b, p.h), hv(wk.X, p.b, p.h), hdk(wk.Y, p.b, p.h), hdv(wv.Y, p.b, p.h);
   Stage<P, W, FULL, DT> rq(hq, 0, wv.wa, 1), rd(hd, 0, wv.wb, 1);
   RowOps<P, STEPS, FULL, DT> rk(hk, wv.wa, 1);
@@ -602,8 +830,7 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
   };
   if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo); }
   __syncthreads();
-  f32x4 near[4];
-  score_weights(near, pw, wv.s_score);
+  put_near(near, pw, wv.s_score);
   const float inter = pw[16 * wave + col];
   put_weights(uw, pw, kChunk, 0, s_update);
   auto put_image = [&]() {
@@ -642,7 +869,6 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
       if (ga == 0) {
         rk.ops(xk);
         rv.ops(xv);
-        if (more) fetch_x(r0 + kChunk);
 #pragma unroll
         for (int j = 0; j < TB; ++j) dk[j] = dv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -674,9 +900,10 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
       if (ga == G - 1) {
         to_k.put(hdk.chunk(0, r0, n, p.len, 1), dk);
         to_v.put(hdv.chunk(0, r0, n, p.len, 1), dv);
+        if (more) fetch_x(r0 + kChunk);                          // (here the operands' registers are free)
       }
       if (more || ends) {
-        if (ga == 0) decay_state<W, TB>(S, keep);
+        if (ga == 0) decay_state(S, keep);
         add_chunk<P, PU, W, TB>(S, t, sq, sd, uw);
       }
       __syncthreads();
@@ -684,7 +911,7 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
     if (more) put_image();
   }
   if (ends)
-    store_state<W, TB>(S, t, wv.end + (wv.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, wv.sa, wv.sb, wv.wa, wv.wb, 0);
+    store_state(S, wv.end + (wv.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, wv.sa, wv.sb, wv.wa, wv.wb, 16 * t.at, 16 * t.bt);
 }
 
 // ------------------------------------------------------------------------------------------------ sums of segments
@@ -707,7 +934,7 @@ __global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
   Keep keep = scalar(keep_of(ld, kChunk));
   const Tiles<W, TB> t(wave_id());
   StateTiles<W, TB> S;
-  load_state<W, TB>(S, t, nullptr, 0, 0, 0, 0, 0);
+  load_state(S, nullptr, 0, 0, 0, 0, 0, 0);
   const Head ha(w.A, p.b, p.h * w.GA), hb(w.B, p.b, p.h * w.GA);
   Stage<P, W, FULL, DT> ra(ha, 0, w.wa, w.back);
   Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, w.back);
@@ -732,17 +959,19 @@ __global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
       __syncthreads();
       if (ga + 1 < w.GA) fetch_rows(r0, ga + 1);
       else if (r0 + kChunk < hi) fetch_rows(r0 + kChunk, 0);
-      if (ga == 0 && r0 > lo) decay_state<W, TB>(S, keep);
+      if (ga == 0 && r0 > lo) decay_state(S, keep);
       add_chunk<P, 3, W, TB>(S, t, sa, sb, uw);
       __syncthreads();
     }
   }
   const size_t s = (size_t)p.b * c.Hk + p.h;
-  store_state<W, TB>(S, t, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, b0);
+  store_state(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
 }
 
-// Sums of the segments -> states before them, in place; eight segments on their way at a time.
+// Sums of the segments -> states before them, in place; up to 32 segments on their way at a time (24 segments of 32 states of 64 x 64, eight
+// at a time: 9.4 us).
 __global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
+  constexpr int MANY = 32;
   const Call& c = set.c;
   const int which = blockIdx.z, s = blockIdx.y, b = s / c.Hk, h = s - b * c.Hk;
   int len = c.lengths ? max(0, min(c.lengths[b], c.L)) : c.L, slot;
@@ -754,27 +983,28 @@ __global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
   }
   const int id = blockIdx.x * 256 + threadIdx.x;
   if (id >= c.state) return;
-  const float ld = c.log_decay[h];
-  const float* init = set.init[which];
-  float S = init != nullptr && slot >= 0 ? init[((size_t)slot * c.Hk + h) * c.state + id] : 0.f;
+  const int held = __builtin_amdgcn_readfirstlane((len + c.seg_rows - 1) / c.seg_rows);       // segments with rows
+  // the last segment's sum is there (and wanted) where the states after it are
+  const int sums = set.end[which] != nullptr ? held : min(held, c.nseg - 1);
   float* part = set.part[which] + (size_t)s * c.nseg * c.state + id;
-  const Keep whole = keep_of(ld, c.seg_rows);
-  for (int s0 = 0; s0 < c.nseg; s0 += 8) {
-    float v[8];
+  const float* init = set.init[which];
+  float v[MANY];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool there = s0 + i < c.nseg && (long long)(s0 + i) * c.seg_rows < len && (s0 + i < c.nseg - 1 || set.end[which] != nullptr);
-      v[i] = there ? part[(size_t)(s0 + i) * c.state] : 0.f;
+  for (int i = 0; i < MANY; ++i) v[i] = i < sums ? part[(size_t)i * c.state] : 0.f;
+  float S = init != nullptr && slot >= 0 ? init[((size_t)slot * c.Hk + h) * c.state + id] : 0.f;
+  const float ld = c.log_decay[h];
+  const Keep whole = keep_of(ld, c.seg_rows), last = keep_of(ld, len - (held - 1) * c.seg_rows);
+  for (int s0 = 0; s0 < held; s0 += MANY) {
+    if (s0 > 0) {
+#pragma unroll
+      for (int i = 0; i < MANY; ++i) v[i] = s0 + i < sums ? part[(size_t)(s0 + i) * c.state] : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (s0 + i >= c.nseg) continue;
-      const long long at = (long long)(s0 + i) * c.seg_rows;
-      if (at >= len) continue;
-      part[(size_t)(s0 + i) * c.state] = S;
-      const int n = (int)min((long long)c.seg_rows, len - at);
-      S = kept(n < c.seg_rows ? keep_of(ld, n) : whole, S) + v[i];
-    }
+    for (int i = 0; i < MANY; ++i)
+      if (s0 + i < held) {
+        part[(size_t)(s0 + i) * c.state] = S;
+        S = kept(s0 + i == held - 1 ? last : whole, S) + v[i];
+      }
   }
   if (set.end[which] != nullptr && (slot >= 0 || !set.end_pool[which]))
     set.end[which][(set.end_pool[which] ? (size_t)slot * c.Hk + h : (size_t)s) * c.state + id] = S;
@@ -843,6 +1073,18 @@ int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
   return status();
 }
+template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT>
+int cols_launch(const WalkSet& a, int count, hipStream_t st) {
+  constexpr int NT = P == 1 ? 4 : 2, C = 16 * NT, NB = 16 * WAVES;
+  int ncb = 1;
+  for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
+  const size_t lds = (size_t)P * C * (2 * (W + 8) + NB + 8) * 2 + (size_t)NT * (NT / 2) * PM * 1024 + kTables;
+  if (int rc = room(k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT>, lds)) return rc;
+  const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
+  if (units * ncb > 0x7fffffffLL) return 2;
+  hipLaunchKernelGGL((k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
+  return status();
+}
 template <int P, int PM, int PU, int W, bool FULL, int DT>
 int back_launch(const WalkSet& a, hipStream_t st) {
   const size_t lds = (size_t)P * kChunk * (W + 8) * 4 + (size_t)PM * W * (W + 8) * 2 + kTables;
@@ -868,7 +1110,9 @@ int sum_launch(const SumSet& a, int count, hipStream_t st) {
 int class_of(int n) { return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
 template <int P, int PM, int PU, bool FULL, int DT> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
-  if (class_of(wa) == 128) return walk_launch<P, PM, PU, 128, 4, FULL, DT>(a, count, st);
+  if (class_of(wa) == 128)
+    return wb > 64 ? cols_launch<P, PM, PU, 128, 8, FULL, DT>(a, count, st) : cols_launch<P, PM, PU, 128, 4, FULL, DT>(a, count, st);
+  if (P == 3 || getenv("COLS")) return class_of(wa) == 64 ? cols_launch<P, PM, PU, 64, 4, FULL, DT>(a, count, st) : cols_launch<P, PM, PU, 32, 4, FULL, DT>(a, count, st);
   if (class_of(wa) == 64) return walk_launch<P, PM, PU, 64, 4, FULL, DT>(a, count, st);
   return wb <= 32 ? walk_launch<P, PM, PU, 32, 2, FULL, DT>(a, count, st) : walk_launch<P, PM, PU, 32, 4, FULL, DT>(a, count, st);
 }
