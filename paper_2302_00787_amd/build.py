@@ -35,7 +35,8 @@ SOURCES = {
     "kernels_state_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kernels_state_step.hip": [],
     "decay_api.hip": [],
-    "kernels_decay.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    # (values that do not change in a loop are worked out there: kept for all turns they take registers that hold more waves otherwise)
+    "kernels_decay.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-mllvm", "-disable-machine-licm"],
     "kernels_decay_step.hip": [],
     "host_fit.cpp": [],
 }

@@ -8,7 +8,6 @@
 // of a in the sums of the state are weighed in 32 bits and have three pieces, as the states themselves are results in fp32.
 #include "decay_common.h"
 
-#include <stdlib.h>
 #include <type_traits>
 
 namespace fs {
@@ -440,8 +439,8 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
     const float* w = near + (kChunk - 1 - 32 * q - col + 4 * g);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      v[r] = q > 0 || col >= 4 * g + r ? sc[0][r] * w[r] : 0.f;
-      v[4 + r] = j0 > 0 ? sc[1][r] * w[r - 16] : 0.f;
+      v[r] = (q > 0 || col >= 4 * g + r ? sc[0][r] : 0.f) * w[r];
+      v[4 + r] = (j0 > 0 ? sc[1][r] : 0.f) * w[r - 16];
     }
     const uint16_t* lb = sb + st::lane_tr(lane, LDB);
     Op<P> bt[TB];
@@ -456,11 +455,11 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
 }
 
 // ------------------------------------------------------------------------------------------------ rows
-constexpr int cols_waves(int P, int W) { return P == 1 ? 4 : (W <= 64 ? 3 : 2); }
+constexpr int cols_waves(int P, int WAVES, bool full, bool shared) { return full && P == 1 && WAVES == 8 && !shared ? 4 : (P == 1 ? 2 : 3); }
 // Waves to a SIMD: what LDS allows, or registers without spills.
-constexpr int walk_waves(int P, int W) { return P == 1 ? (W <= 64 ? 3 : 2) : (W <= 64 ? 2 : 1); }
-template <int P, int PM, int PU, int W, int TB, bool FULL, int DT>
-__global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet set, int ncb) {
+constexpr int walk_waves(bool full, bool shared) { return full && !shared ? 4 : (full ? 3 : 2); }
+template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
+__global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = kChunk * LDA, PB = kChunk * LDB;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1;             // (two pieces are for results in bf16)
   constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
@@ -489,7 +488,7 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state(S, from, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
-  const int back = w.back, GX = w.GX, GA = w.GA, first = w.first;
+  const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first;
   const float s_update = w.s_update;
   const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
   Stage<P, W, FULL, DT> ra(ha, 0, w.wa, back);
@@ -579,8 +578,8 @@ __global__ void __launch_bounds__(256, walk_waves(P, W)) k_decay_walk(WalkSet se
 // The same by columns: a wave has sixteen columns of the state, all of its rows, in accumulators whose order of rows is that of an operand, so
 // that the state never goes through LDS; the rows x do (every wave needs all of them), and so do the chunk's scores, whose tiles the waves share
 // out.  Chunks of 16 NT rows.
-template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT>
-__global__ void __launch_bounds__(64 * WAVES, cols_waves(P, W)) k_decay_cols(WalkSet set, int ncb) {
+template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT, bool SHARED>
+__global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb) {
   constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = C * LDA, PB = C * LDB, NQ = NT / 2;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1, TILES = NT * (NT + 1) / 2;
   extern __shared__ char lds[];
@@ -608,7 +607,7 @@ __global__ void __launch_bounds__(64 * WAVES, cols_waves(P, W)) k_decay_cols(Wal
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state(S, from, w.sa, w.sb, w.wa, w.wb, 0, bw);
-  const int back = w.back, GX = w.GX, GA = w.GA, first = w.first, wb = w.wb;
+  const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first, wb = w.wb;
   const float s_update = w.s_update;
   const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
   Stage<P, W, FULL, DT, C, T> rx(hx, 0, w.wa, back), ra(ha, 0, w.wa, back);
@@ -661,7 +660,7 @@ __global__ void __launch_bounds__(64 * WAVES, cols_waves(P, W)) k_decay_cols(Wal
           const float* wn = near + (kChunk - 1 - 16 * (t - j) - col + 4 * g);
           f32x4 v;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = t > j || col >= 4 * g + r ? sc[r] * wn[r] : 0.f;
+          for (int r = 0; r < 4; ++r) v[r] = (t > j || col >= 4 * g + r ? sc[r] : 0.f) * wn[r];
           uint16_t* to = ps + (t * NQ + (j >> 1)) * PM * 512 + lane * 8 + 4 * (j & 1);
 #pragma unroll
           for (int m = 0; m < PM; ++m) {
@@ -786,8 +785,8 @@ __global__ void __launch_bounds__(64 * WAVES, cols_waves(P, W)) k_decay_cols(Wal
 // Gradients of keys and values in one walk from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
 // dy behind, in LDS as rows of D', of which the one takes columns and the other rows.  set.w[0]: the values (X = V, A = dY, B = Q, Y = dK),
 // set.w[1]: the keys (X = K, A = Q, B = dY, Y = dV).
-template <int P, int PM, int PU, int W, bool FULL, int DT>
-__global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set) {
+template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
+__global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back(WalkSet set) {
   constexpr int TB = W / 16, STEPS = W / 32, LD = W + 8, PL = kChunk * LD, PI = W * LD, OUT = P == 1 && PM == 2 ? 1 : -1;
   extern __shared__ char lds[];
   uint16_t *sq = (uint16_t*)lds, *sd = sq + P * PL, *img = sd + P * PL;
@@ -800,7 +799,7 @@ __global__ void __launch_bounds__(256, P == 1 ? 3 : 1) k_decay_back(WalkSet set)
   const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows), pad = p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows);
   zero_rows(wk.Y, p.b, p.h, 1, max(lo, p.len), pad, 0, wk.wb);
   zero_rows(wv.Y, p.b, p.h, 1, max(lo, p.len), pad, 0, wv.wb);
-  const int s = p.b * c.Hk + p.h, G = wv.GA;
+  const int s = p.b * c.Hk + p.h, G = SHARED ? wv.GA : 1;
   const bool ends = wv.end != nullptr && c.nseg == 1 && (p.slot >= 0 || !wv.end_pool);
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
@@ -1062,36 +1061,36 @@ template <class K> int room(K kernel, size_t bytes) {
   return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? 0 : 5;
 }
 
-template <int P, int PM, int PU, int W, int TB, bool FULL, int DT>
+template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
   const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + (size_t)TB * (W / 32) * PM * 1024 + kTables;
-  if (int rc = room(k_decay_walk<P, PM, PU, W, TB, FULL, DT>, lds)) return rc;
+  if (int rc = room(k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
+  hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
   return status();
 }
-template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT>
+template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT, bool SHARED>
 int cols_launch(const WalkSet& a, int count, hipStream_t st) {
   constexpr int NT = P == 1 ? 4 : 2, C = 16 * NT, NB = 16 * WAVES;
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
   const size_t lds = (size_t)P * C * (2 * (W + 8) + NB + 8) * 2 + (size_t)NT * (NT / 2) * PM * 1024 + kTables;
-  if (int rc = room(k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT>, lds)) return rc;
+  if (int rc = room(k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
+  hipLaunchKernelGGL((k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
   return status();
 }
-template <int P, int PM, int PU, int W, bool FULL, int DT>
+template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
 int back_launch(const WalkSet& a, hipStream_t st) {
   const size_t lds = (size_t)P * kChunk * (W + 8) * 4 + (size_t)PM * W * (W + 8) * 2 + kTables;
-  if (int rc = room(k_decay_back<P, PM, PU, W, FULL, DT>, lds)) return rc;
+  if (int rc = room(k_decay_back<P, PM, PU, W, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   if (units > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_back<P, PM, PU, W, FULL, DT>), dim3((unsigned)units), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((k_decay_back<P, PM, PU, W, FULL, DT, SHARED>), dim3((unsigned)units), dim3(256), lds, st, a);
   return status();
 }
 template <int P, int W, int TB, bool FULL, int DT>
@@ -1109,20 +1108,29 @@ int sum_launch(const SumSet& a, int count, hipStream_t st) {
 
 int class_of(int n) { return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
-template <int P, int PM, int PU, bool FULL, int DT> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
+template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
   if (class_of(wa) == 128)
-    return wb > 64 ? cols_launch<P, PM, PU, 128, 8, FULL, DT>(a, count, st) : cols_launch<P, PM, PU, 128, 4, FULL, DT>(a, count, st);
-  if (P == 3 || getenv("COLS")) return class_of(wa) == 64 ? cols_launch<P, PM, PU, 64, 4, FULL, DT>(a, count, st) : cols_launch<P, PM, PU, 32, 4, FULL, DT>(a, count, st);
-  if (class_of(wa) == 64) return walk_launch<P, PM, PU, 64, 4, FULL, DT>(a, count, st);
-  return wb <= 32 ? walk_launch<P, PM, PU, 32, 2, FULL, DT>(a, count, st) : walk_launch<P, PM, PU, 32, 4, FULL, DT>(a, count, st);
+    return wb > 64 ? cols_launch<P, PM, PU, 128, 8, FULL, DT, SHARED>(a, count, st) : cols_launch<P, PM, PU, 128, 4, FULL, DT, SHARED>(a, count, st);
+  if constexpr (P == 3) {
+    return class_of(wa) == 64 ? cols_launch<P, PM, PU, 64, 4, FULL, DT, SHARED>(a, count, st) : cols_launch<P, PM, PU, 32, 4, FULL, DT, SHARED>(a, count, st);
+  } else {
+    if (class_of(wa) == 64) return walk_launch<P, PM, PU, 64, 4, FULL, DT, SHARED>(a, count, st);
+    return wb <= 32 ? walk_launch<P, PM, PU, 32, 2, FULL, DT, SHARED>(a, count, st) : walk_launch<P, PM, PU, 32, 4, FULL, DT, SHARED>(a, count, st);
+  }
 }
-template <int P, int PM, int PU, bool FULL, int DT> int back_width(const WalkSet& a, int w, hipStream_t st) {
-  return w <= 32 ? back_launch<P, PM, PU, 32, FULL, DT>(a, st) : back_launch<P, PM, PU, 64, FULL, DT>(a, st);
+template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int back_width(const WalkSet& a, int w, hipStream_t st) {
+  return w <= 32 ? back_launch<P, PM, PU, 32, FULL, DT, SHARED>(a, st) : back_launch<P, PM, PU, 64, FULL, DT, SHARED>(a, st);
 }
 template <int P, bool FULL, int DT> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
   if (class_of(wa) == 128) return sum_launch<P, 128, 4, FULL, DT>(a, count, st);
   if (class_of(wa) == 64) return sum_launch<P, 64, 4, FULL, DT>(a, count, st);
   return wb <= 32 ? sum_launch<P, 32, 2, FULL, DT>(a, count, st) : sum_launch<P, 32, 4, FULL, DT>(a, count, st);
+}
+
+// A kernel's form for rows without a ragged end, for heads that share states.  (Where none do, loops of one turn are left out: fewer registers.)
+template <class F> int each_form(bool full, bool shared, F go) {
+  if (full) return shared ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+  return go(std::false_type{}, std::true_type{});
 }
 
 }  // namespace
@@ -1131,8 +1139,9 @@ template <int P, bool FULL, int DT> int sum_width(const SumSet& a, int count, in
 int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, hipStream_t st) {
   WalkSet a = all;
   int wa = 0, wb = 0;
-  bool full = true, ends = false;
+  bool full = true, ends = false, shared = false;
   for (int i = 0; i < count; ++i) {
+    shared = shared || all.w[from + i].GX > 1 || all.w[from + i].GA > 1;
     a.w[i] = all.w[from + i];
     ends = ends || (a.w[i].end != nullptr && a.c.nseg == 1);
     a.prefix[i] = all.prefix[from + i];
@@ -1140,13 +1149,13 @@ int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, 
     wb = max(wb, a.w[i].wb);
     full = full && a.w[i].wa % 8 == 0 && a.w[i].wb % 8 == 0;
   }
-  auto go = [&](auto full_rows) {
-    constexpr bool F = decltype(full_rows)::value;
-    if (dtype == 0) return walk_width<3, 3, 3, F, 0>(a, count, wa, wb, st);
-    if (fine) return walk_width<1, 3, 3, F, 1>(a, count, wa, wb, st);
-    return ends ? walk_width<1, 2, 3, F, 1>(a, count, wa, wb, st) : walk_width<1, 2, 2, F, 1>(a, count, wa, wb, st);
+  auto go = [&](auto full_rows, auto shared_heads) {
+    constexpr bool F = decltype(full_rows)::value, G = decltype(shared_heads)::value;
+    if (dtype == 0) return walk_width<3, 3, 3, F, 0, G>(a, count, wa, wb, st);
+    if (fine) return walk_width<1, 3, 3, F, 1, G>(a, count, wa, wb, st);
+    return ends ? walk_width<1, 2, 3, F, 1, G>(a, count, wa, wb, st) : walk_width<1, 2, 2, F, 1, G>(a, count, wa, wb, st);
   };
-  return full ? go(std::true_type{}) : go(std::false_type{});
+  return each_form(full, shared, go);
 }
 
 // The walks of dK and dV (from, from + 1) as one.
@@ -1159,13 +1168,13 @@ int launch_back(const WalkSet& all, int from, int dtype, bool fine, hipStream_t 
   const Walk& w = a.w[1];
   const int n = max(w.wa, w.wb);
   const bool ends = w.end != nullptr && a.c.nseg == 1;
-  auto go = [&](auto full_rows) {
-    constexpr bool F = decltype(full_rows)::value;
-    if (dtype == 0) return back_width<3, 3, 3, F, 0>(a, n, st);
-    if (fine) return back_width<1, 3, 3, F, 1>(a, n, st);
-    return ends ? back_width<1, 2, 3, F, 1>(a, n, st) : back_width<1, 2, 2, F, 1>(a, n, st);
+  auto go = [&](auto full_rows, auto shared_heads) {
+    constexpr bool F = decltype(full_rows)::value, G = decltype(shared_heads)::value;
+    if (dtype == 0) return back_width<3, 3, 3, F, 0, G>(a, n, st);
+    if (fine) return back_width<1, 3, 3, F, 1, G>(a, n, st);
+    return ends ? back_width<1, 2, 3, F, 1, G>(a, n, st) : back_width<1, 2, 2, F, 1, G>(a, n, st);
   };
-  return w.wa % 8 == 0 && w.wb % 8 == 0 ? go(std::true_type{}) : go(std::false_type{});
+  return each_form(w.wa % 8 == 0 && w.wb % 8 == 0, w.GA > 1, go);
 }
 
 int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st) {
