@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <stdlib.h>
 
 #include "api_common.h"
 #include "decay_common.h"
@@ -14,28 +13,35 @@ namespace {
 
 constexpr long long kMaxRows = 1 << 29;          // rows of one state in a call: they are counted in 32 bits
 
-// Segments of a sequence: as many as fill the chip, of four chunks at least.
+// Segments of a sequence, as many as give the chip workgroups enough (`full`: two eight-wave ones a CU for wide rows, three of four
+// waves for others), of four chunks at least, of two where that leaves CUs without one; the query heads of a key head in workgroups of
+// their own where that does, too.
 struct Plan {
-  int nseg, seg_rows;
+  int nseg, seg_rows, parts;
   size_t states, ends, total;                    // bytes of one set of segment states; of the states that end a walk
 };
-Plan plan(int B, int heads, int L, int d, int dv, int blocks, int sets, bool ends) {
+Plan plan(int B, int H, int heads, int L, int d, int dv, int sets, bool ends) {
   Plan p;
-  const int chunks = ceil_div(std::max(L, 1), dec::kChunk);
-  const long long units = (long long)B * heads * blocks, target = getenv("TARGET") ? atoi(getenv("TARGET")) : 768;
-  const long long nseg = units >= 512 ? 1 : std::max<long long>(1, std::min<long long>((target + units - 1) / units, chunks / 4));
+  const int chunks = ceil_div(std::max(L, 1), dec::kChunk), G = H / heads;
+  const bool wide = std::max(d, dv) > 64;
+  const long long full = wide ? 512 : 768, states = (long long)B * heads;
+  long long nseg = 1;
+  if (states < 512) {
+    nseg = std::min<long long>((full + states - 1) / states, chunks / 4);
+    if (states * nseg < 256) nseg = std::min<long long>((256 + states - 1) / states, chunks / 2);
+    nseg = std::max<long long>(nseg, 1);
+  }
   const int each = ceil_div(chunks, (int)nseg);
   p.nseg = ceil_div(chunks, each);
   p.seg_rows = each * dec::kChunk;
+  p.parts = states * p.nseg < 512 ? G : 1;
   p.states = p.nseg > 1 ? align_up((size_t)B * heads * p.nseg * d * dv * sizeof(float)) : 0;
   p.ends = ends ? align_up((size_t)B * heads * d * dv * sizeof(float)) : 0;
   p.total = sets * p.states + p.ends;
   return p;
 }
-Plan plan_forward(int B, int heads, int L, int d, int dv) { return plan(B, heads, L, d, dv, dec::column_blocks(dv), 1, false); }
-Plan plan_backward(int B, int heads, int L, int d, int dv, bool dbefore) {
-  return plan(B, heads, L, d, dv, dec::column_blocks(std::max(d, dv)), 2, dbefore);
-}
+Plan plan_forward(int B, int H, int heads, int L, int d, int dv) { return plan(B, H, heads, L, d, dv, 1, false); }
+Plan plan_backward(int B, int H, int heads, int L, int d, int dv, bool dbefore) { return plan(B, H, heads, L, d, dv, 2, dbefore); }
 
 int sizes(int B, int H, int heads, int L, int d, int dv) {
   if (B < 1 || L < 0 || d < 1 || dv < 1 || H < 1 || heads < 1 || H % heads) return FS_ERR_INVALID_ARG;
@@ -72,7 +78,7 @@ dec::Call call_of(int B, int heads, int L, int d, int dv, const float* log_decay
 extern "C" {
 
 size_t favorsharp_decay_attention_workspace_bytes(int B, int H, int heads, int L, int d, int dv) {
-  return sizes(B, H, heads, L, d, dv) == FS_OK ? plan_forward(B, heads, L, d, dv).total : 0;
+  return sizes(B, H, heads, L, d, dv) == FS_OK ? plan_forward(B, H, heads, L, d, dv).total : 0;
 }
 
 int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_tensor* V, int B, int H, int heads, int L, int d, int dv,
@@ -86,7 +92,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
   if (!tensor_ok(Q, d, L > 0) || !tensor_ok(K, d, L > 0) || !tensor_ok(V, dv, L > 0) || !tensor_ok(Y, dv, L > 0)) return FS_ERR_INVALID_ARG;
   if (Q->dtype != K->dtype || Q->dtype != V->dtype) return FS_ERR_INVALID_ARG;
   if (!strides_ok({Q, K, V, Y}, L)) return FS_ERR_UNSUPPORTED;
-  const Plan p = plan_forward(B, heads, L, d, dv);
+  const Plan p = plan_forward(B, H, heads, L, d, dv);
   if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
   if (L == 0 && after == nullptr) return FS_OK;
@@ -94,7 +100,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
   float* states = (float*)workspace;
   dec::WalkSet a{};
   a.c = call_of(B, heads, L, d, dv, log_decay, lengths, slots, nslots, after != nullptr, p, left_out);
-  a.w[0] = dec::Walk{dev(Q), dev(K), dev(V), dev(Y), H / heads, 1, d, dv, scale, scale, 1.f, 1, 0, before ? before->S : nullptr,
+  a.w[0] = dec::Walk{dev(Q), dev(K), dev(V), dev(Y), H / heads / p.parts, 1, p.parts, d, dv, scale, scale, 1.f, 1, 0, before ? before->S : nullptr,
                      after ? after->S : nullptr, dv, 1, 1};
   a.prefix[0] = states;
   if (p.nseg > 1) {
@@ -103,6 +109,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
     m.w[0] = a.w[0];
     m.part[0] = states;
     m.last = after != nullptr;
+    m.fine = after != nullptr || Y->dtype == FS_F32;
     if (int rc = dec::launch_sums(m, 1, Q->dtype, s)) return rc;
     dec::JoinSet j{};
     j.c = a.c;
@@ -117,7 +124,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
 }
 
 size_t favorsharp_decay_attention_backward_workspace_bytes(int B, int H, int heads, int L, int d, int dv, int with_dbefore) {
-  return sizes(B, H, heads, L, d, dv) == FS_OK ? plan_backward(B, heads, L, d, dv, with_dbefore != 0).total : 0;
+  return sizes(B, H, heads, L, d, dv) == FS_OK ? plan_backward(B, H, heads, L, d, dv, with_dbefore != 0).total : 0;
 }
 
 int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, const fs_tensor* V, const fs_tensor* dY, int B, int H, int heads,
@@ -134,7 +141,7 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
   if (!tensor_ok(dQ, d, L > 0) || !tensor_ok(dK, d, L > 0) || !tensor_ok(dV, dv, L > 0)) return FS_ERR_INVALID_ARG;
   if (Q->dtype != K->dtype || Q->dtype != V->dtype || Q->dtype != dY->dtype) return FS_ERR_INVALID_ARG;
   if (!strides_ok({Q, K, V, dY, dQ, dK, dV}, L)) return FS_ERR_UNSUPPORTED;
-  const Plan p = plan_backward(B, heads, L, d, dv, dbefore != nullptr);
+  const Plan p = plan_backward(B, H, heads, L, d, dv, dbefore != nullptr);
   if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
   if (L == 0 && dbefore == nullptr) return FS_OK;
@@ -147,19 +154,21 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
   a.c = call_of(B, heads, L, d, dv, log_decay, lengths, slots, nslots, exclusive, p, nullptr);
   const float* last = dafter ? dafter->S : nullptr;
   float* end = dbefore == nullptr ? nullptr : (direct ? dbefore->S : ends);
-  a.w[0] = dec::Walk{dev(dY), dev(V), dev(K), dev(dQ), G, 1, dv, d, scale, scale, 1.f, 1, 0, before ? before->S : nullptr, nullptr, 1, dv, 0};
-  a.w[1] = dec::Walk{dev(V), dev(dY), dev(Q), dev(dK), 1, G, dv, d, scale, 1.f, scale, 0, 1, last, nullptr, 1, dv, 0};
-  a.w[2] = dec::Walk{dev(K), dev(Q), dev(dY), dev(dV), 1, G, d, dv, scale, 1.f, scale, 0, 1, last, end, dv, 1, direct ? 1 : 0};
+  a.w[0] = dec::Walk{dev(dY), dev(V), dev(K), dev(dQ), G / p.parts, 1, p.parts, dv, d, scale, scale, 1.f, 1, 0, before ? before->S : nullptr, nullptr, 1, dv, 0};
+  a.w[1] = dec::Walk{dev(V), dev(dY), dev(Q), dev(dK), 1, G, 1, dv, d, scale, 1.f, scale, 0, 1, last, nullptr, 1, dv, 0};
+  a.w[2] = dec::Walk{dev(K), dev(Q), dev(dY), dev(dV), 1, G, 1, d, dv, scale, 1.f, scale, 0, 1, last, end, dv, 1, direct ? 1 : 0};
   a.prefix[0] = prefix;
   a.prefix[1] = a.prefix[2] = suffix;
+  const bool fine = dQ->dtype == FS_F32 || dK->dtype == FS_F32 || dV->dtype == FS_F32;
   if (p.nseg > 1) {
     dec::SumSet m{};
     m.c = a.c;
-    m.w[0] = dec::Walk{dev(Q), dev(K), dev(V), dev(dY), G, 1, d, dv, 1.f, 1.f, 1.f, 1, 0, nullptr, nullptr, dv, 1, 0};
+    m.w[0] = dec::Walk{dev(Q), dev(K), dev(V), dev(dY), G, 1, 1, d, dv, 1.f, 1.f, 1.f, 1, 0, nullptr, nullptr, dv, 1, 0};
     m.w[1] = a.w[2];
     m.part[0] = prefix;
     m.part[1] = suffix;
     m.last = dbefore != nullptr;
+    m.fine = dbefore != nullptr || fine;
     if (int rc = dec::launch_sums(m, 2, Q->dtype, s)) return rc;
     dec::JoinSet j{};
     j.c = a.c;
@@ -172,7 +181,6 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
     j.count = 2;
     if (int rc = dec::launch_join(j, s)) return rc;
   }
-  const bool fine = dQ->dtype == FS_F32 || dK->dtype == FS_F32 || dV->dtype == FS_F32;
   const bool one = std::max(d, dv) <= 64;           // dK and dV in one walk
   if (int rc = dec::launch_walks(a, 0, one ? 1 : 3, Q->dtype, fine, s)) return rc;
   if (one)

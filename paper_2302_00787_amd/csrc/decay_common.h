@@ -19,7 +19,7 @@ constexpr int kChunk = 64;
 // A walk over the rows of every state.  G heads of X and Y, or of A and B, share a state (the other side has one).
 struct Walk {
   TensorDev X, A, B, Y;
-  int GX, GA;
+  int GX, GA, parts;             // parts: workgroups that share the G heads of X
   int wa, wb;                    // numbers of a row of X and A, of B and Y
   float s_score, s_inter, s_update;
   int first, back;               // back: row r is the sequence's row n - 1 - r
@@ -51,6 +51,7 @@ struct SumSet {
   Walk w[2];                     // A, B, GA, wa, wb, s_update, first, back
   float* part[2];
   int last;                      // the last segment is wanted, too
+  int fine;                      // sums to 24 bits for rows of bf16, too
 };
 // Sums become states before the segments.
 struct JoinSet {

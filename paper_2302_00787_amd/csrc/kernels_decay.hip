@@ -68,13 +68,15 @@ template <int P> __device__ __forceinline__ f32x8 number(const Op<P>& o) {
   return x;
 }
 
-struct Place { int b, h, seg, cb, slot, len; };
-// Units of a grid: (sequence, key head, segment), their column blocks eight workgroups apart, on one XCD.  slot -2: left out.
-__device__ __forceinline__ bool place(const Call& c, int nseg, int ncb, Place* p) {
+struct Place { int b, h, seg, cb, part, slot, len; };
+// Units of a grid: (sequence, key head, segment), their column blocks and parts of the heads eight workgroups apart, on one XCD.  slot -2:
+// left out.
+__device__ __forceinline__ bool place(const Call& c, int nseg, int ncb, int parts, Place* p) {
   // (quotients come from vector instructions: in scalars again, so that addresses are)
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-  const int x = blockIdx.x, q = uniform(x / (8 * ncb)), rest = x - q * 8 * ncb;
-  p->cb = rest >> 3;
+  const int x = blockIdx.x, each = 8 * ncb * parts, q = uniform(x / each), rest = x - q * each;
+  p->part = uniform((rest >> 3) / ncb);
+  p->cb = (rest >> 3) - p->part * ncb;
   const long long u = (long long)q * 8 + (rest & 7);
   if (u >= (long long)c.B * c.Hk * nseg) return false;
   const int s = uniform((int)u / nseg);                       // (the grid has fewer than 2^31 workgroups)
@@ -459,7 +461,7 @@ constexpr int cols_waves(int P, int WAVES, bool full, bool shared) { return full
 // Waves to a SIMD: what LDS allows, or registers without spills.
 constexpr int walk_waves(bool full, bool shared) { return full && !shared ? 4 : (full ? 3 : 2); }
 template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
-__global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb) {
+__global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb, int parts) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = kChunk * LDA, PB = kChunk * LDB;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1;             // (two pieces are for results in bf16)
   constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
@@ -469,14 +471,14 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
-  if (!place(c, c.nseg, ncb, &p)) return;
+  if (!place(c, c.nseg, ncb, parts, &p) || p.part >= w.parts) return;
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = 64 * p.cb;
   if (b0 >= w.wb) return;
-  if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
+  if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.part == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
   const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows);
-  zero_rows(w.Y, p.b, p.h, w.GX, max(lo, p.len), p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows), b0, min(64, w.wb - b0));
+  zero_rows(w.Y, p.b, p.h * w.parts + p.part, w.GX, max(lo, p.len), p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows), b0, min(64, w.wb - b0));
   const int s = p.b * c.Hk + p.h;
-  const bool ends = w.end != nullptr && c.nseg == 1 && (p.slot >= 0 || !w.end_pool);
+  const bool ends = w.end != nullptr && c.nseg == 1 && p.part == 0 && (p.slot >= 0 || !w.end_pool);
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
@@ -490,7 +492,8 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
   load_state(S, from, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
   const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first;
   const float s_update = w.s_update;
-  const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
+  const int hq = (p.h * w.parts + p.part) * GX;
+  const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, hq);
   Stage<P, W, FULL, DT> ra(ha, 0, w.wa, back);
   Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, back);
   RowOps<P, STEPS, FULL, DT> rx(hx, w.wa, back);
@@ -579,7 +582,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 // that the state never goes through LDS; the rows x do (every wave needs all of them), and so do the chunk's scores, whose tiles the waves share
 // out.  Chunks of 16 NT rows.
 template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT, bool SHARED>
-__global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb) {
+__global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb, int parts) {
   constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = C * LDA, PB = C * LDB, NQ = NT / 2;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1, TILES = NT * (NT + 1) / 2;
   extern __shared__ char lds[];
@@ -588,14 +591,14 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
-  if (!place(c, c.nseg, ncb, &p)) return;
+  if (!place(c, c.nseg, ncb, parts, &p) || p.part >= w.parts) return;
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = NB * p.cb, bw = b0 + 16 * CT * wave;
   if (b0 >= w.wb) return;
-  if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
+  if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.part == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
   const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows);
-  zero_rows(w.Y, p.b, p.h, w.GX, max(lo, p.len), p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows), b0, min(NB, w.wb - b0));
+  zero_rows(w.Y, p.b, p.h * w.parts + p.part, w.GX, max(lo, p.len), p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows), b0, min(NB, w.wb - b0));
   const int s = p.b * c.Hk + p.h;
-  const bool ends = w.end != nullptr && c.nseg == 1 && (p.slot >= 0 || !w.end_pool);
+  const bool ends = w.end != nullptr && c.nseg == 1 && p.part == 0 && (p.slot >= 0 || !w.end_pool);
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += T) pw[i] = power(ld, i);
@@ -609,7 +612,8 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   load_state(S, from, w.sa, w.sb, w.wa, w.wb, 0, bw);
   const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first, wb = w.wb;
   const float s_update = w.s_update;
-  const Head hx(w.X, p.b, p.h * GX), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, p.h * GX);
+  const int hq = (p.h * w.parts + p.part) * GX;
+  const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, hq);
   Stage<P, W, FULL, DT, C, T> rx(hx, 0, w.wa, back), ra(ha, 0, w.wa, back);
   Stage<P, NB, FULL, DT, C, T> rb(hb, b0, wb, back);
   const int size = (OUT < 0 ? w.Y.dtype : OUT) == 0 ? 4 : 2, yrow = (back ? C - 1 - col : col) * hy.pitch + (bw + 4 * g) * size;
@@ -794,7 +798,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
   const Call& c = set.c;
   const Walk &wk = set.w[0], &wv = set.w[1];
   Place p;
-  if (!place(c, c.nseg, 1, &p)) return;
+  if (!place(c, c.nseg, 1, 1, &p)) return;
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15;
   const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows), pad = p.seg == c.nseg - 1 ? c.L : min(c.L, lo + c.seg_rows);
   zero_rows(wk.Y, p.b, p.h, 1, max(lo, p.len), pad, 0, wk.wb);
@@ -914,57 +918,75 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
 }
 
 // ------------------------------------------------------------------------------------------------ sums of segments
-template <int P, int W, int TB, bool FULL, int DT>
-__global__ void __launch_bounds__(256) k_decay_sum(SumSet set, int ncb) {
-  constexpr int NB = 16 * TB, PA = kChunk * (W + 8), PB = kChunk * (NB + 8);
+// A wave has sixteen columns of the sums, all of their rows; the rows b are weighed.  PU as in the walks: three pieces where the states after the
+// call are wanted.
+template <int P, int PU, int W, int WAVES, int C, bool FULL, int DT>
+__global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
+  constexpr int T = 64 * WAVES, NB = 16 * WAVES, TA = W / 16, LDA = W + 8, LDB = NB + 8, PA = C * LDA, PB = C * LDB;
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA;
   float *uw = (float*)(sb + P * PB), *pw = uw + kChunk;
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
-  const int wanted = set.last ? c.nseg : c.nseg - 1;
-  if (!place(c, wanted, ncb, &p)) return;
-  const int tid = threadIdx.x, b0 = 64 * p.cb;
-  const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows);
+  if (!place(c, set.last ? c.nseg : c.nseg - 1, ncb, 1, &p)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), b0 = NB * p.cb, first = w.first;
+  const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows), back = w.back, GA = w.GA;
+  const float s_update = w.s_update;
   if (hi <= lo || b0 >= w.wb) return;
   const float ld = c.log_decay[p.h];
-  for (int i = tid; i <= kChunk; i += 256) pw[i] = power(ld, i);
-  Keep keep = scalar(keep_of(ld, kChunk));
-  const Tiles<W, TB> t(wave_id());
-  StateTiles<W, TB> S;
+  for (int i = tid; i <= kChunk; i += T) pw[i] = power(ld, i);
+  Keep keep = scalar(keep_of(ld, C));
+  f32x4 S[TA][1];
   load_state(S, nullptr, 0, 0, 0, 0, 0, 0);
-  const Head ha(w.A, p.b, p.h * w.GA), hb(w.B, p.b, p.h * w.GA);
-  Stage<P, W, FULL, DT> ra(ha, 0, w.wa, w.back);
-  Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, w.back);
+  const Head ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA);
+  Stage<P, W, FULL, DT, C, T> ra(ha, 0, w.wa, back);
+  Stage<P, NB, FULL, DT, C, T> rb(hb, b0, w.wb, back);
   auto fetch_rows = [&](int r0, int ga) {
-    const int n = min(kChunk, hi - r0);
-    ra.fetch(ha.chunk(ga, r0, n, p.len, w.back));
-    rb.fetch(hb.chunk(ga, r0, n, p.len, w.back));
+    const int n = min(C, hi - r0);
+    ra.fetch(ha.chunk(ga, r0, n, p.len, back));
+    rb.fetch(hb.chunk(ga, r0, n, p.len, back));
   };
   fetch_rows(lo, 0);
   __syncthreads();
-  put_weights(uw, pw, kChunk, w.first, w.s_update);
-  for (int r0 = lo; r0 < hi; r0 += kChunk) {
-    int n = min(kChunk, hi - r0);
-    if (n < kChunk) {
+  put_weights(uw, pw, C, first, s_update);
+  const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * wave;
+  for (int r0 = lo; r0 < hi; r0 += C) {
+    int n = min(C, hi - r0);
+    if (n < C) {
       asm("" : "+s"(n));
-      put_weights(uw, pw, n, w.first, w.s_update);
+      put_weights(uw, pw, n, first, s_update);
       keep = scalar(keep_of(ld, n));
     }
-    for (int ga = 0; ga < w.GA; ++ga) {
+    for (int ga = 0; ga < GA; ++ga) {
       ra.store(sa, 0);
       rb.store(sb, b0);
       __syncthreads();
-      if (ga + 1 < w.GA) fetch_rows(r0, ga + 1);
-      else if (r0 + kChunk < hi) fetch_rows(r0 + kChunk, 0);
+      if (ga + 1 < GA) fetch_rows(r0, ga + 1);
+      else if (r0 + C < hi) fetch_rows(r0 + C, 0);
       if (ga == 0 && r0 > lo) decay_state(S, keep);
-      add_chunk<P, 3, W, TB>(S, t, sa, sb, uw);
+#pragma unroll
+      for (int q = 0; q < C / 32; ++q) {
+        phase();
+        const f32x4 w0 = *(const f32x4*)(uw + 4 * (lane >> 4) + 32 * q), w1 = *(const f32x4*)(uw + 4 * (lane >> 4) + 32 * q + 16);
+        const f32x8 wt = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+        const Op<PU> u = pieces<PU>(number<P>(columns<P>(lb + 32 * q * LDB, lb + (32 * q + 16) * LDB, PB)) * wt);
+#pragma unroll
+        for (int i = 0; i < TA; i += 2) {
+          Op<P> a[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + 16 * (i + k), la + (32 * q + 16) * LDA + 16 * (i + k), PA);
+          each_product<P, PU>([&](int m, int y) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) S[i + k][0] = st::mfma(a[k].p[m], u.p[y], S[i + k][0]);
+          });
+        }
+      }
       __syncthreads();
     }
   }
   const size_t s = (size_t)p.b * c.Hk + p.h;
-  store_state(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
+  store_state(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 0, b0 + 16 * wave);
 }
 
 // Sums of the segments -> states before them, in place; up to 32 segments on their way at a time (24 segments of 32 states of 64 x 64, eight
@@ -1061,6 +1083,12 @@ template <class K> int room(K kernel, size_t bytes) {
   return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? 0 : 5;
 }
 
+int most_parts(const WalkSet& a, int count) {
+  int n = 1;
+  for (int i = 0; i < count; ++i) n = max(n, a.w[i].parts);
+  return n;
+}
+
 template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
@@ -1068,8 +1096,9 @@ int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + (size_t)TB * (W / 32) * PM * 1024 + kTables;
   if (int rc = room(k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
-  if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
+  const int parts = most_parts(a, count);
+  if (units * ncb * parts > 0x7fffffffLL) return 2;
+  hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(256), lds, st, a, ncb, parts);
   return status();
 }
 template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT, bool SHARED>
@@ -1080,8 +1109,9 @@ int cols_launch(const WalkSet& a, int count, hipStream_t st) {
   const size_t lds = (size_t)P * C * (2 * (W + 8) + NB + 8) * 2 + (size_t)NT * (NT / 2) * PM * 1024 + kTables;
   if (int rc = room(k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
-  if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
+  const int parts = most_parts(a, count);
+  if (units * ncb * parts > 0x7fffffffLL) return 2;
+  hipLaunchKernelGGL((k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(64 * WAVES), lds, st, a, ncb, parts);
   return status();
 }
 template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
@@ -1093,16 +1123,17 @@ int back_launch(const WalkSet& a, hipStream_t st) {
   hipLaunchKernelGGL((k_decay_back<P, PM, PU, W, FULL, DT, SHARED>), dim3((unsigned)units), dim3(256), lds, st, a);
   return status();
 }
-template <int P, int W, int TB, bool FULL, int DT>
+template <int P, int PU, int W, int WAVES, bool FULL, int DT>
 int sum_launch(const SumSet& a, int count, hipStream_t st) {
+  constexpr int C = P == 1 ? 64 : 32, NB = 16 * WAVES;
   int ncb = 1;
-  for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
-  const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + kTables;
-  if (int rc = room(k_decay_sum<P, W, TB, FULL, DT>, lds)) return rc;
+  for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
+  const size_t lds = (size_t)P * C * (W + 8 + NB + 8) * 2 + kTables;
+  if (int rc = room(k_decay_sum<P, PU, W, WAVES, C, FULL, DT>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * (a.last ? a.c.nseg : a.c.nseg - 1) + 7) / 8 * 8;
   if (units == 0) return 0;
   if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_sum<P, W, TB, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(256), lds, st, a, ncb);
+  hipLaunchKernelGGL((k_decay_sum<P, PU, W, WAVES, C, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
   return status();
 }
 
@@ -1121,10 +1152,10 @@ template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int walk_width(
 template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int back_width(const WalkSet& a, int w, hipStream_t st) {
   return w <= 32 ? back_launch<P, PM, PU, 32, FULL, DT, SHARED>(a, st) : back_launch<P, PM, PU, 64, FULL, DT, SHARED>(a, st);
 }
-template <int P, bool FULL, int DT> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
-  if (class_of(wa) == 128) return sum_launch<P, 128, 4, FULL, DT>(a, count, st);
-  if (class_of(wa) == 64) return sum_launch<P, 64, 4, FULL, DT>(a, count, st);
-  return wb <= 32 ? sum_launch<P, 32, 2, FULL, DT>(a, count, st) : sum_launch<P, 32, 4, FULL, DT>(a, count, st);
+template <int P, int PU, bool FULL, int DT> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
+  if (class_of(wa) == 128) return wb > 64 ? sum_launch<P, PU, 128, 8, FULL, DT>(a, count, st) : sum_launch<P, PU, 128, 4, FULL, DT>(a, count, st);
+  if (class_of(wa) == 64) return wb > 32 ? sum_launch<P, PU, 64, 4, FULL, DT>(a, count, st) : sum_launch<P, PU, 64, 2, FULL, DT>(a, count, st);
+  return wb > 32 ? sum_launch<P, PU, 32, 4, FULL, DT>(a, count, st) : sum_launch<P, PU, 32, 2, FULL, DT>(a, count, st);
 }
 
 // A kernel's form for rows without a ragged end, for heads that share states.  (Where none do, loops of one turn are left out: fewer registers.)
@@ -1185,8 +1216,9 @@ int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st) {
     wb = max(wb, a.w[i].wb);
     full = full && a.w[i].wa % 8 == 0 && a.w[i].wb % 8 == 0;
   }
-  if (dtype == 0) return full ? sum_width<3, true, 0>(a, count, wa, wb, st) : sum_width<3, false, 0>(a, count, wa, wb, st);
-  return full ? sum_width<1, true, 1>(a, count, wa, wb, st) : sum_width<1, false, 1>(a, count, wa, wb, st);
+  if (dtype == 0) return full ? sum_width<3, 3, true, 0>(a, count, wa, wb, st) : sum_width<3, 3, false, 0>(a, count, wa, wb, st);
+  if (a.fine) return full ? sum_width<1, 3, true, 1>(a, count, wa, wb, st) : sum_width<1, 3, false, 1>(a, count, wa, wb, st);
+  return full ? sum_width<1, 2, true, 1>(a, count, wa, wb, st) : sum_width<1, 2, false, 1>(a, count, wa, wb, st);
 }
 
 int launch_join(const JoinSet& a, hipStream_t st) {
