@@ -128,10 +128,18 @@ struct Head {
 };
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
+// Numbers from row to row in LDS: neither rows that sixteen lanes read nor columns that they read transposed meet in a bank so (8 more than the
+// width: twice the cycles for both).
+constexpr int stride(int width) { return width + 16; }
+// Columns of two neighbouring tiles of sixteen in pairs: tile 2 k + h, place 4 i + r is column 32 k + 8 i + 4 h + r, so that a lane's fours of
+// accumulators of the two follow each other.  tile_pair: the first column of a tile; lane_tr8: lane_tr for them.
+__device__ __forceinline__ int tile_pair(int j) { return 32 * (j >> 1) + 4 * (j & 1); }
+__device__ __forceinline__ int lane_tr8(int lane, int ld) { return (4 * (lane >> 4) + ((lane & 15) >> 2)) * ld + 8 * (lane & 3); }
+
 // From memory to LDS as P bf16 pieces: T threads, units of eight numbers.  FULL: rows have no ragged end, and units are loads whose
 // offsets from the chunk's first row stay; else number by number at the ends.
 template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struct Stage {
-  static constexpr int UNITS = W / 8, N = (ROWS * UNITS + T - 1) / T, LD = W + 8, PLANE = ROWS * LD, SIZE = DT == 0 ? 4 : 2;
+  static constexpr int UNITS = W / 8, N = (ROWS * UNITS + T - 1) / T, LD = stride(W), PLANE = ROWS * LD, SIZE = DT == 0 ? 4 : 2;
   static constexpr bool EVEN = ROWS * UNITS % T == 0;        // (else the last threads have no unit)
   Raw8 raw[N];
   int off, step, c, cols;        // offset of the first unit, and from one to the next
@@ -186,9 +194,8 @@ template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struc
   }
 };
 
-// A wave's sixteen rows as operands: a lane has eight numbers 32 k + 8 g .. of row 16 wave + (lane % 16) for each step k, or (PERM) numbers
-// 32 k + 4 g .. and 32 k + 16 + 4 g .., the order in which two stacked accumulators hold theirs.
-template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps {
+// A wave's sixteen rows as operands: a lane has eight numbers 32 k + 8 g .. of row 16 wave + (lane % 16) for each step k.
+template <int P, int STEPS, bool FULL, int DT> struct RowOps {
   static constexpr int SIZE = DT == 0 ? 4 : 2;
   Raw8 raw[STEPS];
   int row, cols;
@@ -200,19 +207,12 @@ template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps 
     const int g = (threadIdx.x & 63) >> 4, shift = k.shift();
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
-      const int first = afresh_lane(row - shift + (PERM ? 4 : 8) * g * SIZE);
-      auto at = [&](int c, int more) { return (PERM ? 4 : 8) * g + c < cols ? first + c * SIZE + more : kNowhere; };
+      const int first = afresh_lane(row - shift + 8 * g * SIZE);
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
-        if constexpr (DT == 0) {
-          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, at(32 * i, 0), 0, 0);
-          raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, PERM ? at(32 * i + 16, 0) : at(32 * i, 16), 0, 0);
-        } else if constexpr (!PERM) {
-          raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, at(32 * i, 0), 0, 0);
-        } else {
-          const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, at(32 * i, 0), 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(r, at(32 * i + 16, 0), 0, 0);
-          raw[i].a = u32x4{x[0], x[1], y[0], y[1]};
-        }
+        const int o = 32 * i + 8 * g < cols ? first + 32 * i * SIZE : kNowhere;
+        raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
+        if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
       }
     } else {
       const bool there = (unsigned)(row - shift) < (unsigned)(k.n * k.pitch);
@@ -220,19 +220,7 @@ template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps 
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-        if constexpr (!PERM) {
-          if (there && 32 * i + 8 * g < cols) raw[i] = st::fetch8<FULL, DT>(t, 0, 32 * i + 8 * g, cols);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int n = 32 * i + 16 * (j >> 2) + 4 * g + (j & 3);
-            if (there && n < cols) {
-              const uint32_t v = __float_as_uint(load_elem(t, n));
-              if (j < 4) raw[i].a[j] = v;
-              else raw[i].b[j - 4] = v;
-            }
-          }
-        }
+        if (there && 32 * i + 8 * g < cols) raw[i] = st::fetch8<FULL, DT>(t, 0, 32 * i + 8 * g, cols);
       }
     }
   }
@@ -241,18 +229,18 @@ template <int P, int STEPS, bool FULL, int DT, bool PERM = false> struct RowOps 
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       if constexpr (P == 1 && FULL) x[i].p[0] = __builtin_bit_cast(bf16x8, raw[i].a);
-      else if constexpr (PERM && !FULL) x[i] = st::as_op<P>(st::expand8<false, 0>(raw[i], 0, 0, 8));
       else x[i] = st::as_op<P>(st::expand8<FULL, DT>(raw[i], DT, 32 * i + 8 * g, cols));
     }
   }
 };
 
-// Numbers b0 + 16 j + 4 g .. of a wave's rows to a result; OUT: its dtype where the kernel knows it (-1: it does not).
+// Numbers b0 + 32 k + 8 g .. of a wave's rows, which two accumulators have, to a result; OUT: its dtype where the kernel knows it (-1: it does
+// not).
 template <int TB, bool FULL, int OUT> struct RowStore {
   int row, b, wb, size;
   __device__ __forceinline__ RowStore(const Head& h, int dtype, int b0, int width, int back) : wb(width), size((OUT < 0 ? dtype : OUT) == 0 ? 4 : 2) {
     const int i = 16 * wave_id() + (threadIdx.x & 15);
-    b = b0 + 4 * ((threadIdx.x & 63) >> 4);
+    b = b0 + 8 * ((threadIdx.x & 63) >> 4);
     row = (back ? kChunk - 1 - i : i) * h.pitch;
   }
   __device__ __forceinline__ void put(const Chunk& k, const f32x4 (&acc)[TB]) const {
@@ -261,18 +249,25 @@ template <int TB, bool FULL, int OUT> struct RowStore {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
       const int at = first + b * size;
 #pragma unroll
-      for (int j = 0; j < TB; ++j) {
+      for (int j = 0; j < TB; j += 2) {
         const int o = b + 16 * j < wb ? at : kNowhere;
-        if (OUT == 0 || (OUT < 0 && size == 4)) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o + 64 * j, 0, 0);
-        else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j], bf16x4)), r, o + 32 * j, 0, 0);
+        if (OUT == 0 || (OUT < 0 && size == 4)) {
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o + 64 * j, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j + 1]), r, o + 64 * j + 16, 0, 0);
+        } else {
+          const f32x8 v = {acc[j][0], acc[j][1], acc[j][2], acc[j][3], acc[j + 1][0], acc[j + 1][1], acc[j + 1][2], acc[j + 1][3]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)), r, o + 32 * j, 0, 0);
+        }
       }
     } else if ((unsigned)first < (unsigned)(k.n * k.pitch)) {
       const TensorDev t{k.at + first, size == 4 ? 0 : 1, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < TB; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (b + 16 * j + i < wb) store_elem(t, b + 16 * j + i, acc[j][i]);
+        for (int i = 0; i < 4; ++i) {
+          const int n = b + tile_pair(j) + i;
+          if (n < wb) store_elem(t, n, acc[j][i]);
+        }
     }
   }
 };
@@ -309,22 +304,23 @@ template <int W, int TB> struct Tiles {
 
 template <int W, int TB> using StateTiles = f32x4[Tiles<W, TB>::AT][Tiles<W, TB>::BT];
 
-// Tiles (i, j) of a state in memory, rows a0 + 16 i .., columns b0 + 16 j ..: element (a, b) at a sa + b sb; zeros outside it.
-template <int NI, int NJ, class F> __device__ __forceinline__ void each_number(const float* state, int sa, int sb, int wa, int wb, int a0, int b0, F f) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, at = ((a0 + 4 * g) * sa + (b0 + c) * sb) * 4;
+// Tiles (ti + i, tj + j) of a state in memory, its rows (RP) or columns (CP) in pairs of tiles, columns from b0 on: element (a, b) at a sa + b sb;
+// zeros outside it.
+template <bool RP, bool CP, int NI, int NJ, class F>
+__device__ __forceinline__ void each_number(const float* state, int sa, int sb, int wa, int wb, int ti, int tj, int b0, F f) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, row = RP ? 8 * g : 4 * g, column = b0 + (CP ? 8 * (c >> 2) + (c & 3) : c);
   const __amdgpu_buffer_rsrc_t m = buffer_of(state, wa * wb * 4);
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+    for (int j = 0; j < NJ; ++j) {
+      const int a = row + (RP ? tile_pair(ti + i) : 16 * (ti + i)), b = column + (CP ? tile_pair(tj + j) : 16 * (tj + j)), at = (a * sa + b * sb) * 4;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const bool in = a0 + 4 * g + 16 * i + r < wa && b0 + c + 16 * j < wb;
-        f(m, i, j, r, in ? at + ((16 * i + r) * sa + 16 * j * sb) * 4 : kNowhere);
-      }
+      for (int r = 0; r < 4; ++r) f(m, i, j, r, a + r < wa && b < wb ? at + r * sa * 4 : kNowhere);
+    }
 }
-template <int NI, int NJ>
-__device__ __forceinline__ void load_state(f32x4 (&S)[NI][NJ], const float* from, int sa, int sb, int wa, int wb, int a0, int b0) {
+template <bool RP, bool CP, int NI, int NJ>
+__device__ __forceinline__ void load_state(f32x4 (&S)[NI][NJ], const float* from, int sa, int sb, int wa, int wb, int ti, int tj, int b0) {
   if (from == nullptr) {
 #pragma unroll
     for (int i = 0; i < NI; ++i)
@@ -332,13 +328,13 @@ __device__ __forceinline__ void load_state(f32x4 (&S)[NI][NJ], const float* from
       for (int j = 0; j < NJ; ++j) S[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     return;
   }
-  each_number<NI, NJ>(from, sa, sb, wa, wb, a0, b0, [&](__amdgpu_buffer_rsrc_t m, int i, int j, int r, int o) {
+  each_number<RP, CP, NI, NJ>(from, sa, sb, wa, wb, ti, tj, b0, [&](__amdgpu_buffer_rsrc_t m, int i, int j, int r, int o) {
     S[i][j][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(m, o, 0, 0));
   });
 }
-template <int NI, int NJ>
-__device__ __forceinline__ void store_state(const f32x4 (&S)[NI][NJ], float* to, int sa, int sb, int wa, int wb, int a0, int b0) {
-  each_number<NI, NJ>(to, sa, sb, wa, wb, a0, b0, [&](__amdgpu_buffer_rsrc_t m, int i, int j, int r, int o) {
+template <bool RP, bool CP, int NI, int NJ>
+__device__ __forceinline__ void store_state(const f32x4 (&S)[NI][NJ], float* to, int sa, int sb, int wa, int wb, int ti, int tj, int b0) {
+  each_number<RP, CP, NI, NJ>(to, sa, sb, wa, wb, ti, tj, b0, [&](__amdgpu_buffer_rsrc_t m, int i, int j, int r, int o) {
     __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[i][j][r]), m, o, 0, 0);
   });
 }
@@ -366,9 +362,9 @@ __device__ __forceinline__ void put_weights(float* uw, const float* pw, int n, i
 // S += sum over the chunk's rows of w a b', w a as PU pieces
 template <int P, int PU, int W, int TB>
 __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, TB>& t, const uint16_t* sa, const uint16_t* sb, const float* uw) {
-  constexpr int LDA = W + 8, LDB = 16 * TB + 8, PA = kChunk * LDA, PB = kChunk * LDB, AT = Tiles<W, TB>::AT, BT = Tiles<W, TB>::BT;
+  constexpr int LDA = stride(W), LDB = stride(16 * TB), PA = kChunk * LDA, PB = kChunk * LDB, AT = Tiles<W, TB>::AT, BT = Tiles<W, TB>::BT;
   const int lane = threadIdx.x & 63;
-  const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + st::lane_tr(lane, LDB);
+  const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + lane_tr8(lane, LDB);
   const float* u = uw + 4 * (lane >> 4);
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
@@ -384,7 +380,7 @@ __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, T
     Op<P> b[BT];
 #pragma unroll
     for (int j = 0; j < BT; ++j) {
-      const uint16_t* p = lb + 32 * q * LDB + 16 * (t.bt + j);
+      const uint16_t* p = lb + 32 * q * LDB + tile_pair(t.bt + j);
       b[j] = columns<P>(p, p + 16 * LDB, PB);
     }
     each_product<PU, P>([&](int x, int y) {
@@ -403,8 +399,9 @@ __device__ __forceinline__ void put_near(float* near, const float* pw, float s) 
   const int i = (int)threadIdx.x - 128;                        // (the third wave; the first has the other weights)
   if (i >= 0 && i < kNear) near[i] = i < kChunk ? s * pw[kChunk - 1 - i] : 0.f;
 }
-// acc[j] += B' (weighed scores of the rows x with the rows A), both of a chunk of n rows in LDS; PERM: the order of x's numbers (RowOps).
-template <int P, int PM, int STEPS, int TB, bool PERM>
+// acc[j] += B' (weighed scores of the rows x with the rows A), both of a chunk in LDS; columns of B in pairs of
+// tiles.
+template <int P, int PM, int STEPS, int TB>
 __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[STEPS], const uint16_t* sa, int LDA, const uint16_t* sb, int LDB,
                                            const float* near) {
   const int wave = wave_id(), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, PA = kChunk * LDA, PB = kChunk * LDB;
@@ -417,20 +414,7 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
     f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
-      auto row = [&](int j) {
-        if constexpr (!PERM) {
-          return st::row_op<P>(sa + (16 * j + col) * LDA + 32 * k + 8 * g, PA);
-        } else {
-          Op<P> o;
-          const uint16_t* p = sa + (16 * j + col) * LDA + 32 * k + 4 * g;
-#pragma unroll
-          for (int i = 0; i < P; ++i) {
-            const u32x2 a = *(const u32x2*)(p + i * PA), b = *(const u32x2*)(p + i * PA + 16);
-            o.p[i] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
-          }
-          return o;
-        }
-      };
+      auto row = [&](int j) { return st::row_op<P>(sa + (16 * j + col) * LDA + 32 * k + 8 * g, PA); };
       const Op<P> o0 = row(j0), o1 = row(j1);
       each_product<P, P>([&](int m, int y) {
         sc[0] = st::mfma(o0.p[m], x[k].p[y], sc[0]);
@@ -444,10 +428,10 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
       v[r] = (q > 0 || col >= 4 * g + r ? sc[0][r] : 0.f) * w[r];
       v[4 + r] = (j0 > 0 ? sc[1][r] : 0.f) * w[r - 16];
     }
-    const uint16_t* lb = sb + st::lane_tr(lane, LDB);
+    const uint16_t* lb = sb + lane_tr8(lane, LDB);
     Op<P> bt[TB];
 #pragma unroll
-    for (int j = 0; j < TB; ++j) bt[j] = columns<P>(lb + 16 * j0 * LDB + 16 * j, lb + 16 * j1 * LDB + 16 * j, PB);
+    for (int j = 0; j < TB; ++j) bt[j] = columns<P>(lb + 16 * j0 * LDB + tile_pair(j), lb + 16 * j1 * LDB + tile_pair(j), PB);
     const Op<PM> o = pieces<PM>(v);
     each_product<P, PM>([&](int m, int y) {
 #pragma unroll
@@ -462,7 +446,7 @@ constexpr int cols_waves(int P, int WAVES, bool full, bool shared) { return full
 constexpr int walk_waves(bool full, bool shared) { return full && !shared ? 4 : (full ? 3 : 2); }
 template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb, int parts) {
-  constexpr int NB = 16 * TB, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = kChunk * LDA, PB = kChunk * LDB;
+  constexpr int NB = 16 * TB, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = kChunk * LDA, PB = kChunk * LDB;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1;             // (two pieces are for results in bf16)
   constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
   extern __shared__ char lds[];
@@ -489,7 +473,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
   const float* from = w.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
-  load_state(S, from, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
+  load_state<false, true>(S, from, w.sa, w.sb, w.wa, w.wb, t.at, t.bt, b0);
   const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first;
   const float s_update = w.s_update;
   const int hq = (p.h * w.parts + p.part) * GX;
@@ -562,7 +546,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 #pragma unroll
           for (int j = 0; j < TB; ++j) scale_by(acc[j], inter);
         }
-        add_scores<P, PM, STEPS, TB, false>(acc, x, sa, LDA, sb, LDB, near);
+        add_scores<P, PM, STEPS, TB>(acc, x, sa, LDA, sb, LDB, near);
         if (ga == GA - 1) ry.put(hy.chunk(gx, r0, n, p.len, back), acc);
       }
       if (ga == GA - 1 && more) fetch_x(r0 + kChunk, 0);       // (here x's registers are free)
@@ -575,7 +559,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
     if (more) put_image();
   }
   if (ends)
-    store_state(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, 16 * t.at, b0 + 16 * t.bt);
+    store_state<false, true>(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, t.at, t.bt, b0);
 }
 
 // The same by columns: a wave has sixteen columns of the state, all of its rows, in accumulators whose order of rows is that of an operand, so
@@ -583,7 +567,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 // out.  Chunks of 16 NT rows.
 template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb, int parts) {
-  constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = W + 8, LDB = NB + 8, PA = C * LDA, PB = C * LDB, NQ = NT / 2;
+  constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB, NQ = NT / 2;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1, TILES = NT * (NT + 1) / 2;
   extern __shared__ char lds[];
   uint16_t *sx = (uint16_t*)lds, *sa = sx + P * PA, *sb = sa + P * PA, *ps = sb + P * PB;
@@ -609,7 +593,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   const float* from = w.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
-  load_state(S, from, w.sa, w.sb, w.wa, w.wb, 0, bw);
+  load_state<true, false>(S, from, w.sa, w.sb, w.wa, w.wb, 0, 0, bw);
   const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first, wb = w.wb;
   const float s_update = w.s_update;
   const int hq = (p.h * w.parts + p.part) * GX;
@@ -684,14 +668,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
             Op<PM> o[CT];
             Op<P> x[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              const uint16_t* q = sx + (16 * t + col) * LDA + 32 * i + 4 * g;
-#pragma unroll
-              for (int m = 0; m < P; ++m) {
-                const u32x2 u = *(const u32x2*)(q + m * PA), v = *(const u32x2*)(q + m * PA + 16);
-                x[t].p[m] = __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], v[0], v[1]});
-              }
-            }
+            for (int t = 0; t < NT; ++t) x[t] = st::row_op<P>(sx + (16 * t + col) * LDA + 32 * i + 8 * g, PA);
 #pragma unroll
             for (int j = 0; j < CT; ++j) {
               const f32x4 u = S[2 * i][j], v = S[2 * i + 1][j];
@@ -715,7 +692,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
         if (last_x && ga + 1 < GA) fetch_rows(r0, ga + 1);
         else if (last_x && more) fetch_rows(r0 + C, 0);
         // scores times rows b
-        const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * CT * wave;
+        const uint16_t *la = sa + lane_tr8(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * CT * wave;
         Op<P> b[NQ][CT];
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
@@ -770,7 +747,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
             for (int i = 0; i < TA; i += 2) {
               Op<P> a[2];
 #pragma unroll
-              for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + 16 * (i + k), la + (32 * q + 16) * LDA + 16 * (i + k), PA);
+              for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + tile_pair(i + k), la + (32 * q + 16) * LDA + tile_pair(i + k), PA);
               each_product<P, PU>([&](int m, int y) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
@@ -783,7 +760,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
         __syncthreads();
       }
   }
-  if (ends) store_state(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, 0, bw);
+  if (ends) store_state<true, false>(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, 0, 0, bw);
 }
 
 // Gradients of keys and values in one walk from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
@@ -791,7 +768,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
 // set.w[1]: the keys (X = K, A = Q, B = dY, Y = dV).
 template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back(WalkSet set) {
-  constexpr int TB = W / 16, STEPS = W / 32, LD = W + 8, PL = kChunk * LD, PI = W * LD, OUT = P == 1 && PM == 2 ? 1 : -1;
+  constexpr int TB = W / 16, STEPS = W / 32, LD = stride(W), PL = kChunk * LD, PI = W * LD, OUT = P == 1 && PM == 2 ? 1 : -1;
   extern __shared__ char lds[];
   uint16_t *sq = (uint16_t*)lds, *sd = sq + P * PL, *img = sd + P * PL;
   float *uw = (float*)(img + PM * PI), *near = uw + kChunk, *pw = near + kNear;
@@ -814,11 +791,10 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
   const float* from = wv.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                     ? set.prefix[1] + ((size_t)s * c.nseg + p.seg) * c.state
                                                        : (p.slot >= 0 ? wv.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
-  load_state(S, from, wv.sa, wv.sb, wv.wa, wv.wb, 16 * t.at, 16 * t.bt);
+  load_state<false, true>(S, from, wv.sa, wv.sb, wv.wa, wv.wb, t.at, t.bt, 0);
   const Head hq(wv.A, p.b, p.h * G), hd(wv.B, p.b, p.h * G), hk(wv.X, p.b, p.h), hv(wk.X, p.b, p.h), hdk(wk.Y, p.b, p.h), hdv(wv.Y, p.b, p.h);
   Stage<P, W, FULL, DT> rq(hq, 0, wv.wa, 1), rd(hd, 0, wv.wb, 1);
-  RowOps<P, STEPS, FULL, DT> rk(hk, wv.wa, 1);
-  RowOps<P, STEPS, FULL, DT, true> rv(hv, wk.wa, 1);
+  RowOps<P, STEPS, FULL, DT> rk(hk, wv.wa, 1), rv(hv, wk.wa, 1);
   const RowStore<TB, FULL, OUT> to_k(hdk, wk.Y.dtype, 0, wk.wb, 1), to_v(hdv, wv.Y.dtype, 0, wv.wb, 1);
   const float s_update = wv.s_update;
   auto fetch_x = [&](int r0) {
@@ -854,7 +830,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
   put_image();
   Op<P> xk[STEPS], xv[STEPS];
   f32x4 dk[TB], dv[TB];
-  const uint16_t *rows = img + col * LD + 8 * g, *cols = img + st::lane_tr(lane, LD);
+  const uint16_t *rows = img + col * LD + 8 * g, *cols = img + lane_tr8(lane, LD);
   for (int r0 = lo; r0 < hi; r0 += kChunk) {
     int n = min(kChunk, hi - r0);
     const bool more = r0 + kChunk < hi;
@@ -886,7 +862,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
           });
           phase();
 #pragma unroll
-          for (int j = 0; j < TB; ++j) o[j] = columns<PM>(cols + 32 * k * LD + 16 * j, cols + (32 * k + 16) * LD + 16 * j, PI);
+          for (int j = 0; j < TB; ++j) o[j] = columns<PM>(cols + 32 * k * LD + tile_pair(j), cols + (32 * k + 16) * LD + tile_pair(j), PI);
           each_product<PM, P>([&](int m, int y) {
 #pragma unroll
             for (int j = 0; j < TB; ++j) dk[j] = st::mfma(o[j].p[m], xv[k].p[y], dk[j]);
@@ -898,8 +874,8 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
           scale_by(dv[j], inter);
         }
       }
-      add_scores<P, PM, STEPS, TB, true>(dk, xv, sd, LD, sq, LD, near);
-      add_scores<P, PM, STEPS, TB, false>(dv, xk, sq, LD, sd, LD, near);
+      add_scores<P, PM, STEPS, TB>(dk, xv, sd, LD, sq, LD, near);
+      add_scores<P, PM, STEPS, TB>(dv, xk, sq, LD, sd, LD, near);
       if (ga == G - 1) {
         to_k.put(hdk.chunk(0, r0, n, p.len, 1), dk);
         to_v.put(hdv.chunk(0, r0, n, p.len, 1), dv);
@@ -914,7 +890,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
     if (more) put_image();
   }
   if (ends)
-    store_state(S, wv.end + (wv.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, wv.sa, wv.sb, wv.wa, wv.wb, 16 * t.at, 16 * t.bt);
+    store_state<false, true>(S, wv.end + (wv.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, wv.sa, wv.sb, wv.wa, wv.wb, t.at, t.bt, 0);
 }
 
 // ------------------------------------------------------------------------------------------------ sums of segments
@@ -922,7 +898,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
 // call are wanted.
 template <int P, int PU, int W, int WAVES, int C, bool FULL, int DT>
 __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
-  constexpr int T = 64 * WAVES, NB = 16 * WAVES, TA = W / 16, LDA = W + 8, LDB = NB + 8, PA = C * LDA, PB = C * LDB;
+  constexpr int T = 64 * WAVES, NB = 16 * WAVES, TA = W / 16, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB;
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA;
   float *uw = (float*)(sb + P * PB), *pw = uw + kChunk;
@@ -938,7 +914,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
   for (int i = tid; i <= kChunk; i += T) pw[i] = power(ld, i);
   Keep keep = scalar(keep_of(ld, C));
   f32x4 S[TA][1];
-  load_state(S, nullptr, 0, 0, 0, 0, 0, 0);
+  load_state<false, false>(S, nullptr, 0, 0, 0, 0, 0, 0, 0);
   const Head ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA);
   Stage<P, W, FULL, DT, C, T> ra(ha, 0, w.wa, back);
   Stage<P, NB, FULL, DT, C, T> rb(hb, b0, w.wb, back);
@@ -986,7 +962,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
     }
   }
   const size_t s = (size_t)p.b * c.Hk + p.h;
-  store_state(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 0, b0 + 16 * wave);
+  store_state<false, false>(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 0, 0, b0 + 16 * wave);
 }
 
 // Sums of the segments -> states before them, in place; up to 32 segments on their way at a time (24 segments of 32 states of 64 x 64, eight
@@ -1093,7 +1069,7 @@ template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
-  const size_t lds = (size_t)P * kChunk * (W + 8 + 16 * TB + 8) * 2 + (size_t)TB * (W / 32) * PM * 1024 + kTables;
+  const size_t lds = (size_t)P * kChunk * (stride(W) + stride(16 * TB)) * 2 + (size_t)TB * (W / 32) * PM * 1024 + kTables;
   if (int rc = room(k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   const int parts = most_parts(a, count);
@@ -1106,7 +1082,7 @@ int cols_launch(const WalkSet& a, int count, hipStream_t st) {
   constexpr int NT = P == 1 ? 4 : 2, C = 16 * NT, NB = 16 * WAVES;
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
-  const size_t lds = (size_t)P * C * (2 * (W + 8) + NB + 8) * 2 + (size_t)NT * (NT / 2) * PM * 1024 + kTables;
+  const size_t lds = (size_t)P * C * (2 * stride(W) + stride(NB)) * 2 + (size_t)NT * (NT / 2) * PM * 1024 + kTables;
   if (int rc = room(k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   const int parts = most_parts(a, count);
@@ -1116,7 +1092,7 @@ int cols_launch(const WalkSet& a, int count, hipStream_t st) {
 }
 template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
 int back_launch(const WalkSet& a, hipStream_t st) {
-  const size_t lds = (size_t)P * kChunk * (W + 8) * 4 + (size_t)PM * W * (W + 8) * 2 + kTables;
+  const size_t lds = (size_t)P * kChunk * stride(W) * 4 + (size_t)PM * W * stride(W) * 2 + kTables;
   if (int rc = room(k_decay_back<P, PM, PU, W, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   if (units > 0x7fffffffLL) return 2;
@@ -1128,7 +1104,7 @@ int sum_launch(const SumSet& a, int count, hipStream_t st) {
   constexpr int C = P == 1 ? 64 : 32, NB = 16 * WAVES;
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
-  const size_t lds = (size_t)P * C * (W + 8 + NB + 8) * 2 + kTables;
+  const size_t lds = (size_t)P * C * (stride(W) + stride(NB)) * 2 + kTables;
   if (int rc = room(k_decay_sum<P, PU, W, WAVES, C, FULL, DT>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * (a.last ? a.c.nseg : a.c.nseg - 1) + 7) / 8 * 8;
   if (units == 0) return 0;
