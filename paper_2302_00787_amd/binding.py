@@ -11,6 +11,7 @@ import contextlib
 import ctypes
 import math
 import os
+import struct
 from ctypes import c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 from typing import NamedTuple
@@ -126,7 +127,7 @@ def lib() -> ctypes.CDLL:
         L.favorsharp_kernel_matvec.argtypes = [c_void_p, P, P, c_int, c_int, c_int, c_float, c_float, c_void_p, c_int,
                                                c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         R, S, F = ctypes.POINTER(FsRotary), ctypes.POINTER(FsState), ctypes.POINTER(FsFeatures)
-        X, D = ctypes.POINTER(FsRotaryAxes), ctypes.POINTER(FsDecayState)
+        V = c_void_p                # of calls whose descriptors are packed together (_packed)
         ws = [c_void_p, c_size_t, c_void_p]
         for name, restype, argtypes in (
                 ("rotary_frequencies", c_int, [c_int, c_double, c_int, c_double, c_int, c_double, c_double, c_void_p]),
@@ -144,12 +145,12 @@ def lib() -> ctypes.CDLL:
                 ("state_append_backward_workspace_bytes", c_size_t, [F, c_int, c_int, c_int, c_int]),
                 ("state_append_backward", c_int, [F, S, c_void_p, S, P, P, c_int, c_int, c_int, c_void_p, R, P, P] + ws),
                 ("rotary_sections", c_int, [c_int, c_void_p, c_double, c_int, c_int, c_void_p, c_void_p]),
-                ("rotary_axes", c_int, [X, P, c_int, P, c_int, c_int, c_int, c_int, c_int, P, P, c_void_p]),
+                ("rotary_axes", c_int, [V, V, c_int, V, c_int, c_int, c_int, c_int, c_int, V, V, c_void_p]),
                 ("decay_attention_workspace_bytes", c_size_t, [c_int] * 6),
-                ("decay_attention", c_int, [P, P, P] + [c_int] * 6 + [c_void_p, c_float, D, D, c_void_p, c_void_p, P, c_void_p] + ws),
+                ("decay_attention", c_int, [V, V, V] + [c_int] * 6 + [c_void_p, c_float, V, V, c_void_p, c_void_p, V, c_void_p] + ws),
                 ("decay_attention_backward_workspace_bytes", c_size_t, [c_int] * 7),
-                ("decay_attention_backward", c_int, [P, P, P, P] + [c_int] * 6 + [c_void_p, c_float, D, D, c_void_p, c_void_p, c_int, P, P, P, D] + ws),
-                ("decay_step", c_int, [D, c_void_p, P, P, P] + [c_int] * 5 + [c_void_p, c_float, P, c_void_p, c_void_p])):
+                ("decay_attention_backward", c_int, [V, V, V, V] + [c_int] * 6 + [c_void_p, c_float, V, V, c_void_p, c_void_p, c_int, V, V, V, V] + ws),
+                ("decay_step", c_int, [V, c_void_p, V, V, V] + [c_int] * 5 + [c_void_p, c_float, V, c_void_p, c_void_p])):
             fn = getattr(L, "favorsharp_" + name)
             fn.restype, fn.argtypes = restype, argtypes
         _lib = L
@@ -517,9 +518,13 @@ class State(NamedTuple):
     shift: torch.Tensor | None
 
 
+# (a tensor is there, so the runtime is up: torch.cuda.current_device() asks for that first)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _on(device):
     """The library launches on the current device: that of the tensors has to be it."""
-    return _SAME_DEVICE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return _SAME_DEVICE if device.index == _current_device() else torch.cuda.device(device)
 
 
 # (current_stream() makes a Stream object, 2.7 of the 17 us of a small call)
@@ -543,12 +548,40 @@ def _room(nbytes: int, device, workspace: torch.Tensor | None):
 
 def _one_device(*tensors) -> torch.device:
     device = tensors[0].device
+    index = tensors[0].get_device()          # (compared as numbers: half the time)
     for t in tensors:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != index:
             raise ValueError("tensors of one call must be on one device")
     if device.type != "cuda":
         raise ValueError("device tensor expected")
     return device
+
+
+# Descriptors of a call in one piece of memory: 40 bytes for each fs_tensor, then what follows them.  (A ctypes structure for each takes
+# twice as long, 0.5 us a tensor of a call whose launch takes 4.)
+_TENSOR, _AXES, _POOL = "Qi4xqqq", "QQQqqqiiif", "Qi4x"
+_CODES = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
+_packs = {}
+
+
+def _packed(tensors, more: str, values):
+    """(what holds it, its address) of the descriptors of [B,H,L,d] tensors and of `values` behind them."""
+    v = []
+    for t in tensors:
+        code = _CODES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {t.dtype}")
+        sb, sh, sl, sd = t.stride()
+        if sd != 1 and t.shape[-1] > 1:
+            raise ValueError("innermost stride must be 1")
+        v += (t.data_ptr(), code, sb, sh, sl)
+    key = (len(tensors), more)
+    pack = _packs.get(key)
+    if pack is None:
+        form = struct.Struct("=" + _TENSOR * len(tensors) + more)
+        pack = _packs[key] = (form.pack, (ctypes.c_char * form.size).from_buffer_copy)
+    held = pack[1](pack[0](*v, *values))
+    return held, ctypes.addressof(held)
 
 
 def _shaped(name: str, t: torch.Tensor, shape):
@@ -590,17 +623,21 @@ def _rotary_desc(rot: Rotary | None, B: int, L: int):
                                  rot.amplitude)), rot_dim
 
 
-def _rotary_axes_desc(rot: RotaryAxes, B: int, L: int):
-    if rot.freqs.dtype != torch.float64 or rot.freqs.dim() != 1 or not rot.freqs.is_contiguous():
+def _rotary_axes(rot: RotaryAxes, B: int, L: int):
+    """The members of fs_rotary_axes."""
+    f, p = rot.freqs, rot.positions
+    if f.dtype != torch.float64 or f.dim() != 1 or not f.is_contiguous():
         raise ValueError("freqs must be a contiguous float64 vector")
-    _int32("axis_of", rot.axis_of, rot.freqs.shape)
-    p = rot.positions
+    axis_of = _int32("axis_of", rot.axis_of, f.shape)
     if p.dtype != torch.int32:
         raise ValueError("positions must be int32")
-    _shaped("positions", p, (p.shape[0], L) if p.dim() == 2 else (p.shape[0], B, L))
-    sa, sb, sl = (p.stride(0), 0, p.stride(1)) if p.dim() == 2 else p.stride()
-    return ctypes.byref(FsRotaryAxes(rot.freqs.data_ptr(), rot.axis_of.data_ptr(), p.data_ptr(), sa, sb, sl, p.shape[0], 2 * rot.freqs.shape[0],
-                                     int(rot.interleaved), rot.amplitude))
+    if p.dim() == 2:
+        _shaped("positions", p, (p.shape[0], L))
+        (sa, sl), sb = p.stride(), 0
+    else:
+        _shaped("positions", p, (p.shape[0], B, L))
+        sa, sb, sl = p.stride()
+    return f.data_ptr(), axis_of, p.data_ptr(), sa, sb, sl, p.shape[0], 2 * f.shape[0], int(rot.interleaved), rot.amplitude
 
 
 def _rotary_tensors(rot: Rotary | RotaryAxes | None):
@@ -656,14 +693,21 @@ def rotary(X: torch.Tensor, rot: Rotary | RotaryAxes, X2: torch.Tensor | None = 
             out2 = _empty((B, H2, L, d), X2.dtype, X.device)
         _shaped("out2", out2, X2.shape)
     device = _one_device(X, X2, out, out2, *_rotary_tensors(rot))
-    axes = isinstance(rot, RotaryAxes)
-    r = _rotary_axes_desc(rot, B, L) if axes else _rotary_desc(rot, B, L)[0]
-    turn = lib().favorsharp_rotary_axes if axes else lib().favorsharp_rotary
+    if isinstance(rot, RotaryAxes):
+        tensors = (X, out) if X2 is None else (X, out, X2, out2)
+        held, at = _packed(tensors, _AXES, _rotary_axes(rot, B, L))
+        second = (at + 80, at + 120) if H2 else (None, None)
+        with _on(device):
+            st = lib().favorsharp_rotary_axes(at + 40 * len(tensors), at, H, second[0], H2, B, L, d, int(transposed), at + 40, second[1],
+                                              _raw_stream(device.index))
+        _check(st, "favorsharp_rotary_axes")
+        return out if X2 is None else (out, out2)
+    r, _ = _rotary_desc(rot, B, L)
     two = (ctypes.byref(_desc4(X2)), ctypes.byref(_desc4(out2))) if H2 else (None, None)
     with _on(device):
-        st = turn(r, ctypes.byref(_desc4(X)), H, two[0], H2, B, L, d, int(transposed), ctypes.byref(_desc4(out)), two[1],
-                  _raw_stream(device.index))
-    _check(st, "favorsharp_rotary_axes" if axes else "favorsharp_rotary")
+        st = lib().favorsharp_rotary(r, ctypes.byref(_desc4(X)), H, two[0], H2, B, L, d, int(transposed), ctypes.byref(_desc4(out)), two[1],
+                                     _raw_stream(device.index))
+    _check(st, "favorsharp_rotary")
     return out if X2 is None else (out, out2)
 
 
@@ -816,26 +860,30 @@ def state_append_backward(f: Features, state: State, dstate: State, K: torch.Ten
 
 
 # ------------------------------------------------------------------ linear attention with a decay for each head
-def _decay_pools(heads: int, d: int, dv: int, B: int, slots, *pools):
-    """fs_decay_state of each pool [slots, heads, d, dv] (None: NULL)."""
-    n = None
+def _decay_checked(Q, K, V, log_decay, L, slots, pools, more=()):
+    """Shapes of a call's tensors: (B, H, heads, d, dv, slots of the pools)."""
+    B, H, n, d = Q.shape
+    heads, dv = K.shape[1], V.shape[3]
+    if K.shape != (B, heads, L, d) or V.shape != (B, heads, L, dv) or n != L:
+        _shaped("Q", Q, (B, H, L, d))
+        _shaped("K", K, (B, heads, L, d))
+        _shaped("V", V, (B, heads, L, dv))
+    for name, t, like in more:
+        _shaped(name, t, (B, H, L, dv) if like is None else like.shape)
+    if log_decay.dtype != torch.float32 or not log_decay.is_contiguous():
+        raise ValueError("log_decay must be contiguous float32")
+    _shaped("log_decay", log_decay, (heads,))
+    size = 0
     for p in pools:
         if p is None:
             continue
         if p.dtype != torch.float32 or not p.is_contiguous():
             raise ValueError("states must be contiguous float32")
-        n = p.shape[0] if n is None else n
-        _shaped("state", p, (n, heads, d, dv))
-        if slots is None and B > n:
+        size = size or p.shape[0]
+        _shaped("state", p, (size, heads, d, dv))
+        if slots is None and B > size:
             raise ValueError("more sequences than slots")
-    return [None if p is None else ctypes.byref(FsDecayState(p.data_ptr(), n)) for p in pools]
-
-
-def _log_decay(log_decay: torch.Tensor, heads: int) -> int:
-    if log_decay.dtype != torch.float32 or not log_decay.is_contiguous():
-        raise ValueError("log_decay must be contiguous float32")
-    _shaped("log_decay", log_decay, (heads,))
-    return log_decay.data_ptr()
+    return B, H, heads, d, dv, size
 
 
 def decay_state_new(slots: int, heads: int, d: int, dv: int, device="cuda") -> torch.Tensor:
@@ -849,21 +897,19 @@ def decay_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay
                     workspace: torch.Tensor | None = None) -> torch.Tensor:
     """favorsharp_decay_attention: Q [B,H,L,d], K [B,heads,L,d], V [B,heads,L,dv], log_decay [heads] -> Y [B,H,L,dv].  before, after: pools
     [slots,heads,d,dv] (the same one: in place)."""
-    B, H, L, d = Q.shape
-    heads, dv = K.shape[1], V.shape[3]
-    _shaped("K", K, (B, heads, L, d))
-    _shaped("V", V, (B, heads, L, dv))
+    L = Q.shape[2]
+    B, H, heads, d, dv, size = _decay_checked(Q, K, V, log_decay, L, slots, (before, after))
     if out is None:
         out = _empty((B, H, L, dv), out_dtype or Q.dtype, Q.device)
     _shaped("out", out, (B, H, L, dv))
     device = _one_device(Q, K, V, out, log_decay, before, after, lengths, slots, left_out, workspace)
-    old, new = _decay_pools(heads, d, dv, B, slots, before, after)
+    held, at = _packed((Q, K, V, out), _POOL + _POOL, (0 if before is None else before.data_ptr(), size, 0 if after is None else after.data_ptr(), size))
     L_ = lib()
-    ws, ws_bytes, held = _room(L_.favorsharp_decay_attention_workspace_bytes(B, H, heads, L, d, dv), device, workspace)
+    ws, ws_bytes, room = _room(L_.favorsharp_decay_attention_workspace_bytes(B, H, heads, L, d, dv), device, workspace)
     with _on(device):
-        st = L_.favorsharp_decay_attention(ctypes.byref(_desc4(Q)), ctypes.byref(_desc4(K)), ctypes.byref(_desc4(V)), B, H, heads, L, d, dv,
-                                           _log_decay(log_decay, heads), scale, old, new, _int32("slots", slots, (B,)),
-                                           _int32("lengths", lengths, (B,)), ctypes.byref(_desc4(out)), _counter("left_out", left_out),
+        st = L_.favorsharp_decay_attention(at, at + 40, at + 80, B, H, heads, L, d, dv, log_decay.data_ptr(), scale,
+                                           None if before is None else at + 160, None if after is None else at + 176,
+                                           _int32("slots", slots, (B,)), _int32("lengths", lengths, (B,)), at + 120, _counter("left_out", left_out),
                                            ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_decay_attention")
     return out
@@ -875,28 +921,25 @@ def decay_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, 
                              dbefore: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """favorsharp_decay_attention_backward: gradients of sum(Y * dY) + sum(after * dafter) -> (dQ, dK, dV, dbefore), dbefore a pool if there
     is one of `before` (or is given), else None.  exclusive: the forward call had `after` (None: it did if there is dafter)."""
-    B, H, L, d = Q.shape
-    heads, dv = K.shape[1], V.shape[3]
-    _shaped("K", K, (B, heads, L, d))
-    _shaped("V", V, (B, heads, L, dv))
-    _shaped("dY", dY, (B, H, L, dv))
+    L = Q.shape[2]
     if grads is None:
         grads = tuple(_empty(t.shape, grad_dtype or t.dtype, t.device) for t in (Q, K, V))
-    for name, t, like in zip(("dQ", "dK", "dV"), grads, (Q, K, V)):
-        _shaped(name, t, like.shape)
     if dbefore is None and before is not None:
         dbefore = torch.empty_like(before)
+    B, H, heads, d, dv, size = _decay_checked(Q, K, V, log_decay, L, slots, (before, dafter, dbefore),
+                                              (("dY", dY, None), ("dQ", grads[0], Q), ("dK", grads[1], K), ("dV", grads[2], V)))
     device = _one_device(Q, K, V, dY, *grads, log_decay, before, dafter, dbefore, lengths, slots, workspace)
-    old, dnew, dold = _decay_pools(heads, d, dv, B, slots, before, dafter, dbefore)
+    pools = (before, dafter, dbefore)
+    held, at = _packed((Q, K, V, dY, *grads), 3 * _POOL, [x for p in pools for x in (0 if p is None else p.data_ptr(), size)])
+    pool = [None if p is None else at + 280 + 16 * i for i, p in enumerate(pools)]
     exclusive = dafter is not None if exclusive is None else exclusive
     L_ = lib()
-    ws, ws_bytes, held = _room(L_.favorsharp_decay_attention_backward_workspace_bytes(B, H, heads, L, d, dv, int(dbefore is not None)), device,
+    ws, ws_bytes, room = _room(L_.favorsharp_decay_attention_backward_workspace_bytes(B, H, heads, L, d, dv, int(dbefore is not None)), device,
                                workspace)
     with _on(device):
-        st = L_.favorsharp_decay_attention_backward(*(ctypes.byref(_desc4(t)) for t in (Q, K, V, dY)), B, H, heads, L, d, dv,
-                                                    _log_decay(log_decay, heads), scale, old, dnew, _int32("slots", slots, (B,)),
-                                                    _int32("lengths", lengths, (B,)), int(exclusive),
-                                                    *(ctypes.byref(_desc4(t)) for t in grads), dold, ws, ws_bytes, _raw_stream(device.index))
+        st = L_.favorsharp_decay_attention_backward(at, at + 40, at + 80, at + 120, B, H, heads, L, d, dv, log_decay.data_ptr(), scale, pool[0], pool[1],
+                                                    _int32("slots", slots, (B,)), _int32("lengths", lengths, (B,)), int(exclusive), at + 160,
+                                                    at + 200, at + 240, pool[2], ws, ws_bytes, _raw_stream(device.index))
     _check(st, "favorsharp_decay_attention_backward")
     return (*grads, dbefore)
 
@@ -905,19 +948,15 @@ def decay_step(state: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.T
                slots: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=None,
                left_out: torch.Tensor | None = None) -> torch.Tensor:
     """favorsharp_decay_step: K [B,heads,1,d], V [B,heads,1,dv] into the states (in place), then Q [B,H,1,d] -> Y [B,H,1,dv]."""
-    B, H, L, d = Q.shape
-    heads, dv = K.shape[1], V.shape[3]
-    _shaped("Q", Q, (B, H, 1, d))
-    _shaped("K", K, (B, heads, 1, d))
-    _shaped("V", V, (B, heads, 1, dv))
+    B, H, heads, d, dv, size = _decay_checked(Q, K, V, log_decay, 1, slots, (state,))
     if out is None:
-        out = _empty((B, H, 1, dv), out_dtype or Q.dtype, Q.device)
-    _shaped("out", out, (B, H, 1, dv))
+        out = Q.new_empty((B, H, 1, dv)) if out_dtype is None and dv % 8 == 0 else _empty((B, H, 1, dv), out_dtype or Q.dtype, Q.device)
+    else:
+        _shaped("out", out, (B, H, 1, dv))
     device = _one_device(Q, K, V, out, log_decay, state, slots, left_out)
-    pool, = _decay_pools(heads, d, dv, B, slots, state)
+    held, at = _packed((Q, K, V, out), _POOL, (state.data_ptr(), size))
     with _on(device):
-        st = lib().favorsharp_decay_step(pool, _int32("slots", slots, (B,)), ctypes.byref(_desc4(Q)), ctypes.byref(_desc4(K)),
-                                         ctypes.byref(_desc4(V)), B, H, heads, d, dv, _log_decay(log_decay, heads), scale,
-                                         ctypes.byref(_desc4(out)), _counter("left_out", left_out), _raw_stream(device.index))
+        st = lib().favorsharp_decay_step(at + 160, _int32("slots", slots, (B,)), at, at + 40, at + 80, B, H, heads, d, dv, log_decay.data_ptr(), scale,
+                                         at + 120, _counter("left_out", left_out), _raw_stream(device.index))
     _check(st, "favorsharp_decay_step")
     return out

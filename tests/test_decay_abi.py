@@ -122,8 +122,12 @@ def test_tensors_of_the_host_are_refused(fs):  # noqa: F811
     with pytest.raises(ValueError, match="shape"):
         fs.decay_step(torch.zeros(1, 2, 8, 8), t, t, t, g)
     with pytest.raises(ValueError, match="slots"):
-        fs._decay_pools(2, 8, 8, 2, None, torch.zeros(1, 2, 8, 8))
+        fs.decay_step(torch.zeros(1, 2, 8, 8), *[torch.zeros(2, 2, 1, 8)] * 3, g)
     with pytest.raises(ValueError, match="float32"):
-        fs._decay_pools(2, 8, 8, 1, None, torch.zeros(1, 2, 8, 8).half())
+        fs.decay_attention(t, t, t, g, before=torch.zeros(1, 2, 8, 8).half())
     with pytest.raises(ValueError, match="shape"):
-        fs._log_decay(torch.zeros(3), 2)
+        fs.decay_attention(t, t, t, torch.zeros(3))
+    with pytest.raises(ValueError, match="shape"):
+        fs.decay_attention(t, t, t, g, before=torch.zeros(3, 2, 8, 8), after=torch.zeros(2, 2, 8, 8))
+    with pytest.raises(ValueError, match="shape"):
+        fs.decay_attention_backward(t, t, t, t[..., :4], g)
