@@ -531,6 +531,11 @@ def _on(device):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+def _new(shape, like: torch.Tensor) -> torch.Tensor:
+    """_empty of a tensor's dtype on its device, at less cost."""
+    return like.new_empty(shape) if shape[-1] % 8 == 0 else _empty(shape, like.dtype, like.device)
+
+
 def _empty(shape, dtype, device) -> torch.Tensor:
     """A result, its rows at multiples of 16 bytes as the library wants them."""
     if shape[-1] % 8 == 0:
@@ -900,8 +905,9 @@ def decay_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay
     L = Q.shape[2]
     B, H, heads, d, dv, size = _decay_checked(Q, K, V, log_decay, L, slots, (before, after))
     if out is None:
-        out = _empty((B, H, L, dv), out_dtype or Q.dtype, Q.device)
-    _shaped("out", out, (B, H, L, dv))
+        out = _new((B, H, L, dv), Q) if out_dtype is None else _empty((B, H, L, dv), out_dtype, Q.device)
+    else:
+        _shaped("out", out, (B, H, L, dv))
     device = _one_device(Q, K, V, out, log_decay, before, after, lengths, slots, left_out, workspace)
     held, at = _packed((Q, K, V, out), _POOL + _POOL, (0 if before is None else before.data_ptr(), size, 0 if after is None else after.data_ptr(), size))
     L_ = lib()
@@ -950,7 +956,7 @@ def decay_step(state: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.T
     """favorsharp_decay_step: K [B,heads,1,d], V [B,heads,1,dv] into the states (in place), then Q [B,H,1,d] -> Y [B,H,1,dv]."""
     B, H, heads, d, dv, size = _decay_checked(Q, K, V, log_decay, 1, slots, (state,))
     if out is None:
-        out = Q.new_empty((B, H, 1, dv)) if out_dtype is None and dv % 8 == 0 else _empty((B, H, 1, dv), out_dtype or Q.dtype, Q.device)
+        out = _new((B, H, 1, dv), Q) if out_dtype is None else _empty((B, H, 1, dv), out_dtype, Q.device)
     else:
         _shaped("out", out, (B, H, 1, dv))
     device = _one_device(Q, K, V, out, log_decay, state, slots, left_out)

@@ -895,8 +895,8 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
 
 // ------------------------------------------------------------------------------------------------ sums of segments
 // A wave has sixteen columns of the sums, all of their rows; the rows b are weighed.  PU as in the walks: three pieces where the states after the
-// call are wanted.
-template <int P, int PU, int W, int WAVES, int C, bool FULL, int DT>
+// call are wanted.  Two chunks are on their way at a time where heads do not share states.
+template <int P, int PU, int W, int WAVES, int C, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
   constexpr int T = 64 * WAVES, NB = 16 * WAVES, TA = W / 16, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB;
   extern __shared__ char lds[];
@@ -907,7 +907,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
   Place p;
   if (!place(c, set.last ? c.nseg : c.nseg - 1, ncb, 1, &p)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), b0 = NB * p.cb, first = w.first;
-  const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows), back = w.back, GA = w.GA;
+  const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows), back = w.back, GA = SHARED ? w.GA : 1;
   const float s_update = w.s_update;
   if (hi <= lo || b0 >= w.wb) return;
   const float ld = c.log_decay[p.h];
@@ -916,18 +916,20 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
   f32x4 S[TA][1];
   load_state<false, false>(S, nullptr, 0, 0, 0, 0, 0, 0, 0);
   const Head ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA);
-  Stage<P, W, FULL, DT, C, T> ra(ha, 0, w.wa, back);
-  Stage<P, NB, FULL, DT, C, T> rb(hb, b0, w.wb, back);
-  auto fetch_rows = [&](int r0, int ga) {
+  constexpr int AHEAD = SHARED || !FULL ? 1 : 2;
+  Stage<P, W, FULL, DT, C, T> ra[2]{{ha, 0, w.wa, back}, {ha, 0, w.wa, back}};
+  Stage<P, NB, FULL, DT, C, T> rb[2]{{hb, b0, w.wb, back}, {hb, b0, w.wb, back}};
+  auto fetch_rows = [&](int i, int r0, int ga) {
     const int n = min(C, hi - r0);
-    ra.fetch(ha.chunk(ga, r0, n, p.len, back));
-    rb.fetch(hb.chunk(ga, r0, n, p.len, back));
+    ra[i].fetch(ha.chunk(ga, r0, n, p.len, back));
+    rb[i].fetch(hb.chunk(ga, r0, n, p.len, back));
   };
-  fetch_rows(lo, 0);
+  fetch_rows(0, lo, 0);
+  if (AHEAD == 2 && lo + C < hi) fetch_rows(1, lo + C, 0);
   __syncthreads();
   put_weights(uw, pw, C, first, s_update);
   const uint16_t *la = sa + st::lane_tr(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * wave;
-  for (int r0 = lo; r0 < hi; r0 += C) {
+  auto chunk = [&](int i, int r0) {
     int n = min(C, hi - r0);
     if (n < C) {
       asm("" : "+s"(n));
@@ -935,11 +937,11 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
       keep = scalar(keep_of(ld, n));
     }
     for (int ga = 0; ga < GA; ++ga) {
-      ra.store(sa, 0);
-      rb.store(sb, b0);
+      ra[i].store(sa, 0);
+      rb[i].store(sb, b0);
       __syncthreads();
-      if (ga + 1 < GA) fetch_rows(r0, ga + 1);
-      else if (r0 + C < hi) fetch_rows(r0 + C, 0);
+      if (ga + 1 < GA) fetch_rows(i, r0, ga + 1);
+      else if (r0 + AHEAD * C < hi) fetch_rows(i, r0 + AHEAD * C, 0);
       if (ga == 0 && r0 > lo) decay_state(S, keep);
 #pragma unroll
       for (int q = 0; q < C / 32; ++q) {
@@ -948,18 +950,22 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
         const f32x8 wt = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
         const Op<PU> u = pieces<PU>(number<P>(columns<P>(lb + 32 * q * LDB, lb + (32 * q + 16) * LDB, PB)) * wt);
 #pragma unroll
-        for (int i = 0; i < TA; i += 2) {
+        for (int t = 0; t < TA; t += 2) {
           Op<P> a[2];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + 16 * (i + k), la + (32 * q + 16) * LDA + 16 * (i + k), PA);
+          for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + 16 * (t + k), la + (32 * q + 16) * LDA + 16 * (t + k), PA);
           each_product<P, PU>([&](int m, int y) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) S[i + k][0] = st::mfma(a[k].p[m], u.p[y], S[i + k][0]);
+            for (int k = 0; k < 2; ++k) S[t + k][0] = st::mfma(a[k].p[m], u.p[y], S[t + k][0]);
           });
         }
       }
       __syncthreads();
     }
+  };
+  for (int r0 = lo; r0 < hi; r0 += AHEAD * C) {
+    chunk(0, r0);
+    if (AHEAD == 2 && r0 + C < hi) chunk(1, r0 + C);
   }
   const size_t s = (size_t)p.b * c.Hk + p.h;
   store_state<false, false>(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 0, 0, b0 + 16 * wave);
@@ -1099,17 +1105,17 @@ int back_launch(const WalkSet& a, hipStream_t st) {
   hipLaunchKernelGGL((k_decay_back<P, PM, PU, W, FULL, DT, SHARED>), dim3((unsigned)units), dim3(256), lds, st, a);
   return status();
 }
-template <int P, int PU, int W, int WAVES, bool FULL, int DT>
+template <int P, int PU, int W, int WAVES, bool FULL, int DT, bool SHARED>
 int sum_launch(const SumSet& a, int count, hipStream_t st) {
   constexpr int C = P == 1 ? 64 : 32, NB = 16 * WAVES;
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
   const size_t lds = (size_t)P * C * (stride(W) + stride(NB)) * 2 + kTables;
-  if (int rc = room(k_decay_sum<P, PU, W, WAVES, C, FULL, DT>, lds)) return rc;
+  if (int rc = room(k_decay_sum<P, PU, W, WAVES, C, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * (a.last ? a.c.nseg : a.c.nseg - 1) + 7) / 8 * 8;
   if (units == 0) return 0;
   if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_sum<P, PU, W, WAVES, C, FULL, DT>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
+  hipLaunchKernelGGL((k_decay_sum<P, PU, W, WAVES, C, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
   return status();
 }
 
@@ -1128,10 +1134,10 @@ template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int walk_width(
 template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int back_width(const WalkSet& a, int w, hipStream_t st) {
   return w <= 32 ? back_launch<P, PM, PU, 32, FULL, DT, SHARED>(a, st) : back_launch<P, PM, PU, 64, FULL, DT, SHARED>(a, st);
 }
-template <int P, int PU, bool FULL, int DT> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
-  if (class_of(wa) == 128) return wb > 64 ? sum_launch<P, PU, 128, 8, FULL, DT>(a, count, st) : sum_launch<P, PU, 128, 4, FULL, DT>(a, count, st);
-  if (class_of(wa) == 64) return wb > 32 ? sum_launch<P, PU, 64, 4, FULL, DT>(a, count, st) : sum_launch<P, PU, 64, 2, FULL, DT>(a, count, st);
-  return wb > 32 ? sum_launch<P, PU, 32, 4, FULL, DT>(a, count, st) : sum_launch<P, PU, 32, 2, FULL, DT>(a, count, st);
+template <int P, int PU, bool FULL, int DT, bool G> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
+  if (class_of(wa) == 128) return wb > 64 ? sum_launch<P, PU, 128, 8, FULL, DT, G>(a, count, st) : sum_launch<P, PU, 128, 4, FULL, DT, G>(a, count, st);
+  if (class_of(wa) == 64) return wb > 32 ? sum_launch<P, PU, 64, 4, FULL, DT, G>(a, count, st) : sum_launch<P, PU, 64, 2, FULL, DT, G>(a, count, st);
+  return wb > 32 ? sum_launch<P, PU, 32, 4, FULL, DT, G>(a, count, st) : sum_launch<P, PU, 32, 2, FULL, DT, G>(a, count, st);
 }
 
 // A kernel's form for rows without a ragged end, for heads that share states.  (Where none do, loops of one turn are left out: fewer registers.)
@@ -1186,15 +1192,19 @@ int launch_back(const WalkSet& all, int from, int dtype, bool fine, hipStream_t 
 
 int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st) {
   int wa = 0, wb = 0;
-  bool full = true;
+  bool full = true, shared = false;
   for (int i = 0; i < count; ++i) {
+    shared = shared || a.w[i].GA > 1;
     wa = max(wa, a.w[i].wa);
     wb = max(wb, a.w[i].wb);
     full = full && a.w[i].wa % 8 == 0 && a.w[i].wb % 8 == 0;
   }
-  if (dtype == 0) return full ? sum_width<3, 3, true, 0>(a, count, wa, wb, st) : sum_width<3, 3, false, 0>(a, count, wa, wb, st);
-  if (a.fine) return full ? sum_width<1, 3, true, 1>(a, count, wa, wb, st) : sum_width<1, 3, false, 1>(a, count, wa, wb, st);
-  return full ? sum_width<1, 2, true, 1>(a, count, wa, wb, st) : sum_width<1, 2, false, 1>(a, count, wa, wb, st);
+  auto go = [&](auto full_rows, auto shared_heads) {
+    constexpr bool F = decltype(full_rows)::value, G = decltype(shared_heads)::value;
+    if (dtype == 0) return sum_width<3, 3, F, 0, G>(a, count, wa, wb, st);
+    return a.fine ? sum_width<1, 3, F, 1, G>(a, count, wa, wb, st) : sum_width<1, 2, F, 1, G>(a, count, wa, wb, st);
+  };
+  return each_form(full, shared, go);
 }
 
 int launch_join(const JoinSet& a, hipStream_t st) {

@@ -84,8 +84,7 @@ struct AxesDev {
   long long sa, sb, sl;
   int axes;
 };
-__device__ __forceinline__ int position_of(const AxesDev& x, int pair, int b, int l) {
-  const int axis = x.axis_of[pair];
+__device__ __forceinline__ int position_of(const AxesDev& x, int axis, int b, int l) {
   return axis >= 0 && axis < x.axes ? x.positions[axis * x.sa + b * x.sb + l * x.sl] : 0;
 }
 
