@@ -137,7 +137,10 @@ int launch_rotary(const RotaryDev& r, const AxesDev& axes, const TensorDev& X, i
   // a token's heads in one thread only where that leaves a workgroup for every place of a CU (32 tokens of 16 heads: 4.2 us a head a
   // thread)
   int parts = 1;
-  while (parts < H + H2 && blocks * parts < 2048) parts *= 2;
+  // (with several axes, whose angles wait for two loads in turn, a quarter of that: B3 L1777, 16 heads of 128, fp32 23 us, 33 at one head a
+  // thread)
+  const int places = axes.axes ? 512 : 2048;
+  while (parts < H + H2 && blocks * parts < places) parts *= 2;
   a.heads_per_part = (H + H2 + parts - 1) / parts;
   const dim3 grid((unsigned)blocks, (H + H2 + a.heads_per_part - 1) / a.heads_per_part);
   auto kernel = axes.axes ? (r.rot % 16 == 0 ? k_rotary<true, true> : k_rotary<false, true>) : (r.rot % 16 == 0 ? k_rotary<true, false> : k_rotary<false, false>);
