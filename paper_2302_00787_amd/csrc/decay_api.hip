@@ -55,6 +55,12 @@ bool strides_ok(std::initializer_list<const fs_tensor*> list, int L) {
     if (L > 1 && t->stride_l > kMaxStride) return false;
   return true;
 }
+// (a sequence of one row may have any stride from row to row: a pitch that fits, as none is used)
+TensorDev rows_of(const fs_tensor* t, int L) {
+  TensorDev x = dev(t);
+  if (L <= 1) x.sl = 128;
+  return x;
+}
 int pools(std::initializer_list<const fs_decay_state*> list, int heads, int* slots) {
   *slots = 0;
   for (const fs_decay_state* s : list) {
@@ -100,7 +106,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
   float* states = (float*)workspace;
   dec::WalkSet a{};
   a.c = call_of(B, heads, L, d, dv, log_decay, lengths, slots, nslots, after != nullptr, p, left_out);
-  a.w[0] = dec::Walk{dev(Q), dev(K), dev(V), dev(Y), H / heads / p.parts, 1, p.parts, d, dv, scale, scale, 1.f, 1, 0, before ? before->S : nullptr,
+  a.w[0] = dec::Walk{rows_of(Q, L), rows_of(K, L), rows_of(V, L), rows_of(Y, L), H / heads / p.parts, 1, p.parts, d, dv, scale, scale, 1.f, 1, 0, before ? before->S : nullptr,
                      after ? after->S : nullptr, dv, 1, 1};
   a.prefix[0] = states;
   if (p.nseg > 1) {
@@ -154,16 +160,16 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
   a.c = call_of(B, heads, L, d, dv, log_decay, lengths, slots, nslots, exclusive, p, nullptr);
   const float* last = dafter ? dafter->S : nullptr;
   float* end = dbefore == nullptr ? nullptr : (direct ? dbefore->S : ends);
-  a.w[0] = dec::Walk{dev(dY), dev(V), dev(K), dev(dQ), G / p.parts, 1, p.parts, dv, d, scale, scale, 1.f, 1, 0, before ? before->S : nullptr, nullptr, 1, dv, 0};
-  a.w[1] = dec::Walk{dev(V), dev(dY), dev(Q), dev(dK), 1, G, 1, dv, d, scale, 1.f, scale, 0, 1, last, nullptr, 1, dv, 0};
-  a.w[2] = dec::Walk{dev(K), dev(Q), dev(dY), dev(dV), 1, G, 1, d, dv, scale, 1.f, scale, 0, 1, last, end, dv, 1, direct ? 1 : 0};
+  a.w[0] = dec::Walk{rows_of(dY, L), rows_of(V, L), rows_of(K, L), rows_of(dQ, L), G / p.parts, 1, p.parts, dv, d, scale, scale, 1.f, 1, 0, before ? before->S : nullptr, nullptr, 1, dv, 0};
+  a.w[1] = dec::Walk{rows_of(V, L), rows_of(dY, L), rows_of(Q, L), rows_of(dK, L), 1, G, 1, dv, d, scale, 1.f, scale, 0, 1, last, nullptr, 1, dv, 0};
+  a.w[2] = dec::Walk{rows_of(K, L), rows_of(Q, L), rows_of(dY, L), rows_of(dV, L), 1, G, 1, d, dv, scale, 1.f, scale, 0, 1, last, end, dv, 1, direct ? 1 : 0};
   a.prefix[0] = prefix;
   a.prefix[1] = a.prefix[2] = suffix;
   const bool fine = dQ->dtype == FS_F32 || dK->dtype == FS_F32 || dV->dtype == FS_F32;
   if (p.nseg > 1) {
     dec::SumSet m{};
     m.c = a.c;
-    m.w[0] = dec::Walk{dev(Q), dev(K), dev(V), dev(dY), G, 1, 1, d, dv, 1.f, 1.f, 1.f, 1, 0, nullptr, nullptr, dv, 1, 0};
+    m.w[0] = dec::Walk{rows_of(Q, L), rows_of(K, L), rows_of(V, L), rows_of(dY, L), G, 1, 1, d, dv, 1.f, 1.f, 1.f, 1, 0, nullptr, nullptr, dv, 1, 0};
     m.w[1] = a.w[2];
     m.part[0] = prefix;
     m.part[1] = suffix;

@@ -272,14 +272,16 @@ template <int TB, bool FULL, int OUT> struct RowStore {
   }
 };
 
-// Zeros for the rows of a segment that lie behind the sequence.
+// Zeros for the rows of a segment that lie behind the sequence, numbers b0 .. b0 + cols - 1 of each.
 __device__ __forceinline__ void zero_rows(const TensorDev& Y, int b, int h, int heads, int from, int to, int b0, int cols) {
   if (from >= to) return;
-  const int per = (to - from) * cols;
+  const int units = (cols + 7) / 8;
+  const long long count = (long long)(to - from) * units;
   for (int i = 0; i < heads; ++i)
-    for (int id = threadIdx.x; id < per; id += blockDim.x) {
-      const int row = id / cols;
-      store_elem(Y, st::row_base(Y, b, h * heads + i, from + row) + b0 + id - row * cols, 0.f);
+    for (long long id = threadIdx.x; id < count; id += blockDim.x) {
+      const long long row = id / units;
+      const int c = 8 * (int)(id - row * units);
+      st::store8(Y, st::row_base(Y, b, h * heads + i, from + (int)row) + b0, c, cols, f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f});
     }
 }
 

@@ -215,6 +215,59 @@ def test_padded_batches(fs, dtype, lengths):
         close(got[3][b], want[3], F32)
 
 
+def test_gradients_of_several_dtypes_and_more_slots_than_sequences(fs):
+    """dQ in fp32, dK and dV in bf16; a pool with slots that no sequence has: zeros there."""
+    import torch
+    for d in (64, 96):
+        c = Case(fs, "bf16", 2, 4, 2, 90, d, d, "slow")
+        start = torch.randn((5, 2, d, d), generator=torch.Generator().manual_seed(5)).cuda()
+        grads = [torch.empty(t.shape, dtype=dt, device="cuda") for t, dt in ((c.Q, torch.float32), (c.K, torch.bfloat16), (c.V, torch.bfloat16))]
+        got = fs.decay_attention_backward(c.Q, c.K, c.V, c.dY, c.g, c.s, before=start, grads=grads)
+        assert all(x is y for x, y in zip(got, grads)) and (got[3][2:] == 0).all()
+        for b in range(2):
+            want = c.backward(b, start[b])
+            for x, w, tol in zip(got, want, (F32, BF16, BF16, F32)):
+                close(x[b], w, tol)
+
+
+@pytest.mark.parametrize("L,H,Hk", [(1, 4, 2), (64, 6, 2), (700, 4, 1)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 128), ("bf16", 128)])
+def test_heads_that_share_states(fs, dtype, d, L, H, Hk):
+    """Few states: every query head has a workgroup of its own; many: they go together.  Sequences that are left out among them."""
+    import torch
+    for B, check in ((3, (0, 2)), (260, (0, 131, 259))):
+        if B * L > 20000:
+            continue
+        c = Case(fs, dtype, B, H, Hk, L, d, 64, "slow")
+        slots = torch.arange(B, dtype=torch.int32).cuda()
+        slots[1] = 0
+        pool = c.S0.clone()
+        Y = fs.decay_attention(c.Q, c.K, c.V, c.g, c.s, before=pool, after=pool, slots=slots)
+        got = fs.decay_attention_backward(c.Q, c.K, c.V, c.dY, c.g, c.s, before=c.S0, dafter=c.dS, slots=slots)
+        assert (Y[1] == 0).all() and all((x[1] == 0).all() for x in got[:3])
+        assert torch.equal(pool[1], c.S0[1]) and (got[3][1] == 0).all()
+        for b in check:
+            y, S = c.forward(b, c.S0[b])
+            close(Y[b], y, tolerance(dtype))
+            close(pool[b], S, F32)
+            want = c.backward(b, c.S0[b], c.dS[b])
+            for x, w in zip(got[:3], want):
+                close(x[b], w, tolerance(dtype))
+            close(got[3][b], want[3], F32)
+
+
+def test_one_row_of_any_stride(fs):
+    """Sequences of one row: from row to row their tensors may have any stride."""
+    import torch
+    c = Case(fs, "bf16", 2, 2, 2, 1, 64, 64, "slow")
+    far = [torch.as_strided(t.contiguous(), t.shape, (128, 64, 1 << 33, 1)) for t in (c.Q, c.K, c.V, c.dY)]
+    Y = fs.decay_attention(*far[:3], c.g, c.s, before=c.S0)
+    assert torch.equal(Y, fs.decay_attention(c.Q, c.K, c.V, c.g, c.s, before=c.S0))
+    got, want = (fs.decay_attention_backward(*t, c.g, c.s, before=c.S0) for t in (far, (c.Q, c.K, c.V, c.dY)))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert torch.equal(fs.decay_step(c.S0.clone(), *far[:3], c.g, c.s), fs.decay_step(c.S0.clone(), c.Q, c.K, c.V, c.g, c.s))
+
+
 def test_no_rows(fs):
     import torch
     c = Case(fs, "bf16", 2, 2, 2, 0, 64, 64, "slow")
@@ -407,12 +460,13 @@ def test_strides(fs):
     close(fs.decay_attention(Q, one, V, g, 0.3), fs.decay_attention(Q, one.contiguous(), V, g, 0.3).cpu(), 0.0)
 
 
-def test_graphs_streams_and_workspaces(fs):
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 128)])
+def test_graphs_streams_and_workspaces(fs, dtype, d):
     """Captured calls replayed on other inputs, with eager work between; two graphs that share a workspace; the ends of a workspace."""
     import torch
-    c = Case(fs, "bf16", 1, 4, 2, 900, 64, 64, "slow")
-    need = max(fs.lib().favorsharp_decay_attention_workspace_bytes(1, 4, 2, 900, 64, 64),
-               fs.lib().favorsharp_decay_attention_backward_workspace_bytes(1, 4, 2, 900, 64, 64, 1))
+    c = Case(fs, dtype, 1, 4, 2, 900, d, d, "slow")
+    need = max(fs.lib().favorsharp_decay_attention_workspace_bytes(1, 4, 2, 900, d, d),
+               fs.lib().favorsharp_decay_attention_backward_workspace_bytes(1, 4, 2, 900, d, d, 1))
     assert need > 0
     room = torch.full((need + 512,), 77, dtype=torch.uint8, device="cuda")
     ws = room[256:256 + need]
