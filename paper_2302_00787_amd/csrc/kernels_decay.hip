@@ -141,20 +141,31 @@ __device__ __forceinline__ int lane_tr8(int lane, int ld) { return (4 * (lane >>
 template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struct Stage {
   static constexpr int UNITS = W / 8, N = (ROWS * UNITS + T - 1) / T, LD = stride(W), PLANE = ROWS * LD, SIZE = DT == 0 ? 4 : 2;
   static constexpr bool EVEN = ROWS * UNITS % T == 0;        // (else the last threads have no unit)
+  // A thread's first unit: its number in the row, its offset from the chunk's first row.  (Found at each fetch by the kernel whose registers are
+  // full: kept, they are what is spilled, and what is read back waits for the loads before it.  H16 L65536 d128 bf16 410 -> 398 us, others
+  // one or two per cent slower so.)
+  static constexpr bool KEPT = !(P == 1 && T == 512 && ROWS == kChunk);
+  struct Unit { int c, off; };
   Raw8 raw[N];
-  int off, step, c, cols;        // offset of the first unit, and from one to the next
+  int b0, cols, pitch, back;
+  Unit first_unit;
   // numbers c0 .. c0 + W - 1 of the rows
-  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int back) : cols(ncols) {
-    c = c0 + 8 * (threadIdx.x % UNITS);
-    const int row = threadIdx.x / UNITS;
-    off = c < cols && (EVEN || row < ROWS) ? (back ? ROWS - 1 - row : row) * h.pitch + c * SIZE : kNowhere;
-    step = (back ? -T / UNITS : T / UNITS) * h.pitch;
+  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int backwards) : b0(c0), cols(ncols), pitch(h.pitch), back(backwards) {
+    if constexpr (KEPT) first_unit = find(threadIdx.x);
+  }
+  __device__ __forceinline__ Unit find(int tid) const {
+    const int row = tid / UNITS, c = b0 + 8 * (tid % UNITS);
+    return {c, c < cols && (EVEN || row < ROWS) ? (back ? ROWS - 1 - row : row) * pitch + c * SIZE : kNowhere};
+  }
+  __device__ __forceinline__ Unit unit() const {
+    if constexpr (KEPT) return first_unit;
+    else return find(afresh_lane(threadIdx.x));
   }
   __device__ __forceinline__ void fetch(const Chunk& k) {
     const int shift = k.shift(ROWS);
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
-      const int first = afresh_lane(off - shift);
+      const int first = afresh_lane(unit().off - shift), step = (back ? -T / UNITS : T / UNITS) * pitch;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int o = first + i * step;
@@ -162,20 +173,24 @@ template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struc
         if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
       }
     } else {
+      const Unit u = unit();
+      const int step = (back ? -T / UNITS : T / UNITS) * pitch;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int o = off + (i * step - shift);
+        const int o = u.off + (i * step - shift);
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-        if (c < cols && (unsigned)o < (unsigned)(k.n * k.pitch))
-          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (o - c * SIZE), DT, 0, 0, 0}, 0, c, cols);
+        if (u.c < cols && (unsigned)o < (unsigned)(k.n * k.pitch))
+          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (o - u.c * SIZE), DT, 0, 0, 0}, 0, u.c, cols);
       }
     }
   }
-  __device__ __forceinline__ void store(uint16_t* s, int c0) const {
+  __device__ __forceinline__ void store(uint16_t* s) const {
+    const int tid = KEPT ? (int)threadIdx.x : afresh_lane(threadIdx.x), c = b0 + 8 * (tid % UNITS);
+    uint16_t* at = s + tid / UNITS * LD + 8 * (tid % UNITS);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (!EVEN && threadIdx.x + T * i >= ROWS * UNITS) break;
-      uint16_t* to = s + (threadIdx.x + T * i) / UNITS * LD + (c - c0);
+      uint16_t* to = at + T / UNITS * i * LD;
       if constexpr (P == 1 && FULL) {
         *(u32x4*)to = raw[i].a;
       } else {
@@ -234,6 +249,10 @@ template <int P, int STEPS, bool FULL, int DT> struct RowOps {
   }
 };
 
+// Results are not read again by these calls: they go past the caches, which keep rows for the next launch (64 sequences of 1024 rows of 8
+// heads of 64 in bf16, forward and backward: 201 -> 184 us).  Not those of the walk by columns: pieces of 32 bytes, which the caches join
+// (410 -> 492 us).
+constexpr int kStream = 2;
 // Numbers b0 + 32 k + 8 g .. of a wave's rows, which two accumulators have, to a result; OUT: its dtype where the kernel knows it (-1: it does
 // not).
 template <int TB, bool FULL, int OUT> struct RowStore {
@@ -252,11 +271,11 @@ template <int TB, bool FULL, int OUT> struct RowStore {
       for (int j = 0; j < TB; j += 2) {
         const int o = b + 16 * j < wb ? at : kNowhere;
         if (OUT == 0 || (OUT < 0 && size == 4)) {
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o + 64 * j, 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j + 1]), r, o + 64 * j + 16, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o + 64 * j, 0, kStream);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j + 1]), r, o + 64 * j + 16, 0, kStream);
         } else {
           const f32x8 v = {acc[j][0], acc[j][1], acc[j][2], acc[j][3], acc[j + 1][0], acc[j + 1][1], acc[j + 1][2], acc[j + 1][3]};
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)), r, o + 32 * j, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)), r, o + 32 * j, 0, kStream);
         }
       }
     } else if ((unsigned)first < (unsigned)(k.n * k.pitch)) {
@@ -524,8 +543,8 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
       keep = scalar(keep_of(ld, n));
     }
     for (int ga = 0; ga < GA; ++ga) {
-      ra.store(sa, 0);
-      rb.store(sb, b0);
+      ra.store(sa);
+      rb.store(sb);
       __syncthreads();
       if (ga + 1 < GA) fetch_rows(r0, ga + 1);
       else if (more) fetch_rows(r0 + kChunk, 0);
@@ -628,10 +647,10 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
     }
     for (int ga = 0; ga < GA; ++ga)
       for (int gx = 0; gx < GX; ++gx) {
-        if (ga == 0) rx.store(sx, 0);
+        if (ga == 0) rx.store(sx);
         if (gx == 0) {
-          ra.store(sa, 0);
-          rb.store(sb, b0);
+          ra.store(sa);
+          rb.store(sb);
         }
         __syncthreads();
         // scores: tiles (t, j <= t) of rows x and rows a in turn to the waves
@@ -666,7 +685,6 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
             for (int t = 0; t < NT; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
-            phase();
             Op<PM> o[CT];
             Op<P> x[NT];
 #pragma unroll
@@ -842,8 +860,8 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
       keep = scalar(keep_of(ld, n));
     }
     for (int ga = 0; ga < G; ++ga) {
-      rq.store(sq, 0);
-      rd.store(sd, 0);
+      rq.store(sq);
+      rd.store(sd);
       __syncthreads();
       if (ga + 1 < G) fetch_rows(r0, ga + 1);
       else if (more) fetch_rows(r0 + kChunk, 0);
@@ -939,8 +957,8 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
       keep = scalar(keep_of(ld, n));
     }
     for (int ga = 0; ga < GA; ++ga) {
-      ra[i].store(sa, 0);
-      rb[i].store(sb, b0);
+      ra[i].store(sa);
+      rb[i].store(sb);
       __syncthreads();
       if (ga + 1 < GA) fetch_rows(i, r0, ga + 1);
       else if (r0 + AHEAD * C < hi) fetch_rows(i, r0 + AHEAD * C, 0);
