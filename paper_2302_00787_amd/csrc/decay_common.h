@@ -69,8 +69,6 @@ int launch_join(const JoinSet& a, hipStream_t st);
 // Pool of gradients: the sums over the sequences that read a slot, in their order (zeros where none does).
 int launch_slot_sums(const Call& c, const float* each, float* pool, hipStream_t st);
 
-inline int column_blocks(int wb) { return (wb + 63) / 64; }
-
 struct StepArgs {
   TensorDev Q, K, V, Y;
   float* state;

@@ -462,10 +462,10 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
 }
 
 // ------------------------------------------------------------------------------------------------ rows
-constexpr int cols_waves(int P, int WAVES, bool full, bool shared) { return full && P == 1 && WAVES == 8 && !shared ? 4 : (P == 1 ? 2 : 3); }
+constexpr int cols_waves(int P, int WAVES, bool full, int shared) { return full && P == 1 && WAVES == 8 && !(shared & 1) ? 4 : (P == 1 ? 2 : 3); }
 // Waves to a SIMD: what LDS allows, or registers without spills.
-constexpr int walk_waves(bool full, bool shared) { return full && !shared ? 4 : (full ? 3 : 2); }
-template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
+constexpr int walk_waves(bool full, int shared) { return full && !shared ? 4 : (full ? 3 : 2); }
+template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, int SHARED>
 __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb, int parts) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = kChunk * LDA, PB = kChunk * LDB;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1;             // (two pieces are for results in bf16)
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<false, true>(S, from, w.sa, w.sb, w.wa, w.wb, t.at, t.bt, b0);
-  const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first;
+  const int back = w.back, GX = SHARED & 2 ? w.GX : 1, GA = SHARED & 1 ? w.GA : 1, first = w.first;
   const float s_update = w.s_update;
   const int hq = (p.h * w.parts + p.part) * GX;
   const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, hq);
@@ -586,7 +586,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 // The same by columns: a wave has sixteen columns of the state, all of its rows, in accumulators whose order of rows is that of an operand, so
 // that the state never goes through LDS; the rows x do (every wave needs all of them), and so do the chunk's scores, whose tiles the waves share
 // out.  Chunks of 16 NT rows.
-template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT, bool SHARED>
+template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT, int SHARED>
 __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb, int parts) {
   constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB, NQ = NT / 2;
   constexpr int OUT = P == 1 && PM == 2 ? 1 : -1, TILES = NT * (NT + 1) / 2;
@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<true, false>(S, from, w.sa, w.sb, w.wa, w.wb, 0, 0, bw);
-  const int back = w.back, GX = SHARED ? w.GX : 1, GA = SHARED ? w.GA : 1, first = w.first, wb = w.wb;
+  const int back = w.back, GX = SHARED & 2 ? w.GX : 1, GA = SHARED & 1 ? w.GA : 1, first = w.first, wb = w.wb;
   const float s_update = w.s_update;
   const int hq = (p.h * w.parts + p.part) * GX;
   const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, hq);
@@ -1091,7 +1091,7 @@ int most_parts(const WalkSet& a, int count) {
   return n;
 }
 
-template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, bool SHARED>
+template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, int SHARED>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
@@ -1103,7 +1103,7 @@ int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(256), lds, st, a, ncb, parts);
   return status();
 }
-template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT, bool SHARED>
+template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT, int SHARED>
 int cols_launch(const WalkSet& a, int count, hipStream_t st) {
   constexpr int NT = P == 1 ? 4 : 2, C = 16 * NT, NB = 16 * WAVES;
   int ncb = 1;
@@ -1141,7 +1141,7 @@ int sum_launch(const SumSet& a, int count, hipStream_t st) {
 
 int class_of(int n) { return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
-template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
+template <int P, int PM, int PU, bool FULL, int DT, int SHARED> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
   if (class_of(wa) == 128)
     return wb > 64 ? cols_launch<P, PM, PU, 128, 8, FULL, DT, SHARED>(a, count, st) : cols_launch<P, PM, PU, 128, 4, FULL, DT, SHARED>(a, count, st);
   if constexpr (P == 3) {
@@ -1172,9 +1172,10 @@ template <class F> int each_form(bool full, bool shared, F go) {
 int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, hipStream_t st) {
   WalkSet a = all;
   int wa = 0, wb = 0;
-  bool full = true, ends = false, shared = false;
+  int shared = 0;                // 1: heads of A and B share states, 2: of X
+  bool full = true, ends = false;
   for (int i = 0; i < count; ++i) {
-    shared = shared || all.w[from + i].GX > 1 || all.w[from + i].GA > 1;
+    shared |= (all.w[from + i].GA > 1 ? 1 : 0) | (all.w[from + i].GX > 1 ? 2 : 0);
     a.w[i] = all.w[from + i];
     ends = ends || (a.w[i].end != nullptr && a.c.nseg == 1);
     a.prefix[i] = all.prefix[from + i];
@@ -1183,12 +1184,16 @@ int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, 
     full = full && a.w[i].wa % 8 == 0 && a.w[i].wb % 8 == 0;
   }
   auto go = [&](auto full_rows, auto shared_heads) {
-    constexpr bool F = decltype(full_rows)::value, G = decltype(shared_heads)::value;
+    constexpr bool F = decltype(full_rows)::value;
+    constexpr int G = decltype(shared_heads)::value;
     if (dtype == 0) return walk_width<3, 3, 3, F, 0, G>(a, count, wa, wb, st);
     if (fine) return walk_width<1, 3, 3, F, 1, G>(a, count, wa, wb, st);
     return ends ? walk_width<1, 2, 3, F, 1, G>(a, count, wa, wb, st) : walk_width<1, 2, 2, F, 1, G>(a, count, wa, wb, st);
   };
-  return each_form(full, shared, go);
+  using std::integral_constant;
+  if (!full) return go(std::false_type{}, integral_constant<int, 3>{});
+  if (shared == 0) return go(std::true_type{}, integral_constant<int, 0>{});
+  return shared == 1 ? go(std::true_type{}, integral_constant<int, 1>{}) : shared == 2 ? go(std::true_type{}, integral_constant<int, 2>{}) : go(std::true_type{}, integral_constant<int, 3>{});
 }
 
 // The walks of dK and dV (from, from + 1) as one.
