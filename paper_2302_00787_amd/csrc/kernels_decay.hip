@@ -1,11 +1,21 @@
-// Linear attention with a decay for each head, rows of prompts and of training: chunks of 64 rows, within a chunk by the scores of its rows,
-// between chunks by the state.  See decay_common.h for the formulas.
+// Linear attention with a decay for each head, rows of prompts and of training: chunks of 64 rows (32 of fp32), within a chunk by the scores
+// of its rows, between chunks by the state.  See decay_common.h for the formulas.
 //
-// A workgroup of four waves walks the chunks of a segment of one state, 64 columns of it, whose numbers stay in the accumulators of
-// the waves.  A wave has sixteen rows of x as operands (read once, from memory); it takes their scores with the chunk's rows a (LDS), weighs
-// them by powers of lambda from registers, and multiplies them with the rows b, and x with the state's image (LDS).  Scores and state are fp32
-// and go into the next product as PM bf16 pieces: two (16 bits) where the results are rounded to bf16 (8), three (24) otherwise.  Rows
-// of a in the sums of the state are weighed in 32 bits and have three pieces, as the states themselves are results in fp32.
+// Segments of a sequence are walked side by side: sums of the segments (k_decay_sum), states before them (k_decay_join), then the walks.
+//   k_decay_walk  rows of bf16 up to 64 numbers.  A wave has sixteen rows of x as operands, read once from memory, and results in whole rows;
+//                 the state's numbers are shared out to the waves' accumulators and reach the others as an image in LDS.
+//   k_decay_cols  wider rows, and all of fp32.  A wave has sixteen columns of the state and of the results, the rows x go through LDS: the
+//                 state never does (an image of 128 x 128 in three pieces would take 96 KB).
+//   k_decay_back  dK and dV of rows up to 64 in one walk: q, dy and the state are read once for both.
+// Scores and states are fp32 and go into the next product as PM bf16 pieces: two (16 bits) where the results are rounded to bf16 (8), three
+// (24) otherwise.  Weighed rows in the sums of a state have PU pieces, three where the state itself is a result.
+//
+// What bounds them: memory up to 64 numbers (4 x 8 states, 16384 rows of 64 in bf16: sums 27 us, 134 MB, a walk 55, 268 MB, dK and dV 84, 403 MB:
+// 4.8 - 5.0 TB/s, where a large copy reaches 5.2), and nearly as much the CU: rows that are in the L2 already take as long for one walk, 70 instead
+// of 82 us with the sums.  Of the cycles of a SIMD there 37 % issue vector and 25 % run matrix instructions, the LDS is busy for about half; two, three
+// or four workgroups a CU make no difference.  Rows of 128 in bf16 (16 states, 65536 rows: sums 143 us, the walk 280, 3.8 TB/s) the CU: rows in the
+// L2 take 318 of 386 us; vector instructions 42 %, matrix 33 %, four barriers a chunk between them; four waves of 32 columns each, with a third
+// fewer reads of the LDS, take as long.  Rows of fp32 six matrix products for one (three pieces of each side).
 #include "decay_common.h"
 
 #include <type_traits>
@@ -19,6 +29,7 @@ using st::Raw8;
 using st::f32x8;
 using st::each_product;
 using st::read_tr;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }      // (a scalar: branches on it, too)
 __device__ __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
@@ -43,6 +54,11 @@ __device__ __forceinline__ int afresh_lane(int x) {
 // Operands of a part of a chunk are not fetched before the part: that would take registers that hold more waves otherwise.
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
+// What a piece leaves of four numbers that are summed, exact.
+__device__ __forceinline__ f32x4 rest_of(f32x4 x, bf16x4 h) {
+  const f32x2_t a = less_piece(f32x2_t{x[0], x[1]}, bf16x2_t{h[0], h[1]}), b = less_piece(f32x2_t{x[2], x[3]}, bf16x2_t{h[2], h[3]});
+  return f32x4{a[0], a[1], b[0], b[1]};
+}
 template <int P> __device__ __forceinline__ Op<P> pieces(f32x8 x) {
   if constexpr (P == 2) {          // (numbers that are summed: one that is not finite makes its neighbour NaN)
     u32x4 h, m;
@@ -126,7 +142,6 @@ struct Head {
     return {at + i * next + (long long)(back ? len - r0 - n : r0) * pitch, n, pitch, back};
   }
 };
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
 // Numbers from row to row in LDS: neither rows that sixteen lanes read nor columns that they read transposed meet in a bank so (8 more than the
 // width: twice the cycles for both).
@@ -462,8 +477,8 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
 }
 
 // ------------------------------------------------------------------------------------------------ rows
-constexpr int cols_waves(int P, int WAVES, bool full, int shared) { return full && P == 1 && WAVES == 8 && !(shared & 1) ? 4 : (P == 1 ? 2 : 3); }
 // Waves to a SIMD: what LDS allows, or registers without spills.
+constexpr int cols_waves(int P, int WAVES, bool full, int shared) { return full && P == 1 && WAVES == 8 && !(shared & 1) ? 4 : (P == 1 ? 2 : 3); }
 constexpr int walk_waves(bool full, int shared) { return full && !shared ? 4 : (full ? 3 : 2); }
 template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, int SHARED>
 __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb, int parts) {
@@ -527,7 +542,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
         for (int k = 0; k < PM; ++k) {
           const bf16x4 h = __builtin_convertvector(x, bf16x4);
           *(bf16x4*)(to + k * 512) = h;
-          x -= __builtin_convertvector(h, f32x4);
+          if (k + 1 < PM) x = rest_of(x, h);
         }
       }
   };
@@ -675,7 +690,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
           for (int m = 0; m < PM; ++m) {
             const bf16x4 h = __builtin_convertvector(v, bf16x4);
             *(bf16x4*)(to + m * 512) = h;
-            v -= __builtin_convertvector(h, f32x4);
+            if (m + 1 < PM) v = rest_of(v, h);
           }
         }
         if (ga == 0) {
@@ -783,7 +798,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   if (ends) store_state<true, false>(S, w.end + (w.end_pool ? (size_t)p.slot * c.Hk + p.h : (size_t)s) * c.state, w.sa, w.sb, w.wa, w.wb, 0, 0, bw);
 }
 
-// Gradients of keys and values in one walk from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
+// Gradients of keys and values in one walk (two walks of rows of 64 in bf16 read 403 MB where this one reads 268) from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
 // dy behind, in LDS as rows of D', of which the one takes columns and the other rows.  set.w[0]: the values (X = V, A = dY, B = Q, Y = dK),
 // set.w[1]: the keys (X = K, A = Q, B = dY, Y = dV).
 template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
@@ -991,10 +1006,10 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
   store_state<false, false>(S, set.part[blockIdx.y] + (s * c.nseg + p.seg) * c.state, w.sa, w.sb, w.wa, w.wb, 0, 0, b0 + 16 * wave);
 }
 
-// Sums of the segments -> states before them, in place; up to 32 segments on their way at a time (24 segments of 32 states of 64 x 64, eight
-// at a time: 9.4 us).
-__global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
-  constexpr int MANY = 32;
+// Sums of the segments -> states before them, in place; up to MANY segments on their way at a time.  What is read behind the segments that have
+// sums is zeros, what is written behind those that have rows is nowhere: no branches (24 segments of 32 states of 64 x 64: 12.4 us with them, 9.6
+// so, of which a launch with a load and a store is about 5).
+template <int MANY> __global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
   const Call& c = set.c;
   const int which = blockIdx.z, s = blockIdx.y, b = s / c.Hk, h = s - b * c.Hk;
   int len = c.lengths ? max(0, min(c.lengths[b], c.L)) : c.L, slot;
@@ -1004,30 +1019,31 @@ __global__ void __launch_bounds__(256) k_decay_join(JoinSet set) {
   } else {
     slot = st::slot_of(c.slots, c.nslots, b);
   }
-  const int id = blockIdx.x * 256 + threadIdx.x;
+  const int id = blockIdx.x * 256 + threadIdx.x, size = c.state * 4;
   if (id >= c.state) return;
   const int held = __builtin_amdgcn_readfirstlane((len + c.seg_rows - 1) / c.seg_rows);       // segments with rows
   // the last segment's sum is there (and wanted) where the states after it are
   const int sums = set.end[which] != nullptr ? held : min(held, c.nseg - 1);
-  float* part = set.part[which] + (size_t)s * c.nseg * c.state + id;
+  const float* part = set.part[which] + (size_t)s * c.nseg * c.state;
+  const __amdgpu_buffer_rsrc_t from = buffer_of(part, sums * size), to = buffer_of(part, held * size);
   const float* init = set.init[which];
   float v[MANY];
 #pragma unroll
-  for (int i = 0; i < MANY; ++i) v[i] = i < sums ? part[(size_t)i * c.state] : 0.f;
+  for (int i = 0; i < MANY; ++i) v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, 4 * id + i * size, 0, 0));
   float S = init != nullptr && slot >= 0 ? init[((size_t)slot * c.Hk + h) * c.state + id] : 0.f;
   const float ld = c.log_decay[h];
-  const Keep whole = keep_of(ld, c.seg_rows), last = keep_of(ld, len - (held - 1) * c.seg_rows);
+  const Keep whole = scalar(keep_of(ld, c.seg_rows)), last = scalar(keep_of(ld, len - (held - 1) * c.seg_rows));
   for (int s0 = 0; s0 < held; s0 += MANY) {
     if (s0 > 0) {
 #pragma unroll
-      for (int i = 0; i < MANY; ++i) v[i] = s0 + i < sums ? part[(size_t)(s0 + i) * c.state] : 0.f;
+      for (int i = 0; i < MANY; ++i) v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, 4 * id + (s0 + i) * size, 0, 0));
     }
 #pragma unroll
-    for (int i = 0; i < MANY; ++i)
-      if (s0 + i < held) {
-        part[(size_t)(s0 + i) * c.state] = S;
-        S = kept(s0 + i == held - 1 ? last : whole, S) + v[i];
-      }
+    for (int i = 0; i < MANY; ++i) {
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S), to, 4 * id + (s0 + i) * size, 0, 0);
+      const float next = kept(s0 + i == held - 1 ? last : whole, S) + v[i];
+      S = s0 + i < held ? next : S;
+    }
   }
   if (set.end[which] != nullptr && (slot >= 0 || !set.end_pool[which]))
     set.end[which][(set.end_pool[which] ? (size_t)slot * c.Hk + h : (size_t)s) * c.state + id] = S;
@@ -1079,7 +1095,7 @@ __global__ void __launch_bounds__(256) k_decay_slot_sums(Call c, const float* ea
 
 int status() { return hipGetLastError() == hipSuccess ? 0 : 5; }
 
-// More LDS than a launch has by itself is asked for once for a kernel and device.
+// More LDS than a launch has by itself is asked for before it, on its device.
 template <class K> int room(K kernel, size_t bytes) {
   if (bytes <= 65536) return 0;
   return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? 0 : 5;
@@ -1233,7 +1249,9 @@ int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st) {
 }
 
 int launch_join(const JoinSet& a, hipStream_t st) {
-  hipLaunchKernelGGL(k_decay_join, dim3((a.c.state + 255) / 256, a.c.B * a.c.Hk, a.count), dim3(256), 0, st, a);
+  const dim3 grid((a.c.state + 255) / 256, a.c.B * a.c.Hk, a.count);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
+  a.c.nseg <= 8 ? go(k_decay_join<8>) : a.c.nseg <= 16 ? go(k_decay_join<16>) : a.c.nseg <= 24 ? go(k_decay_join<24>) : go(k_decay_join<32>);
   return status();
 }
 

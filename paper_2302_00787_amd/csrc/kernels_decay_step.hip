@@ -3,6 +3,8 @@
 // The state is read and written once, which bounds it.  A workgroup has all rows of a state and 4 C4 of its columns: the columns of y are its
 // own, so that nothing is joined.  A thread has four columns of every (256 / C4)th row, all of them on their way before anything is waited for,
 // and keeps them for the query heads that share the state; y is summed over lanes, then over waves, for four heads at a time.
+// 256 x 8 states of 64 x 64, 69 MB: 12.2 us, 5.6 TB/s (in the last cache in part); 8 states: 4.8 us, a launch and a chain of two loads; 45 x 4
+// states of 128 x 128 with four heads each: 9.0.
 #include "decay_common.h"
 
 #include <type_traits>
