@@ -14,7 +14,7 @@
 // 4.8 - 5.0 TB/s, where a large copy reaches 5.2), and nearly as much the CU: rows that are in the L2 already take as long for one walk, 70 instead
 // of 82 us with the sums.  Of the cycles of a SIMD there 37 % issue vector and 25 % run matrix instructions, the LDS is busy for about half; two, three
 // or four workgroups a CU make no difference.  Rows of 128 in bf16 (16 states, 65536 rows: sums 143 us, the walk 280, 3.8 TB/s) the CU: rows in the
-// L2 take 318 of 386 us; vector instructions 42 %, matrix 33 %, four barriers a chunk between them; four waves of 32 columns each, with a third
+// L2 take 318 of 386 us; vector instructions 42 %, matrix 33 %, three barriers a chunk between them; four waves of 32 columns each, with a third
 // fewer reads of the LDS, take as long.  Rows of fp32 six matrix products for one (three pieces of each side).
 #include "decay_common.h"
 
