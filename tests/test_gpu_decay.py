@@ -256,6 +256,21 @@ def test_heads_that_share_states(fs, dtype, d, L, H, Hk):
             close(got[3][b], want[3], F32)
 
 
+@pytest.mark.parametrize("dtype,L", [("bf16", 130), ("f32", 33)])
+def test_many_heads_of_one_state(fs, dtype, L):
+    import torch
+    c = Case(fs, dtype, 1, 64, 1, L, 64, 64, "slow")
+    Y = fs.decay_attention(c.Q, c.K, c.V, c.g, c.s)
+    got = fs.decay_attention_backward(c.Q, c.K, c.V, c.dY, c.g, c.s)
+    close(Y[0], c.forward(0)[0], tolerance(dtype))
+    for x, w in zip(got[:3], c.backward(0)):
+        close(x[0], w, tolerance(dtype))
+    pool = torch.zeros((1, 1, 64, 64), device="cuda")
+    for i in range(3):
+        y = fs.decay_step(pool, *(x[:, :, i:i + 1] for x in (c.Q, c.K, c.V)), c.g, c.s)
+        close(y[0, :, 0], c.forward(0)[0][:, i], tolerance(dtype))
+
+
 def test_one_row_of_any_stride(fs):
     """Sequences of one row: from row to row their tensors may have any stride."""
     import torch
@@ -437,6 +452,39 @@ def test_gradients_against_differences(fs):
         want = (value(*up) - value(*down)) / 2
         size = (grad.double() * direction.double()).norm()
         assert abs(float((grad.double() * direction.double()).sum() - want)) <= 1e-4 * float(size) + 1e-3
+
+
+# ------------------------------------------------------------------------------------------------ numbers that are not finite
+@pytest.mark.parametrize("dtype,d,L", [("bf16", 64, 330), ("bf16", 128, 330), ("f32", 128, 330), ("f32", 32, 1300), ("bf16", 64, 1300)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_numbers_that_are_not_finite_stay_in_their_chunk_and_behind_it(fs, dtype, d, L, bad):
+    """Rows of chunks before the one with the number, other heads and sequences: bit for bit as without it; gradients of rows behind its chunk,
+    too (they are summed from the last row on)."""
+    import torch
+    c = Case(fs, dtype, 2, 4, 2, L, d, d, "slow")
+    t = [x.clone() for x in (c.Q, c.K, c.V, c.dY)]
+    row = 200
+    for which in (1, 2, 3):
+        with_it = [x.clone() for x in t]
+        with_it[which][1, 1, row, 3] = bad                   # a key head, or a query head of the first key head
+        states = [torch.empty_like(c.S0) for _ in range(2)]
+        Y, Z = (fs.decay_attention(*x[:3], c.g, c.s, before=c.S0, after=S) for x, S in zip((t, with_it), states))
+        got, new = (fs.decay_attention_backward(*x, c.g, c.s, before=c.S0) for x in (t, with_it))
+        assert torch.equal(Y[0], Z[0]) and torch.equal(states[0][0], states[1][0])
+        assert all(torch.equal(x[0], y[0]) for x, y in zip(got, new))
+        first = row // 64 * 64
+        assert torch.equal(Y[1, :, :first], Z[1, :, :first])
+        other = 0 if which < 3 else 1                         # a key head without the number, and its query heads
+        q = slice(2 * other, 2 * other + 2)
+        assert torch.equal(Y[1, q], Z[1, q]) and torch.equal(states[0][1, other], states[1][1, other])
+        assert torch.equal(got[0][1, q], new[0][1, q]) and all(torch.equal(x[1, other], y[1, other]) for x, y in zip(got[1:], new[1:]))
+        if which < 3:
+            assert not Z[1, 2:, row].isfinite().all() and torch.equal(got[0][1, :, :first], new[0][1, :, :first])
+        else:
+            # the walk from the last row counts its chunks, and those of its segments, from there
+            after = slice(row + 64, L)
+            assert all(torch.equal(x[1, :, after], y[1, :, after]) for x, y in zip(got[1:3], new[1:3]))
+            assert not new[2][1, 0, :row].isfinite().all()
 
 
 # ------------------------------------------------------------------------------------------------ strides, streams, graphs, workspaces

@@ -60,6 +60,19 @@ def test_rows(fs, dtype, interleaved, B, H, H2, L, d, pairs, order):
     assert torch.equal(again, fs.rotary(X, rot))
 
 
+@pytest.mark.parametrize("pairs,order", [([2, 3, 1, 4, 5, 1], "cyclic"), ([4] * 8, "blocks"), ([0, 3, 0, 0, 2, 0, 0, 3], "cyclic")])
+def test_many_axes(fs, pairs, order):
+    import torch
+    gen = torch.Generator().manual_seed(sum(pairs))
+    freqs, axis_of = fs.rotary_sections(pairs, order=order)
+    places = torch.randint(0, 1 << 16, (len(pairs), 2, 37), generator=gen, dtype=torch.int32)
+    x = torch.randn((2, 3, 37, 64), generator=gen)
+    got = fs.rotary(x.cuda(), fs.RotaryAxes(freqs, axis_of, places.cuda()))
+    want = turned(x.double(), freqs.cpu(), axis_of.cpu(), places, False, 1.0, False)
+    length = x.double().abs().amax(-1, keepdim=True) * math.sqrt(2.0)
+    assert ((got.double().cpu() - want).abs() <= 6 * 2.0 ** -24 * torch.maximum(length, want.abs())).all()
+
+
 def test_one_axis_and_equal_axes_are_plain_positions(fs):
     """Bit for bit: a text's rows, whose positions are the same on all axes, are turned as by plain positions."""
     import torch
