@@ -486,8 +486,8 @@ typedef struct {
 } fs_decay_state;
 
 /* Rows Q [B, H, L, d], K [B, heads, L, d], V [B, heads, L, dv] after what the states `before` hold (NULL: empty ones) -> Y [B, H, L, dv],
- * and the states after the last row into `after` (NULL: not wanted; the same pool as `before`: in place; another: as many slots, those
- * that no sequence names stay as they are; no other overlap).  left_out (device int32, or NULL): the number of sequences that were left
+ * and the states after the last row into `after` (NULL: not wanted; the same pool as `before`: in place, as if it were another; another: as
+ * many slots, those that no sequence names stay as they are; no other overlap).  left_out (device int32, or NULL): the number of sequences that were left
  * out is ADDED to it. */
 size_t favorsharp_decay_attention_workspace_bytes(int B, int H, int heads, int L, int d, int dv);
 int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_tensor* V, int B, int H, int heads, int L, int d, int dv,

@@ -18,7 +18,7 @@ constexpr long long kMaxRows = 1 << 29;          // rows of one state in a call:
 // their own where that does, too.
 struct Plan {
   int nseg, seg_rows, parts;
-  size_t states, ends, total;                    // bytes of one set of segment states; of the states that end a walk
+  size_t states, ends, total;                    // bytes of one set of segment states; of the states that end a walk; of a workspace
 };
 Plan plan(int B, int H, int heads, int L, int d, int dv, int sets, bool ends) {
   Plan p;
@@ -40,7 +40,13 @@ Plan plan(int B, int H, int heads, int L, int d, int dv, int sets, bool ends) {
   p.total = sets * p.states + p.ends;
   return p;
 }
-Plan plan_forward(int B, int H, int heads, int L, int d, int dv) { return plan(B, H, heads, L, d, dv, 1, false); }
+// Workgroups that share the heads of a state read the pool that one of them would write where a call is in place: the states after it stay in
+// the workspace until all have ended.  (Segments read copies of the states before them.)
+Plan plan_forward(int B, int H, int heads, int L, int d, int dv) {
+  Plan p = plan(B, H, heads, L, d, dv, 1, false);
+  if (p.nseg == 1 && p.parts > 1) p.total = p.ends = align_up((size_t)B * heads * d * dv * sizeof(float));
+  return p;
+}
 Plan plan_backward(int B, int H, int heads, int L, int d, int dv, bool dbefore) { return plan(B, H, heads, L, d, dv, 2, dbefore); }
 
 int sizes(int B, int H, int heads, int L, int d, int dv) {
@@ -99,15 +105,17 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
   if (Q->dtype != K->dtype || Q->dtype != V->dtype) return FS_ERR_INVALID_ARG;
   if (!strides_ok({Q, K, V, Y}, L)) return FS_ERR_UNSUPPORTED;
   const Plan p = plan_forward(B, H, heads, L, d, dv);
-  if (p.total > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
-  if (workspace_bytes < p.total) return FS_ERR_WORKSPACE_TOO_SMALL;
+  const bool apart = p.ends > 0 && before != nullptr && after != nullptr && before->S == after->S;
+  const size_t need = p.states + (apart ? p.ends : 0);
+  if (need > 0 && workspace == nullptr) return FS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return FS_ERR_WORKSPACE_TOO_SMALL;
   if (L == 0 && after == nullptr) return FS_OK;
   hipStream_t s = (hipStream_t)stream;
-  float* states = (float*)workspace;
+  float *states = (float*)workspace, *ends = (float*)((char*)workspace + p.states);
   dec::WalkSet a{};
   a.c = call_of(B, heads, L, d, dv, log_decay, lengths, slots, nslots, after != nullptr, p, left_out);
   a.w[0] = dec::Walk{rows_of(Q, L), rows_of(K, L), rows_of(V, L), rows_of(Y, L), H / heads / p.parts, 1, p.parts, d, dv, scale, scale, 1.f, 1, 0, before ? before->S : nullptr,
-                     after ? after->S : nullptr, dv, 1, 1};
+                     apart ? ends : (after ? after->S : nullptr), dv, 1, apart ? 0 : 1};
   a.prefix[0] = states;
   if (p.nseg > 1) {
     dec::SumSet m{};
@@ -126,7 +134,8 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
     j.count = 1;
     if (int rc = dec::launch_join(j, s)) return rc;
   }
-  return dec::launch_walks(a, 0, 1, Q->dtype, Y->dtype == FS_F32, s);
+  if (int rc = dec::launch_walks(a, 0, 1, Q->dtype, Y->dtype == FS_F32, s)) return rc;
+  return apart ? dec::launch_put(a.c, ends, after->S, s) : FS_OK;
 }
 
 size_t favorsharp_decay_attention_backward_workspace_bytes(int B, int H, int heads, int L, int d, int dv, int with_dbefore) {

@@ -66,6 +66,8 @@ int launch_walks(const WalkSet& a, int from, int count, int dtype, bool fine, hi
 int launch_back(const WalkSet& a, int from, int dtype, bool fine, hipStream_t st);
 int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st);
 int launch_join(const JoinSet& a, hipStream_t st);
+// States [state] of the sequences that have a slot of their own, into the pool.
+int launch_put(const Call& c, const float* each, float* pool, hipStream_t st);
 // Pool of gradients: the sums over the sequences that read a slot, in their order (zeros where none does).
 int launch_slot_sums(const Call& c, const float* each, float* pool, hipStream_t st);
 

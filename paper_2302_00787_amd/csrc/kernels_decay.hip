@@ -1049,6 +1049,13 @@ template <int MANY> __global__ void __launch_bounds__(256) k_decay_join(JoinSet 
     set.end[which][(set.end_pool[which] ? (size_t)slot * c.Hk + h : (size_t)s) * c.state + id] = S;
 }
 
+// States that a call in place has kept apart, into their slots (a launch of its own: what reads the pool has ended).
+__global__ void __launch_bounds__(256) k_decay_put(Call c, const float* each, float* pool) {
+  const int s = blockIdx.y, b = s / c.Hk, h = s - b * c.Hk, id = blockIdx.x * 256 + threadIdx.x;
+  const int slot = st::unique_slot_of(c.slots, c.nslots, b);
+  if (slot >= 0 && id < c.state) pool[((size_t)slot * c.Hk + h) * c.state + id] = each[(size_t)s * c.state + id];
+}
+
 // Sums of the readers of a slot, for 64 numbers of its states a workgroup: its sixteen groups of sixteen lanes take every sixteenth
 // reader each, in their order, and are then added in theirs.
 __global__ void __launch_bounds__(256) k_decay_slot_sums(Call c, const float* each, float* pool) {
@@ -1252,6 +1259,11 @@ int launch_join(const JoinSet& a, hipStream_t st) {
   const dim3 grid((a.c.state + 255) / 256, a.c.B * a.c.Hk, a.count);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
   a.c.nseg <= 8 ? go(k_decay_join<8>) : a.c.nseg <= 16 ? go(k_decay_join<16>) : a.c.nseg <= 24 ? go(k_decay_join<24>) : go(k_decay_join<32>);
+  return status();
+}
+
+int launch_put(const Call& c, const float* each, float* pool, hipStream_t st) {
+  hipLaunchKernelGGL(k_decay_put, dim3((c.state + 255) / 256, c.B * c.Hk), dim3(256), 0, st, c, each, pool);
   return status();
 }
 

@@ -131,3 +131,16 @@ def test_tensors_of_the_host_are_refused(fs):  # noqa: F811
         fs.decay_attention(t, t, t, g, before=torch.zeros(3, 2, 8, 8), after=torch.zeros(2, 2, 8, 8))
     with pytest.raises(ValueError, match="shape"):
         fs.decay_attention_backward(t, t, t, t[..., :4], g)
+
+
+@pytest.mark.parametrize("B,H,heads,L,d,dv", [(60, 24, 8, 64, 64, 64), (60, 24, 8, 1, 64, 64), (45, 12, 4, 64, 128, 128), (16, 64, 8, 190, 128, 128), (1, 2, 1, 1, 8, 8),
+                                              (63, 16, 8, 448, 64, 64), (3, 4, 2, 0, 64, 40)])
+def test_shared_heads_in_place_keep_their_states_apart(fs, B, H, heads, L, d, dv):  # noqa: F811
+    """One segment, query heads in workgroups of their own: none of them may write the pool that the others read, so the states after an
+    in-place call need a workspace."""
+    need = fs.lib().favorsharp_decay_attention_workspace_bytes(B, H, heads, L, d, dv)
+    assert need >= B * heads * d * dv * 4
+    t = tensor(fs, 128)
+    for nbytes, ws, want in ((0, None, INVALID), (need - 1, A, SMALL)):
+        assert forward(fs, t, t, t, t, B, H, heads, L, d, dv, before=pool(fs, slots=B), after=pool(fs, slots=B), ws=ws, nbytes=nbytes) == want
+    assert fs.lib().favorsharp_decay_attention_workspace_bytes(B, heads, heads, min(L, 64), d, dv) == 0       # heads of their own

@@ -566,3 +566,50 @@ def test_what_lies_around_the_results(fs):
     assert (kept == 9.0).all()
     for b in range(2):
         close(Y[b], c.forward(b)[0], BF16)
+
+
+# ------------------------------------------------------------------------------------------------ heads that share states, in place
+@pytest.mark.parametrize("dtype,B,H,Hk,L,d,dv", [("bf16", 60, 24, 8, 1, 64, 64), ("bf16", 60, 24, 8, 64, 64, 64), ("f32", 45, 12, 4, 64, 128, 128), ("bf16", 63, 32, 8, 200, 64, 40),
+                                                 ("bf16", 16, 64, 8, 190, 128, 128), ("f32", 60, 64, 8, 33, 24, 33)])
+def test_in_place_is_as_into_another_pool(fs, dtype, B, H, Hk, L, d, dv):
+    """More workgroups than the chip holds, whose heads read the states that the call goes on from: bit for bit what a call into another pool
+    gives, with a padded batch, a sequence without a slot and one that has another's."""
+    import torch
+    c = Case(fs, dtype, B, H, Hk, L, d, dv, "slow", [L if b % 3 else 1 + b * L // (2 * B) for b in range(B)])
+    slots = torch.randperm(B + 2, generator=torch.Generator().manual_seed(B)).to(torch.int32)[:B]
+    slots[3], slots[5] = -1, slots[2]
+    slots = slots.cuda()
+    start = torch.randn((B + 2, Hk, d, dv), generator=torch.Generator().manual_seed(L)).cuda()
+    other, counts = start.clone(), torch.zeros(2, dtype=torch.int32, device="cuda")
+    want = fs.decay_attention(c.Q, c.K, c.V, c.g, c.s, before=start, after=other, lengths=c.lengths, slots=slots, left_out=counts[:1])
+    room = fs.lib().favorsharp_decay_attention_workspace_bytes(B, H, Hk, L, d, dv)
+    ws = torch.full((room + 256,), 77, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        pool = start.clone()
+        got = fs.decay_attention(c.Q, c.K, c.V, c.g, c.s, before=pool, after=pool, lengths=c.lengths, slots=slots, left_out=counts[1:], workspace=ws[:room])
+        assert torch.equal(got, want) and torch.equal(pool, other)
+    assert counts.tolist() == [2, 6] and (ws[room:] == 77).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 96)])
+def test_shared_heads_in_place(fs, dtype, d):
+    """Sequences of 1 to 190 rows, eight query heads to a key head: every head and state against the recurrence, eager and replayed."""
+    import torch
+    B, H, Hk, L = 16, 32, 4, 190
+    c = Case(fs, dtype, B, H, Hk, L, d, d, "slow", [1 + (b * 63) % L for b in range(B)])
+    pool = c.S0.clone()
+    call = lambda: fs.decay_attention(c.Q, c.K, c.V, c.g, c.s, before=pool, after=pool, lengths=c.lengths)      # noqa: E731
+    Y = call()
+    for b in range(B):
+        y, S = c.forward(b, c.S0[b])
+        close(Y[b], y, tolerance(dtype))
+        close(pool[b], S, F32)
+    end = pool.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for _ in range(3):
+        pool.copy_(c.S0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, Y) and torch.equal(pool, end)
