@@ -471,9 +471,7 @@ int favorsharp_state_append_backward(const fs_features* host_features, const fs_
  *   slots, lengths: as for the states above.  Rows l >= lengths[b] are padding: not read, their output rows are zeros.  Where a call
  *   writes states a sequence whose slot is not in the pool, or is also that of an earlier sequence, is left out: its state
  *   stays, its output rows are zeros.  Where it reads them alone sequences may share a slot; those without one are as if it were empty.
- *   All products have the accuracy of fp32 for f32 tensors; for bf16 tensors the states have it, and so have rows that are written
- *   in f32, while rows that are rounded to bf16 have scores and states rounded to 16 bits before their products.  Results are
- *   rounded once, to their dtype.  Numbers below 2^-109 lose bits, as the rest of a number has no exponent there.
+ *   All sums and products have the accuracy of fp32, for tensors of either dtype; results are rounded once, to their dtype.  Numbers below 2^-109 lose bits, as the rest of a number has no exponent there.
  *   log_decay and scale are constants: there is no gradient with respect to them.
  *   d, dv <= 128 (the columns of V and S are independent of each other: wider values are calls on parts of them), B H and
  *   slots * heads <= 65535, L H / heads <= 2^29, stride_l <= 2^22 of tensors of rows.  Q, K, V and dY of a call share a dtype.

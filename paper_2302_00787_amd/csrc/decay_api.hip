@@ -123,7 +123,6 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
     m.w[0] = a.w[0];
     m.part[0] = states;
     m.last = after != nullptr;
-    m.fine = after != nullptr || Y->dtype == FS_F32;
     if (int rc = dec::launch_sums(m, 1, Q->dtype, s)) return rc;
     dec::JoinSet j{};
     j.c = a.c;
@@ -134,7 +133,7 @@ int favorsharp_decay_attention(const fs_tensor* Q, const fs_tensor* K, const fs_
     j.count = 1;
     if (int rc = dec::launch_join(j, s)) return rc;
   }
-  if (int rc = dec::launch_walks(a, 0, 1, Q->dtype, Y->dtype == FS_F32, s)) return rc;
+  if (int rc = dec::launch_walks(a, 0, 1, Q->dtype, s)) return rc;
   return apart ? dec::launch_put(a.c, ends, after->S, s) : FS_OK;
 }
 
@@ -174,7 +173,6 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
   a.w[2] = dec::Walk{rows_of(K, L), rows_of(Q, L), rows_of(dY, L), rows_of(dV, L), 1, G, 1, d, dv, scale, 1.f, scale, 0, 1, last, end, dv, 1, direct ? 1 : 0};
   a.prefix[0] = prefix;
   a.prefix[1] = a.prefix[2] = suffix;
-  const bool fine = dQ->dtype == FS_F32 || dK->dtype == FS_F32 || dV->dtype == FS_F32;
   if (p.nseg > 1) {
     dec::SumSet m{};
     m.c = a.c;
@@ -183,7 +181,6 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
     m.part[0] = prefix;
     m.part[1] = suffix;
     m.last = dbefore != nullptr;
-    m.fine = dbefore != nullptr || fine;
     if (int rc = dec::launch_sums(m, 2, Q->dtype, s)) return rc;
     dec::JoinSet j{};
     j.c = a.c;
@@ -201,9 +198,9 @@ int favorsharp_decay_attention_backward(const fs_tensor* Q, const fs_tensor* K, 
   const bool one = std::max(d, dv) <= 64 && (Q->dtype == FS_BF16 || std::max(d, dv) <= 32 || G > 1);
   // dQ by itself where heads share states: the other two have a form of their own then
   const bool alone = one || G > 1;
-  if (int rc = dec::launch_walks(a, 0, alone ? 1 : 3, Q->dtype, fine, s)) return rc;
+  if (int rc = dec::launch_walks(a, 0, alone ? 1 : 3, Q->dtype, s)) return rc;
   if (alone)
-    if (int rc = one ? dec::launch_back(a, 1, Q->dtype, fine, s) : dec::launch_walks(a, 1, 2, Q->dtype, fine, s)) return rc;
+    if (int rc = one ? dec::launch_back(a, 1, Q->dtype, s) : dec::launch_walks(a, 1, 2, Q->dtype, s)) return rc;
   return dbefore != nullptr && !direct ? dec::launch_slot_sums(a.c, ends, dbefore->S, s) : FS_OK;
 }
 

@@ -51,7 +51,6 @@ struct SumSet {
   Walk w[2];                     // A, B, GA, wa, wb, s_update, first, back
   float* part[2];
   int last;                      // the last segment is wanted, too
-  int fine;                      // sums to 24 bits for rows of bf16, too
 };
 // Sums become states before the segments.
 struct JoinSet {
@@ -62,8 +61,8 @@ struct JoinSet {
   int end_pool[2];
   int count;
 };
-int launch_walks(const WalkSet& a, int from, int count, int dtype, bool fine, hipStream_t st);
-int launch_back(const WalkSet& a, int from, int dtype, bool fine, hipStream_t st);
+int launch_walks(const WalkSet& a, int from, int count, int dtype, hipStream_t st);
+int launch_back(const WalkSet& a, int from, int dtype, hipStream_t st);
 int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st);
 int launch_join(const JoinSet& a, hipStream_t st);
 // States [state] of the sequences that have a slot of their own, into the pool.

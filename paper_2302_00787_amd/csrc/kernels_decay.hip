@@ -7,8 +7,8 @@
 //   k_decay_cols  wider rows, and all of fp32.  A wave has sixteen columns of the state and of the results, the rows x go through LDS: the
 //                 state never does (an image of 128 x 128 in three pieces would take 96 KB).
 //   k_decay_back  dK and dV of rows up to 64 in one walk: q, dy and the state are read once for both.
-// Scores and states are fp32 and go into the next product as PM bf16 pieces: two (16 bits) where the results are rounded to bf16 (8), three
-// (24) otherwise.  Weighed rows in the sums of a state have PU pieces, three where the state itself is a result.
+// Scores, states and the weighed rows in the sums of a state are fp32 and go into the next product as three bf16 pieces (24 bits), for results of
+// either dtype: what a query reads of a state can be far smaller than the state (rows with a mean), and of two pieces' 16 bits it would keep too few.
 //
 // What bounds them: memory up to 64 numbers (4 x 8 states, 16384 rows of 64 in bf16: sums 27 us, 134 MB, a walk 55, 268 MB, dK and dV 84, 403 MB:
 // 4.8 - 5.0 TB/s, where a large copy reaches 5.2), and nearly as much the CU: rows that are in the L2 already take as long for one walk, 70 instead
@@ -59,24 +59,8 @@ __device__ __forceinline__ f32x4 rest_of(f32x4 x, bf16x4 h) {
   const f32x2_t a = less_piece(f32x2_t{x[0], x[1]}, bf16x2_t{h[0], h[1]}), b = less_piece(f32x2_t{x[2], x[3]}, bf16x2_t{h[2], h[3]});
   return f32x4{a[0], a[1], b[0], b[1]};
 }
-template <int P> __device__ __forceinline__ Op<P> pieces(f32x8 x) {
-  if constexpr (P == 2) {          // (numbers that are summed: one that is not finite makes its neighbour NaN)
-    u32x4 h, m;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x2_t v = {x[2 * i], x[2 * i + 1]};
-      const bf16x2_t top = __builtin_convertvector(v, bf16x2_t);
-      h[i] = __builtin_bit_cast(uint32_t, top);
-      m[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(less_piece(v, top), bf16x2_t));
-    }
-    Op<2> o;
-    o.p[0] = __builtin_bit_cast(bf16x8, h);
-    o.p[1] = __builtin_bit_cast(bf16x8, m);
-    return o;
-  } else {
-    return st::as_op<P>(x);
-  }
-}
+constexpr int kPieces = 3;                                  // of a number of 32 bits
+__device__ __forceinline__ Op<kPieces> pieces(f32x8 x) { return st::as_op<kPieces>(x); }
 template <int P> __device__ __forceinline__ f32x8 number(const Op<P>& o) {
   f32x8 x = __builtin_convertvector(o.p[P - 1], f32x8);
 #pragma unroll
@@ -268,11 +252,10 @@ template <int P, int STEPS, bool FULL, int DT> struct RowOps {
 // heads of 64 in bf16, forward and backward: 201 -> 184 us).  Not those of the walk by columns: pieces of 32 bytes, which the caches join
 // (410 -> 492 us).
 constexpr int kStream = 2;
-// Numbers b0 + 32 k + 8 g .. of a wave's rows, which two accumulators have, to a result; OUT: its dtype where the kernel knows it (-1: it does
-// not).
-template <int TB, bool FULL, int OUT> struct RowStore {
+// Numbers b0 + 32 k + 8 g .. of a wave's rows, which two accumulators have, to a result.
+template <int TB, bool FULL> struct RowStore {
   int row, b, wb, size;
-  __device__ __forceinline__ RowStore(const Head& h, int dtype, int b0, int width, int back) : wb(width), size((OUT < 0 ? dtype : OUT) == 0 ? 4 : 2) {
+  __device__ __forceinline__ RowStore(const Head& h, int dtype, int b0, int width, int back) : wb(width), size(dtype == 0 ? 4 : 2) {
     const int i = 16 * wave_id() + (threadIdx.x & 15);
     b = b0 + 8 * ((threadIdx.x & 63) >> 4);
     row = (back ? kChunk - 1 - i : i) * h.pitch;
@@ -285,7 +268,7 @@ template <int TB, bool FULL, int OUT> struct RowStore {
 #pragma unroll
       for (int j = 0; j < TB; j += 2) {
         const int o = b + 16 * j < wb ? at : kNowhere;
-        if (OUT == 0 || (OUT < 0 && size == 4)) {
+        if (size == 4) {
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j]), r, o + 64 * j, 0, kStream);
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j + 1]), r, o + 64 * j + 16, 0, kStream);
         } else {
@@ -395,8 +378,8 @@ template <int NI, int NJ> __device__ __forceinline__ void decay_state(f32x4 (&S)
 __device__ __forceinline__ void put_weights(float* uw, const float* pw, int n, int first, float scale) {
   if (threadIdx.x < kChunk) uw[threadIdx.x] = scale * pw[max(0, n - first - (int)threadIdx.x)];
 }
-// S += sum over the chunk's rows of w a b', w a as PU pieces
-template <int P, int PU, int W, int TB>
+// S += sum over the chunk's rows of w a b'
+template <int P, int W, int TB>
 __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, TB>& t, const uint16_t* sa, const uint16_t* sb, const float* uw) {
   constexpr int LDA = stride(W), LDB = stride(16 * TB), PA = kChunk * LDA, PB = kChunk * LDB, AT = Tiles<W, TB>::AT, BT = Tiles<W, TB>::BT;
   const int lane = threadIdx.x & 63;
@@ -407,11 +390,11 @@ __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, T
     phase();
     const f32x4 w0 = *(const f32x4*)(u + 32 * q), w1 = *(const f32x4*)(u + 32 * q + 16);
     const f32x8 w = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
-    Op<PU> a[AT];
+    Op<kPieces> a[AT];
 #pragma unroll
     for (int i = 0; i < AT; ++i) {
       const uint16_t* p = la + 32 * q * LDA + 16 * (t.at + i);
-      a[i] = pieces<PU>(number<P>(columns<P>(p, p + 16 * LDA, PA)) * w);
+      a[i] = pieces(number<P>(columns<P>(p, p + 16 * LDA, PA)) * w);
     }
     Op<P> b[BT];
 #pragma unroll
@@ -419,7 +402,7 @@ __device__ __forceinline__ void add_chunk(StateTiles<W, TB>& S, const Tiles<W, T
       const uint16_t* p = lb + 32 * q * LDB + tile_pair(t.bt + j);
       b[j] = columns<P>(p, p + 16 * LDB, PB);
     }
-    each_product<PU, P>([&](int x, int y) {
+    each_product<kPieces, P>([&](int x, int y) {
 #pragma unroll
       for (int j = 0; j < BT; ++j)
 #pragma unroll
@@ -437,7 +420,7 @@ __device__ __forceinline__ void put_near(float* near, const float* pw, float s) 
 }
 // acc[j] += B' (weighed scores of the rows x with the rows A), both of a chunk in LDS; columns of B in pairs of
 // tiles.
-template <int P, int PM, int STEPS, int TB>
+template <int P, int STEPS, int TB>
 __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[STEPS], const uint16_t* sa, int LDA, const uint16_t* sb, int LDB,
                                            const float* near) {
   const int wave = wave_id(), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, PA = kChunk * LDA, PB = kChunk * LDB;
@@ -468,8 +451,8 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
     Op<P> bt[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) bt[j] = columns<P>(lb + 16 * j0 * LDB + tile_pair(j), lb + 16 * j1 * LDB + tile_pair(j), PB);
-    const Op<PM> o = pieces<PM>(v);
-    each_product<P, PM>([&](int m, int y) {
+    const Op<kPieces> o = pieces(v);
+    each_product<P, kPieces>([&](int m, int y) {
 #pragma unroll
       for (int j = 0; j < TB; ++j) acc[j] = st::mfma(bt[j].p[m], o.p[y], acc[j]);
     });
@@ -480,11 +463,10 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
 // Waves to a SIMD: what LDS allows, or registers without spills.
 constexpr int cols_waves(int P, int WAVES, bool full, int shared) { return full && P == 1 && WAVES == 8 && !(shared & 1) ? 4 : (P == 1 ? 2 : 3); }
 constexpr int walk_waves(bool full, int shared) { return full && !shared ? 4 : (full ? 3 : 2); }
-template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, int SHARED>
+template <int P, int W, int TB, bool FULL, int DT, int SHARED>
 __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb, int parts) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = kChunk * LDA, PB = kChunk * LDB;
-  constexpr int OUT = P == 1 && PM == 2 ? 1 : -1;             // (two pieces are for results in bf16)
-  constexpr int IMG = STEPS * PM * 512;                       // numbers of one column tile of the state's image
+  constexpr int IMG = STEPS * kPieces * 512;                       // numbers of one column tile of the state's image
   extern __shared__ char lds[];
   uint16_t *sa = (uint16_t*)lds, *sb = sa + P * PA, *img = sb + P * PB;
   float *uw = (float*)(img + TB * IMG), *near = uw + kChunk, *pw = near + kNear;      // weights; lambda^0 .. lambda^64
@@ -517,7 +499,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
   Stage<P, W, FULL, DT> ra(ha, 0, w.wa, back);
   Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, back);
   RowOps<P, STEPS, FULL, DT> rx(hx, w.wa, back);
-  const RowStore<TB, FULL, OUT> ry(hy, w.Y.dtype, b0, w.wb, back);
+  const RowStore<TB, FULL> ry(hy, w.Y.dtype, b0, w.wb, back);
   auto fetch_x = [&](int r0, int gx) { rx.fetch(hx.chunk(gx, r0, min(kChunk, hi - r0), p.len, back)); };
   auto fetch_rows = [&](int r0, int ga) {
     const int n = min(kChunk, hi - r0);
@@ -536,13 +518,13 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 #pragma unroll
       for (int j = 0; j < Tiles<W, TB>::BT; ++j) {
         const int a = 16 * (t.at + i) + 4 * g;
-        uint16_t* to = img + (t.bt + j) * IMG + (a >> 5) * PM * 512 + ((((a & 31) >> 3) * 16 + col) * 8 + (a & 7));
+        uint16_t* to = img + (t.bt + j) * IMG + (a >> 5) * kPieces * 512 + ((((a & 31) >> 3) * 16 + col) * 8 + (a & 7));
         f32x4 x = S[i][j];
 #pragma unroll
-        for (int k = 0; k < PM; ++k) {
+        for (int k = 0; k < kPieces; ++k) {
           const bf16x4 h = __builtin_convertvector(x, bf16x4);
           *(bf16x4*)(to + k * 512) = h;
-          if (k + 1 < PM) x = rest_of(x, h);
+          if (k + 1 < kPieces) x = rest_of(x, h);
         }
       }
   };
@@ -571,10 +553,10 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
           for (int j = 0; j < TB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = 0; k < STEPS; ++k) {
-            Op<PM> o[TB];
+            Op<kPieces> o[TB];
 #pragma unroll
-            for (int j = 0; j < TB; ++j) o[j] = st::image_op<PM>(img + j * IMG + k * PM * 512, lane);
-            each_product<PM, P>([&](int m, int y) {
+            for (int j = 0; j < TB; ++j) o[j] = st::image_op<kPieces>(img + j * IMG + k * kPieces * 512, lane);
+            each_product<kPieces, P>([&](int m, int y) {
 #pragma unroll
               for (int j = 0; j < TB; ++j) acc[j] = st::mfma(o[j].p[m], x[k].p[y], acc[j]);
             });
@@ -582,13 +564,13 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 #pragma unroll
           for (int j = 0; j < TB; ++j) scale_by(acc[j], inter);
         }
-        add_scores<P, PM, STEPS, TB>(acc, x, sa, LDA, sb, LDB, near);
+        add_scores<P, STEPS, TB>(acc, x, sa, LDA, sb, LDB, near);
         if (ga == GA - 1) ry.put(hy.chunk(gx, r0, n, p.len, back), acc);
       }
       if (ga == GA - 1 && more) fetch_x(r0 + kChunk, 0);       // (here x's registers are free)
       if (more || ends) {
         if (ga == 0) decay_state(S, keep);
-        add_chunk<P, PU, W, TB>(S, t, sa, sb, uw);
+        add_chunk<P, W, TB>(S, t, sa, sb, uw);
       }
       __syncthreads();
     }
@@ -601,13 +583,13 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 // The same by columns: a wave has sixteen columns of the state, all of its rows, in accumulators whose order of rows is that of an operand, so
 // that the state never goes through LDS; the rows x do (every wave needs all of them), and so do the chunk's scores, whose tiles the waves share
 // out.  Chunks of 16 NT rows.
-template <int P, int PM, int PU, int W, int WAVES, int NT, bool FULL, int DT, int SHARED>
+template <int P, int W, int WAVES, int NT, bool FULL, int DT, int SHARED>
 __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb, int parts) {
   constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB, NQ = NT / 2;
-  constexpr int OUT = P == 1 && PM == 2 ? 1 : -1, TILES = NT * (NT + 1) / 2;
+  constexpr int TILES = NT * (NT + 1) / 2;
   extern __shared__ char lds[];
   uint16_t *sx = (uint16_t*)lds, *sa = sx + P * PA, *sb = sa + P * PA, *ps = sb + P * PB;
-  float *uw = (float*)(ps + NT * NQ * PM * 512), *near = uw + kChunk, *pw = near + kNear;
+  float *uw = (float*)(ps + NT * NQ * kPieces * 512), *near = uw + kChunk, *pw = near + kNear;
   const Call& c = set.c;
   const Walk& w = set.w[blockIdx.y];
   Place p;
@@ -622,7 +604,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   if (hi <= lo && !ends) return;
   const float ld = c.log_decay[p.h];
   for (int i = tid; i <= kChunk; i += T) pw[i] = power(ld, i);
-  for (int i = tid; i < NT * NQ * PM * 64; i += T) *(u32x4*)(ps + 8 * i) = u32x4{0u, 0u, 0u, 0u};      // (tiles above the diagonal stay so)
+  for (int i = tid; i < NT * NQ * kPieces * 64; i += T) *(u32x4*)(ps + 8 * i) = u32x4{0u, 0u, 0u, 0u};      // (tiles above the diagonal stay so)
   Keep keep = scalar(keep_of(ld, C));
   f32x4 S[TA][CT];
   // (with segments the pool may hold the states after the call already)
@@ -636,7 +618,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, hq);
   Stage<P, W, FULL, DT, C, T> rx(hx, 0, w.wa, back), ra(ha, 0, w.wa, back);
   Stage<P, NB, FULL, DT, C, T> rb(hb, b0, wb, back);
-  const int size = (OUT < 0 ? w.Y.dtype : OUT) == 0 ? 4 : 2, yrow = (back ? C - 1 - col : col) * hy.pitch + (bw + 4 * g) * size;
+  const int size = w.Y.dtype == 0 ? 4 : 2, yrow = (back ? C - 1 - col : col) * hy.pitch + (bw + 4 * g) * size;
   const int ystep = back ? -16 * hy.pitch : 16 * hy.pitch;
   auto fetch_x = [&](int r0, int gx) { rx.fetch(hx.chunk(gx, r0, min(C, hi - r0), p.len, back)); };
   auto fetch_rows = [&](int r0, int ga) {
@@ -685,12 +667,12 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
           f32x4 v;
 #pragma unroll
           for (int r = 0; r < 4; ++r) v[r] = (t > j || col >= 4 * g + r ? sc[r] : 0.f) * wn[r];
-          uint16_t* to = ps + (t * NQ + (j >> 1)) * PM * 512 + lane * 8 + 4 * (j & 1);
+          uint16_t* to = ps + (t * NQ + (j >> 1)) * kPieces * 512 + lane * 8 + 4 * (j & 1);
 #pragma unroll
-          for (int m = 0; m < PM; ++m) {
+          for (int m = 0; m < kPieces; ++m) {
             const bf16x4 h = __builtin_convertvector(v, bf16x4);
             *(bf16x4*)(to + m * 512) = h;
-            if (m + 1 < PM) v = rest_of(v, h);
+            if (m + 1 < kPieces) v = rest_of(v, h);
           }
         }
         if (ga == 0) {
@@ -700,16 +682,16 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
             for (int t = 0; t < NT; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
-            Op<PM> o[CT];
+            Op<kPieces> o[CT];
             Op<P> x[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) x[t] = st::row_op<P>(sx + (16 * t + col) * LDA + 32 * i + 8 * g, PA);
 #pragma unroll
             for (int j = 0; j < CT; ++j) {
               const f32x4 u = S[2 * i][j], v = S[2 * i + 1][j];
-              o[j] = pieces<PM>(f32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
+              o[j] = pieces(f32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
             }
-            each_product<PM, P>([&](int m, int y) {
+            each_product<kPieces, P>([&](int m, int y) {
 #pragma unroll
               for (int j = 0; j < CT; ++j)
 #pragma unroll
@@ -736,8 +718,8 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
           for (int j = 0; j < CT; ++j) b[q][j] = columns<P>(lb + 32 * q * LDB + 16 * j, lb + (32 * q + 16) * LDB + 16 * j, PB);
 #pragma unroll
           for (int t = 2 * q; t < NT; ++t) {
-            const Op<PM> o = st::image_op<PM>(ps + (t * NQ + q) * PM * 512, lane);
-            each_product<P, PM>([&](int m, int y) {
+            const Op<kPieces> o = st::image_op<kPieces>(ps + (t * NQ + q) * kPieces * 512, lane);
+            each_product<P, kPieces>([&](int m, int y) {
 #pragma unroll
               for (int j = 0; j < CT; ++j) acc[j][t] = st::mfma(b[q][j].p[m], o.p[y], acc[j][t]);
             });
@@ -754,7 +736,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
               const int b = bw + 16 * j + 4 * g, o = at + t * ystep + 16 * j * size;
               if constexpr (FULL) {
                 const __amdgpu_buffer_rsrc_t r = k.buffer();
-                if (OUT == 0 || (OUT < 0 && size == 4)) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j][t]), r, b < wb ? o : kNowhere, 0, 0);
+                if (size == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j][t]), r, b < wb ? o : kNowhere, 0, 0);
                 else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j][t], bf16x4)), r, b < wb ? o : kNowhere, 0, 0);
               } else if (16 * t + col < n) {
                 const TensorDev y{k.at + o, size == 4 ? 0 : 1, 0, 0, 0};
@@ -775,15 +757,15 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
             phase();
             const f32x4 w0 = *(const f32x4*)(uw + 4 * g + 32 * q), w1 = *(const f32x4*)(uw + 4 * g + 32 * q + 16);
             const f32x8 wt = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
-            Op<PU> u[CT];
+            Op<kPieces> u[CT];
 #pragma unroll
-            for (int j = 0; j < CT; ++j) u[j] = pieces<PU>(number<P>(b[q][j]) * wt);
+            for (int j = 0; j < CT; ++j) u[j] = pieces(number<P>(b[q][j]) * wt);
 #pragma unroll
             for (int i = 0; i < TA; i += 2) {
               Op<P> a[2];
 #pragma unroll
               for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + tile_pair(i + k), la + (32 * q + 16) * LDA + tile_pair(i + k), PA);
-              each_product<P, PU>([&](int m, int y) {
+              each_product<P, kPieces>([&](int m, int y) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -801,12 +783,12 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
 // Gradients of keys and values in one walk (two walks of rows of 64 in bf16 read 403 MB where this one reads 268) from the last row to the first: dk_j = D_j v_j, dv_j = D_j' k_j with the state D of the rows q and
 // dy behind, in LDS as rows of D', of which the one takes columns and the other rows.  set.w[0]: the values (X = V, A = dY, B = Q, Y = dK),
 // set.w[1]: the keys (X = K, A = Q, B = dY, Y = dV).
-template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
+template <int P, int W, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back(WalkSet set) {
-  constexpr int TB = W / 16, STEPS = W / 32, LD = stride(W), PL = kChunk * LD, PI = W * LD, OUT = P == 1 && PM == 2 ? 1 : -1;
+  constexpr int TB = W / 16, STEPS = W / 32, LD = stride(W), PL = kChunk * LD, PI = W * LD;
   extern __shared__ char lds[];
   uint16_t *sq = (uint16_t*)lds, *sd = sq + P * PL, *img = sd + P * PL;
-  float *uw = (float*)(img + PM * PI), *near = uw + kChunk, *pw = near + kNear;
+  float *uw = (float*)(img + kPieces * PI), *near = uw + kChunk, *pw = near + kNear;
   const Call& c = set.c;
   const Walk &wk = set.w[0], &wv = set.w[1];
   Place p;
@@ -830,7 +812,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
   const Head hq(wv.A, p.b, p.h * G), hd(wv.B, p.b, p.h * G), hk(wv.X, p.b, p.h), hv(wk.X, p.b, p.h), hdk(wk.Y, p.b, p.h), hdv(wv.Y, p.b, p.h);
   Stage<P, W, FULL, DT> rq(hq, 0, wv.wa, 1), rd(hd, 0, wv.wb, 1);
   RowOps<P, STEPS, FULL, DT> rk(hk, wv.wa, 1), rv(hv, wk.wa, 1);
-  const RowStore<TB, FULL, OUT> to_k(hdk, wk.Y.dtype, 0, wk.wb, 1), to_v(hdv, wv.Y.dtype, 0, wv.wb, 1);
+  const RowStore<TB, FULL> to_k(hdk, wk.Y.dtype, 0, wk.wb, 1), to_v(hdv, wv.Y.dtype, 0, wv.wb, 1);
   const float s_update = wv.s_update;
   auto fetch_x = [&](int r0) {
     const int n = min(kChunk, hi - r0);
@@ -855,7 +837,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
         uint16_t* to = img + (16 * (t.bt + j) + col) * LD + 16 * (t.at + i) + 4 * g;
         f32x4 x = S[i][j];
 #pragma unroll
-        for (int k = 0; k < PM; ++k) {
+        for (int k = 0; k < kPieces; ++k) {
           const bf16x4 h = __builtin_convertvector(x, bf16x4);
           *(bf16x4*)(to + k * PI) = h;
           x -= __builtin_convertvector(h, f32x4);
@@ -888,17 +870,17 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
           phase();
-          Op<PM> o[TB];
+          Op<kPieces> o[TB];
 #pragma unroll
-          for (int j = 0; j < TB; ++j) o[j] = st::row_op<PM>(rows + 16 * j * LD + 32 * k, PI);
-          each_product<PM, P>([&](int m, int y) {
+          for (int j = 0; j < TB; ++j) o[j] = st::row_op<kPieces>(rows + 16 * j * LD + 32 * k, PI);
+          each_product<kPieces, P>([&](int m, int y) {
 #pragma unroll
             for (int j = 0; j < TB; ++j) dv[j] = st::mfma(o[j].p[m], xk[k].p[y], dv[j]);
           });
           phase();
 #pragma unroll
-          for (int j = 0; j < TB; ++j) o[j] = columns<PM>(cols + 32 * k * LD + tile_pair(j), cols + (32 * k + 16) * LD + tile_pair(j), PI);
-          each_product<PM, P>([&](int m, int y) {
+          for (int j = 0; j < TB; ++j) o[j] = columns<kPieces>(cols + 32 * k * LD + tile_pair(j), cols + (32 * k + 16) * LD + tile_pair(j), PI);
+          each_product<kPieces, P>([&](int m, int y) {
 #pragma unroll
             for (int j = 0; j < TB; ++j) dk[j] = st::mfma(o[j].p[m], xv[k].p[y], dk[j]);
           });
@@ -909,8 +891,8 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
           scale_by(dv[j], inter);
         }
       }
-      add_scores<P, PM, STEPS, TB>(dk, xv, sd, LD, sq, LD, near);
-      add_scores<P, PM, STEPS, TB>(dv, xk, sq, LD, sd, LD, near);
+      add_scores<P, STEPS, TB>(dk, xv, sd, LD, sq, LD, near);
+      add_scores<P, STEPS, TB>(dv, xk, sq, LD, sd, LD, near);
       if (ga == G - 1) {
         to_k.put(hdk.chunk(0, r0, n, p.len, 1), dk);
         to_v.put(hdv.chunk(0, r0, n, p.len, 1), dv);
@@ -918,7 +900,7 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
       }
       if (more || ends) {
         if (ga == 0) decay_state(S, keep);
-        add_chunk<P, PU, W, TB>(S, t, sq, sd, uw);
+        add_chunk<P, W, TB>(S, t, sq, sd, uw);
       }
       __syncthreads();
     }
@@ -929,9 +911,8 @@ __global__ void __launch_bounds__(256, P == 1 ? (FULL ? 3 : 2) : 1) k_decay_back
 }
 
 // ------------------------------------------------------------------------------------------------ sums of segments
-// A wave has sixteen columns of the sums, all of their rows; the rows b are weighed.  PU as in the walks: three pieces where the states after the
-// call are wanted.  Two chunks are on their way at a time where heads do not share states.
-template <int P, int PU, int W, int WAVES, int C, bool FULL, int DT, bool SHARED>
+// A wave has sixteen columns of the sums, all of their rows; the rows b are weighed.  Two chunks are on their way at a time where heads do not share states.
+template <int P, int W, int WAVES, int C, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
   constexpr int T = 64 * WAVES, NB = 16 * WAVES, TA = W / 16, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB;
   extern __shared__ char lds[];
@@ -983,13 +964,13 @@ __global__ void __launch_bounds__(64 * WAVES) k_decay_sum(SumSet set, int ncb) {
         phase();
         const f32x4 w0 = *(const f32x4*)(uw + 4 * (lane >> 4) + 32 * q), w1 = *(const f32x4*)(uw + 4 * (lane >> 4) + 32 * q + 16);
         const f32x8 wt = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
-        const Op<PU> u = pieces<PU>(number<P>(columns<P>(lb + 32 * q * LDB, lb + (32 * q + 16) * LDB, PB)) * wt);
+        const Op<kPieces> u = pieces(number<P>(columns<P>(lb + 32 * q * LDB, lb + (32 * q + 16) * LDB, PB)) * wt);
 #pragma unroll
         for (int t = 0; t < TA; t += 2) {
           Op<P> a[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + 16 * (t + k), la + (32 * q + 16) * LDA + 16 * (t + k), PA);
-          each_product<P, PU>([&](int m, int y) {
+          each_product<P, kPieces>([&](int m, int y) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) S[t + k][0] = st::mfma(a[k].p[m], u.p[y], S[t + k][0]);
           });
@@ -1114,73 +1095,73 @@ int most_parts(const WalkSet& a, int count) {
   return n;
 }
 
-template <int P, int PM, int PU, int W, int TB, bool FULL, int DT, int SHARED>
+template <int P, int W, int TB, bool FULL, int DT, int SHARED>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
-  const size_t lds = (size_t)P * kChunk * (stride(W) + stride(16 * TB)) * 2 + (size_t)TB * (W / 32) * PM * 1024 + kTables;
-  if (int rc = room(k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>, lds)) return rc;
+  const size_t lds = (size_t)P * kChunk * (stride(W) + stride(16 * TB)) * 2 + (size_t)TB * (W / 32) * kPieces * 1024 + kTables;
+  if (int rc = room(k_decay_walk<P, W, TB, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   const int parts = most_parts(a, count);
   if (units * ncb * parts > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_walk<P, PM, PU, W, TB, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(256), lds, st, a, ncb, parts);
+  hipLaunchKernelGGL((k_decay_walk<P, W, TB, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(256), lds, st, a, ncb, parts);
   return status();
 }
-template <int P, int PM, int PU, int W, int WAVES, bool FULL, int DT, int SHARED>
+template <int P, int W, int WAVES, bool FULL, int DT, int SHARED>
 int cols_launch(const WalkSet& a, int count, hipStream_t st) {
   constexpr int NT = P == 1 ? 4 : 2, C = 16 * NT, NB = 16 * WAVES;
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
-  const size_t lds = (size_t)P * C * (2 * stride(W) + stride(NB)) * 2 + (size_t)NT * (NT / 2) * PM * 1024 + kTables;
-  if (int rc = room(k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>, lds)) return rc;
+  const size_t lds = (size_t)P * C * (2 * stride(W) + stride(NB)) * 2 + (size_t)NT * (NT / 2) * kPieces * 1024 + kTables;
+  if (int rc = room(k_decay_cols<P, W, WAVES, NT, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   const int parts = most_parts(a, count);
   if (units * ncb * parts > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_cols<P, PM, PU, W, WAVES, NT, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(64 * WAVES), lds, st, a, ncb, parts);
+  hipLaunchKernelGGL((k_decay_cols<P, W, WAVES, NT, FULL, DT, SHARED>), dim3((unsigned)(units * ncb * parts), count), dim3(64 * WAVES), lds, st, a, ncb, parts);
   return status();
 }
-template <int P, int PM, int PU, int W, bool FULL, int DT, bool SHARED>
+template <int P, int W, bool FULL, int DT, bool SHARED>
 int back_launch(const WalkSet& a, hipStream_t st) {
-  const size_t lds = (size_t)P * kChunk * stride(W) * 4 + (size_t)PM * W * stride(W) * 2 + kTables;
-  if (int rc = room(k_decay_back<P, PM, PU, W, FULL, DT, SHARED>, lds)) return rc;
+  const size_t lds = (size_t)P * kChunk * stride(W) * 4 + (size_t)kPieces * W * stride(W) * 2 + kTables;
+  if (int rc = room(k_decay_back<P, W, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * a.c.nseg + 7) / 8 * 8;
   if (units > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_back<P, PM, PU, W, FULL, DT, SHARED>), dim3((unsigned)units), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((k_decay_back<P, W, FULL, DT, SHARED>), dim3((unsigned)units), dim3(256), lds, st, a);
   return status();
 }
-template <int P, int PU, int W, int WAVES, bool FULL, int DT, bool SHARED>
+template <int P, int W, int WAVES, bool FULL, int DT, bool SHARED>
 int sum_launch(const SumSet& a, int count, hipStream_t st) {
   constexpr int C = P == 1 ? 64 : 32, NB = 16 * WAVES;
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + NB - 1) / NB);
   const size_t lds = (size_t)P * C * (stride(W) + stride(NB)) * 2 + kTables;
-  if (int rc = room(k_decay_sum<P, PU, W, WAVES, C, FULL, DT, SHARED>, lds)) return rc;
+  if (int rc = room(k_decay_sum<P, W, WAVES, C, FULL, DT, SHARED>, lds)) return rc;
   const long long units = ((long long)a.c.B * a.c.Hk * (a.last ? a.c.nseg : a.c.nseg - 1) + 7) / 8 * 8;
   if (units == 0) return 0;
   if (units * ncb > 0x7fffffffLL) return 2;
-  hipLaunchKernelGGL((k_decay_sum<P, PU, W, WAVES, C, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
+  hipLaunchKernelGGL((k_decay_sum<P, W, WAVES, C, FULL, DT, SHARED>), dim3((unsigned)(units * ncb), count), dim3(64 * WAVES), lds, st, a, ncb);
   return status();
 }
 
 int class_of(int n) { return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
-template <int P, int PM, int PU, bool FULL, int DT, int SHARED> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
+template <int P, bool FULL, int DT, int SHARED> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
   if (class_of(wa) == 128)
-    return wb > 64 ? cols_launch<P, PM, PU, 128, 8, FULL, DT, SHARED>(a, count, st) : cols_launch<P, PM, PU, 128, 4, FULL, DT, SHARED>(a, count, st);
+    return wb > 64 ? cols_launch<P, 128, 8, FULL, DT, SHARED>(a, count, st) : cols_launch<P, 128, 4, FULL, DT, SHARED>(a, count, st);
   if constexpr (P == 3) {
-    return class_of(wa) == 64 ? cols_launch<P, PM, PU, 64, 4, FULL, DT, SHARED>(a, count, st) : cols_launch<P, PM, PU, 32, 4, FULL, DT, SHARED>(a, count, st);
+    return class_of(wa) == 64 ? cols_launch<P, 64, 4, FULL, DT, SHARED>(a, count, st) : cols_launch<P, 32, 4, FULL, DT, SHARED>(a, count, st);
   } else {
-    if (class_of(wa) == 64) return walk_launch<P, PM, PU, 64, 4, FULL, DT, SHARED>(a, count, st);
-    return wb <= 32 ? walk_launch<P, PM, PU, 32, 2, FULL, DT, SHARED>(a, count, st) : walk_launch<P, PM, PU, 32, 4, FULL, DT, SHARED>(a, count, st);
+    if (class_of(wa) == 64) return walk_launch<P, 64, 4, FULL, DT, SHARED>(a, count, st);
+    return wb <= 32 ? walk_launch<P, 32, 2, FULL, DT, SHARED>(a, count, st) : walk_launch<P, 32, 4, FULL, DT, SHARED>(a, count, st);
   }
 }
-template <int P, int PM, int PU, bool FULL, int DT, bool SHARED> int back_width(const WalkSet& a, int w, hipStream_t st) {
-  return w <= 32 ? back_launch<P, PM, PU, 32, FULL, DT, SHARED>(a, st) : back_launch<P, PM, PU, 64, FULL, DT, SHARED>(a, st);
+template <int P, bool FULL, int DT, bool SHARED> int back_width(const WalkSet& a, int w, hipStream_t st) {
+  return w <= 32 ? back_launch<P, 32, FULL, DT, SHARED>(a, st) : back_launch<P, 64, FULL, DT, SHARED>(a, st);
 }
-template <int P, int PU, bool FULL, int DT, bool G> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
-  if (class_of(wa) == 128) return wb > 64 ? sum_launch<P, PU, 128, 8, FULL, DT, G>(a, count, st) : sum_launch<P, PU, 128, 4, FULL, DT, G>(a, count, st);
-  if (class_of(wa) == 64) return wb > 32 ? sum_launch<P, PU, 64, 4, FULL, DT, G>(a, count, st) : sum_launch<P, PU, 64, 2, FULL, DT, G>(a, count, st);
-  return wb > 32 ? sum_launch<P, PU, 32, 4, FULL, DT, G>(a, count, st) : sum_launch<P, PU, 32, 2, FULL, DT, G>(a, count, st);
+template <int P, bool FULL, int DT, bool G> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
+  if (class_of(wa) == 128) return wb > 64 ? sum_launch<P, 128, 8, FULL, DT, G>(a, count, st) : sum_launch<P, 128, 4, FULL, DT, G>(a, count, st);
+  if (class_of(wa) == 64) return wb > 32 ? sum_launch<P, 64, 4, FULL, DT, G>(a, count, st) : sum_launch<P, 64, 2, FULL, DT, G>(a, count, st);
+  return wb > 32 ? sum_launch<P, 32, 4, FULL, DT, G>(a, count, st) : sum_launch<P, 32, 2, FULL, DT, G>(a, count, st);
 }
 
 // A kernel's form for rows without a ragged end, for heads that share states.  (Where none do, loops of one turn are left out: fewer registers.)
@@ -1191,16 +1172,15 @@ template <class F> int each_form(bool full, bool shared, F go) {
 
 }  // namespace
 
-// Walks from .. from + count - 1 in one launch.  fine: results in fp32.
-int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, hipStream_t st) {
+// Walks from .. from + count - 1 in one launch.
+int launch_walks(const WalkSet& all, int from, int count, int dtype, hipStream_t st) {
   WalkSet a = all;
   int wa = 0, wb = 0;
   int shared = 0;                // 1: heads of A and B share states, 2: of X
-  bool full = true, ends = false;
+  bool full = true;
   for (int i = 0; i < count; ++i) {
     shared |= (all.w[from + i].GA > 1 ? 1 : 0) | (all.w[from + i].GX > 1 ? 2 : 0);
     a.w[i] = all.w[from + i];
-    ends = ends || (a.w[i].end != nullptr && a.c.nseg == 1);
     a.prefix[i] = all.prefix[from + i];
     wa = max(wa, a.w[i].wa);
     wb = max(wb, a.w[i].wb);
@@ -1209,9 +1189,7 @@ int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, 
   auto go = [&](auto full_rows, auto shared_heads) {
     constexpr bool F = decltype(full_rows)::value;
     constexpr int G = decltype(shared_heads)::value;
-    if (dtype == 0) return walk_width<3, 3, 3, F, 0, G>(a, count, wa, wb, st);
-    if (fine) return walk_width<1, 3, 3, F, 1, G>(a, count, wa, wb, st);
-    return ends ? walk_width<1, 2, 3, F, 1, G>(a, count, wa, wb, st) : walk_width<1, 2, 2, F, 1, G>(a, count, wa, wb, st);
+    return dtype == 0 ? walk_width<3, F, 0, G>(a, count, wa, wb, st) : walk_width<1, F, 1, G>(a, count, wa, wb, st);
   };
   using std::integral_constant;
   if (!full) return go(std::false_type{}, integral_constant<int, 3>{});
@@ -1220,7 +1198,7 @@ int launch_walks(const WalkSet& all, int from, int count, int dtype, bool fine, 
 }
 
 // The walks of dK and dV (from, from + 1) as one.
-int launch_back(const WalkSet& all, int from, int dtype, bool fine, hipStream_t st) {
+int launch_back(const WalkSet& all, int from, int dtype, hipStream_t st) {
   WalkSet a = all;
   for (int i = 0; i < 2; ++i) {
     a.w[i] = all.w[from + i];
@@ -1228,12 +1206,9 @@ int launch_back(const WalkSet& all, int from, int dtype, bool fine, hipStream_t 
   }
   const Walk& w = a.w[1];
   const int n = max(w.wa, w.wb);
-  const bool ends = w.end != nullptr && a.c.nseg == 1;
   auto go = [&](auto full_rows, auto shared_heads) {
     constexpr bool F = decltype(full_rows)::value, G = decltype(shared_heads)::value;
-    if (dtype == 0) return back_width<3, 3, 3, F, 0, G>(a, n, st);
-    if (fine) return back_width<1, 3, 3, F, 1, G>(a, n, st);
-    return ends ? back_width<1, 2, 3, F, 1, G>(a, n, st) : back_width<1, 2, 2, F, 1, G>(a, n, st);
+    return dtype == 0 ? back_width<3, F, 0, G>(a, n, st) : back_width<1, F, 1, G>(a, n, st);
   };
   return each_form(w.wa % 8 == 0 && w.wb % 8 == 0, w.GA > 1, go);
 }
@@ -1249,8 +1224,7 @@ int launch_sums(const SumSet& a, int count, int dtype, hipStream_t st) {
   }
   auto go = [&](auto full_rows, auto shared_heads) {
     constexpr bool F = decltype(full_rows)::value, G = decltype(shared_heads)::value;
-    if (dtype == 0) return sum_width<3, 3, F, 0, G>(a, count, wa, wb, st);
-    return a.fine ? sum_width<1, 3, F, 1, G>(a, count, wa, wb, st) : sum_width<1, 2, F, 1, G>(a, count, wa, wb, st);
+    return dtype == 0 ? sum_width<3, F, 0, G>(a, count, wa, wb, st) : sum_width<1, F, 1, G>(a, count, wa, wb, st);
   };
   return each_form(full, shared, go);
 }
