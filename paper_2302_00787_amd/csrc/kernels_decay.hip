@@ -462,8 +462,9 @@ __device__ __forceinline__ void add_scores(f32x4 (&acc)[TB], const Op<P> (&x)[ST
 // ------------------------------------------------------------------------------------------------ rows
 // Waves to a SIMD: what LDS allows, or registers without spills.
 constexpr int cols_waves(int P, int WAVES, bool full, int shared) { return full && P == 1 && WAVES == 8 && !(shared & 1) ? 4 : (P == 1 ? 2 : 3); }
-constexpr int walk_waves(bool full, int shared) { return full && !shared ? 4 : (full ? 3 : 2); }
-template <int P, int W, int TB, bool FULL, int DT, int SHARED>
+constexpr int walk_waves(bool full, bool shared) { return full && !shared ? 4 : (full ? 3 : 2); }
+// SHARED: heads of X share states.  (Those of A and B do in k_decay_back and k_decay_cols.)
+template <int P, int W, int TB, bool FULL, int DT, bool SHARED>
 __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(WalkSet set, int ncb, int parts) {
   constexpr int NB = 16 * TB, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = kChunk * LDA, PB = kChunk * LDB;
   constexpr int IMG = STEPS * kPieces * 512;                       // numbers of one column tile of the state's image
@@ -492,21 +493,21 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
                                                       : (p.slot >= 0 ? w.init + ((size_t)p.slot * c.Hk + p.h) * c.state : nullptr);
   load_state<false, true>(S, from, w.sa, w.sb, w.wa, w.wb, t.at, t.bt, b0);
-  const int back = w.back, GX = SHARED & 2 ? w.GX : 1, GA = SHARED & 1 ? w.GA : 1, first = w.first;
+  const int back = w.back, GX = SHARED ? w.GX : 1, first = w.first;
   const float s_update = w.s_update;
   const int hq = (p.h * w.parts + p.part) * GX;
-  const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h * GA), hb(w.B, p.b, p.h * GA), hy(w.Y, p.b, hq);
+  const Head hx(w.X, p.b, hq), ha(w.A, p.b, p.h), hb(w.B, p.b, p.h), hy(w.Y, p.b, hq);
   Stage<P, W, FULL, DT> ra(ha, 0, w.wa, back);
   Stage<P, NB, FULL, DT> rb(hb, b0, w.wb, back);
   RowOps<P, STEPS, FULL, DT> rx(hx, w.wa, back);
   const RowStore<TB, FULL> ry(hy, w.Y.dtype, b0, w.wb, back);
   auto fetch_x = [&](int r0, int gx) { rx.fetch(hx.chunk(gx, r0, min(kChunk, hi - r0), p.len, back)); };
-  auto fetch_rows = [&](int r0, int ga) {
+  auto fetch_rows = [&](int r0) {
     const int n = min(kChunk, hi - r0);
-    ra.fetch(ha.chunk(ga, r0, n, p.len, back));
-    rb.fetch(hb.chunk(ga, r0, n, p.len, back));
+    ra.fetch(ha.chunk(0, r0, n, p.len, back));
+    rb.fetch(hb.chunk(0, r0, n, p.len, back));
   };
-  if (lo < hi) { fetch_rows(lo, 0); fetch_x(lo, 0); }
+  if (lo < hi) { fetch_rows(lo); fetch_x(lo, 0); }
   __syncthreads();
   put_near(near, pw, w.s_score);
   const float inter = w.s_inter * pw[16 * wave + col + first];
@@ -539,41 +540,36 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
       put_weights(uw, pw, n, first, s_update);
       keep = scalar(keep_of(ld, n));
     }
-    for (int ga = 0; ga < GA; ++ga) {
-      ra.store(sa);
-      rb.store(sb);
-      __syncthreads();
-      if (ga + 1 < GA) fetch_rows(r0, ga + 1);
-      else if (more) fetch_rows(r0 + kChunk, 0);
-      for (int gx = 0; gx < GX; ++gx) {
-        if (ga == 0) {
-          rx.ops(x);
-          if (gx + 1 < GX) fetch_x(r0, gx + 1);
+    ra.store(sa);
+    rb.store(sb);
+    __syncthreads();
+    if (more) fetch_rows(r0 + kChunk);
+    for (int gx = 0; gx < GX; ++gx) {
+      rx.ops(x);
+      if (gx + 1 < GX) fetch_x(r0, gx + 1);
 #pragma unroll
-          for (int j = 0; j < TB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < TB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int k = 0; k < STEPS; ++k) {
-            Op<kPieces> o[TB];
+      for (int k = 0; k < STEPS; ++k) {
+        Op<kPieces> o[TB];
 #pragma unroll
-            for (int j = 0; j < TB; ++j) o[j] = st::image_op<kPieces>(img + j * IMG + k * kPieces * 512, lane);
-            each_product<kPieces, P>([&](int m, int y) {
+        for (int j = 0; j < TB; ++j) o[j] = st::image_op<kPieces>(img + j * IMG + k * kPieces * 512, lane);
+        each_product<kPieces, P>([&](int m, int y) {
 #pragma unroll
-              for (int j = 0; j < TB; ++j) acc[j] = st::mfma(o[j].p[m], x[k].p[y], acc[j]);
-            });
-          }
-#pragma unroll
-          for (int j = 0; j < TB; ++j) scale_by(acc[j], inter);
-        }
-        add_scores<P, STEPS, TB>(acc, x, sa, LDA, sb, LDB, near);
-        if (ga == GA - 1) ry.put(hy.chunk(gx, r0, n, p.len, back), acc);
+          for (int j = 0; j < TB; ++j) acc[j] = st::mfma(o[j].p[m], x[k].p[y], acc[j]);
+        });
       }
-      if (ga == GA - 1 && more) fetch_x(r0 + kChunk, 0);       // (here x's registers are free)
-      if (more || ends) {
-        if (ga == 0) decay_state(S, keep);
-        add_chunk<P, W, TB>(S, t, sa, sb, uw);
-      }
-      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < TB; ++j) scale_by(acc[j], inter);
+      add_scores<P, STEPS, TB>(acc, x, sa, LDA, sb, LDB, near);
+      ry.put(hy.chunk(gx, r0, n, p.len, back), acc);
     }
+    if (more) fetch_x(r0 + kChunk, 0);                          // (here x's registers are free)
+    if (more || ends) {
+      decay_state(S, keep);
+      add_chunk<P, W, TB>(S, t, sa, sb, uw);
+    }
+    __syncthreads();
     if (more) put_image();
   }
   if (ends)
@@ -585,7 +581,7 @@ __global__ void __launch_bounds__(256, walk_waves(FULL, SHARED)) k_decay_walk(Wa
 // out.  Chunks of 16 NT rows.
 template <int P, int W, int WAVES, int NT, bool FULL, int DT, int SHARED>
 __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_waves(P, WAVES, FULL, SHARED)) k_decay_cols(WalkSet set, int ncb, int parts) {
-  constexpr int C = 16 * NT, T = 64 * WAVES, CT = 1, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB, NQ = NT / 2;
+  constexpr int C = 16 * NT, T = 64 * WAVES, NB = 16 * WAVES, TA = W / 16, STEPS = W / 32, LDA = stride(W), LDB = stride(NB), PA = C * LDA, PB = C * LDB, NQ = NT / 2;
   constexpr int TILES = NT * (NT + 1) / 2;
   extern __shared__ char lds[];
   uint16_t *sx = (uint16_t*)lds, *sa = sx + P * PA, *sb = sa + P * PA, *ps = sb + P * PB;
@@ -594,7 +590,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   const Walk& w = set.w[blockIdx.y];
   Place p;
   if (!place(c, c.nseg, ncb, parts, &p) || p.part >= w.parts) return;
-  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = NB * p.cb, bw = b0 + 16 * CT * wave;
+  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, g = lane >> 4, col = lane & 15, b0 = NB * p.cb, bw = b0 + 16 * wave;
   if (b0 >= w.wb) return;
   if (c.left_out && p.slot == -2 && p.h == 0 && p.cb == 0 && p.part == 0 && p.seg == 0 && tid == 0 && blockIdx.y == 0) atomicAdd(c.left_out, 1);
   const int lo = p.seg * c.seg_rows, hi = min(p.len, lo + c.seg_rows);
@@ -606,7 +602,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   for (int i = tid; i <= kChunk; i += T) pw[i] = power(ld, i);
   for (int i = tid; i < NT * NQ * kPieces * 64; i += T) *(u32x4*)(ps + 8 * i) = u32x4{0u, 0u, 0u, 0u};      // (tiles above the diagonal stay so)
   Keep keep = scalar(keep_of(ld, C));
-  f32x4 S[TA][CT];
+  f32x4 S[TA][1];
   // (with segments the pool may hold the states after the call already)
   const float* from = w.init == nullptr && p.seg == 0 ? nullptr
                       : c.nseg > 1                    ? set.prefix[blockIdx.y] + ((size_t)s * c.nseg + p.seg) * c.state
@@ -633,7 +629,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
   float inter[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) inter[t] = w.s_inter * pw[16 * t + col + first];
-  f32x4 acc[CT][NT];
+  f32x4 acc[NT];
   for (int r0 = lo; r0 < hi; r0 += C) {
     int n = min(C, hi - r0);
     const bool more = r0 + C < hi;
@@ -677,31 +673,21 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
         }
         if (ga == 0) {
 #pragma unroll
-          for (int j = 0; j < CT; ++j)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
-            Op<kPieces> o[CT];
             Op<P> x[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) x[t] = st::row_op<P>(sx + (16 * t + col) * LDA + 32 * i + 8 * g, PA);
-#pragma unroll
-            for (int j = 0; j < CT; ++j) {
-              const f32x4 u = S[2 * i][j], v = S[2 * i + 1][j];
-              o[j] = pieces(f32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
-            }
+            const f32x4 u = S[2 * i][0], v = S[2 * i + 1][0];
+            const Op<kPieces> o = pieces(f32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
             each_product<kPieces, P>([&](int m, int y) {
 #pragma unroll
-              for (int j = 0; j < CT; ++j)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc[j][t] = st::mfma(o[j].p[m], x[t].p[y], acc[j][t]);
+              for (int t = 0; t < NT; ++t) acc[t] = st::mfma(o.p[m], x[t].p[y], acc[t]);
             });
           }
 #pragma unroll
-          for (int j = 0; j < CT; ++j)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) scale_by(acc[j][t], inter[t]);
+          for (int t = 0; t < NT; ++t) scale_by(acc[t], inter[t]);
         }
         __syncthreads();
         // what the next turn stages: rows a and b from here on, rows x when the results' registers are free
@@ -709,20 +695,16 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
         if (last_x && ga + 1 < GA) fetch_rows(r0, ga + 1);
         else if (last_x && more) fetch_rows(r0 + C, 0);
         // scores times rows b
-        const uint16_t *la = sa + lane_tr8(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * CT * wave;
-        Op<P> b[NQ][CT];
+        const uint16_t *la = sa + lane_tr8(lane, LDA), *lb = sb + st::lane_tr(lane, LDB) + 16 * wave;
+        Op<P> b[NQ];
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           phase();
-#pragma unroll
-          for (int j = 0; j < CT; ++j) b[q][j] = columns<P>(lb + 32 * q * LDB + 16 * j, lb + (32 * q + 16) * LDB + 16 * j, PB);
+          b[q] = columns<P>(lb + 32 * q * LDB, lb + (32 * q + 16) * LDB, PB);
 #pragma unroll
           for (int t = 2 * q; t < NT; ++t) {
             const Op<kPieces> o = st::image_op<kPieces>(ps + (t * NQ + q) * kPieces * 512, lane);
-            each_product<P, kPieces>([&](int m, int y) {
-#pragma unroll
-              for (int j = 0; j < CT; ++j) acc[j][t] = st::mfma(b[q][j].p[m], o.p[y], acc[j][t]);
-            });
+            each_product<P, kPieces>([&](int m, int y) { acc[t] = st::mfma(b[q].p[m], o.p[y], acc[t]); });
           }
         }
         if (ga == GA - 1) {
@@ -730,21 +712,19 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
           const Chunk k = hy.chunk(gx, r0, n, p.len, back);
           const int at = afresh_lane(yrow - k.shift(C));
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
+          for (int t = 0; t < NT; ++t) {
+            const int b = bw + 4 * g, o = at + t * ystep;
+            if constexpr (FULL) {
+              const __amdgpu_buffer_rsrc_t r = k.buffer();
+              if (size == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[t]), r, b < wb ? o : kNowhere, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[t], bf16x4)), r, b < wb ? o : kNowhere, 0, 0);
+            } else if (16 * t + col < n) {
+              const TensorDev y{k.at + o, size == 4 ? 0 : 1, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < CT; ++j) {
-              const int b = bw + 16 * j + 4 * g, o = at + t * ystep + 16 * j * size;
-              if constexpr (FULL) {
-                const __amdgpu_buffer_rsrc_t r = k.buffer();
-                if (size == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[j][t]), r, b < wb ? o : kNowhere, 0, 0);
-                else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, __builtin_convertvector(acc[j][t], bf16x4)), r, b < wb ? o : kNowhere, 0, 0);
-              } else if (16 * t + col < n) {
-                const TensorDev y{k.at + o, size == 4 ? 0 : 1, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (b + i < wb) store_elem(y, i, acc[j][t][i]);
-              }
+              for (int i = 0; i < 4; ++i)
+                if (b + i < wb) store_elem(y, i, acc[t][i]);
             }
+          }
           phase();
         }
         if (gx + 1 < GX) fetch_x(r0, gx + 1);
@@ -757,9 +737,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
             phase();
             const f32x4 w0 = *(const f32x4*)(uw + 4 * g + 32 * q), w1 = *(const f32x4*)(uw + 4 * g + 32 * q + 16);
             const f32x8 wt = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
-            Op<kPieces> u[CT];
-#pragma unroll
-            for (int j = 0; j < CT; ++j) u[j] = pieces(number<P>(b[q][j]) * wt);
+            const Op<kPieces> u = pieces(number<P>(b[q]) * wt);
 #pragma unroll
             for (int i = 0; i < TA; i += 2) {
               Op<P> a[2];
@@ -767,9 +745,7 @@ __global__ void __launch_bounds__(64 * WAVES, P == 3 && W == 128 ? 2 : cols_wave
               for (int k = 0; k < 2; ++k) a[k] = columns<P>(la + 32 * q * LDA + tile_pair(i + k), la + (32 * q + 16) * LDA + tile_pair(i + k), PA);
               each_product<P, kPieces>([&](int m, int y) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                  for (int j = 0; j < CT; ++j) S[i + k][j] = st::mfma(a[k].p[m], u[j].p[y], S[i + k][j]);
+                for (int k = 0; k < 2; ++k) S[i + k][0] = st::mfma(a[k].p[m], u.p[y], S[i + k][0]);
               });
             }
           }
@@ -1095,7 +1071,7 @@ int most_parts(const WalkSet& a, int count) {
   return n;
 }
 
-template <int P, int W, int TB, bool FULL, int DT, int SHARED>
+template <int P, int W, int TB, bool FULL, int DT, bool SHARED>
 int walk_launch(const WalkSet& a, int count, hipStream_t st) {
   int ncb = 1;
   for (int i = 0; i < count; ++i) ncb = max(ncb, (a.w[i].wb + 16 * TB - 1) / (16 * TB));
@@ -1145,18 +1121,26 @@ int sum_launch(const SumSet& a, int count, hipStream_t st) {
 
 int class_of(int n) { return n <= 32 ? 32 : (n <= 64 ? 64 : 128); }
 
+// (Heads of A and B share states, SHARED = 1, where dK and dV are two walks, whose sides are both as wide as the wider one of the rows: more than 64.)
 template <int P, bool FULL, int DT, int SHARED> int walk_width(const WalkSet& a, int count, int wa, int wb, hipStream_t st) {
-  if (class_of(wa) == 128)
-    return wb > 64 ? cols_launch<P, 128, 8, FULL, DT, SHARED>(a, count, st) : cols_launch<P, 128, 4, FULL, DT, SHARED>(a, count, st);
-  if constexpr (P == 3) {
-    return class_of(wa) == 64 ? cols_launch<P, 64, 4, FULL, DT, SHARED>(a, count, st) : cols_launch<P, 32, 4, FULL, DT, SHARED>(a, count, st);
+  if constexpr (SHARED == 1) {
+    return class_of(wa) == 128 && wb > 64 ? cols_launch<P, 128, 8, FULL, DT, SHARED>(a, count, st) : 2;
   } else {
-    if (class_of(wa) == 64) return walk_launch<P, 64, 4, FULL, DT, SHARED>(a, count, st);
-    return wb <= 32 ? walk_launch<P, 32, 2, FULL, DT, SHARED>(a, count, st) : walk_launch<P, 32, 4, FULL, DT, SHARED>(a, count, st);
+    if (class_of(wa) == 128)
+      return wb > 64 ? cols_launch<P, 128, 8, FULL, DT, SHARED>(a, count, st) : cols_launch<P, 128, 4, FULL, DT, SHARED>(a, count, st);
+    if constexpr (P == 3) {
+      return class_of(wa) == 64 ? cols_launch<P, 64, 4, FULL, DT, SHARED>(a, count, st) : cols_launch<P, 32, 4, FULL, DT, SHARED>(a, count, st);
+    } else {
+      if (class_of(wa) == 64) return walk_launch<P, 64, 4, FULL, DT, (SHARED > 0)>(a, count, st);
+      return wb <= 32 ? walk_launch<P, 32, 2, FULL, DT, (SHARED > 0)>(a, count, st) : walk_launch<P, 32, 4, FULL, DT, (SHARED > 0)>(a, count, st);
+    }
   }
 }
+// (fp32 rows of more than 32 only where heads share states)
 template <int P, bool FULL, int DT, bool SHARED> int back_width(const WalkSet& a, int w, hipStream_t st) {
-  return w <= 32 ? back_launch<P, 32, FULL, DT, SHARED>(a, st) : back_launch<P, 64, FULL, DT, SHARED>(a, st);
+  if (w <= 32) return back_launch<P, 32, FULL, DT, SHARED>(a, st);
+  if constexpr (P == 1 || SHARED) return back_launch<P, 64, FULL, DT, SHARED>(a, st);
+  else return 2;
 }
 template <int P, bool FULL, int DT, bool G> int sum_width(const SumSet& a, int count, int wa, int wb, hipStream_t st) {
   if (class_of(wa) == 128) return wb > 64 ? sum_launch<P, 128, 8, FULL, DT, G>(a, count, st) : sum_launch<P, 128, 4, FULL, DT, G>(a, count, st);
@@ -1194,7 +1178,8 @@ int launch_walks(const WalkSet& all, int from, int count, int dtype, hipStream_t
   using std::integral_constant;
   if (!full) return go(std::false_type{}, integral_constant<int, 3>{});
   if (shared == 0) return go(std::true_type{}, integral_constant<int, 0>{});
-  return shared == 1 ? go(std::true_type{}, integral_constant<int, 1>{}) : shared == 2 ? go(std::true_type{}, integral_constant<int, 2>{}) : go(std::true_type{}, integral_constant<int, 3>{});
+  // (heads of X share states in the walks of rows and of dQ, those of A and B in the walks of dK and dV: not in one launch)
+  return shared == 1 ? go(std::true_type{}, integral_constant<int, 1>{}) : go(std::true_type{}, integral_constant<int, 2>{});
 }
 
 // The walks of dK and dV (from, from + 1) as one.
