@@ -140,31 +140,20 @@ __device__ __forceinline__ int lane_tr8(int lane, int ld) { return (4 * (lane >>
 template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struct Stage {
   static constexpr int UNITS = W / 8, N = (ROWS * UNITS + T - 1) / T, LD = stride(W), PLANE = ROWS * LD, SIZE = DT == 0 ? 4 : 2;
   static constexpr bool EVEN = ROWS * UNITS % T == 0;        // (else the last threads have no unit)
-  // A thread's first unit: its number in the row, its offset from the chunk's first row.  (Found at each fetch by the kernel whose registers are
-  // full: kept, they are what is spilled, and what is read back waits for the loads before it.  H16 L65536 d128 bf16 410 -> 398 us, others
-  // one or two per cent slower so.)
-  static constexpr bool KEPT = !(P == 1 && T == 512 && ROWS == kChunk);
-  struct Unit { int c, off; };
   Raw8 raw[N];
-  int b0, cols, pitch, back;
-  Unit first_unit;
+  int cols, pitch, back;
+  int c, off;                    // a thread's first unit: its number in the row, its offset from the chunk's first row
   // numbers c0 .. c0 + W - 1 of the rows
-  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int backwards) : b0(c0), cols(ncols), pitch(h.pitch), back(backwards) {
-    if constexpr (KEPT) first_unit = find(threadIdx.x);
-  }
-  __device__ __forceinline__ Unit find(int tid) const {
-    const int row = tid / UNITS, c = b0 + 8 * (tid % UNITS);
-    return {c, c < cols && (EVEN || row < ROWS) ? (back ? ROWS - 1 - row : row) * pitch + c * SIZE : kNowhere};
-  }
-  __device__ __forceinline__ Unit unit() const {
-    if constexpr (KEPT) return first_unit;
-    else return find(afresh_lane(threadIdx.x));
+  __device__ __forceinline__ Stage(const Head& h, int c0, int ncols, int backwards) : cols(ncols), pitch(h.pitch), back(backwards) {
+    const int row = (int)threadIdx.x / UNITS;
+    c = c0 + 8 * ((int)threadIdx.x % UNITS);
+    off = c < cols && (EVEN || row < ROWS) ? (back ? ROWS - 1 - row : row) * pitch + c * SIZE : kNowhere;
   }
   __device__ __forceinline__ void fetch(const Chunk& k) {
     const int shift = k.shift(ROWS);
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
-      const int first = afresh_lane(unit().off - shift), step = (back ? -T / UNITS : T / UNITS) * pitch;
+      const int first = afresh_lane(off - shift), step = (back ? -T / UNITS : T / UNITS) * pitch;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int o = first + i * step;
@@ -172,19 +161,18 @@ template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struc
         if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
       }
     } else {
-      const Unit u = unit();
       const int step = (back ? -T / UNITS : T / UNITS) * pitch;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int o = u.off + (i * step - shift);
+        const int o = off + (i * step - shift);
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-        if (u.c < cols && (unsigned)o < (unsigned)(k.n * k.pitch))
-          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (o - u.c * SIZE), DT, 0, 0, 0}, 0, u.c, cols);
+        if (c < cols && (unsigned)o < (unsigned)(k.n * k.pitch))
+          raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (o - c * SIZE), DT, 0, 0, 0}, 0, c, cols);
       }
     }
   }
   __device__ __forceinline__ void store(uint16_t* s) const {
-    const int tid = KEPT ? (int)threadIdx.x : afresh_lane(threadIdx.x), c = b0 + 8 * (tid % UNITS);
+    const int tid = threadIdx.x;
     uint16_t* at = s + tid / UNITS * LD + 8 * (tid % UNITS);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
