@@ -1,21 +1,21 @@
-// Linear attention with a decay for each head, rows of prompts and of training: chunks of 64 rows (32 of fp32), within a chunk by the scores
-// of its rows, between chunks by the state.  See decay_common.h for the formulas.
+// Linear attention with a decay for each head, rows of prompts and of training: chunks of 64 rows (32 in the walk by columns and in the sums of fp32
+// rows), within a chunk by the scores of its rows, between chunks by the state.  See decay_common.h for the formulas.
 //
 // Segments of a sequence are walked side by side: sums of the segments (k_decay_sum), states before them (k_decay_join), then the walks.
-//   k_decay_walk  rows of bf16 up to 64 numbers.  A wave has sixteen rows of x as operands, read once from memory, and results in whole rows;
-//                 the state's numbers are shared out to the waves' accumulators and reach the others as an image in LDS.
-//   k_decay_cols  wider rows, and all of fp32.  A wave has sixteen columns of the state and of the results, the rows x go through LDS: the
-//                 state never does (an image of 128 x 128 in three pieces would take 96 KB).
+//   k_decay_walk  rows x and a of bf16 up to 64 numbers, rows b in blocks of 64.  A wave has sixteen rows of x as operands, read once from memory,
+//                 and results in whole rows; the state's numbers are shared out to the waves' accumulators and reach the others as an image in LDS.
+//   k_decay_cols  wider rows x and a, and all of fp32.  A wave has sixteen columns of the state and of the results, the rows x go through LDS:
+//                 the state never does (an image of 128 x 128 in three pieces would take 96 KB).
 //   k_decay_back  dK and dV of rows up to 64 in one walk: q, dy and the state are read once for both.
 // Scores, states and the weighed rows in the sums of a state are fp32 and go into the next product as three bf16 pieces (24 bits), for results of
-// either dtype: what a query reads of a state can be far smaller than the state (rows with a mean), and of two pieces' 16 bits it would keep too few.
+// either dtype: what a query reads of a state can be far smaller than the state (rows with a mean), and two pieces, 16 bits, would keep too
+// little of it (states of mean 22962: 0.0056 - 0.0073 off instead of the rounding to bf16, 0.0017; a tenth to a fifth faster).
 //
-// What bounds them: memory up to 64 numbers (4 x 8 states, 16384 rows of 64 in bf16: sums 27 us, 134 MB, a walk 55, 268 MB, dK and dV 84, 403 MB:
-// 4.8 - 5.0 TB/s, where a large copy reaches 5.2), and nearly as much the CU: rows that are in the L2 already take as long for one walk, 70 instead
-// of 82 us with the sums.  Of the cycles of a SIMD there 37 % issue vector and 25 % run matrix instructions, the LDS is busy for about half; two, three
-// or four workgroups a CU make no difference.  Rows of 128 in bf16 (16 states, 65536 rows: sums 143 us, the walk 280, 3.8 TB/s) the CU: rows in the
-// L2 take 318 of 386 us; vector instructions 42 %, matrix 33 %, three barriers a chunk between them; four waves of 32 columns each, with a third
-// fewer reads of the LDS, take as long.  Rows of fp32 six matrix products for one (three pieces of each side).
+// What bounds them, rows of 64 in bf16 (4 x 8 states, 16384 rows: sums 30 us, 134 MB, a walk 68, 268 MB, dK and dV 108, 403 MB: 3.7 - 4.5 TB/s,
+// where a large copy reaches 5.2): the CU.  Rows that are in the L2 already take nearly as long, 83 instead of 92 us with the sums.  Of the
+// cycles of a SIMD 35 % issue vector and 29 % run matrix instructions (dK and dV 33 and 32).  Rows of 128 in bf16 (16 states, 65536 rows: sums 130 us,
+// the walk 344, 3.1 TB/s) the CU, too: rows in the L2 take 397 of 460 us; vector instructions 33 %, matrix 40 %, three barriers a chunk between them.
+// Rows of fp32 six matrix products for one (three pieces of each side).
 #include "decay_common.h"
 
 #include <type_traits>
@@ -237,8 +237,8 @@ template <int P, int STEPS, bool FULL, int DT> struct RowOps {
 };
 
 // Results are not read again by these calls: they go past the caches, which keep rows for the next launch (64 sequences of 1024 rows of 8
-// heads of 64 in bf16, forward and backward: 201 -> 184 us).  Not those of the walk by columns: pieces of 32 bytes, which the caches join
-// (410 -> 492 us).
+// heads of 64 in bf16, forward and backward: 234 -> 224 us; others within 1 %).  Not those of the walk by columns: pieces of 32 bytes, which the
+// caches join (H16 L65536 d128 465 us, past them 553).
 constexpr int kStream = 2;
 // Numbers b0 + 32 k + 8 g .. of a wave's rows, which two accumulators have, to a result.
 template <int TB, bool FULL> struct RowStore {

@@ -137,8 +137,9 @@ int launch_rotary(const RotaryDev& r, const AxesDev& axes, const TensorDev& X, i
   // a token's heads in one thread only where that leaves a workgroup for every place of a CU (32 tokens of 16 heads: 4.2 us a head a
   // thread)
   int parts = 1;
-  // (with several axes, whose angles wait for two loads in turn, a quarter of that: B3 L1777, 16 heads of 128, fp32 23 us, 33 at one head a
-  // thread)
+  // (with several axes, whose angles wait for two loads in turn, a quarter of that; us, and at 2048: B3 L1777, 16 heads of 128, fp32 18 and 29; B1 L4096,
+  // 32 of 64, bf16 9 and 15; B1 L16384, 16 of 128, bf16 24 and 29; B2 L1024, 10 of 128 6.8 and 7.6; fewer rows
+  // the same)
   const int places = axes.axes ? 512 : 2048;
   while (parts < H + H2 && blocks * parts < places) parts *= 2;
   a.heads_per_part = (H + H2 + parts - 1) / parts;
