@@ -153,10 +153,11 @@ template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struc
     const int shift = k.shift(ROWS);
     if constexpr (FULL) {
       const __amdgpu_buffer_rsrc_t r = k.buffer();
-      const int first = afresh_lane(off - shift), step = (back ? -T / UNITS : T / UNITS) * pitch;
+      const uint32_t first = afresh_lane((int)((uint32_t)off - shift));      // (modulo 2^32, as kNowhere may pass its end)
+      const int step = (back ? -T / UNITS : T / UNITS) * pitch;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int o = first + i * step;
+        const int o = (int)(first + i * step);
         raw[i].a = __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
         if constexpr (DT == 0) raw[i].b = __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0);
       }
@@ -164,7 +165,7 @@ template <int P, int W, bool FULL, int DT, int ROWS = kChunk, int T = 256> struc
       const int step = (back ? -T / UNITS : T / UNITS) * pitch;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int o = off + (i * step - shift);
+        const int o = (int)((uint32_t)off + (i * step - shift));
         raw[i] = Raw8{{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
         if (c < cols && (unsigned)o < (unsigned)(k.n * k.pitch))
           raw[i] = st::fetch8<FULL, DT>(TensorDev{k.at + (o - c * SIZE), DT, 0, 0, 0}, 0, c, cols);
